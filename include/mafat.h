@@ -402,6 +402,129 @@ mafat_status mafat_noalloc_sync_status(void* stream);
 mafat_status mafat_diag_umma(const void* a_dev, const void* b_dev, float* d_dev, int32_t n, int32_t a_in_tmem,
                              void* stream);
 
+/* ---- Language operators ------------------------------------------------------------------
+ *
+ * A feature map in NHWC is a sequence of H * W states per frame.  The calls below are what a
+ * decoder that answers over frames runs next to the convolutions: attention of its tokens to a
+ * frame's states (cross attention), attention of many requests that have a frame, or another
+ * prefix, in common, and the norm between them.  The paper has no counterpart.  They are
+ * forward operators in the two types of the plans: bf16 (products of bf16 values accumulated in
+ * fp32, the softmax's statistics in fp32) and fp32.
+ *
+ * Attention: for each query q, over the keys k_s that it may read,
+ *   out = sum_s e^(scale q.k_s) v_s / sum_s e^(scale q.k_s),   lse = ln sum_s e^(scale q.k_s);
+ * a query that may read no key (or whose scores are all -inf) gets out = 0 and lse = -inf.
+ * Query head h reads key head h / (heads_q / heads_kv).  Keys and values that no query may read
+ * can hold anything, NaN and infinities included.  Strides are in elements, outermost
+ * first, {sequence, token, head}; a head's channels are contiguous; all zero means packed.  They must be
+ * multiples of 16 bytes, at least head_dim and below 2^40 bytes (of a dimension of size 1: any).  head_dim is a multiple of 8, at most 128. */
+
+/* Which kernel a plan uses; for comparisons and tests. */
+typedef enum {
+    MAFAT_ATTN_AUTO = 0,
+    MAFAT_ATTN_ROWS = 1,   /* tiles of few rows: for single tokens */
+    MAFAT_ATTN_TILES = 2   /* tiles of many rows: for prompts and many requests */
+} mafat_attn_kernel;
+
+/* Most parts that the keys of a sequence are split into. */
+#define MAFAT_ATTN_MAX_SPLITS 128
+
+/* Cross attention: n_q tokens of each of `batch` sequences to the n_kv states of its frame.
+ * Zero-initialise and set struct_size. */
+typedef struct {
+    int32_t struct_size;        /* sizeof(mafat_cross_desc) */
+    int32_t dtype;              /* MAFAT_BF16 or MAFAT_FP32 */
+    int32_t batch, n_q, n_kv;   /* n_kv: room for keys, may be 0 */
+    int32_t heads_q, heads_kv, head_dim;
+    float scale;                /* 0: 1 / sqrt(head_dim) */
+    int32_t kernel;             /* mafat_attn_kernel (0: chosen by the sizes) */
+    int32_t splits;             /* parts of the keys that are computed apart and joined (0: chosen) */
+    int32_t dry_run;            /* 1: checks and statistics only; needs no GPU */
+    int64_t q_strides[3], k_strides[3], v_strides[3], out_strides[3];
+} mafat_cross_desc;
+
+/* Attention of prefixes * requests requests, of which each `requests` neighbours share a prefix
+ * (a frame's states): a request's keys are its prefix's and then its own n_own, of which the last n_q
+ * readable ones belong to its n_q queries: token t reads the prefix and its own keys
+ * 0 .. own_len - n_q + t.  The prefix's keys are read once for all requests.  A value that is not
+ * finite among a request's last n_q readable own keys may reach all its n_q queries. */
+typedef struct {
+    int32_t struct_size;        /* sizeof(mafat_prefix_desc) */
+    int32_t dtype;
+    int32_t prefixes, requests, n_q;
+    int32_t n_prefix, n_own;    /* room for keys of a prefix and of a request, may be 0 */
+    int32_t heads_q, heads_kv, head_dim;
+    float scale;
+    int32_t kernel, splits, dry_run;
+    int64_t q_strides[3], prefix_k_strides[3], prefix_v_strides[3], own_k_strides[3], own_v_strides[3], out_strides[3];
+} mafat_prefix_desc;
+
+typedef struct mafat_attn_s mafat_attn_t;
+
+/* Plan an attention: checks sizes and strides, chooses the kernel and the parts for each set of
+ * keys ([0]: the states or the prefix, [1]: a request's own keys) and allocates the parts'
+ * workspace on the current device.  Not for use during stream capture. */
+mafat_status mafat_cross_plan(const mafat_cross_desc* desc, mafat_attn_t** out);
+mafat_status mafat_prefix_plan(const mafat_prefix_desc* desc, mafat_attn_t** out);
+
+/* Run a plan on `stream` (asynchronous, capturable; runs of one plan must not overlap in time:
+ * they share its workspace).  All pointers are device memory of the plan's device, which has to be
+ * the current one; outputs must not overlap other tensors.
+ *   q, out   : [batch][n_q][heads_q][head_dim]   (prefix: batch = prefixes * requests)
+ *   k, v     : [batch][n_kv][heads_kv][head_dim]; prefix_k, prefix_v: [prefixes][n_prefix][...];
+ *              own_k, own_v: [batch][n_own][...]; may be NULL where there is room for no key
+ *   kv_len   : [batch] readable keys, clamped to 0 .. n_kv (NULL: n_kv); prefix_len [prefixes] and
+ *              own_len [batch] alike
+ *   kv_mask  : [batch][n_kv] bytes, 0: the key is not readable (NULL: all are); prefix_mask
+ *              [prefixes][n_prefix] alike
+ *   lse      : [batch][n_q][heads_q] fp32, packed (NULL: not wanted) */
+mafat_status mafat_cross_run(const mafat_attn_t* plan, const void* q, const void* k, const void* v,
+                             const int32_t* kv_len, const uint8_t* kv_mask, void* out, float* lse, void* stream);
+mafat_status mafat_prefix_run(const mafat_attn_t* plan, const void* q, const void* prefix_k, const void* prefix_v,
+                              const int32_t* prefix_len, const uint8_t* prefix_mask, const void* own_k,
+                              const void* own_v, const int32_t* own_len, void* out, float* lse, void* stream);
+
+/* What a plan chose, by set of keys.  struct_size must be set.  Host only; works on dry runs. */
+typedef struct {
+    int32_t struct_size;
+    int32_t kernel[2], splits[2], blocks[2];
+    int32_t parts;              /* of a row, over both sets; more than one are joined */
+    int32_t launches_per_run;
+    int64_t workspace_bytes;
+} mafat_attn_stats_t;
+mafat_status mafat_attn_stats(const mafat_attn_t* plan, mafat_attn_stats_t* out);
+
+/* Synchronise `stream` and read (and clear) the plan's device status: MAFAT_OK or MAFAT_EDEVICE (a
+ * bounded wait inside a kernel ran out). */
+mafat_status mafat_attn_sync_status(const mafat_attn_t* plan, void* stream);
+void mafat_attn_destroy(mafat_attn_t* plan);
+
+/* An output type of mafat_rms_norm besides the plans' types: 8-bit floats (4 exponent bits, 3
+ * mantissa bits, largest value 448, no infinities). */
+#define MAFAT_E4M3 2
+
+/* Root-mean-square norm of rows with the residual's addition:
+ *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * weight,
+ * computed in fp32 and rounded once.  With out_dtype MAFAT_E4M3, y holds the norm divided by a
+ * scale s and rounded to 8 bits, s = max |norm| / 448 over scale_group channels (1 where all are 0):
+ * y * s stands for the norm. */
+typedef struct {
+    int32_t struct_size;        /* sizeof(mafat_norm_desc) */
+    int32_t dtype;              /* of x, residual, weight, residual_out: MAFAT_BF16 or MAFAT_FP32 */
+    int32_t out_dtype;          /* of y: dtype or MAFAT_E4M3 */
+    int32_t cols;               /* at most 16384 */
+    int64_t rows;               /* 0: nothing is done */
+    int32_t scale_group;        /* MAFAT_E4M3: 0 (one scale a row) or 128 (one for each 128 channels) */
+    float eps;
+    int64_t x_stride, residual_stride, residual_out_stride, y_stride;  /* of rows, in elements (0: cols) */
+} mafat_norm_desc;
+
+/* Runs the norm on `stream` (asynchronous, one launch, no workspace, capturable).  residual and
+ * residual_out (h) may be NULL; scales [rows][1 or ceil(cols / 128)] fp32 for MAFAT_E4M3, else NULL.
+ * residual_out, and y of x's type, may be x or residual itself (same address and row stride); other overlaps are refused. */
+mafat_status mafat_rms_norm(const mafat_norm_desc* desc, const void* x, const void* residual, const void* weight,
+                            void* residual_out, void* y, float* scales, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,12 +19,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmafat.so")
 
 MAFAT_CONV, MAFAT_MAXPOOL = 0, 1
-BF16, FP32 = 0, 1
+BF16, FP32, E4M3 = 0, 1, 2
+ATTN_AUTO, ATTN_ROWS, ATTN_TILES = 0, 1, 2
+MAX_SPLITS = 128  # of an attention plan's keys
 STATUS = {0: "OK", 1: "EINVAL", 2: "EUNSUPPORTED", 3: "ENOMEM", 4: "ECUDA", 5: "ETIMEOUT", 6: "ENOFIT",
           7: "EDEVICE"}
 OK, EINVAL, EUNSUPPORTED, ENOMEM, ECUDA, ETIMEOUT, ENOFIT, EDEVICE = range(8)
 
-i32, i64, dbl, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p
+i32, i64, f32, dbl, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double, ctypes.c_void_p
 
 
 class LayerDesc(ctypes.Structure):
@@ -61,6 +63,32 @@ class SearchCandidate(ctypes.Structure):
                 ("us_per_run", dbl), ("status", i32), ("ring_slots", i32)]
 
 
+class CrossDesc(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("dtype", i32), ("batch", i32), ("n_q", i32), ("n_kv", i32), ("heads_q", i32),
+                ("heads_kv", i32), ("head_dim", i32), ("scale", f32), ("kernel", i32), ("splits", i32),
+                ("dry_run", i32), ("q_strides", i64 * 3), ("k_strides", i64 * 3), ("v_strides", i64 * 3),
+                ("out_strides", i64 * 3)]
+
+
+class PrefixDesc(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("dtype", i32), ("prefixes", i32), ("requests", i32), ("n_q", i32),
+                ("n_prefix", i32), ("n_own", i32), ("heads_q", i32), ("heads_kv", i32), ("head_dim", i32),
+                ("scale", f32), ("kernel", i32), ("splits", i32), ("dry_run", i32), ("q_strides", i64 * 3),
+                ("prefix_k_strides", i64 * 3), ("prefix_v_strides", i64 * 3), ("own_k_strides", i64 * 3),
+                ("own_v_strides", i64 * 3), ("out_strides", i64 * 3)]
+
+
+class AttnStats(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("kernel", i32 * 2), ("splits", i32 * 2), ("blocks", i32 * 2), ("parts", i32),
+                ("launches_per_run", i32), ("workspace_bytes", i64)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("dtype", i32), ("out_dtype", i32), ("cols", i32), ("rows", i64),
+                ("scale_group", i32), ("eps", f32), ("x_stride", i64), ("residual_stride", i64),
+                ("residual_out_stride", i64), ("y_stride", i64)]
+
+
 # (name, restype, argtypes) of every entry point of include/mafat.h
 _SIGNATURES = [
     ("mafat_describe_net", i32, [vp, i32, i32, i32, i32, ctypes.POINTER(vp)]),
@@ -95,6 +123,14 @@ _SIGNATURES = [
     ("mafat_diag_umma", i32, [vp, vp, vp, i32, i32, vp]),
     ("mafat_run_fp32_noalloc", i32, [vp, vp, vp, vp]),
     ("mafat_noalloc_sync_status", i32, [vp]),
+    ("mafat_cross_plan", i32, [ctypes.POINTER(CrossDesc), ctypes.POINTER(vp)]),
+    ("mafat_cross_run", i32, [vp] * 9),
+    ("mafat_prefix_plan", i32, [ctypes.POINTER(PrefixDesc), ctypes.POINTER(vp)]),
+    ("mafat_prefix_run", i32, [vp] * 12),
+    ("mafat_attn_stats", i32, [vp, ctypes.POINTER(AttnStats)]),
+    ("mafat_attn_sync_status", i32, [vp, vp]),
+    ("mafat_attn_destroy", None, [vp]),
+    ("mafat_rms_norm", i32, [ctypes.POINTER(NormDesc)] + [vp] * 7),
 ]
 EXPORTED = [s[0] for s in _SIGNATURES]
 
@@ -365,6 +401,179 @@ class Plan:
             self.close()
         except Exception:
             pass
+
+
+def _want(name, t, shape, dtype, strides=None):
+    """Refuses a tensor that is not what the plan was made for: the library sees only its address."""
+    if not hasattr(t, "data_ptr"):
+        return  # a raw address: the caller's word
+    if tuple(t.shape) != shape or _code(t) != dtype or not t.is_cuda:
+        raise MafatError(EINVAL, "%s: %s %s on %s, expected %s of type %s on the GPU"
+                         % (name, tuple(t.shape), t.dtype, t.device, shape, dtype))
+    if strides is None:
+        ok = t.is_contiguous()
+    else:
+        ok = all(n == 1 or a == b for n, a, b in zip(shape, t.stride(), strides))
+    if not ok:
+        raise MafatError(EINVAL, "%s: strides %s are not the plan's" % (name, t.stride()))
+
+
+_CODES = {}
+
+
+def _code(t):
+    """The library's name of a tensor's type; 1 byte masks and int32 lengths by their width."""
+    if not _CODES:
+        import torch
+        _CODES.update({torch.bfloat16: BF16, torch.float32: FP32, torch.float8_e4m3fn: E4M3, torch.bool: "mask",
+                       torch.uint8: "mask", torch.int32: "int32"})
+    return _CODES.get(t.dtype)
+
+
+class _Attention:
+    """What the two kinds of attention plans share."""
+
+    def _make(self, desc, plan, **strides):
+        desc.struct_size = ctypes.sizeof(desc)
+        for name, st in strides.items():
+            if st is not None:
+                getattr(desc, name)[:] = [int(x) for x in st]
+        h = vp()
+        _check(plan(ctypes.byref(desc), ctypes.byref(h)))
+        self.handle = h
+        self.dtype = desc.dtype
+
+    @staticmethod
+    def _layout(n, given):
+        """(shape, strides) of a [sequence][token][head][channel] tensor; strides None where packed."""
+        return n, None if given is None or not any(given) else tuple(given) + (1,)
+
+    def stats(self):
+        """What the plan chose: by set of keys (the states or the prefix; a request's own) the kernel,
+        the splits and the CTAs, and the launches of a run."""
+        s = AttnStats()
+        s.struct_size = ctypes.sizeof(AttnStats)
+        _check(lib.mafat_attn_stats(self.handle, ctypes.byref(s)))
+        return {k: list(v) if isinstance(v, ctypes.Array) else v
+                for k, v in ((k, getattr(s, k)) for k, _ in AttnStats._fields_ if k != "struct_size")}
+
+    def sync_status(self, stream=None, like=None):
+        """Raises MafatError (EDEVICE) if a device-side wait ran out."""
+        _check(lib.mafat_attn_sync_status(self.handle, _stream(stream, like)))
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib.mafat_attn_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class CrossAttention(_Attention):
+    """mafat_cross_plan / mafat_cross_run: attention of n_q tokens of each of `batch` sequences to
+    the n_kv states of its frame (a feature map in NHWC is a sequence of H * W states).
+
+    Strides are {sequence, token, head} in elements (None: packed)."""
+
+    def __init__(self, batch, n_q, n_kv, heads_q, heads_kv, head_dim, dtype=BF16, scale=0.0, q_strides=None,
+                 k_strides=None, v_strides=None, out_strides=None, kernel=ATTN_AUTO, splits=0, dry_run=False):
+        d = CrossDesc(dtype=dtype, batch=batch, n_q=n_q, n_kv=n_kv, heads_q=heads_q, heads_kv=heads_kv,
+                      head_dim=head_dim, scale=scale or 0.0, kernel=kernel, splits=splits, dry_run=int(dry_run))
+        self._make(d, lib.mafat_cross_plan, q_strides=q_strides, k_strides=k_strides, v_strides=v_strides,
+                   out_strides=out_strides)
+        nq, nk = (batch, n_q, heads_q, head_dim), (batch, n_kv, heads_kv, head_dim)
+        self._q, self._out = self._layout(nq, q_strides), self._layout(nq, out_strides)
+        self._k, self._v = self._layout(nk, k_strides), self._layout(nk, v_strides)
+
+    def run(self, q, k, v, out, kv_len=None, kv_mask=None, lse=None, stream=None):
+        """q, out [batch][n_q][heads_q][head_dim]; k, v [batch][n_kv][heads_kv][head_dim]; kv_len
+        [batch] int32; kv_mask [batch][n_kv] bool (False: not readable); lse [batch][n_q][heads_q] fp32."""
+        _want("q", q, self._q[0], self.dtype, self._q[1])
+        _want("k", k, self._k[0], self.dtype, self._k[1])
+        _want("v", v, self._v[0], self.dtype, self._v[1])
+        _want("out", out, self._out[0], self.dtype, self._out[1])
+        if kv_len is not None:
+            _want("kv_len", kv_len, self._k[0][:1], "int32")
+        if kv_mask is not None:
+            _want("kv_mask", kv_mask, self._k[0][:2], "mask")
+        if lse is not None:
+            _want("lse", lse, self._q[0][:3], FP32)
+        _check(lib.mafat_cross_run(self.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(kv_mask), _ptr(out),
+                                   _ptr(lse), _stream(stream, q)))
+
+
+class PrefixAttention(_Attention):
+    """mafat_prefix_plan / mafat_prefix_run: attention of prefixes * requests requests, of which each
+    `requests` neighbours share a prefix (a frame's states) that is read once for all of them; behind it
+    a request has up to n_own keys of its own, the last n_q of them those of its n_q queries."""
+
+    def __init__(self, prefixes, requests, n_q, n_prefix, n_own, heads_q, heads_kv, head_dim, dtype=BF16, scale=0.0,
+                 q_strides=None, prefix_k_strides=None, prefix_v_strides=None, own_k_strides=None,
+                 own_v_strides=None, out_strides=None, kernel=ATTN_AUTO, splits=0, dry_run=False):
+        d = PrefixDesc(dtype=dtype, prefixes=prefixes, requests=requests, n_q=n_q, n_prefix=n_prefix, n_own=n_own,
+                       heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim, scale=scale or 0.0, kernel=kernel,
+                       splits=splits, dry_run=int(dry_run))
+        self._make(d, lib.mafat_prefix_plan, q_strides=q_strides, prefix_k_strides=prefix_k_strides,
+                   prefix_v_strides=prefix_v_strides, own_k_strides=own_k_strides, own_v_strides=own_v_strides,
+                   out_strides=out_strides)
+        n = prefixes * requests
+        nq, no = (n, n_q, heads_q, head_dim), (n, n_own, heads_kv, head_dim)
+        np_ = (prefixes, n_prefix, heads_kv, head_dim)
+        self._q, self._out = self._layout(nq, q_strides), self._layout(nq, out_strides)
+        self._pk, self._pv = self._layout(np_, prefix_k_strides), self._layout(np_, prefix_v_strides)
+        self._ok, self._ov = self._layout(no, own_k_strides), self._layout(no, own_v_strides)
+
+    def run(self, q, prefix_k, prefix_v, own_k, own_v, out, prefix_len=None, prefix_mask=None, own_len=None, lse=None,
+            stream=None):
+        """q, out [prefixes * requests][n_q][heads_q][head_dim]; prefix_k, prefix_v [prefixes][n_prefix]
+        [heads_kv][head_dim]; own_k, own_v [prefixes * requests][n_own][heads_kv][head_dim]; prefix_len
+        [prefixes], own_len [prefixes * requests] int32; prefix_mask [prefixes][n_prefix] bool; lse fp32."""
+        _want("q", q, self._q[0], self.dtype, self._q[1])
+        _want("prefix_k", prefix_k, self._pk[0], self.dtype, self._pk[1])
+        _want("prefix_v", prefix_v, self._pv[0], self.dtype, self._pv[1])
+        _want("own_k", own_k, self._ok[0], self.dtype, self._ok[1])
+        _want("own_v", own_v, self._ov[0], self.dtype, self._ov[1])
+        _want("out", out, self._out[0], self.dtype, self._out[1])
+        if prefix_len is not None:
+            _want("prefix_len", prefix_len, self._pk[0][:1], "int32")
+        if prefix_mask is not None:
+            _want("prefix_mask", prefix_mask, self._pk[0][:2], "mask")
+        if own_len is not None:
+            _want("own_len", own_len, self._q[0][:1], "int32")
+        if lse is not None:
+            _want("lse", lse, self._q[0][:3], FP32)
+        _check(lib.mafat_prefix_run(self.handle, _ptr(q), _ptr(prefix_k), _ptr(prefix_v), _ptr(prefix_len),
+                                    _ptr(prefix_mask), _ptr(own_k), _ptr(own_v), _ptr(own_len), _ptr(out), _ptr(lse),
+                                    _stream(stream, q)))
+
+
+def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_group=0, eps=1e-6, stream=None):
+    """mafat_rms_norm on [rows][cols] tensors: h = x + residual (written to residual_out if given),
+    y = h / sqrt(mean(h^2) + eps) * weight, in x's type, or in float8_e4m3fn with fp32 scales
+    [rows][1] (scale_group 0) or [rows][ceil(cols / 128)] (scale_group 128)."""
+    rows, cols = x.shape
+    dtype, out_dtype = _code(x), _code(y)
+    d = NormDesc(struct_size=ctypes.sizeof(NormDesc), dtype=-1 if dtype is None else dtype,
+                 out_dtype=-1 if out_dtype is None else out_dtype, cols=cols, rows=rows, scale_group=scale_group, eps=eps)
+    for name, t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y)):
+        if t is None:
+            continue
+        if t.dim() != 2:
+            raise MafatError(EINVAL, "%s: [rows][cols] expected" % name)
+        st = t.stride(0) if rows > 1 else cols
+        _want(name, t, (rows, cols), out_dtype if name == "y" else dtype, (st, 1))
+        if rows > 1 and st < cols:
+            raise MafatError(EINVAL, "%s: a row stride is smaller than cols" % name)
+        setattr(d, name + "_stride", st)
+    _want("weight", weight, (cols,), dtype)
+    if scales is not None:
+        _want("scales", scales, (rows, -(-cols // 128) if scale_group else 1), FP32)
+    _check(lib.mafat_rms_norm(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight), _ptr(residual_out), _ptr(y),
+                              _ptr(scales), _stream(stream, x)))
 
 
 def diag_umma(a_dev, b_dev, d_dev, n, a_in_tmem=False, stream=None):

@@ -1,0 +1,457 @@
+// C ABI of the language operators: checks of arguments, plans (workspace and the split of the
+// work) and launches.  See include/mafat.h.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <limits>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "../../include/mafat.h"
+#include "attention.h"
+#include "device_types.h"
+
+mafat_status mafat_internal_fail(mafat_status s, const char* msg);
+void mafat_internal_clear_error();
+
+// One set of keys as a plan sees it.
+struct AttnSegPlan {
+    int32_t n_seq = 0, reqs = 0, n = 0, causal = 0;
+    int64_t k[3] = {0, 0, 0}, v[3] = {0, 0, 0};  // strides: sequence, key, head
+    int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, blocks = 0;
+    int32_t kernel = 0;
+};
+
+struct mafat_attn_s {
+    bool prefix = false, dry_run = false;
+    int device = 0;
+    int32_t dtype = 0, batch = 0, n_q = 0, heads_q = 0, heads_kv = 0, dim = 0;
+    float scale = 0.f;
+    int64_t q[3] = {0, 0, 0}, o[3] = {0, 0, 0};
+    int n_seg = 0;
+    AttnSegPlan seg[2];
+    int parts = 0;
+    int64_t rows_total = 0, workspace_bytes = 0;
+    void* workspace = nullptr;
+    float* part_o = nullptr;
+    float* part_lse = nullptr;
+    uint32_t* status = nullptr;
+};
+
+namespace {
+
+mafat_status fail(mafat_status s, const std::string& msg) { return mafat_internal_fail(s, msg.c_str()); }
+mafat_status cuda_fail(cudaError_t e, const char* what) {
+    return fail(e == cudaErrorMemoryAllocation ? MAFAT_ENOMEM : MAFAT_ECUDA,
+                std::string(what) + ": " + cudaGetErrorString(e));
+}
+
+constexpr int kStatusBytes = 256;
+constexpr int64_t kMaxI32 = std::numeric_limits<int32_t>::max();
+constexpr int kMaxDim = 128;
+
+bool aligned(const void* p, uintptr_t n = 16) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+// Bytes from a tensor's first element to past its last one, for sizes and strides in elements.
+int64_t extent(const int64_t n[3], const int64_t st[3], int64_t inner, int64_t esz) {
+    int64_t last = inner;
+    for (int i = 0; i < 3; ++i) last += (n[i] - 1) * st[i];
+    return last * esz;
+}
+
+bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
+    const char *x = (const char*)a, *y = (const char*)b;
+    return x && y && an > 0 && bn > 0 && x < y + bn && y < x + an;
+}
+
+// Strides given by the caller (all 0: packed), in elements.  They have to keep every 16-byte
+// vector of channels aligned, and the product with the sizes inside 62 bits.
+mafat_status take_strides(const char* what, const int64_t given[3], const int64_t n[3], int64_t dim, int64_t esz,
+                          int64_t out[3]) {
+    if (given[0] == 0 && given[1] == 0 && given[2] == 0) {
+        out[2] = dim;
+        out[1] = n[2] * dim;
+        out[0] = n[1] * n[2] * dim;
+        return MAFAT_OK;
+    }
+    for (int i = 0; i < 3; ++i) {
+        const int64_t st = given[i];
+        if (n[i] > 1 && st < dim)
+            return fail(MAFAT_EINVAL, std::string(what) + ": a stride is smaller than a head's channels");
+        if (st < 0 || st * esz % 16 != 0)
+            return fail(MAFAT_EINVAL, std::string(what) + ": strides must be multiples of 16 bytes");
+        if (st >= ((int64_t)1 << 40) / esz)
+            return fail(MAFAT_EUNSUPPORTED, std::string(what) + ": strides must be below 2^40 bytes");
+        out[i] = n[i] > 1 ? st : dim;  // never used: any valid one
+    }
+    return MAFAT_OK;
+}
+
+// Two elements of a written tensor must not share a place: sorted by stride, each stride has to
+// pass what the dimensions inside it span.
+bool places_distinct(const int64_t n[3], const int64_t st[3], int64_t dim) {
+    int at[3] = {0, 1, 2};
+    std::sort(at, at + 3, [&](int a, int b) { return st[a] < st[b]; });
+    int64_t span = dim;
+    for (int i : at) {
+        if (n[i] == 1) continue;
+        if (st[i] < span) return false;
+        span = (n[i] - 1) * st[i] + span;
+    }
+    return true;
+}
+
+int sm_count(int device) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n <= 0) n = 152;
+    return n;
+}
+
+struct Common {
+    int32_t dtype, batch, n_q, heads_q, heads_kv, dim, kernel, splits, dry_run;
+    float scale;
+    const int64_t *q, *o;
+};
+
+mafat_status check_common(const Common& c) {
+    if (c.dtype != MAFAT_BF16 && c.dtype != MAFAT_FP32) return fail(MAFAT_EINVAL, "dtype must be MAFAT_BF16 or MAFAT_FP32");
+    if (c.batch < 1 || c.n_q < 1) return fail(MAFAT_EINVAL, "batch and n_q must be positive");
+    if (c.heads_q < 1 || c.heads_kv < 1 || c.heads_q % c.heads_kv != 0)
+        return fail(MAFAT_EINVAL, "heads_q must be a positive multiple of heads_kv");
+    if (c.dim < 1) return fail(MAFAT_EINVAL, "head_dim must be positive");
+    if (c.dim > kMaxDim || c.dim % 8 != 0)
+        return fail(MAFAT_EUNSUPPORTED, "head_dim must be a multiple of 8 and at most 128");
+    if (!(c.scale >= 0.f) || std::isinf(c.scale)) return fail(MAFAT_EINVAL, "scale must be positive, or 0 for 1/sqrt(head_dim)");
+    if (c.kernel < MAFAT_ATTN_AUTO || c.kernel > MAFAT_ATTN_TILES) return fail(MAFAT_EINVAL, "unknown kernel");
+    if (c.splits < 0 || c.splits > MAFAT_ATTN_MAX_SPLITS) return fail(MAFAT_EINVAL, "splits out of range");
+    if ((int64_t)c.batch * c.n_q > kMaxI32 / c.heads_q) return fail(MAFAT_EUNSUPPORTED, "too many rows");
+    return MAFAT_OK;
+}
+
+// The work of a segment: tiles of rows, parts of the keys.
+mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms) {
+    g.rows = g.reqs * p.n_q * (p.heads_q / p.heads_kv);
+    g.kernel = c.kernel != MAFAT_ATTN_AUTO ? c.kernel : g.rows <= mafat_attn_simt_rows(false) ? MAFAT_ATTN_ROWS : MAFAT_ATTN_TILES;
+    const int tile_rows = mafat_attn_simt_rows(g.kernel == MAFAT_ATTN_TILES);
+    const int tile_keys = mafat_attn_simt_keys();
+    g.row_tiles = (g.rows + tile_rows - 1) / tile_rows;
+    const int64_t items = (int64_t)g.n_seq * p.heads_kv * g.row_tiles;
+    const int64_t tiles = std::max<int64_t>(1, ((int64_t)g.n + tile_keys - 1) / tile_keys);
+    // parts of the keys: enough CTAs for two on each SM, each with two tiles of keys at least
+    int64_t splits = c.splits;
+    if (splits == 0) splits = items >= 2 * sms ? 1 : std::min<int64_t>(2 * sms / items, (tiles + 1) / 2);
+    g.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, tiles, MAFAT_ATTN_MAX_SPLITS}));
+    if (items * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many blocks");
+    g.blocks = (int32_t)(items * g.splits);
+    g.part0 = p.parts;
+    p.parts += g.splits;
+    return MAFAT_OK;
+}
+
+mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
+    p->dtype = c.dtype;
+    p->batch = c.batch;
+    p->n_q = c.n_q;
+    p->heads_q = c.heads_q;
+    p->heads_kv = c.heads_kv;
+    p->dim = c.dim;
+    p->scale = c.scale == 0.f ? 1.f / std::sqrt((float)c.dim) : c.scale;
+    p->dry_run = c.dry_run != 0;
+    p->rows_total = (int64_t)c.batch * c.n_q * c.heads_q;
+    const int64_t esz = c.dtype == MAFAT_BF16 ? 2 : 4;
+    const int64_t n[3] = {c.batch, c.n_q, c.heads_q};
+    mafat_status st;
+    if ((st = take_strides("q_strides", c.q, n, c.dim, esz, p->q)) != MAFAT_OK) return st;
+    if ((st = take_strides("out_strides", c.o, n, c.dim, esz, p->o)) != MAFAT_OK) return st;
+    if (!places_distinct(n, p->o, c.dim)) return fail(MAFAT_EINVAL, "out_strides: elements share a place");
+    int sms = 152;
+    cudaError_t e;
+    if (!p->dry_run) {
+        if ((e = cudaGetDevice(&p->device)) != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+        sms = sm_count(p->device);
+    }
+    for (int i = 0; i < p->n_seg; ++i)
+        if ((st = plan_segment(*p, p->seg[i], c, sms)) != MAFAT_OK) return st;
+    const int64_t lse_bytes = (p->rows_total * p->parts * 4 + 255) / 256 * 256;
+    p->workspace_bytes = kStatusBytes + (p->parts > 1 ? lse_bytes + p->rows_total * p->parts * p->dim * 4 : 0);
+    if (!p->dry_run) {
+        if ((e = mafat_prepare_attn_simt()) != cudaSuccess) return cuda_fail(e, "attention kernels");
+        if ((e = cudaMalloc(&p->workspace, (size_t)p->workspace_bytes)) != cudaSuccess) return cuda_fail(e, "cudaMalloc");
+        p->status = (uint32_t*)p->workspace;
+        p->part_lse = (float*)((char*)p->workspace + kStatusBytes);
+        p->part_o = (float*)((char*)p->workspace + kStatusBytes + lse_bytes);
+        if ((e = cudaMemset(p->status, 0, kStatusBytes)) != cudaSuccess) return cuda_fail(e, "cudaMemset");
+    }
+    *out = p;
+    mafat_internal_clear_error();
+    return MAFAT_OK;
+}
+
+struct SegData {
+    const void *k, *v;
+    const int32_t* len;
+    const uint8_t* mask;
+};
+
+mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* out, float* lse, cudaStream_t s) {
+    if (p->dry_run) return fail(MAFAT_EINVAL, "plan was created with dry_run");
+    if (!q || !out) return fail(MAFAT_EINVAL, "null q or out");
+    if (!aligned(q) || !aligned(out) || !aligned(lse, 4)) return fail(MAFAT_EINVAL, "q and out must be 16-byte aligned, lse 4-byte");
+    const int64_t esz = p->dtype == MAFAT_BF16 ? 2 : 4;
+    const int64_t nq[3] = {p->batch, p->n_q, p->heads_q};
+    const int64_t out_bytes = extent(nq, p->o, p->dim, esz), lse_bytes = lse ? p->rows_total * 4 : 0;
+    auto clear = [&](const void* x, int64_t bytes) {
+        return !overlap(out, out_bytes, x, bytes) && !overlap(lse, lse_bytes, x, bytes);
+    };
+    if (overlap(out, out_bytes, lse, lse_bytes) || !clear(q, extent(nq, p->q, p->dim, esz)))
+        return fail(MAFAT_EINVAL, "an output overlaps another tensor");
+    MafatAttnArgs a{};
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.q_sb = p->q[0]; a.q_st = p->q[1]; a.q_sh = p->q[2];
+    a.o_sb = p->o[0]; a.o_st = p->o[1]; a.o_sh = p->o[2];
+    a.n_q = p->n_q;
+    a.group = p->heads_q / p->heads_kv;
+    a.heads_q = p->heads_q;
+    a.heads_kv = p->heads_kv;
+    a.dim = p->dim;
+    a.parts = p->parts;
+    a.scale_log2 = (float)((double)p->scale * 1.4426950408889634);
+    a.part_o = p->part_o;
+    a.part_lse = p->part_lse;
+    a.rows_total = p->rows_total;
+    a.status = p->status;
+    a.timeout_ns = 2000000000LL;
+    for (int i = 0; i < p->n_seg; ++i) {
+        const AttnSegPlan& g = p->seg[i];
+        const int64_t nk[3] = {g.n_seq, g.n, p->heads_kv};
+        if (g.n > 0) {
+            if (!d[i].k || !d[i].v) return fail(MAFAT_EINVAL, "null keys or values");
+            if (!aligned(d[i].k) || !aligned(d[i].v)) return fail(MAFAT_EINVAL, "keys and values must be 16-byte aligned");
+            if (!clear(d[i].k, extent(nk, g.k, p->dim, esz)) || !clear(d[i].v, extent(nk, g.v, p->dim, esz)) ||
+                !clear(d[i].mask, (int64_t)g.n_seq * g.n))
+                return fail(MAFAT_EINVAL, "an output overlaps another tensor");
+        }
+        if (!aligned(d[i].len, 4)) return fail(MAFAT_EINVAL, "lengths must be 4-byte aligned");
+        if (!clear(d[i].len, (int64_t)g.n_seq * 4)) return fail(MAFAT_EINVAL, "an output overlaps another tensor");
+    }
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+    if (dev != p->device) return fail(MAFAT_EINVAL, "the current device is not the plan's");
+    for (int i = 0; i < p->n_seg; ++i) {
+        const AttnSegPlan& g = p->seg[i];
+        MafatAttnSeg& x = a.seg[0];
+        x.k = d[i].k;
+        x.v = d[i].v;
+        x.k_sb = g.k[0]; x.k_ss = g.k[1]; x.k_sh = g.k[2];
+        x.v_sb = g.v[0]; x.v_ss = g.v[1]; x.v_sh = g.v[2];
+        x.len = d[i].len;
+        x.mask = d[i].mask;
+        x.n = g.n;
+        x.causal = g.causal;
+        x.reqs = g.reqs;
+        x.n_seq = g.n_seq;
+        x.rows = g.rows;
+        x.row_tiles = g.row_tiles;
+        x.splits = g.splits;
+        x.part0 = g.part0;
+        x.blocks = g.blocks;
+        a.n_seg = 1;
+        e = mafat_launch_attn_simt(a, p->dtype == MAFAT_BF16, g.kernel == MAFAT_ATTN_TILES, s);
+        if (e != cudaSuccess) return cuda_fail(e, "attention launch");
+    }
+    if (p->parts > 1) {
+        e = mafat_launch_attn_join(a, p->dtype == MAFAT_BF16, s);
+        if (e != cudaSuccess) return cuda_fail(e, "join launch");
+    }
+    return MAFAT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+mafat_status mafat_cross_plan(const mafat_cross_desc* d, mafat_attn_t** out) {
+    if (!d || !out) return fail(MAFAT_EINVAL, "null argument");
+    *out = nullptr;
+    if (d->struct_size != (int32_t)sizeof(mafat_cross_desc)) return fail(MAFAT_EINVAL, "struct_size is not the descriptor's");
+    const Common c{d->dtype, d->batch, d->n_q, d->heads_q, d->heads_kv, d->head_dim, d->kernel, d->splits, d->dry_run,
+                   d->scale, d->q_strides, d->out_strides};
+    mafat_status st = check_common(c);
+    if (st != MAFAT_OK) return st;
+    if (d->n_kv < 0) return fail(MAFAT_EINVAL, "n_kv must not be negative");
+    mafat_attn_s* p = new (std::nothrow) mafat_attn_s();
+    if (!p) return fail(MAFAT_ENOMEM, "host allocation failed");
+    p->n_seg = 1;
+    AttnSegPlan& g = p->seg[0];
+    g.n_seq = d->batch;
+    g.reqs = 1;
+    g.n = d->n_kv;
+    const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4, n[3] = {d->batch, d->n_kv, d->heads_kv};
+    if ((st = take_strides("k_strides", d->k_strides, n, d->head_dim, esz, g.k)) != MAFAT_OK ||
+        (st = take_strides("v_strides", d->v_strides, n, d->head_dim, esz, g.v)) != MAFAT_OK ||
+        (st = finish_plan(p, c, out)) != MAFAT_OK)
+        mafat_attn_destroy(p);
+    return st;
+}
+
+mafat_status mafat_cross_run(const mafat_attn_t* p, const void* q, const void* k, const void* v, const int32_t* kv_len,
+                             const uint8_t* kv_mask, void* out, float* lse, void* stream) {
+    if (!p) return fail(MAFAT_EINVAL, "null plan");
+    if (p->prefix) return fail(MAFAT_EINVAL, "the plan is one of mafat_prefix_plan");
+    const SegData d[1] = {{k, v, kv_len, kv_mask}};
+    return run(p, q, d, out, lse, (cudaStream_t)stream);
+}
+
+mafat_status mafat_prefix_plan(const mafat_prefix_desc* d, mafat_attn_t** out) {
+    if (!d || !out) return fail(MAFAT_EINVAL, "null argument");
+    *out = nullptr;
+    if (d->struct_size != (int32_t)sizeof(mafat_prefix_desc)) return fail(MAFAT_EINVAL, "struct_size is not the descriptor's");
+    if (d->prefixes < 1 || d->requests < 1) return fail(MAFAT_EINVAL, "prefixes and requests must be positive");
+    if (d->prefixes > kMaxI32 / d->requests) return fail(MAFAT_EUNSUPPORTED, "too many requests");
+    const Common c{d->dtype, d->prefixes * d->requests, d->n_q, d->heads_q, d->heads_kv, d->head_dim, d->kernel,
+                   d->splits, d->dry_run, d->scale, d->q_strides, d->out_strides};
+    mafat_status st = check_common(c);
+    if (st != MAFAT_OK) return st;
+    if (d->n_prefix < 0 || d->n_own < 0) return fail(MAFAT_EINVAL, "n_prefix and n_own must not be negative");
+    mafat_attn_s* p = new (std::nothrow) mafat_attn_s();
+    if (!p) return fail(MAFAT_ENOMEM, "host allocation failed");
+    p->prefix = true;
+    p->n_seg = 2;
+    AttnSegPlan &g = p->seg[0], &w = p->seg[1];
+    g.n_seq = d->prefixes;
+    g.reqs = d->requests;
+    g.n = d->n_prefix;
+    w.n_seq = c.batch;
+    w.reqs = 1;
+    w.n = d->n_own;
+    w.causal = 1;
+    const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4;
+    const int64_t np[3] = {d->prefixes, d->n_prefix, d->heads_kv}, no[3] = {c.batch, d->n_own, d->heads_kv};
+    if ((st = take_strides("prefix_k_strides", d->prefix_k_strides, np, d->head_dim, esz, g.k)) != MAFAT_OK ||
+        (st = take_strides("prefix_v_strides", d->prefix_v_strides, np, d->head_dim, esz, g.v)) != MAFAT_OK ||
+        (st = take_strides("own_k_strides", d->own_k_strides, no, d->head_dim, esz, w.k)) != MAFAT_OK ||
+        (st = take_strides("own_v_strides", d->own_v_strides, no, d->head_dim, esz, w.v)) != MAFAT_OK ||
+        (st = finish_plan(p, c, out)) != MAFAT_OK)
+        mafat_attn_destroy(p);
+    return st;
+}
+
+mafat_status mafat_prefix_run(const mafat_attn_t* p, const void* q, const void* prefix_k, const void* prefix_v,
+                              const int32_t* prefix_len, const uint8_t* prefix_mask, const void* own_k,
+                              const void* own_v, const int32_t* own_len, void* out, float* lse, void* stream) {
+    if (!p) return fail(MAFAT_EINVAL, "null plan");
+    if (!p->prefix) return fail(MAFAT_EINVAL, "the plan is one of mafat_cross_plan");
+    const SegData d[2] = {{prefix_k, prefix_v, prefix_len, prefix_mask}, {own_k, own_v, own_len, nullptr}};
+    return run(p, q, d, out, lse, (cudaStream_t)stream);
+}
+
+mafat_status mafat_attn_stats(const mafat_attn_t* p, mafat_attn_stats_t* out) {
+    if (!p || !out) return fail(MAFAT_EINVAL, "null argument");
+    if (out->struct_size < (int32_t)sizeof(mafat_attn_stats_t)) return fail(MAFAT_EINVAL, "struct_size too small");
+    mafat_attn_stats_t s{};
+    s.struct_size = (int32_t)sizeof(mafat_attn_stats_t);
+    for (int i = 0; i < p->n_seg; ++i) {
+        s.kernel[i] = p->seg[i].kernel;
+        s.splits[i] = p->seg[i].splits;
+        s.blocks[i] = p->seg[i].blocks;
+    }
+    s.parts = p->parts;
+    s.launches_per_run = p->n_seg + (p->parts > 1 ? 1 : 0);
+    s.workspace_bytes = p->workspace_bytes;
+    *out = s;
+    return MAFAT_OK;
+}
+
+mafat_status mafat_attn_sync_status(const mafat_attn_t* p, void* stream) {
+    if (!p) return fail(MAFAT_EINVAL, "null plan");
+    if (p->dry_run) return fail(MAFAT_EINVAL, "plan was created with dry_run");
+    cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaStreamSynchronize");
+    uint32_t st = 0;
+    if ((e = cudaMemcpy(&st, p->status, sizeof(st), cudaMemcpyDeviceToHost)) != cudaSuccess) return cuda_fail(e, "cudaMemcpy");
+    if (st == MAFAT_DEV_OK) return MAFAT_OK;
+    if ((e = cudaMemset(p->status, 0, kStatusBytes)) != cudaSuccess) return cuda_fail(e, "cudaMemset");
+    return fail(MAFAT_EDEVICE, "a device pipeline wait ran out");
+}
+
+void mafat_attn_destroy(mafat_attn_t* p) {
+    if (!p) return;
+    if (p->workspace) cudaFree(p->workspace);
+    delete p;
+}
+
+mafat_status mafat_rms_norm(const mafat_norm_desc* d, const void* x, const void* residual, const void* weight,
+                            void* residual_out, void* y, float* scales, void* stream) {
+    if (!d) return fail(MAFAT_EINVAL, "null argument");
+    if (d->struct_size != (int32_t)sizeof(mafat_norm_desc)) return fail(MAFAT_EINVAL, "struct_size is not the descriptor's");
+    if (d->dtype != MAFAT_BF16 && d->dtype != MAFAT_FP32) return fail(MAFAT_EINVAL, "dtype must be MAFAT_BF16 or MAFAT_FP32");
+    if (d->out_dtype != d->dtype && d->out_dtype != MAFAT_E4M3) return fail(MAFAT_EINVAL, "out_dtype must be dtype or MAFAT_E4M3");
+    const bool quant = d->out_dtype == MAFAT_E4M3;
+    if (d->rows < 0 || d->cols < 1) return fail(MAFAT_EINVAL, "rows must not be negative and cols must be positive");
+    if (d->cols > mafat_norm_max_cols()) return fail(MAFAT_EUNSUPPORTED, "at most " + std::to_string(mafat_norm_max_cols()) + " cols");
+    if (d->rows > kMaxI32) return fail(MAFAT_EUNSUPPORTED, "too many rows");
+    if (!(d->eps >= 0.f) || std::isinf(d->eps)) return fail(MAFAT_EINVAL, "eps must be finite and not negative");
+    if (quant && d->scale_group != 0 && d->scale_group != 128)
+        return fail(MAFAT_EUNSUPPORTED, "scale_group must be 0 (the row) or 128");
+    if (!quant && d->scale_group != 0) return fail(MAFAT_EINVAL, "scale_group without an 8-bit output");
+    if (d->rows == 0) {
+        mafat_internal_clear_error();
+        return MAFAT_OK;
+    }
+    if (!x || !weight || !y) return fail(MAFAT_EINVAL, "null x, weight or y");
+    if (quant != (scales != nullptr)) return fail(MAFAT_EINVAL, "an 8-bit output takes scales, others take none");
+    const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4, osz = quant ? 1 : esz, vec = 16 / esz;
+    const int64_t st[4] = {d->x_stride, d->residual_stride, d->residual_out_stride, d->y_stride};
+    int64_t row[4];
+    for (int i = 0; i < 4; ++i) {
+        row[i] = st[i] == 0 ? d->cols : st[i];
+        if (row[i] < d->cols) return fail(MAFAT_EINVAL, "a row stride is smaller than cols");
+        if (row[i] > (int64_t)1 << 40) return fail(MAFAT_EUNSUPPORTED, "a row stride is too large");
+    }
+    const void* t[6] = {x, residual, residual_out, y, weight, scales};
+    for (int i = 0; i < 6; ++i)
+        if (!aligned(t[i], i == 5 ? 4 : 16)) return fail(MAFAT_EINVAL, "tensors must be 16-byte aligned (scales: 4-byte)");
+    MafatNormArgs a{};
+    a.groups = !quant ? 0 : d->scale_group == 0 ? 1 : (d->cols + 127) / 128;
+    int64_t bytes[6];
+    for (int i = 0; i < 4; ++i) bytes[i] = t[i] ? ((d->rows - 1) * row[i] + d->cols) * (i == 3 ? osz : esz) : 0;
+    bytes[4] = d->cols * esz;
+    bytes[5] = d->rows * a.groups * 4;
+    // an output may be an input in place: the same rows, of the same type
+    for (int o : {2, 3, 5})
+        for (int i = 0; i < 6; ++i) {
+            if (i == o || !overlap(t[o], bytes[o], t[i], bytes[i])) continue;
+            const bool in_place = i < 2 && o != 5 && t[i] == t[o] && row[i] == row[o] && (o != 3 || osz == esz);
+            if (!in_place) return fail(MAFAT_EINVAL, "an output overlaps another tensor");
+        }
+    bool vectors = d->cols % vec == 0;
+    for (int i = 0; i < 4; ++i)
+        if (t[i]) vectors = vectors && row[i] % vec == 0;
+    a.x = x;
+    a.residual = residual;
+    a.weight = weight;
+    a.residual_out = residual_out;
+    a.y = y;
+    a.scales = scales;
+    a.rows = d->rows;
+    a.x_s = row[0];
+    a.r_s = row[1];
+    a.ro_s = row[2];
+    a.y_s = row[3];
+    a.cols = d->cols;
+    a.eps = d->eps;
+    const cudaError_t e = mafat_launch_norm(a, d->dtype == MAFAT_BF16, vectors,
+                                            !quant ? MAFAT_NORM_PLAIN : d->scale_group == 0 ? MAFAT_NORM_ROW : MAFAT_NORM_BLOCK,
+                                            (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(e, "norm launch");
+    return MAFAT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,74 @@
+// Launch interface of the language operators: attention to one or two sets of keys, the join of
+// its parts, and the root-mean-square norm (host and device visible).
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+// One set of keys and values: n_seq sequences, each read by the n_q queries of `reqs` requests.
+// The rows of a (sequence, key head) are its queries, row = (request * n_q + token) * group + head.
+// A CTA takes one tile of rows and one of `splits` parts of the readable keys.
+struct MafatAttnSeg {
+    const void* k;
+    const void* v;
+    int64_t k_sb, k_ss, k_sh;   // strides in elements: sequence, key, head (the channels are contiguous)
+    int64_t v_sb, v_ss, v_sh;
+    const int32_t* len;         // [n_seq] readable keys (null: n)
+    const uint8_t* mask;        // [n_seq][n] 0: the key is not readable (null: all are)
+    int32_t n;                  // keys that a sequence has room for
+    int32_t causal;             // 1: token t of n_q sees keys 0 .. len - n_q + t
+    int32_t reqs;
+    int32_t n_seq;
+    int32_t rows;               // reqs * n_q * group
+    int32_t row_tiles;
+    int32_t splits;
+    int32_t part0;              // first of its splits among the parts of a row
+    int32_t blocks;             // n_seq * heads_kv * splits * row_tiles
+};
+
+struct MafatAttnArgs {
+    const void* q;
+    void* out;
+    float* lse;                 // [batch][n_q][heads_q] natural logarithm (null: not wanted)
+    int64_t q_sb, q_st, q_sh;
+    int64_t o_sb, o_st, o_sh;
+    int32_t n_q, group, heads_q, heads_kv, dim;
+    int32_t parts;              // parts of a row over all segments; 1: a CTA writes the result itself
+    float scale_log2;           // softmax scale times log2(e)
+    int32_t n_seg;
+    float* part_o;              // [parts][rows_total][dim] results of the parts, each normalised
+    float* part_lse;            // [parts][rows_total] their log2 of the sum of exponentials
+    int64_t rows_total;         // batch * n_q * heads_q, row index = (request * n_q + token) * heads_q + head
+    uint32_t* status;           // [2] status and abort words, as the plans' counter block starts
+    int64_t timeout_ns;
+    MafatAttnSeg seg[2];
+};
+
+// fp32 arithmetic on the CUDA cores; `wide` tiles have 64 rows, others 16.
+cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, bool bf16, bool wide, cudaStream_t s);
+cudaError_t mafat_prepare_attn_simt();
+int mafat_attn_simt_rows(bool wide);
+int mafat_attn_simt_keys();
+
+// Joins the parts of each row.
+cudaError_t mafat_launch_attn_join(const MafatAttnArgs& a, bool bf16, cudaStream_t s);
+
+struct MafatNormArgs {
+    const void* x;
+    const void* residual;       // null: none
+    const void* weight;         // [cols]
+    void* residual_out;         // x + residual (null: not wanted)
+    void* y;
+    float* scales;              // [rows][groups]
+    int64_t rows;
+    int64_t x_s, r_s, ro_s, y_s;  // row strides in elements
+    int32_t cols;
+    int32_t groups;             // scales of a row
+    float eps;
+};
+enum MafatNormQuant { MAFAT_NORM_PLAIN = 0, MAFAT_NORM_ROW = 1, MAFAT_NORM_BLOCK = 2 };
+
+int mafat_norm_max_cols();  // of a row
+// aligned: every row of every matrix starts on a 16-byte boundary (8-bit rows: one as long as a
+// vector of their channels) and has whole vectors
+cudaError_t mafat_launch_norm(const MafatNormArgs& a, bool bf16, bool aligned, MafatNormQuant quant, cudaStream_t s);
