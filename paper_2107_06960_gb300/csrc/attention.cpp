@@ -2,6 +2,7 @@
 // work) and launches.  See include/mafat.h.
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <cudaTypedefs.h>
 
 #include <algorithm>
 #include <cmath>
@@ -17,13 +18,22 @@
 
 mafat_status mafat_internal_fail(mafat_status s, const char* msg);
 void mafat_internal_clear_error();
+void* mafat_internal_encode_tiled();
+
+// A kernel and the shape of its work.
+enum AttnKernel { kSimtRows, kSimtTiles, kTc1, kTc2 };
+struct AttnShape {
+    int rows, keys;  // of a CTA's tile
+    int ctas;        // of an SM
+    int setup;       // what starting and ending a CTA takes, in tiles of keys
+};
 
 // One set of keys as a plan sees it.
 struct AttnSegPlan {
     int32_t n_seq = 0, reqs = 0, n = 0, causal = 0;
     int64_t k[3] = {0, 0, 0}, v[3] = {0, 0, 0};  // strides: sequence, key, head
     int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, blocks = 0;
-    int32_t kernel = 0;
+    AttnKernel kernel = kSimtRows;
 };
 
 struct mafat_attn_s {
@@ -132,23 +142,67 @@ mafat_status check_common(const Common& c) {
     return MAFAT_OK;
 }
 
+AttnShape shape_of(AttnKernel k) {
+    switch (k) {
+        case kTc1: return {128, 128, 2, 2};
+        case kTc2: return {256, 128, 1, 2};
+        case kSimtTiles: return {mafat_attn_simt_rows(true), mafat_attn_simt_keys(), 1, 1};
+        default: return {mafat_attn_simt_rows(false), mafat_attn_simt_keys(), 2, 1};
+    }
+}
+bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
+
+AttnKernel choose_kernel(int32_t dtype, int32_t asked, int32_t rows, int32_t n) {
+    const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= mafat_attn_simt_rows(false));
+    if (few) return kSimtRows;
+    if (dtype == MAFAT_FP32 || n == 0) return kSimtTiles;  // without keys there is nothing to map
+    return rows <= 128 ? kTc1 : kTc2;
+}
+
+// Parts of the keys: the number for which the CTAs of one wave after another end first, each with its
+// run of tiles and its set-up; of equals the fewest (parts are written, read and joined).
+int32_t choose_splits(int64_t items, int64_t tiles, int64_t slots, int setup) {
+    int32_t best = 1;
+    int64_t best_cost = std::numeric_limits<int64_t>::max();
+    for (int32_t n = 1; n <= MAFAT_ATTN_MAX_SPLITS && n <= tiles; ++n) {
+        const int64_t waves = (items * n + slots - 1) / slots;
+        const int64_t cost = waves * ((tiles + n - 1) / n + setup);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = n;
+        }
+    }
+    return best;
+}
+
 // The work of a segment: tiles of rows, parts of the keys.
 mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms) {
     g.rows = g.reqs * p.n_q * (p.heads_q / p.heads_kv);
-    g.kernel = c.kernel != MAFAT_ATTN_AUTO ? c.kernel : g.rows <= mafat_attn_simt_rows(false) ? MAFAT_ATTN_ROWS : MAFAT_ATTN_TILES;
-    const int tile_rows = mafat_attn_simt_rows(g.kernel == MAFAT_ATTN_TILES);
-    const int tile_keys = mafat_attn_simt_keys();
-    g.row_tiles = (g.rows + tile_rows - 1) / tile_rows;
+    g.kernel = choose_kernel(p.dtype, c.kernel, g.rows, g.n);
+    const AttnShape sh = shape_of(g.kernel);
+    g.row_tiles = (g.rows + sh.rows - 1) / sh.rows;
     const int64_t items = (int64_t)g.n_seq * p.heads_kv * g.row_tiles;
-    const int64_t tiles = std::max<int64_t>(1, ((int64_t)g.n + tile_keys - 1) / tile_keys);
-    // parts of the keys: enough CTAs for two on each SM, each with two tiles of keys at least
-    int64_t splits = c.splits;
-    if (splits == 0) splits = items >= 2 * sms ? 1 : std::min<int64_t>(2 * sms / items, (tiles + 1) / 2);
-    g.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, tiles, MAFAT_ATTN_MAX_SPLITS}));
+    const int64_t tiles = std::max<int64_t>(1, ((int64_t)g.n + sh.keys - 1) / sh.keys);
+    g.splits = c.splits ? (int32_t)std::min<int64_t>(c.splits, tiles) : choose_splits(items, tiles, (int64_t)sms * sh.ctas, sh.setup);
     if (items * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many blocks");
     g.blocks = (int32_t)(items * g.splits);
     g.part0 = p.parts;
     p.parts += g.splits;
+    return MAFAT_OK;
+}
+
+// 4-D map {channel, head, key, sequence} of keys or values; boxes of 64 channels x 128 keys of one head.
+// Places past a dimension's end read as zero.
+mafat_status encode_map(CUtensorMap* m, const void* base, const AttnSegPlan& g, const int64_t st[3], int heads, int dim) {
+    const auto fn = (PFN_cuTensorMapEncodeTiled_v12000)mafat_internal_encode_tiled();
+    if (!fn) return fail(MAFAT_ECUDA, "cuTensorMapEncodeTiled unavailable");
+    const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)g.n, (cuuint64_t)g.n_seq};
+    const cuuint64_t strides[3] = {(cuuint64_t)st[2] * 2, (cuuint64_t)st[1] * 2, (cuuint64_t)st[0] * 2};
+    const cuuint32_t box[4] = {64, 1, 128, 1}, estr[4] = {1, 1, 1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(MAFAT_ECUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
     return MAFAT_OK;
 }
 
@@ -179,7 +233,8 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
     const int64_t lse_bytes = (p->rows_total * p->parts * 4 + 255) / 256 * 256;
     p->workspace_bytes = kStatusBytes + (p->parts > 1 ? lse_bytes + p->rows_total * p->parts * p->dim * 4 : 0);
     if (!p->dry_run) {
-        if ((e = mafat_prepare_attn_simt()) != cudaSuccess) return cuda_fail(e, "attention kernels");
+        if ((e = mafat_prepare_attn_simt()) != cudaSuccess || (e = mafat_prepare_attn_tc()) != cudaSuccess)
+            return cuda_fail(e, "attention kernels");
         if ((e = cudaMalloc(&p->workspace, (size_t)p->workspace_bytes)) != cudaSuccess) return cuda_fail(e, "cudaMalloc");
         p->status = (uint32_t*)p->workspace;
         p->part_lse = (float*)((char*)p->workspace + kStatusBytes);
@@ -263,7 +318,16 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         x.part0 = g.part0;
         x.blocks = g.blocks;
         a.n_seg = 1;
-        e = mafat_launch_attn_simt(a, p->dtype == MAFAT_BF16, g.kernel == MAFAT_ATTN_TILES, s);
+        if (is_tc(g.kernel)) {
+            CUtensorMap k, v;
+            mafat_status st;
+            if ((st = encode_map(&k, d[i].k, g, g.k, p->heads_kv, p->dim)) != MAFAT_OK ||
+                (st = encode_map(&v, d[i].v, g, g.v, p->heads_kv, p->dim)) != MAFAT_OK)
+                return st;
+            e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, s);
+        } else {
+            e = mafat_launch_attn_simt(a, p->dtype == MAFAT_BF16, g.kernel != kSimtRows, s);
+        }
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }
     if (p->parts > 1) {
@@ -358,7 +422,7 @@ mafat_status mafat_attn_stats(const mafat_attn_t* p, mafat_attn_stats_t* out) {
     mafat_attn_stats_t s{};
     s.struct_size = (int32_t)sizeof(mafat_attn_stats_t);
     for (int i = 0; i < p->n_seg; ++i) {
-        s.kernel[i] = p->seg[i].kernel;
+        s.kernel[i] = p->seg[i].kernel == kSimtRows ? MAFAT_ATTN_ROWS : MAFAT_ATTN_TILES;
         s.splits[i] = p->seg[i].splits;
         s.blocks[i] = p->seg[i].blocks;
     }

@@ -50,6 +50,12 @@ cudaError_t mafat_prepare_attn_simt();
 int mafat_attn_simt_rows(bool wide);
 int mafat_attn_simt_keys();
 
+// bf16 on the tensor cores: tiles of 128 * slots rows (slots 1 or 2) by 128 keys.  Runs one segment (seg[0]);
+// the maps are 4-D over {channel, head, key, sequence}, boxes of 64 channels x 128 keys, 128-byte swizzle.
+cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
+                                 cudaStream_t s);
+cudaError_t mafat_prepare_attn_tc();
+
 // Joins the parts of each row.
 cudaError_t mafat_launch_attn_join(const MafatAttnArgs& a, bool bf16, cudaStream_t s);
 

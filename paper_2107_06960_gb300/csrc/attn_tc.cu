@@ -1,0 +1,624 @@
+// Attention of many rows in bf16 on the tensor cores (tcgen05, sm_103a): tiles of 128 rows by 128 keys.
+//
+// For a tile of queries Q and each tile of keys K and values V of the CTA's part:
+//   S = Q K^T;  m' = max(m, max S);  P = 2^(c S - c m');  O = 2^(c (m - m')) O + P V;  l alike,
+// with c = scale log2(e).  S and O are fp32 accumulators in tensor memory; m and l are fp32 registers
+// of the thread that has the row.  P is rounded to bf16 for its product (l sums it unrounded) and written
+// over S in tensor memory, from where the second product reads it; nothing of S leaves the SM.
+//
+// A CTA has SLOTS tiles of rows that read the same keys: while the softmax of one runs, the tensor
+// core works for the other.  Warps: 4 for each slot (thread = row), one that issues the products, one
+// that loads K and V by TMA into a ring of tiles, and one that makes the bits of readable keys for
+// tiles that have others, and zeroes the values of those: 0 x NaN would reach O.
+//
+// O is rescaled only where m' is more than 2^8 above the m in use (a power that cancels in O / l and
+// leaves P at most 256, well inside bf16), so that few tiles touch O outside the products.
+//
+// Shared-memory operands are in the 128-byte-swizzled layout: rows of 64 channels, 16-byte chunk c
+// of row r at chunk c ^ (r % 8).  K is read K-major (its channels are the reduction), V MN-major (its keys
+// are), from the same layout.
+#include <cuda_bf16.h>
+
+#include "attn_common.cuh"
+#include "device_types.h"
+
+namespace {
+
+constexpr int kKeys = 128;
+constexpr int kWordsDepth = 8;       // tiles whose bits of readable keys are held
+constexpr float kRescaleLog2 = 8.f;
+
+template <int DP, int SLOTS>
+struct Cfg {
+    static constexpr int kSub = 128 * 128;                 // one 128-row x 64-channel block
+    static constexpr int kTileBytes = DP / 64 * kSub;      // a tile of Q, K or V
+    static constexpr int kStages = SLOTS == 2 ? (DP == 128 ? 5 : 8) : (DP == 128 ? 2 : 5);
+    static constexpr int kSoftmaxWarps = 4 * SLOTS;
+    static constexpr int kMmaWarp = kSoftmaxWarps, kLoadWarp = kSoftmaxWarps + 1, kMaskWarp = kSoftmaxWarps + 2;
+    static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;  // whole warpgroups: the last warp is idle
+    // registers of a thread: at launch (the most that the occupancy leaves), then by role
+    static constexpr int kRegs = SLOTS == 2 ? 168 : 128, kRegsSoftmax = SLOTS == 2 ? 208 : 192,
+                         kRegsOther = SLOTS == 2 ? 80 : 64;
+    static_assert(kRegsSoftmax * SLOTS + kRegsOther <= kRegs * (SLOTS + 1), "setmaxnreg draws on the launch's registers");
+    static constexpr int kTmemCols = 256 * SLOTS;
+    // shared memory, from a 1024-byte boundary
+    static constexpr int kOffKv = SLOTS * kTileBytes;
+    static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
+    static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + SLOTS,
+                         kBarQ = kBarP + SLOTS, kBarMask = kBarQ + 1, kBars = kBarMask + kWordsDepth;
+    static constexpr int kOffWords = kOffBar + (kBars * 8 + 15) / 16 * 16;
+    static constexpr int kOffTmem = kOffWords + kWordsDepth * 16;
+    static constexpr int kOffBroken = kOffTmem + 4;
+    static constexpr int kSmem = kOffBroken + 4 + 1024;
+    static_assert(kSmem <= (SLOTS == 2 ? 232448 : 116224), "shared memory");
+    // the words of tile j are rewritten for tile j + kWordsDepth once V of that tile has landed, which needs
+    // item 2 (j + kWordsDepth) + 1 - kStages of the ring to be done
+    static_assert(kStages <= 2 * kWordsDepth - 2, "words");
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+struct Ctl {
+    uint32_t* status;
+    int64_t limit_ns;
+    volatile int* broken;
+};
+
+__device__ __noinline__ void give_up(uint32_t* status, volatile int* broken) {
+    atomicCAS(status, 0u, (uint32_t)MAFAT_DEV_PIPE);
+    *broken = 1;
+}
+
+// Bounded wait for a barrier's phase.  All waits are for work inside the CTA and end by themselves;
+// one that does not records it, after which every wait of the CTA gives up after 1 ms.  The poll is inside
+// one asm statement: a polling loop in the instruction stream of the issuing warp slows its products.
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, const Ctl& c) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred P1, P2;\n\t.reg .u64 dl, t;\n\t.reg .b32 br;\n\t"
+        "mov.u32 %0, 1;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 P1, [%1], %2;\n\t"
+        "@P1 bra AW_DONE_%=;\n\t"
+        "ld.volatile.shared.b32 br, [%4];\n\t"
+        "setp.ne.b32 P2, br, 0;\n\t"
+        "selp.b64 t, 1000000, %3, P2;\n\t"
+        "mov.u64 dl, %%globaltimer;\n\t"
+        "add.u64 dl, dl, t;\n\t"
+        "AW_POLL_%=:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 P1, [%1], %2;\n\t"
+        "@P1 bra AW_DONE_%=;\n\t"
+        "mov.u64 t, %%globaltimer;\n\t"
+        "setp.lt.u64 P2, t, dl;\n\t"
+        "@P2 bra AW_POLL_%=;\n\t"
+        "mov.u32 %0, 0;\n\t"
+        "AW_DONE_%=:\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "l"(c.limit_ns), "r"(smem_u32(const_cast<int*>(c.broken)))
+        : "memory");
+    if (ok == 0u) give_up(c.status, c.broken);
+}
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// One lane of the converged warp, the same on every call.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t el;
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(el));
+    return el;
+}
+__device__ __forceinline__ void commit_el(uint32_t el, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %0, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}" ::"r"(el), "r"(bar)
+        : "memory");
+}
+// D = A B (+ D) with A and B in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t el, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi,
+                                       uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 e, %0, 0;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 da, {%2, %4};\n\tmov.b64 db, {%3, %4};\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%1], da, db, %5, p;\n\t}" ::"r"(el),
+        "r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc)
+        : "memory");
+}
+// the same with A in tensor memory: lane = row, two bf16 a column
+__device__ __forceinline__ void mma_ts(uint32_t el, uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc,
+                                       uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 e, %0, 0;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 db, {%3, %4};\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], db, %5, p;\n\t}" ::"r"(el),
+        "r"(d), "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc)
+        : "memory");
+}
+// Matrix descriptor, 128-byte swizzle (layout 2 in bits 61-63, version 1 in bits 46-47): start >> 4 in
+// bits 0-13, then leading and stride byte offsets >> 4 in bits 16-29 and 32-45.  K-major: the stride
+// offset is that between groups of 8 rows, the leading one is not used.  MN-major: the stride offset is that between
+// groups of 8 along the reduction, the leading one that between blocks of 64 along N.
+__device__ __forceinline__ uint32_t desc_hi() { return (1024u >> 4) | (1u << 14) | (2u << 29); }
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t leading) {
+    return ((addr & 0x3FFFFu) >> 4) | ((leading >> 4) << 16);
+}
+// fp32 accumulator, bf16 operands; bit 16: B is MN-major
+__device__ __forceinline__ uint32_t instr_desc(int n, bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void tma_tile(uint32_t el, uint32_t dst, const CUtensorMap* map, int c, int head, int key,
+                                         int seq, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %7, 0;\n\t"
+        "@e cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c), "r"(head), "r"(key), "r"(seq), "r"(bar), "r"(el)
+        : "memory");
+}
+__device__ __forceinline__ void expect_el(uint32_t el, uint32_t bar, uint32_t bytes) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %2, 0;\n\t"
+        "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(el)
+        : "memory");
+}
+
+// 32 columns of the thread's lane; valid after ld_wait
+__device__ __forceinline__ void tmem_ld32(uint32_t t, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(t)
+        : "memory");
+}
+// The wait passes the registers through, so that no use of them moves ahead of it (29 a statement).
+__device__ __forceinline__ void ld_wait32(uint32_t* v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+    asm volatile(""
+                 : "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]),
+                   "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]),
+                   "+r"(v[30]), "+r"(v[31])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t t, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(t),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
+        "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
+        "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t t, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16};" ::"r"(t),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// a * s + b for two values
+__device__ __forceinline__ void fma2(uint32_t a0, uint32_t a1, float s, float b, float& r0, float& r1) {
+    asm("{\n\t.reg .b64 a, s, b, r;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 s, {%4, %4};\n\tmov.b64 b, {%5, %5};\n\t"
+        "fma.rn.f32x2 r, a, s, b;\n\tmov.b64 {%0, %1}, r;\n\t}"
+        : "=f"(r0), "=f"(r1)
+        : "r"(a0), "r"(a1), "f"(s), "f"(b));
+}
+__device__ __forceinline__ void add2(float& r0, float& r1, float a0, float a1) {
+    asm("{\n\t.reg .b64 a, r;\n\t"
+        "mov.b64 r, {%0, %1};\n\tmov.b64 a, {%2, %3};\n\t"
+        "add.rn.f32x2 r, r, a;\n\tmov.b64 {%0, %1}, r;\n\t}"
+        : "+f"(r0), "+f"(r1)
+        : "f"(a0), "f"(a1));
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Which tiles of keys have some that are not readable: all with a mask, else the one that passes the
+// length.  The bits of the n-th such tile are in slot n % kWordsDepth.
+struct Tiles {
+    int key0, n, len;
+    bool masked;
+    __device__ __forceinline__ bool partial(int j) const { return masked || key0 + (j + 1) * kKeys > len; }
+    __device__ __forceinline__ int ordinal(int j) const { return masked ? j : 0; }
+};
+
+template <int DP, int SLOTS>
+__global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
+    attn_tc_kernel(const __grid_constant__ MafatAttnArgs a, const __grid_constant__ CUtensorMap kmap,
+                   const __grid_constant__ CUtensorMap vmap) {
+    using C = Cfg<DP, SLOTS>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t base = smem_u32(sm);
+    const uint32_t bars = base + C::kOffBar;
+    auto bar = [&](int i) { return bars + (uint32_t)i * 8u; };
+    volatile uint32_t* words = (volatile uint32_t*)(sm + C::kOffWords);
+    uint32_t* tmem_slot = (uint32_t*)(sm + C::kOffTmem);
+    volatile int* broken = (volatile int*)(sm + C::kOffBroken);
+    const Ctl ctl{a.status, a.timeout_ns, broken};
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+
+    const mafat_attn::Block b(a, 128 * SLOTS, kKeys);
+    const MafatAttnSeg& g = a.seg[0];
+    Tiles t;
+    t.key0 = b.key0;
+    t.n = b.key1 > b.key0 ? (b.key1 - b.key0 + kKeys - 1) / kKeys : 0;
+    t.len = b.len;
+    t.masked = g.mask != nullptr;
+
+    if (warp == C::kLoadWarp && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&kmap)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&vmap)) : "memory");
+        for (int i = 0; i < C::kStages; ++i) {
+            bar_init(bar(C::kBarFull + i), 1);
+            bar_init(bar(C::kBarEmpty + i), 2);  // the products that read the tile, and the mask warp
+        }
+        for (int i = 0; i < SLOTS; ++i) {
+            bar_init(bar(C::kBarS + i), 1);
+            bar_init(bar(C::kBarP + i), 4);
+        }
+        bar_init(bar(C::kBarQ), C::kSoftmaxWarps);
+        for (int i = 0; i < kWordsDepth; ++i) bar_init(bar(C::kBarMask + i), 1);
+        *broken = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == C::kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                     "r"(C::kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp < C::kSoftmaxWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
+        const int slot = warp / 4;
+        const int row0 = b.row0 + slot * 128 + (warp % 4) * 32;  // the warp's first row
+        const int row = row0 + lane;
+        const bool any = row0 < g.rows && t.n > 0;
+        // queries into shared memory: 16-byte chunks, neighbouring lanes in one row
+        if (any) {
+            int64_t off = row < g.rows ? mafat_attn::q_offset(a, g, b, row) : -1;
+            uint8_t* dst = sm + slot * C::kTileBytes;
+            constexpr int kChunks = DP / 8, kRows = 32 / kChunks;
+#pragma unroll 4
+            for (int i = 0; i < 32 / kRows; ++i) {
+                const int r = i * kRows + lane / kChunks, c = lane % kChunks;
+                const int64_t o = __shfl_sync(0xffffffffu, off, r);
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (o >= 0 && c * 8 < a.dim) v = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + c * 8);
+                const int rr = (warp % 4) * 32 + r;
+                *reinterpret_cast<uint4*>(dst + (c / 8) * C::kSub + rr * 128 + ((c % 8) ^ (rr % 8)) * 16) = v;
+            }
+            fence_async();
+        }
+        __syncwarp();
+        if (lane == 0) arrive(bar(C::kBarQ));
+
+        const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
+        const uint32_t ts = tmem + lanes + (uint32_t)(slot * 128);
+        const uint32_t to = tmem + lanes + (uint32_t)(SLOTS * 128 + slot * 128);
+        const int limit = row < g.rows ? mafat_attn::row_limit(a, g, b, row) : 0x7fffffff;
+        const float c = a.scale_log2;
+        float m = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
+        for (int j = 0; j < t.n; ++j) {
+            wait(bar(C::kBarS + slot), (uint32_t)j & 1u, ctl);
+            __syncwarp();  // tensor memory is read by converged warps
+            if (any) {
+                fence_after();
+                uint32_t s[128];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_ld32(ts + 32u * i, s + 32 * i);
+                bool part = false;
+                uint32_t w[4];
+                const int key = t.key0 + j * kKeys;
+                if (t.partial(j) || limit < key + kKeys) {
+                    w[0] = w[1] = w[2] = w[3] = 0xffffffffu;
+                    if (t.partial(j)) {
+                        const int n = t.ordinal(j);
+                        wait(bar(C::kBarMask + n % kWordsDepth), (uint32_t)(n / kWordsDepth) & 1u, ctl);
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = words[(n % kWordsDepth) * 4 + i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int left = limit - key - 32 * i;  // readable by the limit
+                        if (left < 32) w[i] &= left <= 0 ? 0u : (1u << left) - 1u;
+                    }
+                    part = true;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ld_wait32(s + 32 * i);
+                if (part) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (!(w[i / 32] >> (i % 32) & 1u)) s[i] = 0xff800000u;  // -inf
+                }
+                float top[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    top[i] = __uint_as_float(s[i]);
+#pragma unroll
+                    for (int k = i + 4; k < 128; k += 8)
+                        top[i] = k + 4 < 128 ? max3(top[i], __uint_as_float(s[k]), __uint_as_float(s[k + 4]))
+                                             : mafat_attn::max_nan(top[i], __uint_as_float(s[k]));
+                }
+                const float mt = max3(mafat_attn::max_nan(top[0], top[1]), top[2], top[3]);
+                const float mn = mafat_attn::max_nan(m, mt);
+                // also where m is -inf and mt is not; the first tile has no O yet
+                const bool up = (mn - m) * c > kRescaleLog2;
+                if (j == 0) {
+                    m = mt;
+                } else if (__any_sync(0xffffffffu, up)) {
+                    const float keep = up ? mafat_attn::exp2_fast((m - mn) * c) : 1.f;
+                    if (up) m = mn;
+                    l0 *= keep;
+                    l1 *= keep;
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i) {
+                        uint32_t o[32];
+                        tmem_ld32(to + 32u * i, o);
+                        ld_wait32(o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
+                        tmem_st32(to + 32u * i, o);
+                    }
+                }
+                const float off = m == -CUDART_INF_F ? 0.f : -m * c;  // nothing readable yet: 2^-inf = 0
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x, y;
+                        fma2(s[32 * h + 2 * i], s[32 * h + 2 * i + 1], c, off, x, y);
+                        x = mafat_attn::exp2_fast(x);
+                        y = mafat_attn::exp2_fast(y);
+                        add2(l0, l1, x, y);
+                        p[i] = pack(x, y);
+                    }
+                    tmem_st16(ts + 16u * h, p);
+                }
+                st_wait();
+                fence_before();
+            }
+            __syncwarp();
+            if (lane == 0) arrive(bar(C::kBarP + slot));
+        }
+        const float l = l0 + l1;
+        if (t.n > 0) {
+            wait(bar(C::kBarS + slot), (uint32_t)t.n & 1u, ctl);
+            __syncwarp();
+            fence_after();
+        }
+        if (row0 < g.rows) {
+            const float inv = mafat_attn::inverse_sum(l);
+            const mafat_attn::Out w(a, g, b, min(row, g.rows - 1));
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) {
+                uint32_t o[32];
+                if (t.n > 0) {
+                    tmem_ld32(to + 32u * i, o);
+                    ld_wait32(o);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = 0u;
+                }
+                if (row >= g.rows) continue;
+                // a row without readable keys: 0, whatever the products left
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
+                if (a.parts == 1) {
+                    __nv_bfloat16* dst = (__nv_bfloat16*)a.out + w.o + 32 * i;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8)
+                        if (32 * i + k < a.dim)
+                            *reinterpret_cast<uint4*>(dst + k) =
+                                make_uint4(pack(__uint_as_float(o[k]), __uint_as_float(o[k + 1])),
+                                           pack(__uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])),
+                                           pack(__uint_as_float(o[k + 4]), __uint_as_float(o[k + 5])),
+                                           pack(__uint_as_float(o[k + 6]), __uint_as_float(o[k + 7])));
+                } else {
+                    float* dst = a.part_o + w.part * a.dim + 32 * i;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        if (32 * i + k < a.dim)
+                            *reinterpret_cast<uint4*>(dst + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                }
+            }
+            if (row < g.rows) mafat_attn::store_lse(a, w, m, l);
+        }
+        fence_before();
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsOther));
+    if (warp == C::kMmaWarp) {
+        const uint32_t el = elect_one();
+        const uint32_t id_s = instr_desc(kKeys, false), id_o = instr_desc(DP, true), hi = desc_hi();
+        const uint32_t q_lo = desc_lo(base, 16u), k_lo = desc_lo(base + C::kOffKv, 16u),
+                       v_lo = desc_lo(base + C::kOffKv, C::kSub);
+        constexpr uint32_t kTile16 = C::kTileBytes / 16, kSub16 = C::kSub / 16;
+        auto scores = [&](int slot, uint32_t stage) {
+            const uint32_t qa = q_lo + (uint32_t)slot * kTile16, kb = k_lo + stage * kTile16;
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+                const uint32_t step = (uint32_t)(k / 4) * kSub16 + (uint32_t)(k % 4) * 2u;  // 32 bytes along a row
+                mma_ss(el, tmem + (uint32_t)(slot * 128), qa + step, kb + step, hi, id_s, k > 0);
+            }
+        };
+        auto values = [&](int slot, uint32_t stage, uint32_t acc) {
+            const uint32_t vb = v_lo + stage * kTile16;
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k)  // 16 keys: 8 columns of P, two 8-key groups of V
+                mma_ts(el, tmem + (uint32_t)(SLOTS * 128 + slot * 128), tmem + (uint32_t)(slot * 128 + 8 * k),
+                       vb + (uint32_t)k * (2048u / 16u), hi, id_o, k > 0 ? 1u : acc);
+        };
+        if (t.n > 0) {
+            wait(bar(C::kBarQ), 0u, ctl);
+            wait(bar(C::kBarFull + 0), 0u, ctl);
+            fence_after();
+            for (int slot = 0; slot < SLOTS; ++slot) {
+                scores(slot, 0u);
+                commit_el(el, bar(C::kBarS + slot));
+            }
+            commit_el(el, bar(C::kBarEmpty + 0));
+        }
+        uint32_t stage = 1u, phase = 0u;  // of the next item of the ring: V of tile j
+#pragma unroll 1
+        for (int j = 0; j < t.n; ++j) {
+            const uint32_t vs = stage, vphase = phase;
+            if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
+            const uint32_t ks = stage, kphase = phase;
+            const bool more = j + 1 < t.n;
+            if (more && ++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
+#pragma unroll
+            for (int slot = 0; slot < SLOTS; ++slot) {
+                if (slot == 0) {
+                    wait(bar(C::kBarFull) + vs * 8u, vphase, ctl);
+                    if (t.partial(j)) {
+                        const int n = t.ordinal(j);
+                        wait(bar(C::kBarMask + n % kWordsDepth), (uint32_t)(n / kWordsDepth) & 1u, ctl);
+                    }
+                }
+                wait(bar(C::kBarP + slot), (uint32_t)j & 1u, ctl);
+                fence_after();
+                values(slot, vs, j > 0);
+                if (more) {
+                    if (slot == 0) {
+                        wait(bar(C::kBarFull) + ks * 8u, kphase, ctl);
+                        fence_after();
+                    }
+                    scores(slot, ks);
+                }
+                commit_el(el, bar(C::kBarS + slot));
+            }
+            commit_el(el, bar(C::kBarEmpty) + vs * 8u);
+            if (more) commit_el(el, bar(C::kBarEmpty) + ks * 8u);
+        }
+    } else if (warp == C::kLoadWarp) {
+        const uint32_t el = elect_one();
+        uint32_t stage = 0u, phase = 1u;  // the first wait on an empty stage is over at once
+#pragma unroll 1
+        for (int i = 0; i < 2 * t.n; ++i) {
+            wait(bar(C::kBarEmpty) + stage * 8u, phase, ctl);
+            const uint32_t full = bar(C::kBarFull) + stage * 8u, dst = base + C::kOffKv + stage * C::kTileBytes;
+            expect_el(el, full, C::kTileBytes);
+#pragma unroll
+            for (int c = 0; c < DP / 64; ++c)
+                tma_tile(el, dst + c * C::kSub, (i & 1) ? &vmap : &kmap, c * 64, b.head, t.key0 + (i / 2) * kKeys, b.seq,
+                         full);
+            if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
+        }
+    } else if (warp == C::kMaskWarp) {
+        const uint8_t* mask = t.masked ? g.mask + (int64_t)b.seq * g.n : nullptr;
+        uint32_t stage = 0u, phase = 0u;
+#pragma unroll 1
+        for (int i = 0; i < 2 * t.n; ++i) {
+            const int j = i / 2;
+            uint32_t w[4] = {0u, 0u, 0u, 0u};
+            const bool part = (i & 1) && t.partial(j);
+            if (part) {
+                const int key = t.key0 + j * kKeys + lane;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w[k] = __ballot_sync(0xffffffffu, key + 32 * k < t.len && (!mask || mask[key + 32 * k] != 0));
+            }
+            wait(bar(C::kBarFull) + stage * 8u, phase, ctl);
+            if (part) {
+                const int n = t.ordinal(j);
+                if (lane == 0)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) words[(n % kWordsDepth) * 4 + k] = w[k];
+                uint8_t* v = sm + C::kOffKv + stage * C::kTileBytes;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (w[k] == 0xffffffffu) continue;
+                    for (int r = lane / 8; r < 32; r += 4)
+                        if (!(w[k] >> r & 1u))
+#pragma unroll
+                            for (int c = 0; c < DP / 64; ++c)
+                                *reinterpret_cast<uint4*>(v + c * C::kSub + (k * 32 + r) * 128 + (lane % 8) * 16) =
+                                    make_uint4(0u, 0u, 0u, 0u);
+                }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) arrive(bar(C::kBarMask + n % kWordsDepth));
+            }
+            __syncwarp();
+            if (lane == 0) arrive(bar(C::kBarEmpty) + stage * 8u);
+            if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
+        }
+    }
+    }
+    __syncthreads();
+    if (warp == C::kMmaWarp) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols));
+    }
+}
+
+template <int DP, int SLOTS>
+cudaError_t launch(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
+    attn_tc_kernel<DP, SLOTS><<<a.seg[0].blocks, Cfg<DP, SLOTS>::kThreads, Cfg<DP, SLOTS>::kSmem, s>>>(a, k, v);
+    return cudaGetLastError();
+}
+template <int DP, int SLOTS>
+cudaError_t prepare() {
+    using C = Cfg<DP, SLOTS>;
+    cudaFuncAttributes at;
+    cudaError_t e = cudaFuncGetAttributes(&at, attn_tc_kernel<DP, SLOTS>);
+    if (e != cudaSuccess) return e;
+    // with fewer registers at launch than the roles' shares add up to, setmaxnreg.inc would wait forever
+    if (at.numRegs < C::kRegs) return cudaErrorInvalidConfiguration;
+    return cudaFuncSetAttribute(attn_tc_kernel<DP, SLOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                Cfg<DP, SLOTS>::kSmem);
+}
+
+}  // namespace
+
+cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
+                                 cudaStream_t s) {
+    if (slots == 2) return a.dim <= 64 ? launch<64, 2>(a, k, v, s) : launch<128, 2>(a, k, v, s);
+    return a.dim <= 64 ? launch<64, 1>(a, k, v, s) : launch<128, 1>(a, k, v, s);
+}
+
+cudaError_t mafat_prepare_attn_tc() {
+    cudaError_t e;
+    if ((e = prepare<64, 1>()) != cudaSuccess) return e;
+    if ((e = prepare<128, 1>()) != cudaSuccess) return e;
+    if ((e = prepare<64, 2>()) != cudaSuccess) return e;
+    return prepare<128, 2>();
+}
