@@ -13,6 +13,7 @@ tiles each group's output with an N x M grid.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -403,31 +404,47 @@ class Plan:
             pass
 
 
-def _want(name, t, shape, dtype, strides=None):
-    """Refuses a tensor that is not what the plan was made for: the library sees only its address."""
-    if not hasattr(t, "data_ptr"):
-        return  # a raw address: the caller's word
-    if tuple(t.shape) != shape or _code(t) != dtype or not t.is_cuda:
-        raise MafatError(EINVAL, "%s: %s %s on %s, expected %s of type %s on the GPU"
-                         % (name, tuple(t.shape), t.dtype, t.device, shape, dtype))
-    if strides is None:
-        ok = t.is_contiguous()
-    else:
-        ok = all(n == 1 or a == b for n, a, b in zip(shape, t.stride(), strides))
-    if not ok:
-        raise MafatError(EINVAL, "%s: strides %s are not the plan's" % (name, t.stride()))
+def _types():
+    """(torch types, the library's name of each): masks are bytes, lengths int32."""
+    import torch
+    return {BF16: (torch.bfloat16,), FP32: (torch.float32,), E4M3: (torch.float8_e4m3fn,),
+            "mask": (torch.bool, torch.uint8), "int32": (torch.int32,)}
 
 
-_CODES = {}
+_TYPES, _CODES = {}, {}
 
 
 def _code(t):
-    """The library's name of a tensor's type; 1 byte masks and int32 lengths by their width."""
     if not _CODES:
-        import torch
-        _CODES.update({torch.bfloat16: BF16, torch.float32: FP32, torch.float8_e4m3fn: E4M3, torch.bool: "mask",
-                       torch.uint8: "mask", torch.int32: "int32"})
+        _TYPES.update(_types())
+        _CODES.update({dt: code for code, dts in _TYPES.items() for dt in dts})
     return _CODES.get(t.dtype)
+
+
+def _addr(name, t, shape, dtype, strides=None):
+    """Address of a tensor, or of raw memory given as an int.  Refuses a tensor that is not what the plan
+    was made for (the library sees only its address); strides None: packed."""
+    if t is None:
+        return None
+    if not hasattr(t, "data_ptr"):
+        return _ptr(t)  # the caller's word
+    if t.shape != shape or _code(t) != dtype or not t.is_cuda:
+        raise MafatError(EINVAL, "%s: %s %s on %s, expected %s of type %s on the GPU"
+                         % (name, tuple(t.shape), t.dtype, t.device, shape, dtype))
+    if not t.is_contiguous() if strides is None else \
+            any(a != b and n > 1 for n, a, b in zip(shape, t.stride(), strides)):
+        raise MafatError(EINVAL, "%s: strides %s are not the plan's" % (name, t.stride()))
+    return t.data_ptr()
+
+
+def _launch_stream(stream, like):
+    """As _stream; the current stream without making an object of it (a call takes 1 us instead of 3)."""
+    if stream is None and getattr(like, "is_cuda", False):
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(like.get_device())
+    return _stream(stream, like)
 
 
 class _Attention:
@@ -492,18 +509,11 @@ class CrossAttention(_Attention):
     def run(self, q, k, v, out, kv_len=None, kv_mask=None, lse=None, stream=None):
         """q, out [batch][n_q][heads_q][head_dim]; k, v [batch][n_kv][heads_kv][head_dim]; kv_len
         [batch] int32; kv_mask [batch][n_kv] bool (False: not readable); lse [batch][n_q][heads_q] fp32."""
-        _want("q", q, self._q[0], self.dtype, self._q[1])
-        _want("k", k, self._k[0], self.dtype, self._k[1])
-        _want("v", v, self._v[0], self.dtype, self._v[1])
-        _want("out", out, self._out[0], self.dtype, self._out[1])
-        if kv_len is not None:
-            _want("kv_len", kv_len, self._k[0][:1], "int32")
-        if kv_mask is not None:
-            _want("kv_mask", kv_mask, self._k[0][:2], "mask")
-        if lse is not None:
-            _want("lse", lse, self._q[0][:3], FP32)
-        _check(lib.mafat_cross_run(self.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(kv_mask), _ptr(out),
-                                   _ptr(lse), _stream(stream, q)))
+        dt, (nq, sq), (nk, sk) = self.dtype, self._q, self._k
+        _check(lib.mafat_cross_run(
+            self.handle, _addr("q", q, nq, dt, sq), _addr("k", k, nk, dt, sk), _addr("v", v, nk, dt, self._v[1]),
+            _addr("kv_len", kv_len, nk[:1], "int32"), _addr("kv_mask", kv_mask, nk[:2], "mask"),
+            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], FP32), _launch_stream(stream, q)))
 
 
 class PrefixAttention(_Attention):
@@ -532,48 +542,45 @@ class PrefixAttention(_Attention):
         """q, out [prefixes * requests][n_q][heads_q][head_dim]; prefix_k, prefix_v [prefixes][n_prefix]
         [heads_kv][head_dim]; own_k, own_v [prefixes * requests][n_own][heads_kv][head_dim]; prefix_len
         [prefixes], own_len [prefixes * requests] int32; prefix_mask [prefixes][n_prefix] bool; lse fp32."""
-        _want("q", q, self._q[0], self.dtype, self._q[1])
-        _want("prefix_k", prefix_k, self._pk[0], self.dtype, self._pk[1])
-        _want("prefix_v", prefix_v, self._pv[0], self.dtype, self._pv[1])
-        _want("own_k", own_k, self._ok[0], self.dtype, self._ok[1])
-        _want("own_v", own_v, self._ov[0], self.dtype, self._ov[1])
-        _want("out", out, self._out[0], self.dtype, self._out[1])
-        if prefix_len is not None:
-            _want("prefix_len", prefix_len, self._pk[0][:1], "int32")
-        if prefix_mask is not None:
-            _want("prefix_mask", prefix_mask, self._pk[0][:2], "mask")
-        if own_len is not None:
-            _want("own_len", own_len, self._q[0][:1], "int32")
-        if lse is not None:
-            _want("lse", lse, self._q[0][:3], FP32)
-        _check(lib.mafat_prefix_run(self.handle, _ptr(q), _ptr(prefix_k), _ptr(prefix_v), _ptr(prefix_len),
-                                    _ptr(prefix_mask), _ptr(own_k), _ptr(own_v), _ptr(own_len), _ptr(out), _ptr(lse),
-                                    _stream(stream, q)))
+        dt, (nq, sq), (npre, spk), (nown, sok) = self.dtype, self._q, self._pk, self._ok
+        _check(lib.mafat_prefix_run(
+            self.handle, _addr("q", q, nq, dt, sq), _addr("prefix_k", prefix_k, npre, dt, spk),
+            _addr("prefix_v", prefix_v, npre, dt, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], "int32"),
+            _addr("prefix_mask", prefix_mask, npre[:2], "mask"), _addr("own_k", own_k, nown, dt, sok),
+            _addr("own_v", own_v, nown, dt, self._ov[1]), _addr("own_len", own_len, nq[:1], "int32"),
+            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], FP32), _launch_stream(stream, q)))
 
 
 def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_group=0, eps=1e-6, stream=None):
     """mafat_rms_norm on [rows][cols] tensors: h = x + residual (written to residual_out if given),
     y = h / sqrt(mean(h^2) + eps) * weight, in x's type, or in float8_e4m3fn with fp32 scales
     [rows][1] (scale_group 0) or [rows][ceil(cols / 128)] (scale_group 128)."""
-    rows, cols = x.shape
-    dtype, out_dtype = _code(x), _code(y)
-    d = NormDesc(struct_size=ctypes.sizeof(NormDesc), dtype=-1 if dtype is None else dtype,
-                 out_dtype=-1 if out_dtype is None else out_dtype, cols=cols, rows=rows, scale_group=scale_group, eps=eps)
-    for name, t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y)):
-        if t is None:
-            continue
-        if t.dim() != 2:
-            raise MafatError(EINVAL, "%s: [rows][cols] expected" % name)
-        st = t.stride(0) if rows > 1 else cols
-        _want(name, t, (rows, cols), out_dtype if name == "y" else dtype, (st, 1))
-        if rows > 1 and st < cols:
-            raise MafatError(EINVAL, "%s: a row stride is smaller than cols" % name)
-        setattr(d, name + "_stride", st)
-    _want("weight", weight, (cols,), dtype)
-    if scales is not None:
-        _want("scales", scales, (rows, -(-cols // 128) if scale_group else 1), FP32)
-    _check(lib.mafat_rms_norm(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight), _ptr(residual_out), _ptr(y),
-                              _ptr(scales), _stream(stream, x)))
+    if x.dim() != 2:
+        raise MafatError(EINVAL, "x: [rows][cols] expected")
+    shape, dtype, out_dtype = x.shape, _code(x), _code(y)
+    rows, cols = shape
+    strides = [0 if t is None or rows <= 1 else t.stride(0) for t in (x, residual, residual_out, y)]
+    d = _norm_desc(-1 if dtype is None else dtype, -1 if out_dtype is None else out_dtype, rows, cols, scale_group, eps,
+                   *strides)
+    sx, sr, so, sy = [(st, 1) for st in strides]
+    _check(lib.mafat_rms_norm(
+        d, _addr("x", x, shape, dtype, sx), _addr("residual", residual, shape, dtype, sr),
+        _addr("weight", weight, shape[1:], dtype), _addr("residual_out", residual_out, shape, dtype, so),
+        _addr("y", y, shape, out_dtype, sy),
+        _addr("scales", scales, (rows, -(-cols // 128) if scale_group else 1), FP32), _launch_stream(stream, x)))
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_desc(dtype, out_dtype, rows, cols, scale_group, eps, *strides):
+    """The descriptor of a call, by its sizes alone (making one takes longer than the call)."""
+    if any(0 < st < cols for st in strides):
+        raise MafatError(EINVAL, "a row stride is smaller than cols")
+    if rows > 1 and any(st < 0 for st in strides):
+        raise MafatError(EINVAL, "a row stride is negative")
+    d = NormDesc(struct_size=ctypes.sizeof(NormDesc), dtype=dtype, out_dtype=out_dtype, cols=cols, rows=rows,
+                 scale_group=scale_group, eps=eps)
+    d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride = strides
+    return ctypes.byref(d)
 
 
 def diag_umma(a_dev, b_dev, d_dev, n, a_in_tmem=False, stream=None):

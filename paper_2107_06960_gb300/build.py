@@ -19,7 +19,7 @@ ROOT = os.path.dirname(HERE)
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmafat.so")
 SOURCES = ["planner.cpp", "order.cpp", "runtime.cpp", "search.cpp", "kernel_fp32.cu", "kernel_tc.cu", "noalloc.cu",
-           "attention.cpp", "attn_simt.cu", "attn_tc.cu", "attn_join.cu", "rms_norm.cu"]
+           "attention.cpp", "attn_simt.cu", "attn_rows.cu", "attn_tc.cu", "attn_join.cu", "rms_norm.cu"]
 HEADERS = ["planner.h", "device_types.h", "kernels.h", "sched.cuh", "attention.h", "attn_common.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -21,7 +21,7 @@ void mafat_internal_clear_error();
 void* mafat_internal_encode_tiled();
 
 // A kernel and the shape of its work.
-enum AttnKernel { kSimtRows, kSimtTiles, kTc1, kTc2 };
+enum AttnKernel { kSimtRows, kSimtTiles, kRows, kTc1, kTc2 };
 struct AttnShape {
     int rows, keys;  // of a CTA's tile
     int ctas;        // of an SM
@@ -144,6 +144,7 @@ mafat_status check_common(const Common& c) {
 
 AttnShape shape_of(AttnKernel k) {
     switch (k) {
+        case kRows: return {16, mafat_attn_rows_keys(), 2, 2};
         case kTc1: return {128, 128, 2, 2};
         case kTc2: return {256, 128, 1, 2};
         case kSimtTiles: return {mafat_attn_simt_rows(true), mafat_attn_simt_keys(), 1, 1};
@@ -152,10 +153,13 @@ AttnShape shape_of(AttnKernel k) {
 }
 bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
 
+constexpr int kFewRows = 16;  // a tile of the kernels for few rows
+bool is_rows(AttnKernel k) { return k == kSimtRows || k == kRows; }
+
 AttnKernel choose_kernel(int32_t dtype, int32_t asked, int32_t rows, int32_t n) {
-    const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= mafat_attn_simt_rows(false));
-    if (few) return kSimtRows;
-    if (dtype == MAFAT_FP32 || n == 0) return kSimtTiles;  // without keys there is nothing to map
+    const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= kFewRows);
+    if (dtype == MAFAT_FP32) return few ? kSimtRows : kSimtTiles;
+    if (few || n == 0) return kRows;  // without keys there is nothing to map
     return rows <= 128 ? kTc1 : kTc2;
 }
 
@@ -233,7 +237,8 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
     const int64_t lse_bytes = (p->rows_total * p->parts * 4 + 255) / 256 * 256;
     p->workspace_bytes = kStatusBytes + (p->parts > 1 ? lse_bytes + p->rows_total * p->parts * p->dim * 4 : 0);
     if (!p->dry_run) {
-        if ((e = mafat_prepare_attn_simt()) != cudaSuccess || (e = mafat_prepare_attn_tc()) != cudaSuccess)
+        if ((e = mafat_prepare_attn_simt()) != cudaSuccess || (e = mafat_prepare_attn_rows()) != cudaSuccess ||
+            (e = mafat_prepare_attn_tc()) != cudaSuccess)
             return cuda_fail(e, "attention kernels");
         if ((e = cudaMalloc(&p->workspace, (size_t)p->workspace_bytes)) != cudaSuccess) return cuda_fail(e, "cudaMalloc");
         p->status = (uint32_t*)p->workspace;
@@ -326,7 +331,7 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
                 return st;
             e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, s);
         } else {
-            e = mafat_launch_attn_simt(a, p->dtype == MAFAT_BF16, g.kernel != kSimtRows, s);
+            e = g.kernel == kRows ? mafat_launch_attn_rows(a, s) : mafat_launch_attn_simt(a, g.kernel == kSimtTiles, s);
         }
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }
@@ -422,7 +427,7 @@ mafat_status mafat_attn_stats(const mafat_attn_t* p, mafat_attn_stats_t* out) {
     mafat_attn_stats_t s{};
     s.struct_size = (int32_t)sizeof(mafat_attn_stats_t);
     for (int i = 0; i < p->n_seg; ++i) {
-        s.kernel[i] = p->seg[i].kernel == kSimtRows ? MAFAT_ATTN_ROWS : MAFAT_ATTN_TILES;
+        s.kernel[i] = is_rows(p->seg[i].kernel) ? MAFAT_ATTN_ROWS : MAFAT_ATTN_TILES;
         s.splits[i] = p->seg[i].splits;
         s.blocks[i] = p->seg[i].blocks;
     }

@@ -44,11 +44,16 @@ struct MafatAttnArgs {
     MafatAttnSeg seg[2];
 };
 
-// fp32 arithmetic on the CUDA cores; `wide` tiles have 64 rows, others 16.
-cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, bool bf16, bool wide, cudaStream_t s);
+// fp32 on the CUDA cores; `wide` tiles have 64 rows, others 16.
+cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, bool wide, cudaStream_t s);
 cudaError_t mafat_prepare_attn_simt();
 int mafat_attn_simt_rows(bool wide);
 int mafat_attn_simt_keys();
+
+// bf16, tiles of 16 rows by runs of 64 keys.
+cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, cudaStream_t s);
+cudaError_t mafat_prepare_attn_rows();
+int mafat_attn_rows_keys();
 
 // bf16 on the tensor cores: tiles of 128 * slots rows (slots 1 or 2) by 128 keys.  Runs one segment (seg[0]);
 // the maps are 4-D over {channel, head, key, sequence}, boxes of 64 channels x 128 keys, 128-byte swizzle.

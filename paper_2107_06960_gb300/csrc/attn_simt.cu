@@ -7,8 +7,6 @@
 //
 // A thread owns 4 rows x 4 keys of the scores and 4 rows x 2 quarters of the channels of O, so that a
 // 16-byte shared-memory read feeds 8 FMAs; K's and V's tiles are single buffers.
-#include <cuda_bf16.h>
-
 #include "attn_common.cuh"
 
 namespace {
@@ -26,24 +24,12 @@ struct Tile {
 };
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
-                       __uint_as_float(u.y & 0xFFFF0000u));
-}
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
-    __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-    uint2 u;
-    u.x = *reinterpret_cast<uint32_t*>(&a);
-    u.y = *reinterpret_cast<uint32_t*>(&b);
-    *reinterpret_cast<uint2*>(p) = u;
-}
 
 // rows [0, count) of a matrix with `stride` elements between rows into smem; channels past dim and
 // rows that are not readable become zero
-template <int ROWS, int DP, int PITCH, int THREADS, class T, class Ok>
-__device__ __forceinline__ void load_rows(float* dst, const T* src, int64_t stride, int dim, Ok ok) {
+template <int ROWS, int DP, int PITCH, int THREADS, class Ok>
+__device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t stride, int dim, Ok ok) {
     constexpr int kChunks = DP / 4;
 #pragma unroll 4
     for (int i = threadIdx.x; i < ROWS * kChunks; i += THREADS) {
@@ -54,7 +40,7 @@ __device__ __forceinline__ void load_rows(float* dst, const T* src, int64_t stri
     }
 }
 
-template <class T, int BM, int DP>
+template <int BM, int DP>
 __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_constant__ MafatAttnArgs a) {
     using L = Tile<BM, DP>;
     extern __shared__ __align__(16) float sm[];
@@ -73,7 +59,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
             const int r = i / kChunks, c = (i % kChunks) * 4;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (c < a.dim && b.row0 + r < g.rows)
-                v = load4((const T*)a.q + mafat_attn::q_offset(a, g, b, b.row0 + r) + c);
+                v = load4((const float*)a.q + mafat_attn::q_offset(a, g, b, b.row0 + r) + c);
             *reinterpret_cast<float4*>(sq + r * L::kPitch + c) = v;
         }
     }
@@ -87,8 +73,8 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
 #pragma unroll
         for (int d = 0; d < DP / kTX; ++d) o[i][d] = 0.f;
     }
-    const T* kp = (const T*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
-    const T* vp = (const T*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
+    const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
+    const float* vp = (const float*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
     const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
 
     for (int key0 = b.key0; key0 < b.key1; key0 += kBN) {
@@ -186,7 +172,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
             const float4 v = make_float4(o[i][c * 4] * inv, o[i][c * 4 + 1] * inv, o[i][c * 4 + 2] * inv,
                                          o[i][c * 4 + 3] * inv);
             if (a.parts == 1)
-                store4((T*)a.out + w.o + d, v);
+                store4((float*)a.out + w.o + d, v);
             else
                 store4(a.part_o + w.part * a.dim + d, v);
         }
@@ -194,42 +180,32 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
     }
 }
 
-template <class T, int BM, int DP>
+template <int BM, int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
     int blocks = 0;
     for (int i = 0; i < a.n_seg; ++i) blocks += a.seg[i].blocks;
-    attn_simt_kernel<T, BM, DP><<<blocks, Tile<BM, DP>::kThreads, Tile<BM, DP>::kSmem, s>>>(a);
+    attn_simt_kernel<BM, DP><<<blocks, Tile<BM, DP>::kThreads, Tile<BM, DP>::kSmem, s>>>(a);
     return cudaGetLastError();
 }
-template <class T, int BM, int DP>
+template <int BM, int DP>
 cudaError_t prepare() {
-    return cudaFuncSetAttribute(attn_simt_kernel<T, BM, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(attn_simt_kernel<BM, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 Tile<BM, DP>::kSmem);
 }
-template <class T>
-cudaError_t launch_t(const MafatAttnArgs& a, bool wide, cudaStream_t s) {
-    if (wide) return a.dim <= 64 ? launch<T, 64, 64>(a, s) : launch<T, 64, 128>(a, s);
-    return a.dim <= 64 ? launch<T, 16, 64>(a, s) : launch<T, 16, 128>(a, s);
-}
-template <class T>
-cudaError_t prepare_t() {
-    cudaError_t e;
-    if ((e = prepare<T, 64, 64>()) != cudaSuccess) return e;
-    if ((e = prepare<T, 64, 128>()) != cudaSuccess) return e;
-    if ((e = prepare<T, 16, 64>()) != cudaSuccess) return e;
-    return prepare<T, 16, 128>();
-}
-
 }  // namespace
 
 int mafat_attn_simt_rows(bool wide) { return wide ? 64 : 16; }
 int mafat_attn_simt_keys() { return kBN; }
 
 cudaError_t mafat_prepare_attn_simt() {
-    cudaError_t e = prepare_t<float>();
-    return e != cudaSuccess ? e : prepare_t<__nv_bfloat16>();
+    cudaError_t e;
+    if ((e = prepare<64, 64>()) != cudaSuccess) return e;
+    if ((e = prepare<64, 128>()) != cudaSuccess) return e;
+    if ((e = prepare<16, 64>()) != cudaSuccess) return e;
+    return prepare<16, 128>();
 }
 
-cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, bool bf16, bool wide, cudaStream_t s) {
-    return bf16 ? launch_t<__nv_bfloat16>(a, wide, s) : launch_t<float>(a, wide, s);
+cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, bool wide, cudaStream_t s) {
+    if (wide) return a.dim <= 64 ? launch<64, 64>(a, s) : launch<64, 128>(a, s);
+    return a.dim <= 64 ? launch<16, 64>(a, s) : launch<16, 128>(a, s);
 }
