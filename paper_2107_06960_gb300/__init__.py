@@ -404,36 +404,43 @@ class Plan:
             pass
 
 
-def _types():
-    """(torch types, the library's name of each): masks are bytes, lengths int32."""
-    import torch
-    return {BF16: (torch.bfloat16,), FP32: (torch.float32,), E4M3: (torch.float8_e4m3fn,),
-            "mask": (torch.bool, torch.uint8), "int32": (torch.int32,)}
+_TYPES = {}  # library's name of a type -> the torch types that hold it; filled when torch is there
 
 
-_TYPES, _CODES = {}, {}
+def _type(code):
+    """The torch type of a library type's name: masks are bytes (bool or uint8), lengths int32."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({BF16: torch.bfloat16, FP32: torch.float32, E4M3: torch.float8_e4m3fn, "mask": torch.bool,
+                       "byte": torch.uint8, "int32": torch.int32})
+    return _TYPES.get(code)
 
 
 def _code(t):
-    if not _CODES:
-        _TYPES.update(_types())
-        _CODES.update({dt: code for code, dts in _TYPES.items() for dt in dts})
-    return _CODES.get(t.dtype)
+    _type(BF16)
+    return next((code for code, dt in _TYPES.items() if dt is t.dtype), -1)
 
 
 def _addr(name, t, shape, dtype, strides=None):
     """Address of a tensor, or of raw memory given as an int.  Refuses a tensor that is not what the plan
-    was made for (the library sees only its address); strides None: packed."""
+    was made for (the library sees only its address); dtype: a torch type, strides None: packed."""
     if t is None:
         return None
-    if not hasattr(t, "data_ptr"):
-        return _ptr(t)  # the caller's word
-    if t.shape != shape or _code(t) != dtype or not t.is_cuda:
-        raise MafatError(EINVAL, "%s: %s %s on %s, expected %s of type %s on the GPU"
-                         % (name, tuple(t.shape), t.dtype, t.device, shape, dtype))
-    if not t.is_contiguous() if strides is None else \
-            any(a != b and n > 1 for n, a, b in zip(shape, t.stride(), strides)):
-        raise MafatError(EINVAL, "%s: strides %s are not the plan's" % (name, t.stride()))
+    try:
+        if t.dtype is dtype and t.is_cuda and t.shape == shape and (t.is_contiguous() if strides is None
+                                                                    else t.stride() == strides):
+            return t.data_ptr()
+    except AttributeError:
+        if not hasattr(t, "data_ptr"):
+            return _ptr(t)  # the caller's word
+        raise
+    if dtype is _TYPES["mask"] and t.dtype is _TYPES["byte"]:
+        return _addr(name, t, shape, t.dtype, strides)
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape:
+        raise MafatError(EINVAL, "%s: %s %s on %s, expected %s %s on the GPU"
+                         % (name, tuple(t.shape), t.dtype, t.device, tuple(shape), dtype))
+    if strides is None or any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
+        raise MafatError(EINVAL, "%s: strides %s, expected %s" % (name, t.stride(), strides or "packed"))
     return t.data_ptr()
 
 
@@ -459,11 +466,17 @@ class _Attention:
         _check(plan(ctypes.byref(desc), ctypes.byref(h)))
         self.handle = h
         self.dtype = desc.dtype
+        self._types = None
 
     @staticmethod
     def _layout(n, given):
         """(shape, strides) of a [sequence][token][head][channel] tensor; strides None where packed."""
         return n, None if given is None or not any(given) else tuple(given) + (1,)
+
+    def _torch(self):
+        """The torch types of (the plan, lengths, masks, log-sums)."""
+        self._types = _type(self.dtype), _type("int32"), _type("mask"), _type(FP32)
+        return self._types
 
     def stats(self):
         """What the plan chose: by set of keys (the states or the prefix; a request's own) the kernel,
@@ -509,11 +522,11 @@ class CrossAttention(_Attention):
     def run(self, q, k, v, out, kv_len=None, kv_mask=None, lse=None, stream=None):
         """q, out [batch][n_q][heads_q][head_dim]; k, v [batch][n_kv][heads_kv][head_dim]; kv_len
         [batch] int32; kv_mask [batch][n_kv] bool (False: not readable); lse [batch][n_q][heads_q] fp32."""
-        dt, (nq, sq), (nk, sk) = self.dtype, self._q, self._k
+        (dt, i32_, mask, f32_), (nq, sq), (nk, sk) = self._types or self._torch(), self._q, self._k
         _check(lib.mafat_cross_run(
             self.handle, _addr("q", q, nq, dt, sq), _addr("k", k, nk, dt, sk), _addr("v", v, nk, dt, self._v[1]),
-            _addr("kv_len", kv_len, nk[:1], "int32"), _addr("kv_mask", kv_mask, nk[:2], "mask"),
-            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], FP32), _launch_stream(stream, q)))
+            _addr("kv_len", kv_len, nk[:1], i32_), _addr("kv_mask", kv_mask, nk[:2], mask),
+            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], f32_), _launch_stream(stream, q)))
 
 
 class PrefixAttention(_Attention):
@@ -542,45 +555,48 @@ class PrefixAttention(_Attention):
         """q, out [prefixes * requests][n_q][heads_q][head_dim]; prefix_k, prefix_v [prefixes][n_prefix]
         [heads_kv][head_dim]; own_k, own_v [prefixes * requests][n_own][heads_kv][head_dim]; prefix_len
         [prefixes], own_len [prefixes * requests] int32; prefix_mask [prefixes][n_prefix] bool; lse fp32."""
-        dt, (nq, sq), (npre, spk), (nown, sok) = self.dtype, self._q, self._pk, self._ok
+        dt, i32_, mask, f32_ = self._types or self._torch()
+        (nq, sq), (npre, spk), (nown, sok) = self._q, self._pk, self._ok
         _check(lib.mafat_prefix_run(
             self.handle, _addr("q", q, nq, dt, sq), _addr("prefix_k", prefix_k, npre, dt, spk),
-            _addr("prefix_v", prefix_v, npre, dt, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], "int32"),
-            _addr("prefix_mask", prefix_mask, npre[:2], "mask"), _addr("own_k", own_k, nown, dt, sok),
-            _addr("own_v", own_v, nown, dt, self._ov[1]), _addr("own_len", own_len, nq[:1], "int32"),
-            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], FP32), _launch_stream(stream, q)))
+            _addr("prefix_v", prefix_v, npre, dt, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], i32_),
+            _addr("prefix_mask", prefix_mask, npre[:2], mask), _addr("own_k", own_k, nown, dt, sok),
+            _addr("own_v", own_v, nown, dt, self._ov[1]), _addr("own_len", own_len, nq[:1], i32_),
+            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], f32_), _launch_stream(stream, q)))
 
 
 def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_group=0, eps=1e-6, stream=None):
     """mafat_rms_norm on [rows][cols] tensors: h = x + residual (written to residual_out if given),
     y = h / sqrt(mean(h^2) + eps) * weight, in x's type, or in float8_e4m3fn with fp32 scales
     [rows][1] (scale_group 0) or [rows][ceil(cols / 128)] (scale_group 128)."""
-    if x.dim() != 2:
-        raise MafatError(EINVAL, "x: [rows][cols] expected")
-    shape, dtype, out_dtype = x.shape, _code(x), _code(y)
-    rows, cols = shape
-    strides = [0 if t is None or rows <= 1 else t.stride(0) for t in (x, residual, residual_out, y)]
-    d = _norm_desc(-1 if dtype is None else dtype, -1 if out_dtype is None else out_dtype, rows, cols, scale_group, eps,
-                   *strides)
-    sx, sr, so, sy = [(st, 1) for st in strides]
+    shape, dt, out_dt = x.shape, x.dtype, y.dtype
+    packed = x.is_contiguous() and y.is_contiguous() and (residual is None or residual.is_contiguous()) and (
+        residual_out is None or residual_out.is_contiguous())
+    strides = None if packed else tuple(
+        0 if t is None or t.dim() != 2 or t.shape[0] < 2 else t.stride(0) for t in (x, residual, residual_out, y))
+    desc, f32_, scales_shape = _norm_call(shape, dt, out_dt, scale_group, eps, strides)
+    sx, sr, so, sy = (None,) * 4 if packed else [(st, 1) for st in strides]
     _check(lib.mafat_rms_norm(
-        d, _addr("x", x, shape, dtype, sx), _addr("residual", residual, shape, dtype, sr),
-        _addr("weight", weight, shape[1:], dtype), _addr("residual_out", residual_out, shape, dtype, so),
-        _addr("y", y, shape, out_dtype, sy),
-        _addr("scales", scales, (rows, -(-cols // 128) if scale_group else 1), FP32), _launch_stream(stream, x)))
+        desc, _addr("x", x, shape, dt, sx), _addr("residual", residual, shape, dt, sr),
+        _addr("weight", weight, shape[1:], dt), _addr("residual_out", residual_out, shape, dt, so),
+        _addr("y", y, shape, out_dt, sy), _addr("scales", scales, scales_shape, f32_), _launch_stream(stream, x)))
 
 
 @functools.lru_cache(maxsize=256)
-def _norm_desc(dtype, out_dtype, rows, cols, scale_group, eps, *strides):
-    """The descriptor of a call, by its sizes alone (making one takes longer than the call)."""
-    if any(0 < st < cols for st in strides):
-        raise MafatError(EINVAL, "a row stride is smaller than cols")
-    if rows > 1 and any(st < 0 for st in strides):
-        raise MafatError(EINVAL, "a row stride is negative")
-    d = NormDesc(struct_size=ctypes.sizeof(NormDesc), dtype=dtype, out_dtype=out_dtype, cols=cols, rows=rows,
-                 scale_group=scale_group, eps=eps)
-    d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride = strides
-    return ctypes.byref(d)
+def _norm_call(shape, dt, out_dt, scale_group, eps, strides):
+    """The descriptor of a call, by its sizes and types alone (making one takes longer than the call)."""
+    if len(shape) != 2:
+        raise MafatError(EINVAL, "x: [rows][cols] expected")
+    _type(BF16)
+    code = {v: k for k, v in _TYPES.items()}
+    rows, cols = shape
+    d = NormDesc(struct_size=ctypes.sizeof(NormDesc), cols=cols, rows=rows, scale_group=scale_group, eps=eps)
+    d.dtype, d.out_dtype = (c if isinstance(c, int) else -1 for c in (code.get(dt), code.get(out_dt)))
+    if strides is not None:
+        if any(st < 0 or 0 < st < cols for st in strides):
+            raise MafatError(EINVAL, "a row stride is smaller than cols")
+        d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride = strides
+    return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1)
 
 
 def diag_umma(a_dev, b_dev, d_dev, n, a_in_tmem=False, stream=None):

@@ -188,6 +188,7 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
     const int64_t items = (int64_t)g.n_seq * p.heads_kv * g.row_tiles;
     const int64_t tiles = std::max<int64_t>(1, ((int64_t)g.n + sh.keys - 1) / sh.keys);
     g.splits = c.splits ? (int32_t)std::min<int64_t>(c.splits, tiles) : choose_splits(items, tiles, (int64_t)sms * sh.ctas, sh.setup);
+    if (g.n > kMaxI32 - 65536) return fail(MAFAT_EUNSUPPORTED, "too many keys");
     if (items * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many blocks");
     g.blocks = (int32_t)(items * g.splits);
     g.part0 = p.parts;
@@ -280,6 +281,10 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
     a.heads_q = p->heads_q;
     a.heads_kv = p->heads_kv;
     a.dim = p->dim;
+    a.n_q_div = MafatDiv((uint32_t)a.n_q);
+    a.group_div = MafatDiv((uint32_t)a.group);
+    a.heads_q_div = MafatDiv((uint32_t)a.heads_q);
+    a.heads_kv_div = MafatDiv((uint32_t)a.heads_kv);
     a.parts = p->parts;
     a.scale_log2 = (float)((double)p->scale * 1.4426950408889634);
     a.part_o = p->part_o;
@@ -320,9 +325,12 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         x.rows = g.rows;
         x.row_tiles = g.row_tiles;
         x.splits = g.splits;
+        x.row_tiles_div = MafatDiv((uint32_t)g.row_tiles);
+        x.splits_div = MafatDiv((uint32_t)g.splits);
         x.part0 = g.part0;
         x.blocks = g.blocks;
         a.n_seg = 1;
+        a.overlap = i > 0;
         if (is_tc(g.kernel)) {
             CUtensorMap k, v;
             mafat_status st;
@@ -336,6 +344,7 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }
     if (p->parts > 1) {
+        a.overlap = 0;
         e = mafat_launch_attn_join(a, p->dtype == MAFAT_BF16, s);
         if (e != cudaSuccess) return cuda_fail(e, "join launch");
     }

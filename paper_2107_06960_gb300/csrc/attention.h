@@ -5,6 +5,24 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+// Division by a number known at launch, for dividends below 2^31: a product and a shift (Granlund
+// and Montgomery, "Division by invariant integers using multiplication", 1994).
+struct MafatDiv {
+    uint32_t d = 1, mul = 1, shift = 0;
+    __host__ __device__ MafatDiv() {}
+    explicit MafatDiv(uint32_t n) : d(n) {
+        while (shift < 32 && (1ull << shift) < n) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - n)) / n + 1);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t x) const {
+#ifdef __CUDA_ARCH__
+        return (__umulhi(x, mul) + x) >> shift;
+#else
+        return x / d;
+#endif
+    }
+};
+
 // One set of keys and values: n_seq sequences, each read by the n_q queries of `reqs` requests.
 // The rows of a (sequence, key head) are its queries, row = (request * n_q + token) * group + head.
 // A CTA takes one tile of rows and one of `splits` parts of the readable keys.
@@ -22,6 +40,7 @@ struct MafatAttnSeg {
     int32_t rows;               // reqs * n_q * group
     int32_t row_tiles;
     int32_t splits;
+    MafatDiv row_tiles_div, splits_div;
     int32_t part0;              // first of its splits among the parts of a row
     int32_t blocks;             // n_seq * heads_kv * splits * row_tiles
 };
@@ -33,12 +52,16 @@ struct MafatAttnArgs {
     int64_t q_sb, q_st, q_sh;
     int64_t o_sb, o_st, o_sh;
     int32_t n_q, group, heads_q, heads_kv, dim;
+    MafatDiv n_q_div, group_div, heads_q_div, heads_kv_div;
     int32_t parts;              // parts of a row over all segments; 1: a CTA writes the result itself
     float scale_log2;           // softmax scale times log2(e)
     int32_t n_seg;
     float* part_o;              // [parts][rows_total][dim] results of the parts, each normalised
     float* part_lse;            // [parts][rows_total] their log2 of the sum of exponentials
     int64_t rows_total;         // batch * n_q * heads_q, row index = (request * n_q + token) * heads_q + head
+    // 1: an earlier launch of the same run, which has waited for what came before, is all that this one
+    // follows, and not its results: it waits at its end only, for those that join both
+    int32_t overlap;
     uint32_t* status;           // [2] status and abort words, as the plans' counter block starts
     int64_t timeout_ns;
     MafatAttnSeg seg[2];
@@ -77,6 +100,23 @@ struct MafatNormArgs {
     int32_t groups;             // scales of a row
     float eps;
 };
+// Launches fn with programmatic stream serialisation: it may start while the launch before it ends,
+// and waits (griddepcontrol.wait) before it touches memory.
+template <class... P, class... A>
+cudaError_t mafat_launch_overlapped(void (*fn)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at = {};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fn, P(args)...);
+}
+
 enum MafatNormQuant { MAFAT_NORM_PLAIN = 0, MAFAT_NORM_ROW = 1, MAFAT_NORM_BLOCK = 2 };
 
 int mafat_norm_max_cols();  // of a row

@@ -13,65 +13,89 @@ struct Block {
     int len;         // readable keys of the sequence
     int key0, key1;  // its part of them: a run of whole tiles
 
+    // Reads the sequence's length: after launch_begin.
     __device__ __forceinline__ Block(const MafatAttnArgs& a, int tile_rows, int tile_keys) {
-        int i = (int)blockIdx.x;
+        uint32_t i = blockIdx.x;
         seg = 0;
-        if (i >= a.seg[0].blocks) {
-            i -= a.seg[0].blocks;
+        if (i >= (uint32_t)a.seg[0].blocks) {
+            i -= (uint32_t)a.seg[0].blocks;
             seg = 1;
         }
         const MafatAttnSeg& g = a.seg[seg];
-        row0 = (i % g.row_tiles) * tile_rows;
-        i /= g.row_tiles;
-        split = i % g.splits;
-        i /= g.splits;
-        head = i % a.heads_kv;
-        seq = i / a.heads_kv;
+        uint32_t next = g.row_tiles_div.div(i);
+        row0 = (int)(i - next * (uint32_t)g.row_tiles) * tile_rows;
+        i = next;
+        next = g.splits_div.div(i);
+        split = (int)(i - next * (uint32_t)g.splits);
+        i = next;
+        next = a.heads_kv_div.div(i);
+        head = (int)(i - next * (uint32_t)a.heads_kv);
+        seq = (int)next;
         len = g.n;
         if (g.len) len = min(max(g.len[seq], 0), g.n);
         // the keys that some row of the tile sees
         int last = len;
         if (g.causal) {
             const int r1 = min(row0 + tile_rows, g.rows);
-            const int per = a.n_q * a.group;  // rows of a request
             // the latest token among the tile's rows
-            const int t = (row0 / per != (r1 - 1) / per) ? a.n_q - 1 : (r1 - 1) % per / a.group;
+            const uint32_t u0 = a.group_div.div((uint32_t)row0), u1 = a.group_div.div((uint32_t)(r1 - 1));
+            const uint32_t q0 = a.n_q_div.div(u0), q1 = a.n_q_div.div(u1);
+            const int t = q0 != q1 ? a.n_q - 1 : (int)(u1 - q1 * (uint32_t)a.n_q);
             last = min(max(len - a.n_q + t + 1, 0), len);
         }
-        const int64_t tiles = (last + tile_keys - 1) / tile_keys;
-        key0 = (int)(tiles * split / g.splits) * tile_keys;
-        key1 = min((int)(tiles * (split + 1) / g.splits) * tile_keys, last);
+        const uint32_t tiles = ((uint32_t)last + (uint32_t)tile_keys - 1) / (uint32_t)tile_keys;
+        // tiles * split / splits without 64 bits: whole tiles a split, and the rest's share
+        const uint32_t each = g.splits_div.div(tiles), rest = tiles - each * (uint32_t)g.splits;
+        const uint32_t s0 = (uint32_t)split, s1 = s0 + 1;
+        key0 = (int)(each * s0 + g.splits_div.div(rest * s0)) * tile_keys;
+        key1 = min((int)(each * s1 + g.splits_div.div(rest * s1)) * tile_keys, last);
     }
 };
 
-// Where row r of the CTA's (sequence, key head) has its query.
-__device__ __forceinline__ int64_t q_offset(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b, int r) {
-    const int h = r % a.group, u = r / a.group, t = u % a.n_q;
-    const int64_t req = (int64_t)b.seq * g.reqs + u / a.n_q;
-    return req * a.q_sb + (int64_t)t * a.q_st + (int64_t)(b.head * a.group + h) * a.q_sh;
-}
+// Row r of a (sequence, key head): its request among all, token and query head.
+struct Row {
+    int64_t req;
+    int t, h;
+    __device__ __forceinline__ Row(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b, int r) {
+        const uint32_t u = a.group_div.div((uint32_t)r), q = a.n_q_div.div(u);
+        h = b.head * a.group + (r - (int)u * a.group);
+        t = (int)u - (int)q * a.n_q;
+        req = (int64_t)b.seq * g.reqs + q;
+    }
+    __device__ __forceinline__ int64_t query(const MafatAttnArgs& a) const {
+        return req * a.q_sb + (int64_t)t * a.q_st + (int64_t)h * a.q_sh;
+    }
+    // it sees the keys below this one
+    __device__ __forceinline__ int limit(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b) const {
+        return g.causal ? min(max(b.len - a.n_q + t + 1, 0), b.len) : b.len;
+    }
+};
 
-// Row r sees the keys below this one.
-__device__ __forceinline__ int row_limit(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b, int r) {
-    if (!g.causal) return b.len;
-    const int t = r / a.group % a.n_q;
-    return min(max(b.len - a.n_q + t + 1, 0), b.len);
-}
-
-// Where row r's results go.
+// Where a row's results go.
 struct Out {
     int64_t o;     // element of out
     int64_t row;   // row among all
     int64_t part;  // row of the parts' arrays
 
-    __device__ __forceinline__ Out(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b, int r) {
-        const int h = b.head * a.group + r % a.group, u = r / a.group, t = u % a.n_q;
-        const int64_t req = (int64_t)b.seq * g.reqs + u / a.n_q;
-        o = req * a.o_sb + (int64_t)t * a.o_st + (int64_t)h * a.o_sh;
-        row = (req * a.n_q + t) * a.heads_q + h;
+    __device__ __forceinline__ Out(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b, const Row& r) {
+        o = r.req * a.o_sb + (int64_t)r.t * a.o_st + (int64_t)r.h * a.o_sh;
+        row = (r.req * a.n_q + r.t) * a.heads_q + r.h;
         part = (int64_t)(g.part0 + b.split) * a.rows_total + row;
     }
 };
+
+// A launch may start while the one before it ends: it waits before it touches memory that others
+// write, then lets the next one start.  One that follows a launch of its own run, whose results it does not
+// use, waits at its end instead, so that its own end means the end of both.
+__device__ __forceinline__ void launch_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void launch_begin(const MafatAttnArgs& a) {
+    if (!a.overlap) launch_wait();
+    launch_next();
+}
+__device__ __forceinline__ void launch_end(const MafatAttnArgs& a) {
+    if (a.overlap) launch_wait();
+}
 
 // Maximum that keeps a NaN, so that a NaN score reaches the result.
 __device__ __forceinline__ float max_nan(float x, float y) {

@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn_rows_kernel(const __grid_con
     constexpr int kSteps = DP / 16;
     extern __shared__ __align__(128) uint8_t sm[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    mafat_attn::launch_begin(a);
     const mafat_attn::Block b(a, 16, kBN);
     const MafatAttnSeg& g = a.seg[b.seg];
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sm) + warp * C::kRing;
@@ -101,9 +102,9 @@ __global__ void __launch_bounds__(kWarps * 32) attn_rows_kernel(const __grid_con
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int r = b.row0 + lane / 4 + 8 * h;
-        limit[h] = r < g.rows ? mafat_attn::row_limit(a, g, b, r) : 0x7fffffff;
-        const __nv_bfloat16* src =
-            r < g.rows ? (const __nv_bfloat16*)a.q + mafat_attn::q_offset(a, g, b, r) : nullptr;
+        const mafat_attn::Row row(a, g, b, r);
+        limit[h] = r < g.rows ? row.limit(a, g, b) : 0x7fffffff;
+        const __nv_bfloat16* src = r < g.rows ? (const __nv_bfloat16*)a.q + row.query(a) : nullptr;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn_rows_kernel(const __grid_con
             v.z = fmaf(x, u.z, v.z);
             v.w = fmaf(x, u.w, v.w);
         }
-        const mafat_attn::Out out(a, g, b, b.row0 + r);
+        const mafat_attn::Out out(a, g, b, mafat_attn::Row(a, g, b, b.row0 + r));
         if (d == 0) mafat_attn::store_lse(a, out, top, sum);
         if (d >= a.dim) continue;
         const float inv = mafat_attn::inverse_sum(sum);
@@ -245,14 +246,14 @@ __global__ void __launch_bounds__(kWarps * 32) attn_rows_kernel(const __grid_con
         else
             *reinterpret_cast<float4*>(a.part_o + out.part * a.dim + d) = v;
     }
+    mafat_attn::launch_end(a);
 }
 
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
     int blocks = 0;
     for (int i = 0; i < a.n_seg; ++i) blocks += a.seg[i].blocks;
-    attn_rows_kernel<DP><<<blocks, kWarps * 32, Cfg<DP>::kSmem, s>>>(a);
-    return cudaGetLastError();
+    return mafat_launch_overlapped(attn_rows_kernel<DP>, blocks, kWarps * 32, Cfg<DP>::kSmem, s, a);
 }
 template <int DP>
 cudaError_t prepare() {

@@ -48,6 +48,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
     float* sk = sq + BM * L::kPitch;
     float* sv = sk + kBN * L::kPitch;
     float* sp = sv + kBN * DP;
+    mafat_attn::launch_begin(a);
     const mafat_attn::Block b(a, BM, kBN);
     const MafatAttnSeg& g = a.seg[b.seg];
     const int tx = threadIdx.x % kTX, ty = threadIdx.x / kTX;
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
             const int r = i / kChunks, c = (i % kChunks) * 4;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (c < a.dim && b.row0 + r < g.rows)
-                v = load4((const float*)a.q + mafat_attn::q_offset(a, g, b, b.row0 + r) + c);
+                v = load4((const float*)a.q + mafat_attn::Row(a, g, b, b.row0 + r).query(a) + c);
             *reinterpret_cast<float4*>(sq + r * L::kPitch + c) = v;
         }
     }
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
     float m[4], l[4], o[4][DP / kTX];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        limit[i] = mafat_attn::row_limit(a, g, b, b.row0 + ty * 4 + i);
+        limit[i] = mafat_attn::Row(a, g, b, b.row0 + ty * 4 + i).limit(a, g, b);
         m[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
         const int r = b.row0 + ty * 4 + i;
         if (r >= g.rows) continue;
         const float inv = mafat_attn::inverse_sum(l[i]);
-        const mafat_attn::Out w(a, g, b, r);
+        const mafat_attn::Out w(a, g, b, mafat_attn::Row(a, g, b, r));
 #pragma unroll
         for (int c = 0; c < DP / 64; ++c) {
             const int d = c * 64 + tx * 4;
@@ -178,14 +179,14 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
         }
         if (tx == 0) mafat_attn::store_lse(a, w, m[i], l[i]);
     }
+    mafat_attn::launch_end(a);
 }
 
 template <int BM, int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
     int blocks = 0;
     for (int i = 0; i < a.n_seg; ++i) blocks += a.seg[i].blocks;
-    attn_simt_kernel<BM, DP><<<blocks, Tile<BM, DP>::kThreads, Tile<BM, DP>::kSmem, s>>>(a);
-    return cudaGetLastError();
+    return mafat_launch_overlapped(attn_simt_kernel<BM, DP>, blocks, Tile<BM, DP>::kThreads, Tile<BM, DP>::kSmem, s, a);
 }
 template <int BM, int DP>
 cudaError_t prepare() {

@@ -8,8 +8,9 @@
 //
 // A CTA has SLOTS tiles of rows that read the same keys: while the softmax of one runs, the tensor
 // core works for the other.  Warps: 4 for each slot (thread = row), one that issues the products, one
-// that loads K and V by TMA into a ring of tiles, and one that makes the bits of readable keys for
-// tiles that have others, and zeroes the values of those: 0 x NaN would reach O.
+// that loads K and V by TMA into a ring of tiles, and one that zeroes the values past the length, since
+// 0 x NaN would reach O.  With a mask the last two and a third instead copy the readable keys alone, one
+// after another (cp.async): keys that are not readable cost no product.
 //
 // O is rescaled only where m' is more than 2^8 above the m in use (a power that cancels in O / l and
 // leaves P at most 256, well inside bf16), so that few tiles touch O outside the products.
@@ -25,7 +26,6 @@
 namespace {
 
 constexpr int kKeys = 128;
-constexpr int kWordsDepth = 8;       // tiles whose bits of readable keys are held
 constexpr float kRescaleLog2 = 8.f;
 
 template <int DP, int SLOTS>
@@ -33,6 +33,11 @@ struct Cfg {
     static constexpr int kSub = 128 * 128;                 // one 128-row x 64-channel block
     static constexpr int kTileBytes = DP / 64 * kSub;      // a tile of Q, K or V
     static constexpr int kStages = SLOTS == 2 ? (DP == 128 ? 5 : 8) : (DP == 128 ? 2 : 5);
+    // Gathered tile i is said to be there when tile i + kLag has been issued, into the stage of tile
+    // i + kLag - kStages: that one's products must not wait for tile i.  If i is K of tile j + 1, V of tile j (i - 1) is
+    // read after it, so only i - 2 and earlier will do.
+    static constexpr int kLag = kStages >= 5 ? 2 : 0;
+    static_assert(kLag <= kStages - 2, "gathered tiles");
     static constexpr int kSoftmaxWarps = 4 * SLOTS;
     static constexpr int kMmaWarp = kSoftmaxWarps, kLoadWarp = kSoftmaxWarps + 1, kMaskWarp = kSoftmaxWarps + 2;
     static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;  // whole warpgroups: the last warp is idle
@@ -45,15 +50,13 @@ struct Cfg {
     static constexpr int kOffKv = SLOTS * kTileBytes;
     static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
     static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + SLOTS,
-                         kBarQ = kBarP + SLOTS, kBarMask = kBarQ + 1, kBars = kBarMask + kWordsDepth;
-    static constexpr int kOffWords = kOffBar + (kBars * 8 + 15) / 16 * 16;
-    static constexpr int kOffTmem = kOffWords + kWordsDepth * 16;
+                         kBarQ = kBarP + SLOTS, kBarMask = kBarQ + SLOTS, kBars = kBarMask + 1;
+    static constexpr int kOffTmem = kOffBar + (kBars * 8 + 15) / 16 * 16;
     static constexpr int kOffBroken = kOffTmem + 4;
-    static constexpr int kSmem = kOffBroken + 4 + 1024;
+    static constexpr int kOffCount = kOffBroken + 4;                   // readable keys that each warp counted
+    static constexpr int kOffList = kOffCount + kThreads / 32 * 4;     // keys of two tiles, then those left over
+    static constexpr int kSmem = (kOffList + 3 * kKeys * 4 + 15) / 16 * 16 + 1024;
     static_assert(kSmem <= (SLOTS == 2 ? 232448 : 116224), "shared memory");
-    // the words of tile j are rewritten for tile j + kWordsDepth once V of that tile has landed, which needs
-    // item 2 (j + kWordsDepth) + 1 - kStages of the ring to be done
-    static_assert(kStages <= 2 * kWordsDepth - 2, "words");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -164,6 +167,9 @@ __device__ __forceinline__ void tma_tile(uint32_t el, uint32_t dst, const CUtens
         "l"(reinterpret_cast<uint64_t>(map)), "r"(c), "r"(head), "r"(key), "r"(seq), "r"(bar), "r"(el)
         : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ void expect_el(uint32_t el, uint32_t bar, uint32_t bytes) {
     asm volatile(
         "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %2, 0;\n\t"
@@ -197,15 +203,21 @@ __device__ __forceinline__ void ld_wait32(uint32_t* v) {
                  :
                  : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t t, const uint32_t* v) {
+__device__ __forceinline__ void tmem_ld16(uint32_t t, uint32_t* v) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(t),
-        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
-        "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
-        "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(t)
         : "memory");
+}
+__device__ __forceinline__ void ld_wait16(uint32_t* v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t t, const uint32_t* v) {
     asm volatile(
@@ -242,13 +254,13 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Which tiles of keys have some that are not readable: all with a mask, else the one that passes the
-// length.  The bits of the n-th such tile are in slot n % kWordsDepth.
+// The CTA's tiles of keys.  Without a mask they are runs of 128 keys, of which the last may pass the
+// length; with one they are the readable keys of its part one after another, gathered, numbered from 0.
 struct Tiles {
     int key0, n, len;
-    bool masked;
-    __device__ __forceinline__ bool partial(int j) const { return masked || key0 + (j + 1) * kKeys > len; }
-    __device__ __forceinline__ int ordinal(int j) const { return masked ? j : 0; }
+    bool gather;
+    // some keys of tile j are not readable, and their values have to be zeroed (gathered ones are)
+    __device__ __forceinline__ bool partial(int j) const { return !gather && key0 + (j + 1) * kKeys > len; }
 };
 
 template <int DP, int SLOTS>
@@ -261,33 +273,27 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     const uint32_t base = smem_u32(sm);
     const uint32_t bars = base + C::kOffBar;
     auto bar = [&](int i) { return bars + (uint32_t)i * 8u; };
-    volatile uint32_t* words = (volatile uint32_t*)(sm + C::kOffWords);
     uint32_t* tmem_slot = (uint32_t*)(sm + C::kOffTmem);
     volatile int* broken = (volatile int*)(sm + C::kOffBroken);
     const Ctl ctl{a.status, a.timeout_ns, broken};
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-
-    const mafat_attn::Block b(a, 128 * SLOTS, kKeys);
     const MafatAttnSeg& g = a.seg[0];
-    Tiles t;
-    t.key0 = b.key0;
-    t.n = b.key1 > b.key0 ? (b.key1 - b.key0 + kKeys - 1) / kKeys : 0;
-    t.len = b.len;
-    t.masked = g.mask != nullptr;
+    const bool gather = g.mask != nullptr;
 
     if (warp == C::kLoadWarp && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&kmap)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&vmap)) : "memory");
         for (int i = 0; i < C::kStages; ++i) {
-            bar_init(bar(C::kBarFull + i), 1);
-            bar_init(bar(C::kBarEmpty + i), 2);  // the products that read the tile, and the mask warp
+            // gathered tiles are filled by three warps; others by TMA, and are also looked at by the mask warp
+            bar_init(bar(C::kBarFull + i), gather ? 3 : 1);
+            bar_init(bar(C::kBarEmpty + i), gather ? 1 : 2);
         }
         for (int i = 0; i < SLOTS; ++i) {
             bar_init(bar(C::kBarS + i), 1);
             bar_init(bar(C::kBarP + i), 4);
+            bar_init(bar(C::kBarQ + i), 4);
         }
-        bar_init(bar(C::kBarQ), C::kSoftmaxWarps);
-        for (int i = 0; i < kWordsDepth; ++i) bar_init(bar(C::kBarMask + i), 1);
+        bar_init(bar(C::kBarMask), 1);
         *broken = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -298,10 +304,33 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     __syncwarp();
+    mafat_attn::launch_begin(a);
+    const mafat_attn::Block b(a, 128 * SLOTS, kKeys);
+    const uint8_t* mask = gather ? g.mask + (int64_t)b.seq * g.n : nullptr;
+    if (gather) {
+        int n = 0;
+#pragma unroll 8
+        for (int k = b.key0 + (int)threadIdx.x; k < b.key1; k += C::kThreads) n += mask[k] != 0;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) *(volatile int*)(sm + C::kOffCount + warp * 4) = n;
+    }
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = *tmem_slot;
+    Tiles t;
+    t.gather = gather;
+    t.key0 = b.key0;
+    t.len = b.len;
+    t.n = b.key1 > b.key0 ? (b.key1 - b.key0 + kKeys - 1) / kKeys : 0;
+    if (gather) {
+        int n = lane < C::kThreads / 32 ? *(volatile int*)(sm + C::kOffCount + lane * 4) : 0;
+        n = __reduce_add_sync(0xffffffffu, n);
+        t.key0 = 0;
+        t.len = n;
+        t.n = (n + kKeys - 1) / kKeys;
+    }
+    const int live = SLOTS == 2 && b.row0 + 128 < g.rows ? 2 : 1;  // slots that have rows
 
     if (warp < C::kSoftmaxWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
@@ -309,32 +338,37 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         const int row0 = b.row0 + slot * 128 + (warp % 4) * 32;  // the warp's first row
         const int row = row0 + lane;
         const bool any = row0 < g.rows && t.n > 0;
-        // queries into shared memory: 16-byte chunks, neighbouring lanes in one row
+        const mafat_attn::Row at(a, g, b, min(row, g.rows - 1));
+        uint8_t* mine = sm + slot * C::kTileBytes;  // the slot's queries; at the end, its results on their way out
+        constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
+        const int cc = lane % kChunks, cr = lane / kChunks;
         if (any) {
-            int64_t off = row < g.rows ? mafat_attn::q_offset(a, g, b, row) : -1;
-            uint8_t* dst = sm + slot * C::kTileBytes;
-            constexpr int kChunks = DP / 8, kRows = 32 / kChunks;
-#pragma unroll 4
+            const int64_t off = row < g.rows ? at.query(a) : -1;
+            uint4 v[32 / kRows];
+#pragma unroll
             for (int i = 0; i < 32 / kRows; ++i) {
-                const int r = i * kRows + lane / kChunks, c = lane % kChunks;
-                const int64_t o = __shfl_sync(0xffffffffu, off, r);
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (o >= 0 && c * 8 < a.dim) v = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + c * 8);
-                const int rr = (warp % 4) * 32 + r;
-                *reinterpret_cast<uint4*>(dst + (c / 8) * C::kSub + rr * 128 + ((c % 8) ^ (rr % 8)) * 16) = v;
+                const int64_t o = __shfl_sync(0xffffffffu, off, i * kRows + cr);
+                v[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (o >= 0 && cc * 8 < a.dim) v[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + cc * 8);
+            }
+#pragma unroll
+            for (int i = 0; i < 32 / kRows; ++i) {
+                const int r = (warp % 4) * 32 + i * kRows + cr;
+                *reinterpret_cast<uint4*>(mine + (cc / 8) * C::kSub + r * 128 + ((cc % 8) ^ (r % 8)) * 16) = v[i];
             }
             fence_async();
         }
         __syncwarp();
-        if (lane == 0) arrive(bar(C::kBarQ));
+        if (lane == 0) arrive(bar(C::kBarQ + slot));
 
         const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
         const uint32_t ts = tmem + lanes + (uint32_t)(slot * 128);
         const uint32_t to = tmem + lanes + (uint32_t)(SLOTS * 128 + slot * 128);
-        const int limit = row < g.rows ? mafat_attn::row_limit(a, g, b, row) : 0x7fffffff;
+        const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : at.limit(a, g, b);
         const float c = a.scale_log2;
+        const int n_tiles = slot < live ? t.n : 0;
         float m = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
-        for (int j = 0; j < t.n; ++j) {
+        for (int j = 0; j < n_tiles; ++j) {
             wait(bar(C::kBarS + slot), (uint32_t)j & 1u, ctl);
             __syncwarp();  // tensor memory is read by converged warps
             if (any) {
@@ -342,31 +376,13 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 uint32_t s[128];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tmem_ld32(ts + 32u * i, s + 32 * i);
-                bool part = false;
-                uint32_t w[4];
-                const int key = t.key0 + j * kKeys;
-                if (t.partial(j) || limit < key + kKeys) {
-                    w[0] = w[1] = w[2] = w[3] = 0xffffffffu;
-                    if (t.partial(j)) {
-                        const int n = t.ordinal(j);
-                        wait(bar(C::kBarMask + n % kWordsDepth), (uint32_t)(n / kWordsDepth) & 1u, ctl);
-                        __syncwarp();
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = words[(n % kWordsDepth) * 4 + i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int left = limit - key - 32 * i;  // readable by the limit
-                        if (left < 32) w[i] &= left <= 0 ? 0u : (1u << left) - 1u;
-                    }
-                    part = true;
-                }
+                const int left = limit - (t.key0 + j * kKeys);  // readable keys of the tile
 #pragma unroll
                 for (int i = 0; i < 4; ++i) ld_wait32(s + 32 * i);
-                if (part) {
+                if (left < kKeys) {
 #pragma unroll
                     for (int i = 0; i < 128; ++i)
-                        if (!(w[i / 32] >> (i % 32) & 1u)) s[i] = 0xff800000u;  // -inf
+                        if (i >= left) s[i] = 0xff800000u;  // -inf
                 }
                 float top[4];
 #pragma unroll
@@ -389,13 +405,13 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                     l0 *= keep;
                     l1 *= keep;
 #pragma unroll
-                    for (int i = 0; i < DP / 32; ++i) {
-                        uint32_t o[32];
-                        tmem_ld32(to + 32u * i, o);
-                        ld_wait32(o);
+                    for (int i = 0; i < DP / 16; ++i) {
+                        uint32_t o[16];
+                        tmem_ld16(to + 16u * i, o);
+                        ld_wait16(o);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
-                        tmem_st32(to + 32u * i, o);
+                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
+                        tmem_st16(to + 16u * i, o);
                     }
                 }
                 const float off = m == -CUDART_INF_F ? 0.f : -m * c;  // nothing readable yet: 2^-inf = 0
@@ -420,47 +436,67 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             if (lane == 0) arrive(bar(C::kBarP + slot));
         }
         const float l = l0 + l1;
-        if (t.n > 0) {
+        if (n_tiles > 0) {
             wait(bar(C::kBarS + slot), (uint32_t)t.n & 1u, ctl);
             __syncwarp();
             fence_after();
         }
         if (row0 < g.rows) {
             const float inv = mafat_attn::inverse_sum(l);
-            const mafat_attn::Out w(a, g, b, min(row, g.rows - 1));
-#pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
-                uint32_t o[32];
-                if (t.n > 0) {
-                    tmem_ld32(to + 32u * i, o);
-                    ld_wait32(o);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = 0u;
-                }
-                if (row >= g.rows) continue;
-                // a row without readable keys: 0, whatever the products left
-#pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
-                if (a.parts == 1) {
-                    __nv_bfloat16* dst = (__nv_bfloat16*)a.out + w.o + 32 * i;
-#pragma unroll
-                    for (int k = 0; k < 32; k += 8)
-                        if (32 * i + k < a.dim)
-                            *reinterpret_cast<uint4*>(dst + k) =
-                                make_uint4(pack(__uint_as_float(o[k]), __uint_as_float(o[k + 1])),
-                                           pack(__uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])),
-                                           pack(__uint_as_float(o[k + 4]), __uint_as_float(o[k + 5])),
-                                           pack(__uint_as_float(o[k + 6]), __uint_as_float(o[k + 7])));
-                } else {
-                    float* dst = a.part_o + w.part * a.dim + 32 * i;
-#pragma unroll
-                    for (int k = 0; k < 32; k += 4)
-                        if (32 * i + k < a.dim)
-                            *reinterpret_cast<uint4*>(dst + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-                }
-            }
+            const mafat_attn::Out w(a, g, b, at);
             if (row < g.rows) mafat_attn::store_lse(a, w, m, l);
+            // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in one piece:
+            // DP * 2 bytes of each row at a time, bf16 results at once, fp32 parts in two halves.
+            const bool part = a.parts > 1;
+            uint8_t* buf = mine + (warp % 4) * (C::kTileBytes / 4);
+            const int64_t dst = row >= g.rows ? -1 : part ? w.part * a.dim : w.o;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (half == 1 && !part) break;
+                const int cols = part ? DP / 2 : DP;
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i) {
+                    if (i * 16 >= cols) break;
+                    uint32_t o[16];
+                    if (t.n > 0) {
+                        tmem_ld16(to + (uint32_t)(half * (DP / 2) + 16 * i), o);
+                        ld_wait16(o);
+                    }
+                    // a row without readable keys: 0, whatever the products left
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        o[k] = t.n == 0 || l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
+                    if (part) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            *reinterpret_cast<uint4*>(buf + lane * (DP * 2) + (((4 * i + k) ^ (lane % 8)) * 16)) =
+                                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                    } else {
+                        uint32_t p[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) p[k] = pack(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            *reinterpret_cast<uint4*>(buf + lane * (DP * 2) + (((2 * i + k) ^ (lane % 8)) * 16)) =
+                                make_uint4(p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]);
+                    }
+                }
+                __syncwarp();
+                const int d = part ? half * (DP / 2) + cc * 4 : cc * 8;  // channel of the lane's chunk
+#pragma unroll
+                for (int i = 0; i < 32 / kRows; ++i) {
+                    const int r = i * kRows + cr;
+                    const int64_t o = __shfl_sync(0xffffffffu, dst, r);
+                    const uint4 v = *reinterpret_cast<const uint4*>(buf + r * (DP * 2) + ((cc ^ (r % 8)) * 16));
+                    if (o >= 0 && d < a.dim) {
+                        if (part)
+                            *reinterpret_cast<uint4*>(a.part_o + o + d) = v;
+                        else
+                            *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + o + d) = v;
+                    }
+                }
+                __syncwarp();
+            }
         }
         fence_before();
     } else {
@@ -487,10 +523,10 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                        vb + (uint32_t)k * (2048u / 16u), hi, id_o, k > 0 ? 1u : acc);
         };
         if (t.n > 0) {
-            wait(bar(C::kBarQ), 0u, ctl);
             wait(bar(C::kBarFull + 0), 0u, ctl);
-            fence_after();
-            for (int slot = 0; slot < SLOTS; ++slot) {
+            for (int slot = 0; slot < live; ++slot) {
+                wait(bar(C::kBarQ + slot), 0u, ctl);
+                fence_after();
                 scores(slot, 0u);
                 commit_el(el, bar(C::kBarS + slot));
             }
@@ -508,11 +544,9 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             for (int slot = 0; slot < SLOTS; ++slot) {
                 if (slot == 0) {
                     wait(bar(C::kBarFull) + vs * 8u, vphase, ctl);
-                    if (t.partial(j)) {
-                        const int n = t.ordinal(j);
-                        wait(bar(C::kBarMask + n % kWordsDepth), (uint32_t)(n / kWordsDepth) & 1u, ctl);
-                    }
+                    if (t.partial(j)) wait(bar(C::kBarMask), 0u, ctl);
                 }
+                if (slot >= live) break;
                 wait(bar(C::kBarP + slot), (uint32_t)j & 1u, ctl);
                 fence_after();
                 values(slot, vs, j > 0);
@@ -527,6 +561,103 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             }
             commit_el(el, bar(C::kBarEmpty) + vs * 8u);
             if (more) commit_el(el, bar(C::kBarEmpty) + ks * 8u);
+        }
+    } else if (gather) {
+        // Three warps copy the readable keys of the part, 128 at a time, as they are found: the first
+        // lists their numbers, all copy every third group of rows, and say that a tile is there once their
+        // copies have landed: when kLag more have been issued, or at once.
+        const int who = warp - C::kLoadWarp;
+        int* list = (int*)(sm + C::kOffList);  // [2][kKeys], then [kKeys] left over
+        constexpr int kChunks = DP / 8, kRows = 32 / kChunks;
+        constexpr int kSets = 8 / kRows, kGroups = (kKeys / 8 + 2) / 3;  // accesses of 8 rows; groups of 8 rows of a warp
+        const int cc = lane % kChunks, cr = lane / kChunks;
+        const __nv_bfloat16* src[2] = {
+            (const __nv_bfloat16*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh + (cc * 8 < a.dim ? cc * 8 : 0),
+            (const __nv_bfloat16*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh + (cc * 8 < a.dim ? cc * 8 : 0)};
+        const int64_t step[2] = {g.k_ss, g.v_ss};
+        uint32_t at8[kSets];  // place of the lane's chunk in a group of 8 rows
+#pragma unroll
+        for (int i = 0; i < kSets; ++i) {
+            const int r = i * kRows + cr;
+            at8[i] = (uint32_t)(cc / 8 * C::kSub + r * 128 + ((cc % 8) ^ r) * 16);
+        }
+        const bool in_dim = cc * 8 < a.dim;
+        int pos = b.key0, rest = 0;
+        uint32_t seen[4];  // the next 128 bytes of the mask
+        auto look = [&](int at) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = at + i * 32 + lane;
+                seen[i] = k < b.key1 ? mask[k] : 0u;
+            }
+        };
+        if (who == 0) look(pos);
+        uint32_t stage = 0u, phase = 1u, told = 0u;
+        int open = 0;  // tiles copied, not yet said to be there
+#pragma unroll 1
+        for (int j = 0; j < t.n; ++j) {
+            int* keys = list + (j & 1) * kKeys;
+            if (who == 0) {
+                int n = rest;
+                for (int k = lane; k < n; k += 32) keys[k] = list[2 * kKeys + k];
+                __syncwarp();
+                while (n < kKeys && pos < b.key1) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool on = seen[k] != 0u;
+                        const uint32_t bits = __ballot_sync(0xffffffffu, on);
+                        const int at = n + __popc(bits & ((1u << lane) - 1u));
+                        if (on) (at < kKeys ? keys : list + kKeys)[at] = pos + k * 32 + lane;
+                        n += __popc(bits);
+                    }
+                    pos += kKeys;
+                    look(pos);
+                }
+                rest = max(n - kKeys, 0);
+                for (int k = n + lane; k < kKeys; k += 32) keys[k] = -1;
+            }
+            asm volatile("bar.sync 1, 96;" ::: "memory");
+            int key[kGroups][kSets];
+#pragma unroll
+            for (int q = 0; q < kGroups; ++q)
+#pragma unroll
+                for (int i = 0; i < kSets; ++i) {
+                    const int r = (q * 3 + who) * 8 + i * kRows + cr;
+                    key[q][i] = r < kKeys && in_dim ? keys[r] : -1;
+                }
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                wait(bar(C::kBarEmpty) + stage * 8u, phase, ctl);
+                __syncwarp();
+                const uint32_t dst = base + C::kOffKv + stage * C::kTileBytes;
+#pragma unroll
+                for (int q = 0; q < kGroups; ++q)
+                    if (q * 3 + who < kKeys / 8)
+#pragma unroll
+                        for (int i = 0; i < kSets; ++i) {
+                            const int k = key[q][i];
+                            copy16(dst + (uint32_t)(q * 3 + who) * 1024u + at8[i],
+                                   src[kv] + (int64_t)max(k, 0) * step[kv], k >= 0);
+                        }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                ++open;
+                if (open > C::kLag) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(C::kLag) : "memory");
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) arrive(bar(C::kBarFull) + told * 8u);
+                    if (++told == (uint32_t)C::kStages) told = 0u;
+                    --open;
+                }
+                if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        fence_async();
+        __syncwarp();
+        for (; open > 0; --open) {
+            if (lane == 0) arrive(bar(C::kBarFull) + told * 8u);
+            if (++told == (uint32_t)C::kStages) told = 0u;
         }
     } else if (warp == C::kLoadWarp) {
         const uint32_t el = elect_one();
@@ -543,41 +674,22 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
         }
     } else if (warp == C::kMaskWarp) {
-        const uint8_t* mask = t.masked ? g.mask + (int64_t)b.seq * g.n : nullptr;
+        // zeroes the values past the length in the tile that has some
         uint32_t stage = 0u, phase = 0u;
 #pragma unroll 1
         for (int i = 0; i < 2 * t.n; ++i) {
-            const int j = i / 2;
-            uint32_t w[4] = {0u, 0u, 0u, 0u};
-            const bool part = (i & 1) && t.partial(j);
-            if (part) {
-                const int key = t.key0 + j * kKeys + lane;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    w[k] = __ballot_sync(0xffffffffu, key + 32 * k < t.len && (!mask || mask[key + 32 * k] != 0));
-            }
             wait(bar(C::kBarFull) + stage * 8u, phase, ctl);
-            if (part) {
-                const int n = t.ordinal(j);
-                if (lane == 0)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) words[(n % kWordsDepth) * 4 + k] = w[k];
+            __syncwarp();
+            if ((i & 1) && t.partial(i / 2)) {
                 uint8_t* v = sm + C::kOffKv + stage * C::kTileBytes;
+                for (int r = t.len - (t.key0 + (i / 2) * kKeys) + lane / 8; r < kKeys; r += 4)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (w[k] == 0xffffffffu) continue;
-                    for (int r = lane / 8; r < 32; r += 4)
-                        if (!(w[k] >> r & 1u))
-#pragma unroll
-                            for (int c = 0; c < DP / 64; ++c)
-                                *reinterpret_cast<uint4*>(v + c * C::kSub + (k * 32 + r) * 128 + (lane % 8) * 16) =
-                                    make_uint4(0u, 0u, 0u, 0u);
-                }
+                    for (int c = 0; c < DP / 64; ++c)
+                        *reinterpret_cast<uint4*>(v + c * C::kSub + r * 128 + (lane % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 fence_async();
                 __syncwarp();
-                if (lane == 0) arrive(bar(C::kBarMask + n % kWordsDepth));
+                if (lane == 0) arrive(bar(C::kBarMask));
             }
-            __syncwarp();
             if (lane == 0) arrive(bar(C::kBarEmpty) + stage * 8u);
             if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
         }
@@ -588,12 +700,13 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols));
     }
+    mafat_attn::launch_end(a);
 }
 
 template <int DP, int SLOTS>
 cudaError_t launch(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
-    attn_tc_kernel<DP, SLOTS><<<a.seg[0].blocks, Cfg<DP, SLOTS>::kThreads, Cfg<DP, SLOTS>::kSmem, s>>>(a, k, v);
-    return cudaGetLastError();
+    return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS>, a.seg[0].blocks, Cfg<DP, SLOTS>::kThreads,
+                                   Cfg<DP, SLOTS>::kSmem, s, a, k, v);
 }
 template <int DP, int SLOTS>
 cudaError_t prepare() {

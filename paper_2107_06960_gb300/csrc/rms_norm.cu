@@ -18,6 +18,7 @@ namespace {
 constexpr int kRowWarps = 4;   // rows of a block whose rows take one warp each
 constexpr int kMaxWarps = 16;  // of a row
 constexpr int kMaxThread = 32; // channels of a thread
+constexpr int kFewRows = 2048;
 constexpr float kE4m3Max = 448.f;
 
 __device__ __forceinline__ float max_nan(float x, float y) {
@@ -26,23 +27,28 @@ __device__ __forceinline__ float max_nan(float x, float y) {
     return r;
 }
 
-// V channels as one access of V elements
+// V channels as one access of V elements; loaded as they are and widened later, so that what is in
+// flight takes few registers
 template <class T, int V>
 struct Vec;
 template <>
 struct Vec<float, 4> {
-    static __device__ __forceinline__ void load(const float* p, float (&v)[4]) {
-        const float4 u = *reinterpret_cast<const float4*>(p);
-        v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    float4 u;
+    __device__ __forceinline__ void load(const float* p, bool on) {
+        u = on ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; }
     static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
         *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     }
 };
 template <>
 struct Vec<__nv_bfloat16, 8> {
-    static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[8]) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool on) {
+        u = on ? *reinterpret_cast<const uint4*>(p) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -62,12 +68,16 @@ struct Vec<__nv_bfloat16, 8> {
 };
 template <>
 struct Vec<float, 1> {
-    static __device__ __forceinline__ void load(const float* p, float (&v)[1]) { v[0] = *p; }
+    float u;
+    __device__ __forceinline__ void load(const float* p, bool on) { u = on ? *p : 0.f; }
+    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = u; }
     static __device__ __forceinline__ void store(float* p, const float (&v)[1]) { *p = v[0]; }
 };
 template <>
 struct Vec<__nv_bfloat16, 1> {
-    static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[1]) { v[0] = __bfloat162float(*p); }
+    __nv_bfloat16 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool on) { u = on ? *p : __float2bfloat16_rn(0.f); }
+    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __bfloat162float(u); }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[1]) { *p = __float2bfloat16_rn(v[0]); }
 };
 // V values in 8 bits; past the largest value the conversion saturates, a NaN stays one
@@ -90,11 +100,28 @@ __device__ __forceinline__ void store8(uint8_t* p, const float (&v)[V]) {
     }
 }
 
+// The launch may start while the one before it ends.
+__device__ __forceinline__ void launch_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 template <int WIDTH>
 __device__ __forceinline__ float max_over(float v) {
 #pragma unroll
     for (int w = 1; w < WIDTH; w *= 2) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, w));
     return v;
+}
+// v / s by the reciprocal, whose error of 2^-23 is far below a step of 8 bits; for scales so small that it
+// could overflow, by division
+template <int V>
+__device__ __forceinline__ void divide(float (&v)[V], float s) {
+    if (s < 0x1p-100f) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = v[j] / s;
+    } else {
+        const float r = 1.f / s;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] *= r;
+    }
 }
 __device__ __forceinline__ float scale_of(float top) { return top == 0.f ? 1.f : top / kE4m3Max; }
 
@@ -104,32 +131,28 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rms_norm_kernel(const __grid_c
     __shared__ float part[2][kMaxWarps];
     const int lane = threadIdx.x, warp = threadIdx.y, warps = blockDim.y;
     const int64_t row = (int64_t)blockIdx.x * blockDim.z + threadIdx.z;
-    if (row >= a.rows) return;  // only blocks whose rows take one warp each have several rows
+    if (row >= a.rows) return;  // only blocks whose rows take one warp each have several rows: no barrier follows
     const T* x = (const T*)a.x + row * a.x_s;
     const T* r = a.residual ? (const T*)a.residual + row * a.r_s : nullptr;
     const int c0 = (warp * 32 * N + lane) * V;
+    Vec<T, V> vx[N], vr[N], vw[N];
+    launch_wait();
+#pragma unroll
+    for (int i = 0; i < N; ++i) vx[i].load(x + c0 + i * 32 * V, c0 + i * 32 * V < a.cols);
+#pragma unroll
+    for (int i = 0; i < N; ++i) vr[i].load(r + c0 + i * 32 * V, r && c0 + i * 32 * V < a.cols);
+#pragma unroll
+    for (int i = 0; i < N; ++i) vw[i].load((const T*)a.weight + c0 + i * 32 * V, c0 + i * 32 * V < a.cols);
+    launch_next();
     float h[N][V];
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int c = c0 + i * 32 * V;
+        float v[V];
+        vx[i].get(h[i]);
+        vr[i].get(v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) h[i][j] = 0.f;
-        if (c < a.cols) Vec<T, V>::load(x + c, h[i]);
-    }
-    if (r) {
-        float v[N][V];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = c0 + i * 32 * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = 0.f;
-            if (c < a.cols) Vec<T, V>::load(r + c, v[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) h[i][j] += v[i][j];
+        for (int j = 0; j < V; ++j) h[i][j] += v[j];
     }
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -158,9 +181,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rms_norm_kernel(const __grid_c
     for (int i = 0; i < N; ++i) {
         const int c = c0 + i * 32 * V;
         float w[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[j] = 0.f;
-        if (c < a.cols) Vec<T, V>::load((const T*)a.weight + c, w);
+        vw[i].get(w);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             h[i][j] = h[i][j] * inv * w[j];
@@ -189,8 +210,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rms_norm_kernel(const __grid_c
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = c0 + i * 32 * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) h[i][j] = h[i][j] / s;
+            divide(h[i], s);
             if (c < a.cols) store8<V>(y + c, h[i]);
         }
     } else {
@@ -210,8 +230,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rms_norm_kernel(const __grid_c
 #pragma unroll
             for (int i = 0; i < kRuns; ++i) {
                 const int k = g * kRuns + i, c = c0 + k * 32 * V;
-#pragma unroll
-                for (int j = 0; j < V; ++j) h[k][j] = h[k][j] / s;
+                divide(h[k], s);
                 if (c < a.cols) {
                     store8<V>(y + c, h[k]);
                     if (c % 128 == 0) scales[c / 128] = s;
@@ -222,29 +241,24 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rms_norm_kernel(const __grid_c
 }
 
 template <class T, int V, int N>
-void launch(const MafatNormArgs& a, MafatNormQuant q, int warps, cudaStream_t s) {
+cudaError_t launch(const MafatNormArgs& a, MafatNormQuant q, int warps, cudaStream_t s) {
     const int rows = warps == 1 ? kRowWarps : 1;
     const dim3 block(32, warps, rows);
     const unsigned grid = (unsigned)((a.rows + rows - 1) / rows);
-    if (q == MAFAT_NORM_PLAIN)
-        rms_norm_kernel<T, V, N, MAFAT_NORM_PLAIN><<<grid, block, 0, s>>>(a);
-    else if (q == MAFAT_NORM_ROW)
-        rms_norm_kernel<T, V, N, MAFAT_NORM_ROW><<<grid, block, 0, s>>>(a);
-    else
-        rms_norm_kernel<T, V, N, MAFAT_NORM_BLOCK><<<grid, block, 0, s>>>(a);
+    return mafat_launch_overlapped(q == MAFAT_NORM_PLAIN ? rms_norm_kernel<T, V, N, MAFAT_NORM_PLAIN>
+                                   : q == MAFAT_NORM_ROW ? rms_norm_kernel<T, V, N, MAFAT_NORM_ROW>
+                                                         : rms_norm_kernel<T, V, N, MAFAT_NORM_BLOCK>,
+                                   grid, block, 0, s, a);
 }
 
-// Accesses of a thread: the fewest that leave a row to one warp; longer rows take several warps of
-// kMaxThread channels a thread.
+// Accesses of a thread: with rows enough to fill the GPU, the fewest that leave a row to one warp (no
+// barrier, more in flight a thread); with few rows as few as 16 warps allow (a row is there sooner).
 template <class T, int V, int N>
-void launch_v(const MafatNormArgs& a, MafatNormQuant q, cudaStream_t s) {
-    if constexpr (N * V <= kMaxThread) {
-        const int per_warp = 32 * V * N;
-        if (a.cols > per_warp && N * V < kMaxThread)
-            launch_v<T, V, 2 * N>(a, q, s);
-        else
-            launch<T, V, N>(a, q, (a.cols + per_warp - 1) / per_warp, s);
-    }
+cudaError_t launch_v(const MafatNormArgs& a, MafatNormQuant q, cudaStream_t s) {
+    const int per_warp = 32 * V * N;
+    if constexpr (2 * N * V <= kMaxThread)
+        if (a.cols > per_warp * (a.rows < kFewRows ? kMaxWarps : 1)) return launch_v<T, V, 2 * N>(a, q, s);
+    return launch<T, V, N>(a, q, (a.cols + per_warp - 1) / per_warp, s);
 }
 
 }  // namespace
@@ -253,16 +267,6 @@ int mafat_norm_max_cols() { return kMaxWarps * 32 * kMaxThread; }
 
 cudaError_t mafat_launch_norm(const MafatNormArgs& a, bool bf16, bool aligned, MafatNormQuant quant, cudaStream_t s) {
     // the one-element form takes 4 accesses at least: 128 channels of a warp
-    if (bf16) {
-        if (aligned)
-            launch_v<__nv_bfloat16, 8, 1>(a, quant, s);
-        else
-            launch_v<__nv_bfloat16, 1, 4>(a, quant, s);
-    } else {
-        if (aligned)
-            launch_v<float, 4, 1>(a, quant, s);
-        else
-            launch_v<float, 1, 4>(a, quant, s);
-    }
-    return cudaGetLastError();
+    if (bf16) return aligned ? launch_v<__nv_bfloat16, 8, 1>(a, quant, s) : launch_v<__nv_bfloat16, 1, 4>(a, quant, s);
+    return aligned ? launch_v<float, 4, 1>(a, quant, s) : launch_v<float, 1, 4>(a, quant, s);
 }
