@@ -7,7 +7,8 @@
 // over S in tensor memory, from where the second product reads it; nothing of S leaves the SM.
 //
 // A CTA has SLOTS tiles of rows that read the same keys: while the softmax of one runs, the tensor
-// core works for the other.  Warps: 4 for each slot (thread = row), one that issues the products, one
+// core works for the other.  Warps: 8 for each of two slots (two threads a row, each half of the keys), 4 for a
+// single one (a thread a row), one that issues the products, one
 // that loads K and V by TMA into a ring of tiles, and one that zeroes the values past the length, since
 // 0 x NaN would reach O.  With a mask the last two and a third instead copy the readable keys alone, one
 // after another (cp.async): keys that are not readable cost no product.
@@ -38,13 +39,20 @@ struct Cfg {
     // read after it, so only i - 2 and earlier will do.
     static constexpr int kLag = kStages >= 5 ? 2 : 0;
     static_assert(kLag <= kStages - 2, "gathered tiles");
-    static constexpr int kSoftmaxWarps = 4 * SLOTS;
+    // warps that share a row of scores: two halves of its keys, where the CTA has the SM to itself
+    static constexpr int kHalves = SLOTS;
+    static constexpr int kCols = kKeys / kHalves;          // scores of a thread
+    static constexpr int kSlotWarps = 4 * kHalves;
+    static constexpr int kSoftmaxWarps = kSlotWarps * SLOTS;
     static constexpr int kMmaWarp = kSoftmaxWarps, kLoadWarp = kSoftmaxWarps + 1, kMaskWarp = kSoftmaxWarps + 2;
     static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;  // whole warpgroups: the last warp is idle
     // registers of a thread: at launch (the most that the occupancy leaves), then by role
-    static constexpr int kRegs = SLOTS == 2 ? 168 : 128, kRegsSoftmax = SLOTS == 2 ? 208 : 192,
-                         kRegsOther = SLOTS == 2 ? 80 : 64;
-    static_assert(kRegsSoftmax * SLOTS + kRegsOther <= kRegs * (SLOTS + 1), "setmaxnreg draws on the launch's registers");
+    static constexpr int kRegs = SLOTS == 2 ? 96 : 128, kRegsSoftmax = SLOTS == 2 ? 96 : 192,
+                         kRegsOther = SLOTS == 2 ? 88 : 64;
+    static_assert(kRegsSoftmax * kSoftmaxWarps + kRegsOther * 4 <= kRegs * kThreads / 32,
+                  "setmaxnreg draws on the launch's registers");
+    // a row's results leave in passes of this many bytes a thread
+    static constexpr int kOutBytes = DP * 2 / kHalves;
     static constexpr int kTmemCols = 256 * SLOTS;
     // shared memory, from a 1024-byte boundary
     static constexpr int kOffKv = SLOTS * kTileBytes;
@@ -55,7 +63,8 @@ struct Cfg {
     static constexpr int kOffBroken = kOffTmem + 4;
     static constexpr int kOffCount = kOffBroken + 4;                   // readable keys that each warp counted
     static constexpr int kOffList = kOffCount + kThreads / 32 * 4;     // keys of two tiles, then those left over
-    static constexpr int kSmem = (kOffList + 3 * kKeys * 4 + 15) / 16 * 16 + 1024;
+    static constexpr int kOffShare = (kOffList + 3 * kKeys * 4 + 15) / 16 * 16;  // a value of each row, between its halves
+    static constexpr int kSmem = kOffShare + (kHalves == 2 ? SLOTS * 128 * 4 : 0);
     static_assert(kSmem <= (SLOTS == 2 ? 232448 : 116224), "shared memory");
 };
 
@@ -268,9 +277,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     attn_tc_kernel(const __grid_constant__ MafatAttnArgs a, const __grid_constant__ CUtensorMap kmap,
                    const __grid_constant__ CUtensorMap vmap) {
     using C = Cfg<DP, SLOTS>;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* sm = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) uint8_t sm[];
     const uint32_t base = smem_u32(sm);
+    if (base & 1023u) {  // the swizzled layouts need it; the declaration asks for it
+        if (threadIdx.x == 0) atomicCAS(a.status, 0u, (uint32_t)MAFAT_DEV_PIPE);
+        return;
+    }
     const uint32_t bars = base + C::kOffBar;
     auto bar = [&](int i) { return bars + (uint32_t)i * 8u; };
     uint32_t* tmem_slot = (uint32_t*)(sm + C::kOffTmem);
@@ -290,8 +302,8 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         }
         for (int i = 0; i < SLOTS; ++i) {
             bar_init(bar(C::kBarS + i), 1);
-            bar_init(bar(C::kBarP + i), 4);
-            bar_init(bar(C::kBarQ + i), 4);
+            bar_init(bar(C::kBarP + i), C::kSlotWarps);
+            bar_init(bar(C::kBarQ + i), C::kSlotWarps);
         }
         bar_init(bar(C::kBarMask), 1);
         *broken = 0;
@@ -333,27 +345,28 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     const int live = SLOTS == 2 && b.row0 + 128 < g.rows ? 2 : 1;  // slots that have rows
 
     if (warp < C::kSoftmaxWarps) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
-        const int slot = warp / 4;
-        const int row0 = b.row0 + slot * 128 + (warp % 4) * 32;  // the warp's first row
+        if constexpr (C::kRegsSoftmax > C::kRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
+        const int slot = warp / C::kSlotWarps, half = warp / 4 % C::kHalves, quarter = warp % 4;
+        const int row0 = b.row0 + slot * 128 + quarter * 32;  // the warp's first row
         const int row = row0 + lane;
         const bool any = row0 < g.rows && t.n > 0;
         const mafat_attn::Row at(a, g, b, min(row, g.rows - 1));
         uint8_t* mine = sm + slot * C::kTileBytes;  // the slot's queries; at the end, its results on their way out
-        constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
-        const int cc = lane % kChunks, cr = lane / kChunks;
         if (any) {
+            constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
+            constexpr int kLoads = 32 / kRows / C::kHalves;
+            const int cc = lane % kChunks, cr = lane / kChunks;
             const int64_t off = row < g.rows ? at.query(a) : -1;
-            uint4 v[32 / kRows];
+            uint4 v[kLoads];
 #pragma unroll
-            for (int i = 0; i < 32 / kRows; ++i) {
-                const int64_t o = __shfl_sync(0xffffffffu, off, i * kRows + cr);
+            for (int i = 0; i < kLoads; ++i) {
+                const int64_t o = __shfl_sync(0xffffffffu, off, (half * kLoads + i) * kRows + cr);
                 v[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (o >= 0 && cc * 8 < a.dim) v[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + cc * 8);
             }
 #pragma unroll
-            for (int i = 0; i < 32 / kRows; ++i) {
-                const int r = (warp % 4) * 32 + i * kRows + cr;
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = quarter * 32 + (half * kLoads + i) * kRows + cr;
                 *reinterpret_cast<uint4*>(mine + (cc / 8) * C::kSub + r * 128 + ((cc % 8) ^ (r % 8)) * 16) = v[i];
             }
             fence_async();
@@ -361,9 +374,36 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         __syncwarp();
         if (lane == 0) arrive(bar(C::kBarQ + slot));
 
-        const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
+        // the two warps that have halves of the same rows
+        const int pair = 2 + slot * 4 + quarter;
+        volatile float* share = (volatile float*)(sm + C::kOffShare) + slot * 128 + quarter * 32 + lane;
+        auto joined = [&](float x, auto op) {  // op of both halves' values, in both
+            if constexpr (C::kHalves == 2) {
+                if (half == 1) *share = x;
+                asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+                if (half == 0) *share = x = op(x, *share);
+                asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+                if (half == 1) x = *share;
+            }
+            return x;
+        };
+        auto either = [&](bool x) {  // whether it holds for a row of the warp, in either half
+            if constexpr (C::kHalves == 2) {
+                uint32_t r;
+                asm volatile(
+                    "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\t"
+                    "bar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                    : "=r"(r)
+                    : "r"(pair), "r"((uint32_t)x)
+                    : "memory");
+                return r != 0u;
+            }
+            return __any_sync(0xffffffffu, x) != 0;
+        };
+
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t ts = tmem + lanes + (uint32_t)(slot * 128);
-        const uint32_t to = tmem + lanes + (uint32_t)(SLOTS * 128 + slot * 128);
+        const uint32_t to = tmem + lanes + (uint32_t)(SLOTS * 128 + slot * 128 + half * (DP / C::kHalves));
         const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : at.limit(a, g, b);
         const float c = a.scale_log2;
         const int n_tiles = slot < live ? t.n : 0;
@@ -373,15 +413,15 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             __syncwarp();  // tensor memory is read by converged warps
             if (any) {
                 fence_after();
-                uint32_t s[128];
+                uint32_t s[C::kCols];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld32(ts + 32u * i, s + 32 * i);
-                const int left = limit - (t.key0 + j * kKeys);  // readable keys of the tile
+                for (int i = 0; i < C::kCols / 32; ++i) tmem_ld32(ts + (uint32_t)(half * C::kCols + 32 * i), s + 32 * i);
+                const int left = limit - (t.key0 + j * kKeys) - half * C::kCols;  // readable keys of the thread's
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ld_wait32(s + 32 * i);
-                if (left < kKeys) {
+                for (int i = 0; i < C::kCols / 32; ++i) ld_wait32(s + 32 * i);
+                if (left < C::kCols) {
 #pragma unroll
-                    for (int i = 0; i < 128; ++i)
+                    for (int i = 0; i < C::kCols; ++i)
                         if (i >= left) s[i] = 0xff800000u;  // -inf
                 }
                 float top[4];
@@ -389,34 +429,36 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 for (int i = 0; i < 4; ++i) {
                     top[i] = __uint_as_float(s[i]);
 #pragma unroll
-                    for (int k = i + 4; k < 128; k += 8)
-                        top[i] = k + 4 < 128 ? max3(top[i], __uint_as_float(s[k]), __uint_as_float(s[k + 4]))
-                                             : mafat_attn::max_nan(top[i], __uint_as_float(s[k]));
+                    for (int k = i + 4; k < C::kCols; k += 8)
+                        top[i] = k + 4 < C::kCols ? max3(top[i], __uint_as_float(s[k]), __uint_as_float(s[k + 4]))
+                                                  : mafat_attn::max_nan(top[i], __uint_as_float(s[k]));
                 }
-                const float mt = max3(mafat_attn::max_nan(top[0], top[1]), top[2], top[3]);
-                const float mn = mafat_attn::max_nan(m, mt);
-                // also where m is -inf and mt is not; the first tile has no O yet
-                const bool up = (mn - m) * c > kRescaleLog2;
-                if (j == 0) {
-                    m = mt;
-                } else if (__any_sync(0xffffffffu, up)) {
-                    const float keep = up ? mafat_attn::exp2_fast((m - mn) * c) : 1.f;
-                    if (up) m = mn;
-                    l0 *= keep;
-                    l1 *= keep;
+                float mt = max3(mafat_attn::max_nan(top[0], top[1]), top[2], top[3]);
+                // also where m is -inf and mt is not.  After it both halves have read their scores: P may be written over them.
+                if (either(j == 0 || (mt - m) * c > kRescaleLog2)) {
+                    mt = joined(mt, [](float x, float y) { return mafat_attn::max_nan(x, y); });
+                    if (j == 0) {
+                        m = mt;  // there is no O yet
+                    } else {
+                        const bool up = (mt - m) * c > kRescaleLog2;
+                        const float keep = up ? mafat_attn::exp2_fast((m - mt) * c) : 1.f;
+                        if (up) m = mt;
+                        l0 *= keep;
+                        l1 *= keep;
 #pragma unroll
-                    for (int i = 0; i < DP / 16; ++i) {
-                        uint32_t o[16];
-                        tmem_ld16(to + 16u * i, o);
-                        ld_wait16(o);
+                        for (int i = 0; i < DP / C::kHalves / 16; ++i) {
+                            uint32_t o[16];
+                            tmem_ld16(to + 16u * i, o);
+                            ld_wait16(o);
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
-                        tmem_st16(to + 16u * i, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * keep);
+                            tmem_st16(to + 16u * i, o);
+                        }
                     }
                 }
                 const float off = m == -CUDART_INF_F ? 0.f : -m * c;  // nothing readable yet: 2^-inf = 0
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
+                for (int h = 0; h < C::kCols / 32; ++h) {
                     uint32_t p[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
@@ -427,7 +469,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         add2(l0, l1, x, y);
                         p[i] = pack(x, y);
                     }
-                    tmem_st16(ts + 16u * h, p);
+                    tmem_st16(ts + (uint32_t)(half * (C::kCols / 2) + 16 * h), p);
                 }
                 st_wait();
                 fence_before();
@@ -435,31 +477,34 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             __syncwarp();
             if (lane == 0) arrive(bar(C::kBarP + slot));
         }
-        const float l = l0 + l1;
         if (n_tiles > 0) {
             wait(bar(C::kBarS + slot), (uint32_t)t.n & 1u, ctl);
             __syncwarp();
             fence_after();
         }
         if (row0 < g.rows) {
+            const float l = joined(l0 + l1, [](float x, float y) { return x + y; });
             const float inv = mafat_attn::inverse_sum(l);
             const mafat_attn::Out w(a, g, b, at);
-            if (row < g.rows) mafat_attn::store_lse(a, w, m, l);
-            // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in one piece:
-            // DP * 2 bytes of each row at a time, bf16 results at once, fp32 parts in two halves.
+            if (row < g.rows && half == 0) mafat_attn::store_lse(a, w, m, l);
+            // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in whole
+            // pieces: kOutBytes of each row at a time, bf16 results at once, fp32 parts in two passes.
+            constexpr int kChunks = C::kOutBytes / 16, kRows = 32 / kChunks, kSwz = kChunks < 8 ? kChunks : 8;
+            const int cc = lane % kChunks, cr = lane / kChunks;
             const bool part = a.parts > 1;
-            uint8_t* buf = mine + (warp % 4) * (C::kTileBytes / 4);
+            uint8_t* buf = mine + (quarter * C::kHalves + half) * 32 * C::kOutBytes;
             const int64_t dst = row >= g.rows ? -1 : part ? w.part * a.dim : w.o;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (half == 1 && !part) break;
-                const int cols = part ? DP / 2 : DP;
+            for (int pass = 0; pass < 2; ++pass) {
+                if (pass == 1 && !part) break;
+                constexpr int kWide = DP / C::kHalves;       // columns of the thread
+                const int cols = part ? kWide / 2 : kWide;  // of this pass
 #pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
+                for (int i = 0; i < kWide / 16; ++i) {
                     if (i * 16 >= cols) break;
                     uint32_t o[16];
                     if (t.n > 0) {
-                        tmem_ld16(to + (uint32_t)(half * (DP / 2) + 16 * i), o);
+                        tmem_ld16(to + (uint32_t)(pass * (kWide / 2) + 16 * i), o);
                         ld_wait16(o);
                     }
                     // a row without readable keys: 0, whatever the products left
@@ -469,7 +514,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                     if (part) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            *reinterpret_cast<uint4*>(buf + lane * (DP * 2) + (((4 * i + k) ^ (lane % 8)) * 16)) =
+                            *reinterpret_cast<uint4*>(buf + lane * C::kOutBytes + (((4 * i + k) ^ (lane % kSwz)) * 16)) =
                                 make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
                     } else {
                         uint32_t p[8];
@@ -477,17 +522,18 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         for (int k = 0; k < 8; ++k) p[k] = pack(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
 #pragma unroll
                         for (int k = 0; k < 2; ++k)
-                            *reinterpret_cast<uint4*>(buf + lane * (DP * 2) + (((2 * i + k) ^ (lane % 8)) * 16)) =
+                            *reinterpret_cast<uint4*>(buf + lane * C::kOutBytes + (((2 * i + k) ^ (lane % kSwz)) * 16)) =
                                 make_uint4(p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]);
                     }
                 }
                 __syncwarp();
-                const int d = part ? half * (DP / 2) + cc * 4 : cc * 8;  // channel of the lane's chunk
+                // channel of the lane's chunk
+                const int d = half * kWide + (part ? pass * (kWide / 2) + cc * 4 : cc * 8);
 #pragma unroll
                 for (int i = 0; i < 32 / kRows; ++i) {
                     const int r = i * kRows + cr;
                     const int64_t o = __shfl_sync(0xffffffffu, dst, r);
-                    const uint4 v = *reinterpret_cast<const uint4*>(buf + r * (DP * 2) + ((cc ^ (r % 8)) * 16));
+                    const uint4 v = *reinterpret_cast<const uint4*>(buf + r * C::kOutBytes + ((cc ^ (r % kSwz)) * 16));
                     if (o >= 0 && d < a.dim) {
                         if (part)
                             *reinterpret_cast<uint4*>(a.part_o + o + d) = v;
