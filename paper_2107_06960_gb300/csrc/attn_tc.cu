@@ -35,10 +35,8 @@ struct Cfg {
     static constexpr int kTileBytes = DP / 64 * kSub;      // a tile of Q, K or V
     static constexpr int kStages = SLOTS == 2 ? (DP == 128 ? 5 : 8) : (DP == 128 ? 2 : 5);
     // Gathered tile i is said to be there when tile i + kLag has been issued, into the stage of tile
-    // i + kLag - kStages: that one's products must not wait for tile i.  If i is K of tile j + 1, V of tile j (i - 1) is
-    // read after it, so only i - 2 and earlier will do.
+    // i + kLag - kStages, whose products must not wait for those of tile i.
     static constexpr int kLag = kStages >= 5 ? 2 : 0;
-    static_assert(kLag <= kStages - 2, "gathered tiles");
     // warps that share a row of scores: two halves of its keys, where the CTA has the SM to itself
     static constexpr int kHalves = SLOTS;
     static constexpr int kCols = kKeys / kHalves;          // scores of a thread
@@ -53,12 +51,19 @@ struct Cfg {
                   "setmaxnreg draws on the launch's registers");
     // a row's results leave in passes of this many bytes a thread
     static constexpr int kOutBytes = DP * 2 / kHalves;
+    // Tensor memory: buffers of 128 columns for scores and weights, then the slots' O.  Item n of the CTA
+    // (tile n / live, slot n % live) has buffer n % kBufs; with more buffers than slots a slot's next scores
+    // are there when its softmax comes to them.
     static constexpr int kTmemCols = 256 * SLOTS;
+    static constexpr int kBufs = SLOTS == 2 && DP == 64 ? 3 : SLOTS;
+    static_assert(kBufs * 128 + SLOTS * DP <= kTmemCols, "tensor memory");
     // shared memory, from a 1024-byte boundary
     static constexpr int kOffKv = SLOTS * kTileBytes;
     static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
-    static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + SLOTS,
-                         kBarQ = kBarP + SLOTS, kBarMask = kBarQ + SLOTS, kBars = kBarMask + 1;
+    static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + kBufs,
+                         kBarO = kBarP + kBufs, kBarQ = kBarO + SLOTS, kBarMask = kBarQ + SLOTS, kBars = kBarMask + 1;
+    // V of a tile is read after the scores of kBufs - 1 tiles more (one slot) or of one (two slots)
+    static_assert(kLag <= kStages - (kBufs > 2 ? 2 * kBufs - 2 : 2), "gathered tiles");
     static constexpr int kOffTmem = kOffBar + (kBars * 8 + 15) / 16 * 16;
     static constexpr int kOffBroken = kOffTmem + 4;
     static constexpr int kOffCount = kOffBroken + 4;                   // readable keys that each warp counted
@@ -301,9 +306,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             bar_init(bar(C::kBarEmpty + i), gather ? 1 : 2);
         }
         for (int i = 0; i < SLOTS; ++i) {
+            bar_init(bar(C::kBarO + i), 1);
+            bar_init(bar(C::kBarQ + i), C::kSlotWarps);
+        }
+        for (int i = 0; i < C::kBufs; ++i) {
             bar_init(bar(C::kBarS + i), 1);
             bar_init(bar(C::kBarP + i), C::kSlotWarps);
-            bar_init(bar(C::kBarQ + i), C::kSlotWarps);
         }
         bar_init(bar(C::kBarMask), 1);
         *broken = 0;
@@ -343,6 +351,9 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         t.n = (n + kKeys - 1) / kKeys;
     }
     const int live = SLOTS == 2 && b.row0 + 128 < g.rows ? 2 : 1;  // slots that have rows
+    // Scores of a slot are made before its product before them has ended: O is then waited for by a barrier
+    // of its own, else the scores' says that it is there.
+    const bool ahead = live < C::kBufs;
 
     if (warp < C::kSoftmaxWarps) {
         if constexpr (C::kRegsSoftmax > C::kRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
@@ -402,14 +413,16 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         };
 
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const uint32_t ts = tmem + lanes + (uint32_t)(slot * 128);
-        const uint32_t to = tmem + lanes + (uint32_t)(SLOTS * 128 + slot * 128 + half * (DP / C::kHalves));
+        const uint32_t to = tmem + lanes + (uint32_t)(C::kBufs * 128 + slot * DP + half * (DP / C::kHalves));
         const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : at.limit(a, g, b);
         const float c = a.scale_log2;
         const int n_tiles = slot < live ? t.n : 0;
         float m = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
+        int buf = slot;
+        uint32_t uses = 0u;  // parity of the buffer's uses
         for (int j = 0; j < n_tiles; ++j) {
-            wait(bar(C::kBarS + slot), (uint32_t)j & 1u, ctl);
+            wait(bar(C::kBarS) + (uint32_t)buf * 8u, uses, ctl);
+            const uint32_t ts = tmem + lanes + (uint32_t)(buf * 128);
             __syncwarp();  // tensor memory is read by converged warps
             if (any) {
                 fence_after();
@@ -445,6 +458,11 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         if (up) m = mt;
                         l0 *= keep;
                         l1 *= keep;
+                        if (ahead) {  // the scores were made before the product that O waits for
+                            wait(bar(C::kBarO + slot), (uint32_t)(j - 1) & 1u, ctl);
+                            __syncwarp();
+                            fence_after();
+                        }
 #pragma unroll
                         for (int i = 0; i < DP / C::kHalves / 16; ++i) {
                             uint32_t o[16];
@@ -475,10 +493,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 fence_before();
             }
             __syncwarp();
-            if (lane == 0) arrive(bar(C::kBarP + slot));
+            if (lane == 0) arrive(bar(C::kBarP) + (uint32_t)buf * 8u);
+            buf += live;
+            if (buf >= C::kBufs) buf -= C::kBufs, uses ^= 1u;
         }
         if (n_tiles > 0) {
-            wait(bar(C::kBarS + slot), (uint32_t)t.n & 1u, ctl);
+            wait(bar(C::kBarO + slot), ahead ? (uint32_t)(t.n - 1) & 1u : 0u, ctl);
             __syncwarp();
             fence_after();
         }
@@ -553,60 +573,65 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         const uint32_t q_lo = desc_lo(base, 16u), k_lo = desc_lo(base + C::kOffKv, 16u),
                        v_lo = desc_lo(base + C::kOffKv, C::kSub);
         constexpr uint32_t kTile16 = C::kTileBytes / 16, kSub16 = C::kSub / 16;
-        auto scores = [&](int slot, uint32_t stage) {
+        auto scores = [&](int slot, uint32_t stage, int buf) {
             const uint32_t qa = q_lo + (uint32_t)slot * kTile16, kb = k_lo + stage * kTile16;
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k) {
                 const uint32_t step = (uint32_t)(k / 4) * kSub16 + (uint32_t)(k % 4) * 2u;  // 32 bytes along a row
-                mma_ss(el, tmem + (uint32_t)(slot * 128), qa + step, kb + step, hi, id_s, k > 0);
+                mma_ss(el, tmem + (uint32_t)(buf * 128), qa + step, kb + step, hi, id_s, k > 0);
             }
+            commit_el(el, bar(C::kBarS) + (uint32_t)buf * 8u);
         };
-        auto values = [&](int slot, uint32_t stage, uint32_t acc) {
+        auto values = [&](int slot, uint32_t stage, int buf, uint32_t acc, bool last) {
             const uint32_t vb = v_lo + stage * kTile16;
 #pragma unroll
             for (int k = 0; k < kKeys / 16; ++k)  // 16 keys: 8 columns of P, two 8-key groups of V
-                mma_ts(el, tmem + (uint32_t)(SLOTS * 128 + slot * 128), tmem + (uint32_t)(slot * 128 + 8 * k),
+                mma_ts(el, tmem + (uint32_t)(C::kBufs * 128 + slot * DP), tmem + (uint32_t)(buf * 128 + 8 * k),
                        vb + (uint32_t)k * (2048u / 16u), hi, id_o, k > 0 ? 1u : acc);
+            commit_el(last || ahead ? el : 0u, bar(C::kBarO) + (uint32_t)slot * 8u);
         };
-        if (t.n > 0) {
-            wait(bar(C::kBarFull + 0), 0u, ctl);
-            for (int slot = 0; slot < live; ++slot) {
-                wait(bar(C::kBarQ + slot), 0u, ctl);
-                fence_after();
-                scores(slot, 0u);
-                commit_el(el, bar(C::kBarS + slot));
+        // The scores of item n + kBufs follow the values of item n: products run in the order of issue,
+        // so that its buffer is free.  Two places in the ring, each of K or V of a tile and the item's slot.
+        struct Place {
+            uint32_t stage, phase;
+            int slot, tile;
+            __device__ __forceinline__ bool next(int live) {  // true: the tile is done with
+                if (++slot < live) return false;
+                slot = 0;
+                ++tile;
+                stage += 2u;
+                if (stage >= (uint32_t)C::kStages) stage -= (uint32_t)C::kStages, phase ^= 1u;
+                return true;
             }
-            commit_el(el, bar(C::kBarEmpty + 0));
-        }
-        uint32_t stage = 1u, phase = 0u;  // of the next item of the ring: V of tile j
+        };
+        Place ps{0u, 0u, 0, 0}, pv{1u, 0u, 0, 0};
+        int bs = 0, bv = 0;
+        uint32_t uses = 0u;
+        auto next_scores = [&]() {
+            if (ps.tile >= t.n) return;
+            if (ps.slot == 0) wait(bar(C::kBarFull) + ps.stage * 8u, ps.phase, ctl);
+            if (ps.tile == 0) wait(bar(C::kBarQ) + (uint32_t)ps.slot * 8u, 0u, ctl);
+            fence_after();
+            scores(ps.slot, ps.stage, bs);
+            if (++bs == C::kBufs) bs = 0;
+            const uint32_t empty = bar(C::kBarEmpty) + ps.stage * 8u;
+            if (ps.next(live)) commit_el(el, empty);
+        };
 #pragma unroll 1
-        for (int j = 0; j < t.n; ++j) {
-            const uint32_t vs = stage, vphase = phase;
-            if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
-            const uint32_t ks = stage, kphase = phase;
-            const bool more = j + 1 < t.n;
-            if (more && ++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
-#pragma unroll
-            for (int slot = 0; slot < SLOTS; ++slot) {
-                if (slot == 0) {
-                    wait(bar(C::kBarFull) + vs * 8u, vphase, ctl);
-                    if (t.partial(j)) wait(bar(C::kBarMask), 0u, ctl);
-                }
-                if (slot >= live) break;
-                wait(bar(C::kBarP + slot), (uint32_t)j & 1u, ctl);
-                fence_after();
-                values(slot, vs, j > 0);
-                if (more) {
-                    if (slot == 0) {
-                        wait(bar(C::kBarFull) + ks * 8u, kphase, ctl);
-                        fence_after();
-                    }
-                    scores(slot, ks);
-                }
-                commit_el(el, bar(C::kBarS + slot));
+        for (int i = 0; i < C::kBufs; ++i) next_scores();
+#pragma unroll 1
+        while (pv.tile < t.n) {
+            if (pv.slot == 0) {
+                wait(bar(C::kBarFull) + pv.stage * 8u, pv.phase, ctl);
+                if (t.partial(pv.tile)) wait(bar(C::kBarMask), 0u, ctl);
             }
-            commit_el(el, bar(C::kBarEmpty) + vs * 8u);
-            if (more) commit_el(el, bar(C::kBarEmpty) + ks * 8u);
+            wait(bar(C::kBarP) + (uint32_t)bv * 8u, uses, ctl);
+            fence_after();
+            values(pv.slot, pv.stage, bv, pv.tile > 0, pv.tile == t.n - 1);
+            if (++bv == C::kBufs) bv = 0, uses ^= 1u;
+            const uint32_t empty = bar(C::kBarEmpty) + pv.stage * 8u;
+            if (pv.next(live)) commit_el(el, empty);
+            next_scores();
         }
     } else if (gather) {
         // Three warps copy the readable keys of the part, 128 at a time, as they are found: the first
