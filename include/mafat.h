@@ -487,8 +487,8 @@ mafat_status mafat_prefix_run(const mafat_attn_t* plan, const void* q, const voi
 /* What a plan chose, by set of keys.  struct_size must be set.  Host only; works on dry runs. */
 typedef struct {
     int32_t struct_size;
-    int32_t kernel[2], splits[2], blocks[2];
-    int32_t parts;              /* of a row, over both sets; more than one are joined */
+    int32_t kernel[2], splits[2], ctas[2];  /* 0 for a set without room for keys */
+    int32_t parts;              /* of a row that go through the workspace to be joined; 1: none do */
     int32_t launches_per_run;
     int64_t workspace_bytes;
 } mafat_attn_stats_t;

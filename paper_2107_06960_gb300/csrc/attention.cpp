@@ -32,7 +32,7 @@ struct AttnShape {
 struct AttnSegPlan {
     int32_t n_seq = 0, reqs = 0, n = 0, causal = 0;
     int64_t k[3] = {0, 0, 0}, v[3] = {0, 0, 0};  // strides: sequence, key, head
-    int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, blocks = 0;
+    int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, items = 0, ctas = 0;
     AttnKernel kernel = kSimtRows;
 };
 
@@ -44,7 +44,10 @@ struct mafat_attn_s {
     int64_t q[3] = {0, 0, 0}, o[3] = {0, 0, 0};
     int n_seg = 0;
     AttnSegPlan seg[2];
+    // launches: the segments that have room for keys, or the first if none has
+    int n_run = 0, run[2] = {0, 0};
     int parts = 0;
+    bool joined = false;  // the second launch joins the first one's parts with its own results
     int64_t rows_total = 0, workspace_bytes = 0;
     void* workspace = nullptr;
     float* part_o = nullptr;
@@ -153,6 +156,8 @@ AttnShape shape_of(AttnKernel k) {
 }
 bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
 
+// Most parts that a tile of many rows joins at its end: a thread reads them one after another.
+constexpr int kTileJoin = 4;
 constexpr int kFewRows = 16;  // a tile of the kernels for few rows
 bool is_rows(AttnKernel k) { return k == kSimtRows || k == kRows; }
 
@@ -180,17 +185,24 @@ int32_t choose_splits(int64_t items, int64_t tiles, int64_t slots, int setup) {
 }
 
 // The work of a segment: tiles of rows, parts of the keys.
-mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms) {
+mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms, bool second) {
     g.rows = g.reqs * p.n_q * (p.heads_q / p.heads_kv);
     g.kernel = choose_kernel(p.dtype, c.kernel, g.rows, g.n);
     const AttnShape sh = shape_of(g.kernel);
     g.row_tiles = (g.rows + sh.rows - 1) / sh.rows;
-    const int64_t items = (int64_t)g.n_seq * p.heads_kv * g.row_tiles;
+    const int64_t work = (int64_t)g.n_seq * p.heads_kv * g.row_tiles;
     const int64_t tiles = std::max<int64_t>(1, ((int64_t)g.n + sh.keys - 1) / sh.keys);
-    g.splits = c.splits ? (int32_t)std::min<int64_t>(c.splits, tiles) : choose_splits(items, tiles, (int64_t)sms * sh.ctas, sh.setup);
     if (g.n > kMaxI32 - 65536) return fail(MAFAT_EUNSUPPORTED, "too many keys");
-    if (items * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many blocks");
-    g.blocks = (int32_t)(items * g.splits);
+    if (c.splits)
+        g.splits = (int32_t)std::min<int64_t>(c.splits, tiles);
+    else if (second && (2 * work >= sms || tiles <= 8))
+        g.splits = 1;  // whole: it then joins the first launch's parts itself
+    else
+        g.splits = choose_splits(work, tiles, (int64_t)sms * sh.ctas, sh.setup);
+    if (work * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many items of work");
+    g.items = (int32_t)(work * g.splits);
+    // the kernel for few rows takes item after item
+    g.ctas = g.kernel == kRows ? std::min(g.items, sms * sh.ctas) : g.items;
     g.part0 = p.parts;
     p.parts += g.splits;
     return MAFAT_OK;
@@ -234,9 +246,17 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
         sms = sm_count(p->device);
     }
     for (int i = 0; i < p->n_seg; ++i)
-        if ((st = plan_segment(*p, p->seg[i], c, sms)) != MAFAT_OK) return st;
+        if (p->seg[i].n > 0) p->run[p->n_run++] = i;
+    if (p->n_run == 0) p->run[p->n_run++] = 0;
+    for (int i = 0; i < p->n_run; ++i)
+        if ((st = plan_segment(*p, p->seg[p->run[i]], c, sms, i > 0)) != MAFAT_OK) return st;
+    if (p->n_run == 2) {
+        const AttnSegPlan &first = p->seg[p->run[0]], &last = p->seg[p->run[1]];
+        p->joined = last.splits == 1 && first.splits <= (last.kernel == kRows ? mafat_attn_rows_join() : kTileJoin);
+        if (p->joined) p->parts = first.splits;
+    }
     const int64_t lse_bytes = (p->rows_total * p->parts * 4 + 255) / 256 * 256;
-    p->workspace_bytes = kStatusBytes + (p->parts > 1 ? lse_bytes + p->rows_total * p->parts * p->dim * 4 : 0);
+    p->workspace_bytes = kStatusBytes + (p->parts > 1 || p->joined ? lse_bytes + p->rows_total * p->parts * p->dim * 4 : 0);
     if (!p->dry_run) {
         if ((e = mafat_prepare_attn_simt()) != cudaSuccess || (e = mafat_prepare_attn_rows()) != cudaSuccess ||
             (e = mafat_prepare_attn_tc()) != cudaSuccess)
@@ -309,9 +329,10 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
     if (dev != p->device) return fail(MAFAT_EINVAL, "the current device is not the plan's");
-    for (int i = 0; i < p->n_seg; ++i) {
+    for (int r = 0; r < p->n_run; ++r) {
+        const int i = p->run[r];
         const AttnSegPlan& g = p->seg[i];
-        MafatAttnSeg& x = a.seg[0];
+        MafatAttnSeg& x = a.seg;
         x.k = d[i].k;
         x.v = d[i].v;
         x.k_sb = g.k[0]; x.k_ss = g.k[1]; x.k_sh = g.k[2];
@@ -328,9 +349,10 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         x.row_tiles_div = MafatDiv((uint32_t)g.row_tiles);
         x.splits_div = MafatDiv((uint32_t)g.splits);
         x.part0 = g.part0;
-        x.blocks = g.blocks;
-        a.n_seg = 1;
-        a.overlap = i > 0;
+        x.items = g.items;
+        a.overlap = r > 0;
+        a.join = r > 0 && p->joined ? p->parts : 0;
+        a.direct = a.join || (p->parts == 1 && !p->joined);
         if (is_tc(g.kernel)) {
             CUtensorMap k, v;
             mafat_status st;
@@ -339,11 +361,11 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
                 return st;
             e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, s);
         } else {
-            e = g.kernel == kRows ? mafat_launch_attn_rows(a, s) : mafat_launch_attn_simt(a, g.kernel == kSimtTiles, s);
+            e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, s) : mafat_launch_attn_simt(a, g.kernel == kSimtTiles, s);
         }
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }
-    if (p->parts > 1) {
+    if (p->parts > 1 && !p->joined) {
         a.overlap = 0;
         e = mafat_launch_attn_join(a, p->dtype == MAFAT_BF16, s);
         if (e != cudaSuccess) return cuda_fail(e, "join launch");
@@ -435,13 +457,14 @@ mafat_status mafat_attn_stats(const mafat_attn_t* p, mafat_attn_stats_t* out) {
     if (out->struct_size < (int32_t)sizeof(mafat_attn_stats_t)) return fail(MAFAT_EINVAL, "struct_size too small");
     mafat_attn_stats_t s{};
     s.struct_size = (int32_t)sizeof(mafat_attn_stats_t);
-    for (int i = 0; i < p->n_seg; ++i) {
+    for (int r = 0; r < p->n_run; ++r) {
+        const int i = p->run[r];
         s.kernel[i] = is_rows(p->seg[i].kernel) ? MAFAT_ATTN_ROWS : MAFAT_ATTN_TILES;
         s.splits[i] = p->seg[i].splits;
-        s.blocks[i] = p->seg[i].blocks;
+        s.ctas[i] = p->seg[i].ctas;
     }
     s.parts = p->parts;
-    s.launches_per_run = p->n_seg + (p->parts > 1 ? 1 : 0);
+    s.launches_per_run = p->n_run + (p->parts > 1 && !p->joined ? 1 : 0);
     s.workspace_bytes = p->workspace_bytes;
     *out = s;
     return MAFAT_OK;

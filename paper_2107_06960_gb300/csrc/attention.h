@@ -42,7 +42,7 @@ struct MafatAttnSeg {
     int32_t splits;
     MafatDiv row_tiles_div, splits_div;
     int32_t part0;              // first of its splits among the parts of a row
-    int32_t blocks;             // n_seq * heads_kv * splits * row_tiles
+    int32_t items;              // n_seq * heads_kv * splits * row_tiles
 };
 
 struct MafatAttnArgs {
@@ -53,18 +53,19 @@ struct MafatAttnArgs {
     int64_t o_sb, o_st, o_sh;
     int32_t n_q, group, heads_q, heads_kv, dim;
     MafatDiv n_q_div, group_div, heads_q_div, heads_kv_div;
-    int32_t parts;              // parts of a row over all segments; 1: a CTA writes the result itself
+    int32_t parts;              // parts of a row, over all segments
+    // 1: the CTA that has the row writes its result, joined with the `join` parts of an earlier launch; 0: it writes a part
+    int32_t direct, join;
     float scale_log2;           // softmax scale times log2(e)
-    int32_t n_seg;
     float* part_o;              // [parts][rows_total][dim] results of the parts, each normalised
     float* part_lse;            // [parts][rows_total] their log2 of the sum of exponentials
     int64_t rows_total;         // batch * n_q * heads_q, row index = (request * n_q + token) * heads_q + head
     // 1: an earlier launch of the same run, which has waited for what came before, is all that this one
-    // follows, and not its results: it waits at its end only, for those that join both
+    // follows: it waits for its results, or at its end for those that join both
     int32_t overlap;
     uint32_t* status;           // [2] status and abort words, as the plans' counter block starts
     int64_t timeout_ns;
-    MafatAttnSeg seg[2];
+    MafatAttnSeg seg;
 };
 
 // fp32 on the CUDA cores; `wide` tiles have 64 rows, others 16.
@@ -73,13 +74,13 @@ cudaError_t mafat_prepare_attn_simt();
 int mafat_attn_simt_rows(bool wide);
 int mafat_attn_simt_keys();
 
-// bf16, tiles of 16 rows by runs of 64 keys.
-cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, cudaStream_t s);
+// bf16, tiles of 16 rows by runs of 64 keys, ctas CTAs that take one item after another.
+cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, cudaStream_t s);
 cudaError_t mafat_prepare_attn_rows();
 int mafat_attn_rows_keys();
+int mafat_attn_rows_join();  // most parts of an earlier launch that it joins
 
-// bf16 on the tensor cores: tiles of 128 * slots rows (slots 1 or 2) by 128 keys.  Runs one segment (seg[0]);
-// the maps are 4-D over {channel, head, key, sequence}, boxes of 64 channels x 128 keys, 128-byte swizzle.
+// bf16 on the tensor cores: tiles of 128 * slots rows (slots 1 or 2) by 128 keys.  The maps are 4-D over {channel, head, key, sequence}, boxes of 64 channels x 128 keys, 128-byte swizzle.
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
                                  cudaStream_t s);
 cudaError_t mafat_prepare_attn_tc();

@@ -6,22 +6,16 @@
 
 namespace mafat_attn {
 
-// The work of one CTA.  Row tiles of one part of the keys are neighbours in the grid, so that CTAs
-// that run together read the same keys.
+// One item of work.  Row tiles of one part of the keys are neighbours, so that CTAs that run together
+// read the same keys.
 struct Block {
-    int seg, seq, head, split, row0;
+    int seq, head, split, row0;
     int len;         // readable keys of the sequence
     int key0, key1;  // its part of them: a run of whole tiles
 
     // Reads the sequence's length: after launch_begin.
-    __device__ __forceinline__ Block(const MafatAttnArgs& a, int tile_rows, int tile_keys) {
-        uint32_t i = blockIdx.x;
-        seg = 0;
-        if (i >= (uint32_t)a.seg[0].blocks) {
-            i -= (uint32_t)a.seg[0].blocks;
-            seg = 1;
-        }
-        const MafatAttnSeg& g = a.seg[seg];
+    __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows, int tile_keys) {
+        const MafatAttnSeg& g = a.seg;
         uint32_t next = g.row_tiles_div.div(i);
         row0 = (int)(i - next * (uint32_t)g.row_tiles) * tile_rows;
         i = next;
@@ -56,18 +50,18 @@ struct Block {
 struct Row {
     int64_t req;
     int t, h;
-    __device__ __forceinline__ Row(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b, int r) {
+    __device__ __forceinline__ Row(const MafatAttnArgs& a, const Block& b, int r) {
         const uint32_t u = a.group_div.div((uint32_t)r), q = a.n_q_div.div(u);
         h = b.head * a.group + (r - (int)u * a.group);
         t = (int)u - (int)q * a.n_q;
-        req = (int64_t)b.seq * g.reqs + q;
+        req = (int64_t)b.seq * a.seg.reqs + q;
     }
     __device__ __forceinline__ int64_t query(const MafatAttnArgs& a) const {
         return req * a.q_sb + (int64_t)t * a.q_st + (int64_t)h * a.q_sh;
     }
     // it sees the keys below this one
-    __device__ __forceinline__ int limit(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b) const {
-        return g.causal ? min(max(b.len - a.n_q + t + 1, 0), b.len) : b.len;
+    __device__ __forceinline__ int limit(const MafatAttnArgs& a, const Block& b) const {
+        return a.seg.causal ? min(max(b.len - a.n_q + t + 1, 0), b.len) : b.len;
     }
 };
 
@@ -77,16 +71,16 @@ struct Out {
     int64_t row;   // row among all
     int64_t part;  // row of the parts' arrays
 
-    __device__ __forceinline__ Out(const MafatAttnArgs& a, const MafatAttnSeg& g, const Block& b, const Row& r) {
+    __device__ __forceinline__ Out(const MafatAttnArgs& a, const Block& b, const Row& r) {
         o = r.req * a.o_sb + (int64_t)r.t * a.o_st + (int64_t)r.h * a.o_sh;
         row = (r.req * a.n_q + r.t) * a.heads_q + r.h;
-        part = (int64_t)(g.part0 + b.split) * a.rows_total + row;
+        part = (int64_t)(a.seg.part0 + b.split) * a.rows_total + row;
     }
 };
 
 // A launch may start while the one before it ends: it waits before it touches memory that others
 // write, then lets the next one start.  One that follows a launch of its own run, whose results it does not
-// use, waits at its end instead, so that its own end means the end of both.
+// use at first, waits for them before it joins them, or at its end, so that its own end means the end of both.
 __device__ __forceinline__ void launch_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void launch_begin(const MafatAttnArgs& a) {
@@ -118,10 +112,29 @@ __device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 
 // The row's log2 of its sum of exponentials, -inf where no key is readable.
 __device__ __forceinline__ void store_lse(const MafatAttnArgs& a, const Out& w, float m, float l) {
     const float lse2 = l == 0.f ? -CUDART_INF_F : fmaf(m, a.scale_log2, log2f(l));
-    if (a.parts > 1)
+    if (!a.direct)
         a.part_lse[w.part] = lse2;
     else if (a.lse)
         a.lse[w.row] = lse2 * CUDART_LN2_F;
 }
+
+// How a row's result is joined with its parts of an earlier launch:
+// out = own * O + sum_p 2^(lse_p - top) * inv * O_p.
+struct Join {
+    float top, own, inv;
+    __device__ __forceinline__ Join(const MafatAttnArgs& a, const Out& w, float m, float l) {
+        const float mine = l == 0.f ? -CUDART_INF_F : fmaf(m, a.scale_log2, log2f(l));
+        top = mine;
+        for (int p = 0; p < a.join; ++p) top = max_nan(top, a.part_lse[(int64_t)p * a.rows_total + w.row]);
+        if (top == -CUDART_INF_F) top = 0.f;  // no readable key anywhere: all factors are zero
+        const float x = exp2_fast(mine - top);
+        float sum = x;
+        for (int p = 0; p < a.join; ++p) sum += exp2_fast(a.part_lse[(int64_t)p * a.rows_total + w.row] - top);
+        inv = inverse_sum(sum);
+        own = l == 0.f ? 0.f : x * inv / l;
+        lse2 = sum == 0.f ? -CUDART_INF_F : top + log2f(sum);
+    }
+    float lse2;
+};
 
 }  // namespace mafat_attn

@@ -3,10 +3,11 @@
 //
 // Bound by reading K and V once: 16 rows give each 16-byte vector 16 x 16 operations, far from
 // what the tensor core could do, so the work is to keep copies in flight.  A warp has every fourth run of 16
-// keys of its CTA's part, a ring of STAGES runs of its own in shared memory (cp.async, no barrier between
-// warps) and its own running maximum, sum and O; the four are joined once, at the end.  The products
-// are the 16 x 8 x 16 ones of a single warp, whose operands are registers: S's accumulators are
-// P's operand as they are.  P is rounded to bf16 for its product; all else is fp32.
+// keys of an item's part, a ring of kStages runs of its own in shared memory (cp.async, no barrier between
+// warps) and its own running maximum, sum and O; the four are joined once, at the item's end.  A CTA
+// takes one item after another, and its copies run ahead into the next one: without that every item began with an empty
+// ring.  The products are the 16 x 8 x 16 ones of a single warp, whose operands are registers: S's
+// accumulators are P's operand as they are.  P is rounded to bf16 for its product; all else is fp32.
 //
 // Keys that are not readable are not copied but filled with zeros, so that 0 x NaN cannot reach O.
 #include <cuda_bf16.h>
@@ -16,17 +17,20 @@
 namespace {
 
 constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
 constexpr int kRun = 16;                // keys of a warp at a time
 constexpr int kBN = kWarps * kRun;
 
 template <int DP>
 struct Cfg {
-    static constexpr int kStages = DP == 128 ? 3 : 4;
+    static constexpr int kStages = DP == 128 ? 2 : 4;
     static constexpr int kMatrix = kRun * DP * 2;       // bytes of a run of K or V
     static constexpr int kRing = kStages * 2 * kMatrix;  // of a warp
-    static constexpr int kSmem = kWarps * kRing;
+    static constexpr int kOffQ = kWarps * kRing;         // queries of this item and of the next
+    static constexpr int kQ = 16 * DP * 2;
+    static constexpr int kOffJoin = kOffQ + 2 * kQ;
     static constexpr int kPitch = DP + 4;                // floats of a row of O while the warps are joined
-    static_assert(kWarps * 16 * (kPitch + 2) * 4 <= kSmem, "the join's space is the rings'");
+    static constexpr int kSmem = kOffJoin + kWarps * 16 * (kPitch + 2) * 4;
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
@@ -55,205 +59,298 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// The copying side's place: a run of an item.
+struct Ahead {
+    uint32_t item;
+    int run, runs, first, len;
+    const __nv_bfloat16 *k, *v;
+    const uint8_t* mask;
+
+    __device__ __forceinline__ void open(const MafatAttnArgs& a, int warp) {
+        run = runs = 0;
+        if (item >= (uint32_t)a.seg.items) return;
+        const MafatAttnSeg& g = a.seg;
+        const mafat_attn::Block b(a, item, 16, kBN);
+        first = b.key0 + warp * kRun;
+        runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
+        len = b.len;
+        k = (const __nv_bfloat16*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
+        v = (const __nv_bfloat16*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
+        mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
+    }
+};
+
 template <int DP>
-__global__ void __launch_bounds__(kWarps * 32) attn_rows_kernel(const __grid_constant__ MafatAttnArgs a) {
+__global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ MafatAttnArgs a) {
     using C = Cfg<DP>;
     constexpr int kChunks = DP / 8;        // 16-byte chunks of a row
+    constexpr int kRows = 32 / kChunks;    // rows of one access of a warp
     constexpr int kSteps = DP / 16;
     extern __shared__ __align__(128) uint8_t sm[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    mafat_attn::launch_begin(a);
-    const mafat_attn::Block b(a, 16, kBN);
-    const MafatAttnSeg& g = a.seg[b.seg];
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sm) + warp * C::kRing;
-    const __nv_bfloat16* kp = (const __nv_bfloat16*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
-    const __nv_bfloat16* vp = (const __nv_bfloat16*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
-    const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
-    const int first = b.key0 + warp * kRun;
-    const int runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
-
-    // run i into its stage: chunk c of key r at chunk c ^ (r % 8) of its row
-    constexpr int kRows = 32 / kChunks;  // keys of one access of the warp
+    const MafatAttnSeg& g = a.seg;
+    const uint32_t smem = (uint32_t)__cvta_generic_to_shared(sm), ring = smem + warp * C::kRing;
     const int cc = lane % kChunks, cr = lane / kChunks;
     const bool in_dim = cc * 8 < a.dim;
-    auto load = [&](int i) {
-        if (i < runs) {
-            const int key = first + i * kBN;
-            const uint32_t st = ring + (uint32_t)(i % C::kStages) * (2 * C::kMatrix);
+    mafat_attn::launch_begin(a);
+
+    // the next run into its stage: chunk c of key r at chunk c ^ (r % 8) of its row; empty past the last item
+    Ahead ld;
+    ld.item = blockIdx.x;
+    ld.open(a, warp);
+    uint32_t ld_stage = 0u, stage = 0u;
+    auto load = [&]() {
+        while (ld.run == ld.runs && ld.item < (uint32_t)g.items) {
+            ld.item += gridDim.x;
+            ld.open(a, warp);
+        }
+        if (ld.run < ld.runs) {
+            const int key = ld.first + ld.run * kBN;
+            const uint32_t st = ring + ld_stage * (2 * C::kMatrix);
 #pragma unroll
             for (int r0 = 0; r0 < kRun; r0 += kRows) {
                 const int r = r0 + cr, k = key + r;
-                const bool on = in_dim && k < b.len && (!mask || mask[k] != 0);
+                const bool on = in_dim && k < ld.len && (!ld.mask || ld.mask[k] != 0);
                 const uint32_t at = st + (uint32_t)(r * (DP * 2) + ((cc ^ (r % 8)) * 16));
-                // a place that is not read still needs an address inside the tensor
+                // a place that is not read still gets an address inside the tensor
                 const int64_t kk = on ? k : 0;
-                copy16(at, kp + (on ? kk * g.k_ss + cc * 8 : 0), on);
-                copy16(at + C::kMatrix, vp + (on ? kk * g.v_ss + cc * 8 : 0), on);
+                copy16(at, ld.k + (on ? kk * g.k_ss + cc * 8 : 0), on);
+                copy16(at + C::kMatrix, ld.v + (on ? kk * g.v_ss + cc * 8 : 0), on);
             }
+            ++ld.run;
+            if (++ld_stage == (uint32_t)C::kStages) ld_stage = 0u;
         }
         copies_done();
     };
+    // a warp's share of an item's queries, rows past the last zero
+    auto load_queries = [&](uint32_t item, uint32_t which) {
+        if (item < (uint32_t)g.items) {
+            const mafat_attn::Block b(a, item, 16, kBN);
 #pragma unroll
-    for (int i = 0; i < C::kStages - 1; ++i) load(i);
-
-    // queries: operand rows lane / 4 and lane / 4 + 8
-    uint32_t q[kSteps][4];
-    int limit[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = b.row0 + lane / 4 + 8 * h;
-        const mafat_attn::Row row(a, g, b, r);
-        limit[h] = r < g.rows ? row.limit(a, g, b) : 0x7fffffff;
-        const __nv_bfloat16* src = r < g.rows ? (const __nv_bfloat16*)a.q + row.query(a) : nullptr;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int d = s * 16 + e * 8 + (lane % 4) * 2;
-                q[s][h + 2 * e] = src && d < a.dim ? *reinterpret_cast<const uint32_t*>(src + d) : 0u;
+            for (int r0 = 0; r0 < 16 / kWarps; r0 += kRows) {
+                const int r = warp * (16 / kWarps) + r0 + cr, row = min(b.row0 + r, g.rows - 1);
+                const bool on = in_dim && b.row0 + r < g.rows;
+                const int64_t off = mafat_attn::Row(a, b, row).query(a);
+                copy16(smem + C::kOffQ + which * C::kQ + (uint32_t)(r * (DP * 2) + ((cc ^ (r % 8)) * 16)),
+                       (const __nv_bfloat16*)a.q + off + (on ? cc * 8 : 0), on);
             }
-    }
-
-    float m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
-    float o[DP / 8][4];
+        }
+    };
+    load_queries(blockIdx.x, 0u);
 #pragma unroll
-    for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+    for (int i = 0; i < C::kStages - 1; ++i) load();
+    bool waited = !a.overlap;  // for the launch whose parts are joined
 
     // ldmatrix addresses: lane 8i + j gives row j of matrix i
     const int mi = lane / 8, mj = lane % 8;
     const int k_row = (mi / 2) * 8 + mj, k_chunk = mi % 2;   // K: keys 0-7 and 8-15, each with channels 0-7 and 8-15
     const int v_row = (mi % 2) * 8 + mj, v_chunk = mi / 2;   // V: channels 0-7 and 8-15, each with keys 0-7 and 8-15
+    float* so = (float*)(sm + C::kOffJoin);
+    float* sml = so + kWarps * 16 * C::kPitch;
+
+    uint32_t which = 0u;
+#pragma unroll 1
+    for (uint32_t item = blockIdx.x; item < (uint32_t)g.items; item += gridDim.x, which ^= 1u) {
+        const mafat_attn::Block b(a, item, 16, kBN);
+        const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
+        const int first = b.key0 + warp * kRun;
+        const int runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
+        // this item's queries are there (each warp's share), and the item before is joined
+        wait_copies<0>();
+        __syncthreads();
+        uint32_t q[kSteps][4];
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t)  // rows 0-7 and 8-15 with channels 0-7, then with 8-15
+            ldm4(q[t], smem + C::kOffQ + which * C::kQ + (uint32_t)(v_row * (DP * 2) + (((2 * t + v_chunk) ^ (v_row % 8)) * 16)));
+        load_queries(item + gridDim.x, which ^ 1u);  // lands with the next run
+        int limit[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = b.row0 + lane / 4 + 8 * h;
+            limit[h] = r < g.rows ? mafat_attn::Row(a, b, r).limit(a, b) : 0x7fffffff;
+        }
+        float m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
+        float o[DP / 8][4];
+#pragma unroll
+        for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
 
 #pragma unroll 1
-    for (int i = 0; i < runs; ++i) {
-        load(i + C::kStages - 1);
-        wait_copies<C::kStages - 1>();
-        __syncwarp();
-        const int key = first + i * kBN;
-        const uint32_t st = ring + (uint32_t)(i % C::kStages) * (2 * C::kMatrix);
-        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        for (int i = 0; i < runs; ++i) {
+            load();
+            wait_copies<C::kStages - 1>();
+            __syncwarp();
+            const int key = first + i * kBN;
+            const uint32_t st = ring + stage * (2 * C::kMatrix);
+            if (++stage == (uint32_t)C::kStages) stage = 0u;
+            float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-            uint32_t f[4];
-            ldm4(f, st + (uint32_t)(k_row * (DP * 2) + (((2 * t + k_chunk) ^ (k_row % 8)) * 16)));
-            mma(s[0], q[t], f[0], f[1]);
-            mma(s[1], q[t], f[2], f[3]);
-        }
-        if (mask || key + kRun > limit[0] || key + kRun > limit[1]) {
+            for (int t = 0; t < kSteps; ++t) {
+                uint32_t f[4];
+                ldm4(f, st + (uint32_t)(k_row * (DP * 2) + (((2 * t + k_chunk) ^ (k_row % 8)) * 16)));
+                mma(s[0], q[t], f[0], f[1]);
+                mma(s[1], q[t], f[2], f[3]);
+            }
+            if (mask || key + kRun > limit[0] || key + kRun > limit[1]) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int k = key + n * 8 + (lane % 4) * 2 + e % 2;
+                        if (k >= b.len || k >= limit[e / 2] || (mask && mask[k] == 0)) s[n][e] = -CUDART_INF_F;
+                    }
+            }
+            float keep[2], off[2];
+            bool up = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float top = mafat_attn::max_nan(mafat_attn::max_nan(s[0][2 * h], s[0][2 * h + 1]),
+                                                mafat_attn::max_nan(s[1][2 * h], s[1][2 * h + 1]));
+                top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const float mn = mafat_attn::max_nan(m[h], top);
+                up = up || mn != m[h];
+                off[h] = mn == -CUDART_INF_F ? 0.f : -mn * a.scale_log2;
+                keep[h] = mafat_attn::exp2_fast(fmaf(m[h], a.scale_log2, off[h]));
+                m[h] = mn;
+            }
+            if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) l[h] *= keep[h];
+#pragma unroll
+                for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][e] *= keep[e / 2];
+            }
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int k = key + n * 8 + (lane % 4) * 2 + e % 2;
-                    if (k >= b.len || k >= limit[e / 2] || (mask && mask[k] == 0)) s[n][e] = -CUDART_INF_F;
+                    s[n][e] = mafat_attn::exp2_fast(fmaf(s[n][e], a.scale_log2, off[e / 2]));
+                    l[e / 2] += s[n][e];
                 }
+            const uint32_t p[4] = {pack(s[0][0], s[0][1]), pack(s[0][2], s[0][3]), pack(s[1][0], s[1][1]), pack(s[1][2], s[1][3])};
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) {
+                uint32_t f[4];
+                ldm4_t(f, st + C::kMatrix + (uint32_t)(v_row * (DP * 2) + (((2 * t + v_chunk) ^ (v_row % 8)) * 16)));
+                mma(o[2 * t], p, f[0], f[1]);
+                mma(o[2 * t + 1], p, f[2], f[3]);
+            }
+            __syncwarp();  // the stage is written again by a later copy
         }
-        float keep[2], off[2];
-        bool up = false;
+
+        // join the warps: O, m and l of each in shared memory
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float top = mafat_attn::max_nan(mafat_attn::max_nan(s[0][2 * h], s[0][2 * h + 1]),
-                                            mafat_attn::max_nan(s[1][2 * h], s[1][2 * h + 1]));
-            top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const float mn = mafat_attn::max_nan(m[h], top);
-            up = up || mn != m[h];
-            off[h] = mn == -CUDART_INF_F ? 0.f : -mn * a.scale_log2;
-            keep[h] = mafat_attn::exp2_fast(fmaf(m[h], a.scale_log2, off[h]));
-            m[h] = mn;
-        }
-        if (__any_sync(0xffffffffu, up)) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) l[h] *= keep[h];
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+            const int r = lane / 4 + 8 * h;
+            if (lane % 4 == 0) {
+                sml[(warp * 16 + r) * 2] = m[h];
+                sml[(warp * 16 + r) * 2 + 1] = l[h];
+            }
 #pragma unroll
             for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][e] *= keep[e / 2];
+                *reinterpret_cast<float2*>(so + (warp * 16 + r) * C::kPitch + n * 8 + (lane % 4) * 2) =
+                    make_float2(o[n][2 * h], o[n][2 * h + 1]);
         }
+        __syncthreads();
+        if (a.join && !waited) {
+            mafat_attn::launch_wait();
+            waited = true;
+        }
+        const int rows = min(16, g.rows - b.row0);
+        constexpr int kQuads = DP / 4, kSets = 32 / kQuads;  // lanes of a row; rows of a warp, and parts of a lane
+        const int d = lane % kQuads * 4;
+#pragma unroll 1
+        for (int r0 = warp * kSets; r0 < rows; r0 += kWarps * kSets) {
+            const int r = min(r0 + lane / kQuads, rows - 1);
+            const bool mine = r0 + lane / kQuads < rows;
+            float top = -CUDART_INF_F, mw[kWarps];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[n][e] = mafat_attn::exp2_fast(fmaf(s[n][e], a.scale_log2, off[e / 2]));
-                l[e / 2] += s[n][e];
+            for (int w = 0; w < kWarps; ++w) {
+                mw[w] = sml[(w * 16 + r) * 2];
+                top = mafat_attn::max_nan(top, mw[w]);
             }
-        const uint32_t p[4] = {pack(s[0][0], s[0][1]), pack(s[0][2], s[0][3]), pack(s[1][0], s[1][1]), pack(s[1][2], s[1][3])};
+            const float off = top == -CUDART_INF_F ? 0.f : -top * a.scale_log2;
+            float sum = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-            uint32_t f[4];
-            ldm4_t(f, st + C::kMatrix + (uint32_t)(v_row * (DP * 2) + (((2 * t + v_chunk) ^ (v_row % 8)) * 16)));
-            mma(o[2 * t], p, f[0], f[1]);
-            mma(o[2 * t + 1], p, f[2], f[3]);
+            for (int w = 0; w < kWarps; ++w) {
+                const float x = mafat_attn::exp2_fast(fmaf(mw[w], a.scale_log2, off));
+                sum = fmaf(x, sml[(w * 16 + r) * 2 + 1], sum);
+                const float4 u = *reinterpret_cast<const float4*>(so + (w * 16 + r) * C::kPitch + d);
+                v.x = fmaf(x, u.x, v.x);
+                v.y = fmaf(x, u.y, v.y);
+                v.z = fmaf(x, u.z, v.z);
+                v.w = fmaf(x, u.w, v.w);
+            }
+            const mafat_attn::Out out(a, b, mafat_attn::Row(a, b, b.row0 + r));
+            float inv = mafat_attn::inverse_sum(sum);
+            if (a.join) {  // with the parts of the launch before: a lane has the weight of every kQuads-th
+                const float own = sum == 0.f ? -CUDART_INF_F : fmaf(top, a.scale_log2, log2f(sum));
+                float lse[kSets], best = own;
+#pragma unroll
+                for (int k = 0; k < kSets; ++k) {
+                    const int p = k * kQuads + lane % kQuads;
+                    lse[k] = p < a.join ? a.part_lse[(int64_t)p * a.rows_total + out.row] : -CUDART_INF_F;
+                    best = mafat_attn::max_nan(best, lse[k]);
+                }
+#pragma unroll
+                for (int w = 1; w < kQuads; w *= 2) best = mafat_attn::max_nan(best, __shfl_xor_sync(0xffffffffu, best, w));
+                const float base = best == -CUDART_INF_F ? 0.f : best;
+                float total = 0.f;
+#pragma unroll
+                for (int k = 0; k < kSets; ++k) total += lse[k] = mafat_attn::exp2_fast(lse[k] - base);
+#pragma unroll
+                for (int w = 1; w < kQuads; w *= 2) total += __shfl_xor_sync(0xffffffffu, total, w);
+                const float x = mafat_attn::exp2_fast(own - base);
+                total += x;
+                inv = sum == 0.f ? 0.f : x / sum;  // then all are divided by the total
+                v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+                const float* src = a.part_o + out.row * a.dim + d;
+                // eight parts' loads on their way together
+#pragma unroll
+                for (int k = 0; k < kSets; ++k)
+#pragma unroll 1
+                    for (int p0 = k * kQuads; p0 < min((k + 1) * kQuads, a.join); p0 += 8) {
+                        float4 u[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            u[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (p0 + e < a.join && d < a.dim)
+                                u[e] = *reinterpret_cast<const float4*>(src + (int64_t)(p0 + e) * a.rows_total * a.dim);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {  // past the last part: u is zero
+                            const float f = __shfl_sync(0xffffffffu, lse[k], (lane & ~(kQuads - 1)) + (p0 + e) % kQuads);
+                            v = make_float4(fmaf(f, u[e].x, v.x), fmaf(f, u[e].y, v.y), fmaf(f, u[e].z, v.z),
+                                            fmaf(f, u[e].w, v.w));
+                        }
+                    }
+                inv = mafat_attn::inverse_sum(total);
+                if (mine && d == 0 && a.lse)
+                    a.lse[out.row] = total == 0.f ? -CUDART_INF_F : (base + log2f(total)) * CUDART_LN2_F;
+            } else if (mine && d == 0) {
+                mafat_attn::store_lse(a, out, top, sum);
+            }
+            if (!mine || d >= a.dim) continue;
+            v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+            if (a.direct)
+                *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + out.o + d) = make_uint2(pack(v.x, v.y), pack(v.z, v.w));
+            else
+                *reinterpret_cast<float4*>(a.part_o + out.part * a.dim + d) = v;
         }
-        __syncwarp();  // the stage is written again by the next iteration's copies
     }
     wait_copies<0>();
-    __syncthreads();
-
-    // join the warps: O, m and l of each in shared memory
-    float* so = (float*)sm;
-    float* sml = so + kWarps * 16 * C::kPitch;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-        const int r = lane / 4 + 8 * h;
-        if (lane % 4 == 0) {
-            sml[(warp * 16 + r) * 2] = m[h];
-            sml[(warp * 16 + r) * 2 + 1] = l[h];
-        }
-#pragma unroll
-        for (int n = 0; n < DP / 8; ++n)
-            *reinterpret_cast<float2*>(so + (warp * 16 + r) * C::kPitch + n * 8 + (lane % 4) * 2) =
-                make_float2(o[n][2 * h], o[n][2 * h + 1]);
-    }
-    __syncthreads();
-    const int rows = min(16, g.rows - b.row0);
-    constexpr int kQuads = DP / 4;
-    for (int i = threadIdx.x; i < rows * kQuads; i += kWarps * 32) {
-        const int r = i / kQuads, d = i % kQuads * 4;
-        float top = -CUDART_INF_F, mw[kWarps];
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            mw[w] = sml[(w * 16 + r) * 2];
-            top = mafat_attn::max_nan(top, mw[w]);
-        }
-        const float off = top == -CUDART_INF_F ? 0.f : -top * a.scale_log2;
-        float sum = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float x = mafat_attn::exp2_fast(fmaf(mw[w], a.scale_log2, off));
-            sum = fmaf(x, sml[(w * 16 + r) * 2 + 1], sum);
-            const float4 u = *reinterpret_cast<const float4*>(so + (w * 16 + r) * C::kPitch + d);
-            v.x = fmaf(x, u.x, v.x);
-            v.y = fmaf(x, u.y, v.y);
-            v.z = fmaf(x, u.z, v.z);
-            v.w = fmaf(x, u.w, v.w);
-        }
-        const mafat_attn::Out out(a, g, b, mafat_attn::Row(a, g, b, b.row0 + r));
-        if (d == 0) mafat_attn::store_lse(a, out, top, sum);
-        if (d >= a.dim) continue;
-        const float inv = mafat_attn::inverse_sum(sum);
-        v.x *= inv;
-        v.y *= inv;
-        v.z *= inv;
-        v.w *= inv;
-        if (a.parts == 1)
-            *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + out.o + d) = make_uint2(pack(v.x, v.y), pack(v.z, v.w));
-        else
-            *reinterpret_cast<float4*>(a.part_o + out.part * a.dim + d) = v;
-    }
     mafat_attn::launch_end(a);
 }
 
 template <int DP>
-cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
-    int blocks = 0;
-    for (int i = 0; i < a.n_seg; ++i) blocks += a.seg[i].blocks;
-    return mafat_launch_overlapped(attn_rows_kernel<DP>, blocks, kWarps * 32, Cfg<DP>::kSmem, s, a);
+cudaError_t launch(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
+    return mafat_launch_overlapped(attn_rows_kernel<DP>, (unsigned)ctas, kThreads, Cfg<DP>::kSmem, s, a);
 }
 template <int DP>
 cudaError_t prepare() {
@@ -263,9 +360,10 @@ cudaError_t prepare() {
 }  // namespace
 
 int mafat_attn_rows_keys() { return kBN; }
+int mafat_attn_rows_join() { return 32; }
 
-cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, cudaStream_t s) {
-    return a.dim <= 64 ? launch<64>(a, s) : launch<128>(a, s);
+cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
+    return a.dim <= 64 ? launch<64>(a, ctas, s) : launch<128>(a, ctas, s);
 }
 
 cudaError_t mafat_prepare_attn_rows() {

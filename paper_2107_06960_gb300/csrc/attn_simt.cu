@@ -49,8 +49,8 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
     float* sv = sk + kBN * L::kPitch;
     float* sp = sv + kBN * DP;
     mafat_attn::launch_begin(a);
-    const mafat_attn::Block b(a, BM, kBN);
-    const MafatAttnSeg& g = a.seg[b.seg];
+    const mafat_attn::Block b(a, blockIdx.x, BM, kBN);
+    const MafatAttnSeg& g = a.seg;
     const int tx = threadIdx.x % kTX, ty = threadIdx.x / kTX;
 
     // queries
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
             const int r = i / kChunks, c = (i % kChunks) * 4;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (c < a.dim && b.row0 + r < g.rows)
-                v = load4((const float*)a.q + mafat_attn::Row(a, g, b, b.row0 + r).query(a) + c);
+                v = load4((const float*)a.q + mafat_attn::Row(a, b, b.row0 + r).query(a) + c);
             *reinterpret_cast<float4*>(sq + r * L::kPitch + c) = v;
         }
     }
@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
     float m[4], l[4], o[4][DP / kTX];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        limit[i] = mafat_attn::Row(a, g, b, b.row0 + ty * 4 + i).limit(a, g, b);
+        limit[i] = mafat_attn::Row(a, b, b.row0 + ty * 4 + i).limit(a, b);
         m[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
@@ -164,29 +164,39 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
         for (int w = 1; w < kTX; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
         const int r = b.row0 + ty * 4 + i;
         if (r >= g.rows) continue;
-        const float inv = mafat_attn::inverse_sum(l[i]);
-        const mafat_attn::Out w(a, g, b, mafat_attn::Row(a, g, b, r));
+        float inv = mafat_attn::inverse_sum(l[i]), top = 0.f, scale = 0.f;
+        const mafat_attn::Out w(a, b, mafat_attn::Row(a, b, r));
+        if (a.join) {
+            mafat_attn::launch_wait();
+            const mafat_attn::Join jn(a, w, m[i], l[i]);
+            inv = jn.own;
+            top = jn.top;
+            scale = jn.inv;
+            if (tx == 0 && a.lse) a.lse[w.row] = jn.lse2 * CUDART_LN2_F;
+        } else if (tx == 0) {
+            mafat_attn::store_lse(a, w, m[i], l[i]);
+        }
 #pragma unroll
         for (int c = 0; c < DP / 64; ++c) {
             const int d = c * 64 + tx * 4;
             if (d >= a.dim) continue;
-            const float4 v = make_float4(o[i][c * 4] * inv, o[i][c * 4 + 1] * inv, o[i][c * 4 + 2] * inv,
-                                         o[i][c * 4 + 3] * inv);
-            if (a.parts == 1)
-                store4((float*)a.out + w.o + d, v);
-            else
-                store4(a.part_o + w.part * a.dim + d, v);
+            float4 v = make_float4(o[i][c * 4] * inv, o[i][c * 4 + 1] * inv, o[i][c * 4 + 2] * inv,
+                                   o[i][c * 4 + 3] * inv);
+            for (int p = 0; p < a.join; ++p) {
+                const int64_t at = (int64_t)p * a.rows_total + w.row;
+                const float f = mafat_attn::exp2_fast(a.part_lse[at] - top) * scale;
+                const float4 u = load4(a.part_o + at * a.dim + d);
+                v = make_float4(fmaf(f, u.x, v.x), fmaf(f, u.y, v.y), fmaf(f, u.z, v.z), fmaf(f, u.w, v.w));
+            }
+            store4(a.direct ? (float*)a.out + w.o + d : a.part_o + w.part * a.dim + d, v);
         }
-        if (tx == 0) mafat_attn::store_lse(a, w, m[i], l[i]);
     }
     mafat_attn::launch_end(a);
 }
 
 template <int BM, int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
-    int blocks = 0;
-    for (int i = 0; i < a.n_seg; ++i) blocks += a.seg[i].blocks;
-    return mafat_launch_overlapped(attn_simt_kernel<BM, DP>, blocks, Tile<BM, DP>::kThreads, Tile<BM, DP>::kSmem, s, a);
+    return mafat_launch_overlapped(attn_simt_kernel<BM, DP>, a.seg.items, Tile<BM, DP>::kThreads, Tile<BM, DP>::kSmem, s, a);
 }
 template <int BM, int DP>
 cudaError_t prepare() {

@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     volatile int* broken = (volatile int*)(sm + C::kOffBroken);
     const Ctl ctl{a.status, a.timeout_ns, broken};
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-    const MafatAttnSeg& g = a.seg[0];
+    const MafatAttnSeg& g = a.seg;
     const bool gather = g.mask != nullptr;
 
     if (warp == C::kLoadWarp && lane == 0) {
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     }
     __syncwarp();
     mafat_attn::launch_begin(a);
-    const mafat_attn::Block b(a, 128 * SLOTS, kKeys);
+    const mafat_attn::Block b(a, blockIdx.x, 128 * SLOTS, kKeys);
     const uint8_t* mask = gather ? g.mask + (int64_t)b.seq * g.n : nullptr;
     if (gather) {
         int n = 0;
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         const int row0 = b.row0 + slot * 128 + quarter * 32;  // the warp's first row
         const int row = row0 + lane;
         const bool any = row0 < g.rows && t.n > 0;
-        const mafat_attn::Row at(a, g, b, min(row, g.rows - 1));
+        const mafat_attn::Row at(a, b, min(row, g.rows - 1));
         uint8_t* mine = sm + slot * C::kTileBytes;  // the slot's queries; at the end, its results on their way out
         if (any) {
             constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
 
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t to = tmem + lanes + (uint32_t)(C::kBufs * 128 + slot * DP + half * (DP / C::kHalves));
-        const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : at.limit(a, g, b);
+        const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : at.limit(a, b);
         const float c = a.scale_log2;
         const int n_tiles = slot < live ? t.n : 0;
         float m = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
@@ -502,16 +502,26 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             __syncwarp();
             fence_after();
         }
+        float join_top = 0.f, join_inv = 0.f;
         if (row0 < g.rows) {
             const float l = joined(l0 + l1, [](float x, float y) { return x + y; });
-            const float inv = mafat_attn::inverse_sum(l);
-            const mafat_attn::Out w(a, g, b, at);
-            if (row < g.rows && half == 0) mafat_attn::store_lse(a, w, m, l);
+            float inv = mafat_attn::inverse_sum(l);
+            const mafat_attn::Out w(a, b, at);
+            if (a.join) {
+                mafat_attn::launch_wait();
+                const mafat_attn::Join jn(a, w, m, l);
+                inv = jn.own;
+                join_top = jn.top;
+                join_inv = jn.inv;
+                if (row < g.rows && half == 0 && a.lse) a.lse[w.row] = jn.lse2 * CUDART_LN2_F;
+            } else if (row < g.rows && half == 0) {
+                mafat_attn::store_lse(a, w, m, l);
+            }
             // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in whole
             // pieces: kOutBytes of each row at a time, bf16 results at once, fp32 parts in two passes.
             constexpr int kChunks = C::kOutBytes / 16, kRows = 32 / kChunks, kSwz = kChunks < 8 ? kChunks : 8;
             const int cc = lane % kChunks, cr = lane / kChunks;
-            const bool part = a.parts > 1;
+            const bool part = !a.direct;
             uint8_t* buf = mine + (quarter * C::kHalves + half) * 32 * C::kOutBytes;
             const int64_t dst = row >= g.rows ? -1 : part ? w.part * a.dim : w.o;
 #pragma unroll
@@ -531,6 +541,21 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
 #pragma unroll
                     for (int k = 0; k < 16; ++k)
                         o[k] = t.n == 0 || l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
+                    const int d0 = half * kWide + 16 * i;
+                    for (int p = 0; p < a.join; ++p) {
+                        const int64_t at_p = (int64_t)p * a.rows_total + w.row;
+                        const float f = mafat_attn::exp2_fast(a.part_lse[at_p] - join_top) * join_inv;
+                        const float* src = a.part_o + at_p * a.dim + d0;
+#pragma unroll
+                        for (int k = 0; k < 16; k += 4) {
+                            if (d0 + k >= a.dim) continue;
+                            const float4 v = *reinterpret_cast<const float4*>(src + k);
+                            o[k] = __float_as_uint(fmaf(f, v.x, __uint_as_float(o[k])));
+                            o[k + 1] = __float_as_uint(fmaf(f, v.y, __uint_as_float(o[k + 1])));
+                            o[k + 2] = __float_as_uint(fmaf(f, v.z, __uint_as_float(o[k + 2])));
+                            o[k + 3] = __float_as_uint(fmaf(f, v.w, __uint_as_float(o[k + 3])));
+                        }
+                    }
                     if (part) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
@@ -776,7 +801,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
 
 template <int DP, int SLOTS>
 cudaError_t launch(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
-    return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS>, a.seg[0].blocks, Cfg<DP, SLOTS>::kThreads,
+    return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS>, a.seg.items, Cfg<DP, SLOTS>::kThreads,
                                    Cfg<DP, SLOTS>::kSmem, s, a, k, v);
 }
 template <int DP, int SLOTS>

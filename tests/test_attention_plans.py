@@ -79,8 +79,19 @@ def test_splits_cover_the_keys_and_the_workspace_their_parts(mf, dtype):
                 assert s["launches_per_run"] == (1 if s["parts"] == 1 else 2)
                 rows = 2 * n_q * 8
                 assert s["workspace_bytes"] >= (rows * s["parts"] * (64 + 1) * 4 if s["parts"] > 1 else 0)
+
+
+def test_the_second_launch_joins_the_parts_where_it_has_whole_rows(mf):
     s = mf.PrefixAttention(**PREFIX).stats()
-    assert s["parts"] == sum(s["splits"]) >= 2
+    assert s["splits"][1] == 1 and s["parts"] == s["splits"][0] and s["launches_per_run"] == 2
+    assert s["workspace_bytes"] >= 6 * 8 * s["parts"] * 65 * 4
+    s = mf.PrefixAttention(**{**PREFIX, "n_own": 20000, "splits": 5}).stats()
+    assert s["splits"] == [2, 5] and s["parts"] == 7 and s["launches_per_run"] == 3
+    for empty, used in (("n_own", 0), ("n_prefix", 1)):
+        s = mf.PrefixAttention(**{**PREFIX, empty: 0, "splits": 1}).stats()
+        assert s["parts"] == 1 and s["launches_per_run"] == 1 and s["ctas"][used] > 0 and s["ctas"][1 - used] == 0
+    s = mf.PrefixAttention(**{**PREFIX, "n_own": 0, "n_prefix": 0}).stats()
+    assert s["parts"] == 1 and s["launches_per_run"] == 1
 
 
 def test_a_single_sequence_may_have_any_stride_where_it_is_not_used(mf):
