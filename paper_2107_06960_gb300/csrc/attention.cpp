@@ -21,7 +21,7 @@ void mafat_internal_clear_error();
 void* mafat_internal_encode_tiled();
 
 // A kernel and the shape of its work.
-enum AttnKernel { kSimtRows, kSimtTiles, kRows, kTc1, kTc2 };
+enum AttnKernel { kSimt8, kSimt64, kSimt128, kRows, kTc1, kTc2 };
 struct AttnShape {
     int rows, keys;  // of a CTA's tile
     int ctas;        // of an SM
@@ -33,7 +33,7 @@ struct AttnSegPlan {
     int32_t n_seq = 0, reqs = 0, n = 0, causal = 0;
     int64_t k[3] = {0, 0, 0}, v[3] = {0, 0, 0};  // strides: sequence, key, head
     int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, items = 0, ctas = 0;
-    AttnKernel kernel = kSimtRows;
+    AttnKernel kernel = kSimt8;
 };
 
 struct mafat_attn_s {
@@ -150,8 +150,9 @@ AttnShape shape_of(AttnKernel k) {
         case kRows: return {16, mafat_attn_rows_keys(), 2, 2};
         case kTc1: return {128, 128, 2, 2};
         case kTc2: return {256, 128, 1, 2};
-        case kSimtTiles: return {mafat_attn_simt_rows(true), mafat_attn_simt_keys(), 1, 1};
-        default: return {mafat_attn_simt_rows(false), mafat_attn_simt_keys(), 2, 1};
+        case kSimt128: return {128, mafat_attn_simt_keys(), 1, 2};
+        case kSimt64: return {64, mafat_attn_simt_keys(), 1, 2};
+        default: return {8, mafat_attn_simt_keys(), 1, 2};
     }
 }
 bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
@@ -159,11 +160,11 @@ bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
 // Most parts that a tile of many rows joins at its end: a thread reads them one after another.
 constexpr int kTileJoin = 4;
 constexpr int kFewRows = 16;  // a tile of the kernels for few rows
-bool is_rows(AttnKernel k) { return k == kSimtRows || k == kRows; }
+bool is_rows(AttnKernel k) { return k == kSimt8 || k == kRows; }
 
 AttnKernel choose_kernel(int32_t dtype, int32_t asked, int32_t rows, int32_t n) {
     const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= kFewRows);
-    if (dtype == MAFAT_FP32) return few ? kSimtRows : kSimtTiles;
+    if (dtype == MAFAT_FP32) return few ? kSimt8 : rows <= 64 ? kSimt64 : kSimt128;
     if (few || n == 0) return kRows;  // without keys there is nothing to map
     return rows <= 128 ? kTc1 : kTc2;
 }
@@ -361,7 +362,7 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
                 return st;
             e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, s);
         } else {
-            e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, s) : mafat_launch_attn_simt(a, g.kernel == kSimtTiles, s);
+            e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, s) : mafat_launch_attn_simt(a, shape_of(g.kernel).rows, s);
         }
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }

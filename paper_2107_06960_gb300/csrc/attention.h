@@ -68,10 +68,9 @@ struct MafatAttnArgs {
     MafatAttnSeg seg;
 };
 
-// fp32 on the CUDA cores; `wide` tiles have 64 rows, others 16.
-cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, bool wide, cudaStream_t s);
+// fp32 on the CUDA cores, tiles of 8, 64 or 128 rows.
+cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s);
 cudaError_t mafat_prepare_attn_simt();
-int mafat_attn_simt_rows(bool wide);
 int mafat_attn_simt_keys();
 
 // bf16, tiles of 16 rows by runs of 64 keys, ctas CTAs that take one item after another.

@@ -1,17 +1,103 @@
 // Attention in fp32 on the CUDA cores, for fp32 plans.
 //
-// For a row with query q and readable keys s:  O = sum_s exp(c q.k_s) v_s / sum_s exp(c q.k_s).
-// A CTA takes BM rows of one (sequence, key head) and one part of its keys, 64 keys at a time, and
-// keeps for each row the running maximum m of q.k_s, the sum l and the unnormalised O, all fp32:
-// a tile's scores raise m to m', and l and O are multiplied by 2^(c' (m - m')), c' = c log2(e).
+// For a row with query q and readable keys s:  O = sum_s exp(c q.k_s) v_s / sum_s exp(c q.k_s), with
+// the running maximum m of q.k_s, the sum l and the unnormalised O of each row, all fp32: a tile's scores
+// raise m to m', and l and O are multiplied by 2^(c' (m - m')), c' = c log2(e).
 //
-// A thread owns 4 rows x 4 keys of the scores and 4 rows x 2 quarters of the channels of O, so that a
-// 16-byte shared-memory read feeds 8 FMAs; K's and V's tiles are single buffers.
+// Two neighbouring products are one packed instruction (fma.rn.f32x2, each rounded as alone), which
+// leaves issue slots to the shared-memory reads.  Keys that are not readable are filled with zeros as they
+// are copied (cp.async), so that 0 x NaN cannot reach O.
+//
+// Many rows (attn_simt_kernel): bound by FMAs and, close behind, by shared-memory reads (83 % of their rate with
+// 60 % of the FMAs').  A CTA takes BM rows, 64 keys at a time; a thread has 4 rows x 4 keys of the scores, then 4
+// rows x DP / 16 channels of O.  K's and V's tiles are single buffers: the next K is copied while the
+// values are summed, the next V while the scores are made.  A warp with 16 rows x 64 keys (queries and
+// weights broadcast, fewer reads an FMA, 8 warps instead of 16) was 4 % slower.
+//
+// Few rows (attn_simt_few_kernel): bound by reading K and V.  The warps of a CTA share the R rows and split the
+// keys, each with a ring of runs of 16 keys of its own and its own m, l and O, joined at the end.
 #include "attn_common.cuh"
 
 namespace {
 
 constexpr int kBN = 64;
+
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+
+__device__ __forceinline__ void copy16(float* dst, const float* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+                 "r"(on ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// r += a * b, two values at once
+__device__ __forceinline__ void fma2(float2& r, float2 a, float2 b) {
+    asm("{\n\t.reg .b64 x, y, z;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%0, %1};\n\t"
+        "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "+f"(r.x), "+f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+}
+
+// One row's share of the online softmax for the N scores of a lane, whose warp has the row's others:
+// s becomes the weights; returns the factor of what was summed before.
+template <int N>
+__device__ __forceinline__ float softmax_step(float (&s)[N], float& m, float& l, float scale_log2) {
+    float top = s[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) top = mafat_attn::max_nan(top, s[j]);
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, w));
+    const float mn = mafat_attn::max_nan(m, top);
+    const float base = mn == -INFINITY ? 0.f : mn * scale_log2;  // no readable key yet: 2^-inf = 0
+    const float keep = mafat_attn::exp2_fast(fmaf(m, scale_log2, -base));
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        s[j] = mafat_attn::exp2_fast(fmaf(s[j], scale_log2, -base));
+        sum += s[j];
+    }
+    l = l * keep + sum;  // of the lane's keys
+    return keep;
+}
+
+// Writes a row's four channels from d, joined with the parts of the launch before.
+struct Writer {
+    mafat_attn::Out at;
+    float own, top, inv;
+    __device__ __forceinline__ Writer(const MafatAttnArgs& a, const mafat_attn::Block& b, int r, float m, float l, bool first)
+        : at(a, b, mafat_attn::Row(a, b, r)), own(mafat_attn::inverse_sum(l)), top(0.f), inv(0.f) {
+        if (a.join) {
+            mafat_attn::launch_wait();
+            const mafat_attn::Join jn(a, at, m, l);
+            own = jn.own;
+            top = jn.top;
+            inv = jn.inv;
+            if (first && a.lse) a.lse[at.row] = jn.lse2 * CUDART_LN2_F;
+        } else if (first) {
+            mafat_attn::store_lse(a, at, m, l);
+        }
+    }
+    __device__ __forceinline__ void put(const MafatAttnArgs& a, int d, float4 v) const {
+        if (d >= a.dim) return;
+        v = make_float4(v.x * own, v.y * own, v.z * own, v.w * own);
+        for (int p = 0; p < a.join; ++p) {
+            const int64_t row = (int64_t)p * a.rows_total + at.row;
+            const float f = mafat_attn::exp2_fast(a.part_lse[row] - top) * inv;
+            const float4 u = load4(a.part_o + row * a.dim + d);
+            v = make_float4(fmaf(f, u.x, v.x), fmaf(f, u.y, v.y), fmaf(f, u.z, v.z), fmaf(f, u.w, v.w));
+        }
+        store4(a.direct ? (float*)a.out + at.o + d : a.part_o + at.part * a.dim + d, v);
+    }
+};
+
+// ---- many rows --------------------------------------------------------------------------------
+
 constexpr int kTX = 16;  // threads along the keys / channels
 
 template <int BM, int DP>
@@ -23,21 +109,18 @@ struct Tile {
     static constexpr int kSmem = kFloats * 4;
 };
 
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-
-// rows [0, count) of a matrix with `stride` elements between rows into smem; channels past dim and
-// rows that are not readable become zero
+// copies ROWS rows of a matrix with `stride` elements between rows; channels past dim and rows that
+// are not readable become zero
 template <int ROWS, int DP, int PITCH, int THREADS, class Ok>
-__device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t stride, int dim, Ok ok) {
+__device__ __forceinline__ void copy_rows(float* dst, const float* src, int64_t stride, int dim, Ok ok) {
     constexpr int kChunks = DP / 4;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = threadIdx.x; i < ROWS * kChunks; i += THREADS) {
         const int r = i / kChunks, c = (i % kChunks) * 4;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < dim && ok(r)) v = load4(src + (int64_t)r * stride + c);
-        *reinterpret_cast<float4*>(dst + r * PITCH + c) = v;
+        const bool on = c < dim && ok(r);
+        copy16(dst + r * PITCH + c, src + (on ? (int64_t)r * stride + c : 0), on);
     }
+    copies_done();
 }
 
 template <int BM, int DP>
@@ -52,70 +135,85 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
     const mafat_attn::Block b(a, blockIdx.x, BM, kBN);
     const MafatAttnSeg& g = a.seg;
     const int tx = threadIdx.x % kTX, ty = threadIdx.x / kTX;
+    const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
+    const float* vp = (const float*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
+    const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
+    auto copy_k = [&](int key0) {
+        copy_rows<kBN, DP, L::kPitch, L::kThreads>(sk, kp + (int64_t)key0 * g.k_ss, g.k_ss, a.dim, [&](int r) {
+            return key0 + r < b.len && (!mask || mask[key0 + r] != 0);
+        });
+    };
+    auto copy_v = [&](int key0) {
+        copy_rows<kBN, DP, DP, L::kThreads>(sv, vp + (int64_t)key0 * g.v_ss, g.v_ss, a.dim, [&](int r) {
+            return key0 + r < b.len && (!mask || mask[key0 + r] != 0);
+        });
+    };
 
-    // queries
+    // queries, then the first keys
     {
         constexpr int kChunks = DP / 4;
+#pragma unroll 4
         for (int i = threadIdx.x; i < BM * kChunks; i += L::kThreads) {
             const int r = i / kChunks, c = (i % kChunks) * 4;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (c < a.dim && b.row0 + r < g.rows)
-                v = load4((const float*)a.q + mafat_attn::Row(a, b, b.row0 + r).query(a) + c);
-            *reinterpret_cast<float4*>(sq + r * L::kPitch + c) = v;
+            const bool on = c < a.dim && b.row0 + r < g.rows;
+            copy16(sq + r * L::kPitch + c,
+                   (const float*)a.q + (on ? mafat_attn::Row(a, b, b.row0 + r).query(a) + c : 0), on);
         }
+        if (b.key0 < b.key1) copy_k(b.key0);
+        copies_done();
     }
+    constexpr int kO = DP / kTX / 2;  // pairs of channels: c * 64 + tx * 4 + {0, 1}, {2, 3}
     int limit[4];
-    float m[4], l[4], o[4][DP / kTX];
+    float m[4], l[4];
+    float2 o[4][kO];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         limit[i] = mafat_attn::Row(a, b, b.row0 + ty * 4 + i).limit(a, b);
         m[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
-        for (int d = 0; d < DP / kTX; ++d) o[i][d] = 0.f;
+        for (int d = 0; d < kO; ++d) o[i][d] = make_float2(0.f, 0.f);
     }
-    const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
-    const float* vp = (const float*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
-    const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
 
+#pragma unroll 1
     for (int key0 = b.key0; key0 < b.key1; key0 += kBN) {
-        auto ok = [&](int r) { return key0 + r < b.len && (!mask || mask[key0 + r] != 0); };
-        __syncthreads();
-        load_rows<kBN, DP, L::kPitch, L::kThreads>(sk, kp + (int64_t)key0 * g.k_ss, g.k_ss, a.dim, ok);
-        load_rows<kBN, DP, DP, L::kThreads>(sv, vp + (int64_t)key0 * g.v_ss, g.v_ss, a.dim, ok);
-        __syncthreads();
-        float s[4][4];
+        wait_copies<0>();
+        __syncthreads();  // K is there, and all are done with V
+        copy_v(key0);
+        float2 acc[4][4];  // sums over even and odd channels
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+            for (int j = 0; j < 4; ++j) acc[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
         for (int d = 0; d < DP; d += 4) {
             float4 x[4], y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(sq + (ty * 4 + i) * L::kPitch + d);
+            for (int i = 0; i < 4; ++i) x[i] = load4(sq + (ty * 4 + i) * L::kPitch + d);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(sk + (tx + kTX * j) * L::kPitch + d);
+            for (int j = 0; j < 4; ++j) y[j] = load4(sk + (tx + kTX * j) * L::kPitch + d);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[i][j] = fmaf(x[i].x, y[j].x, s[i][j]);
-                    s[i][j] = fmaf(x[i].y, y[j].y, s[i][j]);
-                    s[i][j] = fmaf(x[i].z, y[j].z, s[i][j]);
-                    s[i][j] = fmaf(x[i].w, y[j].w, s[i][j]);
+                    fma2(acc[i][j], make_float2(x[i].x, x[i].y), make_float2(y[j].x, y[j].y));
+                    fma2(acc[i][j], make_float2(x[i].z, x[i].w), make_float2(y[j].z, y[j].w));
                 }
         }
         bool seen[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) seen[j] = ok(tx + kTX * j);
+        for (int j = 0; j < 4; ++j) {
+            const int k = key0 + tx + kTX * j;
+            seen[j] = k < b.len && (!mask || mask[k] != 0);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float top = -INFINITY;
+            float s[4], top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (!seen[j] || key0 + tx + kTX * j >= limit[i]) s[i][j] = -INFINITY;
-                top = mafat_attn::max_nan(top, s[i][j]);
+                s[j] = acc[i][j].x + acc[i][j].y;
+                if (!seen[j] || key0 + tx + kTX * j >= limit[i]) s[j] = -INFINITY;
+                top = mafat_attn::max_nan(top, s[j]);
             }
 #pragma unroll
             for (int w = 1; w < kTX; w *= 2) top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, w));
@@ -126,97 +224,253 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                s[i][j] = mafat_attn::exp2_fast(fmaf(s[i][j], a.scale_log2, -base));
-                sum += s[i][j];
-                sp[(ty * 4 + i) * L::kPPitch + tx + kTX * j] = s[i][j];
+                s[j] = mafat_attn::exp2_fast(fmaf(s[j], a.scale_log2, -base));
+                sum += s[j];
+                sp[(ty * 4 + i) * L::kPPitch + tx + kTX * j] = s[j];
             }
             l[i] = l[i] * keep + sum;
 #pragma unroll
-            for (int d = 0; d < DP / kTX; ++d) o[i][d] *= keep;
+            for (int d = 0; d < kO; ++d) o[i][d] = make_float2(o[i][d].x * keep, o[i][d].y * keep);
         }
-        __syncwarp();  // a row's scores are written and read by the 16 threads of one half warp
+        wait_copies<0>();
+        __syncthreads();  // V is there, and all are done with K (P is read by the half warp that wrote it)
+        if (key0 + kBN < b.key1) copy_k(key0 + kBN);
 #pragma unroll 2
         for (int k = 0; k < kBN; k += 4) {
             float4 p[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(sp + (ty * 4 + i) * L::kPPitch + k);
+            for (int i = 0; i < 4; ++i) p[i] = load4(sp + (ty * 4 + i) * L::kPPitch + k);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
 #pragma unroll
                 for (int c = 0; c < DP / 64; ++c) {
-                    const float4 v = *reinterpret_cast<const float4*>(sv + (k + e) * DP + c * 64 + tx * 4);
+                    const float4 v = load4(sv + (k + e) * DP + c * 64 + tx * 4);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float w = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
-                        o[i][c * 4 + 0] = fmaf(w, v.x, o[i][c * 4 + 0]);
-                        o[i][c * 4 + 1] = fmaf(w, v.y, o[i][c * 4 + 1]);
-                        o[i][c * 4 + 2] = fmaf(w, v.z, o[i][c * 4 + 2]);
-                        o[i][c * 4 + 3] = fmaf(w, v.w, o[i][c * 4 + 3]);
+                        fma2(o[i][2 * c], make_float2(w, w), make_float2(v.x, v.y));
+                        fma2(o[i][2 * c + 1], make_float2(w, w), make_float2(v.z, v.w));
                     }
                 }
             }
         }
-        __syncwarp();
     }
+    wait_copies<0>();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
         for (int w = 1; w < kTX; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
         const int r = b.row0 + ty * 4 + i;
         if (r >= g.rows) continue;
-        float inv = mafat_attn::inverse_sum(l[i]), top = 0.f, scale = 0.f;
-        const mafat_attn::Out w(a, b, mafat_attn::Row(a, b, r));
-        if (a.join) {
-            mafat_attn::launch_wait();
-            const mafat_attn::Join jn(a, w, m[i], l[i]);
-            inv = jn.own;
-            top = jn.top;
-            scale = jn.inv;
-            if (tx == 0 && a.lse) a.lse[w.row] = jn.lse2 * CUDART_LN2_F;
-        } else if (tx == 0) {
-            mafat_attn::store_lse(a, w, m[i], l[i]);
+        const Writer w(a, b, r, m[i], l[i], tx == 0);
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c)
+            w.put(a, c * 64 + tx * 4, make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y));
+    }
+    mafat_attn::launch_end(a);
+}
+
+// ---- few rows -----------------------------------------------------------------------------------
+
+constexpr int kFewWarps = 4, kRun = 16;  // keys of a warp at a time
+
+template <int R, int DP>
+struct Few {
+    static constexpr int kThreads = kFewWarps * 32;
+    static constexpr int kStages = DP == 128 ? 3 : 4;
+    static constexpr int kPitch = DP + 4;
+    static constexpr int kStage = kRun * (kPitch + DP);               // floats of a run of K and V
+    static constexpr int kWarp = kStages * kStage + R * kRun;         // and the weights
+    static constexpr int kSmem = (R * DP + kFewWarps * kWarp) * 4;
+    static_assert(kFewWarps * R * (DP + 2) <= kFewWarps * kWarp, "the join's space is the rings'");
+};
+
+template <int R, int DP>
+__global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __grid_constant__ MafatAttnArgs a) {
+    using L = Few<R, DP>;
+    constexpr int kCh = DP / 32;
+    extern __shared__ __align__(16) float sm[];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    float* sq = sm;
+    float* ring = sm + R * DP + warp * L::kWarp;
+    float* sp = ring + L::kStages * L::kStage;
+    mafat_attn::launch_begin(a);
+    const mafat_attn::Block b(a, blockIdx.x, R, kBN);
+    const MafatAttnSeg& g = a.seg;
+    const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
+    const float* vp = (const float*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
+    const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
+    const int first = b.key0 + warp * kRun;
+    const int runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
+    constexpr int kChunks = DP / 4, kRows = 32 / kChunks;  // 1 row of an access, or 2
+    const int cc = lane % kChunks * 4, cr = lane / kChunks;
+    auto load = [&](int i) {
+        if (i < runs) {
+            const int key = first + i * kBN;
+            float* k_dst = ring + (i % L::kStages) * L::kStage;
+            float* v_dst = k_dst + kRun * L::kPitch;
+#pragma unroll
+            for (int r0 = 0; r0 < kRun; r0 += kRows) {
+                const int r = r0 + cr, k = key + r;
+                const bool on = cc < a.dim && k < b.len && (!mask || mask[k] != 0);
+                copy16(k_dst + r * L::kPitch + cc, kp + (on ? (int64_t)k * g.k_ss + cc : 0), on);
+                copy16(v_dst + r * DP + cc, vp + (on ? (int64_t)k * g.v_ss + cc : 0), on);
+            }
+        }
+        copies_done();
+    };
+    for (int i = threadIdx.x; i < R * kChunks; i += L::kThreads) {
+        const int r = i / kChunks, c = i % kChunks * 4;
+        const bool on = c < a.dim && b.row0 + r < g.rows;
+        copy16(sq + r * DP + c, (const float*)a.q + (on ? mafat_attn::Row(a, b, b.row0 + r).query(a) + c : 0), on);
+    }
+#pragma unroll
+    for (int i = 0; i < L::kStages - 1; ++i) load(i);
+    wait_copies<L::kStages - 2>();
+    __syncthreads();  // the queries came with the first run
+
+    float m[R], l[R];
+    float2 o[R][kCh / 2];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+#pragma unroll
+        for (int d = 0; d < kCh / 2; ++d) o[i][d] = make_float2(0.f, 0.f);
+    }
+    // scores: a lane has one key and every second quad of channels
+    const int key_of = lane % kRun, part = lane / kRun;
+#pragma unroll 1
+    for (int i = 0; i < runs; ++i) {
+        load(i + L::kStages - 1);
+        wait_copies<L::kStages - 1>();
+        __syncwarp();
+        const int key = first + i * kBN;
+        const float* sk = ring + (i % L::kStages) * L::kStage;
+        const float* sv = sk + kRun * L::kPitch;
+        float2 acc[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[r] = make_float2(0.f, 0.f);
+#pragma unroll 4
+        for (int d = part * 4; d < DP; d += 8) {
+            const float4 y = load4(sk + key_of * L::kPitch + d);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float4 x = load4(sq + r * DP + d);
+                fma2(acc[r], make_float2(x.x, x.y), make_float2(y.x, y.y));
+                fma2(acc[r], make_float2(x.z, x.w), make_float2(y.z, y.w));
+            }
+        }
+        const int k = key + key_of;
+        const bool seen = k < b.len && (!mask || mask[k] != 0);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int limit = g.causal ? mafat_attn::Row(a, b, b.row0 + r).limit(a, b) : b.len;
+            float s[1] = {acc[r].x + acc[r].y};
+            s[0] += __shfl_xor_sync(0xffffffffu, s[0], kRun);
+            if (!seen || k >= limit) s[0] = -INFINITY;
+            const float keep = softmax_step(s, m[r], l[r], a.scale_log2);  // l: each key in two lanes
+            if (part == 0) sp[r * kRun + key_of] = s[0];
+#pragma unroll
+            for (int d = 0; d < kCh / 2; ++d) o[r][d] = make_float2(o[r][d].x * keep, o[r][d].y * keep);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e0 = 0; e0 < kRun; e0 += 4) {
+            float2 v[4][kCh / 2];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (kCh == 4) {
+                    const float4 u = load4(sv + (e0 + e) * DP + lane * 4);
+                    v[e][0] = make_float2(u.x, u.y);
+                    v[e][1] = make_float2(u.z, u.w);
+                } else {
+                    v[e][0] = *reinterpret_cast<const float2*>(sv + (e0 + e) * DP + lane * 2);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float4 p = load4(sp + r * kRun + e0);
+#pragma unroll
+                for (int d = 0; d < kCh / 2; ++d) {
+                    fma2(o[r][d], make_float2(p.x, p.x), v[0][d]);
+                    fma2(o[r][d], make_float2(p.y, p.y), v[1][d]);
+                    fma2(o[r][d], make_float2(p.z, p.z), v[2][d]);
+                    fma2(o[r][d], make_float2(p.w, p.w), v[3][d]);
+                }
+            }
+        }
+        __syncwarp();  // the stage is written again by the next copies, the weights by the next run
+    }
+    wait_copies<0>();
+    __syncthreads();
+    // join the warps: O, m and l of each in shared memory
+    float* so = sm + R * DP;
+    float* sml = so + kFewWarps * R * DP;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int w = 1; w < kRun; w *= 2) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
+        if (lane == 0) {
+            sml[(warp * R + r) * 2] = m[r];
+            sml[(warp * R + r) * 2 + 1] = l[r];
         }
 #pragma unroll
-        for (int c = 0; c < DP / 64; ++c) {
-            const int d = c * 64 + tx * 4;
-            if (d >= a.dim) continue;
-            float4 v = make_float4(o[i][c * 4] * inv, o[i][c * 4 + 1] * inv, o[i][c * 4 + 2] * inv,
-                                   o[i][c * 4 + 3] * inv);
-            for (int p = 0; p < a.join; ++p) {
-                const int64_t at = (int64_t)p * a.rows_total + w.row;
-                const float f = mafat_attn::exp2_fast(a.part_lse[at] - top) * scale;
-                const float4 u = load4(a.part_o + at * a.dim + d);
-                v = make_float4(fmaf(f, u.x, v.x), fmaf(f, u.y, v.y), fmaf(f, u.z, v.z), fmaf(f, u.w, v.w));
-            }
-            store4(a.direct ? (float*)a.out + w.o + d : a.part_o + w.part * a.dim + d, v);
+        for (int d = 0; d < kCh / 2; ++d)
+            *reinterpret_cast<float2*>(so + (warp * R + r) * DP + lane * kCh + 2 * d) = o[r][d];
+    }
+    __syncthreads();
+    const int rows = min(R, g.rows - b.row0);
+    for (int i = threadIdx.x; i < rows * kChunks; i += L::kThreads) {
+        const int r = i / kChunks, d = i % kChunks * 4;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kFewWarps; ++w) top = mafat_attn::max_nan(top, sml[(w * R + r) * 2]);
+        const float off = top == -INFINITY ? 0.f : -top * a.scale_log2;
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kFewWarps; ++w) {
+            const float x = mafat_attn::exp2_fast(fmaf(sml[(w * R + r) * 2], a.scale_log2, off));
+            sum = fmaf(x, sml[(w * R + r) * 2 + 1], sum);
+            const float4 u = load4(so + (w * R + r) * DP + d);
+            v = make_float4(fmaf(x, u.x, v.x), fmaf(x, u.y, v.y), fmaf(x, u.z, v.z), fmaf(x, u.w, v.w));
         }
+        const Writer w(a, b, b.row0 + r, top, sum, d == 0);
+        w.put(a, d, v);
     }
     mafat_attn::launch_end(a);
 }
 
 template <int BM, int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
-    return mafat_launch_overlapped(attn_simt_kernel<BM, DP>, a.seg.items, Tile<BM, DP>::kThreads, Tile<BM, DP>::kSmem, s, a);
+    using L = Tile<BM, DP>;
+    return mafat_launch_overlapped(attn_simt_kernel<BM, DP>, a.seg.items, L::kThreads, L::kSmem, s, a);
 }
-template <int BM, int DP>
-cudaError_t prepare() {
-    return cudaFuncSetAttribute(attn_simt_kernel<BM, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                Tile<BM, DP>::kSmem);
+template <int R, int DP>
+cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
+    return mafat_launch_overlapped(attn_simt_few_kernel<R, DP>, a.seg.items, Few<R, DP>::kThreads, Few<R, DP>::kSmem, s, a);
 }
+cudaError_t prepare(const void* fn, int smem) {
+    return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+}
+
 }  // namespace
 
-int mafat_attn_simt_rows(bool wide) { return wide ? 64 : 16; }
 int mafat_attn_simt_keys() { return kBN; }
 
 cudaError_t mafat_prepare_attn_simt() {
     cudaError_t e;
-    if ((e = prepare<64, 64>()) != cudaSuccess) return e;
-    if ((e = prepare<64, 128>()) != cudaSuccess) return e;
-    if ((e = prepare<16, 64>()) != cudaSuccess) return e;
-    return prepare<16, 128>();
+    if ((e = prepare((const void*)attn_simt_few_kernel<8, 64>, Few<8, 64>::kSmem)) != cudaSuccess) return e;
+    if ((e = prepare((const void*)attn_simt_few_kernel<8, 128>, Few<8, 128>::kSmem)) != cudaSuccess) return e;
+    if ((e = prepare((const void*)attn_simt_kernel<64, 64>, Tile<64, 64>::kSmem)) != cudaSuccess) return e;
+    if ((e = prepare((const void*)attn_simt_kernel<64, 128>, Tile<64, 128>::kSmem)) != cudaSuccess) return e;
+    if ((e = prepare((const void*)attn_simt_kernel<128, 64>, Tile<128, 64>::kSmem)) != cudaSuccess) return e;
+    return prepare((const void*)attn_simt_kernel<128, 128>, Tile<128, 128>::kSmem);
 }
 
-cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, bool wide, cudaStream_t s) {
-    if (wide) return a.dim <= 64 ? launch<64, 64>(a, s) : launch<64, 128>(a, s);
-    return a.dim <= 64 ? launch<16, 64>(a, s) : launch<16, 128>(a, s);
+cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s) {
+    if (rows == 8) return a.dim <= 64 ? launch_few<8, 64>(a, s) : launch_few<8, 128>(a, s);
+    if (rows == 64) return a.dim <= 64 ? launch<64, 64>(a, s) : launch<64, 128>(a, s);
+    return a.dim <= 64 ? launch<128, 64>(a, s) : launch<128, 128>(a, s);
 }
