@@ -21,7 +21,7 @@ void mafat_internal_clear_error();
 void* mafat_internal_encode_tiled();
 
 // A kernel and the shape of its work.
-enum AttnKernel { kSimt8, kSimt64, kSimt128, kRows, kTc1, kTc2 };
+enum AttnKernel { kSimt4, kSimt8, kSimt64, kSimt128, kRows, kTc1, kTc2 };
 struct AttnShape {
     int rows, keys;  // of a CTA's tile
     int ctas;        // of an SM
@@ -33,7 +33,7 @@ struct AttnSegPlan {
     int32_t n_seq = 0, reqs = 0, n = 0, causal = 0;
     int64_t k[3] = {0, 0, 0}, v[3] = {0, 0, 0};  // strides: sequence, key, head
     int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, items = 0, ctas = 0;
-    AttnKernel kernel = kSimt8;
+    AttnKernel kernel = kRows;
 };
 
 struct mafat_attn_s {
@@ -145,26 +145,30 @@ mafat_status check_common(const Common& c) {
     return MAFAT_OK;
 }
 
-AttnShape shape_of(AttnKernel k) {
+AttnShape shape_of(AttnKernel k, int dim) {
     switch (k) {
         case kRows: return {16, mafat_attn_rows_keys(), 2, 2};
         case kTc1: return {128, 128, 2, 2};
         case kTc2: return {256, 128, 1, 2};
         case kSimt128: return {128, mafat_attn_simt_keys(), 1, 2};
         case kSimt64: return {64, mafat_attn_simt_keys(), 1, 2};
-        default: return {8, mafat_attn_simt_keys(), 1, 2};
+        case kSimt8: return {8, mafat_attn_simt_keys(), dim <= 64 ? 2 : 1, 2};
+        default: return {4, mafat_attn_simt_keys(), dim <= 64 ? 2 : 1, 2};
     }
 }
 bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
 
 // Most parts that a tile of many rows joins at its end: a thread reads them one after another.
 constexpr int kTileJoin = 4;
-constexpr int kFewRows = 16;  // a tile of the kernels for few rows
-bool is_rows(AttnKernel k) { return k == kSimt8 || k == kRows; }
+// Most rows for which the kernels for few rows are taken.  bf16: one tile of 16 (at 32 rows over 64 sequences
+// of 1444 keys its second pass over the keys makes it 70 us against 35 of the tensor-core tiles; at 16 both take 36, and less
+// of it to start).  fp32: three tiles of 8 (144 us against 182 at 24 rows, 190 against 182 at 32).
+constexpr int kFewRows = 16, kFewRows32 = 24;
+bool is_rows(AttnKernel k) { return k == kSimt4 || k == kSimt8 || k == kRows; }
 
 AttnKernel choose_kernel(int32_t dtype, int32_t asked, int32_t rows, int32_t n) {
-    const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= kFewRows);
-    if (dtype == MAFAT_FP32) return few ? kSimt8 : rows <= 64 ? kSimt64 : kSimt128;
+    const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= (dtype == MAFAT_FP32 ? kFewRows32 : kFewRows));
+    if (dtype == MAFAT_FP32) return few ? (rows <= 4 ? kSimt4 : kSimt8) : rows <= 64 ? kSimt64 : kSimt128;
     if (few || n == 0) return kRows;  // without keys there is nothing to map
     return rows <= 128 ? kTc1 : kTc2;
 }
@@ -189,7 +193,7 @@ int32_t choose_splits(int64_t items, int64_t tiles, int64_t slots, int setup) {
 mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms, bool second) {
     g.rows = g.reqs * p.n_q * (p.heads_q / p.heads_kv);
     g.kernel = choose_kernel(p.dtype, c.kernel, g.rows, g.n);
-    const AttnShape sh = shape_of(g.kernel);
+    const AttnShape sh = shape_of(g.kernel, p.dim);
     g.row_tiles = (g.rows + sh.rows - 1) / sh.rows;
     const int64_t work = (int64_t)g.n_seq * p.heads_kv * g.row_tiles;
     const int64_t tiles = std::max<int64_t>(1, ((int64_t)g.n + sh.keys - 1) / sh.keys);
@@ -362,7 +366,7 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
                 return st;
             e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, s);
         } else {
-            e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, s) : mafat_launch_attn_simt(a, shape_of(g.kernel).rows, s);
+            e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, s) : mafat_launch_attn_simt(a, shape_of(g.kernel, p->dim).rows, s);
         }
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }

@@ -15,7 +15,7 @@
 // weights broadcast, fewer reads an FMA, 8 warps instead of 16) was 4 % slower.
 //
 // Few rows (attn_simt_few_kernel): bound by reading K and V.  The warps of a CTA share the R rows and split the
-// keys, each with a ring of runs of 16 keys of its own and its own m, l and O, joined at the end.
+// keys, each with a ring of runs of 8 keys of its own and its own m, l and O, joined at the end.
 #include "attn_common.cuh"
 
 namespace {
@@ -272,12 +272,12 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
 
 // ---- few rows -----------------------------------------------------------------------------------
 
-constexpr int kFewWarps = 4, kRun = 16;  // keys of a warp at a time
+constexpr int kFewWarps = 8, kRun = 8;  // keys of a warp at a time
 
 template <int R, int DP>
 struct Few {
     static constexpr int kThreads = kFewWarps * 32;
-    static constexpr int kStages = DP == 128 ? 3 : 4;
+    static constexpr int kStages = 3;  // with 64 channels two CTAs share an SM
     static constexpr int kPitch = DP + 4;
     static constexpr int kStage = kRun * (kPitch + DP);               // floats of a run of K and V
     static constexpr int kWarp = kStages * kStage + R * kRun;         // and the weights
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
 #pragma unroll
         for (int d = 0; d < kCh / 2; ++d) o[i][d] = make_float2(0.f, 0.f);
     }
-    // scores: a lane has one key and every second quad of channels
+    // scores: a lane has one key and every fourth quad of channels
     const int key_of = lane % kRun, part = lane / kRun;
 #pragma unroll 1
     for (int i = 0; i < runs; ++i) {
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[r] = make_float2(0.f, 0.f);
 #pragma unroll 4
-        for (int d = part * 4; d < DP; d += 8) {
+        for (int d = part * 4; d < DP; d += 4 * (32 / kRun)) {
             const float4 y = load4(sk + key_of * L::kPitch + d);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -367,9 +367,10 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
         for (int r = 0; r < R; ++r) {
             const int limit = g.causal ? mafat_attn::Row(a, b, b.row0 + r).limit(a, b) : b.len;
             float s[1] = {acc[r].x + acc[r].y};
-            s[0] += __shfl_xor_sync(0xffffffffu, s[0], kRun);
+#pragma unroll
+            for (int w = kRun; w < 32; w *= 2) s[0] += __shfl_xor_sync(0xffffffffu, s[0], w);
             if (!seen || k >= limit) s[0] = -INFINITY;
-            const float keep = softmax_step(s, m[r], l[r], a.scale_log2);  // l: each key in two lanes
+            const float keep = softmax_step(s, m[r], l[r], a.scale_log2);  // l: each key in four lanes
             if (part == 0) sp[r * kRun + key_of] = s[0];
 #pragma unroll
             for (int d = 0; d < kCh / 2; ++d) o[r][d] = make_float2(o[r][d].x * keep, o[r][d].y * keep);
@@ -461,6 +462,8 @@ int mafat_attn_simt_keys() { return kBN; }
 
 cudaError_t mafat_prepare_attn_simt() {
     cudaError_t e;
+    if ((e = prepare((const void*)attn_simt_few_kernel<4, 64>, Few<4, 64>::kSmem)) != cudaSuccess) return e;
+    if ((e = prepare((const void*)attn_simt_few_kernel<4, 128>, Few<4, 128>::kSmem)) != cudaSuccess) return e;
     if ((e = prepare((const void*)attn_simt_few_kernel<8, 64>, Few<8, 64>::kSmem)) != cudaSuccess) return e;
     if ((e = prepare((const void*)attn_simt_few_kernel<8, 128>, Few<8, 128>::kSmem)) != cudaSuccess) return e;
     if ((e = prepare((const void*)attn_simt_kernel<64, 64>, Tile<64, 64>::kSmem)) != cudaSuccess) return e;
@@ -470,6 +473,7 @@ cudaError_t mafat_prepare_attn_simt() {
 }
 
 cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s) {
+    if (rows == 4) return a.dim <= 64 ? launch_few<4, 64>(a, s) : launch_few<4, 128>(a, s);
     if (rows == 8) return a.dim <= 64 ? launch_few<8, 64>(a, s) : launch_few<8, 128>(a, s);
     if (rows == 64) return a.dim <= 64 ? launch<64, 64>(a, s) : launch<64, 128>(a, s);
     return a.dim <= 64 ? launch<128, 64>(a, s) : launch<128, 128>(a, s);
