@@ -6,11 +6,10 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstring>
+#include <cstdarg>
+#include <cstdio>
 #include <limits>
 #include <new>
-#include <string>
-#include <vector>
 
 #include "../../include/mafat.h"
 #include "attention.h"
@@ -57,10 +56,21 @@ struct mafat_attn_s {
 
 namespace {
 
-mafat_status fail(mafat_status s, const std::string& msg) { return mafat_internal_fail(s, msg.c_str()); }
+// Nothing that throws passes a C entry: messages are made on the stack, and keeping one may fail.
+mafat_status fail(mafat_status s, const char* format, ...) {
+    char msg[256];
+    va_list args;
+    va_start(args, format);
+    vsnprintf(msg, sizeof(msg), format, args);
+    va_end(args);
+    try {
+        return mafat_internal_fail(s, msg);
+    } catch (...) {
+        return s;
+    }
+}
 mafat_status cuda_fail(cudaError_t e, const char* what) {
-    return fail(e == cudaErrorMemoryAllocation ? MAFAT_ENOMEM : MAFAT_ECUDA,
-                std::string(what) + ": " + cudaGetErrorString(e));
+    return fail(e == cudaErrorMemoryAllocation ? MAFAT_ENOMEM : MAFAT_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
 constexpr int kStatusBytes = 256;
@@ -94,11 +104,11 @@ mafat_status take_strides(const char* what, const int64_t given[3], const int64_
     for (int i = 0; i < 3; ++i) {
         const int64_t st = given[i];
         if (n[i] > 1 && st < dim)
-            return fail(MAFAT_EINVAL, std::string(what) + ": a stride is smaller than a head's channels");
+            return fail(MAFAT_EINVAL, "%s: a stride is smaller than a head's channels", what);
         if (st < 0 || st * esz % 16 != 0)
-            return fail(MAFAT_EINVAL, std::string(what) + ": strides must be multiples of 16 bytes");
+            return fail(MAFAT_EINVAL, "%s: strides must be multiples of 16 bytes", what);
         if (st >= ((int64_t)1 << 40) / esz)
-            return fail(MAFAT_EUNSUPPORTED, std::string(what) + ": strides must be below 2^40 bytes");
+            return fail(MAFAT_EUNSUPPORTED, "%s: strides must be below 2^40 bytes", what);
         out[i] = n[i] > 1 ? st : dim;  // never used: any valid one
     }
     return MAFAT_OK;
@@ -224,7 +234,7 @@ mafat_status encode_map(CUtensorMap* m, const void* base, const AttnSegPlan& g, 
     const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return fail(MAFAT_ECUDA, "cuTensorMapEncodeTiled failed (" + std::to_string((int)r) + ")");
+    if (r != CUDA_SUCCESS) return fail(MAFAT_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
     return MAFAT_OK;
 }
 
@@ -501,7 +511,7 @@ mafat_status mafat_rms_norm(const mafat_norm_desc* d, const void* x, const void*
     if (d->out_dtype != d->dtype && d->out_dtype != MAFAT_E4M3) return fail(MAFAT_EINVAL, "out_dtype must be dtype or MAFAT_E4M3");
     const bool quant = d->out_dtype == MAFAT_E4M3;
     if (d->rows < 0 || d->cols < 1) return fail(MAFAT_EINVAL, "rows must not be negative and cols must be positive");
-    if (d->cols > mafat_norm_max_cols()) return fail(MAFAT_EUNSUPPORTED, "at most " + std::to_string(mafat_norm_max_cols()) + " cols");
+    if (d->cols > mafat_norm_max_cols()) return fail(MAFAT_EUNSUPPORTED, "at most %d cols", mafat_norm_max_cols());
     if (d->rows > kMaxI32) return fail(MAFAT_EUNSUPPORTED, "too many rows");
     if (!(d->eps >= 0.f) || std::isinf(d->eps)) return fail(MAFAT_EINVAL, "eps must be finite and not negative");
     if (quant && d->scale_group != 0 && d->scale_group != 128)

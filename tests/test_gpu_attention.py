@@ -299,3 +299,53 @@ def test_tensors_that_are_not_the_plans_are_refused(mf):
             plan.run(**{**good, **change})
         assert e.value.status == mf.EINVAL
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_sizes(mf, seed):
+    """Sizes, types, lengths, masks and layouts at random, whatever kernel they go to."""
+    import random
+    r = random.Random(seed)
+    dtype, D, Hk = r.choice([0, 0, 1]), 8 * r.randint(1, 16), r.choice([1, 2, 3, 5])
+    H = Hk * r.choice([1, 2, 4, 7, 8])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    if r.random() < 0.5:
+        B, T, S = r.randint(1, 5), r.choice([1, 1, r.randint(2, 300)]), r.randint(1, 1500)
+        ln = [r.randint(0, S) for _ in range(B)] if r.random() < 0.5 else None
+        mask = torch.rand(B, S, generator=g, device="cuda") < r.random() if r.random() < 0.5 else None
+        _cross(mf, B, T, S, H, Hk, D, dtype, kv_len=ln, kv_mask=mask, seed=seed, poison=True, layout=r.choice(["bshd", "bhsd"]))
+    else:
+        G, R, T = r.randint(1, 3), r.randint(1, 9), r.choice([1, 1, r.randint(2, 40)])
+        P, S = r.randint(1, 900), r.randint(1, 300)
+        own = [r.randint(0, S) for _ in range(G * R)]
+        pl = [r.randint(0, P) for _ in range(G)] if r.random() < 0.5 else None
+        mask = torch.rand(G, P, generator=g, device="cuda") < r.random() if r.random() < 0.5 else None
+        _prefix(mf, G, R, T, P, S, H, Hk, D, dtype, own_len=own, prefix_len=pl, prefix_mask=mask, seed=seed, poison=True,
+                strided=r.random() < 0.5)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_without_lse_and_with_raw_addresses(mf, dtype):
+    """lse is optional; addresses are taken as they are given, and refused where they cannot be right."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    dt = _dt(mf, dtype)
+    q, k, v = (_randn(g, s, dt) for s in ((2, 3, 4, 64), (2, 90, 2, 64), (2, 90, 2, 64)))
+    o = [torch.empty_like(q) for _ in range(2)]
+    plan = mf.CrossAttention(2, 3, 90, 4, 2, 64, dtype=dtype)
+    plan.run(q, k, v, o[0])
+    s = torch.cuda.current_stream().cuda_stream
+    plan.run(q.data_ptr(), k.data_ptr(), v.data_ptr(), o[1].data_ptr(), stream=s)
+    plan.sync_status(like=q)
+    assert torch.equal(o[0], o[1])
+    addresses = dict(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), out=o[1].data_ptr())
+    for name in addresses:
+        for wrong in (0, addresses[name] + 2, addresses["out" if name != "out" else "k"]):
+            with pytest.raises(mf.MafatError) as e:
+                plan.run(**{**addresses, name: wrong}, stream=s)
+            assert e.value.status == mf.EINVAL
+    for name in ("kv_len", "lse"):
+        with pytest.raises(mf.MafatError):
+            plan.run(**addresses, **{name: o[1].data_ptr() + 1}, stream=s)
+    torch.cuda.synchronize()
