@@ -1,5 +1,6 @@
 // What the attention kernels share: which rows and keys a CTA has, where its results go.
 #pragma once
+#include <cuda_bf16.h>
 #include <math_constants.h>
 
 #include "attention.h"
@@ -136,5 +137,77 @@ struct Join {
     }
     float lse2;
 };
+
+__device__ __forceinline__ void put4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void put4(__nv_bfloat16* p, float4 v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2*>(p) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// A warp joins the parts of a row: O = sum_i w_i O_i / sum_i w_i with w_i = 2^(lse_i - max lse).  A lane
+// has four channels, of every WAYS-th part (2 where a row has 64 channels at most, else 1).  The weights are
+// made first, a lane each, so that the loads of sixteen parts a lane are on their way together.  The order of the sums is
+// fixed, so results do not change from run to run.  SETS: a row has 32 * SETS parts at most.
+template <class T, int WAYS, int SETS>
+__device__ __forceinline__ void join_row(const MafatAttnArgs& a, int64_t row) {
+    constexpr int kLanes = 32 / WAYS, kUnroll = 16;
+    const int lane = threadIdx.x % 32, way = lane / kLanes, d = lane % kLanes * 4;
+    const bool in_dim = d < a.dim;
+    float lse[SETS], top = -CUDART_INF_F;
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+        const int p = i * 32 + lane;
+        lse[i] = p < a.parts ? __ldcg(a.part_lse + (int64_t)p * a.rows_total + row) : -CUDART_INF_F;
+        top = max_nan(top, lse[i]);
+    }
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, w));
+    const float base = top == -CUDART_INF_F ? 0.f : top;
+    float sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+        if (i * 32 >= a.parts) break;
+        const float w = exp2_fast(lse[i] - base);
+        sum += w;
+        const int n = min(32, a.parts - i * 32);
+        const float* src = a.part_o + ((int64_t)(i * 32) * a.rows_total + row) * a.dim + d;
+#pragma unroll 1
+        for (int p0 = 0; p0 < n; p0 += kUnroll * WAYS) {
+            float4 v[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int p = p0 + u * WAYS + way;
+                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (p < n && in_dim)
+                    v[u] = __ldcg(reinterpret_cast<const float4*>(src + (int64_t)p * a.rows_total * a.dim));
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const float x = __shfl_sync(0xffffffffu, w, (p0 + u * WAYS + way) & 31);  // past n: v is zero
+                acc.x = fmaf(x, v[u].x, acc.x);
+                acc.y = fmaf(x, v[u].y, acc.y);
+                acc.z = fmaf(x, v[u].z, acc.z);
+                acc.w = fmaf(x, v[u].w, acc.w);
+            }
+        }
+    }
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+    if (WAYS == 2) {
+        acc.x += __shfl_xor_sync(0xffffffffu, acc.x, 16);
+        acc.y += __shfl_xor_sync(0xffffffffu, acc.y, 16);
+        acc.z += __shfl_xor_sync(0xffffffffu, acc.z, 16);
+        acc.w += __shfl_xor_sync(0xffffffffu, acc.w, 16);
+    }
+    const float inv = inverse_sum(sum);
+    const uint32_t u = a.heads_q_div.div((uint32_t)row), req = a.n_q_div.div(u);
+    const int h = (int)((uint32_t)row - u * (uint32_t)a.heads_q), t = (int)(u - req * (uint32_t)a.n_q);
+    if (way == 0 && in_dim)
+        put4((T*)a.out + (int64_t)req * a.o_sb + (int64_t)t * a.o_st + (int64_t)h * a.o_sh + d,
+             make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+    if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -CUDART_INF_F : (base + log2f(sum)) * CUDART_LN2_F;
+}
 
 }  // namespace mafat_attn

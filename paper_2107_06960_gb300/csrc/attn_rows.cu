@@ -10,8 +10,6 @@
 // accumulators are P's operand as they are.  P is rounded to bf16 for its product; all else is fp32.
 //
 // Keys that are not readable are not copied but filled with zeros, so that 0 x NaN cannot reach O.
-#include <cuda_bf16.h>
-
 #include "attn_common.cuh"
 
 namespace {

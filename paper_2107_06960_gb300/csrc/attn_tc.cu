@@ -19,7 +19,7 @@
 // Shared-memory operands are in the 128-byte-swizzled layout: rows of 64 channels, 16-byte chunk c
 // of row r at chunk c ^ (r % 8).  K is read K-major (its channels are the reduction), V MN-major (its keys
 // are), from the same layout.
-#include <cuda_bf16.h>
+#include <type_traits>
 
 #include "attn_common.cuh"
 #include "device_types.h"
@@ -61,7 +61,7 @@ struct Cfg {
     static constexpr int kOffKv = SLOTS * kTileBytes;
     static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
     static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + kBufs,
-                         kBarO = kBarP + kBufs, kBarQ = kBarO + SLOTS, kBarMask = kBarQ + SLOTS, kBars = kBarMask + 1;
+                         kBarO = kBarP + kBufs, kBarMask = kBarO + SLOTS, kBars = kBarMask + 1;
     // V of a tile is read after the scores of kBufs - 1 tiles more (one slot) or of one (two slots)
     static_assert(kLag <= kStages - (kBufs > 2 ? 2 * kBufs - 2 : 2), "gathered tiles");
     static constexpr int kOffTmem = kOffBar + (kBars * 8 + 15) / 16 * 16;
@@ -307,7 +307,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         }
         for (int i = 0; i < SLOTS; ++i) {
             bar_init(bar(C::kBarO + i), 1);
-            bar_init(bar(C::kBarQ + i), C::kSlotWarps);
         }
         for (int i = 0; i < C::kBufs; ++i) {
             bar_init(bar(C::kBarS + i), 1);
@@ -316,6 +315,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         bar_init(bar(C::kBarMask), 1);
         *broken = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
     }
     if (warp == C::kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
@@ -334,6 +334,46 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         n = __reduce_add_sync(0xffffffffu, n);
         if (lane == 0) *(volatile int*)(sm + C::kOffCount + warp * 4) = n;
     }
+    // K and V can be on their way, and the queries be loaded, before all warps are here
+    uint32_t ahead_loads = 0u;
+    auto load_tile = [&](uint32_t el, int i, uint32_t stage) {
+        const uint32_t full = bar(C::kBarFull) + stage * 8u, dst = base + C::kOffKv + stage * C::kTileBytes;
+        expect_el(el, full, C::kTileBytes);
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c)
+            tma_tile(el, dst + c * C::kSub, (i & 1) ? &vmap : &kmap, c * 64, b.head, b.key0 + (i / 2) * kKeys, b.seq, full);
+    };
+    if (!gather && warp == C::kLoadWarp && b.key1 > b.key0) {
+        const uint32_t el = elect_one();
+        ahead_loads = 2u;
+        load_tile(el, 0, 0u);
+        load_tile(el, 1, 1u);
+    }
+    if (warp < C::kSoftmaxWarps) {
+        const int slot = warp / C::kSlotWarps, half = warp / 4 % C::kHalves, quarter = warp % 4;
+        const int row0 = b.row0 + slot * 128 + quarter * 32, row = row0 + lane;
+        if (row0 < g.rows && b.key1 > b.key0) {
+            constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
+            constexpr int kLoads = 32 / kRows / C::kHalves;
+            uint8_t* mine = sm + slot * C::kTileBytes;
+            const int cc = lane % kChunks, cr = lane / kChunks;
+            const int64_t off = row < g.rows ? mafat_attn::Row(a, b, row).query(a) : -1;
+            uint4 v[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int64_t o = __shfl_sync(0xffffffffu, off, (half * kLoads + i) * kRows + cr);
+                v[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (o >= 0 && cc * 8 < a.dim) v[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + cc * 8);
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = quarter * 32 + (half * kLoads + i) * kRows + cr;
+                *reinterpret_cast<uint4*>(mine + (cc / 8) * C::kSub + r * 128 + ((cc % 8) ^ (r % 8)) * 16) = v[i];
+            }
+            fence_async();
+        }
+    }
+    __syncwarp();
     fence_before();
     __syncthreads();
     fence_after();
@@ -363,28 +403,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         const bool any = row0 < g.rows && t.n > 0;
         const mafat_attn::Row at(a, b, min(row, g.rows - 1));
         uint8_t* mine = sm + slot * C::kTileBytes;  // the slot's queries; at the end, its results on their way out
-        if (any) {
-            constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
-            constexpr int kLoads = 32 / kRows / C::kHalves;
-            const int cc = lane % kChunks, cr = lane / kChunks;
-            const int64_t off = row < g.rows ? at.query(a) : -1;
-            uint4 v[kLoads];
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int64_t o = __shfl_sync(0xffffffffu, off, (half * kLoads + i) * kRows + cr);
-                v[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (o >= 0 && cc * 8 < a.dim) v[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + cc * 8);
-            }
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int r = quarter * 32 + (half * kLoads + i) * kRows + cr;
-                *reinterpret_cast<uint4*>(mine + (cc / 8) * C::kSub + r * 128 + ((cc % 8) ^ (r % 8)) * 16) = v[i];
-            }
-            fence_async();
-        }
-        __syncwarp();
-        if (lane == 0) arrive(bar(C::kBarQ + slot));
-
         // the two warps that have halves of the same rows
         const int pair = 2 + slot * 4 + quarter;
         volatile float* share = (volatile float*)(sm + C::kOffShare) + slot * 128 + quarter * 32 + lane;
@@ -502,12 +520,19 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             __syncwarp();
             fence_after();
         }
-        float join_top = 0.f, join_inv = 0.f;
-        if (row0 < g.rows) {
+        // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in whole pieces:
+        // kOutBytes of each row at a time, bf16 results at once, fp32 parts in two passes.  joins: with the parts of
+        // the launch before (apart, so that the form without them stays short).
+        auto results = [&](auto joins) {
+            constexpr bool kJoins = decltype(joins)::value;
+            constexpr int kWide = DP / C::kHalves;           // columns of the thread
+            constexpr int kStep = kWide >= 64 ? 32 : 16;     // read at a time
+            constexpr int kChunks = C::kOutBytes / 16, kRows = 32 / kChunks, kSwz = kChunks < 8 ? kChunks : 8;
+            const int cc = lane % kChunks, cr = lane / kChunks;
             const float l = joined(l0 + l1, [](float x, float y) { return x + y; });
-            float inv = mafat_attn::inverse_sum(l);
+            float inv = mafat_attn::inverse_sum(l), join_top = 0.f, join_inv = 0.f;
             const mafat_attn::Out w(a, b, at);
-            if (a.join) {
+            if constexpr (kJoins) {
                 mafat_attn::launch_wait();
                 const mafat_attn::Join jn(a, w, m, l);
                 inv = jn.own;
@@ -517,58 +542,60 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             } else if (row < g.rows && half == 0) {
                 mafat_attn::store_lse(a, w, m, l);
             }
-            // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in whole
-            // pieces: kOutBytes of each row at a time, bf16 results at once, fp32 parts in two passes.
-            constexpr int kChunks = C::kOutBytes / 16, kRows = 32 / kChunks, kSwz = kChunks < 8 ? kChunks : 8;
-            const int cc = lane % kChunks, cr = lane / kChunks;
-            const bool part = !a.direct;
+            const bool part = !a.direct, none = t.n == 0 || l == 0.f;
             uint8_t* buf = mine + (quarter * C::kHalves + half) * 32 * C::kOutBytes;
             const int64_t dst = row >= g.rows ? -1 : part ? w.part * a.dim : w.o;
+            uint8_t* my = buf + lane * C::kOutBytes;
+            auto put = [&](int chunk, uint4 v) { *reinterpret_cast<uint4*>(my + ((chunk ^ (lane % kSwz)) * 16)) = v; };
 #pragma unroll
             for (int pass = 0; pass < 2; ++pass) {
                 if (pass == 1 && !part) break;
-                constexpr int kWide = DP / C::kHalves;       // columns of the thread
                 const int cols = part ? kWide / 2 : kWide;  // of this pass
 #pragma unroll
-                for (int i = 0; i < kWide / 16; ++i) {
-                    if (i * 16 >= cols) break;
-                    uint32_t o[16];
+                for (int i = 0; i < kWide / kStep; ++i) {
+                    if (i * kStep >= cols) break;
+                    uint32_t o[kStep];
                     if (t.n > 0) {
-                        tmem_ld16(to + (uint32_t)(pass * (kWide / 2) + 16 * i), o);
-                        ld_wait16(o);
+                        const uint32_t src = to + (uint32_t)(pass * (kWide / 2) + kStep * i);
+                        if constexpr (kStep == 32) {
+                            tmem_ld32(src, o);
+                            ld_wait32(o);
+                        } else {
+                            tmem_ld16(src, o);
+                            ld_wait16(o);
+                        }
                     }
                     // a row without readable keys: 0, whatever the products left
 #pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        o[k] = t.n == 0 || l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
-                    const int d0 = half * kWide + 16 * i;
-                    for (int p = 0; p < a.join; ++p) {
-                        const int64_t at_p = (int64_t)p * a.rows_total + w.row;
-                        const float f = mafat_attn::exp2_fast(a.part_lse[at_p] - join_top) * join_inv;
-                        const float* src = a.part_o + at_p * a.dim + d0;
+                    for (int k = 0; k < kStep; ++k) o[k] = none ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
+                    if constexpr (kJoins) {
+                        const int d0 = half * kWide + kStep * i;
+                        for (int p = 0; p < a.join; ++p) {
+                            const int64_t at_p = (int64_t)p * a.rows_total + w.row;
+                            const float f = mafat_attn::exp2_fast(a.part_lse[at_p] - join_top) * join_inv;
+                            const float* src = a.part_o + at_p * a.dim + d0;
 #pragma unroll
-                        for (int k = 0; k < 16; k += 4) {
-                            if (d0 + k >= a.dim) continue;
-                            const float4 v = *reinterpret_cast<const float4*>(src + k);
-                            o[k] = __float_as_uint(fmaf(f, v.x, __uint_as_float(o[k])));
-                            o[k + 1] = __float_as_uint(fmaf(f, v.y, __uint_as_float(o[k + 1])));
-                            o[k + 2] = __float_as_uint(fmaf(f, v.z, __uint_as_float(o[k + 2])));
-                            o[k + 3] = __float_as_uint(fmaf(f, v.w, __uint_as_float(o[k + 3])));
+                            for (int k = 0; k < kStep; k += 4) {
+                                if (d0 + k >= a.dim) continue;
+                                const float4 v = *reinterpret_cast<const float4*>(src + k);
+                                o[k] = __float_as_uint(fmaf(f, v.x, __uint_as_float(o[k])));
+                                o[k + 1] = __float_as_uint(fmaf(f, v.y, __uint_as_float(o[k + 1])));
+                                o[k + 2] = __float_as_uint(fmaf(f, v.z, __uint_as_float(o[k + 2])));
+                                o[k + 3] = __float_as_uint(fmaf(f, v.w, __uint_as_float(o[k + 3])));
+                            }
                         }
                     }
                     if (part) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            *reinterpret_cast<uint4*>(buf + lane * C::kOutBytes + (((4 * i + k) ^ (lane % kSwz)) * 16)) =
-                                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                        for (int k = 0; k < kStep / 4; ++k)
+                            put(kStep / 4 * i + k, make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
                     } else {
-                        uint32_t p[8];
+                        uint32_t p[kStep / 2];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) p[k] = pack(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+                        for (int k = 0; k < kStep / 2; ++k) p[k] = pack(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
 #pragma unroll
-                        for (int k = 0; k < 2; ++k)
-                            *reinterpret_cast<uint4*>(buf + lane * C::kOutBytes + (((2 * i + k) ^ (lane % kSwz)) * 16)) =
-                                make_uint4(p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]);
+                        for (int k = 0; k < kStep / 8; ++k)
+                            put(kStep / 8 * i + k, make_uint4(p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]));
                     }
                 }
                 __syncwarp();
@@ -588,6 +615,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 }
                 __syncwarp();
             }
+        };
+        if (row0 < g.rows) {
+            if (a.join)
+                results(std::true_type());
+            else
+                results(std::false_type());
         }
         fence_before();
     } else {
@@ -635,7 +668,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         auto next_scores = [&]() {
             if (ps.tile >= t.n) return;
             if (ps.slot == 0) wait(bar(C::kBarFull) + ps.stage * 8u, ps.phase, ctl);
-            if (ps.tile == 0) wait(bar(C::kBarQ) + (uint32_t)ps.slot * 8u, 0u, ctl);
             fence_after();
             scores(ps.slot, ps.stage, bs);
             if (++bs == C::kBufs) bs = 0;
@@ -757,16 +789,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         }
     } else if (warp == C::kLoadWarp) {
         const uint32_t el = elect_one();
-        uint32_t stage = 0u, phase = 1u;  // the first wait on an empty stage is over at once
+        uint32_t stage = ahead_loads % (uint32_t)C::kStages;
+        uint32_t phase = ahead_loads < (uint32_t)C::kStages ? 1u : 0u;  // the first wait on an empty stage is over at once
 #pragma unroll 1
-        for (int i = 0; i < 2 * t.n; ++i) {
+        for (int i = (int)ahead_loads; i < 2 * t.n; ++i) {
             wait(bar(C::kBarEmpty) + stage * 8u, phase, ctl);
-            const uint32_t full = bar(C::kBarFull) + stage * 8u, dst = base + C::kOffKv + stage * C::kTileBytes;
-            expect_el(el, full, C::kTileBytes);
-#pragma unroll
-            for (int c = 0; c < DP / 64; ++c)
-                tma_tile(el, dst + c * C::kSub, (i & 1) ? &vmap : &kmap, c * 64, b.head, t.key0 + (i / 2) * kKeys, b.seq,
-                         full);
+            load_tile(el, i, stage);
             if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
         }
     } else if (warp == C::kMaskWarp) {
