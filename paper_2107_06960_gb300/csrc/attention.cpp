@@ -19,12 +19,13 @@ mafat_status mafat_internal_fail(mafat_status s, const char* msg);
 void mafat_internal_clear_error();
 void* mafat_internal_encode_tiled();
 
-// A kernel and the shape of its work.
-enum AttnKernel { kSimt4, kSimt8, kSimt64, kSimt128, kRows, kTc1, kTc2 };
+// A kernel, the shape of its work and what it takes (measured on GB300, back to back).
+enum AttnKernel { kSimt4, kSimt8, kSimt64, kRows, kTc1, kTc2 };
 struct AttnShape {
-    int rows, keys;  // of a CTA's tile
-    int ctas;        // of an SM
-    int setup;       // what starting and ending a CTA takes, in tiles of keys
+    int rows, keys;   // of a CTA's tile
+    int ctas;         // of an SM that do not slow each other down
+    double tile_us;   // a tile of keys, where memory does not bound it
+    double setup_us;  // the start and end of an item
 };
 
 // One set of keys as a plan sees it.
@@ -156,14 +157,15 @@ mafat_status check_common(const Common& c) {
 }
 
 AttnShape shape_of(AttnKernel k, int dim) {
+    const bool wide = dim > 64;
+    const int simt = mafat_attn_simt_keys();
     switch (k) {
-        case kRows: return {16, mafat_attn_rows_keys(), 2, 2};
-        case kTc1: return {128, 128, 2, 2};
-        case kTc2: return {256, 128, 1, 2};
-        case kSimt128: return {128, mafat_attn_simt_keys(), 1, 2};
-        case kSimt64: return {64, mafat_attn_simt_keys(), 1, 2};
-        case kSimt8: return {8, mafat_attn_simt_keys(), dim <= 64 ? 2 : 1, 2};
-        default: return {4, mafat_attn_simt_keys(), dim <= 64 ? 2 : 1, 2};
+        case kRows: return {16, mafat_attn_rows_keys(), 2, wide ? 0.95 : 0.45, 0.7};
+        case kTc1: return {128, 128, 2, wide ? 1.1 : 0.95, 3.0};
+        case kTc2: return {256, 128, 1, wide ? 1.5 : 1.0, 4.0};
+        case kSimt64: return {64, simt, 1, wide ? 7.8 : 3.9, 3.0};
+        case kSimt8: return {8, simt, wide ? 1 : 2, 1.2, 2.0};
+        default: return {4, simt, wide ? 1 : 2, 1.2, 2.0};
     }
 }
 bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
@@ -178,21 +180,27 @@ bool is_rows(AttnKernel k) { return k == kSimt4 || k == kSimt8 || k == kRows; }
 
 AttnKernel choose_kernel(int32_t dtype, int32_t asked, int32_t rows, int32_t n) {
     const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= (dtype == MAFAT_FP32 ? kFewRows32 : kFewRows));
-    if (dtype == MAFAT_FP32) return few ? (rows <= 4 ? kSimt4 : kSimt8) : rows <= 64 ? kSimt64 : kSimt128;
+    if (dtype == MAFAT_FP32) return few ? (rows <= 4 ? kSimt4 : kSimt8) : kSimt64;
     if (few || n == 0) return kRows;  // without keys there is nothing to map
     return rows <= 128 ? kTc1 : kTc2;
 }
 
-// Parts of the keys: the number for which the CTAs of one wave after another end first, each with its
-// run of tiles and its set-up; of equals the fewest (parts are written, read and joined).
-int32_t choose_splits(int64_t items, int64_t tiles, int64_t slots, int setup) {
+// Parts of the keys: the number that the model below gives the least time.  The CTAs run in waves of
+// `slots`, each for its tiles of keys, which take as long as their bytes do at the memory's rate where that is
+// more; parts are written and read again, join_round of a row at a time, by a launch that joins them.  Fewer win a tie (1 %).
+int32_t choose_splits(const AttnShape& sh, int64_t items, int64_t tiles, int64_t slots, double tile_bytes, double part_bytes,
+                      int join_round) {
+    constexpr double kBytesPerUs = 6.2e6, kJoinUs = 0.2, kJoinRoundUs = 1.6, kJoinBytesPerUs = 6e6;
     int32_t best = 1;
-    int64_t best_cost = std::numeric_limits<int64_t>::max();
+    double best_us = 0.;
     for (int32_t n = 1; n <= MAFAT_ATTN_MAX_SPLITS && n <= tiles; ++n) {
-        const int64_t waves = (items * n + slots - 1) / slots;
-        const int64_t cost = waves * ((tiles + n - 1) / n + setup);
-        if (cost < best_cost) {
-            best_cost = cost;
+        const int64_t ctas = items * n, waves = (ctas + slots - 1) / slots, each = (tiles + n - 1) / n;
+        const double tile_us = std::max(sh.tile_us, (double)std::min(ctas, slots) * tile_bytes / kBytesPerUs);
+        double us = (double)waves * ((double)each * tile_us + sh.setup_us);
+        if (n > 1)
+            us += kJoinUs + (n + join_round - 1) / join_round * kJoinRoundUs + 2. * n * part_bytes / kJoinBytesPerUs;
+        if (n == 1 || us < 0.99 * best_us) {
+            best_us = us;
             best = n;
         }
     }
@@ -213,7 +221,10 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
     else if (second && (2 * work >= sms || tiles <= 8))
         g.splits = 1;  // whole: it then joins the first launch's parts itself
     else
-        g.splits = choose_splits(work, tiles, (int64_t)sms * sh.ctas, sh.setup);
+        // row tiles of a sequence read its keys together
+        g.splits = choose_splits(sh, work, tiles, (int64_t)sms * sh.ctas,
+                                 2. * sh.keys * p.dim * (p.dtype == MAFAT_BF16 ? 2 : 4) / g.row_tiles,
+                                 4. * p.dim * (double)p.rows_total, p.dim <= 64 ? 32 : 16);
     if (work * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many items of work");
     g.items = (int32_t)(work * g.splits);
     // the kernel for few rows takes item after item

@@ -68,7 +68,7 @@ struct MafatAttnArgs {
     MafatAttnSeg seg;
 };
 
-// fp32 on the CUDA cores, tiles of 4, 8, 64 or 128 rows.
+// fp32 on the CUDA cores, tiles of 4, 8 or 64 rows.
 cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s);
 cudaError_t mafat_prepare_attn_simt();
 int mafat_attn_simt_keys();

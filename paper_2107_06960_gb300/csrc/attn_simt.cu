@@ -9,7 +9,7 @@
 // are copied (cp.async), so that 0 x NaN cannot reach O.
 //
 // Many rows (attn_simt_kernel): bound by FMAs and, close behind, by shared-memory reads (83 % of their rate with
-// 60 % of the FMAs').  A CTA takes BM rows, 64 keys at a time; a thread has 4 rows x 4 keys of the scores, then 4
+// 60 % of the FMAs').  A CTA takes 64 rows, 64 keys at a time, two CTAs an SM; a thread has 4 rows x 4 keys of the scores, then 4
 // rows x DP / 16 channels of O.  K's and V's tiles are single buffers: the next K is copied while the
 // values are summed, the next V while the scores are made.  A warp with 16 rows x 64 keys (queries and
 // weights broadcast, fewer reads an FMA, 8 warps instead of 16) was 4 % slower.
@@ -99,15 +99,18 @@ struct Writer {
 // ---- many rows --------------------------------------------------------------------------------
 
 constexpr int kTX = 16;  // threads along the keys / channels
+constexpr int kBM = 64;
 
-template <int BM, int DP>
+template <int DP>
 struct Tile {
-    static constexpr int kThreads = BM / 4 * kTX;
-    static constexpr int kPitch = DP + 4;        // K and Q rows: 16-byte reads of 8 rows hit all banks
-    static constexpr int kPPitch = kBN + 4;
-    static constexpr int kFloats = BM * kPitch + kBN * kPitch + kBN * DP + BM * kPPitch;
-    static constexpr int kSmem = kFloats * 4;
+    static constexpr int kThreads = kBM / 4 * kTX;
+    static constexpr int kPitch = DP + 4;  // K rows: 16-byte reads of 8 rows hit all banks
+    static constexpr int kSmem = (kBM * DP + kBN * kPitch + kBN * DP + kBM * kBN) * 4;
+    static_assert(kSmem <= 115712, "two CTAs on an SM");
 };
+// Queries and weights have no padding: a warp reads two rows four apart, whose quads are swapped in one of them so
+// that they lie in different banks.
+__device__ __forceinline__ int quad_of(int row, int quad) { return quad ^ (row / 4 % 2); }
 
 // copies ROWS rows of a matrix with `stride` elements between rows; channels past dim and rows that
 // are not readable become zero
@@ -123,16 +126,16 @@ __device__ __forceinline__ void copy_rows(float* dst, const float* src, int64_t 
     copies_done();
 }
 
-template <int BM, int DP>
-__global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_constant__ MafatAttnArgs a) {
-    using L = Tile<BM, DP>;
+template <int DP>
+__global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __grid_constant__ MafatAttnArgs a) {
+    using L = Tile<DP>;
     extern __shared__ __align__(16) float sm[];
     float* sq = sm;
-    float* sk = sq + BM * L::kPitch;
+    float* sk = sq + kBM * DP;
     float* sv = sk + kBN * L::kPitch;
     float* sp = sv + kBN * DP;
     mafat_attn::launch_begin(a);
-    const mafat_attn::Block b(a, blockIdx.x, BM, kBN);
+    const mafat_attn::Block b(a, blockIdx.x, kBM, kBN);
     const MafatAttnSeg& g = a.seg;
     const int tx = threadIdx.x % kTX, ty = threadIdx.x / kTX;
     const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
@@ -153,10 +156,10 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
     {
         constexpr int kChunks = DP / 4;
 #pragma unroll 4
-        for (int i = threadIdx.x; i < BM * kChunks; i += L::kThreads) {
+        for (int i = threadIdx.x; i < kBM * kChunks; i += L::kThreads) {
             const int r = i / kChunks, c = (i % kChunks) * 4;
             const bool on = c < a.dim && b.row0 + r < g.rows;
-            copy16(sq + r * L::kPitch + c,
+            copy16(sq + r * DP + quad_of(r, c / 4) * 4,
                    (const float*)a.q + (on ? mafat_attn::Row(a, b, b.row0 + r).query(a) + c : 0), on);
         }
         if (b.key0 < b.key1) copy_k(b.key0);
@@ -189,7 +192,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
         for (int d = 0; d < DP; d += 4) {
             float4 x[4], y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = load4(sq + (ty * 4 + i) * L::kPitch + d);
+            for (int i = 0; i < 4; ++i) x[i] = load4(sq + (ty * 4 + i) * DP + quad_of(ty * 4, d / 4) * 4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) y[j] = load4(sk + (tx + kTX * j) * L::kPitch + d);
 #pragma unroll
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
             for (int j = 0; j < 4; ++j) {
                 s[j] = mafat_attn::exp2_fast(fmaf(s[j], a.scale_log2, -base));
                 sum += s[j];
-                sp[(ty * 4 + i) * L::kPPitch + tx + kTX * j] = s[j];
+                sp[(ty * 4 + i) * kBN + quad_of(ty * 4, (tx + kTX * j) / 4) * 4 + tx % 4] = s[j];
             }
             l[i] = l[i] * keep + sum;
 #pragma unroll
@@ -239,7 +242,7 @@ __global__ void __launch_bounds__(BM / 4 * kTX) attn_simt_kernel(const __grid_co
         for (int k = 0; k < kBN; k += 4) {
             float4 p[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = load4(sp + (ty * 4 + i) * L::kPPitch + k);
+            for (int i = 0; i < 4; ++i) p[i] = load4(sp + (ty * 4 + i) * kBN + quad_of(ty * 4, k / 4) * 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
 #pragma unroll
@@ -443,10 +446,9 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
     mafat_attn::launch_end(a);
 }
 
-template <int BM, int DP>
+template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
-    using L = Tile<BM, DP>;
-    return mafat_launch_overlapped(attn_simt_kernel<BM, DP>, a.seg.items, L::kThreads, L::kSmem, s, a);
+    return mafat_launch_overlapped(attn_simt_kernel<DP>, a.seg.items, Tile<DP>::kThreads, Tile<DP>::kSmem, s, a);
 }
 template <int R, int DP>
 cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
@@ -466,15 +468,12 @@ cudaError_t mafat_prepare_attn_simt() {
     if ((e = prepare((const void*)attn_simt_few_kernel<4, 128>, Few<4, 128>::kSmem)) != cudaSuccess) return e;
     if ((e = prepare((const void*)attn_simt_few_kernel<8, 64>, Few<8, 64>::kSmem)) != cudaSuccess) return e;
     if ((e = prepare((const void*)attn_simt_few_kernel<8, 128>, Few<8, 128>::kSmem)) != cudaSuccess) return e;
-    if ((e = prepare((const void*)attn_simt_kernel<64, 64>, Tile<64, 64>::kSmem)) != cudaSuccess) return e;
-    if ((e = prepare((const void*)attn_simt_kernel<64, 128>, Tile<64, 128>::kSmem)) != cudaSuccess) return e;
-    if ((e = prepare((const void*)attn_simt_kernel<128, 64>, Tile<128, 64>::kSmem)) != cudaSuccess) return e;
-    return prepare((const void*)attn_simt_kernel<128, 128>, Tile<128, 128>::kSmem);
+    if ((e = prepare((const void*)attn_simt_kernel<64>, Tile<64>::kSmem)) != cudaSuccess) return e;
+    return prepare((const void*)attn_simt_kernel<128>, Tile<128>::kSmem);
 }
 
 cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s) {
     if (rows == 4) return a.dim <= 64 ? launch_few<4, 64>(a, s) : launch_few<4, 128>(a, s);
     if (rows == 8) return a.dim <= 64 ? launch_few<8, 64>(a, s) : launch_few<8, 128>(a, s);
-    if (rows == 64) return a.dim <= 64 ? launch<64, 64>(a, s) : launch<64, 128>(a, s);
-    return a.dim <= 64 ? launch<128, 64>(a, s) : launch<128, 128>(a, s);
+    return a.dim <= 64 ? launch<64>(a, s) : launch<128>(a, s);
 }
