@@ -110,9 +110,17 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // 1 / sum, and 0 for a row that no key is readable for: its result is zero.
 __device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
+// The running maximum of a row is kept as `base`, its score times c = scale log2(e) in fp32, rounded once; weights are
+// 2^(fma(s, c, -base)), and what was summed at another base is multiplied by 2^(base - new base), which is 1
+// where it did not move.  (Making both from the score would be off by the product's rounding, a share of 2^-24 of the
+// exponent in every tile, always the same way: 8e-6 of the result after some hundred tiles.)
+// Before the first readable key base is -inf, and nothing is to be subtracted: 2^-inf = 0.
+__device__ __forceinline__ float subtrahend(float base) { return base == -CUDART_INF_F ? 0.f : base; }
+
 // The row's log2 of its sum of exponentials, -inf where no key is readable.
-__device__ __forceinline__ void store_lse(const MafatAttnArgs& a, const Out& w, float m, float l) {
-    const float lse2 = l == 0.f ? -CUDART_INF_F : fmaf(m, a.scale_log2, log2f(l));
+__device__ __forceinline__ float row_lse2(float base, float l) { return l == 0.f ? -CUDART_INF_F : base + log2f(l); }
+__device__ __forceinline__ void store_lse(const MafatAttnArgs& a, const Out& w, float base, float l) {
+    const float lse2 = row_lse2(base, l);
     if (!a.direct)
         a.part_lse[w.part] = lse2;
     else if (a.lse)
@@ -123,8 +131,8 @@ __device__ __forceinline__ void store_lse(const MafatAttnArgs& a, const Out& w, 
 // out = own * O + sum_p 2^(lse_p - top) * inv * O_p.
 struct Join {
     float top, own, inv;
-    __device__ __forceinline__ Join(const MafatAttnArgs& a, const Out& w, float m, float l) {
-        const float mine = l == 0.f ? -CUDART_INF_F : fmaf(m, a.scale_log2, log2f(l));
+    __device__ __forceinline__ Join(const MafatAttnArgs& a, const Out& w, float base, float l) {
+        const float mine = row_lse2(base, l);
         top = mine;
         for (int p = 0; p < a.join; ++p) top = max_nan(top, a.part_lse[(int64_t)p * a.rows_total + w.row]);
         if (top == -CUDART_INF_F) top = 0.f;  // no readable key anywhere: all factors are zero

@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             const int r = b.row0 + lane / 4 + 8 * h;
             limit[h] = r < g.rows ? mafat_attn::Row(a, b, r).limit(a, b) : 0x7fffffff;
         }
-        float m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
+        float base[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
         float o[DP / 8][4];
 #pragma unroll
         for (int n = 0; n < DP / 8; ++n)
@@ -207,11 +207,11 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                                                 mafat_attn::max_nan(s[1][2 * h], s[1][2 * h + 1]));
                 top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const float mn = mafat_attn::max_nan(m[h], top);
-                up = up || mn != m[h];
-                off[h] = mn == -CUDART_INF_F ? 0.f : -mn * a.scale_log2;
-                keep[h] = mafat_attn::exp2_fast(fmaf(m[h], a.scale_log2, off[h]));
-                m[h] = mn;
+                const float next = mafat_attn::max_nan(base[h], top * a.scale_log2);
+                up = up || next != base[h];
+                off[h] = -mafat_attn::subtrahend(next);
+                keep[h] = mafat_attn::exp2_fast(base[h] + off[h]);
+                base[h] = next;
             }
             if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
@@ -239,14 +239,14 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             __syncwarp();  // the stage is written again by a later copy
         }
 
-        // join the warps: O, m and l of each in shared memory
+        // join the warps: O, base and l of each in shared memory
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
             const int r = lane / 4 + 8 * h;
             if (lane % 4 == 0) {
-                sml[(warp * 16 + r) * 2] = m[h];
+                sml[(warp * 16 + r) * 2] = base[h];
                 sml[(warp * 16 + r) * 2 + 1] = l[h];
             }
 #pragma unroll
@@ -272,12 +272,12 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                 mw[w] = sml[(w * 16 + r) * 2];
                 top = mafat_attn::max_nan(top, mw[w]);
             }
-            const float off = top == -CUDART_INF_F ? 0.f : -top * a.scale_log2;
+            const float off = mafat_attn::subtrahend(top);
             float sum = 0.f;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float x = mafat_attn::exp2_fast(fmaf(mw[w], a.scale_log2, off));
+                const float x = mafat_attn::exp2_fast(mw[w] - off);
                 sum = fmaf(x, sml[(w * 16 + r) * 2 + 1], sum);
                 const float4 u = *reinterpret_cast<const float4*>(so + (w * 16 + r) * C::kPitch + d);
                 v.x = fmaf(x, u.x, v.x);
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             const mafat_attn::Out out(a, b, mafat_attn::Row(a, b, b.row0 + r));
             float inv = mafat_attn::inverse_sum(sum);
             if (a.join) {  // with the parts of the launch before: a lane has the weight of every kQuads-th
-                const float own = sum == 0.f ? -CUDART_INF_F : fmaf(top, a.scale_log2, log2f(sum));
+                const float own = mafat_attn::row_lse2(top, sum);
                 float lse[kSets], best = own;
 #pragma unroll
                 for (int k = 0; k < kSets; ++k) {

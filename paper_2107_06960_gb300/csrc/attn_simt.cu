@@ -15,7 +15,7 @@
 // weights broadcast, fewer reads an FMA, 8 warps instead of 16) was 4 % slower.
 //
 // Few rows (attn_simt_few_kernel): bound by reading K and V.  The warps of a CTA share the R rows and split the
-// keys, each with a ring of runs of 8 keys of its own and its own m, l and O, joined at the end.
+// keys, each with a ring of runs of 8 keys of its own and its own maximum, sum and O, joined at the end.
 #include "attn_common.cuh"
 
 namespace {
@@ -46,20 +46,19 @@ __device__ __forceinline__ void fma2(float2& r, float2 a, float2 b) {
 // One row's share of the online softmax for the N scores of a lane, whose warp has the row's others:
 // s becomes the weights; returns the factor of what was summed before.
 template <int N>
-__device__ __forceinline__ float softmax_step(float (&s)[N], float& m, float& l, float scale_log2) {
+__device__ __forceinline__ float softmax_step(float (&s)[N], float& base, float& l, float scale_log2) {
     float top = s[0];
 #pragma unroll
     for (int j = 1; j < N; ++j) top = mafat_attn::max_nan(top, s[j]);
 #pragma unroll
     for (int w = 1; w < 32; w *= 2) top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, w));
-    const float mn = mafat_attn::max_nan(m, top);
-    const float base = mn == -INFINITY ? 0.f : mn * scale_log2;  // no readable key yet: 2^-inf = 0
-    const float keep = mafat_attn::exp2_fast(fmaf(m, scale_log2, -base));
-    m = mn;
+    const float next = mafat_attn::max_nan(base, top * scale_log2), off = mafat_attn::subtrahend(next);
+    const float keep = mafat_attn::exp2_fast(base - off);
+    base = next;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        s[j] = mafat_attn::exp2_fast(fmaf(s[j], scale_log2, -base));
+        s[j] = mafat_attn::exp2_fast(fmaf(s[j], scale_log2, -off));
         sum += s[j];
     }
     l = l * keep + sum;  // of the lane's keys
@@ -70,17 +69,17 @@ __device__ __forceinline__ float softmax_step(float (&s)[N], float& m, float& l,
 struct Writer {
     mafat_attn::Out at;
     float own, top, inv;
-    __device__ __forceinline__ Writer(const MafatAttnArgs& a, const mafat_attn::Block& b, int r, float m, float l, bool first)
+    __device__ __forceinline__ Writer(const MafatAttnArgs& a, const mafat_attn::Block& b, int r, float base, float l, bool first)
         : at(a, b, mafat_attn::Row(a, b, r)), own(mafat_attn::inverse_sum(l)), top(0.f), inv(0.f) {
         if (a.join) {
             mafat_attn::launch_wait();
-            const mafat_attn::Join jn(a, at, m, l);
+            const mafat_attn::Join jn(a, at, base, l);
             own = jn.own;
             top = jn.top;
             inv = jn.inv;
             if (first && a.lse) a.lse[at.row] = jn.lse2 * CUDART_LN2_F;
         } else if (first) {
-            mafat_attn::store_lse(a, at, m, l);
+            mafat_attn::store_lse(a, at, base, l);
         }
     }
     __device__ __forceinline__ void put(const MafatAttnArgs& a, int d, float4 v) const {
@@ -167,12 +166,12 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
     }
     constexpr int kO = DP / kTX / 2;  // pairs of channels: c * 64 + tx * 4 + {0, 1}, {2, 3}
     int limit[4];
-    float m[4], l[4];
+    float base[4], l[4];
     float2 o[4][kO];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         limit[i] = mafat_attn::Row(a, b, b.row0 + ty * 4 + i).limit(a, b);
-        m[i] = -INFINITY;
+        base[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
         for (int d = 0; d < kO; ++d) o[i][d] = make_float2(0.f, 0.f);
@@ -204,6 +203,7 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
                 }
         }
         bool seen[4];
+        float keep[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int k = key0 + tx + kTX * j;
@@ -220,24 +220,28 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
             }
 #pragma unroll
             for (int w = 1; w < kTX; w *= 2) top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, w));
-            const float mn = mafat_attn::max_nan(m[i], top);
-            const float base = mn == -INFINITY ? 0.f : mn * a.scale_log2;  // no readable key yet: 2^-inf = 0
-            const float keep = mafat_attn::exp2_fast(fmaf(m[i], a.scale_log2, -base));
-            m[i] = mn;
+            const float next = mafat_attn::max_nan(base[i], top * a.scale_log2), off = mafat_attn::subtrahend(next);
+            keep[i] = mafat_attn::exp2_fast(base[i] - off);
+            base[i] = next;
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                s[j] = mafat_attn::exp2_fast(fmaf(s[j], a.scale_log2, -base));
+                s[j] = mafat_attn::exp2_fast(fmaf(s[j], a.scale_log2, -off));
                 sum += s[j];
                 sp[(ty * 4 + i) * kBN + quad_of(ty * 4, (tx + kTX * j) / 4) * 4 + tx % 4] = s[j];
             }
-            l[i] = l[i] * keep + sum;
-#pragma unroll
-            for (int d = 0; d < kO; ++d) o[i][d] = make_float2(o[i][d].x * keep, o[i][d].y * keep);
+            l[i] = l[i] * keep[i] + sum;
         }
         wait_copies<0>();
         __syncthreads();  // V is there, and all are done with K (P is read by the half warp that wrote it)
         if (key0 + kBN < b.key1) copy_k(key0 + kBN);
+        // the tile's sum by itself, then added: O's size sets the rounding of one addition a tile, not of 64 (6000 keys
+        // in one part: 1.4e-6 of the result without it, the weights' 3e-7 with it)
+        float2 sum[4][kO];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int d = 0; d < kO; ++d) sum[i][d] = make_float2(0.f, 0.f);
 #pragma unroll 2
         for (int k = 0; k < kBN; k += 4) {
             float4 p[4];
@@ -251,12 +255,17 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float w = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
-                        fma2(o[i][2 * c], make_float2(w, w), make_float2(v.x, v.y));
-                        fma2(o[i][2 * c + 1], make_float2(w, w), make_float2(v.z, v.w));
+                        fma2(sum[i][2 * c], make_float2(w, w), make_float2(v.x, v.y));
+                        fma2(sum[i][2 * c + 1], make_float2(w, w), make_float2(v.z, v.w));
                     }
                 }
             }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int d = 0; d < kO; ++d)
+                o[i][d] = make_float2(fmaf(o[i][d].x, keep[i], sum[i][d].x), fmaf(o[i][d].y, keep[i], sum[i][d].y));
     }
     wait_copies<0>();
 #pragma unroll
@@ -265,7 +274,7 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
         for (int w = 1; w < kTX; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
         const int r = b.row0 + ty * 4 + i;
         if (r >= g.rows) continue;
-        const Writer w(a, b, r, m[i], l[i], tx == 0);
+        const Writer w(a, b, r, base[i], l[i], tx == 0);
 #pragma unroll
         for (int c = 0; c < DP / 64; ++c)
             w.put(a, c * 64 + tx * 4, make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y));
@@ -289,7 +298,7 @@ struct Few {
 };
 
 template <int R, int DP>
-__global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __grid_constant__ MafatAttnArgs a) {
+__global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_few_kernel(const __grid_constant__ MafatAttnArgs a) {
     using L = Few<R, DP>;
     constexpr int kCh = DP / 32;
     extern __shared__ __align__(16) float sm[];
@@ -332,11 +341,11 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
     wait_copies<L::kStages - 2>();
     __syncthreads();  // the queries came with the first run
 
-    float m[R], l[R];
+    float base[R], l[R];
     float2 o[R][kCh / 2];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        m[i] = -INFINITY;
+        base[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
         for (int d = 0; d < kCh / 2; ++d) o[i][d] = make_float2(0.f, 0.f);
@@ -373,7 +382,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
 #pragma unroll
             for (int w = kRun; w < 32; w *= 2) s[0] += __shfl_xor_sync(0xffffffffu, s[0], w);
             if (!seen || k >= limit) s[0] = -INFINITY;
-            const float keep = softmax_step(s, m[r], l[r], a.scale_log2);  // l: each key in four lanes
+            const float keep = softmax_step(s, base[r], l[r], a.scale_log2);  // l: each key in four lanes
             if (part == 0) sp[r * kRun + key_of] = s[0];
 #pragma unroll
             for (int d = 0; d < kCh / 2; ++d) o[r][d] = make_float2(o[r][d].x * keep, o[r][d].y * keep);
@@ -408,7 +417,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
     }
     wait_copies<0>();
     __syncthreads();
-    // join the warps: O, m and l of each in shared memory
+    // join the warps: O, base and l of each in shared memory
     float* so = sm + R * DP;
     float* sml = so + kFewWarps * R * DP;
 #pragma unroll
@@ -416,7 +425,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
 #pragma unroll
         for (int w = 1; w < kRun; w *= 2) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
         if (lane == 0) {
-            sml[(warp * R + r) * 2] = m[r];
+            sml[(warp * R + r) * 2] = base[r];
             sml[(warp * R + r) * 2 + 1] = l[r];
         }
 #pragma unroll
@@ -430,12 +439,12 @@ __global__ void __launch_bounds__(kFewWarps * 32) attn_simt_few_kernel(const __g
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kFewWarps; ++w) top = mafat_attn::max_nan(top, sml[(w * R + r) * 2]);
-        const float off = top == -INFINITY ? 0.f : -top * a.scale_log2;
+        const float off = mafat_attn::subtrahend(top);
         float sum = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kFewWarps; ++w) {
-            const float x = mafat_attn::exp2_fast(fmaf(sml[(w * R + r) * 2], a.scale_log2, off));
+            const float x = mafat_attn::exp2_fast(sml[(w * R + r) * 2] - off);
             sum = fmaf(x, sml[(w * R + r) * 2 + 1], sum);
             const float4 u = load4(so + (w * R + r) * DP + d);
             v = make_float4(fmaf(x, u.x, v.x), fmaf(x, u.y, v.y), fmaf(x, u.z, v.z), fmaf(x, u.w, v.w));

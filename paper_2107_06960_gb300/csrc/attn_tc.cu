@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : at.limit(a, b);
         const float c = a.scale_log2;
         const int n_tiles = slot < live ? t.n : 0;
-        float m = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
+        float from = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;  // the base in use: at most 2^8 below the maximum
         int buf = slot;
         uint32_t uses = 0u;  // parity of the buffer's uses
         for (int j = 0; j < n_tiles; ++j) {
@@ -464,16 +464,17 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         top[i] = k + 4 < C::kCols ? max3(top[i], __uint_as_float(s[k]), __uint_as_float(s[k + 4]))
                                                   : mafat_attn::max_nan(top[i], __uint_as_float(s[k]));
                 }
-                float mt = max3(mafat_attn::max_nan(top[0], top[1]), top[2], top[3]);
-                // also where m is -inf and mt is not.  After it both halves have read their scores: P may be written over them.
-                if (either(j == 0 || (mt - m) * c > kRescaleLog2)) {
-                    mt = joined(mt, [](float x, float y) { return mafat_attn::max_nan(x, y); });
+                const float mt = max3(mafat_attn::max_nan(top[0], top[1]), top[2], top[3]);
+                // also where the base is -inf and mt is not.  After it both halves have read their scores: P may be
+                // written over them.
+                if (either(j == 0 || mt * c - from > kRescaleLog2)) {
+                    const float next = joined(mt, [](float x, float y) { return mafat_attn::max_nan(x, y); }) * c;
                     if (j == 0) {
-                        m = mt;  // there is no O yet
+                        from = next;  // there is no O yet
                     } else {
-                        const bool up = (mt - m) * c > kRescaleLog2;
-                        const float keep = up ? mafat_attn::exp2_fast((m - mt) * c) : 1.f;
-                        if (up) m = mt;
+                        const bool up = next - from > kRescaleLog2;
+                        const float keep = up ? mafat_attn::exp2_fast(from - next) : 1.f;
+                        if (up) from = next;
                         l0 *= keep;
                         l1 *= keep;
                         if (ahead) {  // the scores were made before the product that O waits for
@@ -492,7 +493,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         }
                     }
                 }
-                const float off = m == -CUDART_INF_F ? 0.f : -m * c;  // nothing readable yet: 2^-inf = 0
+                const float off = -mafat_attn::subtrahend(from);
 #pragma unroll
                 for (int h = 0; h < C::kCols / 32; ++h) {
                     uint32_t p[16];
@@ -534,13 +535,13 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             const mafat_attn::Out w(a, b, at);
             if constexpr (kJoins) {
                 mafat_attn::launch_wait();
-                const mafat_attn::Join jn(a, w, m, l);
+                const mafat_attn::Join jn(a, w, from, l);
                 inv = jn.own;
                 join_top = jn.top;
                 join_inv = jn.inv;
                 if (row < g.rows && half == 0 && a.lse) a.lse[w.row] = jn.lse2 * CUDART_LN2_F;
             } else if (row < g.rows && half == 0) {
-                mafat_attn::store_lse(a, w, m, l);
+                mafat_attn::store_lse(a, w, from, l);
             }
             const bool part = !a.direct, none = t.n == 0 || l == 0.f;
             uint8_t* buf = mine + (quarter * C::kHalves + half) * 32 * C::kOutBytes;

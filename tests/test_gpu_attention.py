@@ -349,3 +349,22 @@ def test_without_lse_and_with_raw_addresses(mf, dtype):
         with pytest.raises(mf.MafatError):
             plan.run(**addresses, **{name: o[1].data_ptr() + 1}, stream=s)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_long_fp32_sums_round_as_sums_do(mf, kernel):
+    """24000 keys of nearly equal weight in one part: O is a random walk of n terms, whose every addition rounds by
+    2^-25 of it (root mean square, about), so 2^-25 sqrt(n / 2) of the result; twice that, and 1e-6 for the weights.
+    A factor a tile that is not exactly 1 where the maximum stays would show as a drift of the weights."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(12)
+    T, S, D = 6, 24000, 64
+    q, k, v = (_randn(g, s, torch.float32) for s in ((1, T, 4, D), (1, S, 1, D), (1, S, 1, D)))
+    k[0, 0] = 3 * q[0, 0, 0] / q[0, 0, 0].norm() ** 2 * 8 / 0.37  # the maximum comes first for one row
+    o = torch.empty_like(q)
+    plan = mf.CrossAttention(1, T, S, 4, 1, D, dtype=mf.FP32, kernel=kernel, splits=1, scale=0.37 / 8)
+    plan.run(q, k, v, o)
+    plan.sync_status(like=q)
+    ref = attention64(q[0], [(k[0], v[0], torch.ones(T, S, dtype=torch.bool, device="cuda"))], 0.37 / 8)[0]
+    off = ((o[0].double() - ref).square().mean() / ref.square().mean()).sqrt().item()
+    assert off <= 2 * 2.0 ** -25 * math.sqrt(S / 2) + 1e-6, off
