@@ -224,7 +224,7 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
         // row tiles of a sequence read its keys together
         g.splits = choose_splits(sh, work, tiles, (int64_t)sms * sh.ctas,
                                  2. * sh.keys * p.dim * (p.dtype == MAFAT_BF16 ? 2 : 4) / g.row_tiles,
-                                 4. * p.dim * (double)p.rows_total, p.dim <= 64 ? 32 : 16);
+                                 4. * p.dim * (double)p.rows_total, p.n_run == 2 || p.dim <= 64 ? 32 : 16);
     if (work * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many items of work");
     g.items = (int32_t)(work * g.splits);
     // the kernel for few rows takes item after item
