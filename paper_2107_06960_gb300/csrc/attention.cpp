@@ -47,6 +47,7 @@ struct mafat_attn_s {
     // launches: the segments that have room for keys, or the first if none has
     int n_run = 0, run[2] = {0, 0};
     int parts = 0;
+    int cluster = 1;      // CTAs of a cluster that joins its parts itself
     bool joined = false;  // the second launch joins the first one's parts with its own results
     int64_t rows_total = 0, workspace_bytes = 0;
     void* workspace = nullptr;
@@ -172,6 +173,8 @@ bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
 
 // Most parts that a tile of many rows joins at its end: a thread reads them one after another.
 constexpr int kTileJoin = 4;
+constexpr int kMostCluster = 8;
+constexpr double kClusterJoinUs = 1.0, kClusterGainUs = 1.0;
 // Most rows for which the kernels for few rows are taken.  bf16: one tile of 16 (at 32 rows over 64 sequences
 // of 1444 keys its second pass over the keys makes it 70 us against 35 of the tensor-core tiles; at 16 both take 36, and less
 // of it to start).  fp32: three tiles of 8 (144 us against 182 at 24 rows, 190 against 182 at 32).
@@ -188,21 +191,25 @@ AttnKernel choose_kernel(int32_t dtype, int32_t asked, int32_t rows, int32_t n) 
 // Parts of the keys: the number that the model below gives the least time.  The CTAs run in waves of
 // `slots`, each for its tiles of keys, which take as long as their bytes do at the memory's rate where that is
 // more; parts are written and read again, join_round of a row at a time, by a launch that joins them.  Fewer win a tie (1 %).
-int32_t choose_splits(const AttnShape& sh, int64_t items, int64_t tiles, int64_t slots, double tile_bytes, double part_bytes,
-                      int join_round) {
-    constexpr double kBytesPerUs = 6.2e6, kJoinUs = 0.2, kJoinRoundUs = 1.6, kJoinBytesPerUs = 6e6;
-    int32_t best = 1;
-    double best_us = 0.;
+struct Split {
+    int32_t n;
+    double us;
+};
+double tiles_us(const AttnShape& sh, int64_t items, int64_t tiles, int64_t slots, double tile_bytes, int32_t n) {
+    constexpr double kBytesPerUs = 6.2e6;
+    const int64_t ctas = items * n, waves = (ctas + slots - 1) / slots, each = (tiles + n - 1) / n;
+    const double tile_us = std::max(sh.tile_us, (double)std::min(ctas, slots) * tile_bytes / kBytesPerUs);
+    return (double)waves * ((double)each * tile_us + sh.setup_us);
+}
+Split choose_splits(const AttnShape& sh, int64_t items, int64_t tiles, int64_t slots, double tile_bytes, double part_bytes,
+                    int join_round) {
+    constexpr double kJoinUs = 0.2, kJoinRoundUs = 1.6, kJoinBytesPerUs = 6e6;
+    Split best{1, 0.};
     for (int32_t n = 1; n <= MAFAT_ATTN_MAX_SPLITS && n <= tiles; ++n) {
-        const int64_t ctas = items * n, waves = (ctas + slots - 1) / slots, each = (tiles + n - 1) / n;
-        const double tile_us = std::max(sh.tile_us, (double)std::min(ctas, slots) * tile_bytes / kBytesPerUs);
-        double us = (double)waves * ((double)each * tile_us + sh.setup_us);
+        double us = tiles_us(sh, items, tiles, slots, tile_bytes, n);
         if (n > 1)
             us += kJoinUs + (n + join_round - 1) / join_round * kJoinRoundUs + 2. * n * part_bytes / kJoinBytesPerUs;
-        if (n == 1 || us < 0.99 * best_us) {
-            best_us = us;
-            best = n;
-        }
+        if (n == 1 || us < 0.99 * best.us) best = {n, us};
     }
     return best;
 }
@@ -220,11 +227,25 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
         g.splits = (int32_t)std::min<int64_t>(c.splits, tiles);
     else if (second && (2 * work >= sms || tiles <= 8))
         g.splits = 1;  // whole: it then joins the first launch's parts itself
-    else
+    else {
         // row tiles of a sequence read its keys together
-        g.splits = choose_splits(sh, work, tiles, (int64_t)sms * sh.ctas,
-                                 2. * sh.keys * p.dim * (p.dtype == MAFAT_BF16 ? 2 : 4) / g.row_tiles,
-                                 4. * p.dim * (double)p.rows_total, p.n_run == 2 || p.dim <= 64 ? 32 : 16);
+        const double tile_bytes = 2. * sh.keys * p.dim * (p.dtype == MAFAT_BF16 ? 2 : 4) / g.row_tiles;
+        const int64_t slots = (int64_t)sms * sh.ctas;
+        const Split best = choose_splits(sh, work, tiles, slots, tile_bytes, 4. * p.dim * (double)p.rows_total,
+                                         p.n_run == 2 || p.dim <= 64 ? 32 : 16);
+        g.splits = best.n;
+        // Small calls: a cluster joins its parts itself, which saves the launch for it.  bf16: 5.2 us against 5.8 for one
+        // token of 8 heads over 1444 states, 7.6 against 8.7 for 16 requests, 6.5 against 7.8 for 4 over 676 of 32
+        // heads; fp32's longer tiles want more parts than a cluster has more often.
+        if (p.n_run == 1 && is_rows(g.kernel) && g.row_tiles == 1 && best.n > 1)
+            for (int32_t n = kMostCluster; n > 1; n /= 2)
+                if (n <= tiles && work * n <= slots &&
+                    tiles_us(sh, work, tiles, slots, tile_bytes, n) + kClusterJoinUs <=
+                        best.us + (p.dtype == MAFAT_BF16 ? kClusterGainUs : 0.)) {
+                    g.splits = p.cluster = n;
+                    break;
+                }
+    }
     if (work * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many items of work");
     g.items = (int32_t)(work * g.splits);
     // the kernel for few rows takes item after item
@@ -281,6 +302,7 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
         p->joined = last.splits == 1 && first.splits <= (last.kernel == kRows ? mafat_attn_rows_join() : kTileJoin);
         if (p->joined) p->parts = first.splits;
     }
+    if (p->cluster > 1) p->parts = 1;  // none goes through the workspace
     const int64_t lse_bytes = (p->rows_total * p->parts * 4 + 255) / 256 * 256;
     p->workspace_bytes = kStatusBytes + (p->parts > 1 || p->joined ? lse_bytes + p->rows_total * p->parts * p->dim * 4 : 0);
     if (!p->dry_run) {
@@ -378,6 +400,7 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         x.items = g.items;
         a.overlap = r > 0;
         a.join = r > 0 && p->joined ? p->parts : 0;
+        a.cluster = p->cluster;
         a.direct = a.join || (p->parts == 1 && !p->joined);
         if (is_tc(g.kernel)) {
             CUtensorMap k, v;

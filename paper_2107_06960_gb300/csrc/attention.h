@@ -56,6 +56,8 @@ struct MafatAttnArgs {
     int32_t parts;              // parts of a row, over all segments
     // 1: the CTA that has the row writes its result, joined with the `join` parts of an earlier launch; 0: it writes a part
     int32_t direct, join;
+    // more than 1: the CTAs with a row's parts are a cluster of this many, and join them among themselves
+    int32_t cluster;
     float scale_log2;           // softmax scale times log2(e)
     float* part_o;              // [parts][rows_total][dim] results of the parts, each normalised
     float* part_lse;            // [parts][rows_total] their log2 of the sum of exponentials
@@ -102,19 +104,28 @@ struct MafatNormArgs {
 };
 // Launches fn with programmatic stream serialisation: it may start while the launch before it ends,
 // and waits (griddepcontrol.wait) before it touches memory.
+// Clusters of `cluster` CTAs along x.
 template <class... P, class... A>
-cudaError_t mafat_launch_overlapped(void (*fn)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A&... args) {
+cudaError_t mafat_launch_clusters(int cluster, void (*fn)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                                  const A&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute at = {};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, fn, P(args)...);
+}
+template <class... P, class... A>
+cudaError_t mafat_launch_overlapped(void (*fn)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A&... args) {
+    return mafat_launch_clusters(1, fn, grid, block, smem, s, args...);
 }
 
 enum MafatNormQuant { MAFAT_NORM_PLAIN = 0, MAFAT_NORM_ROW = 1, MAFAT_NORM_BLOCK = 2 };

@@ -28,7 +28,7 @@ struct Cfg {
     static constexpr int kQ = 16 * DP * 2;
     static constexpr int kOffJoin = kOffQ + 2 * kQ;
     static constexpr int kPitch = DP + 4;                // floats of a row of O while the warps are joined
-    static constexpr int kSmem = kOffJoin + kWarps * 16 * (kPitch + 2) * 4;
+    static constexpr int kSmem = kOffJoin + (kWarps * 16 * (kPitch + 2) + 16) * 4;
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     const int v_row = (mi % 2) * 8 + mj, v_chunk = mi / 2;   // V: channels 0-7 and 8-15, each with keys 0-7 and 8-15
     float* so = (float*)(sm + C::kOffJoin);
     float* sml = so + kWarps * 16 * C::kPitch;
+    float* part_lse = sml + kWarps * 16 * 2;  // of a row, for the cluster
 
     uint32_t which = 0u;
 #pragma unroll 1
@@ -332,15 +333,21 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                 if (mine && d == 0 && a.lse)
                     a.lse[out.row] = total == 0.f ? -CUDART_INF_F : (base + log2f(total)) * CUDART_LN2_F;
             } else if (mine && d == 0) {
-                mafat_attn::store_lse(a, out, top, sum);
+                if (a.cluster > 1)
+                    part_lse[r] = mafat_attn::row_lse2(top, sum);
+                else
+                    mafat_attn::store_lse(a, out, top, sum);
             }
             if (!mine || d >= a.dim) continue;
             v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-            if (a.direct)
+            if (a.cluster > 1)  // in place of the first warp's, which this thread has read
+                *reinterpret_cast<float4*>(so + r * C::kPitch + d) = v;
+            else if (a.direct)
                 *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + out.o + d) = make_uint2(pack(v.x, v.y), pack(v.z, v.w));
             else
                 *reinterpret_cast<float4*>(a.part_o + out.part * a.dim + d) = v;
         }
+        if (a.cluster > 1) mafat_attn::join_cluster<__nv_bfloat16, kWarps>(a, b, so, C::kPitch, part_lse, rows);
     }
     wait_copies<0>();
     mafat_attn::launch_end(a);
@@ -348,7 +355,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
-    return mafat_launch_overlapped(attn_rows_kernel<DP>, (unsigned)ctas, kThreads, Cfg<DP>::kSmem, s, a);
+    return mafat_launch_clusters(a.cluster, attn_rows_kernel<DP>, (unsigned)ctas, kThreads, Cfg<DP>::kSmem, s, a);
 }
 template <int DP>
 cudaError_t prepare() {

@@ -294,7 +294,7 @@ struct Few {
     static constexpr int kStage = kRun * (kPitch + DP);               // floats of a run of K and V
     static constexpr int kWarp = kStages * kStage + R * kRun;         // and the weights
     static constexpr int kSmem = (R * DP + kFewWarps * kWarp) * 4;
-    static_assert(kFewWarps * R * (DP + 2) <= kFewWarps * kWarp, "the join's space is the rings'");
+    static_assert(kFewWarps * R * (DP + 2) + R <= kFewWarps * kWarp, "the join's space is the rings'");
 };
 
 template <int R, int DP>
@@ -420,6 +420,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
     // join the warps: O, base and l of each in shared memory
     float* so = sm + R * DP;
     float* sml = so + kFewWarps * R * DP;
+    float* part_lse = sml + kFewWarps * R * 2;  // of a row, for the cluster
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -449,9 +450,16 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
             const float4 u = load4(so + (w * R + r) * DP + d);
             v = make_float4(fmaf(x, u.x, v.x), fmaf(x, u.y, v.y), fmaf(x, u.z, v.z), fmaf(x, u.w, v.w));
         }
-        const Writer w(a, b, b.row0 + r, top, sum, d == 0);
-        w.put(a, d, v);
+        if (a.cluster > 1) {  // in place of the first warp's, which this thread has read
+            const float inv = mafat_attn::inverse_sum(sum);
+            store4(so + r * DP + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+            if (d == 0) part_lse[r] = mafat_attn::row_lse2(top, sum);
+        } else {
+            const Writer w(a, b, b.row0 + r, top, sum, d == 0);
+            w.put(a, d, v);
+        }
     }
+    if (a.cluster > 1) mafat_attn::join_cluster<float, kFewWarps>(a, b, so, DP, part_lse, rows);
     mafat_attn::launch_end(a);
 }
 
@@ -461,7 +469,7 @@ cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
 }
 template <int R, int DP>
 cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
-    return mafat_launch_overlapped(attn_simt_few_kernel<R, DP>, a.seg.items, Few<R, DP>::kThreads, Few<R, DP>::kSmem, s, a);
+    return mafat_launch_clusters(a.cluster, attn_simt_few_kernel<R, DP>, a.seg.items, Few<R, DP>::kThreads, Few<R, DP>::kSmem, s, a);
 }
 cudaError_t prepare(const void* fn, int smem) {
     return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);

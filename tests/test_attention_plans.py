@@ -75,7 +75,9 @@ def test_splits_cover_the_keys_and_the_workspace_their_parts(mf, dtype):
         for n_q in (1, 5, 700):
             for splits in (0, 1, 7, 128):
                 s = mf.CrossAttention(**{**CROSS, "n_kv": n_kv, "n_q": n_q, "splits": splits, "dtype": dtype}).stats()
-                assert 1 <= s["splits"][0] <= mf.MAX_SPLITS and s["parts"] == s["splits"][0]
+                assert 1 <= s["splits"][0] <= mf.MAX_SPLITS
+                # a cluster of CTAs joins the parts of a small call without the workspace
+                assert s["parts"] == s["splits"][0] or (splits == 0 and s["parts"] == 1 and s["splits"][0] in (2, 4, 8))
                 assert s["launches_per_run"] == (1 if s["parts"] == 1 else 2)
                 rows = 2 * n_q * 8
                 assert s["workspace_bytes"] >= (rows * s["parts"] * (64 + 1) * 4 if s["parts"] > 1 else 0)
