@@ -19,13 +19,18 @@ mafat_status mafat_internal_fail(mafat_status s, const char* msg);
 void mafat_internal_clear_error();
 void* mafat_internal_encode_tiled();
 
-// A kernel, the shape of its work and what it takes (measured on GB300, back to back).
+// A kernel, the shape of its work and the time that it takes, in us, measured on GB300 with launches back to back over
+// 16 to 400 sequences of 32 to 1444 keys: the terms of Model::us.
 enum AttnKernel { kSimt4, kSimt8, kSimt64, kRows, kTc1, kTc2 };
 struct AttnShape {
-    int rows, keys;   // of a CTA's tile
-    int ctas;         // of an SM that do not slow each other down
-    double tile_us;   // a tile of keys, where memory does not bound it
-    double setup_us;  // the start and end of an item
+    int rows, keys;  // of a CTA's tile
+    int ctas;        // of an SM
+    double fixed;    // a launch
+    double setup;    // start and end of an item
+    double tile;     // a tile of keys, for a CTA that has its SM alone
+    double shared;   // the same with another CTA on the SM
+    double sm_item, sm_tile;  // an SM's time for an item and a tile when it has many (0: as above)
+    double part;     // writing a part instead of a result
 };
 
 // One set of keys as a plan sees it.
@@ -159,95 +164,120 @@ mafat_status check_common(const Common& c) {
 
 AttnShape shape_of(AttnKernel k, int dim) {
     const bool wide = dim > 64;
-    const int simt = mafat_attn_simt_keys();
+    const int simt = mafat_attn_simt_keys(), rows = mafat_attn_rows_keys();
     switch (k) {
-        case kRows: return {16, mafat_attn_rows_keys(), 2, wide ? 0.95 : 0.45, 0.7};
-        case kTc1: return {128, 128, 2, wide ? 1.1 : 0.95, 3.0};
-        case kTc2: return {256, 128, 1, wide ? 1.5 : 1.0, 4.0};
-        case kSimt64: return {64, simt, 1, wide ? 7.8 : 3.9, 3.0};
-        case kSimt8: return {8, simt, wide ? 1 : 2, 1.2, 2.0};
-        default: return {4, simt, wide ? 1 : 2, 1.2, 2.0};
+        case kRows:
+            return wide ? AttnShape{16, rows, 2, 3.2, 0.4, 0.87, 1.05, 1.1, 0.63, 0} : AttnShape{16, rows, 2, 2.7, 0.3, 0.5, 0.72, 0.65, 0.36, 0};
+        case kTc1: return wide ? AttnShape{128, 128, 2, 0.2, 4.5, 1.15, 2.3, 0, 0, 1.5} : AttnShape{128, 128, 2, 0.7, 2.8, 0.96, 1.45, 0, 0, 1.0};
+        case kTc2: return wide ? AttnShape{256, 128, 1, 0.35, 5.25, 1.45, 1.45, 0, 0, 1.5} : AttnShape{256, 128, 1, 0.5, 4.2, 1.05, 1.05, 0, 0, 1.0};
+        case kSimt64: return wide ? AttnShape{64, simt, 1, 2.0, 1.2, 7.8, 7.8, 0, 0, 0} : AttnShape{64, simt, 1, 2.0, 1.2, 4.4, 4.4, 0, 0, 0};
+        case kSimt8: return wide ? AttnShape{8, simt, 1, 2.8, 0.8, 1.9, 1.9, 0, 0, 0} : AttnShape{8, simt, 2, 2.5, 0.5, 1.17, 2.0, 1.0, 1.02, 0};
+        default: return wide ? AttnShape{4, simt, 1, 2.8, 0.8, 1.2, 1.2, 0, 0, 0} : AttnShape{4, simt, 2, 2.5, 0.5, 0.7, 1.2, 0.8, 0.6, 0};
     }
 }
 bool is_tc(AttnKernel k) { return k == kTc1 || k == kTc2; }
 
-// Most parts that a tile of many rows joins at its end: a thread reads them one after another.
-constexpr int kTileJoin = 4;
-constexpr int kMostCluster = 8;
-constexpr double kClusterJoinUs = 1.0, kClusterGainUs = 1.0;
-// Most rows for which the kernels for few rows are taken.  bf16: one tile of 16 (at 32 rows over 64 sequences
-// of 1444 keys its second pass over the keys makes it 70 us against 35 of the tensor-core tiles; at 16 both take 36, and less
-// of it to start).  fp32: three tiles of 8 (144 us against 182 at 24 rows, 190 against 182 at 32).
-constexpr int kFewRows = 16, kFewRows32 = 24;
 bool is_rows(AttnKernel k) { return k == kSimt4 || k == kSimt8 || k == kRows; }
 
-AttnKernel choose_kernel(int32_t dtype, int32_t asked, int32_t rows, int32_t n) {
-    const bool few = asked == MAFAT_ATTN_ROWS || (asked == MAFAT_ATTN_AUTO && rows <= (dtype == MAFAT_FP32 ? kFewRows32 : kFewRows));
-    if (dtype == MAFAT_FP32) return few ? (rows <= 4 ? kSimt4 : kSimt8) : kSimt64;
-    if (few || n == 0) return kRows;  // without keys there is nothing to map
-    return rows <= 128 ? kTc1 : kTc2;
-}
+// What a segment asks of a kernel, and how long that takes.
+struct Model {
+    AttnShape sh;
+    int sms;
+    int64_t items, tiles;  // (sequence, key head, tile of rows); tiles of keys of each
+    double bytes;          // of all keys and values, once
+    double part_bytes;     // of one part of all rows
+    int join_round;        // parts of a row that a join reads together
 
-// Parts of the keys: the number that the model below gives the least time.  The CTAs run in waves of
-// `slots`, each for its tiles of keys, which take as long as their bytes do at the memory's rate where that is
-// more; parts are written and read again, join_round of a row at a time, by a launch that joins them.  Fewer win a tie (1 %).
-struct Split {
-    int32_t n;
+    // n parts: waves of CTAs, the SMs' throughput or the memory's, whichever is longest
+    double us(int32_t n) const {
+        const int64_t ctas = items * n, slots = (int64_t)sms * sh.ctas, waves = (ctas + slots - 1) / slots;
+        const double each = (double)((tiles + n - 1) / n);
+        double t = sh.fixed + (double)waves * (sh.setup + each * (ctas <= sms ? sh.tile : sh.shared));
+        if (sh.sm_tile > 0) t = std::max(t, sh.fixed + (double)ctas / sms * (sh.sm_item + each * sh.sm_tile));
+        return std::max(t, sh.fixed + sh.setup + bytes / 6.2e6);
+    }
+    // a launch that joins n parts: round trips, and the parts' bytes there and back
+    double join_us(int32_t n) const {
+        return sh.part + 0.2 + 1.6 * ((n + join_round - 1) / join_round) + 2. * n * part_bytes / 6e6;
+    }
+};
+struct Choice {
+    int32_t n;       // parts
+    int cluster;     // CTAs of a cluster that joins them, or 1
     double us;
 };
-double tiles_us(const AttnShape& sh, int64_t items, int64_t tiles, int64_t slots, double tile_bytes, int32_t n) {
-    constexpr double kBytesPerUs = 6.2e6;
-    const int64_t ctas = items * n, waves = (ctas + slots - 1) / slots, each = (tiles + n - 1) / n;
-    const double tile_us = std::max(sh.tile_us, (double)std::min(ctas, slots) * tile_bytes / kBytesPerUs);
-    return (double)waves * ((double)each * tile_us + sh.setup_us);
-}
-Split choose_splits(const AttnShape& sh, int64_t items, int64_t tiles, int64_t slots, double tile_bytes, double part_bytes,
-                    int join_round) {
-    constexpr double kJoinUs = 0.2, kJoinRoundUs = 1.6, kJoinBytesPerUs = 6e6;
-    Split best{1, 0.};
-    for (int32_t n = 1; n <= MAFAT_ATTN_MAX_SPLITS && n <= tiles; ++n) {
-        double us = tiles_us(sh, items, tiles, slots, tile_bytes, n);
-        if (n > 1)
-            us += kJoinUs + (n + join_round - 1) / join_round * kJoinRoundUs + 2. * n * part_bytes / kJoinBytesPerUs;
-        if (n == 1 || us < 0.99 * best.us) best = {n, us};
+
+// The number of parts of the least time; fewer win a tie (1 %).
+Choice choose_splits(const Model& m) {
+    Choice best{1, 1, m.us(1)};
+    for (int32_t n = 2; n <= MAFAT_ATTN_MAX_SPLITS && n <= m.tiles; ++n) {
+        const double us = m.us(n) + m.join_us(n);
+        if (us < 0.99 * best.us) best = {n, 1, us};
     }
     return best;
 }
 
-// The work of a segment: tiles of rows, parts of the keys.
+// Most parts that a tile of many rows joins at its end, and that a cluster has.
+constexpr int kTileJoin = 16, kMostCluster = 8;
+// What a cluster's join takes, and the joining of another launch's parts is worth.
+constexpr double kClusterJoinUs = 0.7, kOwnJoinUs = 1.0;
+
+int64_t row_tiles(const AttnShape& sh, int32_t rows) { return (rows + sh.rows - 1) / sh.rows; }
+
+// The work of a segment: the kernel, tiles of rows, parts of the keys.
 mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms, bool second) {
-    g.rows = g.reqs * p.n_q * (p.heads_q / p.heads_kv);
-    g.kernel = choose_kernel(p.dtype, c.kernel, g.rows, g.n);
-    const AttnShape sh = shape_of(g.kernel, p.dim);
-    g.row_tiles = (g.rows + sh.rows - 1) / sh.rows;
-    const int64_t work = (int64_t)g.n_seq * p.heads_kv * g.row_tiles;
-    const int64_t tiles = std::max<int64_t>(1, ((int64_t)g.n + sh.keys - 1) / sh.keys);
     if (g.n > kMaxI32 - 65536) return fail(MAFAT_EUNSUPPORTED, "too many keys");
-    if (c.splits)
-        g.splits = (int32_t)std::min<int64_t>(c.splits, tiles);
-    else if (second && (2 * work >= sms || tiles <= 8))
-        g.splits = 1;  // whole: it then joins the first launch's parts itself
-    else {
-        // row tiles of a sequence read its keys together
-        const double tile_bytes = 2. * sh.keys * p.dim * (p.dtype == MAFAT_BF16 ? 2 : 4) / g.row_tiles;
-        const int64_t slots = (int64_t)sms * sh.ctas;
-        const Split best = choose_splits(sh, work, tiles, slots, tile_bytes, 4. * p.dim * (double)p.rows_total,
-                                         p.n_run == 2 || p.dim <= 64 ? 32 : 16);
-        g.splits = best.n;
-        // Small calls: a cluster joins its parts itself, which saves the launch for it.  bf16: 5.2 us against 5.8 for one
-        // token of 8 heads over 1444 states, 7.6 against 8.7 for 16 requests, 6.5 against 7.8 for 4 over 676 of 32
-        // heads; fp32's longer tiles want more parts than a cluster has more often.
-        if (p.n_run == 1 && is_rows(g.kernel) && g.row_tiles == 1 && best.n > 1)
-            for (int32_t n = kMostCluster; n > 1; n /= 2)
-                if (n <= tiles && work * n <= slots &&
-                    tiles_us(sh, work, tiles, slots, tile_bytes, n) + kClusterJoinUs <=
-                        best.us + (p.dtype == MAFAT_BF16 ? kClusterGainUs : 0.)) {
-                    g.splits = p.cluster = n;
-                    break;
-                }
+    g.rows = g.reqs * p.n_q * (p.heads_q / p.heads_kv);
+    const bool bf16 = p.dtype == MAFAT_BF16;
+    AttnKernel kernels[3];
+    int n_kernels = 0;
+    if (c.kernel != MAFAT_ATTN_TILES || g.n == 0) {  // without keys there is nothing to map
+        if (bf16)
+            kernels[n_kernels++] = kRows;
+        else
+            kernels[n_kernels++] = g.rows <= 4 ? kSimt4 : kSimt8;
     }
-    if (work * g.splits > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many items of work");
-    g.items = (int32_t)(work * g.splits);
+    if (c.kernel != MAFAT_ATTN_ROWS && g.n > 0) {
+        kernels[n_kernels++] = bf16 ? kTc1 : kSimt64;
+        if (bf16 && g.rows > 128) kernels[n_kernels++] = kTc2;
+    }
+    Choice best{0, 1, 0.};
+    for (int i = 0; i < n_kernels; ++i) {
+        Model m;
+        m.sh = shape_of(kernels[i], p.dim);
+        m.sms = sms;
+        m.items = (int64_t)g.n_seq * p.heads_kv * row_tiles(m.sh, g.rows);
+        m.tiles = std::max<int64_t>(1, ((int64_t)g.n + m.sh.keys - 1) / m.sh.keys);
+        m.bytes = 2. * g.n_seq * g.n * p.heads_kv * p.dim * (bf16 ? 2 : 4);
+        m.part_bytes = 4. * p.dim * (double)p.rows_total;
+        m.join_round = p.n_run == 2 || p.dim <= 64 ? 32 : 16;
+        Choice x = choose_splits(m);
+        if (c.splits) {
+            x = {(int32_t)std::min<int64_t>(c.splits, m.tiles), 1, 0.};
+            x.us = m.us(x.n);
+        } else if (second && m.us(1) <= x.us + kOwnJoinUs) {
+            x = {1, 1, m.us(1)};  // whole: it then joins the first launch's parts itself
+        } else if (p.n_run == 1 && is_rows(kernels[i]) && m.items == (int64_t)g.n_seq * p.heads_kv && x.n > 1) {
+            // A cluster joins its parts itself, which saves the launch for it: 5.2 us against 5.8 for one token of 8
+            // heads over 1444 states, 7.6 against 8.7 for 16 requests, 6.5 against 7.8 for 4 over 676 of 32 heads.
+            for (int32_t n = kMostCluster; n > 1 && x.cluster == 1; n /= 2)
+                // clusters of CTAs that fill their SM find half of the SMs, not all, side by side
+                if (n <= m.tiles && m.items * n <= (int64_t)sms * m.sh.ctas / (m.sh.ctas == 1 ? 2 : 1) &&
+                    m.us(n) + kClusterJoinUs <= x.us)
+                    x = {n, n, m.us(n) + kClusterJoinUs};
+        }
+        if (best.n == 0 || x.us < best.us) {
+            best = x;
+            g.kernel = kernels[i];
+        }
+    }
+    const AttnShape sh = shape_of(g.kernel, p.dim);
+    g.row_tiles = (int32_t)row_tiles(sh, g.rows);
+    g.splits = best.n;
+    p.cluster = best.cluster;
+    const int64_t items = (int64_t)g.n_seq * p.heads_kv * g.row_tiles * g.splits;
+    if (items > kMaxI32 / 4) return fail(MAFAT_EUNSUPPORTED, "too many items of work");
+    g.items = (int32_t)items;
     // the kernel for few rows takes item after item
     g.ctas = g.kernel == kRows ? std::min(g.items, sms * sh.ctas) : g.items;
     g.part0 = p.parts;

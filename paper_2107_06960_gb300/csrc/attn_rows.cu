@@ -78,7 +78,9 @@ struct Ahead {
     }
 };
 
-template <int DP>
+// CLUSTER: a cluster's CTAs have an item's parts and join them (an instance of its own: in one kernel it cost the
+// other form's inner loop 20 %)
+template <int DP, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ MafatAttnArgs a) {
     using C = Cfg<DP>;
     constexpr int kChunks = DP / 8;        // 16-byte chunks of a row
@@ -333,21 +335,21 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                 if (mine && d == 0 && a.lse)
                     a.lse[out.row] = total == 0.f ? -CUDART_INF_F : (base + log2f(total)) * CUDART_LN2_F;
             } else if (mine && d == 0) {
-                if (a.cluster > 1)
+                if constexpr (CLUSTER)
                     part_lse[r] = mafat_attn::row_lse2(top, sum);
                 else
                     mafat_attn::store_lse(a, out, top, sum);
             }
             if (!mine || d >= a.dim) continue;
             v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-            if (a.cluster > 1)  // in place of the first warp's, which this thread has read
+            if constexpr (CLUSTER)  // in place of the first warp's, which this thread has read
                 *reinterpret_cast<float4*>(so + r * C::kPitch + d) = v;
             else if (a.direct)
                 *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + out.o + d) = make_uint2(pack(v.x, v.y), pack(v.z, v.w));
             else
                 *reinterpret_cast<float4*>(a.part_o + out.part * a.dim + d) = v;
         }
-        if (a.cluster > 1) mafat_attn::join_cluster<__nv_bfloat16, kWarps>(a, b, so, C::kPitch, part_lse, rows);
+        if constexpr (CLUSTER) mafat_attn::join_cluster<__nv_bfloat16, kWarps>(a, b, so, C::kPitch, part_lse, rows);
     }
     wait_copies<0>();
     mafat_attn::launch_end(a);
@@ -355,11 +357,15 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
-    return mafat_launch_clusters(a.cluster, attn_rows_kernel<DP>, (unsigned)ctas, kThreads, Cfg<DP>::kSmem, s, a);
+    return mafat_launch_clusters(a.cluster, a.cluster > 1 ? attn_rows_kernel<DP, true> : attn_rows_kernel<DP, false>,
+                                 (unsigned)ctas, kThreads, Cfg<DP>::kSmem, s, a);
 }
 template <int DP>
 cudaError_t prepare() {
-    return cudaFuncSetAttribute(attn_rows_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP>::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               Cfg<DP>::kSmem);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(attn_rows_kernel<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP>::kSmem);
 }
 
 }  // namespace

@@ -297,7 +297,7 @@ struct Few {
     static_assert(kFewWarps * R * (DP + 2) + R <= kFewWarps * kWarp, "the join's space is the rings'");
 };
 
-template <int R, int DP>
+template <int R, int DP, bool CLUSTER>
 __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_few_kernel(const __grid_constant__ MafatAttnArgs a) {
     using L = Few<R, DP>;
     constexpr int kCh = DP / 32;
@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
             const float4 u = load4(so + (w * R + r) * DP + d);
             v = make_float4(fmaf(x, u.x, v.x), fmaf(x, u.y, v.y), fmaf(x, u.z, v.z), fmaf(x, u.w, v.w));
         }
-        if (a.cluster > 1) {  // in place of the first warp's, which this thread has read
+        if constexpr (CLUSTER) {  // in place of the first warp's, which this thread has read
             const float inv = mafat_attn::inverse_sum(sum);
             store4(so + r * DP + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
             if (d == 0) part_lse[r] = mafat_attn::row_lse2(top, sum);
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
             w.put(a, d, v);
         }
     }
-    if (a.cluster > 1) mafat_attn::join_cluster<float, kFewWarps>(a, b, so, DP, part_lse, rows);
+    if constexpr (CLUSTER) mafat_attn::join_cluster<float, kFewWarps>(a, b, so, DP, part_lse, rows);
     mafat_attn::launch_end(a);
 }
 
@@ -469,10 +469,17 @@ cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
 }
 template <int R, int DP>
 cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
-    return mafat_launch_clusters(a.cluster, attn_simt_few_kernel<R, DP>, a.seg.items, Few<R, DP>::kThreads, Few<R, DP>::kSmem, s, a);
+    return mafat_launch_clusters(a.cluster,
+                                 a.cluster > 1 ? attn_simt_few_kernel<R, DP, true> : attn_simt_few_kernel<R, DP, false>,
+                                 a.seg.items, Few<R, DP>::kThreads, Few<R, DP>::kSmem, s, a);
 }
 cudaError_t prepare(const void* fn, int smem) {
     return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+}
+template <int R, int DP>
+cudaError_t prepare_few() {
+    const cudaError_t e = prepare((const void*)attn_simt_few_kernel<R, DP, false>, Few<R, DP>::kSmem);
+    return e != cudaSuccess ? e : prepare((const void*)attn_simt_few_kernel<R, DP, true>, Few<R, DP>::kSmem);
 }
 
 }  // namespace
@@ -481,10 +488,8 @@ int mafat_attn_simt_keys() { return kBN; }
 
 cudaError_t mafat_prepare_attn_simt() {
     cudaError_t e;
-    if ((e = prepare((const void*)attn_simt_few_kernel<4, 64>, Few<4, 64>::kSmem)) != cudaSuccess) return e;
-    if ((e = prepare((const void*)attn_simt_few_kernel<4, 128>, Few<4, 128>::kSmem)) != cudaSuccess) return e;
-    if ((e = prepare((const void*)attn_simt_few_kernel<8, 64>, Few<8, 64>::kSmem)) != cudaSuccess) return e;
-    if ((e = prepare((const void*)attn_simt_few_kernel<8, 128>, Few<8, 128>::kSmem)) != cudaSuccess) return e;
+    if ((e = prepare_few<4, 64>()) != cudaSuccess || (e = prepare_few<4, 128>()) != cudaSuccess) return e;
+    if ((e = prepare_few<8, 64>()) != cudaSuccess || (e = prepare_few<8, 128>()) != cudaSuccess) return e;
     if ((e = prepare((const void*)attn_simt_kernel<64>, Tile<64>::kSmem)) != cudaSuccess) return e;
     return prepare((const void*)attn_simt_kernel<128>, Tile<128>::kSmem);
 }

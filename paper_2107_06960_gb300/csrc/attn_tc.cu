@@ -543,9 +543,9 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             } else if (row < g.rows && half == 0) {
                 mafat_attn::store_lse(a, w, from, l);
             }
-            const bool part = !a.direct, none = t.n == 0 || l == 0.f;
+            const bool part = !a.direct || kJoins, none = t.n == 0 || l == 0.f;  // fp32 on the way
             uint8_t* buf = mine + (quarter * C::kHalves + half) * 32 * C::kOutBytes;
-            const int64_t dst = row >= g.rows ? -1 : part ? w.part * a.dim : w.o;
+            const int64_t dst = row >= g.rows ? -1 : a.direct ? w.o : w.part * a.dim;
             uint8_t* my = buf + lane * C::kOutBytes;
             auto put = [&](int chunk, uint4 v) { *reinterpret_cast<uint4*>(my + ((chunk ^ (lane % kSwz)) * 16)) = v; };
 #pragma unroll
@@ -569,23 +569,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                     // a row without readable keys: 0, whatever the products left
 #pragma unroll
                     for (int k = 0; k < kStep; ++k) o[k] = none ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
-                    if constexpr (kJoins) {
-                        const int d0 = half * kWide + kStep * i;
-                        for (int p = 0; p < a.join; ++p) {
-                            const int64_t at_p = (int64_t)p * a.rows_total + w.row;
-                            const float f = mafat_attn::exp2_fast(a.part_lse[at_p] - join_top) * join_inv;
-                            const float* src = a.part_o + at_p * a.dim + d0;
-#pragma unroll
-                            for (int k = 0; k < kStep; k += 4) {
-                                if (d0 + k >= a.dim) continue;
-                                const float4 v = *reinterpret_cast<const float4*>(src + k);
-                                o[k] = __float_as_uint(fmaf(f, v.x, __uint_as_float(o[k])));
-                                o[k + 1] = __float_as_uint(fmaf(f, v.y, __uint_as_float(o[k + 1])));
-                                o[k + 2] = __float_as_uint(fmaf(f, v.z, __uint_as_float(o[k + 2])));
-                                o[k + 3] = __float_as_uint(fmaf(f, v.w, __uint_as_float(o[k + 3])));
-                            }
-                        }
-                    }
                     if (part) {
 #pragma unroll
                         for (int k = 0; k < kStep / 4; ++k)
@@ -602,16 +585,45 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 __syncwarp();
                 // channel of the lane's chunk
                 const int d = half * kWide + (part ? pass * (kWide / 2) + cc * 4 : cc * 8);
+                constexpr int kPieces = 32 / kRows;  // rows of a lane
+                if constexpr (kJoins) {
+                    float4 v[kPieces];
 #pragma unroll
-                for (int i = 0; i < 32 / kRows; ++i) {
-                    const int r = i * kRows + cr;
-                    const int64_t o = __shfl_sync(0xffffffffu, dst, r);
-                    const uint4 v = *reinterpret_cast<const uint4*>(buf + r * C::kOutBytes + ((cc ^ (r % kSwz)) * 16));
-                    if (o >= 0 && d < a.dim) {
-                        if (part)
-                            *reinterpret_cast<uint4*>(a.part_o + o + d) = v;
-                        else
-                            *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + o + d) = v;
+                    for (int i = 0; i < kPieces; ++i) {
+                        const int r = i * kRows + cr;
+                        v[i] = *reinterpret_cast<const float4*>(buf + r * C::kOutBytes + ((cc ^ (r % kSwz)) * 16));
+                    }
+#pragma unroll 1
+                    for (int p = 0; p < a.join; ++p) {  // a part of all rows at a time, whole rows of it
+                        const float mine_f = mafat_attn::exp2_fast(a.part_lse[(int64_t)p * a.rows_total + w.row] - join_top) * join_inv;
+                        const float* src = a.part_o + (int64_t)p * a.rows_total * a.dim + d;
+#pragma unroll
+                        for (int i = 0; i < kPieces; ++i) {
+                            const int r = i * kRows + cr;
+                            const float f = __shfl_sync(0xffffffffu, mine_f, r);
+                            const int64_t at_row = __shfl_sync(0xffffffffu, w.row, r);
+                            float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (d < a.dim) u = *reinterpret_cast<const float4*>(src + at_row * a.dim);
+                            v[i] = make_float4(fmaf(f, u.x, v[i].x), fmaf(f, u.y, v[i].y), fmaf(f, u.z, v[i].z), fmaf(f, u.w, v[i].w));
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i) {
+                        const int64_t o = __shfl_sync(0xffffffffu, dst, i * kRows + cr);
+                        if (o >= 0 && d < a.dim) mafat_attn::put4((__nv_bfloat16*)a.out + o + d, v[i]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i) {
+                        const int r = i * kRows + cr;
+                        const int64_t o = __shfl_sync(0xffffffffu, dst, r);
+                        const uint4 v = *reinterpret_cast<const uint4*>(buf + r * C::kOutBytes + ((cc ^ (r % kSwz)) * 16));
+                        if (o >= 0 && d < a.dim) {
+                            if (part)
+                                *reinterpret_cast<uint4*>(a.part_o + o + d) = v;
+                            else
+                                *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + o + d) = v;
+                        }
                     }
                 }
                 __syncwarp();
