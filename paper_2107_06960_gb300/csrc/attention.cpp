@@ -587,7 +587,7 @@ mafat_status mafat_rms_norm(const mafat_norm_desc* d, const void* x, const void*
     }
     if (!x || !weight || !y) return fail(MAFAT_EINVAL, "null x, weight or y");
     if (quant != (scales != nullptr)) return fail(MAFAT_EINVAL, "an 8-bit output takes scales, others take none");
-    const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4, osz = quant ? 1 : esz, vec = 16 / esz;
+    const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4, osz = quant ? 1 : esz;
     const int64_t st[4] = {d->x_stride, d->residual_stride, d->residual_out_stride, d->y_stride};
     int64_t row[4];
     for (int i = 0; i < 4; ++i) {
@@ -611,9 +611,10 @@ mafat_status mafat_rms_norm(const mafat_norm_desc* d, const void* x, const void*
             const bool in_place = i < 2 && o != 5 && t[i] == t[o] && row[i] == row[o] && (o != 3 || osz == esz);
             if (!in_place) return fail(MAFAT_EINVAL, "an output overlaps another tensor");
         }
-    bool vectors = d->cols % vec == 0;
+    int64_t steps = d->cols;  // rows start and end on multiples of its lowest bit
     for (int i = 0; i < 4; ++i)
-        if (t[i]) vectors = vectors && row[i] % vec == 0;
+        if (t[i]) steps |= row[i];
+    const int vec = (int)std::min<int64_t>(steps & -steps, 8);
     a.x = x;
     a.residual = residual;
     a.weight = weight;
@@ -627,7 +628,7 @@ mafat_status mafat_rms_norm(const mafat_norm_desc* d, const void* x, const void*
     a.y_s = row[3];
     a.cols = d->cols;
     a.eps = d->eps;
-    const cudaError_t e = mafat_launch_norm(a, d->dtype == MAFAT_BF16, vectors,
+    const cudaError_t e = mafat_launch_norm(a, d->dtype == MAFAT_BF16, vec,
                                             !quant ? MAFAT_NORM_PLAIN : d->scale_group == 0 ? MAFAT_NORM_ROW : MAFAT_NORM_BLOCK,
                                             (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "norm launch");

@@ -131,6 +131,5 @@ cudaError_t mafat_launch_overlapped(void (*fn)(P...), dim3 grid, dim3 block, siz
 enum MafatNormQuant { MAFAT_NORM_PLAIN = 0, MAFAT_NORM_ROW = 1, MAFAT_NORM_BLOCK = 2 };
 
 int mafat_norm_max_cols();  // of a row
-// aligned: every row of every matrix starts on a 16-byte boundary (8-bit rows: one as long as a
-// vector of their channels) and has whole vectors
-cudaError_t mafat_launch_norm(const MafatNormArgs& a, bool bf16, bool aligned, MafatNormQuant quant, cudaStream_t s);
+// vec: a power of two that divides cols and every matrix's row stride: the rows can be accessed by as many channels
+cudaError_t mafat_launch_norm(const MafatNormArgs& a, bool bf16, int vec, MafatNormQuant quant, cudaStream_t s);

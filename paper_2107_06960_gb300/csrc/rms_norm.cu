@@ -67,6 +67,31 @@ struct Vec<__nv_bfloat16, 8> {
     }
 };
 template <>
+struct Vec<float, 2> {
+    float2 u;
+    __device__ __forceinline__ void load(const float* p, bool on) {
+        u = on ? *reinterpret_cast<const float2*>(p) : make_float2(0.f, 0.f);
+    }
+    __device__ __forceinline__ void get(float (&v)[2]) const { v[0] = u.x; v[1] = u.y; }
+    static __device__ __forceinline__ void store(float* p, const float (&v)[2]) {
+        *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    }
+};
+template <>
+struct Vec<__nv_bfloat16, 2> {
+    uint32_t u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool on) {
+        u = on ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+    }
+    __device__ __forceinline__ void get(float (&v)[2]) const {
+        v[0] = __uint_as_float(u << 16);
+        v[1] = __uint_as_float(u & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[2]) {
+        *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(v[0], v[1]);
+    }
+};
+template <>
 struct Vec<float, 1> {
     float u;
     __device__ __forceinline__ void load(const float* p, bool on) { u = on ? *p : 0.f; }
@@ -85,6 +110,8 @@ template <int V>
 __device__ __forceinline__ void store8(uint8_t* p, const float (&v)[V]) {
     if constexpr (V == 1) {
         *p = (uint8_t)__nv_cvt_float_to_fp8(v[0], __NV_SATFINITE, __NV_E4M3);
+    } else if constexpr (V == 2) {
+        *reinterpret_cast<uint16_t*>(p) = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
     } else {
         uint32_t w[V / 4];
 #pragma unroll
@@ -104,8 +131,10 @@ __device__ __forceinline__ void store8(uint8_t* p, const float (&v)[V]) {
 __device__ __forceinline__ void launch_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// of values that are not negative, whose bits are ordered as they are and a NaN's are above all
 template <int WIDTH>
 __device__ __forceinline__ float max_over(float v) {
+    if constexpr (WIDTH == 32) return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 #pragma unroll
     for (int w = 1; w < WIDTH; w *= 2) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, w));
     return v;
@@ -252,12 +281,16 @@ cudaError_t launch(const MafatNormArgs& a, MafatNormQuant q, int warps, cudaStre
 }
 
 // Accesses of a thread: with rows enough to fill the GPU, the fewest that leave a row to one warp (no
-// barrier, more in flight a thread); with few rows as few as 16 warps allow (a row is there sooner).
+// barrier, more in flight a thread), as far as its registers go (with block scales fewer channels: in us, at 16244
+// rows of 1568 fp32 64.6 with 32 a thread, 52.6 with 16, 53.2 with 8; of 1571 bf16 98.7, 83.2, 71.9); with few rows
+// as few as 16 warps allow (a row is there sooner).
 template <class T, int V, int N>
 cudaError_t launch_v(const MafatNormArgs& a, MafatNormQuant q, cudaStream_t s) {
     const int per_warp = 32 * V * N;
+    const int most = q != MAFAT_NORM_BLOCK ? kMaxThread : V == 1 ? 8 : 16;
+    const bool one_warp = a.rows >= kFewRows && 2 * N * V <= most;
     if constexpr (2 * N * V <= kMaxThread)
-        if (a.cols > per_warp * (a.rows < kFewRows ? kMaxWarps : 1)) return launch_v<T, V, 2 * N>(a, q, s);
+        if (a.cols > per_warp * (one_warp ? 1 : kMaxWarps)) return launch_v<T, V, 2 * N>(a, q, s);
     return launch<T, V, N>(a, q, (a.cols + per_warp - 1) / per_warp, s);
 }
 
@@ -265,8 +298,13 @@ cudaError_t launch_v(const MafatNormArgs& a, MafatNormQuant q, cudaStream_t s) {
 
 int mafat_norm_max_cols() { return kMaxWarps * 32 * kMaxThread; }
 
-cudaError_t mafat_launch_norm(const MafatNormArgs& a, bool bf16, bool aligned, MafatNormQuant quant, cudaStream_t s) {
-    // the one-element form takes 4 accesses at least: 128 channels of a warp
-    if (bf16) return aligned ? launch_v<__nv_bfloat16, 8, 1>(a, quant, s) : launch_v<__nv_bfloat16, 1, 4>(a, quant, s);
-    return aligned ? launch_v<float, 4, 1>(a, quant, s) : launch_v<float, 1, 4>(a, quant, s);
+cudaError_t mafat_launch_norm(const MafatNormArgs& a, bool bf16, int vec, MafatNormQuant quant, cudaStream_t s) {
+    // a warp has 128 channels at least: 4 accesses of one, 2 of two
+    if (bf16)
+        return vec >= 8   ? launch_v<__nv_bfloat16, 8, 1>(a, quant, s)
+               : vec >= 2 ? launch_v<__nv_bfloat16, 2, 2>(a, quant, s)
+                          : launch_v<__nv_bfloat16, 1, 4>(a, quant, s);
+    return vec >= 4   ? launch_v<float, 4, 1>(a, quant, s)
+           : vec >= 2 ? launch_v<float, 2, 2>(a, quant, s)
+                      : launch_v<float, 1, 4>(a, quant, s);
 }

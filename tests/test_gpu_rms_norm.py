@@ -87,6 +87,25 @@ def test_row_strides(mf, dt, quant, pad, cols):
 
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("quant", [None, "row", "128"])
+@pytest.mark.parametrize("cols,pad", [(126, 0), (334, 0), (1001, 1), (1568, 2), (1570, 0), (1571, 0)])
+def test_many_rows(mf, dt, quant, cols, pad):
+    """Rows enough for a warp to take a whole row; rows that start on 2, 4 or 8 bytes only."""
+    _norm(mf, 2500, cols, dt, quant, pad=pad)
+
+
+@pytest.mark.parametrize("cols", [256, 250, 251])
+def test_block_of_nan(mf, cols):
+    x = torch.randn((2100, cols), device="cuda")
+    x[7, 3] = -math.nan  # as a sum of squares it reaches all of the row
+    w = torch.ones(cols, device="cuda")
+    y, s = torch.empty((2100, cols), device="cuda", dtype=E4M3), torch.empty((2100, 2), device="cuda")
+    mf.rms_norm(x, w, y, scales=s, scale_group=128)
+    bad = torch.isnan(s).any(-1)
+    assert bad[7] and bad.sum() == 1 and torch.isnan(y[7].float()).all()
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("quant", ["row", "128"])
 def test_zero_blocks_have_scale_one(mf, dt, quant):
     def change(x, r, w):
