@@ -5,13 +5,15 @@
 // raise m to m', and l and O are multiplied by 2^(c' (m - m')), c' = c log2(e).
 //
 // Two neighbouring products are one packed instruction (fma.rn.f32x2, each rounded as alone), which
-// leaves issue slots to the shared-memory reads.  Keys that are not readable are filled with zeros as they
-// are copied (cp.async), so that 0 x NaN cannot reach O.
+// leaves issue slots to the shared-memory reads.  Keys that are not readable are not read: zeros stand in the places of
+// a tile without a key (cp.async fills them), so that 0 x NaN cannot reach O.
 //
 // Many rows (attn_simt_kernel): bound by FMAs and, close behind, by shared-memory reads (83 % of their rate with
 // 60 % of the FMAs').  A CTA takes 64 rows, 64 keys at a time, two CTAs an SM; a thread has 4 rows x 4 keys of the scores, then 4
 // rows x DP / 16 channels of O.  K's and V's tiles are single buffers: the next K is copied while the
-// values are summed, the next V while the scores are made.  A warp with 16 rows x 64 keys (queries and
+// values are summed, the next V while the scores are made.  With a mask the tiles are of readable keys alone: one warp
+// lists the next tile's while the scores are made (8 x 1024 tokens, 8 heads of 64 channels over 1444 states, in us:
+// half of them readable 339, all 633; 643 with tiles of all keys either way).  A warp with 16 rows x 64 keys (queries and
 // weights broadcast, fewer reads an FMA, 8 warps instead of 16) was 4 % slower.
 //
 // Few rows (attn_simt_few_kernel): bound by reading K and V.  The warps of a CTA share the R rows and split the
@@ -111,21 +113,59 @@ struct Tile {
 // that they lie in different banks.
 __device__ __forceinline__ int quad_of(int row, int quad) { return quad ^ (row / 4 % 2); }
 
-// copies ROWS rows of a matrix with `stride` elements between rows; channels past dim and rows that
-// are not readable become zero
-template <int ROWS, int DP, int PITCH, int THREADS, class Ok>
-__device__ __forceinline__ void copy_rows(float* dst, const float* src, int64_t stride, int dim, Ok ok) {
+// copies rows of a matrix with `stride` elements between rows, the r-th from row key(r); channels past dim and rows
+// whose key is negative become zero
+template <int ROWS, int DP, int PITCH, int THREADS, class Key>
+__device__ __forceinline__ void copy_rows(float* dst, const float* src, int64_t stride, int dim, Key key) {
     constexpr int kChunks = DP / 4;
 #pragma unroll 8
     for (int i = threadIdx.x; i < ROWS * kChunks; i += THREADS) {
-        const int r = i / kChunks, c = (i % kChunks) * 4;
-        const bool on = c < dim && ok(r);
-        copy16(dst + r * PITCH + c, src + (on ? (int64_t)r * stride + c : 0), on);
+        const int r = i / kChunks, c = (i % kChunks) * 4, k = key(r);
+        const bool on = c < dim && k >= 0;
+        copy16(dst + r * PITCH + c, src + (on ? (int64_t)k * stride + c : 0), on);
     }
     copies_done();
 }
 
-template <int DP>
+// Lists the readable keys of a part, kBN at a time, by one warp.  The bytes of the mask that a list starts with are
+// read before they are used.
+struct Readable {
+    static constexpr int kBytes = 4;  // of a lane
+    const uint8_t* mask;
+    int pos, end, lane;
+    uint8_t m[kBytes];
+    __device__ __forceinline__ void read() {
+#pragma unroll
+        for (int i = 0; i < kBytes; ++i) m[i] = pos + 32 * i + lane < end ? mask[pos + 32 * i + lane] : 0;
+    }
+    // the key of place r goes to list[r * PITCH], -1 to the places after the last; returns how many there are
+    template <int PITCH>
+    __device__ __forceinline__ int list(int* list) {
+        int n = 0;
+#pragma unroll 1
+        for (;;) {
+#pragma unroll
+            for (int i = 0; i < kBytes; ++i) {
+                const uint32_t on = __ballot_sync(0xffffffffu, m[i] != 0);
+                const int at = n + __popc(on & ((1u << lane) - 1u));
+                if (m[i] != 0 && at < kBN) list[at * PITCH] = pos + 32 * i + lane;
+                n += __popc(on);
+            }
+            if (n >= kBN) {
+                __syncwarp();
+                pos = list[(kBN - 1) * PITCH] + 1;
+                return kBN;
+            }
+            pos += 32 * kBytes;
+            if (pos >= end) break;
+            read();
+        }
+        for (int r = n + lane; r < kBN; r += 32) list[r * PITCH] = -1;
+        return n;
+    }
+};
+
+template <int DP, bool MASK>
 __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __grid_constant__ MafatAttnArgs a) {
     using L = Tile<DP>;
     extern __shared__ __align__(16) float sm[];
@@ -139,16 +179,24 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
     const int tx = threadIdx.x % kTX, ty = threadIdx.x / kTX;
     const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
     const float* vp = (const float*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
-    const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
-    auto copy_k = [&](int key0) {
-        copy_rows<kBN, DP, L::kPitch, L::kThreads>(sk, kp + (int64_t)key0 * g.k_ss, g.k_ss, a.dim, [&](int r) {
-            return key0 + r < b.len && (!mask || mask[key0 + r] != 0);
-        });
+    // MASK: tiles are of readable keys alone, whose numbers stand in two lists in the padding of K's rows
+    int* lists = (int*)(sk + DP);
+    Readable readable{MASK ? g.mask + (int64_t)b.seq * g.n : nullptr, b.key0, min(b.key1, b.len), (int)threadIdx.x, {}};
+    auto list_next = [&](int buf) {
+        const int n = readable.list<L::kPitch>(lists + buf);
+        if (threadIdx.x == 0) lists[2 + buf] = n;
     };
-    auto copy_v = [&](int key0) {
-        copy_rows<kBN, DP, DP, L::kThreads>(sv, vp + (int64_t)key0 * g.v_ss, g.v_ss, a.dim, [&](int r) {
-            return key0 + r < b.len && (!mask || mask[key0 + r] != 0);
-        });
+    int tile = 0, key0 = b.key0;
+    bool more = b.key0 < b.key1;
+    auto key_of = [&](int r) {  // of the tile's place r; negative: none
+        if constexpr (MASK) return lists[r * L::kPitch + (tile & 1)];
+        return key0 + r < b.len ? key0 + r : -1;
+    };
+    auto copy_k = [&]() {
+        copy_rows<kBN, DP, L::kPitch, L::kThreads>(sk, kp, g.k_ss, a.dim, key_of);
+    };
+    auto copy_v = [&]() {
+        copy_rows<kBN, DP, DP, L::kThreads>(sv, vp, g.v_ss, a.dim, key_of);
     };
 
     // queries, then the first keys
@@ -161,7 +209,15 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
             copy16(sq + r * DP + quad_of(r, c / 4) * 4,
                    (const float*)a.q + (on ? mafat_attn::Row(a, b, b.row0 + r).query(a) + c : 0), on);
         }
-        if (b.key0 < b.key1) copy_k(b.key0);
+        if constexpr (MASK) {
+            if (threadIdx.x < 32) {
+                readable.read();
+                list_next(0);
+            }
+            __syncthreads();
+            more = lists[2] > 0;
+        }
+        if (more) copy_k();
         copies_done();
     }
     constexpr int kO = DP / kTX / 2;  // pairs of channels: c * 64 + tx * 4 + {0, 1}, {2, 3}
@@ -178,10 +234,11 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
     }
 
 #pragma unroll 1
-    for (int key0 = b.key0; key0 < b.key1; key0 += kBN) {
+    while (more) {
         wait_copies<0>();
         __syncthreads();  // K is there, and all are done with V
-        copy_v(key0);
+        copy_v();
+        if (MASK && threadIdx.x < 32) readable.read();
         float2 acc[4][4];  // sums over even and odd channels
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -202,20 +259,17 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
                     fma2(acc[i][j], make_float2(x[i].z, x[i].w), make_float2(y[j].z, y[j].w));
                 }
         }
-        bool seen[4];
+        int key[4];
         float keep[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = key0 + tx + kTX * j;
-            seen[j] = k < b.len && (!mask || mask[k] != 0);
-        }
+        for (int j = 0; j < 4; ++j) key[j] = key_of(tx + kTX * j);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float s[4], top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 s[j] = acc[i][j].x + acc[i][j].y;
-                if (!seen[j] || key0 + tx + kTX * j >= limit[i]) s[j] = -INFINITY;
+                if (key[j] < 0 || key[j] >= limit[i]) s[j] = -INFINITY;
                 top = mafat_attn::max_nan(top, s[j]);
             }
 #pragma unroll
@@ -232,9 +286,16 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
             }
             l[i] = l[i] * keep[i] + sum;
         }
+        if (MASK && threadIdx.x < 32) list_next((tile & 1) ^ 1);
         wait_copies<0>();
         __syncthreads();  // V is there, and all are done with K (P is read by the half warp that wrote it)
-        if (key0 + kBN < b.key1) copy_k(key0 + kBN);
+        ++tile;
+        key0 += kBN;
+        if constexpr (MASK)
+            more = lists[2 + (tile & 1)] > 0;
+        else
+            more = key0 < b.key1;
+        if (more) copy_k();
         // the tile's sum by itself, then added: O's size sets the rounding of one addition a tile, not of 64 (6000 keys
         // in one part: 1.4e-6 of the result without it, the weights' 3e-7 with it)
         float2 sum[4][kO];
@@ -465,7 +526,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
 
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
-    return mafat_launch_overlapped(attn_simt_kernel<DP>, a.seg.items, Tile<DP>::kThreads, Tile<DP>::kSmem, s, a);
+    return mafat_launch_overlapped(a.seg.mask ? attn_simt_kernel<DP, true> : attn_simt_kernel<DP, false>, a.seg.items,
+                                   Tile<DP>::kThreads, Tile<DP>::kSmem, s, a);
 }
 template <int R, int DP>
 cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
@@ -475,6 +537,11 @@ cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
 }
 cudaError_t prepare(const void* fn, int smem) {
     return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+}
+template <int DP>
+cudaError_t prepare_tiles() {
+    const cudaError_t e = prepare((const void*)attn_simt_kernel<DP, false>, Tile<DP>::kSmem);
+    return e != cudaSuccess ? e : prepare((const void*)attn_simt_kernel<DP, true>, Tile<DP>::kSmem);
 }
 template <int R, int DP>
 cudaError_t prepare_few() {
@@ -490,8 +557,8 @@ cudaError_t mafat_prepare_attn_simt() {
     cudaError_t e;
     if ((e = prepare_few<4, 64>()) != cudaSuccess || (e = prepare_few<4, 128>()) != cudaSuccess) return e;
     if ((e = prepare_few<8, 64>()) != cudaSuccess || (e = prepare_few<8, 128>()) != cudaSuccess) return e;
-    if ((e = prepare((const void*)attn_simt_kernel<64>, Tile<64>::kSmem)) != cudaSuccess) return e;
-    return prepare((const void*)attn_simt_kernel<128>, Tile<128>::kSmem);
+    if ((e = prepare_tiles<64>()) != cudaSuccess) return e;
+    return prepare_tiles<128>();
 }
 
 cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s) {

@@ -101,6 +101,17 @@ def test_cross_masks(mf, kernel, dtype, T, D):
     _cross(mf, 5, T, S, 4, 2, D, dtype, kv_mask=mask, kv_len=[500, 500, 500, 470, 301], kernel=kernel, poison=True)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("T,D", [(90, 128), (90, 64)])
+def test_cross_sparse_masks(mf, dtype, splits, T, D):
+    """Readable keys in numbers around a tile's, with gaps longer than what is looked at at once."""
+    at = torch.arange(1500, device="cuda")
+    mask = torch.stack([at % 23 == 22, (at >= 700) & (at < 764), (at >= 600) & (at < 729), (at < 64) | (at >= 1499), at % 200 < 65,
+                        (at < 127) | ((at >= 500) & (at < 628)), at >= 0])
+    _cross(mf, 7, T, 1500, 2, 1, D, dtype, kv_mask=mask, kv_len=[1500] * 6 + [1345], kernel=2, splits=splits, poison=True, repeat=2)
+
+
 @pytest.mark.parametrize("kernel", KERNELS)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_cross_strides(mf, kernel, dtype):
