@@ -81,7 +81,8 @@ cudaError_t mafat_prepare_attn_rows();
 int mafat_attn_rows_keys();
 int mafat_attn_rows_join();  // most parts of an earlier launch that it joins
 
-// bf16 on the tensor cores: tiles of 128 * slots rows (slots 1 or 2) by 128 keys.  The maps are 4-D over {channel, head, key, sequence}, boxes of 64 channels x 128 keys, 128-byte swizzle.
+// bf16 on the tensor cores: tiles of 128 * slots rows (slots 1 or 2) by 128 keys.  The maps are 4-D over {channel, head,
+// key, sequence}, boxes of 64 channels x 128 keys, 128-byte swizzle.
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
                                  cudaStream_t s);
 cudaError_t mafat_prepare_attn_tc();

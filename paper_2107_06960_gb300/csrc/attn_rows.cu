@@ -10,6 +10,10 @@
 // accumulators are P's operand as they are.  P is rounded to bf16 for its product; all else is fp32.
 //
 // Keys that are not readable are not copied but filled with zeros, so that 0 x NaN cannot reach O.
+//
+// One token of 64 sequences, 32 query and 8 key heads, 1444 keys: 61 us or 6.2 TB/s with 128 channels, 34 us or 5.5 TB/s
+// with 64; under 40 % of the issue slots are taken.  One token of one sequence (8 query and 4 key heads, 1444 keys) is
+// bound by round trips: 5.2 us in 4 clusters of 8 CTAs, 5.8 with a launch that joins the parts.
 #include "attn_common.cuh"
 
 namespace {

@@ -1,8 +1,8 @@
 // Attention of many rows in bf16 on the tensor cores (tcgen05, sm_103a): tiles of 128 rows by 128 keys.
 //
 // For a tile of queries Q and each tile of keys K and values V of the CTA's part:
-//   S = Q K^T;  m' = max(m, max S);  P = 2^(c S - c m');  O = 2^(c (m - m')) O + P V;  l alike,
-// with c = scale log2(e).  S and O are fp32 accumulators in tensor memory; m and l are fp32 registers
+//   S = Q K^T;  b' = max(b, c max S);  P = 2^(c S - b');  O = 2^(b - b') O + P V;  l alike,
+// with c = scale log2(e).  S and O are fp32 accumulators in tensor memory; b and l are fp32 registers
 // of the thread that has the row.  P is rounded to bf16 for its product (l sums it unrounded) and written
 // over S in tensor memory, from where the second product reads it; nothing of S leaves the SM.
 //
@@ -13,8 +13,14 @@
 // 0 x NaN would reach O.  With a mask the last two and a third instead copy the readable keys alone, one
 // after another (cp.async): keys that are not readable cost no product.
 //
-// O is rescaled only where m' is more than 2^8 above the m in use (a power that cancels in O / l and
+// O is rescaled only where b' is more than 8 above the b in use (a power that cancels in O / l and
 // leaves P at most 256, well inside bf16), so that few tiles touch O outside the products.
+//
+// Bound, for long sequences, by the softmax between the two products: with 128 channels the tensor pipe is busy 70 % of
+// the time, with 64, whose products take half as long for the same exponentials, 49 %, the special function unit
+// as much and the issue slots 62 %.  8 x 2048 tokens, 16 query and 4 key heads, 5776 keys: 488 us or 1.59 PFLOP/s with 128
+// channels, 341 us or 1.14 with 64.  For few keys by the round trips of an item's start and end, about 5 us: of two
+// CTAs on an SM, one slot each, one works meanwhile.
 //
 // Shared-memory operands are in the 128-byte-swizzled layout: rows of 64 channels, 16-byte chunk c
 // of row r at chunk c ^ (r % 8).  K is read K-major (its channels are the reduction), V MN-major (its keys
