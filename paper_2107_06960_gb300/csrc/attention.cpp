@@ -437,6 +437,8 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         a.overlap = r > 0;
         a.join = r > 0 && p->joined ? p->parts : 0;
         a.cluster = p->cluster;
+        // where a CTA has several items; of more sequences it has so many that they level it
+        a.ordered = g.kernel == kRows && x.len && g.n_seq > 1 && g.n_seq <= kMafatMostOrdered && g.items > g.ctas;
         a.direct = a.join || (p->parts == 1 && !p->joined);
         if (is_tc(g.kernel)) {
             CUtensorMap k, v;

@@ -45,6 +45,8 @@ struct MafatAttnSeg {
     int32_t items;              // n_seq * heads_kv * splits * row_tiles
 };
 
+constexpr int kMafatMostOrdered = 128;
+
 struct MafatAttnArgs {
     const void* q;
     void* out;
@@ -58,6 +60,7 @@ struct MafatAttnArgs {
     int32_t direct, join;
     // more than 1: the CTAs with a row's parts are a cluster of this many, and join them among themselves
     int32_t cluster;
+    int32_t ordered;            // 1: attn_rows takes the longest of the n_seq sequences (at most kMafatMostOrdered) first
     float scale_log2;           // softmax scale times log2(e)
     float* part_o;              // [parts][rows_total][dim] results of the parts, each normalised
     float* part_lse;            // [parts][rows_total] their log2 of the sum of exponentials

@@ -7,6 +7,19 @@
 
 namespace mafat_attn {
 
+__device__ __forceinline__ int length_of(const MafatAttnSeg& g, int seq) {
+    return g.len ? min(max(g.len[seq], 0), g.n) : g.n;
+}
+
+// The j-th sequence and its length, as they are given.
+struct AsGiven {
+    const MafatAttnSeg& g;
+    __device__ __forceinline__ int operator()(int j, int& len) const {
+        len = length_of(g, j);
+        return j;
+    }
+};
+
 // One item of work.  Row tiles of one part of the keys are neighbours, so that CTAs that run together
 // read the same keys.
 struct Block {
@@ -15,7 +28,10 @@ struct Block {
     int key0, key1;  // its part of them: a run of whole tiles
 
     // Reads the sequence's length: after launch_begin.
-    __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows, int tile_keys) {
+    __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows, int tile_keys)
+        : Block(a, i, tile_rows, tile_keys, AsGiven{a.seg}) {}
+    template <class Seq>
+    __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows, int tile_keys, Seq seq_of) {
         const MafatAttnSeg& g = a.seg;
         uint32_t next = g.row_tiles_div.div(i);
         row0 = (int)(i - next * (uint32_t)g.row_tiles) * tile_rows;
@@ -25,9 +41,7 @@ struct Block {
         i = next;
         next = a.heads_kv_div.div(i);
         head = (int)(i - next * (uint32_t)a.heads_kv);
-        seq = (int)next;
-        len = g.n;
-        if (g.len) len = min(max(g.len[seq], 0), g.n);
+        seq = seq_of((int)next, len);
         // the keys that some row of the tile sees
         int last = len;
         if (g.causal) {

@@ -9,6 +9,10 @@
 // ring.  The products are the 16 x 8 x 16 ones of a single warp, whose operands are registers: S's
 // accumulators are P's operand as they are.  P is rounded to bf16 for its product; all else is fp32.
 //
+// Items of the longest sequences are taken first, and a CTA's next from the other end of the order: 64 sequences of half
+// to all of 1444 keys (one token, 32 query and 8 key heads) take 49.5 us, as they are given 55, 128 channels; 29.4 and
+// 31.5 with 64.  (In the kernels whose CTAs have one item each, finding its sequence cost what it brought.)
+//
 // Keys that are not readable are not copied but filled with zeros, so that 0 x NaN cannot reach O.
 //
 // One token of 64 sequences, 32 query and 8 key heads, 1444 keys: 61 us or 6.2 TB/s with 128 channels, 34 us or 5.5 TB/s
@@ -61,18 +65,72 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// The CTA's items: one of every round of gridDim.x, from one end of a round and from the other in turn, so that with the
+// longest sequences first each has long ones and short ones.
+struct Items {
+    uint32_t item, edge;
+    __device__ __forceinline__ Items() : item(blockIdx.x), edge(2 * gridDim.x - 1) {}
+    __device__ __forceinline__ uint32_t next() const { return edge - item; }
+    __device__ __forceinline__ void step() {
+        item = edge - item;
+        edge += 2 * gridDim.x;
+    }
+};
+// The j-th sequence and its length; with a table of them the j-th longest.
+struct Table {
+    const MafatAttnSeg& g;
+    const int2* order;  // null: as they are given
+    __device__ __forceinline__ int operator()(int j, int& len) const {
+        const int2 x = order ? order[j] : make_int2(j, mafat_attn::length_of(g, j));
+        len = x.y;
+        return x.x;
+    }
+};
+// Fills the table, longest first, by counting for each sequence those before it: a ballot of each 32, for kTogether
+// sequences of a warp at a time.
+__device__ __forceinline__ void order_sequences(const MafatAttnSeg& g, int2* order) {
+    constexpr int kSets = kMafatMostOrdered / 32, kTogether = 4, kStep = kTogether * kWarps;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int len[kSets];
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) len[i] = i * 32 + lane < g.n_seq ? mafat_attn::length_of(g, i * 32 + lane) : -1;
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+        const int n = min(32, g.n_seq - i * 32);
+#pragma unroll 1
+        for (int s0 = warp; s0 < n; s0 += kStep) {
+            int mine[kTogether], place[kTogether];
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+                mine[k] = __shfl_sync(0xffffffffu, len[i], (s0 + k * kWarps) & 31);
+                place[k] = 0;
+            }
+#pragma unroll
+            for (int u = 0; u < kSets; ++u)
+                if (u * 32 < g.n_seq)
+#pragma unroll
+                    for (int k = 0; k < kTogether; ++k)
+                        place[k] += __popc(__ballot_sync(
+                            0xffffffffu, len[u] > mine[k] || (len[u] == mine[k] && u * 32 + lane < i * 32 + s0 + k * kWarps)));
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k)
+                if (lane == 0 && s0 + k * kWarps < n) order[place[k]] = make_int2(i * 32 + s0 + k * kWarps, mine[k]);
+        }
+    }
+    __syncthreads();
+}
+
 // The copying side's place: a run of an item.
-struct Ahead {
-    uint32_t item;
+struct Ahead : Items {
     int run, runs, first, len;
     const __nv_bfloat16 *k, *v;
     const uint8_t* mask;
 
-    __device__ __forceinline__ void open(const MafatAttnArgs& a, int warp) {
+    __device__ __forceinline__ void open(const MafatAttnArgs& a, int warp, Table table) {
         run = runs = 0;
         if (item >= (uint32_t)a.seg.items) return;
         const MafatAttnSeg& g = a.seg;
-        const mafat_attn::Block b(a, item, 16, kBN);
+        const mafat_attn::Block b(a, item, 16, kBN, table);
         first = b.key0 + warp * kRun;
         runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
         len = b.len;
@@ -98,15 +156,18 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     const bool in_dim = cc * 8 < a.dim;
     mafat_attn::launch_begin(a);
 
+    __shared__ int2 order[kMafatMostOrdered];
+    const Table table{g, a.ordered ? order : nullptr};
+    if (a.ordered) order_sequences(g, order);
+
     // the next run into its stage: chunk c of key r at chunk c ^ (r % 8) of its row; empty past the last item
     Ahead ld;
-    ld.item = blockIdx.x;
-    ld.open(a, warp);
+    ld.open(a, warp, table);
     uint32_t ld_stage = 0u, stage = 0u;
     auto load = [&]() {
         while (ld.run == ld.runs && ld.item < (uint32_t)g.items) {
-            ld.item += gridDim.x;
-            ld.open(a, warp);
+            ld.step();
+            ld.open(a, warp, table);
         }
         if (ld.run < ld.runs) {
             const int key = ld.first + ld.run * kBN;
@@ -129,7 +190,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     // a warp's share of an item's queries, rows past the last zero
     auto load_queries = [&](uint32_t item, uint32_t which) {
         if (item < (uint32_t)g.items) {
-            const mafat_attn::Block b(a, item, 16, kBN);
+            const mafat_attn::Block b(a, item, 16, kBN, table);
 #pragma unroll
             for (int r0 = 0; r0 < 16 / kWarps; r0 += kRows) {
                 const int r = warp * (16 / kWarps) + r0 + cr, row = min(b.row0 + r, g.rows - 1);
@@ -155,8 +216,8 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 
     uint32_t which = 0u;
 #pragma unroll 1
-    for (uint32_t item = blockIdx.x; item < (uint32_t)g.items; item += gridDim.x, which ^= 1u) {
-        const mafat_attn::Block b(a, item, 16, kBN);
+    for (Items it; it.item < (uint32_t)g.items; it.step(), which ^= 1u) {
+        const mafat_attn::Block b(a, it.item, 16, kBN, table);
         const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
         const int first = b.key0 + warp * kRun;
         const int runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
@@ -167,7 +228,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 #pragma unroll
         for (int t = 0; t < kSteps; ++t)  // rows 0-7 and 8-15 with channels 0-7, then with 8-15
             ldm4(q[t], smem + C::kOffQ + which * C::kQ + (uint32_t)(v_row * (DP * 2) + (((2 * t + v_chunk) ^ (v_row % 8)) * 16)));
-        load_queries(item + gridDim.x, which ^ 1u);  // lands with the next run
+        load_queries(it.next(), which ^ 1u);  // lands with the next run
         int limit[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {

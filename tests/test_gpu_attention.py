@@ -114,6 +114,16 @@ def test_cross_sparse_masks(mf, dtype, splits, T, D):
 
 @pytest.mark.parametrize("kernel", KERNELS)
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,H,Hk,D", [(100, 1, 8, 8, 64), (128, 3, 4, 4, 128), (129, 1, 4, 4, 64), (77, 70, 8, 8, 128), (2, 1400, 16, 16, 64)])
+def test_cross_many_sequences(mf, kernel, dtype, B, T, H, Hk, D):
+    """More work than the GPU holds at once: lengths of zero, equal ones, past the room."""
+    ln = [(37 * i * i + 11 * i) % 300 for i in range(B)]
+    ln[:2], ln[-2:] = [0, 400], [64, 64]
+    _cross(mf, B, T, 290, H, Hk, D, dtype, kv_len=ln, kernel=kernel, poison=True, repeat=2)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("dtype", TYPES)
 def test_cross_strides(mf, kernel, dtype):
     _cross(mf, 2, 37, 211, 6, 3, 56, dtype, kernel=kernel, layout="bhsd", kv_len=[211, 100])
     _cross(mf, 2, 1, 211, 6, 3, 128, dtype, kernel=kernel, layout="bhsd")
