@@ -18,8 +18,8 @@
 //
 // Bound, for long sequences, by the softmax between the two products: with 128 channels the tensor pipe is busy 70 % of
 // the time, with 64, whose products take half as long for the same exponentials, 49 %, the special function unit
-// as much and the issue slots 62 %.  8 x 2048 tokens, 16 query and 4 key heads, 5776 keys: 488 us or 1.59 PFLOP/s with 128
-// channels, 341 us or 1.14 with 64.  For few keys by the round trips of an item's start and end, about 5 us: of two
+// as much and the issue slots 62 %.  8 x 2048 tokens, 16 query and 4 key heads, 5776 keys: 480 us or 1.61 PFLOP/s with 128
+// channels, 339 us or 1.14 with 64.  For few keys by the round trips of an item's start and end, about 5 us: of two
 // CTAs on an SM, one slot each, one works meanwhile.
 //
 // Shared-memory operands are in the 128-byte-swizzled layout: rows of 64 channels, 16-byte chunk c
@@ -63,11 +63,15 @@ struct Cfg {
     static constexpr int kTmemCols = 256 * SLOTS;
     static constexpr int kBufs = SLOTS == 2 && DP == 64 ? 3 : SLOTS;
     static_assert(kBufs * 128 + SLOTS * DP <= kTmemCols, "tensor memory");
+    // Without a buffer more than slots the product with V starts when half of each thread's weights are there: 2 x 1216
+    // tokens of 16 heads of 128 channels over 5776 keys take 67.4 us, with whole weights 70.1; with a buffer more (two
+    // slots of 64 channels) the other slot's products fill that time, and halves cost 50.7 against 49.7.
+    static constexpr int kPParts = kBufs > SLOTS ? 1 : 2;
     // shared memory, from a 1024-byte boundary
     static constexpr int kOffKv = SLOTS * kTileBytes;
     static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
     static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + kBufs,
-                         kBarO = kBarP + kBufs, kBarMask = kBarO + SLOTS, kBars = kBarMask + 1;
+                         kBarO = kBarP + kPParts * kBufs, kBarMask = kBarO + SLOTS, kBars = kBarMask + 1;
     // V of a tile is read after the scores of kBufs - 1 tiles more (one slot) or of one (two slots)
     static_assert(kLag <= kStages - (kBufs > 2 ? 2 * kBufs - 2 : 2), "gathered tiles");
     static constexpr int kOffTmem = kOffBar + (kBars * 8 + 15) / 16 * 16;
@@ -316,7 +320,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         }
         for (int i = 0; i < C::kBufs; ++i) {
             bar_init(bar(C::kBarS + i), 1);
-            bar_init(bar(C::kBarP + i), C::kSlotWarps);
+            for (int part = 0; part < C::kPParts; ++part) bar_init(bar(C::kBarP + i * C::kPParts + part), C::kSlotWarps);
         }
         bar_init(bar(C::kBarMask), 1);
         *broken = 0;
@@ -513,12 +517,20 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         p[i] = pack(x, y);
                     }
                     tmem_st16(ts + (uint32_t)(half * (C::kCols / 2) + 16 * h), p);
+                    if (C::kPParts == 2 && h == C::kCols / 64 - 1) {  // the product with half of the thread's keys can begin
+                        st_wait();
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive(bar(C::kBarP) + (uint32_t)(buf * C::kPParts) * 8u);
+                    }
                 }
                 st_wait();
                 fence_before();
+            } else if (C::kPParts == 2 && lane == 0) {
+                arrive(bar(C::kBarP) + (uint32_t)(buf * C::kPParts) * 8u);
             }
             __syncwarp();
-            if (lane == 0) arrive(bar(C::kBarP) + (uint32_t)buf * 8u);
+            if (lane == 0) arrive(bar(C::kBarP) + (uint32_t)(buf * C::kPParts + C::kPParts - 1) * 8u);
             buf += live;
             if (buf >= C::kBufs) buf -= C::kBufs, uses ^= 1u;
         }
@@ -659,12 +671,21 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             }
             commit_el(el, bar(C::kBarS) + (uint32_t)buf * 8u);
         };
+        uint32_t uses = 0u;  // parity of the uses of P's buffers
         auto values = [&](int slot, uint32_t stage, int buf, uint32_t acc, bool last) {
             const uint32_t vb = v_lo + stage * kTile16;
 #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)  // 16 keys: 8 columns of P, two 8-key groups of V
-                mma_ts(el, tmem + (uint32_t)(C::kBufs * 128 + slot * DP), tmem + (uint32_t)(buf * 128 + 8 * k),
-                       vb + (uint32_t)k * (2048u / 16u), hi, id_o, k > 0 ? 1u : acc);
+            for (int part = 0; part < C::kPParts; ++part) {  // of each softmax thread's keys
+                wait(bar(C::kBarP) + (uint32_t)(buf * C::kPParts + part) * 8u, uses, ctl);
+                fence_after();
+                constexpr int kRun = C::kCols / 16 / C::kPParts;  // steps of a thread's keys in the part
+#pragma unroll
+                for (int i = 0; i < kKeys / 16 / C::kPParts; ++i) {  // 16 keys: 8 columns of P, two 8-key groups of V
+                    const int k = i / kRun * (C::kCols / 16) + part * kRun + i % kRun;
+                    mma_ts(el, tmem + (uint32_t)(C::kBufs * 128 + slot * DP), tmem + (uint32_t)(buf * 128 + 8 * k),
+                           vb + (uint32_t)k * (2048u / 16u), hi, id_o, part + i > 0 ? 1u : acc);
+                }
+            }
             commit_el(last || ahead ? el : 0u, bar(C::kBarO) + (uint32_t)slot * 8u);
         };
         // The scores of item n + kBufs follow the values of item n: products run in the order of issue,
@@ -683,7 +704,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         };
         Place ps{0u, 0u, 0, 0}, pv{1u, 0u, 0, 0};
         int bs = 0, bv = 0;
-        uint32_t uses = 0u;
         auto next_scores = [&]() {
             if (ps.tile >= t.n) return;
             if (ps.slot == 0) wait(bar(C::kBarFull) + ps.stage * 8u, ps.phase, ctl);
@@ -701,8 +721,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 wait(bar(C::kBarFull) + pv.stage * 8u, pv.phase, ctl);
                 if (t.partial(pv.tile)) wait(bar(C::kBarMask), 0u, ctl);
             }
-            wait(bar(C::kBarP) + (uint32_t)bv * 8u, uses, ctl);
-            fence_after();
             values(pv.slot, pv.stage, bv, pv.tile > 0, pv.tile == t.n - 1);
             if (++bv == C::kBufs) bv = 0, uses ^= 1u;
             const uint32_t empty = bar(C::kBarEmpty) + pv.stage * 8u;
