@@ -31,7 +31,13 @@ struct Block {
     __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows, int tile_keys)
         : Block(a, i, tile_rows, tile_keys, AsGiven{a.seg}) {}
     template <class Seq>
-    __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows, int tile_keys, Seq seq_of) {
+    __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows, int tile_keys, Seq seq_of)
+        : Block(a, i, tile_rows) {
+        seq = seq_of(seq, len);
+        set_keys(a, tile_rows, tile_keys);
+    }
+    // The item alone, with its sequence as they are given; set_keys follows once len is there.
+    __device__ __forceinline__ Block(const MafatAttnArgs& a, uint32_t i, int tile_rows) {
         const MafatAttnSeg& g = a.seg;
         uint32_t next = g.row_tiles_div.div(i);
         row0 = (int)(i - next * (uint32_t)g.row_tiles) * tile_rows;
@@ -41,7 +47,10 @@ struct Block {
         i = next;
         next = a.heads_kv_div.div(i);
         head = (int)(i - next * (uint32_t)a.heads_kv);
-        seq = seq_of((int)next, len);
+        seq = (int)next;
+    }
+    __device__ __forceinline__ void set_keys(const MafatAttnArgs& a, int tile_rows, int tile_keys) {
+        const MafatAttnSeg& g = a.seg;
         // the keys that some row of the tile sees
         int last = len;
         if (g.causal) {

@@ -334,8 +334,26 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     __syncwarp();
+    // queries, whose places are known before the launch before has ended; they and the length come together
+    mafat_attn::Block b(a, blockIdx.x, 128 * SLOTS);
+    constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
+    constexpr int kLoads = 32 / kRows / C::kHalves;
+    const int q_slot = warp / C::kSlotWarps, q_half = warp / 4 % C::kHalves, q_quarter = warp % 4;
+    const int q_row0 = b.row0 + q_slot * 128 + q_quarter * 32, cc = lane % kChunks, cr = lane / kChunks;
+    const bool q_any = warp < C::kSoftmaxWarps && q_row0 < g.rows;
+    const int64_t q_off = q_any && q_row0 + lane < g.rows ? mafat_attn::Row(a, b, q_row0 + lane).query(a) : -1;
+    uint4 q[kLoads];
     mafat_attn::launch_begin(a);
-    const mafat_attn::Block b(a, blockIdx.x, 128 * SLOTS, kKeys);
+    if (q_any) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int64_t o = __shfl_sync(0xffffffffu, q_off, (q_half * kLoads + i) * kRows + cr);
+            q[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (o >= 0 && cc * 8 < a.dim) q[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + cc * 8);
+        }
+    }
+    b.len = mafat_attn::length_of(g, b.seq);
+    b.set_keys(a, 128 * SLOTS, kKeys);
     const uint8_t* mask = gather ? g.mask + (int64_t)b.seq * g.n : nullptr;
     if (gather) {
         int n = 0;
@@ -359,29 +377,14 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         load_tile(el, 0, 0u);
         load_tile(el, 1, 1u);
     }
-    if (warp < C::kSoftmaxWarps) {
-        const int slot = warp / C::kSlotWarps, half = warp / 4 % C::kHalves, quarter = warp % 4;
-        const int row0 = b.row0 + slot * 128 + quarter * 32, row = row0 + lane;
-        if (row0 < g.rows && b.key1 > b.key0) {
-            constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
-            constexpr int kLoads = 32 / kRows / C::kHalves;
-            uint8_t* mine = sm + slot * C::kTileBytes;
-            const int cc = lane % kChunks, cr = lane / kChunks;
-            const int64_t off = row < g.rows ? mafat_attn::Row(a, b, row).query(a) : -1;
-            uint4 v[kLoads];
+    if (q_any) {
+        uint8_t* to = sm + q_slot * C::kTileBytes;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int64_t o = __shfl_sync(0xffffffffu, off, (half * kLoads + i) * kRows + cr);
-                v[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (o >= 0 && cc * 8 < a.dim) v[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + cc * 8);
-            }
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int r = quarter * 32 + (half * kLoads + i) * kRows + cr;
-                *reinterpret_cast<uint4*>(mine + (cc / 8) * C::kSub + r * 128 + ((cc % 8) ^ (r % 8)) * 16) = v[i];
-            }
-            fence_async();
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = q_quarter * 32 + (q_half * kLoads + i) * kRows + cr;
+            *reinterpret_cast<uint4*>(to + (cc / 8) * C::kSub + r * 128 + ((cc % 8) ^ (r % 8)) * 16) = q[i];
         }
+        fence_async();
     }
     __syncwarp();
     fence_before();
@@ -534,11 +537,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             buf += live;
             if (buf >= C::kBufs) buf -= C::kBufs, uses ^= 1u;
         }
-        if (n_tiles > 0) {
-            wait(bar(C::kBarO + slot), ahead ? (uint32_t)(t.n - 1) & 1u : 0u, ctl);
-            __syncwarp();
-            fence_after();
-        }
         // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in whole pieces:
         // kOutBytes of each row at a time, bf16 results at once, fp32 parts in two passes.  joins: with the parts of
         // the launch before (apart, so that the form without them stays short).
@@ -565,6 +563,11 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             uint8_t* buf = mine + (quarter * C::kHalves + half) * 32 * C::kOutBytes;
             const int64_t dst = row >= g.rows ? -1 : a.direct ? w.o : w.part * a.dim;
             uint8_t* my = buf + lane * C::kOutBytes;
+            if (n_tiles > 0) {
+                wait(bar(C::kBarO + slot), ahead ? (uint32_t)(t.n - 1) & 1u : 0u, ctl);
+                __syncwarp();
+                fence_after();
+            }
             auto put = [&](int chunk, uint4 v) { *reinterpret_cast<uint4*>(my + ((chunk ^ (lane % kSwz)) * 16)) = v; };
 #pragma unroll
             for (int pass = 0; pass < 2; ++pass) {
@@ -631,17 +634,21 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         if (o >= 0 && d < a.dim) mafat_attn::put4((__nv_bfloat16*)a.out + o + d, v[i]);
                     }
                 } else {
+                    constexpr int kTogether = 8;  // read before they are written: writes might be to what is read
+                    uint8_t* to_out = part ? (uint8_t*)(a.part_o + d) : (uint8_t*)((__nv_bfloat16*)a.out + d);
 #pragma unroll
-                    for (int i = 0; i < kPieces; ++i) {
-                        const int r = i * kRows + cr;
-                        const int64_t o = __shfl_sync(0xffffffffu, dst, r);
-                        const uint4 v = *reinterpret_cast<const uint4*>(buf + r * C::kOutBytes + ((cc ^ (r % kSwz)) * 16));
-                        if (o >= 0 && d < a.dim) {
-                            if (part)
-                                *reinterpret_cast<uint4*>(a.part_o + o + d) = v;
-                            else
-                                *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + o + d) = v;
+                    for (int i0 = 0; i0 < kPieces; i0 += kTogether) {
+                        int64_t o[kTogether];
+                        uint4 v[kTogether];
+#pragma unroll
+                        for (int i = 0; i < kTogether; ++i) {
+                            const int r = (i0 + i) * kRows + cr;
+                            o[i] = __shfl_sync(0xffffffffu, dst, r);
+                            v[i] = *reinterpret_cast<const uint4*>(buf + r * C::kOutBytes + ((cc ^ (r % kSwz)) * 16));
                         }
+#pragma unroll
+                        for (int i = 0; i < kTogether; ++i)
+                            if (o[i] >= 0 && d < a.dim) *reinterpret_cast<uint4*>(to_out + o[i] * (part ? 4 : 2)) = v[i];
                     }
                 }
                 __syncwarp();
