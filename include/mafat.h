@@ -490,6 +490,9 @@ typedef struct {
     int32_t kernel[2], splits[2], ctas[2];  /* 0 for a set without room for keys */
     int32_t parts;              /* of a row that go through the workspace to be joined; 1: none do */
     int32_t launches_per_run;
+    /* not 0: a run without a prefix mask is one launch instead, of so many CTAs of MAFAT_ATTN_TILES that read both
+     * sets for rows of one request each and keep no parts */
+    int32_t whole_ctas;
     int64_t workspace_bytes;
 } mafat_attn_stats_t;
 mafat_status mafat_attn_stats(const mafat_attn_t* plan, mafat_attn_stats_t* out);

@@ -81,7 +81,7 @@ class PrefixDesc(ctypes.Structure):
 
 class AttnStats(ctypes.Structure):
     _fields_ = [("struct_size", i32), ("kernel", i32 * 2), ("splits", i32 * 2), ("ctas", i32 * 2), ("parts", i32),
-                ("launches_per_run", i32), ("workspace_bytes", i64)]
+                ("launches_per_run", i32), ("whole_ctas", i32), ("workspace_bytes", i64)]
 
 
 class NormDesc(ctypes.Structure):

@@ -39,6 +39,7 @@ struct AttnSegPlan {
     int64_t k[3] = {0, 0, 0}, v[3] = {0, 0, 0};  // strides: sequence, key, head
     int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, items = 0, ctas = 0;
     AttnKernel kernel = kRows;
+    double us = 0.;  // by the model
 };
 
 struct mafat_attn_s {
@@ -51,6 +52,8 @@ struct mafat_attn_s {
     AttnSegPlan seg[2];
     // launches: the segments that have room for keys, or the first if none has
     int n_run = 0, run[2] = {0, 0};
+    // the own keys' work when one launch of the tensor-core kernel does both sets (a run without a mask); items 0: never
+    AttnSegPlan both;
     int parts = 0;
     int cluster = 1;      // CTAs of a cluster that joins its parts itself
     bool joined = false;  // the second launch joins the first one's parts with its own results
@@ -277,6 +280,7 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
             g.kernel = kernels[i];
         }
     }
+    g.us = best.us;
     const AttnShape sh = shape_of(g.kernel, p.dim);
     g.row_tiles = (int32_t)row_tiles(sh, g.rows);
     g.splits = best.n;
@@ -289,6 +293,38 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
     g.part0 = p.parts;
     p.parts += g.splits;
     return MAFAT_OK;
+}
+
+// Whether both sets of keys of a prefix plan are better read by the same tiles of rows, of one request each: no parts and
+// no second launch, where requests have rows enough to fill tiles or there is little to do.  In us, two launches and one:
+// 8 requests of 61 tokens about each of 4 frames of 5776 states (16 query and 4 key heads, 128 channels) 78.4, 68.0;
+// 32 of 46 tokens over 4 x 103 (8 and 4 heads of 80) 34.6, 18.7; 3 of a token over 2 x 100 (8 and 2 of 64) 6.1, 5.4; 16 of
+// a token over 1444 (16 and 4 of 64) 7.3, 15.5; 8 of 64 over 3 x 13852 (8 and 4 of 128) 75, 133.
+// Two launches whose first has whole results were measured to take 1 to 1.45 times what the model has for them (with
+// parts, the launch to join them, which it counts, falls away).
+constexpr double kTwoLaunches = 1.2;
+void plan_both(mafat_attn_s& p, const Common& c, int sms) {
+    if (p.dtype != MAFAT_BF16 || p.n_run != 2 || c.splits != 0 || c.kernel == MAFAT_ATTN_ROWS) return;
+    const AttnSegPlan &first = p.seg[p.run[0]], &own = p.seg[p.run[1]];
+    double best = first.us + own.us;
+    if (first.splits == 1) best = kTwoLaunches * (best + kOwnJoinUs);
+    for (AttnKernel k : {kTc1, kTc2}) {
+        if (k == kTc2 && own.rows <= 128) continue;
+        Model m{};
+        m.sh = shape_of(k, p.dim);
+        m.sms = sms;
+        m.items = (int64_t)own.n_seq * p.heads_kv * row_tiles(m.sh, own.rows);
+        m.tiles = ((int64_t)first.n + m.sh.keys - 1) / m.sh.keys + ((int64_t)own.n + m.sh.keys - 1) / m.sh.keys;
+        m.bytes = 4. * p.heads_kv * p.dim * ((double)first.n_seq * first.n + (double)own.n_seq * own.n);
+        if (m.items > kMaxI32 / 4 || m.us(1) >= best) continue;
+        best = m.us(1);
+        p.both = own;
+        p.both.kernel = k;
+        p.both.row_tiles = (int32_t)row_tiles(m.sh, own.rows);
+        p.both.splits = 1;
+        p.both.part0 = 0;
+        p.both.items = p.both.ctas = (int32_t)m.items;
+    }
 }
 
 // 4-D map {channel, head, key, sequence} of keys or values; boxes of 64 channels x 128 keys of one head.
@@ -337,6 +373,7 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
         const AttnSegPlan &first = p->seg[p->run[0]], &last = p->seg[p->run[1]];
         p->joined = last.splits == 1 && first.splits <= (last.kernel == kRows ? mafat_attn_rows_join() : kTileJoin);
         if (p->joined) p->parts = first.splits;
+        plan_both(*p, c, sms);
     }
     if (p->cluster > 1) p->parts = 1;  // none goes through the workspace
     const int64_t lse_bytes = (p->rows_total * p->parts * 4 + 255) / 256 * 256;
@@ -413,9 +450,10 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
     if (dev != p->device) return fail(MAFAT_EINVAL, "the current device is not the plan's");
-    for (int r = 0; r < p->n_run; ++r) {
+    const bool both = p->both.items > 0 && !d[p->run[0]].mask;
+    for (int r = both ? 1 : 0; r < p->n_run; ++r) {
         const int i = p->run[r];
-        const AttnSegPlan& g = p->seg[i];
+        const AttnSegPlan& g = both ? p->both : p->seg[i];
         MafatAttnSeg& x = a.seg;
         x.k = d[i].k;
         x.v = d[i].v;
@@ -434,25 +472,36 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         x.splits_div = MafatDiv((uint32_t)g.splits);
         x.part0 = g.part0;
         x.items = g.items;
-        a.overlap = r > 0;
-        a.join = r > 0 && p->joined ? p->parts : 0;
+        a.overlap = r > 0 && !both;
+        a.join = r > 0 && p->joined && !both ? p->parts : 0;
         a.cluster = p->cluster;
         // where a CTA has several items; of more sequences it has so many that they level it
         a.ordered = g.kernel == kRows && x.len && g.n_seq > 1 && g.n_seq <= kMafatMostOrdered && g.items > g.ctas;
-        a.direct = a.join || (p->parts == 1 && !p->joined);
+        a.direct = both || a.join || (p->parts == 1 && !p->joined);
         if (is_tc(g.kernel)) {
             CUtensorMap k, v;
             mafat_status st;
             if ((st = encode_map(&k, d[i].k, g, g.k, p->heads_kv, p->dim)) != MAFAT_OK ||
                 (st = encode_map(&v, d[i].v, g, g.v, p->heads_kv, p->dim)) != MAFAT_OK)
                 return st;
-            e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, s);
+            MafatAttnPrefix prefix;
+            if (both) {
+                const AttnSegPlan& f = p->seg[p->run[0]];
+                const SegData& fd = d[p->run[0]];
+                if ((st = encode_map(&prefix.k, fd.k, f, f.k, p->heads_kv, p->dim)) != MAFAT_OK ||
+                    (st = encode_map(&prefix.v, fd.v, f, f.v, p->heads_kv, p->dim)) != MAFAT_OK)
+                    return st;
+                prefix.len = fd.len;
+                prefix.n = f.n;
+                prefix.per = MafatDiv((uint32_t)f.reqs);
+            }
+            e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, both ? &prefix : nullptr, s);
         } else {
             e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, s) : mafat_launch_attn_simt(a, shape_of(g.kernel, p->dim).rows, s);
         }
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }
-    if (p->parts > 1 && !p->joined) {
+    if (p->parts > 1 && !p->joined && !both) {
         a.overlap = 0;
         e = mafat_launch_attn_join(a, p->dtype == MAFAT_BF16, s);
         if (e != cudaSuccess) return cuda_fail(e, "join launch");
@@ -552,6 +601,7 @@ mafat_status mafat_attn_stats(const mafat_attn_t* p, mafat_attn_stats_t* out) {
     }
     s.parts = p->parts;
     s.launches_per_run = p->n_run + (p->parts > 1 && !p->joined ? 1 : 0);
+    s.whole_ctas = p->both.ctas;
     s.workspace_bytes = p->workspace_bytes;
     *out = s;
     return MAFAT_OK;

@@ -86,8 +86,15 @@ int mafat_attn_rows_join();  // most parts of an earlier launch that it joins
 
 // bf16 on the tensor cores: tiles of 128 * slots rows (slots 1 or 2) by 128 keys.  The maps are 4-D over {channel, head,
 // key, sequence}, boxes of 64 channels x 128 keys, 128-byte swizzle.
+// prefix: null, or keys that come before the segment's own and that `per` of its sequences after another share.
+struct MafatAttnPrefix {
+    CUtensorMap k, v;
+    const int32_t* len;         // of each prefix (null: n)
+    int32_t n;
+    MafatDiv per;
+};
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
-                                 cudaStream_t s);
+                                 const MafatAttnPrefix* prefix, cudaStream_t s);
 cudaError_t mafat_prepare_attn_tc();
 
 // Joins the parts of each row.

@@ -71,7 +71,7 @@ struct Cfg {
     static constexpr int kOffKv = SLOTS * kTileBytes;
     static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
     static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + kBufs,
-                         kBarO = kBarP + kPParts * kBufs, kBarMask = kBarO + SLOTS, kBars = kBarMask + 1;
+                         kBarO = kBarP + kPParts * kBufs, kBarMask = kBarO + SLOTS, kBars = kBarMask + 2;
     // V of a tile is read after the scores of kBufs - 1 tiles more (one slot) or of one (two slots)
     static_assert(kLag <= kStages - (kBufs > 2 ? 2 * kBufs - 2 : 2), "gathered tiles");
     static constexpr int kOffTmem = kOffBar + (kBars * 8 + 15) / 16 * 16;
@@ -280,18 +280,30 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
 
 // The CTA's tiles of keys.  Without a mask they are runs of 128 keys, of which the last may pass the
 // length; with one they are the readable keys of its part one after another, gathered, numbered from 0.
+template <bool BOTH>
 struct Tiles {
     int key0, n, len;
     bool gather;
+    int n0, len0;  // BOTH: the tiles and keys of the prefix, which come first
+    __device__ __forceinline__ bool of_prefix(int j) const { return BOTH && j < n0; }
+    // place of tile j's first key in its set
+    __device__ __forceinline__ int first(int j) const {
+        return of_prefix(j) ? j * kKeys : key0 + (BOTH ? j - n0 : j) * kKeys;
+    }
+    __device__ __forceinline__ int length(int j) const { return of_prefix(j) ? len0 : len; }
     // some keys of tile j are not readable, and their values have to be zeroed (gathered ones are)
-    __device__ __forceinline__ bool partial(int j) const { return !gather && key0 + (j + 1) * kKeys > len; }
+    __device__ __forceinline__ bool partial(int j) const { return !gather && first(j) + kKeys > length(j); }
 };
 
-template <int DP, int SLOTS>
+struct NoPrefix {};
+
+// Prefix: MafatAttnPrefix where the rows' keys are those of a prefix and then their own
+template <int DP, int SLOTS, class Prefix>
 __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     attn_tc_kernel(const __grid_constant__ MafatAttnArgs a, const __grid_constant__ CUtensorMap kmap,
-                   const __grid_constant__ CUtensorMap vmap) {
+                   const __grid_constant__ CUtensorMap vmap, const __grid_constant__ Prefix prefix) {
     using C = Cfg<DP, SLOTS>;
+    constexpr bool kBoth = std::is_same<Prefix, MafatAttnPrefix>::value;
     extern __shared__ __align__(1024) uint8_t sm[];
     const uint32_t base = smem_u32(sm);
     if (base & 1023u) {  // the swizzled layouts need it; the declaration asks for it
@@ -305,7 +317,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     const Ctl ctl{a.status, a.timeout_ns, broken};
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const MafatAttnSeg& g = a.seg;
-    const bool gather = g.mask != nullptr;
+    const bool gather = !kBoth && g.mask != nullptr;
 
     if (warp == C::kLoadWarp && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&kmap)) : "memory");
@@ -322,7 +334,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             bar_init(bar(C::kBarS + i), 1);
             for (int part = 0; part < C::kPParts; ++part) bar_init(bar(C::kBarP + i * C::kPParts + part), C::kSlotWarps);
         }
-        bar_init(bar(C::kBarMask), 1);
+        for (int i = 0; i < 2; ++i) bar_init(bar(C::kBarMask + i), 1);
         *broken = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
@@ -353,7 +365,19 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         }
     }
     b.len = mafat_attn::length_of(g, b.seq);
+    Tiles<kBoth> t;
+    t.n0 = t.len0 = 0;
+    int prefix_seq = 0;
+    if constexpr (kBoth) {
+        prefix_seq = (int)prefix.per.div((uint32_t)b.seq);
+        t.len0 = prefix.len ? min(max(prefix.len[prefix_seq], 0), prefix.n) : prefix.n;
+        t.n0 = (t.len0 + kKeys - 1) / kKeys;
+    }
     b.set_keys(a, 128 * SLOTS, kKeys);
+    t.gather = gather;
+    t.key0 = b.key0;
+    t.len = b.len;
+    t.n = t.n0 + (b.key1 > b.key0 ? (b.key1 - b.key0 + kKeys - 1) / kKeys : 0);
     const uint8_t* mask = gather ? g.mask + (int64_t)b.seq * g.n : nullptr;
     if (gather) {
         int n = 0;
@@ -368,10 +392,16 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         const uint32_t full = bar(C::kBarFull) + stage * 8u, dst = base + C::kOffKv + stage * C::kTileBytes;
         expect_el(el, full, C::kTileBytes);
 #pragma unroll
-        for (int c = 0; c < DP / 64; ++c)
-            tma_tile(el, dst + c * C::kSub, (i & 1) ? &vmap : &kmap, c * 64, b.head, b.key0 + (i / 2) * kKeys, b.seq, full);
+        for (int c = 0; c < DP / 64; ++c) {
+            if constexpr (kBoth)
+                if (t.of_prefix(i / 2)) {
+                    tma_tile(el, dst + c * C::kSub, (i & 1) ? &prefix.v : &prefix.k, c * 64, b.head, t.first(i / 2), prefix_seq, full);
+                    continue;
+                }
+            tma_tile(el, dst + c * C::kSub, (i & 1) ? &vmap : &kmap, c * 64, b.head, t.first(i / 2), b.seq, full);
+        }
     };
-    if (!gather && warp == C::kLoadWarp && b.key1 > b.key0) {
+    if (!gather && warp == C::kLoadWarp && t.n > 0) {
         const uint32_t el = elect_one();
         ahead_loads = 2u;
         load_tile(el, 0, 0u);
@@ -391,11 +421,6 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     __syncthreads();
     fence_after();
     const uint32_t tmem = *tmem_slot;
-    Tiles t;
-    t.gather = gather;
-    t.key0 = b.key0;
-    t.len = b.len;
-    t.n = b.key1 > b.key0 ? (b.key1 - b.key0 + kKeys - 1) / kKeys : 0;
     if (gather) {
         int n = lane < C::kThreads / 32 ? *(volatile int*)(sm + C::kOffCount + lane * 4) : 0;
         n = __reduce_add_sync(0xffffffffu, n);
@@ -460,7 +485,8 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 uint32_t s[C::kCols];
 #pragma unroll
                 for (int i = 0; i < C::kCols / 32; ++i) tmem_ld32(ts + (uint32_t)(half * C::kCols + 32 * i), s + 32 * i);
-                const int left = limit - (t.key0 + j * kKeys) - half * C::kCols;  // readable keys of the thread's
+                // readable keys of the thread's
+                const int left = (t.of_prefix(j) ? t.len0 : limit) - t.first(j) - half * C::kCols;
 #pragma unroll
                 for (int i = 0; i < C::kCols / 32; ++i) ld_wait32(s + 32 * i);
                 if (left < C::kCols) {
@@ -726,7 +752,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         while (pv.tile < t.n) {
             if (pv.slot == 0) {
                 wait(bar(C::kBarFull) + pv.stage * 8u, pv.phase, ctl);
-                if (t.partial(pv.tile)) wait(bar(C::kBarMask), 0u, ctl);
+                if (t.partial(pv.tile)) wait(bar(C::kBarMask + t.of_prefix(pv.tile)), 0u, ctl);
             }
             values(pv.slot, pv.stage, bv, pv.tile > 0, pv.tile == t.n - 1);
             if (++bv == C::kBufs) bv = 0, uses ^= 1u;
@@ -850,13 +876,13 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             __syncwarp();
             if ((i & 1) && t.partial(i / 2)) {
                 uint8_t* v = sm + C::kOffKv + stage * C::kTileBytes;
-                for (int r = t.len - (t.key0 + (i / 2) * kKeys) + lane / 8; r < kKeys; r += 4)
+                for (int r = t.length(i / 2) - t.first(i / 2) + lane / 8; r < kKeys; r += 4)
 #pragma unroll
                     for (int c = 0; c < DP / 64; ++c)
                         *reinterpret_cast<uint4*>(v + c * C::kSub + r * 128 + (lane % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 fence_async();
                 __syncwarp();
-                if (lane == 0) arrive(bar(C::kBarMask));
+                if (lane == 0) arrive(bar(C::kBarMask + t.of_prefix(i / 2)));
             }
             if (lane == 0) arrive(bar(C::kBarEmpty) + stage * 8u);
             if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
@@ -872,28 +898,37 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
 }
 
 template <int DP, int SLOTS>
-cudaError_t launch(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
-    return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS>, a.seg.items, Cfg<DP, SLOTS>::kThreads,
-                                   Cfg<DP, SLOTS>::kSmem, s, a, k, v);
+cudaError_t launch(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, const MafatAttnPrefix* prefix,
+                   cudaStream_t s) {
+    using C = Cfg<DP, SLOTS>;
+    if (prefix)
+        return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS, MafatAttnPrefix>, a.seg.items, C::kThreads, C::kSmem, s, a,
+                                       k, v, *prefix);
+    return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS, NoPrefix>, a.seg.items, C::kThreads, C::kSmem, s, a, k, v,
+                                   NoPrefix());
 }
-template <int DP, int SLOTS>
-cudaError_t prepare() {
+template <int DP, int SLOTS, class Prefix>
+cudaError_t prepare_form() {
     using C = Cfg<DP, SLOTS>;
     cudaFuncAttributes at;
-    cudaError_t e = cudaFuncGetAttributes(&at, attn_tc_kernel<DP, SLOTS>);
+    cudaError_t e = cudaFuncGetAttributes(&at, attn_tc_kernel<DP, SLOTS, Prefix>);
     if (e != cudaSuccess) return e;
     // with fewer registers at launch than the roles' shares add up to, setmaxnreg.inc would wait forever
     if (at.numRegs < C::kRegs) return cudaErrorInvalidConfiguration;
-    return cudaFuncSetAttribute(attn_tc_kernel<DP, SLOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                Cfg<DP, SLOTS>::kSmem);
+    return cudaFuncSetAttribute(attn_tc_kernel<DP, SLOTS, Prefix>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+}
+template <int DP, int SLOTS>
+cudaError_t prepare() {
+    const cudaError_t e = prepare_form<DP, SLOTS, NoPrefix>();
+    return e != cudaSuccess ? e : prepare_form<DP, SLOTS, MafatAttnPrefix>();
 }
 
 }  // namespace
 
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
-                                 cudaStream_t s) {
-    if (slots == 2) return a.dim <= 64 ? launch<64, 2>(a, k, v, s) : launch<128, 2>(a, k, v, s);
-    return a.dim <= 64 ? launch<64, 1>(a, k, v, s) : launch<128, 1>(a, k, v, s);
+                                 const MafatAttnPrefix* prefix, cudaStream_t s) {
+    if (slots == 2) return a.dim <= 64 ? launch<64, 2>(a, k, v, prefix, s) : launch<128, 2>(a, k, v, prefix, s);
+    return a.dim <= 64 ? launch<64, 1>(a, k, v, prefix, s) : launch<128, 1>(a, k, v, prefix, s);
 }
 
 cudaError_t mafat_prepare_attn_tc() {

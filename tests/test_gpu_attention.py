@@ -389,3 +389,21 @@ def test_long_fp32_sums_round_as_sums_do(mf, kernel):
     ref = attention64(q[0], [(k[0], v[0], torch.ones(T, S, dtype=torch.bool, device="cuda"))], 0.37 / 8)[0]
     off = ((o[0].double() - ref).square().mean() / ref.square().mean()).sqrt().item()
     assert off <= 2 * 2.0 ** -25 * math.sqrt(S / 2) + 1e-6, off
+
+
+@pytest.mark.parametrize("mask", [False, True])
+@pytest.mark.parametrize("G,R,T,P,S,H,Hk,D", [
+    (2, 5, 30, 150, 70, 8, 2, 64), (3, 2, 70, 128, 256, 8, 2, 128), (2, 3, 90, 40, 301, 4, 1, 80), (1, 2, 33, 300, 33, 8, 8, 128),
+    (2, 3, 1, 100, 20, 8, 2, 64)])
+def test_prefix_in_one_launch(mf, mask, G, R, T, P, S, H, Hk, D):
+    """Both sets read by the same tiles of rows (with a mask of the prefix, by two launches): lengths of zero on either side
+    and on both, below the tokens', around tiles, past the room."""
+    plan = mf.PrefixAttention(G, R, T, P, S, H, Hk, D)
+    assert plan.stats()["whole_ctas"] > 0
+    lens = [S, 0, T - 1, min(S, 128), S + 5, max(0, T - 7), 1]
+    pl = [P, 0, 129][:G]
+    kw = {}
+    if mask:
+        at = torch.arange(P, device="cuda")
+        kw["prefix_mask"] = torch.stack([at % 3 > 0, at < 0, at >= P // 2][:G])
+    _prefix(mf, G, R, T, P, S, H, Hk, D, mf.BF16, prefix_len=pl, own_len=[lens[i % 7] for i in range(G * R)], poison=True, **kw)
