@@ -71,7 +71,7 @@ struct Cfg {
     static constexpr int kOffKv = SLOTS * kTileBytes;
     static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
     static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + kBufs,
-                         kBarO = kBarP + kPParts * kBufs, kBarMask = kBarO + SLOTS, kBars = kBarMask + 2;
+                         kBarO = kBarP + kPParts * kBufs, kBarEnd = kBarO + SLOTS, kBarMask = kBarEnd + SLOTS, kBars = kBarMask + 2;
     // V of a tile is read after the scores of kBufs - 1 tiles more (one slot) or of one (two slots)
     static_assert(kLag <= kStages - (kBufs > 2 ? 2 * kBufs - 2 : 2), "gathered tiles");
     static constexpr int kOffTmem = kOffBar + (kBars * 8 + 15) / 16 * 16;
@@ -329,6 +329,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         }
         for (int i = 0; i < SLOTS; ++i) {
             bar_init(bar(C::kBarO + i), 1);
+            bar_init(bar(C::kBarEnd + i), 1);
         }
         for (int i = 0; i < C::kBufs; ++i) {
             bar_init(bar(C::kBarS + i), 1);
@@ -429,9 +430,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         t.n = (n + kKeys - 1) / kKeys;
     }
     const int live = SLOTS == 2 && b.row0 + 128 < g.rows ? 2 : 1;  // slots that have rows
+    // Buffers in use: the scores of tile j wait for the slot's product of tile j - 2 at the least, so that who waits for
+    // that of tile j - 1 is less than two phases of its barrier behind.
+    const int bufs = C::kBufs > 2 && live == 1 ? 2 : C::kBufs;
     // Scores of a slot are made before its product before them has ended: O is then waited for by a barrier
     // of its own, else the scores' says that it is there.
-    const bool ahead = live < C::kBufs;
+    const bool ahead = live < bufs;
 
     if (warp < C::kSoftmaxWarps) {
         if constexpr (C::kRegsSoftmax > C::kRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
@@ -561,7 +565,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             __syncwarp();
             if (lane == 0) arrive(bar(C::kBarP) + (uint32_t)(buf * C::kPParts + C::kPParts - 1) * 8u);
             buf += live;
-            if (buf >= C::kBufs) buf -= C::kBufs, uses ^= 1u;
+            if (buf >= bufs) buf -= bufs, uses ^= 1u;
         }
         // Through shared memory, 16-byte chunks swizzled over the rows, so that a row leaves in whole pieces:
         // kOutBytes of each row at a time, bf16 results at once, fp32 parts in two passes.  joins: with the parts of
@@ -590,7 +594,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             const int64_t dst = row >= g.rows ? -1 : a.direct ? w.o : w.part * a.dim;
             uint8_t* my = buf + lane * C::kOutBytes;
             if (n_tiles > 0) {
-                wait(bar(C::kBarO + slot), ahead ? (uint32_t)(t.n - 1) & 1u : 0u, ctl);
+                wait(bar(C::kBarEnd + slot), 0u, ctl);
                 __syncwarp();
                 fence_after();
             }
@@ -660,7 +664,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                         if (o >= 0 && d < a.dim) mafat_attn::put4((__nv_bfloat16*)a.out + o + d, v[i]);
                     }
                 } else {
-                    constexpr int kTogether = 8;  // read before they are written: writes might be to what is read
+                    constexpr int kTogether = kPieces < 8 ? kPieces : 8;  // read before they are written: writes might be to what is read
                     uint8_t* to_out = part ? (uint8_t*)(a.part_o + d) : (uint8_t*)((__nv_bfloat16*)a.out + d);
 #pragma unroll
                     for (int i0 = 0; i0 < kPieces; i0 += kTogether) {
@@ -719,7 +723,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                            vb + (uint32_t)k * (2048u / 16u), hi, id_o, part + i > 0 ? 1u : acc);
                 }
             }
-            commit_el(last || ahead ? el : 0u, bar(C::kBarO) + (uint32_t)slot * 8u);
+            commit_el(last || ahead ? el : 0u, bar(last ? C::kBarEnd : C::kBarO) + (uint32_t)slot * 8u);
         };
         // The scores of item n + kBufs follow the values of item n: products run in the order of issue,
         // so that its buffer is free.  Two places in the ring, each of K or V of a tile and the item's slot.
@@ -742,12 +746,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             if (ps.slot == 0) wait(bar(C::kBarFull) + ps.stage * 8u, ps.phase, ctl);
             fence_after();
             scores(ps.slot, ps.stage, bs);
-            if (++bs == C::kBufs) bs = 0;
+            if (++bs == bufs) bs = 0;
             const uint32_t empty = bar(C::kBarEmpty) + ps.stage * 8u;
             if (ps.next(live)) commit_el(el, empty);
         };
 #pragma unroll 1
-        for (int i = 0; i < C::kBufs; ++i) next_scores();
+        for (int i = 0; i < bufs; ++i) next_scores();
 #pragma unroll 1
         while (pv.tile < t.n) {
             if (pv.slot == 0) {
@@ -755,7 +759,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                 if (t.partial(pv.tile)) wait(bar(C::kBarMask + t.of_prefix(pv.tile)), 0u, ctl);
             }
             values(pv.slot, pv.stage, bv, pv.tile > 0, pv.tile == t.n - 1);
-            if (++bv == C::kBufs) bv = 0, uses ^= 1u;
+            if (++bv == bufs) bv = 0, uses ^= 1u;
             const uint32_t empty = bar(C::kBarEmpty) + pv.stage * 8u;
             if (pv.next(live)) commit_el(el, empty);
             next_scores();

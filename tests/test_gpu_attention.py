@@ -122,6 +122,19 @@ def test_cross_many_sequences(mf, kernel, dtype, B, T, H, Hk, D):
     _cross(mf, B, T, 290, H, Hk, D, dtype, kv_len=ln, kernel=kernel, poison=True, repeat=2)
 
 
+@pytest.mark.parametrize("mask", [False, True])
+@pytest.mark.parametrize("D", [64, 40, 128, 96])
+@pytest.mark.parametrize("T", [150, 256, 333, 385])
+def test_cross_tiles_of_256_rows(mf, T, D, mask):
+    """Work for all SMs in tiles of two slots, of which the last tile has one or both, and some rows of each."""
+    B, S = 152 // (-(-T // 256)), 700
+    plan = mf.CrossAttention(B, T, S, 1, 1, D)
+    assert plan.stats()["ctas"][0] == B * (-(-T // 256)) * plan.stats()["splits"][0]
+    at = torch.arange(S, device="cuda")
+    kw = {"kv_mask": torch.stack([at % (2 + i % 5) > 0 for i in range(B)])} if mask else {}
+    _cross(mf, B, T, S, 1, 1, D, mf.BF16, kv_len=[(97 * i + 300) % 760 for i in range(B)], poison=True, repeat=3, **kw)
+
+
 @pytest.mark.parametrize("kernel", KERNELS)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_cross_strides(mf, kernel, dtype):
