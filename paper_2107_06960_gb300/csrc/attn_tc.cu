@@ -40,9 +40,6 @@ struct Cfg {
     static constexpr int kSub = 128 * 128;                 // one 128-row x 64-channel block
     static constexpr int kTileBytes = DP / 64 * kSub;      // a tile of Q, K or V
     static constexpr int kStages = SLOTS == 2 ? (DP == 128 ? 5 : 8) : (DP == 128 ? 2 : 5);
-    // Gathered tile i is said to be there when tile i + kLag has been issued, into the stage of tile
-    // i + kLag - kStages, whose products must not wait for those of tile i.
-    static constexpr int kLag = kStages >= 5 ? 2 : 0;
     // warps that share a row of scores: two halves of its keys, where the CTA has the SM to itself
     static constexpr int kHalves = SLOTS;
     static constexpr int kCols = kKeys / kHalves;          // scores of a thread
@@ -72,8 +69,6 @@ struct Cfg {
     static constexpr int kOffBar = kOffKv + kStages * kTileBytes;
     static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarS = 2 * kStages, kBarP = kBarS + kBufs,
                          kBarO = kBarP + kPParts * kBufs, kBarEnd = kBarO + SLOTS, kBarMask = kBarEnd + SLOTS, kBars = kBarMask + 2;
-    // V of a tile is read after the scores of kBufs - 1 tiles more (one slot) or of one (two slots)
-    static_assert(kLag <= kStages - (kBufs > 2 ? 2 * kBufs - 2 : 2), "gathered tiles");
     static constexpr int kOffTmem = kOffBar + (kBars * 8 + 15) / 16 * 16;
     static constexpr int kOffBroken = kOffTmem + 4;
     static constexpr int kOffCount = kOffBroken + 4;                   // readable keys that each warp counted
@@ -323,8 +318,8 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&kmap)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&vmap)) : "memory");
         for (int i = 0; i < C::kStages; ++i) {
-            // gathered tiles are filled by three warps; others by TMA, and are also looked at by the mask warp
-            bar_init(bar(C::kBarFull + i), gather ? 3 : 1);
+            // gathered tiles are filled by three warps' threads; others by TMA, and are also looked at by the mask warp
+            bar_init(bar(C::kBarFull + i), gather ? 96 : 1);
             bar_init(bar(C::kBarEmpty + i), gather ? 1 : 2);
         }
         for (int i = 0; i < SLOTS; ++i) {
@@ -741,9 +736,13 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         };
         Place ps{0u, 0u, 0, 0}, pv{1u, 0u, 0, 0};
         int bs = 0, bv = 0;
+        auto wait_tile = [&](uint32_t stage, uint32_t phase) {
+            wait(bar(C::kBarFull) + stage * 8u, phase, ctl);
+            if (gather) fence_async();  // the copies' threads have not waited for them
+        };
         auto next_scores = [&]() {
             if (ps.tile >= t.n) return;
-            if (ps.slot == 0) wait(bar(C::kBarFull) + ps.stage * 8u, ps.phase, ctl);
+            if (ps.slot == 0) wait_tile(ps.stage, ps.phase);
             fence_after();
             scores(ps.slot, ps.stage, bs);
             if (++bs == bufs) bs = 0;
@@ -755,7 +754,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
 #pragma unroll 1
         while (pv.tile < t.n) {
             if (pv.slot == 0) {
-                wait(bar(C::kBarFull) + pv.stage * 8u, pv.phase, ctl);
+                wait_tile(pv.stage, pv.phase);
                 if (t.partial(pv.tile)) wait(bar(C::kBarMask + t.of_prefix(pv.tile)), 0u, ctl);
             }
             values(pv.slot, pv.stage, bv, pv.tile > 0, pv.tile == t.n - 1);
@@ -766,8 +765,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         }
     } else if (gather) {
         // Three warps copy the readable keys of the part, 128 at a time, as they are found: the first
-        // lists their numbers, all copy every third group of rows, and say that a tile is there once their
-        // copies have landed: when kLag more have been issued, or at once.
+        // lists their numbers, all copy every third group of rows, and their copies' landing says that a tile is there.
         const int who = warp - C::kLoadWarp;
         int* list = (int*)(sm + C::kOffList);  // [2][kKeys], then [kKeys] left over
         constexpr int kChunks = DP / 8, kRows = 32 / kChunks;
@@ -794,8 +792,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             }
         };
         if (who == 0) look(pos);
-        uint32_t stage = 0u, phase = 1u, told = 0u;
-        int open = 0;  // tiles copied, not yet said to be there
+        uint32_t stage = 0u, phase = 1u;
 #pragma unroll 1
         for (int j = 0; j < t.n; ++j) {
             int* keys = list + (j & 1) * kKeys;
@@ -841,26 +838,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
                             copy16(dst + (uint32_t)(q * 3 + who) * 1024u + at8[i],
                                    src[kv] + (int64_t)max(k, 0) * step[kv], k >= 0);
                         }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                ++open;
-                if (open > C::kLag) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(C::kLag) : "memory");
-                    fence_async();
-                    __syncwarp();
-                    if (lane == 0) arrive(bar(C::kBarFull) + told * 8u);
-                    if (++told == (uint32_t)C::kStages) told = 0u;
-                    --open;
-                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar(C::kBarFull) + stage * 8u)
+                             : "memory");
                 if (++stage == (uint32_t)C::kStages) stage = 0u, phase ^= 1u;
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        fence_async();
-        __syncwarp();
-        for (; open > 0; --open) {
-            if (lane == 0) arrive(bar(C::kBarFull) + told * 8u);
-            if (++told == (uint32_t)C::kStages) told = 0u;
-        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == C::kLoadWarp) {
         const uint32_t el = elect_one();
         uint32_t stage = ahead_loads % (uint32_t)C::kStages;
