@@ -26,6 +26,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kRun = 16;                // keys of a warp at a time
 constexpr int kBN = kWarps * kRun;
+constexpr int kMostJoin = 32;           // parts of the launch before
 
 template <int DP>
 struct Cfg {
@@ -356,6 +357,19 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             const mafat_attn::Out out(a, b, mafat_attn::Row(a, b, b.row0 + r));
             float inv = mafat_attn::inverse_sum(sum);
             if (a.join) {  // with the parts of the launch before: a lane has the weight of every kQuads-th
+                // sixteen parts' loads on their way together, the first with those of the weights
+                constexpr int kTogether = 16;
+                const float* src = a.part_o + out.row * a.dim + d;
+                float4 u[kTogether];
+                auto load_parts = [&](int p0) {
+#pragma unroll
+                    for (int e = 0; e < kTogether; ++e) {
+                        u[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (p0 + e < a.join && d < a.dim)
+                            u[e] = *reinterpret_cast<const float4*>(src + (int64_t)(p0 + e) * a.rows_total * a.dim);
+                    }
+                };
+                load_parts(0);
                 const float own = mafat_attn::row_lse2(top, sum);
                 float lse[kSets], best = own;
 #pragma unroll
@@ -376,26 +390,18 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                 total += x;
                 inv = sum == 0.f ? 0.f : x / sum;  // then all are divided by the total
                 v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-                const float* src = a.part_o + out.row * a.dim + d;
-                // eight parts' loads on their way together
 #pragma unroll
-                for (int k = 0; k < kSets; ++k)
-#pragma unroll 1
-                    for (int p0 = k * kQuads; p0 < min((k + 1) * kQuads, a.join); p0 += 8) {
-                        float4 u[8];
+                for (int p0 = 0; p0 < kMostJoin; p0 += kTogether) {
+                    if (p0 >= a.join) break;
+                    if (p0 > 0) load_parts(p0);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            u[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (p0 + e < a.join && d < a.dim)
-                                u[e] = *reinterpret_cast<const float4*>(src + (int64_t)(p0 + e) * a.rows_total * a.dim);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {  // past the last part: u is zero
-                            const float f = __shfl_sync(0xffffffffu, lse[k], (lane & ~(kQuads - 1)) + (p0 + e) % kQuads);
-                            v = make_float4(fmaf(f, u[e].x, v.x), fmaf(f, u[e].y, v.y), fmaf(f, u[e].z, v.z),
-                                            fmaf(f, u[e].w, v.w));
-                        }
+                    for (int e = 0; e < kTogether; ++e) {  // past the last part: u is zero
+                        const float f =
+                            __shfl_sync(0xffffffffu, lse[p0 / kQuads], (lane & ~(kQuads - 1)) + (p0 + e) % kQuads);
+                        v = make_float4(fmaf(f, u[e].x, v.x), fmaf(f, u[e].y, v.y), fmaf(f, u[e].z, v.z),
+                                        fmaf(f, u[e].w, v.w));
                     }
+                }
                 inv = mafat_attn::inverse_sum(total);
                 if (mine && d == 0 && a.lse)
                     a.lse[out.row] = total == 0.f ? -CUDART_INF_F : (base + log2f(total)) * CUDART_LN2_F;
@@ -436,7 +442,7 @@ cudaError_t prepare() {
 }  // namespace
 
 int mafat_attn_rows_keys() { return kBN; }
-int mafat_attn_rows_join() { return 32; }
+int mafat_attn_rows_join() { return kMostJoin; }
 
 cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
     return a.dim <= 64 ? launch<64>(a, ctas, s) : launch<128>(a, ctas, s);
