@@ -157,10 +157,12 @@ struct Join {
     __device__ __forceinline__ Join(const MafatAttnArgs& a, const Out& w, float base, float l) {
         const float mine = row_lse2(base, l);
         top = mine;
+#pragma unroll 4
         for (int p = 0; p < a.join; ++p) top = max_nan(top, a.part_lse[(int64_t)p * a.rows_total + w.row]);
         if (top == -CUDART_INF_F) top = 0.f;  // no readable key anywhere: all factors are zero
         const float x = exp2_fast(mine - top);
         float sum = x;
+#pragma unroll 4
         for (int p = 0; p < a.join; ++p) sum += exp2_fast(a.part_lse[(int64_t)p * a.rows_total + w.row] - top);
         inv = inverse_sum(sum);
         own = l == 0.f ? 0.f : x * inv / l;
