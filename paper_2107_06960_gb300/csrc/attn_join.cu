@@ -3,7 +3,7 @@
 // With the parts' results O_p, each normalised, and their log2 sums z_p:  O = sum_p 2^(z_p - z) O_p / sum_p 2^(z_p - z),
 // z = max z_p: three fp32 operations for 4 bytes read.  Bound by the round trips of its loads for few rows (a warp a row
 // has the loads of 16 or 32 parts on their way together, 1.6 us a round), by the parts' bytes (in L2, just written) for
-// many: 8192 rows of 128 channels add 14 us with 2 parts and 32 with 8, 2 to 3.5 TB/s there and back.
+// many: 8192 rows of 128 channels add 13 us with 2 parts and 26 with 8, 1.3 to 2.6 TB/s there and back.
 #include "attn_common.cuh"
 
 namespace {

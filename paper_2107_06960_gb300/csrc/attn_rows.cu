@@ -10,12 +10,12 @@
 // accumulators are P's operand as they are.  P is rounded to bf16 for its product; all else is fp32.
 //
 // Items of the longest sequences are taken first, and a CTA's next from the other end of the order: 64 sequences of half
-// to all of 1444 keys (one token, 32 query and 8 key heads) take 49.5 us, as they are given 55, 128 channels; 29.4 and
+// to all of 1444 keys (one token, 32 query and 8 key heads) take 48 us, as they are given 54, 128 channels; 29 and
 // 31.5 with 64.  (In the kernels whose CTAs have one item each, finding its sequence cost what it brought.)
 //
 // Keys that are not readable are not copied but filled with zeros, so that 0 x NaN cannot reach O.
 //
-// One token of 64 sequences, 32 query and 8 key heads, 1444 keys: 61 us or 6.2 TB/s with 128 channels, 34 us or 5.5 TB/s
+// One token of 64 sequences, 32 query and 8 key heads, 1444 keys: 59 us or 6.4 TB/s with 128 channels, 34 us or 5.5 TB/s
 // with 64; under 40 % of the issue slots are taken.  One token of one sequence (8 query and 4 key heads, 1444 keys) is
 // bound by round trips: 5.2 us in 4 clusters of 8 CTAs, 5.8 with a launch that joins the parts.
 #include "attn_common.cuh"

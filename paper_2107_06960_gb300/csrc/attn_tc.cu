@@ -16,9 +16,12 @@
 // O is rescaled only where b' is more than 8 above the b in use (a power that cancels in O / l and
 // leaves P at most 256, well inside bf16), so that few tiles touch O outside the products.
 //
-// Bound, for long sequences, by the softmax between the two products: with 128 channels the tensor pipe is busy 70 % of
-// the time, with 64, whose products take half as long for the same exponentials, 49 %, the special function unit
-// as much and the issue slots 62 %.  8 x 2048 tokens, 16 query and 4 key heads, 5776 keys: 480 us or 1.61 PFLOP/s with 128
+// Rows whose keys are a shared prefix and then their own are done in one launch where that is better (attention.cpp has
+// the rule): the tiles of the prefix come first, each set with its own maps, length and partial last tile.
+//
+// Bound, for long sequences, by the softmax between the two products: with 128 channels the tensor pipe is busy 74 % of
+// the time, with 64, whose products take half as long for the same exponentials, 50 %, the special function unit
+// as much and the issue slots 63 %.  8 x 2048 tokens, 16 query and 4 key heads, 5776 keys: 480 us or 1.61 PFLOP/s with 128
 // channels, 339 us or 1.14 with 64.  For few keys by the round trips of an item's start and end, about 5 us: of two
 // CTAs on an SM, one slot each, one works meanwhile.
 //
