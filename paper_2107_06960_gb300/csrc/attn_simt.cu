@@ -46,25 +46,18 @@ __device__ __forceinline__ void fma2(float2& r, float2 a, float2 b) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
 }
 
-// One row's share of the online softmax for the N scores of a lane, whose warp has the row's others:
-// s becomes the weights; returns the factor of what was summed before.
-template <int N>
-__device__ __forceinline__ float softmax_step(float (&s)[N], float& base, float& l, float scale_log2) {
-    float top = s[0];
+// One row's share of the online softmax for the score of a lane, whose WIDTH neighbours have the row's others:
+// s becomes the weight; returns the factor of what was summed before.
+template <int WIDTH>
+__device__ __forceinline__ float softmax_step(float& s, float& base, float& l, float scale_log2) {
+    float top = s;
 #pragma unroll
-    for (int j = 1; j < N; ++j) top = mafat_attn::max_nan(top, s[j]);
-#pragma unroll
-    for (int w = 1; w < 32; w *= 2) top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, w));
+    for (int w = 1; w < WIDTH; w *= 2) top = mafat_attn::max_nan(top, __shfl_xor_sync(0xffffffffu, top, w));
     const float next = mafat_attn::max_nan(base, top * scale_log2), off = mafat_attn::subtrahend(next);
     const float keep = mafat_attn::exp2_fast(base - off);
     base = next;
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        s[j] = mafat_attn::exp2_fast(fmaf(s[j], scale_log2, -off));
-        sum += s[j];
-    }
-    l = l * keep + sum;  // of the lane's keys
+    s = mafat_attn::exp2_fast(fmaf(s, scale_log2, -off));
+    l = l * keep + s;  // of the lane's keys
     return keep;
 }
 
@@ -437,17 +430,24 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
         }
         const int k = key + key_of;
         const bool seen = k < b.len && (!mask || mask[k] != 0);
+        float keep[R];
+        bool moved = false;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int limit = g.causal ? mafat_attn::Row(a, b, b.row0 + r).limit(a, b) : b.len;
-            float s[1] = {acc[r].x + acc[r].y};
+            float s = acc[r].x + acc[r].y;
 #pragma unroll
-            for (int w = kRun; w < 32; w *= 2) s[0] += __shfl_xor_sync(0xffffffffu, s[0], w);
-            if (!seen || k >= limit) s[0] = -INFINITY;
-            const float keep = softmax_step(s, base[r], l[r], a.scale_log2);  // l: each key in four lanes
-            if (part == 0) sp[r * kRun + key_of] = s[0];
+            for (int w = kRun; w < 32; w *= 2) s += __shfl_xor_sync(0xffffffffu, s, w);
+            if (!seen || k >= limit) s = -INFINITY;
+            keep[r] = softmax_step<kRun>(s, base[r], l[r], a.scale_log2);  // l: each key in four lanes
+            moved = moved || keep[r] != 1.f;
+            if (part == 0) sp[r * kRun + key_of] = s;
+        }
+        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-            for (int d = 0; d < kCh / 2; ++d) o[r][d] = make_float2(o[r][d].x * keep, o[r][d].y * keep);
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int d = 0; d < kCh / 2; ++d) o[r][d] = make_float2(o[r][d].x * keep[r], o[r][d].y * keep[r]);
         }
         __syncwarp();
 #pragma unroll
