@@ -267,8 +267,8 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
         } else if (second && m.us(1) <= x.us + kOwnJoinUs) {
             x = {1, 1, m.us(1)};  // whole: it then joins the first launch's parts itself
         } else if (p.n_run == 1 && is_rows(kernels[i]) && m.items == (int64_t)g.n_seq * p.heads_kv && x.n > 1) {
-            // A cluster joins its parts itself, which saves the launch for it: 5.2 us against 5.8 for one token of 8
-            // heads over 1444 states, 7.6 against 8.7 for 16 requests, 6.5 against 7.8 for 4 over 676 of 32 heads.
+            // A cluster joins its parts itself, which saves the launch for it: 5.1 us against 5.8 for one token of 8
+            // heads over 1444 states, 7.2 against 8.7 for 16 requests, 6.3 against 7.4 for 4 over 676 of 32 heads.
             for (int32_t n = kMostCluster; n > 1 && x.cluster == 1; n /= 2)
                 // clusters of CTAs that fill their SM find half of the SMs, not all, side by side
                 if (n <= m.tiles && m.items * n <= (int64_t)sms * m.sh.ctas / (m.sh.ctas == 1 ? 2 : 1) &&

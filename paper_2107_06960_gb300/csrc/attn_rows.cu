@@ -17,7 +17,7 @@
 //
 // One token of 64 sequences, 32 query and 8 key heads, 1444 keys: 59 us or 6.4 TB/s with 128 channels, 34 us or 5.5 TB/s
 // with 64; under 40 % of the issue slots are taken.  One token of one sequence (8 query and 4 key heads, 1444 keys) is
-// bound by round trips: 5.2 us in 4 clusters of 8 CTAs, 5.8 with a launch that joins the parts.
+// bound by round trips: 5.1 us in 4 clusters of 8 CTAs, 5.8 with a launch that joins the parts.
 #include "attn_common.cuh"
 
 namespace {
@@ -28,16 +28,19 @@ constexpr int kRun = 16;                // keys of a warp at a time
 constexpr int kBN = kWarps * kRun;
 constexpr int kMostJoin = 32;           // parts of the launch before
 
-template <int DP>
+template <int DP, bool CLUSTER>
 struct Cfg {
     static constexpr int kStages = DP == 128 ? 2 : 4;
     static constexpr int kMatrix = kRun * DP * 2;       // bytes of a run of K or V
     static constexpr int kRing = kStages * 2 * kMatrix;  // of a warp
     static constexpr int kOffQ = kWarps * kRing;         // queries of this item and of the next
     static constexpr int kQ = 16 * DP * 2;
-    static constexpr int kOffJoin = kOffQ + 2 * kQ;
+    // in a cluster there is no next item: the others' parts of rows come to where its queries would be, and beyond
+    static constexpr int kOffParts = kOffQ + kQ, kParts = mafat_attn::ClusterParts<16, DP>::kBytes;
+    static constexpr int kOffJoin = kOffQ + (CLUSTER ? kQ + kParts : 2 * kQ);
     static constexpr int kPitch = DP + 4;                // floats of a row of O while the warps are joined
-    static constexpr int kSmem = kOffJoin + (kWarps * 16 * (kPitch + 2) + 16) * 4;
+    static constexpr int kSmem = kOffJoin + kWarps * 16 * (kPitch + 2) * 4;
+    static_assert(kSmem + 1024 <= 115712, "two CTAs on an SM, with the order's table");
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
@@ -145,7 +148,8 @@ struct Ahead : Items {
 // other form's inner loop 20 %)
 template <int DP, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ MafatAttnArgs a) {
-    using C = Cfg<DP>;
+    using C = Cfg<DP, CLUSTER>;
+    using Parts = mafat_attn::ClusterParts<16, DP>;
     constexpr int kChunks = DP / 8;        // 16-byte chunks of a row
     constexpr int kRows = 32 / kChunks;    // rows of one access of a warp
     constexpr int kSteps = DP / 16;
@@ -155,6 +159,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     const uint32_t smem = (uint32_t)__cvta_generic_to_shared(sm), ring = smem + warp * C::kRing;
     const int cc = lane % kChunks, cr = lane / kChunks;
     const bool in_dim = cc * 8 < a.dim;
+    if constexpr (CLUSTER) Parts::start();
     mafat_attn::launch_begin(a);
 
     __shared__ int2 order[kMafatMostOrdered];
@@ -213,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     const int v_row = (mi % 2) * 8 + mj, v_chunk = mi / 2;   // V: channels 0-7 and 8-15, each with keys 0-7 and 8-15
     float* so = (float*)(sm + C::kOffJoin);
     float* sml = so + kWarps * 16 * C::kPitch;
-    float* part_lse = sml + kWarps * 16 * 2;  // of a row, for the cluster
+    const Parts parts(a, sm + C::kOffParts);
 
     uint32_t which = 0u;
 #pragma unroll 1
@@ -328,6 +333,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             mafat_attn::launch_wait();
             waited = true;
         }
+        if constexpr (CLUSTER) Parts::started();
         const int rows = min(16, g.rows - b.row0);
         constexpr int kQuads = DP / 4, kSets = 32 / kQuads;  // lanes of a row; rows of a warp, and parts of a lane
         const int d = lane % kQuads * 4;
@@ -407,20 +413,20 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                     a.lse[out.row] = total == 0.f ? -CUDART_INF_F : (base + log2f(total)) * CUDART_LN2_F;
             } else if (mine && d == 0) {
                 if constexpr (CLUSTER)
-                    part_lse[r] = mafat_attn::row_lse2(top, sum);
+                    parts.put_sum(r, mafat_attn::row_lse2(top, sum));
                 else
                     mafat_attn::store_lse(a, out, top, sum);
             }
             if (!mine || d >= a.dim) continue;
             v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-            if constexpr (CLUSTER)  // in place of the first warp's, which this thread has read
-                *reinterpret_cast<float4*>(so + r * C::kPitch + d) = v;
+            if constexpr (CLUSTER)
+                parts.put(r, d, v);
             else if (a.direct)
                 *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + out.o + d) = make_uint2(pack(v.x, v.y), pack(v.z, v.w));
             else
                 *reinterpret_cast<float4*>(a.part_o + out.part * a.dim + d) = v;
         }
-        if constexpr (CLUSTER) mafat_attn::join_cluster<__nv_bfloat16, kWarps>(a, b, so, C::kPitch, part_lse, rows);
+        if constexpr (CLUSTER) parts.template join<__nv_bfloat16, kWarps>(a, b, rows);
     }
     wait_copies<0>();
     mafat_attn::launch_end(a);
@@ -429,14 +435,14 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
     return mafat_launch_clusters(a.cluster, a.cluster > 1 ? attn_rows_kernel<DP, true> : attn_rows_kernel<DP, false>,
-                                 (unsigned)ctas, kThreads, Cfg<DP>::kSmem, s, a);
+                                 (unsigned)ctas, kThreads, a.cluster > 1 ? Cfg<DP, true>::kSmem : Cfg<DP, false>::kSmem, s, a);
 }
 template <int DP>
 cudaError_t prepare() {
     const cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               Cfg<DP>::kSmem);
+                                               Cfg<DP, false>::kSmem);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(attn_rows_kernel<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP>::kSmem);
+    return cudaFuncSetAttribute(attn_rows_kernel<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP, true>::kSmem);
 }
 
 }  // namespace

@@ -341,26 +341,29 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
 
 constexpr int kFewWarps = 8, kRun = 8;  // keys of a warp at a time
 
-template <int R, int DP>
+template <int R, int DP, bool CLUSTER>
 struct Few {
     static constexpr int kThreads = kFewWarps * 32;
     static constexpr int kStages = 3;  // with 64 channels two CTAs share an SM
     static constexpr int kPitch = DP + 4;
     static constexpr int kStage = kRun * (kPitch + DP);               // floats of a run of K and V
     static constexpr int kWarp = kStages * kStage + R * kRun;         // and the weights
-    static constexpr int kSmem = (R * DP + kFewWarps * kWarp) * 4;
-    static_assert(kFewWarps * R * (DP + 2) + R <= kFewWarps * kWarp, "the join's space is the rings'");
+    static constexpr int kOffParts = (R * DP + kFewWarps * kWarp) * 4;
+    static constexpr int kSmem = kOffParts + (CLUSTER ? mafat_attn::ClusterParts<R, DP>::kBytes : 0);
+    static_assert(kFewWarps * R * (DP + 2) <= kFewWarps * kWarp, "the join's space is the rings'");
 };
 
 template <int R, int DP, bool CLUSTER>
 __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_few_kernel(const __grid_constant__ MafatAttnArgs a) {
-    using L = Few<R, DP>;
+    using L = Few<R, DP, CLUSTER>;
+    using Parts = mafat_attn::ClusterParts<R, DP>;
     constexpr int kCh = DP / 32;
     extern __shared__ __align__(16) float sm[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     float* sq = sm;
     float* ring = sm + R * DP + warp * L::kWarp;
     float* sp = ring + L::kStages * L::kStage;
+    if constexpr (CLUSTER) Parts::start();
     mafat_attn::launch_begin(a);
     const mafat_attn::Block b(a, blockIdx.x, R, kBN);
     const MafatAttnSeg& g = a.seg;
@@ -482,7 +485,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
     // join the warps: O, base and l of each in shared memory
     float* so = sm + R * DP;
     float* sml = so + kFewWarps * R * DP;
-    float* part_lse = sml + kFewWarps * R * 2;  // of a row, for the cluster
+    const Parts parts(a, (uint8_t*)sm + L::kOffParts);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -497,6 +500,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
     }
     __syncthreads();
     const int rows = min(R, g.rows - b.row0);
+    if constexpr (CLUSTER) Parts::started();
     for (int i = threadIdx.x; i < rows * kChunks; i += L::kThreads) {
         const int r = i / kChunks, d = i % kChunks * 4;
         float top = -INFINITY;
@@ -512,16 +516,16 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
             const float4 u = load4(so + (w * R + r) * DP + d);
             v = make_float4(fmaf(x, u.x, v.x), fmaf(x, u.y, v.y), fmaf(x, u.z, v.z), fmaf(x, u.w, v.w));
         }
-        if constexpr (CLUSTER) {  // in place of the first warp's, which this thread has read
+        if constexpr (CLUSTER) {
             const float inv = mafat_attn::inverse_sum(sum);
-            store4(so + r * DP + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-            if (d == 0) part_lse[r] = mafat_attn::row_lse2(top, sum);
+            if (d < a.dim) parts.put(r, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+            if (d == 0) parts.put_sum(r, mafat_attn::row_lse2(top, sum));
         } else {
             const Writer w(a, b, b.row0 + r, top, sum, d == 0);
             w.put(a, d, v);
         }
     }
-    if constexpr (CLUSTER) mafat_attn::join_cluster<float, kFewWarps>(a, b, so, DP, part_lse, rows);
+    if constexpr (CLUSTER) parts.template join<float, kFewWarps>(a, b, rows);
     mafat_attn::launch_end(a);
 }
 
@@ -534,7 +538,8 @@ template <int R, int DP>
 cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
     return mafat_launch_clusters(a.cluster,
                                  a.cluster > 1 ? attn_simt_few_kernel<R, DP, true> : attn_simt_few_kernel<R, DP, false>,
-                                 a.seg.items, Few<R, DP>::kThreads, Few<R, DP>::kSmem, s, a);
+                                 a.seg.items, kFewWarps * 32,
+                                 a.cluster > 1 ? Few<R, DP, true>::kSmem : Few<R, DP, false>::kSmem, s, a);
 }
 cudaError_t prepare(const void* fn, int smem) {
     return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -546,8 +551,8 @@ cudaError_t prepare_tiles() {
 }
 template <int R, int DP>
 cudaError_t prepare_few() {
-    const cudaError_t e = prepare((const void*)attn_simt_few_kernel<R, DP, false>, Few<R, DP>::kSmem);
-    return e != cudaSuccess ? e : prepare((const void*)attn_simt_few_kernel<R, DP, true>, Few<R, DP>::kSmem);
+    const cudaError_t e = prepare((const void*)attn_simt_few_kernel<R, DP, false>, Few<R, DP, false>::kSmem);
+    return e != cudaSuccess ? e : prepare((const void*)attn_simt_few_kernel<R, DP, true>, Few<R, DP, true>::kSmem);
 }
 
 }  // namespace
