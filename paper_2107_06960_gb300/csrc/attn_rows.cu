@@ -49,6 +49,8 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// also for those that are in no group yet
+__device__ __forceinline__ void wait_all_copies() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -227,8 +229,9 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
         const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
         const int first = b.key0 + warp * kRun;
         const int runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
-        // this item's queries are there (each warp's share), and the item before is joined
-        wait_copies<0>();
+        // this item's queries are there (each warp's share), and the item before is joined.  Their copies are in the
+        // group of the run after them; a warp that had no run in the item before has closed no group since.
+        wait_all_copies();
         __syncthreads();
         uint32_t q[kSteps][4];
 #pragma unroll
