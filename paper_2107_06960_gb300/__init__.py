@@ -573,7 +573,9 @@ class PrefixAttention(_Attention):
 def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_group=0, eps=1e-6, stream=None):
     """mafat_rms_norm on [rows][cols] tensors: h = x + residual (written to residual_out if given),
     y = h / sqrt(mean(h^2) + eps) * weight, in x's type, or in float8_e4m3fn with fp32 scales
-    [rows][1] (scale_group 0) or [rows][ceil(cols / 128)] (scale_group 128)."""
+    [rows][1] (scale_group 0) or [rows][ceil(cols / 128)] (scale_group 128).
+
+    Rows may be those of a wider matrix, 16-byte aligned at the first; rows broadcast by expand() are refused."""
     shape, dt, out_dt = x.shape, x.dtype, y.dtype
     # The common call, all packed: checked in one expression (a look at an attribute takes 50 ns, a call
     # of _addr 300).
@@ -590,14 +592,23 @@ def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_
                 None if residual_out is None else residual_out.data_ptr(), y.data_ptr(),
                 _addr("scales", scales, scales_shape, f32_), _launch_stream(stream, x)))
             return
-    strides = tuple(0 if t is None or t.dim() != 2 or t.shape[0] < 2 else t.stride(0)
-                    for t in (x, residual, residual_out, y))
+    strides = tuple(_row_stride(*t) for t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y)))
     desc, f32_, scales_shape = _norm_call(shape, dt, out_dt, scale_group, eps, strides)
     sx, sr, so, sy = [(st, 1) for st in strides]
     _check(lib.mafat_rms_norm(
         desc, _addr("x", x, shape, dt, sx), _addr("residual", residual, shape, dt, sr),
         _addr("weight", weight, shape[1:], dt), _addr("residual_out", residual_out, shape, dt, so),
         _addr("y", y, shape, out_dt, sy), _addr("scales", scales, scales_shape, f32_), _launch_stream(stream, x)))
+
+
+def _row_stride(name, t):
+    """The descriptor's stride of rows, 0 where there is nothing to step to.  Rows that share places (a row expanded
+    to many has a stride of 0, which would stand for packed ones) are refused."""
+    if t is None or t.dim() != 2 or t.shape[0] < 2:
+        return 0
+    if t.stride(0) < t.shape[1]:
+        raise MafatError(EINVAL, "%s: a row stride of %d is smaller than cols" % (name, t.stride(0)))
+    return t.stride(0)
 
 
 @functools.lru_cache(maxsize=256)
@@ -611,8 +622,6 @@ def _norm_call(shape, dt, out_dt, scale_group, eps, strides):
     d = NormDesc(struct_size=ctypes.sizeof(NormDesc), cols=cols, rows=rows, scale_group=scale_group, eps=eps)
     d.dtype, d.out_dtype = (c if isinstance(c, int) else -1 for c in (code.get(dt), code.get(out_dt)))
     if strides is not None:
-        if any(st < 0 or 0 < st < cols for st in strides):
-            raise MafatError(EINVAL, "a row stride is smaller than cols")
         d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride = strides
     return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1)
 
