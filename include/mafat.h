@@ -509,7 +509,7 @@ void mafat_attn_destroy(mafat_attn_t* plan);
 /* Root-mean-square norm of rows with the residual's addition:
  *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * weight,
  * computed in fp32 and rounded once.  With out_dtype MAFAT_E4M3, y holds the norm divided by a
- * scale s and rounded to 8 bits, s = max |norm| / 448 over scale_group channels (1 where all are 0):
+ * scale s and rounded to 8 bits, s = max |norm| / 448 over scale_group channels (1 where that is 0 in fp32):
  * y * s stands for the norm. */
 typedef struct {
     int32_t struct_size;        /* sizeof(mafat_norm_desc) */

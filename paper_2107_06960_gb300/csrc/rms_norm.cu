@@ -1,7 +1,7 @@
 // Root-mean-square norm with the residual's addition:
 //   h = x + r,  y = h / sqrt(mean(h^2) + eps) * w,
 // y in the inputs' type or in 8 bits: y / s rounded to e4m3 with s = max |y| / 448 over the row or
-// over each 128 channels (s = 1 where all are zero).
+// over each 128 channels (s = 1 where that is 0 in fp32).
 //
 // One pass: a row's sums stay in registers between the sum of squares and the output, so that x, r
 // are read and h, y written once; bound by those bytes.  Everything is fp32 until a result is
@@ -157,7 +157,11 @@ __device__ __forceinline__ void divide(float (&v)[V], float s) {
         for (int j = 0; j < V; ++j) v[j] *= r;
     }
 }
-__device__ __forceinline__ float scale_of(float top) { return top == 0.f ? 1.f : top / kE4m3Max; }
+// 1 where the quotient is 0, which it also is for values below 448 * 2^-150
+__device__ __forceinline__ float scale_of(float top) {
+    const float s = top / kE4m3Max;
+    return s == 0.f ? 1.f : s;
+}
 
 // V channels an access, N accesses a thread.  blockDim = (32, warps of a row, rows).
 template <class T, int V, int N, MafatNormQuant Q>
