@@ -522,7 +522,8 @@ typedef struct {
     int64_t x_stride, residual_stride, residual_out_stride, y_stride;  /* of rows, in elements (0: cols) */
 } mafat_norm_desc;
 
-/* Runs the norm on `stream` (asynchronous, one launch, no workspace, capturable).  residual and
+/* Runs the norm on `stream` (asynchronous, one launch, no workspace, capturable).  All pointers are device memory of the
+ * current device, 16-byte aligned (scales: 4-byte).  residual and
  * residual_out (h) may be NULL; scales [rows][1 or ceil(cols / 128)] fp32 for MAFAT_E4M3, else NULL.
  * residual_out, and y of x's type, may be x or residual itself (same address and row stride); other overlaps are refused. */
 mafat_status mafat_rms_norm(const mafat_norm_desc* desc, const void* x, const void* residual, const void* weight,

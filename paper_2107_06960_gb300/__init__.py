@@ -416,44 +416,52 @@ def _type(code):
     return _TYPES.get(code)
 
 
-def _code(t):
-    _type(BF16)
-    return next((code for code, dt in _TYPES.items() if dt is t.dtype), -1)
+def _current_device():
+    """Index of the GPU that kernels are launched on.  For when there is a tensor on one."""
+    global _current_device
+    import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current_device()
 
 
-def _addr(name, t, shape, dtype, strides=None):
+def _addr(name, t, shape, dtype, device, strides=None):
     """Address of a tensor, or of raw memory given as an int.  Refuses a tensor that is not what the plan
-    was made for (the library sees only its address); dtype: a torch type, strides None: packed."""
+    was made for (the library sees only its address); dtype: a torch type, device: an index (None: the current one),
+    strides None: packed."""
     if t is None:
         return None
     try:
-        if t.dtype is dtype and t.is_cuda and t.shape == shape and (t.is_contiguous() if strides is None
-                                                                    else t.stride() == strides):
+        if t.dtype is dtype and t.get_device() == device and t.shape == shape and (
+                t.is_contiguous() if strides is None else t.stride() == strides):
             return t.data_ptr()
     except AttributeError:
         if not hasattr(t, "data_ptr"):
             return _ptr(t)  # the caller's word
         raise
     if dtype is _TYPES["mask"] and t.dtype is _TYPES["byte"]:
-        return _addr(name, t, shape, t.dtype, strides)
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape:
-        raise MafatError(EINVAL, "%s: %s %s on %s, expected %s %s on the GPU"
-                         % (name, tuple(t.shape), t.dtype, t.device, tuple(shape), dtype))
-    if strides is None or any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
+        return _addr(name, t, shape, t.dtype, device, strides)
+    if device is None and t.is_cuda:
+        device = _current_device()
+    if t.dtype is not dtype or not t.is_cuda or t.get_device() != device or t.shape != shape:
+        raise MafatError(EINVAL, "%s: %s %s on %s, expected %s %s on %s"
+                         % (name, tuple(t.shape), t.dtype, t.device, tuple(shape), dtype,
+                            "a GPU" if device is None else "cuda:%d" % device))
+    if not t.is_contiguous() if strides is None else any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
         raise MafatError(EINVAL, "%s: strides %s, expected %s" % (name, t.stride(), strides or "packed"))
     return t.data_ptr()
 
 
-def _launch_stream(stream, like):
-    """As _stream; the current stream without making an object of it (a call takes 1 us instead of 3)."""
+def _launch_stream(stream, on, like):
+    """As _stream; the current stream of GPU `on`, where the tensors are, without making an object of it (a call takes
+    1 us instead of 3)."""
     global _raw_stream
-    if stream is None and getattr(like, "is_cuda", False):
-        if _raw_stream is None:
-            import torch
-            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-                lambda device: torch.cuda.current_stream(device).cuda_stream)
-        return _raw_stream(like.get_device())
-    return _stream(stream, like)
+    if stream is not None or on is None or not hasattr(like, "get_device"):
+        return _stream(stream, like)
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _raw_stream(on)
 
 
 _raw_stream = None  # device index -> its current stream's handle
@@ -472,6 +480,8 @@ class _Attention:
         self.handle = h
         self.dtype = desc.dtype
         self._types = None
+        # of the plan and so of its tensors; a run refuses to start while another is the current one
+        self.device = None if desc.dry_run else _current_device()
 
     @staticmethod
     def _layout(n, given):
@@ -528,10 +538,12 @@ class CrossAttention(_Attention):
         """q, out [batch][n_q][heads_q][head_dim]; k, v [batch][n_kv][heads_kv][head_dim]; kv_len
         [batch] int32; kv_mask [batch][n_kv] bool (False: not readable); lse [batch][n_q][heads_q] fp32."""
         (dt, i32_, mask, f32_), (nq, sq), (nk, sk) = self._types or self._torch(), self._q, self._k
+        on = self.device
         _check(lib.mafat_cross_run(
-            self.handle, _addr("q", q, nq, dt, sq), _addr("k", k, nk, dt, sk), _addr("v", v, nk, dt, self._v[1]),
-            _addr("kv_len", kv_len, nk[:1], i32_), _addr("kv_mask", kv_mask, nk[:2], mask),
-            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], f32_), _launch_stream(stream, q)))
+            self.handle, _addr("q", q, nq, dt, on, sq), _addr("k", k, nk, dt, on, sk),
+            _addr("v", v, nk, dt, on, self._v[1]), _addr("kv_len", kv_len, nk[:1], i32_, on),
+            _addr("kv_mask", kv_mask, nk[:2], mask, on), _addr("out", out, nq, dt, on, self._out[1]),
+            _addr("lse", lse, nq[:3], f32_, on), _launch_stream(stream, on, q)))
 
 
 class PrefixAttention(_Attention):
@@ -562,12 +574,14 @@ class PrefixAttention(_Attention):
         [prefixes], own_len [prefixes * requests] int32; prefix_mask [prefixes][n_prefix] bool; lse fp32."""
         dt, i32_, mask, f32_ = self._types or self._torch()
         (nq, sq), (npre, spk), (nown, sok) = self._q, self._pk, self._ok
+        on = self.device
         _check(lib.mafat_prefix_run(
-            self.handle, _addr("q", q, nq, dt, sq), _addr("prefix_k", prefix_k, npre, dt, spk),
-            _addr("prefix_v", prefix_v, npre, dt, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], i32_),
-            _addr("prefix_mask", prefix_mask, npre[:2], mask), _addr("own_k", own_k, nown, dt, sok),
-            _addr("own_v", own_v, nown, dt, self._ov[1]), _addr("own_len", own_len, nq[:1], i32_),
-            _addr("out", out, nq, dt, self._out[1]), _addr("lse", lse, nq[:3], f32_), _launch_stream(stream, q)))
+            self.handle, _addr("q", q, nq, dt, on, sq), _addr("prefix_k", prefix_k, npre, dt, on, spk),
+            _addr("prefix_v", prefix_v, npre, dt, on, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], i32_, on),
+            _addr("prefix_mask", prefix_mask, npre[:2], mask, on), _addr("own_k", own_k, nown, dt, on, sok),
+            _addr("own_v", own_v, nown, dt, on, self._ov[1]), _addr("own_len", own_len, nq[:1], i32_, on),
+            _addr("out", out, nq, dt, on, self._out[1]), _addr("lse", lse, nq[:3], f32_, on),
+            _launch_stream(stream, on, q)))
 
 
 def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_group=0, eps=1e-6, stream=None):
@@ -576,29 +590,31 @@ def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_
     [rows][1] (scale_group 0) or [rows][ceil(cols / 128)] (scale_group 128).
 
     Rows may be those of a wider matrix, 16-byte aligned at the first; rows broadcast by expand() are refused."""
-    shape, dt, out_dt = x.shape, x.dtype, y.dtype
+    shape, dt, out_dt, on = x.shape, x.dtype, y.dtype, x.get_device()
+    if on < 0 or on != _current_device():  # where kernels are launched
+        raise MafatError(EINVAL, "x is on %s, which is not the current GPU" % x.device)
     # The common call, all packed: checked in one expression (a look at an attribute takes 50 ns, a call
     # of _addr 300).
-    if (x.is_contiguous() and x.is_cuda and y.shape == shape and y.is_contiguous() and y.is_cuda
-            and weight.dtype is dt and weight.is_contiguous() and weight.is_cuda
+    if (x.is_contiguous() and y.shape == shape and y.is_contiguous() and y.get_device() == on
+            and weight.dtype is dt and weight.is_contiguous() and weight.get_device() == on
             and (residual is None or (residual.dtype is dt and residual.shape == shape and residual.is_contiguous()
-                                      and residual.is_cuda))
+                                      and residual.get_device() == on))
             and (residual_out is None or (residual_out.dtype is dt and residual_out.shape == shape
-                                          and residual_out.is_contiguous() and residual_out.is_cuda))):
-        desc, f32_, scales_shape = _norm_call(shape, dt, out_dt, scale_group, eps, None)
-        if weight.shape == shape[1:]:
+                                          and residual_out.is_contiguous() and residual_out.get_device() == on))):
+        desc, f32_, scales_shape, weight_shape = _norm_call(shape, dt, out_dt, scale_group, eps, None)
+        if weight.shape == weight_shape:
             _check(lib.mafat_rms_norm(
                 desc, x.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
                 None if residual_out is None else residual_out.data_ptr(), y.data_ptr(),
-                _addr("scales", scales, scales_shape, f32_), _launch_stream(stream, x)))
+                _addr("scales", scales, scales_shape, f32_, on), _launch_stream(stream, on, x)))
             return
     strides = tuple(_row_stride(*t) for t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y)))
-    desc, f32_, scales_shape = _norm_call(shape, dt, out_dt, scale_group, eps, strides)
+    desc, f32_, scales_shape, weight_shape = _norm_call(shape, dt, out_dt, scale_group, eps, strides)
     sx, sr, so, sy = [(st, 1) for st in strides]
     _check(lib.mafat_rms_norm(
-        desc, _addr("x", x, shape, dt, sx), _addr("residual", residual, shape, dt, sr),
-        _addr("weight", weight, shape[1:], dt), _addr("residual_out", residual_out, shape, dt, so),
-        _addr("y", y, shape, out_dt, sy), _addr("scales", scales, scales_shape, f32_), _launch_stream(stream, x)))
+        desc, _addr("x", x, shape, dt, on, sx), _addr("residual", residual, shape, dt, on, sr),
+        _addr("weight", weight, weight_shape, dt, on), _addr("residual_out", residual_out, shape, dt, on, so),
+        _addr("y", y, shape, out_dt, on, sy), _addr("scales", scales, scales_shape, f32_, on), _launch_stream(stream, on, x)))
 
 
 def _row_stride(name, t):
@@ -623,7 +639,7 @@ def _norm_call(shape, dt, out_dt, scale_group, eps, strides):
     d.dtype, d.out_dtype = (c if isinstance(c, int) else -1 for c in (code.get(dt), code.get(out_dt)))
     if strides is not None:
         d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride = strides
-    return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1)
+    return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1), (cols,)
 
 
 def diag_umma(a_dev, b_dev, d_dev, n, a_in_tmem=False, stream=None):
