@@ -85,6 +85,8 @@ mafat_status cuda_fail(cudaError_t e, const char* what) {
 
 constexpr int kStatusBytes = 256;
 constexpr int64_t kMaxI32 = std::numeric_limits<int32_t>::max();
+// rows and keys: a tile past the last still has a number in 32 bits
+constexpr int64_t kMostCounted = kMaxI32 - 65536;
 constexpr int kMaxDim = 128;
 
 bool aligned(const void* p, uintptr_t n = 16) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -163,7 +165,7 @@ mafat_status check_common(const Common& c) {
     if (!(c.scale >= 0.f) || std::isinf(c.scale)) return fail(MAFAT_EINVAL, "scale must be positive, or 0 for 1/sqrt(head_dim)");
     if (c.kernel < MAFAT_ATTN_AUTO || c.kernel > MAFAT_ATTN_TILES) return fail(MAFAT_EINVAL, "unknown kernel");
     if (c.splits < 0 || c.splits > MAFAT_ATTN_MAX_SPLITS) return fail(MAFAT_EINVAL, "splits out of range");
-    if ((int64_t)c.batch * c.n_q > kMaxI32 / c.heads_q) return fail(MAFAT_EUNSUPPORTED, "too many rows");
+    if ((int64_t)c.batch * c.n_q > kMostCounted / c.heads_q) return fail(MAFAT_EUNSUPPORTED, "too many rows");
     return MAFAT_OK;
 }
 
@@ -237,7 +239,7 @@ int64_t row_tiles(const AttnShape& sh, int32_t rows) { return (rows + sh.rows - 
 
 // The work of a segment: the kernel, tiles of rows, parts of the keys.
 mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms, bool second) {
-    if (g.n > kMaxI32 - 65536) return fail(MAFAT_EUNSUPPORTED, "too many keys");
+    if (g.n > kMostCounted) return fail(MAFAT_EUNSUPPORTED, "too many keys");
     g.rows = g.reqs * p.n_q * (p.heads_q / p.heads_kv);
     const bool bf16 = p.dtype == MAFAT_BF16;
     AttnKernel kernels[3];
