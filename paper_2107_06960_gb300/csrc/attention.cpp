@@ -105,24 +105,22 @@ bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
 
 // Strides given by the caller (all 0: packed), in elements.  They have to keep every 16-byte
 // vector of channels aligned, and what they span with the sizes inside 62 bits of bytes, so that no offset passes 64.
+// Where there is nothing to step to (one element of a dimension, or none at all) any stride is taken, and a valid one kept.
 mafat_status take_strides(const char* what, const int64_t given[3], const int64_t n[3], int64_t dim, int64_t esz,
                           int64_t out[3]) {
     const int64_t most = ((int64_t)1 << 40) / esz;
-    const bool packed = given[0] == 0 && given[1] == 0 && given[2] == 0;
+    const bool packed = given[0] == 0 && given[1] == 0 && given[2] == 0, empty = n[0] == 0 || n[1] == 0 || n[2] == 0;
     __int128 span = dim, next = dim;  // of the packed: the stride of a dimension by those inside it
     for (int i = 2; i >= 0; --i) {
+        out[i] = dim;
+        if (n[i] <= 1 || empty) continue;
         const __int128 st = packed ? next : (__int128)given[i];
-        if (!packed && n[i] > 1 && st < dim)
-            return fail(MAFAT_EINVAL, "%s: a stride is smaller than a head's channels", what);
-        if (!packed && (st < 0 || st * esz % 16 != 0))
-            return fail(MAFAT_EINVAL, "%s: strides must be multiples of 16 bytes", what);
-        if ((!packed || n[i] > 1) && st >= most)
-            return fail(MAFAT_EUNSUPPORTED, "%s: strides must be below 2^40 bytes", what);
-        out[i] = n[i] > 1 ? (int64_t)st : dim;  // else never used: any valid one
-        if (n[i] > 1) {
-            span += (__int128)(n[i] - 1) * out[i];
-            next *= n[i];
-        }
+        if (st < dim) return fail(MAFAT_EINVAL, "%s: a stride is smaller than a head's channels", what);
+        if (st * esz % 16 != 0) return fail(MAFAT_EINVAL, "%s: strides must be multiples of 16 bytes", what);
+        if (st >= most) return fail(MAFAT_EUNSUPPORTED, "%s: strides must be below 2^40 bytes", what);
+        out[i] = (int64_t)st;
+        span += (n[i] - 1) * st;
+        next *= n[i];
     }
     if (span * esz > (__int128)1 << 62) return fail(MAFAT_EUNSUPPORTED, "%s: the tensor spans more than 2^62 bytes", what);
     return MAFAT_OK;
