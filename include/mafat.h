@@ -446,7 +446,8 @@ typedef struct {
 /* Attention of prefixes * requests requests, of which each `requests` neighbours share a prefix
  * (a frame's states): a request's keys are its prefix's and then its own n_own, of which the last n_q
  * readable ones belong to its n_q queries: token t reads the prefix and its own keys
- * 0 .. own_len - n_q + t.  The prefix's keys are read once for all requests.  A value that is not
+ * 0 .. own_len - n_q + t.  Tiles of rows hold several requests of a prefix, which read its keys once; where one launch reads
+ * both sets (whole_ctas of the statistics) each request's tiles read the prefix's.  A value that is not
  * finite among a request's last n_q readable own keys may reach all its n_q queries. */
 typedef struct {
     int32_t struct_size;        /* sizeof(mafat_prefix_desc) */
@@ -487,11 +488,12 @@ mafat_status mafat_prefix_run(const mafat_attn_t* plan, const void* q, const voi
 /* What a plan chose, by set of keys.  struct_size must be set.  Host only; works on dry runs. */
 typedef struct {
     int32_t struct_size;
-    int32_t kernel[2], splits[2], ctas[2];  /* 0 for a set without room for keys */
+    /* 0 for a set without room for keys; without room in any, the first has a launch that writes the empty rows' results */
+    int32_t kernel[2], splits[2], ctas[2];
     int32_t parts;              /* of a row that go through the workspace to be joined; 1: none do */
     int32_t launches_per_run;
     /* not 0: a run without a prefix mask is one launch instead, of so many CTAs of MAFAT_ATTN_TILES that read both
-     * sets for rows of one request each and keep no parts */
+     * sets for rows of one request each and keep no parts; the other fields, the workspace among them, are those of a run with one */
     int32_t whole_ctas;
     int64_t workspace_bytes;
 } mafat_attn_stats_t;
@@ -508,7 +510,7 @@ void mafat_attn_destroy(mafat_attn_t* plan);
 
 /* Root-mean-square norm of rows with the residual's addition:
  *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * weight,
- * computed in fp32 and rounded once.  With out_dtype MAFAT_E4M3, y holds the norm divided by a
+ * computed in fp32 and rounded once (y is 0 where the sum of squares passes fp32's range).  With out_dtype MAFAT_E4M3, y holds the norm divided by a
  * scale s and rounded to 8 bits, s = max |norm| / 448 over scale_group channels (1 where that is 0 in fp32):
  * y * s stands for the norm. */
 typedef struct {

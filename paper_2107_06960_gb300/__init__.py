@@ -548,8 +548,8 @@ class CrossAttention(_Attention):
 
 class PrefixAttention(_Attention):
     """mafat_prefix_plan / mafat_prefix_run: attention of prefixes * requests requests, of which each
-    `requests` neighbours share a prefix (a frame's states) that is read once for all of them; behind it
-    a request has up to n_own keys of its own, the last n_q of them those of its n_q queries."""
+    `requests` neighbours share a prefix (a frame's states); behind it a request has up to n_own keys of its own,
+    the last n_q of them those of its n_q queries.  The prefix is read once for the requests that share a tile of rows."""
 
     def __init__(self, prefixes, requests, n_q, n_prefix, n_own, heads_q, heads_kv, head_dim, dtype=BF16, scale=0.0,
                  q_strides=None, prefix_k_strides=None, prefix_v_strides=None, own_k_strides=None,

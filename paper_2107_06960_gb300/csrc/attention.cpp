@@ -168,11 +168,15 @@ mafat_status check_common(const Common& c) {
 }
 
 // Each kernel where it is the quickest; in us, with as many parts as are best for each:
-//   bf16, 64 sequences of 1444 keys, one key head of 128 channels   16 rows: kRows 11.8, kTc1 17.8; 32 rows: 21.3, 18.1
-//   bf16, 152 sequences of 256 rows, one head   64 channels, 128 keys: kTc1 5.5, kTc2 5.8; 2048 keys: 23.9, 20.8;
-//                                               128 channels, 128 keys: 7.7, 7.5; 2048 keys: 37.2, 34.7
-//   fp32, 64 sequences of 1444 keys, 8 key heads of 128 channels    4 rows: kSimt4 133, kSimt8 173, kSimt64 576;
-//                                               8 rows: 228, 174, 576; 16 rows: 451, 312, 580; 32 rows: 873, 619, 586
+//   bf16, 64 sequences of 1444 keys, one key head of 128 channels   16 rows: kRows 10.5, kTc1 15.7; 32 rows: 18.7, 16.0
+//   bf16, 152 sequences of 256 rows, one head   64 channels, 128 keys: kTc1 4.9, kTc2 5.2; 2048 keys: 23.7, 19.9;
+//                                               128 channels, 128 keys: 7.0, 6.8; 2048 keys: 37.3, 35.4
+//   fp32, 64 sequences of 1444 keys, 8 key heads of 128 channels    4 rows: kSimt4 130, kSimt8 172, kSimt64 573;
+//                                               8 rows: 224, 173, 573; 16 rows: 442, 314, 577; 32 rows: 856, 622, 583
+// The terms are those of earlier forms of the kernels.  146 drawn plans (1 to 64 sequences, 30 to 6000 keys, 1 to 1024
+// tokens) take, as shares of the model's time, quartiles and ends: kTc1 0.95 0.98 1.05 (0.89 to 1.12), kTc2 0.92 0.97 1.04
+// (0.90 to 1.13), kRows 0.83 0.93 1.00 (0.70 to 1.30), kSimt64 0.92 0.97 1.09 (0.88 to 1.77: a last wave of few CTAs, which
+// the model takes for one an SM), kSimt4 and kSimt8 0.78 to 0.87, 0.82 to 0.93, 0.99 (0.70 to 1.24).
 AttnShape shape_of(AttnKernel k, int dim) {
     const bool wide = dim > 64;
     const int simt = mafat_attn_simt_keys(), rows = mafat_attn_rows_keys();
@@ -228,9 +232,12 @@ Choice choose_splits(const Model& m) {
     return best;
 }
 
-// Most parts that a tile of many rows joins at its end, and that a cluster has.
+// Most parts that a tile of many rows joins at its end, and that a cluster has.  2 x 8 requests of 40 tokens about 3000
+// states, 100 own keys, 16 query and 4 key heads, in us: three parts joined by the own keys' tiles 22.5 (64 channels) and
+// 32.5 (128), by a launch 24.6 and 33.6.
 constexpr int kTileJoin = 16, kMostCluster = 8;
-// What a cluster's join takes, and the joining of another launch's parts is worth.
+// What a cluster's join takes (one token over 1444 states in clusters of 8: 4.9 us, the same work without a join 4.4), and
+// the joining of another launch's parts is worth (above: 1.1 to 2.1 us).
 constexpr double kClusterJoinUs = 0.7, kOwnJoinUs = 1.0;
 
 int64_t row_tiles(const AttnShape& sh, int32_t rows) { return (rows + sh.rows - 1) / sh.rows; }

@@ -14,7 +14,8 @@
 // after another (cp.async): keys that are not readable cost no product.
 //
 // O is rescaled only where b' is more than 8 above the b in use (a power that cancels in O / l and
-// leaves P at most 256, well inside bf16), so that few tiles touch O outside the products.
+// leaves P at most 256, well inside bf16), so that few tiles touch O outside the products.  That, and weights in the
+// scores' place in tensor memory, are published methods of attention on this hardware.
 //
 // Rows whose keys are a shared prefix and then their own are done in one launch where that is better (attention.cpp has
 // the rule): the tiles of the prefix come first, each set with its own maps, length and partial last tile.
