@@ -485,6 +485,21 @@ mafat_status mafat_prefix_run(const mafat_attn_t* plan, const void* q, const voi
                               const int32_t* prefix_len, const uint8_t* prefix_mask, const void* own_k,
                               const void* own_v, const int32_t* own_len, void* out, float* lse, void* stream);
 
+/* Attention of drafted tokens, a tree for each request: as mafat_prefix_plan, but what token t of a request (a node of its
+ * tree) reads of the request's own keys are all before the tree's and those of the nodes that its bits name: the nodes on
+ * its way from the tree's root, t itself among them.  The last nodes[b] readable own keys are the tree's, node j's the j-th of
+ * them.  The descriptor is mafat_prefix_desc, with n_q nodes at most; plans of this kind are run by mafat_tree_run alone.
+ *   tree     : [batch][n_q][ceil(n_q / 32)] words, bit j % 32 of word j / 32 of row t: t reads node j; bits of nodes that the
+ *              request does not have are not looked at.  tree_shared not 0: [1][n_q][...], one for all requests
+ *   nodes    : [batch] nodes of each tree, clamped to 0 .. n_q (NULL: n_q); later rows get out = 0 and lse = -inf
+ * The rest is as in mafat_prefix_run; a causal chain is the tree whose row t has its first t + 1 bits set.  A value that
+ * is not finite among the keys of a request's nodes may reach all its queries. */
+mafat_status mafat_tree_plan(const mafat_prefix_desc* desc, mafat_attn_t** out);
+mafat_status mafat_tree_run(const mafat_attn_t* plan, const void* q, const void* prefix_k, const void* prefix_v,
+                            const int32_t* prefix_len, const uint8_t* prefix_mask, const void* own_k, const void* own_v,
+                            const int32_t* own_len, const int32_t* nodes, const uint32_t* tree, int32_t tree_shared,
+                            void* out, float* lse, void* stream);
+
 /* What a plan chose, by set of keys.  struct_size must be set.  Host only; works on dry runs. */
 typedef struct {
     int32_t struct_size;
@@ -530,6 +545,128 @@ typedef struct {
  * residual_out, and y of x's type, may be x or residual itself (same address and row stride); other overlaps are refused. */
 mafat_status mafat_rms_norm(const mafat_norm_desc* desc, const void* x, const void* residual, const void* weight,
                             void* residual_out, void* y, float* scales, void* stream);
+
+/* The norms around a block (an attention, a product) with its gate and the residual's scale:
+ *   n = x / sqrt(mean(x^2) + eps) * post_weight       (n = x without post_weight)
+ *   h = residual_scale * residual + branch_scale * gate * n
+ *   y = h / sqrt(mean(h^2) + eps) * weight
+ * computed in fp32 and rounded once each (y of the unrounded h); a norm is 0 where its sum of squares passes fp32's range.
+ * With out_dtype MAFAT_E4M3, y is in 8 bits with scales as in mafat_rms_norm. */
+typedef struct {
+    int32_t struct_size;        /* sizeof(mafat_block_norm_desc) */
+    int32_t dtype;              /* of x, residual, the weights, gate, residual_out: MAFAT_BF16 or MAFAT_FP32 */
+    int32_t out_dtype;          /* of y: dtype or MAFAT_E4M3 */
+    int32_t cols;               /* at most 16384 */
+    int64_t rows;               /* 0: nothing is done */
+    int64_t gate_rows;          /* neighbours that share a row of gate, a divisor of rows (0: all rows share one) */
+    int32_t scale_group;        /* MAFAT_E4M3: 0 (one scale a row) or 128 (one for each 128 channels) */
+    float eps;
+    float branch_scale, residual_scale;  /* finite */
+    int64_t x_stride, residual_stride, residual_out_stride, y_stride, gate_stride;  /* of rows, in elements (0: cols) */
+} mafat_block_norm_desc;
+
+/* Runs the norms on `stream` (asynchronous, one launch, no workspace, capturable).  All pointers are device memory of the
+ * current device, 16-byte aligned (scales: 4-byte).  post_weight, gate [rows / gate_rows][cols] and residual_out (h) may be NULL;
+ * weight and y are both given or both NULL (h alone is wanted).  residual_out, and y of x's type, may be x or residual itself
+ * (same address and row stride); other overlaps are refused. */
+mafat_status mafat_block_norm(const mafat_block_norm_desc* desc, const void* x, const void* residual, const void* post_weight,
+                              const void* gate, const void* weight, void* residual_out, void* y, float* scales, void* stream);
+
+/* Rotary positions: pair i of a head's first rot_dim channels is turned by angle = position * frequency[i],
+ *   (a, b) -> magnitude * (a cos - b sin, a sin + b cos),
+ * pairs being channels (i, i + rot_dim / 2), or neighbours (2i, 2i + 1) where interleaved; the other channels stay.
+ * frequency[i] = base^(-2i / rot_dim) radians a position, scaled for texts longer than the first ones:
+ *   LINEAR : divided by factor
+ *   BASE   : of the base times factor^(rot_dim / (rot_dim - 2)), which divides the lowest frequency by factor
+ *   BLEND  : of a pair that turns w times within first_positions, divided by factor where w <= slow, kept where w >= fast,
+ *            in between the two weighted by (w - slow) / (fast - slow); magnitude is 0.1 ln(factor) + 1 unless given
+ *            (Peng et al., "YaRN", 2023)
+ * or any that the caller gives.  Frequencies are kept as 64-bit fractions of a turn, so that the angle, past whole turns, is as
+ * good at far positions as at near ones.  The rest is fp32, rounded once. */
+typedef enum { MAFAT_ROTARY_PLAIN = 0, MAFAT_ROTARY_LINEAR = 1, MAFAT_ROTARY_BASE = 2, MAFAT_ROTARY_BLEND = 3 } mafat_rotary_scaling;
+
+/* Zero-initialise and set struct_size. */
+typedef struct {
+    int32_t struct_size;        /* sizeof(mafat_rotary_desc) */
+    int32_t dtype;              /* MAFAT_BF16 or MAFAT_FP32 */
+    int32_t head_dim;           /* a multiple of 8, at most 256 */
+    int32_t rot_dim;            /* even, at most head_dim (0: head_dim) */
+    int32_t interleaved;        /* 1: neighbours are pairs */
+    int32_t scaling;            /* mafat_rotary_scaling */
+    double base;                /* above 1 (0: 10000) */
+    double factor;              /* at least 1 (0: 1) */
+    double first_positions;     /* BLEND: the positions that the frequencies were made for */
+    double fast, slow;          /* BLEND: 0 < slow < fast (both 0: 32 and 1) */
+    double magnitude;           /* positive (0: 1, or BLEND's) */
+    const double* frequencies;  /* [rot_dim / 2] host, at most 65536, instead of base and scaling (NULL: none) */
+    int32_t dry_run;            /* 1: checks only; needs no GPU */
+} mafat_rotary_desc;
+
+typedef struct mafat_rotary_s mafat_rotary_t;
+
+/* Makes the table of frequencies on the current device.  Not for use during stream capture. */
+mafat_status mafat_rotary_plan(const mafat_rotary_desc* desc, mafat_rotary_t** out);
+
+/* One call's sizes and strides ({sequence, token, head} in elements, the rules of the attention plans). */
+typedef struct {
+    int32_t struct_size;        /* sizeof(mafat_rotary_call) */
+    int32_t batch, n_q;         /* 0: nothing is done */
+    int32_t heads_q, heads_kv;
+    int32_t room;               /* places of a sequence in k_out and v_out */
+    int64_t q_strides[3], q_out_strides[3], k_strides[3], v_strides[3], k_out_strides[3], v_out_strides[3];
+} mafat_rotary_call;
+
+/* Rotates queries, and rotates keys into their places of the cache with their values, on `stream` (asynchronous, one
+ * launch, no workspace, capturable; calls of one plan may overlap in time).  Device memory of the plan's device, which
+ * has to be the current one; q with q_out, k with k_out, v with v_out are given or NULL.
+ *   positions : [batch][n_q]
+ *   places    : [batch][n_q] place of each token in k_out and v_out; outside 0 .. room - 1: the token's key and value are
+ *               not written.  Two tokens of a sequence with one place leave it with channels of either.  NULL: token t's
+ *               is t, and room is n_q
+ *   q, q_out  : [batch][n_q][heads_q][head_dim];  k, v : [batch][n_q][heads_kv][head_dim]
+ *   k_out, v_out : [batch][room][heads_kv][head_dim]
+ * q_out may be q, and without places k_out k and v_out v (same strides); tensors side by side in one matrix are taken as
+ * such; other overlaps with an output are refused. */
+mafat_status mafat_rotary_run(const mafat_rotary_t* plan, const mafat_rotary_call* call, const int32_t* positions,
+                              const int32_t* places, const void* q, void* q_out, const void* k, void* k_out, const void* v,
+                              void* v_out, void* stream);
+/* The plan's frequencies [rot_dim / 2], radians a position, and its magnitude, to host memory (either may be NULL).
+ * Host only; works on dry runs. */
+mafat_status mafat_rotary_frequencies(const mafat_rotary_t* plan, double* frequencies, double* magnitude);
+void mafat_rotary_destroy(mafat_rotary_t* plan);
+
+/* What requests ask of their next token: for row (b, t) of logits, t one of n_q tokens of request b, in fp32,
+ *   x = logit;  where the token has been said:  x = x / repetition (x > 0) or x * repetition
+ *   x = x - frequency * n - presence * [n > 0]    n: how often the answer has it
+ *   x = x + bias;  x = -inf where the grammar's mask does not allow the token
+ * rounded once.  Said are the request's first lengths[b] tokens and, for row t, the drafted tokens that its bits of `tree`
+ * name; the answer is what comes after the first prompt_lengths[b].  Ids outside 0 .. vocab - 1 count for nothing. */
+typedef struct {
+    int32_t struct_size;        /* sizeof(mafat_logits_desc) */
+    int32_t dtype;              /* of logits: MAFAT_BF16 or MAFAT_FP32 */
+    int32_t out_dtype;          /* of out: dtype or MAFAT_FP32 */
+    int32_t batch, n_q;         /* 0: nothing is done */
+    int32_t vocab;
+    int32_t room;               /* of a request's tokens; with n_q below 2^19 */
+    int32_t n_bias;             /* entries of a request, at most 4095 */
+    int32_t n_masks;
+    int32_t tree_shared, bias_shared;  /* not 0: one tree, one list of biases for all requests */
+    int64_t logits_stride, out_stride; /* of rows, in elements (0: vocab) */
+} mafat_logits_desc;
+
+/* Runs on `stream` (asynchronous, one launch, no workspace, capturable).  Device memory of the current device; logits and
+ * out aligned to their elements, the rest to 4 bytes.  out may be logits itself (same type and row stride); other
+ * overlaps are refused.  All but logits and out may be NULL:
+ *   tokens [batch][room], lengths [batch] (clamped to 0 .. room; NULL: room), prompt_lengths [batch] (clamped; NULL: 0)
+ *   repetition, presence, frequency [batch] (NULL: 1, 0, 0; repetition above 0)
+ *   drafts [batch][n_q] with tree [batch][n_q][ceil(n_q / 32)] words (NULL with drafts: token t has its own and those before it)
+ *   bias_ids, bias [batch][n_bias]; of an id that is there twice the last entry counts; ids below 0: unused places
+ *   masks [n_masks][ceil(vocab / 32)] words, bit i % 32 of word i / 32: token i is allowed; mask_rows [batch][n_q]: each
+ *   row's mask, none where it is outside 0 .. n_masks - 1 (NULL: row b * n_q + t has mask b * n_q + t) */
+mafat_status mafat_adjust_logits(const mafat_logits_desc* desc, const void* logits, const int32_t* tokens, const int32_t* lengths,
+                                 const int32_t* prompt_lengths, const float* repetition, const float* presence,
+                                 const float* frequency, const int32_t* drafts, const uint32_t* tree, const int32_t* bias_ids,
+                                 const float* bias, const uint32_t* masks, const int32_t* mask_rows, void* out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -23,6 +23,7 @@ MAFAT_CONV, MAFAT_MAXPOOL = 0, 1
 BF16, FP32, E4M3 = 0, 1, 2
 ATTN_AUTO, ATTN_ROWS, ATTN_TILES = 0, 1, 2
 MAX_SPLITS = 128  # of an attention plan's keys
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BLEND = range(4)
 STATUS = {0: "OK", 1: "EINVAL", 2: "EUNSUPPORTED", 3: "ENOMEM", 4: "ECUDA", 5: "ETIMEOUT", 6: "ENOFIT",
           7: "EDEVICE"}
 OK, EINVAL, EUNSUPPORTED, ENOMEM, ECUDA, ETIMEOUT, ENOFIT, EDEVICE = range(8)
@@ -90,6 +91,31 @@ class NormDesc(ctypes.Structure):
                 ("residual_out_stride", i64), ("y_stride", i64)]
 
 
+class BlockNormDesc(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("dtype", i32), ("out_dtype", i32), ("cols", i32), ("rows", i64),
+                ("gate_rows", i64), ("scale_group", i32), ("eps", f32), ("branch_scale", f32), ("residual_scale", f32),
+                ("x_stride", i64), ("residual_stride", i64), ("residual_out_stride", i64), ("y_stride", i64),
+                ("gate_stride", i64)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("dtype", i32), ("head_dim", i32), ("rot_dim", i32), ("interleaved", i32),
+                ("scaling", i32), ("base", dbl), ("factor", dbl), ("first_positions", dbl), ("fast", dbl), ("slow", dbl),
+                ("magnitude", dbl), ("frequencies", ctypes.POINTER(dbl)), ("dry_run", i32)]
+
+
+class RotaryCall(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("batch", i32), ("n_q", i32), ("heads_q", i32), ("heads_kv", i32), ("room", i32),
+                ("q_strides", i64 * 3), ("q_out_strides", i64 * 3), ("k_strides", i64 * 3), ("v_strides", i64 * 3),
+                ("k_out_strides", i64 * 3), ("v_out_strides", i64 * 3)]
+
+
+class LogitsDesc(ctypes.Structure):
+    _fields_ = [("struct_size", i32), ("dtype", i32), ("out_dtype", i32), ("batch", i32), ("n_q", i32), ("vocab", i32),
+                ("room", i32), ("n_bias", i32), ("n_masks", i32), ("tree_shared", i32), ("bias_shared", i32),
+                ("logits_stride", i64), ("out_stride", i64)]
+
+
 # (name, restype, argtypes) of every entry point of include/mafat.h
 _SIGNATURES = [
     ("mafat_describe_net", i32, [vp, i32, i32, i32, i32, ctypes.POINTER(vp)]),
@@ -132,6 +158,14 @@ _SIGNATURES = [
     ("mafat_attn_sync_status", i32, [vp, vp]),
     ("mafat_attn_destroy", None, [vp]),
     ("mafat_rms_norm", i32, [ctypes.POINTER(NormDesc)] + [vp] * 7),
+    ("mafat_tree_plan", i32, [ctypes.POINTER(PrefixDesc), ctypes.POINTER(vp)]),
+    ("mafat_tree_run", i32, [vp] * 11 + [i32] + [vp] * 3),
+    ("mafat_block_norm", i32, [ctypes.POINTER(BlockNormDesc)] + [vp] * 9),
+    ("mafat_rotary_plan", i32, [ctypes.POINTER(RotaryDesc), ctypes.POINTER(vp)]),
+    ("mafat_rotary_run", i32, [vp, ctypes.POINTER(RotaryCall)] + [vp] * 9),
+    ("mafat_rotary_frequencies", i32, [vp, ctypes.POINTER(dbl), ctypes.POINTER(dbl)]),
+    ("mafat_rotary_destroy", None, [vp]),
+    ("mafat_adjust_logits", i32, [ctypes.POINTER(LogitsDesc)] + [vp] * 15),
 ]
 EXPORTED = [s[0] for s in _SIGNATURES]
 
@@ -550,6 +584,7 @@ class PrefixAttention(_Attention):
     """mafat_prefix_plan / mafat_prefix_run: attention of prefixes * requests requests, of which each
     `requests` neighbours share a prefix (a frame's states); behind it a request has up to n_own keys of its own,
     the last n_q of them those of its n_q queries.  The prefix is read once for the requests that share a tile of rows."""
+    _plan = "mafat_prefix_plan"
 
     def __init__(self, prefixes, requests, n_q, n_prefix, n_own, heads_q, heads_kv, head_dim, dtype=BF16, scale=0.0,
                  q_strides=None, prefix_k_strides=None, prefix_v_strides=None, own_k_strides=None,
@@ -557,7 +592,7 @@ class PrefixAttention(_Attention):
         d = PrefixDesc(dtype=dtype, prefixes=prefixes, requests=requests, n_q=n_q, n_prefix=n_prefix, n_own=n_own,
                        heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim, scale=scale or 0.0, kernel=kernel,
                        splits=splits, dry_run=int(dry_run))
-        self._make(d, lib.mafat_prefix_plan, q_strides=q_strides, prefix_k_strides=prefix_k_strides,
+        self._make(d, getattr(lib, self._plan), q_strides=q_strides, prefix_k_strides=prefix_k_strides,
                    prefix_v_strides=prefix_v_strides, own_k_strides=own_k_strides, own_v_strides=own_v_strides,
                    out_strides=out_strides)
         n = prefixes * requests
@@ -580,6 +615,32 @@ class PrefixAttention(_Attention):
             _addr("prefix_v", prefix_v, npre, dt, on, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], i32_, on),
             _addr("prefix_mask", prefix_mask, npre[:2], mask, on), _addr("own_k", own_k, nown, dt, on, sok),
             _addr("own_v", own_v, nown, dt, on, self._ov[1]), _addr("own_len", own_len, nq[:1], i32_, on),
+            _addr("out", out, nq, dt, on, self._out[1]), _addr("lse", lse, nq[:3], f32_, on),
+            _launch_stream(stream, on, q)))
+
+
+class TreeAttention(PrefixAttention):
+    """mafat_tree_plan / mafat_tree_run: attention of drafted tokens, a tree of up to n_q nodes for each request, to the prefix
+    that neighbours share and to the request's own keys: all before the tree's, and of the tree's those that a
+    node's bits name.  Made as PrefixAttention is."""
+    _plan = "mafat_tree_plan"
+
+    def run(self, q, prefix_k, prefix_v, own_k, own_v, tree, out, nodes=None, prefix_len=None, prefix_mask=None,
+            own_len=None, lse=None, stream=None):
+        """tree [prefixes * requests][n_q][ceil(n_q / 32)] int32 words (or [1][n_q][...], one for all): bit j % 32 of word
+        j / 32 of row t says that token t reads node j; nodes [prefixes * requests] int32, of each tree (None: n_q): its keys
+        are the last of the own_len readable ones, and rows past them get 0.  The rest as in PrefixAttention."""
+        dt, i32_, mask, f32_ = self._types or self._torch()
+        (nq, sq), (npre, spk), (nown, sok) = self._q, self._pk, self._ok
+        on, n_q = self.device, nq[1]
+        shared = getattr(tree, "shape", nq)[0] == 1
+        _check(lib.mafat_tree_run(
+            self.handle, _addr("q", q, nq, dt, on, sq), _addr("prefix_k", prefix_k, npre, dt, on, spk),
+            _addr("prefix_v", prefix_v, npre, dt, on, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], i32_, on),
+            _addr("prefix_mask", prefix_mask, npre[:2], mask, on), _addr("own_k", own_k, nown, dt, on, sok),
+            _addr("own_v", own_v, nown, dt, on, self._ov[1]), _addr("own_len", own_len, nq[:1], i32_, on),
+            _addr("nodes", nodes, nq[:1], i32_, on),
+            _addr("tree", tree, (1 if shared else nq[0], n_q, (n_q + 31) // 32), i32_, on), int(shared),
             _addr("out", out, nq, dt, on, self._out[1]), _addr("lse", lse, nq[:3], f32_, on),
             _launch_stream(stream, on, q)))
 
@@ -640,6 +701,196 @@ def _norm_call(shape, dt, out_dt, scale_group, eps, strides):
     if strides is not None:
         d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride = strides
     return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1), (cols,)
+
+
+def block_norm(x, residual, residual_out=None, post_weight=None, gate=None, branch_scale=1.0, residual_scale=1.0,
+               weight=None, y=None, scales=None, scale_group=0, eps=1e-6, stream=None):
+    """mafat_block_norm on [rows][cols] tensors, the norms around a block whose result is x:
+    n = x / sqrt(mean(x^2) + eps) * post_weight (x without it), h = residual_scale * residual + branch_scale * gate * n
+    (written to residual_out if given), y = h / sqrt(mean(h^2) + eps) * weight, in x's type or, with scales and
+    scale_group as of rms_norm, in float8_e4m3fn.
+
+    gate [cols], or [n][cols] of which each row is for rows / n neighbours.  Rows as of rms_norm."""
+    shape, dt, on = x.shape, x.dtype, x.get_device()
+    if on < 0 or on != _current_device():  # where kernels are launched
+        raise MafatError(EINVAL, "x is on %s, which is not the current GPU" % x.device)
+    gate2 = gate if gate is None or gate.dim() != 1 else gate[None]
+    rows = tuple(_row_stride(*t) for t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y), ("gate", gate2)))
+    desc, f32_, scales_shape, weight_shape, gate_shape = _block_norm_call(
+        shape, dt, None if y is None else y.dtype, None if gate is None else gate2.shape[0], scale_group, eps, branch_scale,
+        residual_scale, rows)
+    sx, sr, so, sy, sg = [(st, 1) for st in rows]
+    _check(lib.mafat_block_norm(
+        desc, _addr("x", x, shape, dt, on, sx), _addr("residual", residual, shape, dt, on, sr),
+        _addr("post_weight", post_weight, weight_shape, dt, on), _addr("gate", gate2, gate_shape, dt, on, sg),
+        _addr("weight", weight, weight_shape, dt, on), _addr("residual_out", residual_out, shape, dt, on, so),
+        _addr("y", y, shape, None if y is None else y.dtype, on, sy), _addr("scales", scales, scales_shape, f32_, on),
+        _launch_stream(stream, on, x)))
+
+
+@functools.lru_cache(maxsize=256)
+def _block_norm_call(shape, dt, out_dt, gates, scale_group, eps, branch_scale, residual_scale, strides):
+    """As _norm_call."""
+    if len(shape) != 2:
+        raise MafatError(EINVAL, "x: [rows][cols] expected")
+    _type(BF16)
+    code = {v: k for k, v in _TYPES.items()}
+    rows, cols = shape
+    if gates is not None and (gates < 1 or rows % gates):
+        raise MafatError(EINVAL, "gate: its rows must divide x's")
+    d = BlockNormDesc(struct_size=ctypes.sizeof(BlockNormDesc), cols=cols, rows=rows, gate_rows=rows // gates if gates else 0,
+                      scale_group=scale_group, eps=eps, branch_scale=branch_scale, residual_scale=residual_scale)
+    d.dtype, d.out_dtype = (c if isinstance(c, int) else -1 for c in (code.get(dt), code.get(dt if out_dt is None else out_dt)))
+    d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride, d.gate_stride = strides
+    return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1), (cols,), (gates or 1, cols)
+
+
+class Rotary:
+    """mafat_rotary_plan / mafat_rotary_run: rotary positions of queries and keys, whose first rot_dim channels of a head
+    are turned in pairs (i, i + rot_dim / 2), or of neighbours where interleaved, by position * frequency.
+
+    scaling: ROTARY_PLAIN, ROTARY_LINEAR (frequencies divided by factor), ROTARY_BASE (of a larger base) or ROTARY_BLEND
+    (by how often a pair turns within first_positions); or the frequencies themselves, [rot_dim / 2] radians a position."""
+
+    def __init__(self, head_dim, rot_dim=0, dtype=BF16, interleaved=False, base=0.0, scaling=ROTARY_PLAIN, factor=1.0,
+                 first_positions=0, fast=0.0, slow=0.0, magnitude=0.0, frequencies=None, dry_run=False):
+        d = RotaryDesc(struct_size=ctypes.sizeof(RotaryDesc), dtype=dtype, head_dim=head_dim, rot_dim=rot_dim,
+                       interleaved=int(interleaved), scaling=scaling, base=base, factor=factor,
+                       first_positions=first_positions, fast=fast, slow=slow, magnitude=magnitude, dry_run=int(dry_run))
+        self.pairs = (rot_dim or head_dim) // 2
+        if frequencies is not None:
+            frequencies = [float(f) for f in frequencies]
+            if len(frequencies) != self.pairs:
+                raise MafatError(EINVAL, "frequencies: one for each of %d pairs expected" % self.pairs)
+            d.frequencies = (dbl * max(1, self.pairs))(*frequencies)
+        h = vp()
+        _check(lib.mafat_rotary_plan(ctypes.byref(d), ctypes.byref(h)))
+        self.handle, self.head_dim, self.dtype = h, head_dim, dtype
+        self.device = None if dry_run else _current_device()
+        self._torch = None
+
+    def frequencies(self):
+        """(radians a position of each pair, the rotated channels' factor)."""
+        f, m = (dbl * self.pairs)(), dbl()
+        _check(lib.mafat_rotary_frequencies(self.handle, f, ctypes.byref(m)))
+        return list(f), m.value
+
+    def run(self, positions, q=None, q_out=None, k=None, k_out=None, v=None, v_out=None, places=None, stream=None):
+        """positions [batch][n_q] int32; q, q_out [batch][n_q][heads_q][head_dim]; k, v [batch][n_q][heads_kv][head_dim]
+        to places [batch][n_q] int32 of k_out, v_out [batch][room][heads_kv][head_dim] (outside them: not written; None:
+        token t's is t).  Any strides that are multiples of 16 bytes; q_out may be q, and without places k_out k, v_out v."""
+        dt, i32_ = self._torch or self._types()
+        on = self.device
+        shape = tuple(positions.shape)
+        laid = tuple(None if t is None else (t.shape, t.stride()) for t in (q, q_out, k, k_out, v, v_out))
+        call, shapes = _rotary_call(shape, self.head_dim, laid)
+        addresses = [None if t is None else _addr(name, t, s, dt, on, t.stride()) for name, t, s in
+                     zip(("q", "q_out", "k", "k_out", "v", "v_out"), (q, q_out, k, k_out, v, v_out), shapes)]
+        _check(lib.mafat_rotary_run(self.handle, call, _addr("positions", positions, shape, i32_, on),
+                                    _addr("places", places, shape, i32_, on), *addresses, _launch_stream(stream, on, positions)))
+
+    def _types(self):
+        self._torch = _type(self.dtype), _type("int32")
+        return self._torch
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib.mafat_rotary_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+@functools.lru_cache(maxsize=256)
+def _rotary_call(positions, dim, laid):
+    """The call's sizes by its tensors' (shape, strides), and the shapes that they have to have."""
+    if len(positions) != 2:
+        raise MafatError(EINVAL, "positions: [batch][n_q] expected")
+    names = ("q", "q_out", "k", "k_out", "v", "v_out")
+    for name, x in zip(names, laid):
+        if x is not None and len(x[0]) != 4:
+            raise MafatError(EINVAL, "%s: [batch][tokens][heads][channels] expected" % name)
+    batch, n_q = positions
+    keys = laid[2] or laid[4]
+    cache = laid[3] or laid[5]
+    heads_q, heads_kv = laid[0][0][2] if laid[0] else 1, keys[0][2] if keys else 1
+    room = cache[0][1] if cache else n_q
+    c = RotaryCall(struct_size=ctypes.sizeof(RotaryCall), batch=batch, n_q=n_q, heads_q=heads_q, heads_kv=heads_kv, room=room)
+    for name, x in zip(names, laid):
+        if x is None:
+            continue
+        (*sizes, _), (*steps, inner) = x
+        if inner != 1 or any(n > 1 and s < dim for n, s in zip(sizes, steps)):
+            raise MafatError(EINVAL, "%s: a head's channels must be contiguous, and not shared" % name)
+        getattr(c, name + "_strides")[:] = [s if n > 1 else max(s, dim) for n, s in zip(sizes, steps)]
+    q, k, o = (batch, n_q, heads_q, dim), (batch, n_q, heads_kv, dim), (batch, room, heads_kv, dim)
+    return ctypes.byref(c), (q, q, k, o, k, o)
+
+
+def adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None, repetition=None, presence=None, frequency=None,
+                  drafts=None, tree=None, bias_ids=None, bias=None, masks=None, mask_rows=None, stream=None):
+    """mafat_adjust_logits: penalties for repeated tokens, biases and grammar masks on logits [batch][n_q][vocab] or
+    [batch][vocab]; out alike, of the same type or fp32 (may be logits itself).
+
+    tokens [batch][room] int32, of which each request has said lengths [batch], the first prompt_lengths [batch] as its prompt;
+    repetition, presence, frequency [batch] fp32; drafts [batch][n_q] int32 that row t has said too where bit t of the
+    tree's words says so (tree [batch or 1][n_q][ceil(n_q / 32)] int32; None: its own and those before); bias_ids int32 and
+    bias fp32 [batch or 1][n]; masks [n][ceil(vocab / 32)] int32 words of allowed tokens, mask_rows [batch][n_q] int32 (or
+    [batch]) each row's (outside 0 .. n - 1: none; without mask_rows one for each row)."""
+    on = logits.get_device()
+    if on < 0 or on != _current_device():
+        raise MafatError(EINVAL, "logits are on %s, which is not the current GPU" % logits.device)
+    first = [None if t is None else t.shape for t in (tokens, tree, bias_ids, masks)]
+    desc, f32_, i32_, s = _logits_call(logits.shape, logits.stride(), out.stride(), logits.dtype, out.dtype, *first)
+    rows = s["rows"] if mask_rows is None or mask_rows.dim() == 2 else s["batch"]
+    _check(lib.mafat_adjust_logits(
+        desc, _addr("logits", logits, logits.shape, logits.dtype, on, logits.stride()), _addr("tokens", tokens, s["tokens"], i32_, on),
+        _addr("lengths", lengths, s["batch"], i32_, on), _addr("prompt_lengths", prompt_lengths, s["batch"], i32_, on),
+        _addr("repetition", repetition, s["batch"], f32_, on), _addr("presence", presence, s["batch"], f32_, on),
+        _addr("frequency", frequency, s["batch"], f32_, on), _addr("drafts", drafts, s["rows"], i32_, on),
+        _addr("tree", tree, s["tree"], i32_, on), _addr("bias_ids", bias_ids, s["bias"], i32_, on),
+        _addr("bias", bias, s["bias"], f32_, on), _addr("masks", masks, s["masks"], i32_, on),
+        _addr("mask_rows", mask_rows, rows, i32_, on), _addr("out", out, logits.shape, out.dtype, on, out.stride()),
+        _launch_stream(stream, on, logits)))
+
+
+@functools.lru_cache(maxsize=256)
+def _logits_call(shape, in_strides, out_strides, dt, out_dt, tokens, tree, bias, masks):
+    """As _norm_call: the descriptor, and the shapes that the other tensors have to have."""
+    if len(shape) not in (2, 3):
+        raise MafatError(EINVAL, "logits: [batch][n_q][vocab] or [batch][vocab] expected")
+    for name, x, n in (("tokens", tokens, 2), ("tree", tree, 3), ("bias_ids", bias, 2), ("masks", masks, 2)):
+        if x is not None and len(x) != n:
+            raise MafatError(EINVAL, "%s: %d dimensions expected" % (name, n))
+    _type(BF16)
+    code = {v: k for k, v in _TYPES.items()}
+    batch, n_q, vocab = shape[0], shape[1] if len(shape) == 3 else 1, shape[-1]
+    d = LogitsDesc(struct_size=ctypes.sizeof(LogitsDesc), batch=batch, n_q=n_q, vocab=vocab, room=tokens[1] if tokens else 0,
+                   n_bias=bias[1] if bias else 0, n_masks=masks[0] if masks else 0,
+                   tree_shared=int(tree is not None and tree[0] == 1), bias_shared=int(bias is not None and bias[0] == 1))
+    d.dtype, d.out_dtype = (c if isinstance(c, int) else -1 for c in (code.get(dt), code.get(out_dt)))
+    d.logits_stride, d.out_stride = (_logits_stride(n, shape, st) for n, st in (("logits", in_strides), ("out", out_strides)))
+    return ctypes.byref(d), _type(FP32), _type("int32"), {
+        "batch": (batch,), "rows": (batch, n_q), "tokens": (batch, d.room),
+        "tree": (1 if d.tree_shared else batch, n_q, (n_q + 31) // 32), "bias": (1 if d.bias_shared else batch, d.n_bias),
+        "masks": (d.n_masks, (vocab + 31) // 32)}
+
+
+def _logits_stride(name, shape, strides):
+    """Of rows, which have to be apart by the same step; 0 where there is one row."""
+    rows = [(n, st) for n, st in zip(shape[:-1], strides[:-1]) if n > 1]
+    if shape[-1] > 1 and strides[-1] != 1:
+        raise MafatError(EINVAL, "%s: a row's logits must be contiguous" % name)
+    if not rows or 0 in shape:
+        return 0
+    step = rows[-1][1]
+    if step < shape[-1] or (len(rows) == 2 and rows[0][1] != rows[1][0] * step):
+        raise MafatError(EINVAL, "%s: rows must be apart by one step, of vocab at least" % name)
+    return step
 
 
 def diag_umma(a_dev, b_dev, d_dev, n, a_in_tmem=False, stream=None):

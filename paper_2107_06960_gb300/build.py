@@ -19,8 +19,10 @@ ROOT = os.path.dirname(HERE)
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmafat.so")
 SOURCES = ["planner.cpp", "order.cpp", "runtime.cpp", "search.cpp", "kernel_fp32.cu", "kernel_tc.cu", "noalloc.cu",
-           "attention.cpp", "attn_simt.cu", "attn_rows.cu", "attn_tc.cu", "attn_join.cu", "rms_norm.cu"]
-HEADERS = ["planner.h", "device_types.h", "kernels.h", "sched.cuh", "attention.h", "attn_common.cuh"]
+           "attention.cpp", "attn_simt.cu", "attn_rows.cu", "attn_tc.cu", "attn_tc_tree.cu", "attn_join.cu", "rms_norm.cu",
+           "decode.cpp", "block_norm.cu", "rotary.cu", "logits.cu"]
+HEADERS = ["planner.h", "device_types.h", "kernels.h", "sched.cuh", "attention.h", "attn_common.cuh",
+           "attn_tc.cuh", "decode.h", "lm_checks.h", "row_common.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

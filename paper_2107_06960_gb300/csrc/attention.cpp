@@ -6,17 +6,13 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
-#include <limits>
 #include <new>
 
 #include "../../include/mafat.h"
 #include "attention.h"
 #include "device_types.h"
+#include "lm_checks.h"
 
-mafat_status mafat_internal_fail(mafat_status s, const char* msg);
-void mafat_internal_clear_error();
 void* mafat_internal_encode_tiled();
 
 // A kernel, the shape of its work and the time that it takes, in us, measured on GB300 with launches back to back over
@@ -42,8 +38,12 @@ struct AttnSegPlan {
     double us = 0.;  // by the model
 };
 
+enum AttnKind { kCross, kPrefix, kTree };
+const char* const kAttnPlans[] = {"mafat_cross_plan", "mafat_prefix_plan", "mafat_tree_plan"};
+
 struct mafat_attn_s {
-    bool prefix = false, dry_run = false;
+    AttnKind kind = kCross;
+    bool dry_run = false;
     int device = 0;
     int32_t dtype = 0, batch = 0, n_q = 0, heads_q = 0, heads_kv = 0, dim = 0;
     float scale = 0.f;
@@ -66,79 +66,12 @@ struct mafat_attn_s {
 
 namespace {
 
-// Nothing that throws passes a C entry: messages are made on the stack, and keeping one may fail.
-mafat_status fail(mafat_status s, const char* format, ...) {
-    char msg[256];
-    va_list args;
-    va_start(args, format);
-    vsnprintf(msg, sizeof(msg), format, args);
-    va_end(args);
-    try {
-        return mafat_internal_fail(s, msg);
-    } catch (...) {
-        return s;
-    }
-}
-mafat_status cuda_fail(cudaError_t e, const char* what) {
-    return fail(e == cudaErrorMemoryAllocation ? MAFAT_ENOMEM : MAFAT_ECUDA, "%s: %s", what, cudaGetErrorString(e));
-}
+using namespace mafat_lm;
 
 constexpr int kStatusBytes = 256;
-constexpr int64_t kMaxI32 = std::numeric_limits<int32_t>::max();
 // rows and keys: a tile past the last still has a number in 32 bits
 constexpr int64_t kMostCounted = kMaxI32 - 65536;
 constexpr int kMaxDim = 128;
-
-bool aligned(const void* p, uintptr_t n = 16) { return ((uintptr_t)p & (n - 1)) == 0; }
-
-// Bytes from a tensor's first element to past its last one, for sizes and strides in elements.
-int64_t extent(const int64_t n[3], const int64_t st[3], int64_t inner, int64_t esz) {
-    int64_t last = inner;
-    for (int i = 0; i < 3; ++i) last += (n[i] - 1) * st[i];
-    return last * esz;
-}
-
-bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
-    const char *x = (const char*)a, *y = (const char*)b;
-    return x && y && an > 0 && bn > 0 && x < y + bn && y < x + an;
-}
-
-// Strides given by the caller (all 0: packed), in elements.  They have to keep every 16-byte
-// vector of channels aligned, and what they span with the sizes inside 62 bits of bytes, so that no offset passes 64.
-// Where there is nothing to step to (one element of a dimension, or none at all) any stride is taken, and a valid one kept.
-mafat_status take_strides(const char* what, const int64_t given[3], const int64_t n[3], int64_t dim, int64_t esz,
-                          int64_t out[3]) {
-    const int64_t most = ((int64_t)1 << 40) / esz;
-    const bool packed = given[0] == 0 && given[1] == 0 && given[2] == 0, empty = n[0] == 0 || n[1] == 0 || n[2] == 0;
-    __int128 span = dim, next = dim;  // of the packed: the stride of a dimension by those inside it
-    for (int i = 2; i >= 0; --i) {
-        out[i] = dim;
-        if (n[i] <= 1 || empty) continue;
-        const __int128 st = packed ? next : (__int128)given[i];
-        if (st < dim) return fail(MAFAT_EINVAL, "%s: a stride is smaller than a head's channels", what);
-        if (st * esz % 16 != 0) return fail(MAFAT_EINVAL, "%s: strides must be multiples of 16 bytes", what);
-        if (st >= most) return fail(MAFAT_EUNSUPPORTED, "%s: strides must be below 2^40 bytes", what);
-        out[i] = (int64_t)st;
-        span += (n[i] - 1) * st;
-        next *= n[i];
-    }
-    if (span * esz > (__int128)1 << 62) return fail(MAFAT_EUNSUPPORTED, "%s: the tensor spans more than 2^62 bytes", what);
-    return MAFAT_OK;
-}
-
-// Two elements of a written tensor must not share a place: sorted by stride, each stride has to
-// pass what the dimensions inside it span.
-bool places_distinct(const int64_t n[3], const int64_t st[3], int64_t dim) {
-    int at[3] = {0, 1, 2};
-    std::sort(at, at + 3, [&](int a, int b) { return st[a] < st[b]; });
-    int64_t span = dim;
-    for (int i : at) {
-        if (n[i] == 1) continue;
-        if (st[i] < span) return false;
-        span = (n[i] - 1) * st[i] + span;
-    }
-    return true;
-}
 
 int sm_count(int device) {
     int n = 0;
@@ -408,7 +341,16 @@ struct SegData {
     const uint8_t* mask;
 };
 
-mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* out, float* lse, cudaStream_t s) {
+// What a tree's run has more.
+struct TreeData {
+    const int32_t* nodes = nullptr;
+    const uint32_t* tree = nullptr;
+    bool shared = false;
+};
+
+mafat_status run(const mafat_attn_s* p, AttnKind kind, const void* q, const SegData* d, const TreeData& tree, void* out,
+                 float* lse, cudaStream_t s) {
+    if (p->kind != kind) return fail(MAFAT_EINVAL, "the plan is one of %s", kAttnPlans[p->kind]);
     if (p->dry_run) return fail(MAFAT_EINVAL, "plan was created with dry_run");
     if (!q || !out) return fail(MAFAT_EINVAL, "null q or out");
     if (!aligned(q) || !aligned(out) || !aligned(lse, 4)) return fail(MAFAT_EINVAL, "q and out must be 16-byte aligned, lse 4-byte");
@@ -455,6 +397,16 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         if (!aligned(d[i].len, 4)) return fail(MAFAT_EINVAL, "lengths must be 4-byte aligned");
         if (!clear(d[i].len, (int64_t)g.n_seq * 4)) return fail(MAFAT_EINVAL, "an output overlaps another tensor");
     }
+    const int32_t tree_words = (p->n_q + 31) / 32;
+    if (kind == kTree) {
+        if (!tree.tree) return fail(MAFAT_EINVAL, "null tree");
+        if (!aligned(tree.tree, 4) || !aligned(tree.nodes, 4)) return fail(MAFAT_EINVAL, "tree and nodes must be 4-byte aligned");
+        if (!clear(tree.tree, (int64_t)(tree.shared ? 1 : p->batch) * p->n_q * tree_words * 4) ||
+            !clear(tree.nodes, (int64_t)p->batch * 4))
+            return fail(MAFAT_EINVAL, "an output overlaps another tensor");
+        a.tree = 1;
+        a.nodes = tree.nodes;
+    }
     int dev = -1;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
@@ -470,6 +422,9 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
         x.v_sb = g.v[0]; x.v_ss = g.v[1]; x.v_sh = g.v[2];
         x.len = d[i].len;
         x.mask = d[i].mask;
+        x.tree = i == 1 ? tree.tree : nullptr;
+        x.tree_s = tree.shared ? 0 : (int64_t)p->n_q * tree_words;
+        x.tree_words = tree_words;
         x.n = g.n;
         x.causal = g.causal;
         x.reqs = g.reqs;
@@ -518,6 +473,41 @@ mafat_status run(const mafat_attn_s* p, const void* q, const SegData* d, void* o
     return MAFAT_OK;
 }
 
+// kind: kPrefix, or kTree, whose own keys each row reads by its bits
+mafat_status prefix_plan(const mafat_prefix_desc* d, AttnKind kind, mafat_attn_t** out) {
+    if (!d || !out) return fail(MAFAT_EINVAL, "null argument");
+    *out = nullptr;
+    if (d->struct_size != (int32_t)sizeof(mafat_prefix_desc)) return fail(MAFAT_EINVAL, "struct_size is not the descriptor's");
+    if (d->prefixes < 1 || d->requests < 1) return fail(MAFAT_EINVAL, "prefixes and requests must be positive");
+    if (d->prefixes > kMaxI32 / d->requests) return fail(MAFAT_EUNSUPPORTED, "too many requests");
+    const Common c{d->dtype, d->prefixes * d->requests, d->n_q, d->heads_q, d->heads_kv, d->head_dim, d->kernel,
+                   d->splits, d->dry_run, d->scale, d->q_strides, d->out_strides};
+    mafat_status st = check_common(c);
+    if (st != MAFAT_OK) return st;
+    if (d->n_prefix < 0 || d->n_own < 0) return fail(MAFAT_EINVAL, "n_prefix and n_own must not be negative");
+    mafat_attn_s* p = new (std::nothrow) mafat_attn_s();
+    if (!p) return fail(MAFAT_ENOMEM, "host allocation failed");
+    p->kind = kind;
+    p->n_seg = 2;
+    AttnSegPlan &g = p->seg[0], &w = p->seg[1];
+    g.n_seq = d->prefixes;
+    g.reqs = d->requests;
+    g.n = d->n_prefix;
+    w.n_seq = c.batch;
+    w.reqs = 1;
+    w.n = d->n_own;
+    w.causal = kind == kPrefix;
+    const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4;
+    const int64_t np[3] = {d->prefixes, d->n_prefix, d->heads_kv}, no[3] = {c.batch, d->n_own, d->heads_kv};
+    if ((st = take_strides("prefix_k_strides", d->prefix_k_strides, np, d->head_dim, esz, g.k)) != MAFAT_OK ||
+        (st = take_strides("prefix_v_strides", d->prefix_v_strides, np, d->head_dim, esz, g.v)) != MAFAT_OK ||
+        (st = take_strides("own_k_strides", d->own_k_strides, no, d->head_dim, esz, w.k)) != MAFAT_OK ||
+        (st = take_strides("own_v_strides", d->own_v_strides, no, d->head_dim, esz, w.v)) != MAFAT_OK ||
+        (st = finish_plan(p, c, out)) != MAFAT_OK)
+        mafat_attn_destroy(p);
+    return st;
+}
+
 }  // namespace
 
 extern "C" {
@@ -549,52 +539,29 @@ mafat_status mafat_cross_plan(const mafat_cross_desc* d, mafat_attn_t** out) {
 mafat_status mafat_cross_run(const mafat_attn_t* p, const void* q, const void* k, const void* v, const int32_t* kv_len,
                              const uint8_t* kv_mask, void* out, float* lse, void* stream) {
     if (!p) return fail(MAFAT_EINVAL, "null plan");
-    if (p->prefix) return fail(MAFAT_EINVAL, "the plan is one of mafat_prefix_plan");
     const SegData d[1] = {{k, v, kv_len, kv_mask}};
-    return run(p, q, d, out, lse, (cudaStream_t)stream);
+    return run(p, kCross, q, d, TreeData(), out, lse, (cudaStream_t)stream);
 }
 
-mafat_status mafat_prefix_plan(const mafat_prefix_desc* d, mafat_attn_t** out) {
-    if (!d || !out) return fail(MAFAT_EINVAL, "null argument");
-    *out = nullptr;
-    if (d->struct_size != (int32_t)sizeof(mafat_prefix_desc)) return fail(MAFAT_EINVAL, "struct_size is not the descriptor's");
-    if (d->prefixes < 1 || d->requests < 1) return fail(MAFAT_EINVAL, "prefixes and requests must be positive");
-    if (d->prefixes > kMaxI32 / d->requests) return fail(MAFAT_EUNSUPPORTED, "too many requests");
-    const Common c{d->dtype, d->prefixes * d->requests, d->n_q, d->heads_q, d->heads_kv, d->head_dim, d->kernel,
-                   d->splits, d->dry_run, d->scale, d->q_strides, d->out_strides};
-    mafat_status st = check_common(c);
-    if (st != MAFAT_OK) return st;
-    if (d->n_prefix < 0 || d->n_own < 0) return fail(MAFAT_EINVAL, "n_prefix and n_own must not be negative");
-    mafat_attn_s* p = new (std::nothrow) mafat_attn_s();
-    if (!p) return fail(MAFAT_ENOMEM, "host allocation failed");
-    p->prefix = true;
-    p->n_seg = 2;
-    AttnSegPlan &g = p->seg[0], &w = p->seg[1];
-    g.n_seq = d->prefixes;
-    g.reqs = d->requests;
-    g.n = d->n_prefix;
-    w.n_seq = c.batch;
-    w.reqs = 1;
-    w.n = d->n_own;
-    w.causal = 1;
-    const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4;
-    const int64_t np[3] = {d->prefixes, d->n_prefix, d->heads_kv}, no[3] = {c.batch, d->n_own, d->heads_kv};
-    if ((st = take_strides("prefix_k_strides", d->prefix_k_strides, np, d->head_dim, esz, g.k)) != MAFAT_OK ||
-        (st = take_strides("prefix_v_strides", d->prefix_v_strides, np, d->head_dim, esz, g.v)) != MAFAT_OK ||
-        (st = take_strides("own_k_strides", d->own_k_strides, no, d->head_dim, esz, w.k)) != MAFAT_OK ||
-        (st = take_strides("own_v_strides", d->own_v_strides, no, d->head_dim, esz, w.v)) != MAFAT_OK ||
-        (st = finish_plan(p, c, out)) != MAFAT_OK)
-        mafat_attn_destroy(p);
-    return st;
-}
+mafat_status mafat_prefix_plan(const mafat_prefix_desc* d, mafat_attn_t** out) { return prefix_plan(d, kPrefix, out); }
 
 mafat_status mafat_prefix_run(const mafat_attn_t* p, const void* q, const void* prefix_k, const void* prefix_v,
                               const int32_t* prefix_len, const uint8_t* prefix_mask, const void* own_k,
                               const void* own_v, const int32_t* own_len, void* out, float* lse, void* stream) {
     if (!p) return fail(MAFAT_EINVAL, "null plan");
-    if (!p->prefix) return fail(MAFAT_EINVAL, "the plan is one of mafat_cross_plan");
     const SegData d[2] = {{prefix_k, prefix_v, prefix_len, prefix_mask}, {own_k, own_v, own_len, nullptr}};
-    return run(p, q, d, out, lse, (cudaStream_t)stream);
+    return run(p, kPrefix, q, d, TreeData(), out, lse, (cudaStream_t)stream);
+}
+
+mafat_status mafat_tree_plan(const mafat_prefix_desc* d, mafat_attn_t** out) { return prefix_plan(d, kTree, out); }
+
+mafat_status mafat_tree_run(const mafat_attn_t* p, const void* q, const void* prefix_k, const void* prefix_v,
+                            const int32_t* prefix_len, const uint8_t* prefix_mask, const void* own_k, const void* own_v,
+                            const int32_t* own_len, const int32_t* nodes, const uint32_t* tree, int32_t tree_shared,
+                            void* out, float* lse, void* stream) {
+    if (!p) return fail(MAFAT_EINVAL, "null plan");
+    const SegData d[2] = {{prefix_k, prefix_v, prefix_len, prefix_mask}, {own_k, own_v, own_len, nullptr}};
+    return run(p, kTree, q, d, TreeData{nodes, tree, tree_shared != 0}, out, lse, (cudaStream_t)stream);
 }
 
 mafat_status mafat_attn_stats(const mafat_attn_t* p, mafat_attn_stats_t* out) {

@@ -33,6 +33,10 @@ struct MafatAttnSeg {
     int64_t v_sb, v_ss, v_sh;
     const int32_t* len;         // [n_seq] readable keys (null: n)
     const uint8_t* mask;        // [n_seq][n] 0: the key is not readable (null: all are)
+    // of a tree's own keys: for each of a sequence's n_q nodes the bits of those on its way from the root (null: no tree)
+    const uint32_t* tree;
+    int64_t tree_s;             // words of a sequence (0: all share one tree)
+    int32_t tree_words;         // of a node
     int32_t n;                  // keys that a sequence has room for
     int32_t causal;             // 1: token t of n_q sees keys 0 .. len - n_q + t
     int32_t reqs;
@@ -54,6 +58,8 @@ struct MafatAttnArgs {
     int64_t q_sb, q_st, q_sh;
     int64_t o_sb, o_st, o_sh;
     int32_t n_q, group, heads_q, heads_kv, dim;
+    int32_t tree;               // 1: queries are nodes of trees
+    const int32_t* nodes;       // [batch] of each tree (null: n_q)
     MafatDiv n_q_div, group_div, heads_q_div, heads_kv_div;
     int32_t parts;              // parts of a row, over all segments
     // 1: the CTA that has the row writes its result, joined with the `join` parts of an earlier launch; 0: it writes a part
@@ -96,6 +102,10 @@ struct MafatAttnPrefix {
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
                                  const MafatAttnPrefix* prefix, cudaStream_t s);
 cudaError_t mafat_prepare_attn_tc();
+// of these, the forms for trees
+cudaError_t mafat_launch_attn_tc_tree(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
+                                      const MafatAttnPrefix* prefix, cudaStream_t s);
+cudaError_t mafat_prepare_attn_tc_tree();
 
 // Joins the parts of each row.
 cudaError_t mafat_launch_attn_join(const MafatAttnArgs& a, bool bf16, cudaStream_t s);
@@ -144,3 +154,14 @@ enum MafatNormQuant { MAFAT_NORM_PLAIN = 0, MAFAT_NORM_ROW = 1, MAFAT_NORM_BLOCK
 int mafat_norm_max_cols();  // of a row
 // vec: a power of two that divides cols and every matrix's row stride: the rows can be accessed by as many channels
 cudaError_t mafat_launch_norm(const MafatNormArgs& a, bool bf16, int vec, MafatNormQuant quant, cudaStream_t s);
+
+// The norms around a block: `n` is the norm after it, whose x is the block's result.
+struct MafatBlockNormArgs {
+    MafatNormArgs n;            // y null: not wanted
+    const void* post_weight;    // [cols] of the norm of x (null: none)
+    const void* gate;           // [rows / rows of a gate][cols] (null: none)
+    int64_t g_s;
+    MafatDiv gate_div;          // rows that share a gate
+    float branch, keep;         // scales of the block's result and of the residual
+};
+cudaError_t mafat_launch_block_norm(const MafatBlockNormArgs& a, bool bf16, int vec, MafatNormQuant quant, cudaStream_t s);

@@ -89,6 +89,45 @@ struct Row {
     }
 };
 
+// The form for trees of drafted tokens (TREE of the kernels): a request has nodes_of() queries, and one of them reads of its
+// request's own keys all before the tree's and those that its bits name.
+__device__ __forceinline__ int nodes_of(const MafatAttnArgs& a, int64_t req) {
+    return a.nodes ? min(max(a.nodes[req], 0), a.n_q) : a.n_q;
+}
+// whether the row is one of its tree's nodes
+template <bool TREE>
+__device__ __forceinline__ bool live(const MafatAttnArgs& a, const Row& r) {
+    return !TREE || r.t < nodes_of(a, r.req);
+}
+// As Row::limit; a row past its tree's nodes sees nothing.
+template <bool TREE>
+__device__ __forceinline__ int limit_of(const MafatAttnArgs& a, const Block& b, const Row& r) {
+    if constexpr (TREE) return live<TREE>(a, r) ? b.len : 0;
+    return r.limit(a, b);
+}
+// The first key of the tree; past all keys where the set has none.
+__device__ __forceinline__ int tree_first(const MafatAttnArgs& a, const Block& b) {
+    return a.seg.tree ? b.len - nodes_of(a, b.seq) : 0x7fffffff;
+}
+struct Way {
+    const uint32_t* bits;
+    __device__ __forceinline__ Way() : bits(nullptr) {}
+    __device__ __forceinline__ Way(const MafatAttnArgs& a, const Block& b, const Row& r)
+        : bits(a.seg.tree + (int64_t)b.seq * a.seg.tree_s + (int64_t)r.t * a.seg.tree_words) {}
+    // key: at most the tree's last
+    __device__ __forceinline__ bool holds(int key, int first) const {
+        const int n = key - first;
+        return n < 0 || (bits[n / 32] >> (n % 32) & 1u) != 0u;
+    }
+    // whether it holds each of the 32 keys from `key`, bit by bit; past the last node none
+    __device__ __forceinline__ uint32_t from(int key, int first, int words) const {
+        const int n = key - first, i = n >> 5;  // rounded down also where n is negative
+        const uint32_t lo = i < 0 ? 0xffffffffu : i < words ? bits[i] : 0u;
+        const uint32_t hi = i + 1 < 0 ? 0xffffffffu : i + 1 < words ? bits[i + 1] : 0u;
+        return __funnelshift_r(lo, hi, (uint32_t)n & 31u);
+    }
+};
+
 // Where a row's results go.
 struct Out {
     int64_t o;     // element of out

@@ -147,8 +147,8 @@ struct Ahead : Items {
 };
 
 // CLUSTER: a cluster's CTAs have an item's parts and join them (an instance of its own: in one kernel it cost the
-// other form's inner loop 20 %)
-template <int DP, bool CLUSTER>
+// other form's inner loop 20 %).  TREE: queries are nodes of trees, whose bits are looked at in runs that have such keys.
+template <int DP, bool CLUSTER, bool TREE>
 __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ MafatAttnArgs a) {
     using C = Cfg<DP, CLUSTER>;
     using Parts = mafat_attn::ClusterParts<16, DP>;
@@ -239,10 +239,17 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             ldm4(q[t], smem + C::kOffQ + which * C::kQ + (uint32_t)(v_row * (DP * 2) + (((2 * t + v_chunk) ^ (v_row % 8)) * 16)));
         load_queries(it.next(), which ^ 1u);  // lands with the next run
         int limit[2];
+        mafat_attn::Way way[2];
+        const int first_node = TREE ? mafat_attn::tree_first(a, b) : 0x7fffffff;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = b.row0 + lane / 4 + 8 * h;
-            limit[h] = r < g.rows ? mafat_attn::Row(a, b, r).limit(a, b) : 0x7fffffff;
+            limit[h] = 0x7fffffff;
+            if (!TREE || r < g.rows) {
+                const mafat_attn::Row row(a, b, r);
+                if (r < g.rows) limit[h] = mafat_attn::limit_of<TREE>(a, b, row);
+                if (TREE && g.tree) way[h] = mafat_attn::Way(a, b, row);
+            }
         }
         float base[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
         float o[DP / 8][4];
@@ -275,6 +282,17 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                         const int k = key + n * 8 + (lane % 4) * 2 + e % 2;
                         if (k >= b.len || k >= limit[e / 2] || (mask && mask[k] == 0)) s[n][e] = -CUDART_INF_F;
                     }
+            }
+            if (TREE && key + kRun > first_node) {
+                uint32_t held[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    held[h] = way[h].bits ? way[h].from(key, first_node, g.tree_words) >> (lane % 4 * 2) : 0xffffffffu;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if ((held[e / 2] >> (n * 8 + e % 2) & 1u) == 0u) s[n][e] = -CUDART_INF_F;
             }
             float keep[2], off[2];
             bool up = false;
@@ -435,17 +453,26 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     mafat_attn::launch_end(a);
 }
 
-template <int DP>
-cudaError_t launch(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
-    return mafat_launch_clusters(a.cluster, a.cluster > 1 ? attn_rows_kernel<DP, true> : attn_rows_kernel<DP, false>,
+template <int DP, bool TREE>
+cudaError_t launch_form(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
+    return mafat_launch_clusters(a.cluster, a.cluster > 1 ? attn_rows_kernel<DP, true, TREE> : attn_rows_kernel<DP, false, TREE>,
                                  (unsigned)ctas, kThreads, a.cluster > 1 ? Cfg<DP, true>::kSmem : Cfg<DP, false>::kSmem, s, a);
 }
 template <int DP>
-cudaError_t prepare() {
-    const cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+cudaError_t launch(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
+    return a.tree ? launch_form<DP, true>(a, ctas, s) : launch_form<DP, false>(a, ctas, s);
+}
+template <int DP, bool TREE>
+cudaError_t prepare_form() {
+    const cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<DP, false, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                Cfg<DP, false>::kSmem);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(attn_rows_kernel<DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP, true>::kSmem);
+    return cudaFuncSetAttribute(attn_rows_kernel<DP, true, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP, true>::kSmem);
+}
+template <int DP>
+cudaError_t prepare() {
+    const cudaError_t e = prepare_form<DP, false>();
+    return e != cudaSuccess ? e : prepare_form<DP, true>();
 }
 
 }  // namespace

@@ -159,7 +159,7 @@ struct Readable {
     }
 };
 
-template <int DP, bool MASK>
+template <int DP, bool MASK, bool TREE>
 __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __grid_constant__ MafatAttnArgs a) {
     using L = Tile<DP>;
     extern __shared__ __align__(16) float sm[];
@@ -218,9 +218,10 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
     int limit[4];
     float base[4], l[4];
     float2 o[4][kO];
+    const int first_node = TREE ? mafat_attn::tree_first(a, b) : 0x7fffffff;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        limit[i] = mafat_attn::Row(a, b, b.row0 + ty * 4 + i).limit(a, b);
+        limit[i] = mafat_attn::limit_of<TREE>(a, b, mafat_attn::Row(a, b, TREE ? min(b.row0 + ty * 4 + i, g.rows - 1) : b.row0 + ty * 4 + i));
         base[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
@@ -264,6 +265,9 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
             for (int j = 0; j < 4; ++j) {
                 s[j] = acc[i][j].x + acc[i][j].y;
                 if (key[j] < 0 || key[j] >= limit[i]) s[j] = -INFINITY;
+                if (TREE && key[j] >= first_node &&
+                    !mafat_attn::Way(a, b, mafat_attn::Row(a, b, min(b.row0 + ty * 4 + i, g.rows - 1))).holds(key[j], first_node))
+                    s[j] = -INFINITY;
                 top = mafat_attn::max_nan(top, s[j]);
             }
 #pragma unroll
@@ -353,7 +357,7 @@ struct Few {
     static_assert(kFewWarps * R * (DP + 2) <= kFewWarps * kWarp, "the join's space is the rings'");
 };
 
-template <int R, int DP, bool CLUSTER>
+template <int R, int DP, bool CLUSTER, bool TREE>
 __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_few_kernel(const __grid_constant__ MafatAttnArgs a) {
     using L = Few<R, DP, CLUSTER>;
     using Parts = mafat_attn::ClusterParts<R, DP>;
@@ -408,6 +412,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
 #pragma unroll
         for (int d = 0; d < kCh / 2; ++d) o[i][d] = make_float2(0.f, 0.f);
     }
+    const int first_node = TREE ? mafat_attn::tree_first(a, b) : 0x7fffffff;
     // scores: a lane has one key and every fourth quad of channels
     const int key_of = lane % kRun, part = lane / kRun;
 #pragma unroll 1
@@ -437,11 +442,19 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
         bool moved = false;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int limit = g.causal ? mafat_attn::Row(a, b, b.row0 + r).limit(a, b) : b.len;
+            int limit = b.len;
+            bool held = true;
+            if constexpr (TREE) {
+                const mafat_attn::Row row(a, b, min(b.row0 + r, g.rows - 1));
+                limit = mafat_attn::limit_of<true>(a, b, row);
+                if (seen && k >= first_node) held = mafat_attn::Way(a, b, row).holds(k, first_node);
+            } else if (g.causal) {
+                limit = mafat_attn::Row(a, b, b.row0 + r).limit(a, b);
+            }
             float s = acc[r].x + acc[r].y;
 #pragma unroll
             for (int w = kRun; w < 32; w *= 2) s += __shfl_xor_sync(0xffffffffu, s, w);
-            if (!seen || k >= limit) s = -INFINITY;
+            if (!seen || k >= limit || !held) s = -INFINITY;
             keep[r] = softmax_step<kRun>(s, base[r], l[r], a.scale_log2);  // l: each key in four lanes
             moved = moved || keep[r] != 1.f;
             if (part == 0) sp[r * kRun + key_of] = s;
@@ -529,30 +542,48 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
     mafat_attn::launch_end(a);
 }
 
+template <int DP, bool TREE>
+cudaError_t launch_form(const MafatAttnArgs& a, cudaStream_t s) {
+    return mafat_launch_overlapped(a.seg.mask ? attn_simt_kernel<DP, true, TREE> : attn_simt_kernel<DP, false, TREE>,
+                                   a.seg.items, Tile<DP>::kThreads, Tile<DP>::kSmem, s, a);
+}
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
-    return mafat_launch_overlapped(a.seg.mask ? attn_simt_kernel<DP, true> : attn_simt_kernel<DP, false>, a.seg.items,
-                                   Tile<DP>::kThreads, Tile<DP>::kSmem, s, a);
+    return a.tree ? launch_form<DP, true>(a, s) : launch_form<DP, false>(a, s);
+}
+template <int R, int DP, bool TREE>
+cudaError_t launch_few_form(const MafatAttnArgs& a, cudaStream_t s) {
+    return mafat_launch_clusters(a.cluster,
+                                 a.cluster > 1 ? attn_simt_few_kernel<R, DP, true, TREE> : attn_simt_few_kernel<R, DP, false, TREE>,
+                                 a.seg.items, kFewWarps * 32,
+                                 a.cluster > 1 ? Few<R, DP, true>::kSmem : Few<R, DP, false>::kSmem, s, a);
 }
 template <int R, int DP>
 cudaError_t launch_few(const MafatAttnArgs& a, cudaStream_t s) {
-    return mafat_launch_clusters(a.cluster,
-                                 a.cluster > 1 ? attn_simt_few_kernel<R, DP, true> : attn_simt_few_kernel<R, DP, false>,
-                                 a.seg.items, kFewWarps * 32,
-                                 a.cluster > 1 ? Few<R, DP, true>::kSmem : Few<R, DP, false>::kSmem, s, a);
+    return a.tree ? launch_few_form<R, DP, true>(a, s) : launch_few_form<R, DP, false>(a, s);
 }
 cudaError_t prepare(const void* fn, int smem) {
     return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
 }
+template <int DP, bool TREE>
+cudaError_t prepare_tiles_form() {
+    const cudaError_t e = prepare((const void*)attn_simt_kernel<DP, false, TREE>, Tile<DP>::kSmem);
+    return e != cudaSuccess ? e : prepare((const void*)attn_simt_kernel<DP, true, TREE>, Tile<DP>::kSmem);
+}
 template <int DP>
 cudaError_t prepare_tiles() {
-    const cudaError_t e = prepare((const void*)attn_simt_kernel<DP, false>, Tile<DP>::kSmem);
-    return e != cudaSuccess ? e : prepare((const void*)attn_simt_kernel<DP, true>, Tile<DP>::kSmem);
+    const cudaError_t e = prepare_tiles_form<DP, false>();
+    return e != cudaSuccess ? e : prepare_tiles_form<DP, true>();
+}
+template <int R, int DP, bool TREE>
+cudaError_t prepare_few_form() {
+    const cudaError_t e = prepare((const void*)attn_simt_few_kernel<R, DP, false, TREE>, Few<R, DP, false>::kSmem);
+    return e != cudaSuccess ? e : prepare((const void*)attn_simt_few_kernel<R, DP, true, TREE>, Few<R, DP, true>::kSmem);
 }
 template <int R, int DP>
 cudaError_t prepare_few() {
-    const cudaError_t e = prepare((const void*)attn_simt_few_kernel<R, DP, false>, Few<R, DP, false>::kSmem);
-    return e != cudaSuccess ? e : prepare((const void*)attn_simt_few_kernel<R, DP, true>, Few<R, DP, true>::kSmem);
+    const cudaError_t e = prepare_few_form<R, DP, false>();
+    return e != cudaSuccess ? e : prepare_few_form<R, DP, true>();
 }
 
 }  // namespace

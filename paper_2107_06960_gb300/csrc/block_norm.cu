@@ -1,0 +1,139 @@
+// The norms around a block, with its gate and the residual's scale:
+//   n = x / sqrt(mean(x^2) + eps) * w1;  h = a r + b g n;  y = h / sqrt(mean(h^2) + eps) * w2,
+// y in the inputs' type or in 8 bits with scales, as the norm alone has them.
+//
+// One pass: a row stays in registers between its two sums of squares and the output, so that x, r are read and h, y
+// written once; bound by those bytes.  All is fp32 until a result is rounded, once; y is of the unrounded h.
+#include "row_common.cuh"
+
+namespace {
+
+constexpr int kRowWarps = 4;   // rows of a block whose rows take one warp each
+constexpr int kMaxWarps = 16;  // of a row
+constexpr int kMaxThread = 32; // channels of a thread
+constexpr int kFewRows = 2048;
+
+// Sum over the row's warps; `part` is not used by another sum of the row.
+__device__ __forceinline__ float row_sum(float v, float* part, int warps) {
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) v += __shfl_xor_sync(0xffffffffu, v, w);
+    if (warps > 1) {
+        if (threadIdx.x == 0) part[threadIdx.y] = v;
+        __syncthreads();
+        v = (int)threadIdx.x < warps ? part[threadIdx.x] : 0.f;
+#pragma unroll
+        for (int w = 1; w < 32; w *= 2) v += __shfl_xor_sync(0xffffffffu, v, w);
+    }
+    return v;
+}
+
+// V channels an access, N accesses a thread.  blockDim = (32, warps of a row, rows).
+template <class T, int V, int N, MafatNormQuant Q>
+__global__ void __launch_bounds__(kMaxWarps * 32) block_norm_kernel(const __grid_constant__ MafatBlockNormArgs a) {
+    __shared__ float part[3][kMaxWarps];
+    const int lane = threadIdx.x, warp = threadIdx.y, warps = blockDim.y;
+    const int64_t row = (int64_t)blockIdx.x * blockDim.z + threadIdx.z;
+    if (row >= a.n.rows) return;  // only blocks whose rows take one warp each have several rows: no barrier follows
+    const int cols = a.n.cols;
+    const int c0 = (warp * 32 * N + lane) * V;
+    Vec<T, V> vx[N], vr[N], vw[N];
+    launch_wait();
+    const T* x = (const T*)a.n.x + row * a.n.x_s;
+    const T* r = (const T*)a.n.residual + row * a.n.r_s;
+#pragma unroll
+    for (int i = 0; i < N; ++i) vx[i].load(x + c0 + i * 32 * V, c0 + i * 32 * V < cols);
+#pragma unroll
+    for (int i = 0; i < N; ++i) vr[i].load(r + c0 + i * 32 * V, c0 + i * 32 * V < cols);
+    launch_next();
+    float h[N][V];
+#pragma unroll
+    for (int i = 0; i < N; ++i) vx[i].get(h[i]);
+    if (a.post_weight) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) vw[i].load((const T*)a.post_weight + c0 + i * 32 * V, c0 + i * 32 * V < cols);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum = fmaf(h[i][j], h[i][j], sum);
+        const float inv = 1.f / sqrtf(row_sum(sum, part[0], warps) / (float)cols + a.n.eps);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float w[V];
+            vw[i].get(w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[i][j] = h[i][j] * inv * w[j];
+        }
+    }
+    if (a.gate) {
+        const T* gate = (const T*)a.gate + (int64_t)a.gate_div.div((uint32_t)row) * a.g_s;
+#pragma unroll
+        for (int i = 0; i < N; ++i) vw[i].load(gate + c0 + i * 32 * V, c0 + i * 32 * V < cols);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float w[V];
+            vw[i].get(w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[i][j] *= w[j];
+        }
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float v[V];
+        vr[i].get(v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            h[i][j] = fmaf(a.branch, h[i][j], a.keep * v[j]);
+            sum = fmaf(h[i][j], h[i][j], sum);
+        }
+    }
+    if (a.n.residual_out) {
+        T* ro = (T*)a.n.residual_out + row * a.n.ro_s;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = c0 + i * 32 * V;
+            if (c < cols) Vec<T, V>::store(ro + c, h[i]);
+        }
+    }
+    if (!a.n.y) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) vw[i].load((const T*)a.n.weight + c0 + i * 32 * V, c0 + i * 32 * V < cols);
+    const float inv = 1.f / sqrtf(row_sum(sum, part[1], warps) / (float)cols + a.n.eps);
+    finish_row<T, V, N, Q>(a.n, row, c0, h, vw, inv, part[2], warps);
+}
+
+template <class T, int V, int N>
+cudaError_t launch(const MafatBlockNormArgs& a, MafatNormQuant q, int warps, cudaStream_t s) {
+    const int rows = warps == 1 ? kRowWarps : 1;
+    const dim3 block(32, warps, rows);
+    const unsigned grid = (unsigned)((a.n.rows + rows - 1) / rows);
+    return mafat_launch_overlapped(q == MAFAT_NORM_PLAIN ? block_norm_kernel<T, V, N, MAFAT_NORM_PLAIN>
+                                   : q == MAFAT_NORM_ROW ? block_norm_kernel<T, V, N, MAFAT_NORM_ROW>
+                                                         : block_norm_kernel<T, V, N, MAFAT_NORM_BLOCK>,
+                                   grid, block, 0, s, a);
+}
+
+// Accesses of a thread, as of the norm alone.
+template <class T, int V, int N>
+cudaError_t launch_v(const MafatBlockNormArgs& a, MafatNormQuant q, cudaStream_t s) {
+    const int per_warp = 32 * V * N;
+    const int most = q != MAFAT_NORM_BLOCK ? kMaxThread : V == 1 ? 8 : 16;
+    const bool one_warp = a.n.rows >= kFewRows && 2 * N * V <= most;
+    if constexpr (2 * N * V <= kMaxThread)
+        if (a.n.cols > per_warp * (one_warp ? 1 : kMaxWarps)) return launch_v<T, V, 2 * N>(a, q, s);
+    return launch<T, V, N>(a, q, (a.n.cols + per_warp - 1) / per_warp, s);
+}
+
+}  // namespace
+
+cudaError_t mafat_launch_block_norm(const MafatBlockNormArgs& a, bool bf16, int vec, MafatNormQuant quant, cudaStream_t s) {
+    // a warp has 128 channels at least: 4 accesses of one, 2 of two
+    if (bf16)
+        return vec >= 8   ? launch_v<__nv_bfloat16, 8, 1>(a, quant, s)
+               : vec >= 2 ? launch_v<__nv_bfloat16, 2, 2>(a, quant, s)
+                          : launch_v<__nv_bfloat16, 1, 4>(a, quant, s);
+    return vec >= 4   ? launch_v<float, 4, 1>(a, quant, s)
+           : vec >= 2 ? launch_v<float, 2, 2>(a, quant, s)
+                      : launch_v<float, 1, 4>(a, quant, s);
+}

@@ -1,0 +1,59 @@
+// Launch interface of the operators of a decoding step beside attention and norms: rotary positions and
+// adjusted logits (host and device visible).
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "attention.h"
+
+// One of a call's tensors and where it goes; strides in elements: sequence, token or place, head.
+struct MafatRotaryTensor {
+    const void* in;
+    void* out;                  // null: not given
+    int64_t in_sb, in_st, in_sh;
+    int64_t out_sb, out_st, out_sh;
+    int32_t heads;
+    int32_t groups;             // of heads, a CTA each
+    bool placed;                // it goes to the tokens' places
+};
+
+struct MafatRotaryArgs {
+    MafatRotaryTensor t[3];     // queries, keys, values (not rotated)
+    const uint64_t* turns;      // [rot / 2] fractions of a turn a position, times 2^64
+    const int32_t* positions;   // [tokens]
+    const int32_t* places;      // [tokens] (null: each token's own)
+    int64_t tokens;
+    MafatDiv n_q_div;
+    int32_t n_q, room;
+    int32_t dim, rot;
+    int32_t pairs;              // accesses of pairs a head
+    int32_t lanes;              // threads of a token: those, and accesses of the channels that stay
+    int32_t per_block;          // tokens of a block
+    MafatDiv lanes_div;
+    int32_t per_group;          // heads of a group
+    float magnitude;
+};
+// vec: channels of an access
+cudaError_t mafat_launch_rotary(const MafatRotaryArgs& a, bool bf16, bool interleaved, int vec, cudaStream_t s);
+
+struct MafatLogitsArgs {
+    const void* logits;
+    void* out;
+    int64_t in_s, out_s;        // of rows, in elements
+    const int32_t* tokens;      // [batch][room] (null: none)
+    const int32_t* lengths;     // null: room
+    const int32_t* prompt;      // null: 0
+    const float *repetition, *presence, *frequency;
+    const int32_t* drafts;      // [batch][n_q] (null: none)
+    const uint32_t* tree;       // null: a chain
+    int64_t tree_s;             // words of a request (0: all share one tree)
+    const int32_t* bias_ids;
+    const float* bias;
+    int64_t bias_s;             // entries of a request (0: all share them)
+    const uint32_t* masks;
+    const int32_t* mask_rows;
+    MafatDiv n_q_div;
+    int32_t n_q, vocab, room, n_bias, n_masks, tree_words, mask_words;
+};
+cudaError_t mafat_launch_logits(const MafatLogitsArgs& a, bool bf16, bool out_bf16, int64_t rows, cudaStream_t s);
+int mafat_logits_run();  // tokens of a row that a CTA has at least
