@@ -647,7 +647,7 @@ typedef struct {
     int32_t out_dtype;          /* of out: dtype or MAFAT_FP32 */
     int32_t batch, n_q;         /* 0: nothing is done */
     int32_t vocab;
-    int32_t room;               /* of a request's tokens; with n_q below 2^19 */
+    int32_t room;               /* of a request's tokens; with n_q below 2^18 */
     int32_t n_bias;             /* entries of a request, at most 4095 */
     int32_t n_masks;
     int32_t tree_shared, bias_shared;  /* not 0: one tree, one list of biases for all requests */

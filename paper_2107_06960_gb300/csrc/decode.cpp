@@ -359,7 +359,7 @@ mafat_status mafat_adjust_logits(const mafat_logits_desc* d, const void* logits,
     if (d->vocab < 1) return fail(MAFAT_EINVAL, "vocab must be positive");
     if (d->vocab > 1 << 30) return fail(MAFAT_EUNSUPPORTED, "too many tokens in the vocabulary");
     if (d->room < 0 || d->n_bias < 0 || d->n_masks < 0) return fail(MAFAT_EINVAL, "room, n_bias and n_masks must not be negative");
-    if ((int64_t)d->room + d->n_q >= 1 << 19) return fail(MAFAT_EUNSUPPORTED, "at most 2^19 - 1 tokens of a request");
+    if ((int64_t)d->room + d->n_q >= 1 << 18) return fail(MAFAT_EUNSUPPORTED, "at most 2^18 - 1 tokens of a request");
     if (d->n_bias > 4095) return fail(MAFAT_EUNSUPPORTED, "at most 4095 biases of a request");
     const int64_t rows = (int64_t)d->batch * d->n_q;
     if (rows == 0) {
@@ -415,14 +415,14 @@ mafat_status mafat_adjust_logits(const mafat_logits_desc* d, const void* logits,
     a.masks = masks;
     a.mask_rows = mask_rows;
     a.n_q = d->n_q;
-    a.n_q_div = MafatDiv((uint32_t)d->n_q);
+    a.pass = !in_place || masks != nullptr;
     a.vocab = d->vocab;
     a.room = d->room;
     a.n_bias = d->n_bias;
     a.n_masks = d->n_masks;
     a.tree_words = (int32_t)words;
     a.mask_words = (int32_t)mask_words;
-    const cudaError_t e = mafat_launch_logits(a, d->dtype == MAFAT_BF16, d->out_dtype == MAFAT_BF16, rows, (cudaStream_t)stream);
+    const cudaError_t e = mafat_launch_logits(a, d->dtype == MAFAT_BF16, d->out_dtype == MAFAT_BF16, d->batch, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "logits launch");
     return MAFAT_OK;
 }

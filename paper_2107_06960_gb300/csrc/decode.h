@@ -52,8 +52,11 @@ struct MafatLogitsArgs {
     int64_t bias_s;             // entries of a request (0: all share them)
     const uint32_t* masks;
     const int32_t* mask_rows;
-    MafatDiv n_q_div;
+    // set by the launch: runs of the vocabulary, groups of a request's rows; rows of a group
+    MafatDiv runs_div, groups_div;
+    int32_t rows_of_cta;
+    int32_t pass;               // 0: out is logits and nothing is masked: only what is noted is written
     int32_t n_q, vocab, room, n_bias, n_masks, tree_words, mask_words;
 };
-cudaError_t mafat_launch_logits(const MafatLogitsArgs& a, bool bf16, bool out_bf16, int64_t rows, cudaStream_t s);
+cudaError_t mafat_launch_logits(MafatLogitsArgs& a, bool bf16, bool out_bf16, int64_t batch, cudaStream_t s);
 int mafat_logits_run();  // tokens of a row that a CTA has at least

@@ -2,166 +2,339 @@
 //   x = logit;  said: x / r (x > 0) or x r;  x - f n - p [n > 0];  x + bias;  -inf where the grammar's mask forbids,
 // in fp32, rounded once.
 //
-// Bound by reading a row and writing it once.  A CTA has a run of a row's tokens.  Their logits are asked for first; while
-// they are on their way, the CTA goes over what the request has said and notes what falls into its run in a table in shared
-// memory, a word a token: how often the answer has it, whether the prompt does, and its bias.  The sums are of whole numbers, so
-// that their order does not matter.
+// Bound by reading a row and writing it once: nearly all logits pass as they are, or as the mask's -inf.  A CTA has a run of
+// the vocabulary for some rows of a request.  While the first row's logits are on their way it goes over what the request
+// has said, drafted and biased, and notes what falls into its run in a table in shared memory, a word a token, and each token
+// there once in a list; when all rows have passed, the tokens of the list are written again, a lane each.  (Common tokens are
+// neighbours in a vocabulary: in the pass over all of them their divisions fell to a few warps.)  The table's sums are
+// of whole numbers, so that their order does not matter.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
 #include "decode.h"
 #include "row_common.cuh"
 
+#include <algorithm>
+
 namespace {
 
-constexpr int kThreads = 256;
-// a token's word: entry of the biases (number + 1) | the prompt has it | how often the answer has it
+constexpr int kMostRows = 16;  // of a CTA
+constexpr int kAhead = 8;  // tokens of a history that a thread asks for at once
+// a token's word: entry of the biases (number + 1) | a draft has it | the prompt has it | how often the answer has it
 constexpr int kBiasShift = 20;
-constexpr uint32_t kPrompt = 1u << 19, kCount = kPrompt - 1u;
-
-struct Row {
-    float repetition, presence, frequency;
-    const float* bias;
-
-    __device__ __forceinline__ float adjust(float x, uint32_t word) const {
-        if (word == 0u) return x;
-        const uint32_t n = word & kCount;
-        if ((word & (kPrompt | kCount)) != 0u) x = x > 0.f ? x / repetition : x * repetition;
-        x -= frequency * (float)n;
-        if (n > 0u) x -= presence;
-        if (word >> kBiasShift != 0u) x += bias[(word >> kBiasShift) - 1u];
-        return x;
-    }
-};
-
-template <int V>
-__device__ __forceinline__ void store_all(float* p, const float (&v)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-}
-template <int V>
-__device__ __forceinline__ void store_all(__nv_bfloat16* p, const float (&v)[V]) { Vec<__nv_bfloat16, V>::store(p, v); }
+constexpr uint32_t kDraft = 1u << 19, kPrompt = 1u << 18, kCount = kPrompt - 1u;
 
 __device__ __forceinline__ float wide(float x) { return x; }
 __device__ __forceinline__ float wide(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void narrow(float* p, float x) { *p = x; }
 __device__ __forceinline__ void narrow(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// N accesses of 16 bytes a thread
-template <class T, class O, int N>
-__global__ void __launch_bounds__(kThreads) logits_kernel(const __grid_constant__ MafatLogitsArgs a, MafatDiv chunks) {
-    constexpr int V = 16 / sizeof(T), kRun = kThreads * N * V;
-    __shared__ __align__(16) uint32_t table[kRun];
-    const uint32_t row = chunks.div(blockIdx.x), chunk = blockIdx.x - row * chunks.d;
-    const uint32_t b = a.n_q_div.div(row), t = row - b * (uint32_t)a.n_q;
-    const T* in = (const T*)a.logits + (int64_t)row * a.in_s;
-    O* out = (O*)a.out + (int64_t)row * a.out_s;
-    // the run starts on 16 bytes of the input, before the row's first token where that is not there
-    const int first = (int)(chunk * kRun) - (int)((uintptr_t)in / sizeof(T) % V);
-    const int tid = threadIdx.x;
-    launch_wait();
-    launch_next();
-    Vec<T, V> v[N];
+// 16 bytes of logits on their way to `out`, 16 bytes at a time where `whole`; MASK: those without a bit in `allowed` as -inf
+template <bool MASK>
+__device__ __forceinline__ void put(float* out, const Vec<float, 4>& v, uint32_t allowed, bool whole) {
+    float x[4];
+    v.get(x);
+    if constexpr (MASK)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int e = first + (i * kThreads + tid) * V;
-        v[i].load(in + e, e >= 0 && e + V <= a.vocab);
+        for (int j = 0; j < 4; ++j)
+            if ((allowed >> j & 1u) == 0u) x[j] = -CUDART_INF_F;
+    if (whole) {
+        Vec<float, 4>::store(out, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[j] = x[j];
     }
+}
+template <bool MASK>
+__device__ __forceinline__ void put(float* out, const Vec<__nv_bfloat16, 8>& v, uint32_t allowed, bool whole) {
+    float x[8];
+    v.get(x);
 #pragma unroll
-    for (int i = tid; i < kRun / 4; i += kThreads) *reinterpret_cast<uint4*>(table + 4 * i) = make_uint4(0u, 0u, 0u, 0u);
-    __syncthreads();
-    Row r{1.f, 0.f, 0.f, a.bias ? a.bias + (int64_t)b * a.bias_s : nullptr};
-    if (a.repetition) r.repetition = a.repetition[b];
-    if (a.presence) r.presence = a.presence[b];
-    if (a.frequency) r.frequency = a.frequency[b];
-    if (a.bias_ids) {
-        const int32_t* ids = a.bias_ids + (int64_t)b * a.bias_s;
-        for (int i = tid; i < a.n_bias; i += kThreads) {
-            const uint32_t at = (uint32_t)ids[i] - (uint32_t)first;
-            if (at < (uint32_t)kRun) atomicMax(table + at, (uint32_t)(i + 1) << kBiasShift);  // the last of an id
+    for (int j = 0; j < 8; j += 4) {
+        Vec<float, 4> part;
+        part.u = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+        put<MASK>(out + j, part, allowed >> j, whole);
+    }
+}
+template <bool MASK>
+__device__ __forceinline__ void put(__nv_bfloat16* out, const Vec<__nv_bfloat16, 8>& v, uint32_t allowed, bool whole) {
+    uint32_t w[4] = {v.u.x, v.u.y, v.u.z, v.u.w};
+    if constexpr (MASK)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t two = allowed >> (2 * j), keep = (two & 1u) * 0xffffu + (two & 2u) * 0x7fff8000u;
+            w[j] = (w[j] & keep) | (0xff80ff80u & ~keep);  // -inf
         }
-        __syncthreads();
-    }
-    if (a.tokens) {
-        const int32_t* ids = a.tokens + (int64_t)b * a.room;
-        const int len = a.lengths ? min(max(a.lengths[b], 0), a.room) : a.room;
-        const int prompt = a.prompt ? a.prompt[b] : 0;
-#pragma unroll 4
-        for (int i = tid; i < len; i += kThreads) {
-            const uint32_t at = (uint32_t)ids[i] - (uint32_t)first;
-            if (at >= (uint32_t)kRun) continue;
-            if (i < prompt)
-                atomicOr(table + at, kPrompt);
-            else
-                atomicAdd(table + at, 1u);
-        }
-    }
-    if (a.drafts) {
-        const uint32_t* bits = a.tree ? a.tree + (int64_t)b * a.tree_s + (int64_t)t * a.tree_words : nullptr;
-        for (int i = tid; i < a.n_q; i += kThreads) {
-            const uint32_t at = (uint32_t)a.drafts[(int64_t)b * a.n_q + i] - (uint32_t)first;
-            const bool held = bits ? (bits[i / 32] >> (i % 32) & 1u) != 0u : i <= (int)t;
-            if (held && at < (uint32_t)kRun) atomicAdd(table + at, 1u);
-        }
-    }
-    const uint32_t* mask = nullptr;
-    if (a.masks) {
-        const int64_t m = a.mask_rows ? a.mask_rows[row] : (int64_t)row;
-        if (m >= 0 && m < a.n_masks) mask = a.masks + m * a.mask_words;
-    }
-    __syncthreads();
-    const bool whole = ((uintptr_t)(out + first) & 15u) == 0u;  // the output can be written 16 bytes at a time
+    if (whole) {
+        *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int at = (i * kThreads + tid) * V, e = first + at;
-        if (e >= a.vocab) break;
-        if (e >= 0 && e + V <= a.vocab) {
-            uint32_t allowed = 0xffffffffu;
-            if (mask) {
-                const uint32_t lo = mask[e >> 5], hi = (e & 31) + V > 32 ? mask[(e >> 5) + 1] : 0u;
-                allowed = __funnelshift_r(lo, hi, (uint32_t)e & 31u);
-            }
-            float x[V];
-            v[i].get(x);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                x[j] = r.adjust(x[j], table[at + j]);
-                if ((allowed >> j & 1u) == 0u) x[j] = -CUDART_INF_F;
-            }
-            if (whole) {
-                store_all<V>(out + e, x);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) narrow(out + e + j, x[j]);
-            }
-        } else {
-            for (int j = 0; j < V; ++j) {
-                const int k = e + j;
-                if (k < 0 || k >= a.vocab) continue;
-                float x = r.adjust(wide(in[k]), table[at + j]);
-                if (mask && (mask[k >> 5] >> (k & 31) & 1u) == 0u) x = -CUDART_INF_F;
-                narrow(out + k, x);
-            }
+        for (int j = 0; j < 4; ++j) {
+            out[2 * j] = __ushort_as_bfloat16((unsigned short)w[j]);
+            out[2 * j + 1] = __ushort_as_bfloat16((unsigned short)(w[j] >> 16));
         }
     }
 }
 
-template <class T, class O, int N>
-cudaError_t launch(const MafatLogitsArgs& a, int64_t rows, cudaStream_t s) {
-    constexpr int V = 16 / sizeof(T), kRun = kThreads * N * V;
-    const int64_t chunks = ((int64_t)a.vocab + V - 1 + kRun - 1) / kRun;  // a row may start V - 1 tokens late
-    return mafat_launch_overlapped(logits_kernel<T, O, N>, (unsigned)(rows * chunks), kThreads, 0, s, a, MafatDiv((uint32_t)chunks));
+__device__ __forceinline__ bool allows(const uint32_t* mask, int token) {
+    return !mask || (mask[token >> 5] >> (token & 31) & 1u) != 0u;
 }
+
+// A CTA's run of a row: THREADS threads of N accesses of 16 bytes.  It starts on 16 bytes of the input, before the row's first
+// token where that does not.
+template <class T, int THREADS, int N>
+struct Run {
+    static constexpr int V = 16 / sizeof(T), kTokens = THREADS * N * V, kStep = THREADS * V;
+    static_assert(kTokens <= 65536 && kStep % 32 == 0, "places in 16 bits; a thread's accesses begin at one bit of a word");
+    int first, mine, vocab;  // the run's first token, that of the thread's first access
+    bool inner;              // all of the run are the row's
+    __device__ __forceinline__ Run(const MafatLogitsArgs& a, int run, const T* in)
+        : first(run * kTokens - (int)((uintptr_t)in / sizeof(T) % V)), mine(first + (int)threadIdx.x * V), vocab(a.vocab),
+          inner(first >= 0 && first + kTokens <= a.vocab) {}
+    __device__ __forceinline__ bool inside(int i) const { return inner || (mine + i * kStep >= 0 && mine + i * kStep + V <= vocab); }
+    __device__ __forceinline__ void load(const T* in, Vec<T, V> (&v)[N]) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i].load(in + mine + i * kStep, inside(i));
+    }
+    // the words with the thread's bits of a mask; from the second on where an access can pass a word's end
+    struct Bits {
+        uint32_t lo[N], hi[N];
+    };
+    __device__ __forceinline__ void look(const uint32_t* mask, Bits& bits) const {
+        const uint32_t* words = mask + (mine >> 5);
+        const bool two = (mine & 31) + V > 32;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool on = mask && inside(i);
+            bits.lo[i] = on ? words[i * (kStep / 32)] : 0u;
+            bits.hi[i] = on && two ? words[i * (kStep / 32) + 1] : 0u;
+        }
+    }
+    template <bool MASK, class O>
+    __device__ __forceinline__ void pass(const T* in, O* out, const uint32_t* mask, const Vec<T, V> (&v)[N], const Bits& bits) const {
+        const bool whole = ((uintptr_t)(out + first) & 15u) == 0u;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = mine + i * kStep;
+            if (inside(i)) {
+                put<MASK>(out + e, v[i], MASK ? __funnelshift_r(bits.lo[i], bits.hi[i], (uint32_t)mine & 31u) : 0u, whole);
+            } else if (e < vocab) {
+#pragma unroll 1
+                for (int k = max(e, 0); k < min(e + V, vocab); ++k) narrow(out + k, !MASK || allows(mask, k) ? wide(in[k]) : -CUDART_INF_F);
+            }
+        }
+    }
+};
+
+template <class T, class O, int THREADS, int N, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_constant__ MafatLogitsArgs a) {
+    using S = Run<T, THREADS, N>;
+    extern __shared__ __align__(16) uint32_t table[];
+    uint16_t* list = (uint16_t*)(table + S::kTokens);
+    __shared__ int listed, masks[kMostRows];
+    const int tid = threadIdx.x;
+    const uint32_t i0 = a.runs_div.div(blockIdx.x), b = a.groups_div.div(i0);
+    const int t0 = (int)(i0 - b * a.groups_div.d) * a.rows_of_cta, rows = min(a.rows_of_cta, a.n_q - t0);
+    const int64_t row0 = (int64_t)b * a.n_q + t0;
+    const T* in = (const T*)a.logits + row0 * a.in_s;
+    O* out = (O*)a.out + row0 * a.out_s;
+    const S s(a, (int)(blockIdx.x - i0 * a.runs_div.d), in);
+    launch_wait();
+    launch_next();
+    Vec<T, S::V> v[N];
+    if (a.pass) s.load(in, v);
+    // what the CTA needs of the request is asked for together: the first of each list before the first barrier
+    const bool any = a.tokens || a.drafts || a.bias_ids;
+    const int32_t* bias_ids = a.bias_ids + (int64_t)b * a.bias_s;
+    const int32_t* drafts = a.drafts + (int64_t)b * a.n_q;
+    int32_t said[kAhead];
+    auto look = [&](int from) {  // up to the room, so that the length is not waited for
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = from + i * THREADS + tid;
+            said[i] = a.tokens && k < a.room ? a.tokens[(int64_t)b * a.room + k] : -1;
+        }
+    };
+    look(0);
+    const int32_t bias_id = a.bias_ids && tid < a.n_bias ? bias_ids[tid] : -1, draft = a.drafts && tid < a.n_q ? drafts[tid] : -1;
+    int len = 0, prompt = 0;
+    if (a.tokens) {
+        len = a.lengths ? min(max(a.lengths[b], 0), a.room) : a.room;
+        prompt = a.prompt ? a.prompt[b] : 0;
+    }
+    if (tid < rows) {  // the number of each row's mask, or -1
+        int64_t m = -1;
+        if (a.masks) m = a.mask_rows ? a.mask_rows[row0 + tid] : row0 + tid;
+        masks[tid] = m < a.n_masks ? (int)m : -1;
+    }
+    if (any) {
+#pragma unroll
+        for (int i = tid * 4; i < S::kTokens; i += THREADS * 4) *reinterpret_cast<uint4*>(table + i) = make_uint4(0u, 0u, 0u, 0u);
+        if (tid == 0) listed = 0;
+    }
+    __syncthreads();
+    auto mask_of = [&](int t) -> const uint32_t* { return masks[t] < 0 ? nullptr : a.masks + (int64_t)masks[t] * a.mask_words; };
+    typename S::Bits bits;
+    s.look(a.pass ? mask_of(0) : nullptr, bits);
+    if (any) {
+        auto place = [&](int32_t id) { return (uint32_t)id - (uint32_t)s.first; };  // kTokens and more: elsewhere
+        auto note = [&](uint32_t at, uint32_t was) {
+            if (was == 0u) list[atomicAdd(&listed, 1)] = (uint16_t)at;
+        };
+        if (a.bias_ids) {
+            for (int i = tid; i < a.n_bias; i += THREADS) {
+                const uint32_t at = place(i == tid ? bias_id : bias_ids[i]);
+                if (at < (uint32_t)S::kTokens) note(at, atomicMax(table + at, (uint32_t)(i + 1) << kBiasShift));  // the last of an id
+            }
+            __syncthreads();
+        }
+        for (int from = 0; from < len; from += kAhead * THREADS) {
+            if (from > 0) look(from);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int k = from + i * THREADS + tid;
+                const uint32_t at = place(said[i]);
+                if (k < len && at < (uint32_t)S::kTokens)
+                    note(at, k < prompt ? atomicOr(table + at, kPrompt) : atomicAdd(table + at, 1u));
+            }
+        }
+        if (a.drafts)
+            for (int i = tid; i < a.n_q; i += THREADS) {
+                const uint32_t at = place(i == tid ? draft : drafts[i]);
+                if (at < (uint32_t)S::kTokens) note(at, atomicOr(table + at, kDraft));
+            }
+    }
+    // The noted tokens of all rows, kTogether of a thread at a time.  The logits of the first ones are asked for before
+    // the rows pass.
+    constexpr int kTogether = N < 4 ? N : 4;
+    struct Patch {
+        float x[kTogether];
+        int at[kTogether], row[kTogether];  // row: negative where there is nothing to write
+    } patch;
+    int t = 0, i = tid, n = 0;
+    auto fetch = [&]() {
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            while (i >= n && t < rows) i -= n, ++t;
+            patch.row[u] = -1;
+            if (t < rows) {
+                patch.at[u] = list[i];
+                const int token = s.first + patch.at[u];
+                // an id may be past the row's ends, and still in the run
+                if (token >= 0 && token < a.vocab) {
+                    patch.x[u] = wide(in[t * a.in_s + token]);
+                    if (allows(mask_of(t), token)) patch.row[u] = t;
+                }
+            }
+            i += THREADS;
+        }
+    };
+    if (any) {
+        __syncthreads();  // table and list are there
+        n = listed;
+        if (n == 0) t = rows;
+        fetch();
+    }
+    if (a.pass) {
+#pragma unroll 1
+        for (int r = 0;; ++r) {
+            const T* from = in + r * a.in_s;
+            O* to = out + r * a.out_s;
+            Vec<T, S::V> next[N];
+            typename S::Bits next_bits;
+            if (r + 1 < rows) {
+                s.load(from + a.in_s, next);
+                s.look(mask_of(r + 1), next_bits);
+            }
+            const uint32_t* mask = mask_of(r);
+            if (mask)
+                s.template pass<true>(from, to, mask, v, bits);
+            else
+                s.template pass<false>(from, to, mask, v, bits);
+            if (r + 1 == rows) break;
+            bits = next_bits;
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = next[k];
+        }
+    }
+    if (n == 0) return;
+    const float repetition = a.repetition ? a.repetition[b] : 1.f, presence = a.presence ? a.presence[b] : 0.f,
+                frequency = a.frequency ? a.frequency[b] : 0.f;
+    const float* bias = a.bias + (int64_t)b * a.bias_s;
+    const uint32_t* tree = a.tree + (int64_t)b * a.tree_s;
+    __syncthreads();  // what is written over is there
+#pragma unroll 1
+    for (;;) {
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const int row = patch.row[u];
+            if (row < 0) continue;
+            const int token = s.first + patch.at[u];
+            const uint32_t word = table[patch.at[u]];
+            uint32_t count = word & kCount;
+            if (word & kDraft) {  // those that the row's bits name, or up to its own
+                const uint32_t* way = a.tree ? tree + (int64_t)(t0 + row) * a.tree_words : nullptr;
+                const int end = way ? a.n_q : t0 + row + 1;
+                for (int j = 0; j < end; ++j) count += drafts[j] == token && (!way || (way[j / 32] >> (j % 32) & 1u));
+            }
+            float y = patch.x[u];
+            if (count > 0u || (word & kPrompt)) y = y > 0.f ? y / repetition : y * repetition;
+            y -= frequency * (float)count;
+            if (count > 0u) y -= presence;
+            if (word >> kBiasShift) y += bias[(word >> kBiasShift) - 1u];
+            narrow(out + row * a.out_s + token, y);
+        }
+        if (t >= rows) break;
+        fetch();
+    }
+}
+
+bool noted(const MafatLogitsArgs& a) { return a.tokens || a.drafts || a.bias_ids; }
+
+// A request's rows are shared by as many CTAs as leave `least` in all, so that the table serves several rows.
+template <class T, class O, int THREADS, int N, int BLOCKS>
+cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_t s) {
+    using S = Run<T, THREADS, N>;
+    // rows that start alike share a CTA; a row may start V - 1 tokens late
+    const bool alike = a.in_s * sizeof(T) % 16 == 0;
+    const int late = alike && (uintptr_t)a.logits % 16 == 0 ? 0 : S::V - 1;
+    const int64_t runs = ((int64_t)a.vocab + late + S::kTokens - 1) / S::kTokens;
+    int rows = alike ? kMostRows : 1;
+    while (rows > 1 && (rows >= 2 * a.n_q || batch * ((a.n_q + rows - 1) / rows) * runs < least)) rows /= 2;
+    const int64_t groups = (a.n_q + rows - 1) / rows;
+    a.rows_of_cta = rows;
+    a.runs_div = MafatDiv((uint32_t)runs);
+    a.groups_div = MafatDiv((uint32_t)groups);
+    const int64_t listed = (a.tokens ? a.room : 0) + (int64_t)(a.drafts ? a.n_q : 0) + (a.bias_ids ? a.n_bias : 0);
+    const size_t smem = noted(a) ? S::kTokens * 4 + (std::min<int64_t>(S::kTokens, listed) * 2 + 15) / 16 * 16 : 0;
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, O, THREADS, N, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kTokens * 6);
+        if (e != cudaSuccess) return e;
+    }
+    return mafat_launch_overlapped(logits_kernel<T, O, THREADS, N, BLOCKS>, (unsigned)(batch * groups * runs), THREADS, smem, s, a);
+}
+
+// Each CTA goes over the whole history: the longer that is, the more threads it has, and the more tokens where there are many
+// logits.  256, 512 and 1024 threads (1024 with one access each, with four), in us:
+//   64 x 16 rows of 131072 bf16, 2048 said           105, 122, 140, 128      16 rows of 32000, 512 said     3.6, 4.0, 4.7, 9.4
+//   102 rows of 111872 bf16, 6305 said              34.8, 33.3, 49.1, 36.2   4 x 27 of 8892 fp32, 5139      13.6, 12.5, 13.0, 9.7
+//   7 rows of 50001 fp32, 20000 said                20.3, 13.6, 10.4, 15.8   5 x 24 of 40256 bf16, 16270    39.5, 31.5, 25.1, 37.9
+//   95 rows of 128890 fp32, 21842 said               104, 89, 117, 59        40 x 36 of 21617 bf16, 8686    159, 151, 207, 145
 template <class T, class O>
-cudaError_t launch_n(const MafatLogitsArgs& a, int64_t rows, cudaStream_t s) {
-    return launch<T, O, 4>(a, rows, s);
+cudaError_t launch_all(MafatLogitsArgs& a, int64_t batch, cudaStream_t s) {
+    constexpr int kSms = 152;
+    const int said = a.tokens ? a.room : 0;
+    if (said <= 2048) return launch<T, O, 256, 2, 5>(a, batch, 4 * 5 * kSms, s);
+    if (said <= 8192) return launch<T, O, 512, 2, 2>(a, batch, 4 * kSms, s);
+    if (batch * a.n_q * a.vocab * (int64_t)sizeof(T) <= 16 << 20) return launch<T, O, 1024, 1, 1>(a, batch, kSms * 9 / 10, s);
+    return launch<T, O, 1024, 4, 1>(a, batch, 4 * kSms, s);
 }
 
 }  // namespace
 
-int mafat_logits_run() { return kThreads * 4; }
+int mafat_logits_run() { return 256 * 2 * 4; }
 
-cudaError_t mafat_launch_logits(const MafatLogitsArgs& a, bool bf16, bool out_bf16, int64_t rows, cudaStream_t s) {
-    if (!bf16) return launch_n<float, float>(a, rows, s);
-    return out_bf16 ? launch_n<__nv_bfloat16, __nv_bfloat16>(a, rows, s) : launch_n<__nv_bfloat16, float>(a, rows, s);
+cudaError_t mafat_launch_logits(MafatLogitsArgs& a, bool bf16, bool out_bf16, int64_t batch, cudaStream_t s) {
+    if (!bf16) return launch_all<float, float>(a, batch, s);
+    return out_bf16 ? launch_all<__nv_bfloat16, __nv_bfloat16>(a, batch, s) : launch_all<__nv_bfloat16, float>(a, batch, s);
 }

@@ -183,7 +183,7 @@ def _logits(mf, at=None, null=(), **change):
 
 @pytest.mark.parametrize("change,status", [
     (dict(struct_size=1), "EINVAL"), (dict(dtype=2), "EINVAL"), (dict(out_dtype=0), "EINVAL"), (dict(batch=-1), "EINVAL"), (dict(n_q=-1), "EINVAL"),
-    (dict(vocab=0), "EINVAL"), (dict(vocab=(1 << 30) + 1), "EUNSUPPORTED"), (dict(room=-1), "EINVAL"), (dict(room=(1 << 19) - 3), "EUNSUPPORTED"),
+    (dict(vocab=0), "EINVAL"), (dict(vocab=(1 << 30) + 1), "EUNSUPPORTED"), (dict(room=-1), "EINVAL"), (dict(room=(1 << 18) - 3), "EUNSUPPORTED"),
     (dict(n_bias=-1), "EINVAL"), (dict(n_bias=4096), "EUNSUPPORTED"), (dict(n_masks=-1), "EINVAL"), (dict(batch=1 << 30), "EUNSUPPORTED"),
     (dict(logits_stride=999), "EINVAL"), (dict(out_stride=-1000), "EINVAL"), (dict(out_stride=1 << 31), "EUNSUPPORTED"),
     (dict(null=("logits",)), "EINVAL"), (dict(null=("out",)), "EINVAL"), (dict(null=("bias",)), "EINVAL"), (dict(null=("bias_ids",)), "EINVAL"),
