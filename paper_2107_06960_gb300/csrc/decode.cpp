@@ -23,7 +23,6 @@ namespace {
 
 using namespace mafat_lm;
 
-constexpr int kMaxRotaryDim = 256;
 constexpr double kTurn = 6.283185307179586476925286766559;
 
 // [rot / 2] radians a position
@@ -171,8 +170,8 @@ mafat_status mafat_rotary_plan(const mafat_rotary_desc* d, mafat_rotary_t** out)
     if (d->struct_size != (int32_t)sizeof(mafat_rotary_desc)) return fail(MAFAT_EINVAL, "struct_size is not the descriptor's");
     if (d->dtype != MAFAT_BF16 && d->dtype != MAFAT_FP32) return fail(MAFAT_EINVAL, "dtype must be MAFAT_BF16 or MAFAT_FP32");
     if (d->head_dim < 1) return fail(MAFAT_EINVAL, "head_dim must be positive");
-    if (d->head_dim > kMaxRotaryDim || d->head_dim % 8 != 0)
-        return fail(MAFAT_EUNSUPPORTED, "head_dim must be a multiple of 8 and at most %d", kMaxRotaryDim);
+    if (d->head_dim > mafat_rotary_most_dim() || d->head_dim % 8 != 0)
+        return fail(MAFAT_EUNSUPPORTED, "head_dim must be a multiple of 8 and at most %d", mafat_rotary_most_dim());
     const int32_t rot = d->rot_dim == 0 ? d->head_dim : d->rot_dim;
     if (rot < 2 || rot > d->head_dim || rot % 2 != 0) return fail(MAFAT_EINVAL, "rot_dim must be even, and at most head_dim");
     if (d->scaling < MAFAT_ROTARY_PLAIN || d->scaling > MAFAT_ROTARY_BLEND) return fail(MAFAT_EINVAL, "unknown scaling");
@@ -300,13 +299,6 @@ mafat_status mafat_rotary_run(const mafat_rotary_t* p, const mafat_rotary_call* 
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
     if (dev != p->device) return fail(MAFAT_EINVAL, "the current device is not the plan's");
     MafatRotaryArgs a{};
-    // an access is inside the rotated channels, and inside each half of them
-    const int vec = lowest_bit(p->interleaved ? p->rot : p->rot / 2, esz == 2 ? 8 : 4);
-    a.pairs = p->interleaved ? (p->rot + 2 * vec - 1) / (2 * vec) : p->rot / 2 / vec;
-    a.lanes = a.pairs + (p->dim - p->rot) / vec;
-    a.per_block = 256 / a.lanes;
-    a.lanes_div = MafatDiv((uint32_t)a.lanes);
-    a.per_group = 8;
     for (int i = 0; i < 3; ++i) {
         if (!in[i]) continue;
         MafatRotaryTensor& t = a.t[i];
@@ -315,8 +307,6 @@ mafat_status mafat_rotary_run(const mafat_rotary_t* p, const mafat_rotary_call* 
         t.in_sb = st[i][0]; t.in_st = st[i][1]; t.in_sh = st[i][2];
         t.out_sb = st_out[i][0]; t.out_st = st_out[i][1]; t.out_sh = st_out[i][2];
         t.heads = (int32_t)n[i][2];
-        t.groups = (t.heads + a.per_group - 1) / a.per_group;
-        t.placed = i > 0;
     }
     a.turns = p->turns;
     a.positions = positions;
@@ -328,7 +318,7 @@ mafat_status mafat_rotary_run(const mafat_rotary_t* p, const mafat_rotary_call* 
     a.dim = p->dim;
     a.rot = p->rot;
     a.magnitude = (float)p->magnitude;
-    e = mafat_launch_rotary(a, p->dtype == MAFAT_BF16, p->interleaved, vec, (cudaStream_t)stream);
+    e = mafat_launch_rotary(a, p->dtype == MAFAT_BF16, p->interleaved, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "rotary launch");
     return MAFAT_OK;
 }

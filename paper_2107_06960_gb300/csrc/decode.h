@@ -9,16 +9,14 @@
 // One of a call's tensors and where it goes; strides in elements: sequence, token or place, head.
 struct MafatRotaryTensor {
     const void* in;
-    void* out;                  // null: not given
+    void* out;
     int64_t in_sb, in_st, in_sh;
     int64_t out_sb, out_st, out_sh;
-    int32_t heads;
-    int32_t groups;             // of heads, a CTA each
-    bool placed;                // it goes to the tokens' places
+    int32_t heads;              // 0: not given
 };
 
 struct MafatRotaryArgs {
-    MafatRotaryTensor t[3];     // queries, keys, values (not rotated)
+    MafatRotaryTensor t[3];     // queries; keys and values, which go to the tokens' places
     const uint64_t* turns;      // [rot / 2] fractions of a turn a position, times 2^64
     const int32_t* positions;   // [tokens]
     const int32_t* places;      // [tokens] (null: each token's own)
@@ -26,15 +24,13 @@ struct MafatRotaryArgs {
     MafatDiv n_q_div;
     int32_t n_q, room;
     int32_t dim, rot;
-    int32_t pairs;              // accesses of pairs a head
-    int32_t lanes;              // threads of a token: those, and accesses of the channels that stay
-    int32_t per_block;          // tokens of a block
-    MafatDiv lanes_div;
-    int32_t per_group;          // heads of a group
     float magnitude;
+    // set by the launch: items of a head (pairs, then channels that stay), tokens of a CTA, heads that it has at a time
+    int32_t pairs, lanes, per_block, steps;
+    MafatDiv lanes_div, steps_div, half_div;
 };
-// vec: channels of an access
-cudaError_t mafat_launch_rotary(const MafatRotaryArgs& a, bool bf16, bool interleaved, int vec, cudaStream_t s);
+int mafat_rotary_most_dim();
+cudaError_t mafat_launch_rotary(MafatRotaryArgs& a, bool bf16, bool interleaved, cudaStream_t s);
 
 struct MafatLogitsArgs {
     const void* logits;

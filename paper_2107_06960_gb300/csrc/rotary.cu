@@ -4,9 +4,15 @@
 //
 // Bound by reading and writing queries, keys and values once.  A frequency is a 64-bit fraction of a turn: its product with the
 // position, modulo 2^64, is the fraction past whole turns, to 2^-33 of a turn whatever the position; sine and
-// cosine are taken of that fraction in fp32, on -1/2 .. 1/2.  A thread has V channels and their partners of a token, and turns
-// those of one head after another by the same sines and cosines.
+// cosine are taken of that fraction in fp32, on -1/2 .. 1/2.  A CTA has a few tokens with all their heads: their sines and
+// cosines are made once, while the first channels are on their way.  A thread has the same pairs of one head after another.
+//
+// 8 x 2048 tokens of 32 query and 8 key heads of 128 channels, bf16, with their values: 62.8 us or 6.4 TB/s; a form whose
+// threads made the sines of their own pairs before they asked for channels took 77.6.  64 tokens of as many heads: 2.4 us,
+// a launch and two round trips (the tokens' positions, then their angles' table, beside the channels).
 #include <cuda_bf16.h>
+
+#include <algorithm>
 
 #include "decode.h"
 #include "row_common.cuh"
@@ -14,72 +20,103 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTogether = 4;  // heads whose loads are on their way together
+constexpr int kMostTokens = 16;  // of a CTA
+constexpr int kMostPairs = 128;  // of a head
+constexpr int kTogether = 4;     // accesses of pairs of a thread that are on their way together
 
-// V channels that are copied as they are
-template <class T, int V>
-__device__ __forceinline__ void copy(T* out, const T* in) {
-    struct alignas(sizeof(T) * V) Piece {
-        T v[V];
-    };
-    *reinterpret_cast<Piece*>(out) = *reinterpret_cast<const Piece*>(in);
-}
+// 16 bytes that are copied as they are
+template <class T>
+struct alignas(16) Piece {
+    T v[16 / sizeof(T)];
+};
 
+// V channels an access; an item is two accesses, of pairs of channels or of neighbours that stay.
 template <class T, int V, bool INTERLEAVED>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ MafatRotaryArgs a) {
-    // the block's tensor and group of heads
-    int group = blockIdx.y, which = 0;
-    while (group >= a.t[which].groups) group -= a.t[which++].groups;
-    const MafatRotaryTensor& x = a.t[which];
-    const int slot = (int)a.lanes_div.div(threadIdx.x), lane = (int)threadIdx.x - slot * a.lanes;
-    const int64_t token = (int64_t)blockIdx.x * a.per_block + slot;
-    if (slot >= a.per_block || token >= a.tokens) return;
-    const int64_t b = a.n_q_div.div((uint32_t)token), t = token - b * a.n_q;
+__global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ MafatRotaryArgs a) {
+    __shared__ __align__(16) float cosines[kMostTokens * kMostPairs], sines[kMostTokens * kMostPairs];
+    const int tid = threadIdx.x, half = a.rot / 2;
+    const int64_t token0 = (int64_t)blockIdx.x * a.per_block;
+    const int tokens = (int)min((int64_t)a.per_block, a.tokens - token0);
+    // the thread's token, first head and item; threads past the last token have none
+    const int row = (int)a.lanes_div.div((uint32_t)tid), lane = tid - row * a.lanes;
+    const int slot = (int)a.steps_div.div((uint32_t)row), head0 = row - slot * a.steps;
+    const bool mine = slot < tokens;
+    const uint32_t token = (uint32_t)token0 + (uint32_t)(mine ? slot : 0);
+    const int64_t b = a.n_q_div.div(token), t = (int64_t)token - b * a.n_q;
     launch_wait();
     launch_next();
-    const int64_t place = x.placed && a.places ? a.places[token] : t;
-    if (place < 0 || (x.placed && place >= a.room)) return;
-    const T* in = (const T*)x.in + b * x.in_sb + t * x.in_st;
-    T* out = (T*)x.out + b * x.out_sb + place * x.out_st;
-    const int h0 = group * a.per_group, h1 = min(h0 + a.per_group, x.heads);
-    if (which == 2) {  // values, 16 bytes at a time
-        constexpr int kWide = 16 / sizeof(T);
-        for (int h = h0; h < h1; ++h)
-            for (int c = lane * kWide; c < a.dim; c += a.lanes * kWide) copy<T, kWide>(out + h * x.out_sh + c, in + h * x.in_sh + c);
-        return;
-    }
-    if (lane >= a.pairs) {  // channels that stay
-        const int c = a.rot + (lane - a.pairs) * V;
-        for (int h = h0; h < h1; ++h) copy<T, V>(out + h * x.out_sh + c, in + h * x.in_sh + c);
-        return;
-    }
-    // an access has V pairs' first channels, and V on their second ones; neighbours: V / 2 pairs each
-    const int c0 = INTERLEAVED ? lane * 2 * V : lane * V, c1 = INTERLEAVED ? c0 + V : c0 + a.rot / 2;
-    float cs[V], sn[V];
-    const int64_t position = a.positions[token];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int i = lane * V + j;
-        // past the last pair where an odd number of them is interleaved
-        const uint64_t turn = !INTERLEAVED || i < a.rot / 2 ? a.turns[i] * (uint64_t)position : 0u;
-        const int32_t top = (int32_t)((turn + 0x80000000u) >> 32);  // of half turns 2^-31
-        sincospif((float)top * 0x1p-31f, &sn[j], &cs[j]);
-        sn[j] *= a.magnitude;
-        cs[j] *= a.magnitude;
-    }
-    const bool second = !INTERLEAVED || c1 < a.rot;
-#pragma unroll 1
-    for (int h = h0; h < h1; h += kTogether) {
-        Vec<T, V> va[kTogether], vb[kTogether];
+    int64_t place = t;
+    if (a.places) place = a.places[token];
+    const bool kept = place >= 0 && place < a.room;  // there is a place for the key and the value
+    const MafatRotaryTensor &tq = a.t[0], &tk = a.t[1], &tv = a.t[2];
+    const int heads = mine ? tq.heads + tk.heads : 0;
+    const bool turned = lane < a.pairs;
+    const int c0 = !turned ? a.rot + (lane - a.pairs) * 2 * V : INTERLEAVED ? lane * 2 * V : lane * V;
+    const int c1 = turned && !INTERLEAVED ? c0 + half : c0 + V;
+    // of an odd number of neighbouring accesses the last item has one
+    const bool two = c1 < (turned ? a.rot : a.dim);
+    const T* q_in = (const T*)tq.in + b * tq.in_sb + t * tq.in_st;
+    const T* k_in = (const T*)tk.in + b * tk.in_sb + t * tk.in_st;
+    Vec<T, V> va[kTogether], vb[kTogether];
+    auto load = [&](int h0) {
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
-            const T* p = in + min(h + u, h1 - 1) * x.in_sh;
-            va[u].load(p + c0, h + u < h1);
-            vb[u].load(p + c1, h + u < h1 && second);
+            const int h = h0 + u * a.steps;
+            const T* in = h < tq.heads ? q_in + h * tq.in_sh : k_in + (h - tq.heads) * tk.in_sh;
+            va[u].load(in + c0, h < heads);
+            vb[u].load(in + c1, h < heads && two);
         }
+    };
+    load(head0);
+    for (int i = tid; i < tokens * half; i += kThreads) {
+        const int of = (int)a.half_div.div((uint32_t)i), pair = i - of * half;
+        const uint64_t turn = a.turns[pair] * (uint64_t)(int64_t)a.positions[token0 + of];
+        const int32_t top = (int32_t)((turn + 0x80000000u) >> 32);  // of half turns 2^-31
+        float s, c;
+        sincospif((float)top * 0x1p-31f, &s, &c);
+        cosines[of * kMostPairs + pair] = c * a.magnitude;
+        sines[of * kMostPairs + pair] = s * a.magnitude;
+    }
+    if (mine && kept && tv.heads > 0) {  // values, 16 bytes at a time
+        constexpr int kWide = 16 / sizeof(T);
+        const T* in = (const T*)tv.in + b * tv.in_sb + t * tv.in_st;
+        T* out = (T*)tv.out + b * tv.out_sb + place * tv.out_st;
+#pragma unroll 1
+        for (int h = head0; h < tv.heads; h += a.steps)
+#pragma unroll 1
+            for (int d = lane * kWide; d < a.dim; d += a.lanes * kWide * 2) {
+                const int e = d + a.lanes * kWide;
+                const Piece<T> x = *reinterpret_cast<const Piece<T>*>(in + h * tv.in_sh + d);
+                Piece<T> y;
+                if (e < a.dim) y = *reinterpret_cast<const Piece<T>*>(in + h * tv.in_sh + e);
+                *reinterpret_cast<Piece<T>*>(out + h * tv.out_sh + d) = x;
+                if (e < a.dim) *reinterpret_cast<Piece<T>*>(out + h * tv.out_sh + e) = y;
+            }
+    }
+    __syncthreads();  // sines and cosines are there
+    if (head0 >= heads) return;
+    float cs[V], sn[V];
+    if (turned) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {  // past the last pair of an item with one access: not used
+            cs[j] = cosines[slot * kMostPairs + lane * V + j];
+            sn[j] = sines[slot * kMostPairs + lane * V + j];
+        }
+    }
+    T* q_out = (T*)tq.out + b * tq.out_sb + t * tq.out_st;
+    T* k_out = (T*)tk.out + b * tk.out_sb + place * tk.out_st;
+#pragma unroll 1
+    for (int h0 = head0;;) {
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
-            if (h + u >= h1) break;
+            const int h = h0 + u * a.steps;
+            if (h >= heads || (h >= tq.heads && !kept)) break;
+            T* out = h < tq.heads ? q_out + h * tq.out_sh : k_out + (h - tq.heads) * tk.out_sh;
+            if (!turned) {
+                *reinterpret_cast<Vec<T, V>*>(out + c0) = va[u];
+                if (two) *reinterpret_cast<Vec<T, V>*>(out + c1) = vb[u];
+                continue;
+            }
             float p[V], q[V], y[V], z[V];
             va[u].get(p);
             vb[u].get(q);
@@ -99,17 +136,18 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
                     z[j] = p[j] * sn[j] + q[j] * cs[j];
                 }
             }
-            T* o = out + (h + u) * x.out_sh;
-            Vec<T, V>::store(o + c0, y);
-            if (second) Vec<T, V>::store(o + c1, z);
+            Vec<T, V>::store(out + c0, y);
+            if (two) Vec<T, V>::store(out + c1, z);
         }
+        h0 += kTogether * a.steps;
+        if (h0 >= heads) break;
+        load(h0);
     }
 }
 
 template <class T, int V, bool INTERLEAVED>
 cudaError_t launch(const MafatRotaryArgs& a, cudaStream_t s) {
-    const dim3 grid((unsigned)((a.tokens + a.per_block - 1) / a.per_block), a.t[0].groups + a.t[1].groups + a.t[2].groups);
-    return mafat_launch_overlapped(rotary_kernel<T, V, INTERLEAVED>, grid, kThreads, 0, s, a);
+    return mafat_launch_overlapped(rotary_kernel<T, V, INTERLEAVED>, (unsigned)((a.tokens + a.per_block - 1) / a.per_block), kThreads, 0, s, a);
 }
 template <class T, bool INTERLEAVED>
 cudaError_t launch_v(const MafatRotaryArgs& a, int vec, cudaStream_t s) {
@@ -122,7 +160,23 @@ cudaError_t launch_v(const MafatRotaryArgs& a, int vec, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t mafat_launch_rotary(const MafatRotaryArgs& a, bool bf16, bool interleaved, int vec, cudaStream_t s) {
+int mafat_rotary_most_dim() { return 2 * kMostPairs; }
+
+cudaError_t mafat_launch_rotary(MafatRotaryArgs& a, bool bf16, bool interleaved, cudaStream_t s) {
+    // an access is inside the rotated channels, and inside each half of them
+    const int run = interleaved ? a.rot : a.rot / 2, vec = std::min(run & -run, bf16 ? 8 : 4);
+    a.pairs = interleaved ? (a.rot + 2 * vec - 1) / (2 * vec) : a.rot / 2 / vec;
+    a.lanes = a.pairs + (a.dim - a.rot + 2 * vec - 1) / (2 * vec);
+    a.lanes_div = MafatDiv((uint32_t)a.lanes);
+    a.half_div = MafatDiv((uint32_t)a.rot / 2);
+    // A thread has 8 heads of a token (8 x 2048 tokens of 32 + 8 heads of 128 channels: 62.8 us, with 4 heads 68.0, with 2 116.8),
+    // fewer where that leaves CTAs for all SMs (5 x 676 tokens of 8 + 2 heads: a CTA an SM 8.1, two 8.7, four 12.6).
+    constexpr int kHeads = 8, kSms = 152;
+    const int heads = std::max(a.t[0].heads + a.t[1].heads, a.t[2].heads), rows = kThreads / a.lanes;
+    a.per_block = std::max(1, std::min(rows / ((heads + kHeads - 1) / kHeads), kMostTokens));
+    while (a.per_block > 1 && a.tokens < (int64_t)kSms * a.per_block) a.per_block = (a.per_block + 1) / 2;
+    a.steps = std::min(heads, rows / a.per_block);
+    a.steps_div = MafatDiv((uint32_t)a.steps);
     if (bf16) return interleaved ? launch_v<__nv_bfloat16, true>(a, vec, s) : launch_v<__nv_bfloat16, false>(a, vec, s);
     return interleaved ? launch_v<float, true>(a, vec, s) : launch_v<float, false>(a, vec, s);
 }
