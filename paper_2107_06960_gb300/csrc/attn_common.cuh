@@ -109,6 +109,11 @@ __device__ __forceinline__ int limit_of(const MafatAttnArgs& a, const Block& b, 
 __device__ __forceinline__ int tree_first(const MafatAttnArgs& a, const Block& b) {
     return a.seg.tree ? b.len - nodes_of(a, b.seq) : 0x7fffffff;
 }
+// Tiles of a request's own keys whose rows are past its nodes read none.
+template <bool TREE>
+__device__ __forceinline__ void leave_dead(const MafatAttnArgs& a, Block& b) {
+    if (TREE && a.seg.reqs == 1 && b.row0 >= nodes_of(a, b.seq) * a.group) b.key1 = b.key0;
+}
 struct Way {
     const uint32_t* bits;
     __device__ __forceinline__ Way() : bits(nullptr) {}

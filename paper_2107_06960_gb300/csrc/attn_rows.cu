@@ -132,11 +132,13 @@ struct Ahead : Items {
     const __nv_bfloat16 *k, *v;
     const uint8_t* mask;
 
+    template <bool TREE>
     __device__ __forceinline__ void open(const MafatAttnArgs& a, int warp, Table table) {
         run = runs = 0;
         if (item >= (uint32_t)a.seg.items) return;
         const MafatAttnSeg& g = a.seg;
-        const mafat_attn::Block b(a, item, 16, kBN, table);
+        mafat_attn::Block b(a, item, 16, kBN, table);
+        mafat_attn::leave_dead<TREE>(a, b);
         first = b.key0 + warp * kRun;
         runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
         len = b.len;
@@ -170,12 +172,12 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 
     // the next run into its stage: chunk c of key r at chunk c ^ (r % 8) of its row; empty past the last item
     Ahead ld;
-    ld.open(a, warp, table);
+    ld.open<TREE>(a, warp, table);
     uint32_t ld_stage = 0u, stage = 0u;
     auto load = [&]() {
         while (ld.run == ld.runs && ld.item < (uint32_t)g.items) {
             ld.step();
-            ld.open(a, warp, table);
+            ld.open<TREE>(a, warp, table);
         }
         if (ld.run < ld.runs) {
             const int key = ld.first + ld.run * kBN;
@@ -225,7 +227,8 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     uint32_t which = 0u;
 #pragma unroll 1
     for (Items it; it.item < (uint32_t)g.items; it.step(), which ^= 1u) {
-        const mafat_attn::Block b(a, it.item, 16, kBN, table);
+        mafat_attn::Block b(a, it.item, 16, kBN, table);
+        mafat_attn::leave_dead<TREE>(a, b);
         const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
         const int first = b.key0 + warp * kRun;
         const int runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;

@@ -168,7 +168,8 @@ __global__ void __launch_bounds__(kBM / 4 * kTX, 2) attn_simt_kernel(const __gri
     float* sv = sk + kBN * L::kPitch;
     float* sp = sv + kBN * DP;
     mafat_attn::launch_begin(a);
-    const mafat_attn::Block b(a, blockIdx.x, kBM, kBN);
+    mafat_attn::Block b(a, blockIdx.x, kBM, kBN);
+    mafat_attn::leave_dead<TREE>(a, b);
     const MafatAttnSeg& g = a.seg;
     const int tx = threadIdx.x % kTX, ty = threadIdx.x / kTX;
     const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
@@ -369,7 +370,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
     float* sp = ring + L::kStages * L::kStage;
     if constexpr (CLUSTER) Parts::start();
     mafat_attn::launch_begin(a);
-    const mafat_attn::Block b(a, blockIdx.x, R, kBN);
+    mafat_attn::Block b(a, blockIdx.x, R, kBN);
+    mafat_attn::leave_dead<TREE>(a, b);
     const MafatAttnSeg& g = a.seg;
     const float* kp = (const float*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
     const float* vp = (const float*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;

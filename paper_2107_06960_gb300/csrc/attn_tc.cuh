@@ -376,6 +376,12 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         t.n0 = (t.len0 + kKeys - 1) / kKeys;
     }
     b.set_keys(a, 128 * SLOTS, kKeys);
+    // TREE: a request's rows past its nodes are its last
+    const int rows = TREE && g.reqs == 1 ? mafat_attn::nodes_of(a, b.seq) * a.group : g.rows;
+    if (TREE && b.row0 >= rows) {
+        t.n0 = 0;
+        b.key1 = b.key0;
+    }
     t.gather = gather;
     t.key0 = b.key0;
     t.len = b.len;
@@ -430,7 +436,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         t.len = n;
         t.n = (n + kKeys - 1) / kKeys;
     }
-    const int live = SLOTS == 2 && b.row0 + 128 < g.rows ? 2 : 1;  // slots that have rows
+    const int live = SLOTS == 2 && b.row0 + 128 < rows ? 2 : 1;  // slots that have rows
     // Buffers in use: the scores of tile j wait for the slot's product of tile j - 2 at the least, so that who waits for
     // that of tile j - 1 is less than two phases of its barrier behind.
     const int bufs = C::kBufs > 2 && live == 1 ? 2 : C::kBufs;
@@ -475,10 +481,9 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
 
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t to = tmem + lanes + (uint32_t)(C::kBufs * 128 + slot * DP + half * (DP / C::kHalves));
-        const int sees = mafat_attn::limit_of<TREE>(a, b, at);
-        const int limit = row >= g.rows ? 0x7fffffff : gather ? (!TREE || sees > 0 ? t.len : 0) : sees;
-        // of the prefix's tiles, where both are read
-        const int limit0 = !kBoth ? 0 : !TREE || mafat_attn::live<TREE>(a, at) ? t.len0 : 0;
+        // TREE: a row past its tree's nodes goes with the others, and its sum is dropped at the end
+        const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : TREE ? b.len : at.limit(a, b);
+        const bool dead = TREE && !mafat_attn::live<TREE>(a, at);
         const int first_node = TREE ? mafat_attn::tree_first(a, b) : 0x7fffffff;
         mafat_attn::Way way;
         if (TREE && g.tree) way = mafat_attn::Way(a, b, at);
@@ -505,7 +510,7 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
 #pragma unroll
                 for (int i = 0; i < C::kCols / 32; ++i) tmem_ld32(ts + (uint32_t)(half * C::kCols + 32 * i), s + 32 * i);
                 // readable keys of the thread's
-                const int left = (t.of_prefix(j) ? limit0 : limit) - t.first(j) - half * C::kCols;
+                const int left = (t.of_prefix(j) ? t.len0 : limit) - t.first(j) - half * C::kCols;
 #pragma unroll
                 for (int i = 0; i < C::kCols / 32; ++i) ld_wait32(s + 32 * i);
                 if (left < C::kCols) {
@@ -596,7 +601,8 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
             constexpr int kStep = kWide >= 64 ? 32 : 16;     // read at a time
             constexpr int kChunks = C::kOutBytes / 16, kRows = 32 / kChunks, kSwz = kChunks < 8 ? kChunks : 8;
             const int cc = lane % kChunks, cr = lane / kChunks;
-            const float l = joined(l0 + l1, [](float x, float y) { return x + y; });
+            float l = joined(l0 + l1, [](float x, float y) { return x + y; });
+            if (dead) l = 0.f;
             float inv = mafat_attn::inverse_sum(l), join_top = 0.f, join_inv = 0.f;
             const mafat_attn::Out w(a, b, at);
             if constexpr (kJoins) {

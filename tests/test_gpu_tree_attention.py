@@ -42,6 +42,7 @@ def _tree(mf, G, R, T, P, S, H, Hk, D, dtype, nodes=None, own_len=None, prefix_l
             return torch.where(seen.cuda()[:, :, None, None], x, fill)
         readable = torch.arange(S)[None] < torch.tensor(lens).clamp(0, S)[:, None]
         pk, pv, ok, ov = spoil(pk, seen_p), spoil(pv, seen_p), spoil(ok, readable), spoil(ov, readable)
+        q[torch.arange(T)[None].cuda() >= torch.tensor(counts).cuda()[:, None]] = math.nan  # of places without a node
     kw = {}
     o = torch.full((n, T, H, D), math.nan, dtype=dt, device="cuda")
     if layout == "side":  # queries, keys and values of the caches in wider rows
