@@ -6,7 +6,10 @@ prefix that all requests about the frame share, its cross-attention layers look 
 beside the text, and a norm with the residual's addition stands before each.  The last norm comes out in
 8 bits with a scale a row.  The prompts of all requests go through at once, then single tokens.
 
-    python examples/answer_frames.py [--frames 2] [--requests 4] [--prompt 13] [--steps 8]
+With --draft each step verifies a tree of drafted tokens instead of taking one: rotary positions, attention of the tree to the
+frame and the request's cache, norms on both sides of a gated block, and logits with penalties for what was said.
+
+    python examples/answer_frames.py [--frames 2] [--requests 4] [--prompt 13] [--steps 8] [--draft 7]
 
 Products with weight matrices are torch's; everything else is the framework's.
 """
@@ -111,6 +114,125 @@ class Decoder:
         return (y.to(BF16) @ self.head).float() * scales  # an 8-bit product would take y and its scales as they are
 
 
+def tree_words(parents):
+    """Words of a tree's ways from the root, [1][n][ceil(n / 32)], for parents before their children."""
+    n = len(parents)
+    way = torch.zeros(n, n, dtype=torch.bool)
+    for j, parent in enumerate(parents):
+        if parent >= 0:
+            way[j] = way[parent]
+        way[j, j] = True
+    way = torch.nn.functional.pad(way.long(), (0, -n % 32)).view(n, -1, 32)
+    words = (way << torch.arange(32)).sum(-1)
+    return torch.where(words >= 2 ** 31, words - 2 ** 32, words).to(torch.int32)[None].cuda()
+
+
+class DraftingDecoder(Decoder):
+    """Each step reads a tree of `nodes` drafted tokens of every request, whose root is the last token taken, and keeps those
+    on the way that its logits agree with.  Here the drafts are what follows a token by embedding and head alone."""
+
+    def __init__(self, *args, nodes=7, **kw):
+        super().__init__(*args, **kw)
+        self.nodes = nodes
+        g = torch.Generator(device="cuda")
+        g.manual_seed(5)
+        self.after_gain = [torch.ones(self.width, device="cuda", dtype=BF16) for _ in range(2 * self.layers)]
+        self.gate = [(1 + 0.1 * torch.randn(self.width, generator=g, device="cuda")).to(BF16) for _ in range(2 * self.layers)]
+        self.rotary = mf.Rotary(self.dim, scaling=mf.ROTARY_BLEND, factor=2.0, first_positions=1024)
+        self.next_tokens = (self.embedding.float() @ self.head.float()).topk(2).indices
+        self.parents = [(j + 1) // 2 - 1 for j in range(nodes)]  # two children a node
+        self.ways = tree_words(self.parents)
+        self.said = torch.zeros(self.batch, self.room, device="cuda", dtype=torch.int32)
+        self.repetition = torch.full((self.batch,), 1.2, device="cuda")
+        self.frequency = torch.full((self.batch,), 0.1, device="cuda")
+
+    def tree_plan(self, n_q):
+        if ("tree", n_q) not in self.plans:
+            side, both = (self.heads + 2 * self.heads_kv) * self.dim, 2 * self.heads_kv * self.dim
+            kv = (self.n_states * both, both, self.dim)
+            self.plans["tree", n_q] = mf.TreeAttention(self.frames, self.requests, n_q, self.n_states, self.room, self.heads, self.heads_kv,
+                                                       self.dim, q_strides=(n_q * side, side, self.dim), prefix_k_strides=kv,
+                                                       prefix_v_strides=kv)
+        return self.plans["tree", n_q]
+
+    def between(self, x, residual, i):
+        """The norm behind block i - 1 and its gate, the residual's addition, the norm before block i."""
+        h, y = torch.empty_like(x), torch.empty_like(x)
+        behind = {} if i == 0 else dict(post_weight=self.after_gain[i - 1], gate=self.gate[i - 1], residual_scale=0.95)
+        mf.block_norm(x, residual, h, weight=self.gain[i], y=y, **behind)
+        return h, y
+
+    def read_tree(self, tokens, ways, positions):
+        """tokens, positions [batch][n], a tree behind self.length tokens of each request: adjusted logits, fp32."""
+        n = tokens.shape[1]
+        places = self.length[:, None] + torch.arange(n, device="cuda", dtype=torch.int32)
+        x = self.embedding[tokens.reshape(-1)]
+        h, q_cols = torch.zeros_like(x), self.heads * self.dim
+        for i in range(self.layers):
+            h, y = self.between(x, h, 2 * i)
+            qkv = (y @ self.self_in[i]).view(self.batch, n, -1, self.dim)
+            q, k, v = qkv.split([self.heads, self.heads_kv, self.heads_kv], 2)
+            self.rotary.run(positions, q=q, q_out=q, k=k, k_out=self.cache[i][0], v=v, v_out=self.cache[i][1], places=places)
+            o = torch.empty(q.shape, device="cuda", dtype=BF16)
+            self.tree_plan(n).run(q, *self.states[i][0], *self.cache[i], ways, o, own_len=self.length + n)
+            x = o.view(-1, q_cols) @ self.out[i][0]
+            h, y = self.between(x, h, 2 * i + 1)
+            q = (y @ self.cross_in[i]).view(self.frames, self.requests * n, self.heads, self.dim)
+            o = torch.empty_like(q)
+            self.plan("cross", n).run(q, *self.states[i][1], o)
+            x = o.view(-1, q_cols) @ self.out[i][1]
+        h, y = self.between(x, h, 2 * self.layers)
+        logits = (y @ self.head).view(self.batch, n, -1)
+        out = torch.empty(logits.shape, device="cuda")
+        mf.adjust_logits(logits, out, tokens=self.said, lengths=self.length, repetition=self.repetition, frequency=self.frequency,
+                         drafts=tokens.to(torch.int32), tree=ways)
+        return out
+
+    def keep(self, tokens, path, count):
+        """The first count [batch] nodes of each path [batch][n] become the request's next tokens."""
+        n, rows = path.shape[1], torch.arange(self.batch, device="cuda")[:, None]
+        at = self.length[:, None].long() + torch.arange(n, device="cuda")
+        for c in self.cache:
+            c[:, rows, at] = c[:, rows, self.length[:, None].long() + path]
+        self.said[rows, at] = tokens.gather(1, path).to(torch.int32)
+        self.length += count.to(torch.int32)
+
+    def read_prompt(self, tokens):
+        n = tokens.shape[1]
+        positions = torch.arange(n, device="cuda", dtype=torch.int32).expand(self.batch, n).contiguous()
+        logits = self.read_tree(tokens, tree_words(range(-1, n - 1)), positions)
+        path = torch.arange(n, device="cuda").expand(self.batch, n)
+        self.keep(tokens, path, torch.full((self.batch,), n, device="cuda"))
+        return logits[:, -1].argmax(-1)
+
+    def step(self, last):
+        """last [batch], the token to go on from: the tokens that follow it [batch][depth], how many of them count, the new last."""
+        tokens, depth = [last], [0]
+        for j in range(1, self.nodes):
+            tokens.append(self.next_tokens[tokens[self.parents[j]], (j - 1) % 2])
+            depth.append(depth[self.parents[j]] + 1)
+        tokens = torch.stack(tokens, 1)
+        positions = self.length[:, None] + torch.tensor(depth, device="cuda", dtype=torch.int32)
+        best = self.read_tree(tokens, self.ways, positions.contiguous()).argmax(-1)
+        # down from the root, as long as a drafted child is what its parent's logits ask for
+        at = torch.zeros(self.batch, device="cuda", dtype=torch.long)
+        path, on = [at], torch.ones(self.batch, device="cuda", dtype=torch.bool)
+        count = torch.ones(self.batch, device="cuda", dtype=torch.long)
+        for _ in range(max(depth)):
+            want, here = best.gather(1, at[:, None])[:, 0], at
+            for child in (2 * here + 1, 2 * here + 2):
+                inside = child.clamp(max=self.nodes - 1)
+                hit = on & (child < self.nodes) & (tokens.gather(1, inside[:, None])[:, 0] == want) & (at == here)
+                at = torch.where(hit, child, at)
+            on = on & (at != here)
+            count += on
+            path.append(at)
+        path = torch.stack(path, 1)
+        taken = best.gather(1, path)  # what each node on the way asks for; the last of them is not drafted
+        self.keep(tokens, path, count)
+        return taken, count, taken.gather(1, count[:, None] - 1)[:, 0]
+
+
 def frame_states(frames, size=224, seed=7):
     """Feature maps of random frames by the 16-layer front-end: [frames][(size / 16)^2][256]."""
     layers = synth.YOLO16
@@ -125,13 +247,39 @@ def frame_states(frames, size=224, seed=7):
     return states.view(frames, h * w, c)
 
 
+def answer_with_drafts(a):
+    """As many tokens of each request as there are steps, or more; returns the first ones of each."""
+    states = frame_states(a.frames)
+    room = a.prompt + (a.steps + 1) * (a.draft.bit_length() + 1) + a.draft
+    d = DraftingDecoder(a.frames, a.requests, states.shape[1], states.shape[2], room=room, nodes=a.draft)
+    d.read_frames(states)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    last = d.read_prompt(torch.randint(0, d.embedding.shape[0], (d.batch, a.prompt), generator=g, device="cuda"))
+    answers, kept = [[int(x)] for x in last], 0
+    for _ in range(a.steps - 1):
+        tokens, count, last = d.step(last)
+        kept += int(count.sum())
+        for answer, row, n in zip(answers, tokens.tolist(), count.tolist()):
+            answer.extend(row[:n])
+    for plan in d.plans.values():
+        plan.sync_status(like=last)
+    print("%.2f tokens of a request a step" % (kept / max(1, (a.steps - 1) * d.batch)))
+    for n, row in enumerate(answers):
+        print("frame %d, request %d: %s" % (n // a.requests, n % a.requests, " ".join(map(str, row))))
+    return torch.tensor([row[:a.steps] for row in answers])
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--frames", type=int, default=2)
     ap.add_argument("--requests", type=int, default=4)
     ap.add_argument("--prompt", type=int, default=13)
     ap.add_argument("--steps", type=int, default=8)
+    ap.add_argument("--draft", type=int, default=0, help="nodes of a tree of drafted tokens, 0: none")
     a = ap.parse_args(argv)
+    if a.draft:
+        return answer_with_drafts(a)
     states = frame_states(a.frames)
     d = Decoder(a.frames, a.requests, states.shape[1], states.shape[2], room=a.prompt + a.steps)
     d.read_frames(states)
