@@ -34,6 +34,7 @@ struct AttnSegPlan {
     int32_t n_seq = 0, reqs = 0, n = 0, causal = 0;
     int64_t k[3] = {0, 0, 0}, v[3] = {0, 0, 0};  // strides: sequence, key, head
     int32_t rows = 0, row_tiles = 0, splits = 0, part0 = 0, items = 0, ctas = 0;
+    uint32_t cut = 0;  // as MafatAttnSeg's
     AttnKernel kernel = kRows;
     double us = 0.;  // by the model
 };
@@ -175,6 +176,25 @@ constexpr double kClusterJoinUs = 0.7, kOwnJoinUs = 1.0;
 
 int64_t row_tiles(const AttnShape& sh, int32_t rows) { return (rows + sh.rows - 1) / sh.rows; }
 
+// One CTA an SM that leaves SMs idle: those take the last keys of all items, in as many rounds as that needs, while the others
+// have the rest.  64 trees of 16 nodes about 23104 states (128 items of 181 tiles on 152 SMs), with their own keys: 265 us, 278 with
+// whole items.
+struct Cut {
+    uint32_t share;  // of the first part; 0: whole items
+    double us;
+};
+Cut choose_cut(const AttnShape& sh, int sms, int64_t items, int64_t tiles, double part_bytes) {
+    const int64_t idle = sms - items;
+    if (sh.ctas != 1 || idle < 1 || items < idle) return {0, 0.};
+    const double rounds = (double)((items + idle - 1) / idle), whole = sh.setup + (double)tiles * sh.tile;
+    const int64_t second = (int64_t)((whole - rounds * sh.setup) / ((rounds + 1.) * sh.tile));
+    if (second < 1) return {0, 0.};
+    const double us = sh.fixed + std::max(sh.setup + (double)(tiles - second) * sh.tile, rounds * (sh.setup + (double)second * sh.tile)) +
+                      2. * part_bytes / 6e6 + 0.3;  // a part more there and back
+    if (us > 0.98 * (sh.fixed + whole)) return {0, 0.};
+    return {(uint32_t)std::ceil((double)(tiles - second) / (double)tiles * 4294967296.), us};
+}
+
 // The work of a segment: the kernel, tiles of rows, parts of the keys.
 mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int sms, bool second) {
     if (g.n > kMostCounted) return fail(MAFAT_EUNSUPPORTED, "too many keys");
@@ -225,6 +245,16 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
     g.us = best.us;
     const AttnShape sh = shape_of(g.kernel, p.dim);
     g.row_tiles = (int32_t)row_tiles(sh, g.rows);
+    g.cut = 0;
+    if (p.kind == kTree && p.n_run == 2 && !second && c.splits == 0 && g.kernel == kTc2 && best.n == 1) {
+        Cut cut = choose_cut(sh, sms, (int64_t)g.n_seq * p.heads_kv * g.row_tiles, (g.n + sh.keys - 1) / sh.keys,
+                             4. * p.dim * (double)p.rows_total);
+        if (cut.share) {
+            best.n = 2;
+            g.cut = cut.share;
+            g.us = cut.us;
+        }
+    }
     g.splits = best.n;
     p.cluster = best.cluster;
     const int64_t items = (int64_t)g.n_seq * p.heads_kv * g.row_tiles * g.splits;
@@ -261,6 +291,7 @@ void plan_both(mafat_attn_s& p, const Common& c, int sms) {
         if (m.items > kMaxI32 / 4 || m.us(1) >= best) continue;
         best = m.us(1);
         p.both = own;
+        p.both.cut = 0;
         p.both.kernel = k;
         p.both.row_tiles = (int32_t)row_tiles(m.sh, own.rows);
         p.both.splits = 1;
@@ -436,6 +467,7 @@ mafat_status run(const mafat_attn_s* p, AttnKind kind, const void* q, const SegD
         x.splits_div = MafatDiv((uint32_t)g.splits);
         x.part0 = g.part0;
         x.items = g.items;
+        x.cut = g.cut;
         a.overlap = r > 0 && !both;
         a.join = r > 0 && p->joined && !both ? p->parts : 0;
         a.cluster = p->cluster;

@@ -47,6 +47,9 @@ struct MafatAttnSeg {
     MafatDiv row_tiles_div, splits_div;
     int32_t part0;              // first of its splits among the parts of a row
     int32_t items;              // n_seq * heads_kv * splits * row_tiles
+    // of a tree's tiles of many rows: not 0: two splits, of which the first has this share (in 2^-32) of a sequence's tiles of
+    // keys; items of the first come before those of the second
+    uint32_t cut;
 };
 
 constexpr int kMafatMostOrdered = 128;

@@ -349,7 +349,15 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
     }
     __syncwarp();
     // queries, whose places are known before the launch before has ended; they and the length come together
-    mafat_attn::Block b(a, blockIdx.x, 128 * SLOTS);
+    uint32_t item = blockIdx.x, part = 0u;
+    if (TREE && g.cut) {
+        const uint32_t half = (uint32_t)g.items / 2u;
+        part = item >= half ? 1u : 0u;
+        item -= part * half;
+        const uint32_t rest = g.row_tiles_div.div(item);
+        item += (rest + part) * (uint32_t)g.row_tiles;  // (rest * 2 + part) * row_tiles + the tile
+    }
+    mafat_attn::Block b(a, TREE ? item : blockIdx.x, 128 * SLOTS);
     constexpr int kChunks = DP / 8, kRows = 32 / kChunks;  // 16-byte chunks of a row; rows of a warp's access
     constexpr int kLoads = 32 / kRows / C::kHalves;
     const int q_slot = warp / C::kSlotWarps, q_half = warp / 4 % C::kHalves, q_quarter = warp % 4;
@@ -376,6 +384,11 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         t.n0 = (t.len0 + kKeys - 1) / kKeys;
     }
     b.set_keys(a, 128 * SLOTS, kKeys);
+    if (TREE && g.cut) {
+        const int first = (int)__umulhi((uint32_t)(b.len + kKeys - 1) / kKeys, g.cut) * kKeys;
+        b.key0 = part ? first : 0;
+        b.key1 = part ? b.len : min(first, b.len);
+    }
     // TREE: a request's rows past its nodes are its last
     const int rows = TREE && g.reqs == 1 ? mafat_attn::nodes_of(a, b.seq) * a.group : g.rows;
     if (TREE && b.row0 >= rows) {
