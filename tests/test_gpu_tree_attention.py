@@ -181,3 +181,11 @@ def test_empty_and_wide_trees_of_one_request(mf):
     """More nodes than one tile of rows has, with one head for all."""
     _tree(mf, 1, 1, 300, 129, 500, 3, 1, 64, mf.BF16)
     _tree(mf, 1, 1, 300, 129, 500, 2, 1, 64, mf.FP32, nodes=[257])
+
+
+@pytest.mark.parametrize("D,P,lens", [(128, 12000, [12000, 12000]), (128, 12000, [9999, 300]), (64, 9000, [0, 1]), (64, 9000, [8000, 127])])
+def test_keys_that_idle_sms_take(mf, D, P, lens):
+    """Prefixes whose tiles leave SMs idle: two parts of unequal length, also of sequences shorter than the first."""
+    o, _, plan = _tree(mf, 2, 32, 16, P, 100, 32, 8, D, mf.BF16, prefix_len=lens, nodes=[1 + (5 * b) % 16 for b in range(64)], poison=True)
+    s = plan.stats()
+    assert s["splits"][0] == 2 and s["ctas"][0] % 2 == 0 and s["ctas"][0] // 2 < 152
