@@ -57,6 +57,7 @@ struct mafat_attn_s {
     AttnSegPlan both;
     int parts = 0;
     int cluster = 1;      // CTAs of a cluster that joins its parts itself
+    int both_cluster = 1;  // the same where one launch does both sets
     bool joined = false;  // the second launch joins the first one's parts with its own results
     int64_t rows_total = 0, workspace_bytes = 0;
     void* workspace = nullptr;
@@ -274,7 +275,7 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
 // a token over 1444 (16 and 4 of 64) 7.3, 15.5; 8 of 64 over 3 x 13852 (8 and 4 of 128) 75, 133.
 // Two launches whose first has whole results were measured to take 1 to 1.45 times what the model has for them (with
 // parts, the launch to join them, which it counts, falls away).
-constexpr double kTwoLaunches = 1.2;
+constexpr double kTwoLaunches = 1.2, kClusterShare = 0.8;
 void plan_both(mafat_attn_s& p, const Common& c, int sms) {
     if (p.dtype != MAFAT_BF16 || p.n_run != 2 || c.splits != 0 || c.kernel == MAFAT_ATTN_ROWS) return;
     const AttnSegPlan &first = p.seg[p.run[0]], &own = p.seg[p.run[1]];
@@ -297,6 +298,30 @@ void plan_both(mafat_attn_s& p, const Common& c, int sms) {
         p.both.splits = 1;
         p.both.part0 = 0;
         p.both.items = p.both.ctas = (int32_t)m.items;
+    }
+    // Few rows of trees: clusters that split both sets' keys.  In us, as above (no clusters) and in clusters: a tree of 8 nodes over
+    // 1444 + 96 keys (16 and 4 heads of 64) 7.5, 6.9; 8 of them (8 and 2 of 128) 13.4, 10.1; 4 x 2 trees of 3 over 96 + 116 (8 and 2 of
+    // 64) 6.0, 5.4; 5 of 3 over 4663 + 4 (8 and 1 of 40) 9.8, 11.3.  Of 35 drawn plans they were slower in all whose time by the
+    // model was more than kClusterShare of the others', and in 3 of the 28 below it, by up to 0.8.
+    if (p.kind != kTree || c.kernel == MAFAT_ATTN_TILES || (int64_t)first.n + own.n > kMaxI32 / 16) return;
+    Model m{};
+    m.sh = shape_of(kRows, p.dim);
+    m.sms = sms;
+    m.items = (int64_t)own.n_seq * p.heads_kv * row_tiles(m.sh, own.rows);
+    m.tiles = ((int64_t)first.n + m.sh.keys - 1) / m.sh.keys + ((int64_t)own.n + m.sh.keys - 1) / m.sh.keys;
+    m.bytes = 4. * p.heads_kv * p.dim * ((double)own.n_seq * first.n + (double)own.n_seq * own.n);
+    best *= kClusterShare;
+    for (int32_t n = kMostCluster; n > 1; n /= 2) {
+        const double us = m.us(n) + kClusterJoinUs;
+        if (n > m.tiles || m.items * n > (int64_t)sms * m.sh.ctas || us >= best) continue;
+        best = us;
+        p.both = own;
+        p.both.kernel = kRows;
+        p.both.row_tiles = (int32_t)row_tiles(m.sh, own.rows);
+        p.both.splits = p.both_cluster = n;
+        p.both.part0 = 0;
+        p.both.cut = 0;
+        p.both.items = p.both.ctas = (int32_t)(m.items * n);
     }
 }
 
@@ -470,7 +495,7 @@ mafat_status run(const mafat_attn_s* p, AttnKind kind, const void* q, const SegD
         x.cut = g.cut;
         a.overlap = r > 0 && !both;
         a.join = r > 0 && p->joined && !both ? p->parts : 0;
-        a.cluster = p->cluster;
+        a.cluster = both ? p->both_cluster : p->cluster;
         // where a CTA has several items; of more sequences it has so many that they level it
         a.ordered = g.kernel == kRows && x.len && g.n_seq > 1 && g.n_seq <= kMafatMostOrdered && g.items > g.ctas;
         a.direct = both || a.join || (p->parts == 1 && !p->joined);
@@ -493,7 +518,13 @@ mafat_status run(const mafat_attn_s* p, AttnKind kind, const void* q, const SegD
             }
             e = mafat_launch_attn_tc(a, k, v, g.kernel == kTc2 ? 2 : 1, both ? &prefix : nullptr, s);
         } else {
-            e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, s) : mafat_launch_attn_simt(a, shape_of(g.kernel, p->dim).rows, s);
+            MafatRowsPrefix prefix;
+            if (both) {
+                const AttnSegPlan& f = p->seg[p->run[0]];
+                const SegData& fd = d[p->run[0]];
+                prefix = {fd.k, fd.v, f.k[0], f.k[1], f.k[2], f.v[0], f.v[1], f.v[2], fd.len, f.n, MafatDiv((uint32_t)f.reqs)};
+            }
+            e = g.kernel == kRows ? mafat_launch_attn_rows(a, g.ctas, both ? &prefix : nullptr, s) : mafat_launch_attn_simt(a, shape_of(g.kernel, p->dim).rows, s);
         }
         if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     }

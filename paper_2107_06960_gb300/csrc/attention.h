@@ -88,7 +88,17 @@ cudaError_t mafat_prepare_attn_simt();
 int mafat_attn_simt_keys();
 
 // bf16, tiles of 16 rows by runs of 64 keys, ctas CTAs that take one item after another.
-cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, cudaStream_t s);
+// prefix: null, or keys that come before the segment's own and that `per` of its sequences after another share; of trees
+// in clusters alone.
+struct MafatRowsPrefix {
+    const void* k;
+    const void* v;
+    int64_t k_sb, k_ss, k_sh, v_sb, v_ss, v_sh;
+    const int32_t* len;         // of each prefix (null: n)
+    int32_t n;
+    MafatDiv per;
+};
+cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, const MafatRowsPrefix* prefix, cudaStream_t s);
 cudaError_t mafat_prepare_attn_rows();
 int mafat_attn_rows_keys();
 int mafat_attn_rows_join();  // most parts of an earlier launch that it joins

@@ -124,11 +124,17 @@ struct Way {
         const int n = key - first;
         return n < 0 || (bits[n / 32] >> (n % 32) & 1u) != 0u;
     }
+};
+// The same with the first word, all that most trees have, read ahead.
+struct WayAhead : Way {
+    uint32_t first_word;
+    __device__ __forceinline__ WayAhead() : first_word(0u) {}
+    __device__ __forceinline__ WayAhead(const MafatAttnArgs& a, const Block& b, const Row& r) : Way(a, b, r), first_word(*bits) {}
     // whether it holds each of the 32 keys from `key`, bit by bit; past the last node none
     __device__ __forceinline__ uint32_t from(int key, int first, int words) const {
         const int n = key - first, i = n >> 5;  // rounded down also where n is negative
-        const uint32_t lo = i < 0 ? 0xffffffffu : i < words ? bits[i] : 0u;
-        const uint32_t hi = i + 1 < 0 ? 0xffffffffu : i + 1 < words ? bits[i + 1] : 0u;
+        const uint32_t lo = i < 0 ? 0xffffffffu : i == 0 ? first_word : i < words ? bits[i] : 0u;
+        const uint32_t hi = i < -1 ? 0xffffffffu : i == -1 ? first_word : i + 1 < words ? bits[i + 1] : 0u;
         return __funnelshift_r(lo, hi, (uint32_t)n & 31u);
     }
 };

@@ -18,6 +18,8 @@
 // One token of 64 sequences, 32 query and 8 key heads, 1444 keys: 59 us or 6.4 TB/s with 128 channels, 34 us or 5.5 TB/s
 // with 64; under 40 % of the issue slots are taken.  One token of one sequence (8 query and 4 key heads, 1444 keys) is
 // bound by round trips: 5.1 us in 4 clusters of 8 CTAs, 5.8 with a launch that joins the parts.
+#include <type_traits>
+
 #include "attn_common.cuh"
 
 namespace {
@@ -126,22 +128,53 @@ __device__ __forceinline__ void order_sequences(const MafatAttnSeg& g, int2* ord
     __syncthreads();
 }
 
+struct NoPrefix {};
+
+// Keys of two sets as one: first the prefix's tiles, of which the last may be partly empty, then the own keys.
+template <class Prefix>
+struct Sets {
+    static constexpr bool kBoth = std::is_same<Prefix, MafatRowsPrefix>::value;
+    int seq, len0, own0;  // of the prefix: which, readable keys; where own keys begin
+    __device__ __forceinline__ Sets() : seq(0), len0(0), own0(0) {}
+    // the item's keys, a run of whole tiles of both sets' (splits: the cluster's CTAs)
+    __device__ __forceinline__ Sets(const MafatAttnArgs& a, mafat_attn::Block& b, const Prefix& prefix) : Sets() {
+        if constexpr (kBoth) {
+            seq = (int)prefix.per.div((uint32_t)b.seq);
+            len0 = prefix.len ? min(max(prefix.len[seq], 0), prefix.n) : prefix.n;
+            own0 = (len0 + kBN - 1) / kBN * kBN;
+            const uint32_t tiles = (uint32_t)(own0 + b.len + kBN - 1) / kBN, s = (uint32_t)b.split;
+            b.key0 = (int)a.seg.splits_div.div(tiles * s) * kBN;
+            b.key1 = min((int)a.seg.splits_div.div(tiles * (s + 1u)) * kBN, own0 + b.len);
+        }
+    }
+    __device__ __forceinline__ bool of_prefix(int key) const { return kBoth && key < own0; }
+    // The item of a CTA: a cluster's are the parts of one tile of rows, which are not neighbours where there are more tiles.
+    static __device__ __forceinline__ uint32_t item(const MafatAttnArgs& a, uint32_t i) {
+        if constexpr (!kBoth) return i;
+        const MafatAttnSeg& g = a.seg;
+        const uint32_t tile = g.splits_div.div(i), pair = g.row_tiles_div.div(tile);
+        return (pair * (uint32_t)g.splits + i - tile * (uint32_t)g.splits) * (uint32_t)g.row_tiles + tile - pair * (uint32_t)g.row_tiles;
+    }
+};
+
 // The copying side's place: a run of an item.
 struct Ahead : Items {
-    int run, runs, first, len;
+    int run, runs, first, len, head;
     const __nv_bfloat16 *k, *v;
     const uint8_t* mask;
 
-    template <bool TREE>
-    __device__ __forceinline__ void open(const MafatAttnArgs& a, int warp, Table table) {
+    template <bool TREE, class Prefix>
+    __device__ __forceinline__ void open(const MafatAttnArgs& a, int warp, Table table, const Prefix& prefix, Sets<Prefix>& sets) {
         run = runs = 0;
         if (item >= (uint32_t)a.seg.items) return;
         const MafatAttnSeg& g = a.seg;
-        mafat_attn::Block b(a, item, 16, kBN, table);
+        mafat_attn::Block b(a, Sets<Prefix>::item(a, item), 16, kBN, table);
+        sets = Sets<Prefix>(a, b, prefix);
         mafat_attn::leave_dead<TREE>(a, b);
         first = b.key0 + warp * kRun;
         runs = b.key1 > first ? (b.key1 - first + kBN - 1) / kBN : 0;
         len = b.len;
+        head = b.head;
         k = (const __nv_bfloat16*)g.k + (int64_t)b.seq * g.k_sb + (int64_t)b.head * g.k_sh;
         v = (const __nv_bfloat16*)g.v + (int64_t)b.seq * g.v_sb + (int64_t)b.head * g.v_sh;
         mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
@@ -150,8 +183,10 @@ struct Ahead : Items {
 
 // CLUSTER: a cluster's CTAs have an item's parts and join them (an instance of its own: in one kernel it cost the
 // other form's inner loop 20 %).  TREE: queries are nodes of trees, whose bits are looked at in runs that have such keys.
-template <int DP, bool CLUSTER, bool TREE>
-__global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ MafatAttnArgs a) {
+// Prefix: MafatRowsPrefix where both sets of keys are read as one.
+template <int DP, bool CLUSTER, bool TREE, class Prefix>
+__global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_constant__ MafatAttnArgs a, const __grid_constant__ Prefix prefix) {
+    constexpr bool kBoth = Sets<Prefix>::kBoth;
     using C = Cfg<DP, CLUSTER>;
     using Parts = mafat_attn::ClusterParts<16, DP>;
     constexpr int kChunks = DP / 8;        // 16-byte chunks of a row
@@ -172,25 +207,39 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 
     // the next run into its stage: chunk c of key r at chunk c ^ (r % 8) of its row; empty past the last item
     Ahead ld;
-    ld.open<TREE>(a, warp, table);
+    Sets<Prefix> sets;
+    ld.open<TREE>(a, warp, table, prefix, sets);
     uint32_t ld_stage = 0u, stage = 0u;
     auto load = [&]() {
         while (ld.run == ld.runs && ld.item < (uint32_t)g.items) {
             ld.step();
-            ld.open<TREE>(a, warp, table);
+            ld.open<TREE>(a, warp, table, prefix, sets);
         }
         if (ld.run < ld.runs) {
-            const int key = ld.first + ld.run * kBN;
+            int key = ld.first + ld.run * kBN, len = ld.len;
             const uint32_t st = ring + ld_stage * (2 * C::kMatrix);
+            const __nv_bfloat16 *k_from = ld.k, *v_from = ld.v;
+            int64_t k_step = g.k_ss, v_step = g.v_ss;
+            if constexpr (kBoth) {
+                if (sets.of_prefix(key)) {
+                    k_from = (const __nv_bfloat16*)prefix.k + (int64_t)sets.seq * prefix.k_sb + (int64_t)ld.head * prefix.k_sh;
+                    v_from = (const __nv_bfloat16*)prefix.v + (int64_t)sets.seq * prefix.v_sb + (int64_t)ld.head * prefix.v_sh;
+                    k_step = prefix.k_ss;
+                    v_step = prefix.v_ss;
+                    len = sets.len0;
+                } else {
+                    key -= sets.own0;
+                }
+            }
 #pragma unroll
             for (int r0 = 0; r0 < kRun; r0 += kRows) {
                 const int r = r0 + cr, k = key + r;
-                const bool on = in_dim && k < ld.len && (!ld.mask || ld.mask[k] != 0);
+                const bool on = in_dim && k < len && (!ld.mask || ld.mask[k] != 0);
                 const uint32_t at = st + (uint32_t)(r * (DP * 2) + ((cc ^ (r % 8)) * 16));
                 // a place that is not read still gets an address inside the tensor
                 const int64_t kk = on ? k : 0;
-                copy16(at, ld.k + (on ? kk * g.k_ss + cc * 8 : 0), on);
-                copy16(at + C::kMatrix, ld.v + (on ? kk * g.v_ss + cc * 8 : 0), on);
+                copy16(at, k_from + (on ? kk * k_step + cc * 8 : 0), on);
+                copy16(at + C::kMatrix, v_from + (on ? kk * v_step + cc * 8 : 0), on);
             }
             ++ld.run;
             if (++ld_stage == (uint32_t)C::kStages) ld_stage = 0u;
@@ -200,7 +249,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     // a warp's share of an item's queries, rows past the last zero
     auto load_queries = [&](uint32_t item, uint32_t which) {
         if (item < (uint32_t)g.items) {
-            const mafat_attn::Block b(a, item, 16, kBN, table);
+            const mafat_attn::Block b(a, Sets<Prefix>::item(a, item), 16, kBN, table);
 #pragma unroll
             for (int r0 = 0; r0 < 16 / kWarps; r0 += kRows) {
                 const int r = warp * (16 / kWarps) + r0 + cr, row = min(b.row0 + r, g.rows - 1);
@@ -227,7 +276,8 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
     uint32_t which = 0u;
 #pragma unroll 1
     for (Items it; it.item < (uint32_t)g.items; it.step(), which ^= 1u) {
-        mafat_attn::Block b(a, it.item, 16, kBN, table);
+        mafat_attn::Block b(a, Sets<Prefix>::item(a, it.item), 16, kBN, table);
+        if constexpr (kBoth) Sets<Prefix>(a, b, prefix);
         mafat_attn::leave_dead<TREE>(a, b);
         const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
         const int first = b.key0 + warp * kRun;
@@ -242,7 +292,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             ldm4(q[t], smem + C::kOffQ + which * C::kQ + (uint32_t)(v_row * (DP * 2) + (((2 * t + v_chunk) ^ (v_row % 8)) * 16)));
         load_queries(it.next(), which ^ 1u);  // lands with the next run
         int limit[2];
-        mafat_attn::Way way[2];
+        mafat_attn::WayAhead way[2];
         const int first_node = TREE ? mafat_attn::tree_first(a, b) : 0x7fffffff;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -251,7 +301,8 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             if (!TREE || r < g.rows) {
                 const mafat_attn::Row row(a, b, r);
                 if (r < g.rows) limit[h] = mafat_attn::limit_of<TREE>(a, b, row);
-                if (TREE && g.tree) way[h] = mafat_attn::Way(a, b, row);
+                if (kBoth && r < g.rows) limit[h] = mafat_attn::live<TREE>(a, row) ? 0x7fffffff : 0;  // the length bounds them
+                if (TREE && g.tree) way[h] = mafat_attn::WayAhead(a, b, row);
             }
         }
         float base[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
@@ -266,7 +317,15 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             load();
             wait_copies<C::kStages - 1>();
             __syncwarp();
-            const int key = first + i * kBN;
+            int key = first + i * kBN, len = b.len;
+            bool own = true;  // the request's keys
+            if constexpr (kBoth) {
+                own = !sets.of_prefix(key);
+                if (own)
+                    key -= sets.own0;
+                else
+                    len = sets.len0;
+            }
             const uint32_t st = ring + stage * (2 * C::kMatrix);
             if (++stage == (uint32_t)C::kStages) stage = 0u;
             float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -277,16 +336,18 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
                 mma(s[0], q[t], f[0], f[1]);
                 mma(s[1], q[t], f[2], f[3]);
             }
-            if (mask || key + kRun > limit[0] || key + kRun > limit[1]) {
+            // of two sets a row sees either's keys, or none
+            const int most[2] = {kBoth ? min(limit[0], len) : limit[0], kBoth ? min(limit[1], len) : limit[1]};
+            if (mask || key + kRun > most[0] || key + kRun > most[1]) {
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int k = key + n * 8 + (lane % 4) * 2 + e % 2;
-                        if (k >= b.len || k >= limit[e / 2] || (mask && mask[k] == 0)) s[n][e] = -CUDART_INF_F;
+                        if (k >= len || k >= most[e / 2] || (mask && mask[k] == 0)) s[n][e] = -CUDART_INF_F;
                     }
             }
-            if (TREE && key + kRun > first_node) {
+            if (TREE && own && key + kRun > first_node) {
                 uint32_t held[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -458,24 +519,29 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 
 template <int DP, bool TREE>
 cudaError_t launch_form(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
-    return mafat_launch_clusters(a.cluster, a.cluster > 1 ? attn_rows_kernel<DP, true, TREE> : attn_rows_kernel<DP, false, TREE>,
-                                 (unsigned)ctas, kThreads, a.cluster > 1 ? Cfg<DP, true>::kSmem : Cfg<DP, false>::kSmem, s, a);
+    return mafat_launch_clusters(a.cluster, a.cluster > 1 ? attn_rows_kernel<DP, true, TREE, NoPrefix> : attn_rows_kernel<DP, false, TREE, NoPrefix>,
+                                 (unsigned)ctas, kThreads, a.cluster > 1 ? Cfg<DP, true>::kSmem : Cfg<DP, false>::kSmem, s, a, NoPrefix());
 }
 template <int DP>
-cudaError_t launch(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
+cudaError_t launch(const MafatAttnArgs& a, int ctas, const MafatRowsPrefix* prefix, cudaStream_t s) {
+    if (prefix)
+        return mafat_launch_clusters(a.cluster, attn_rows_kernel<DP, true, true, MafatRowsPrefix>, (unsigned)ctas, kThreads,
+                                     Cfg<DP, true>::kSmem, s, a, *prefix);
     return a.tree ? launch_form<DP, true>(a, ctas, s) : launch_form<DP, false>(a, ctas, s);
 }
 template <int DP, bool TREE>
 cudaError_t prepare_form() {
-    const cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<DP, false, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    const cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<DP, false, TREE, NoPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                Cfg<DP, false>::kSmem);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(attn_rows_kernel<DP, true, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP, true>::kSmem);
+    return cudaFuncSetAttribute(attn_rows_kernel<DP, true, TREE, NoPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP, true>::kSmem);
 }
 template <int DP>
 cudaError_t prepare() {
-    const cudaError_t e = prepare_form<DP, false>();
-    return e != cudaSuccess ? e : prepare_form<DP, true>();
+    cudaError_t e = prepare_form<DP, false>();
+    if (e != cudaSuccess || (e = prepare_form<DP, true>()) != cudaSuccess) return e;
+    return cudaFuncSetAttribute(attn_rows_kernel<DP, true, true, MafatRowsPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                Cfg<DP, true>::kSmem);
 }
 
 }  // namespace
@@ -483,8 +549,8 @@ cudaError_t prepare() {
 int mafat_attn_rows_keys() { return kBN; }
 int mafat_attn_rows_join() { return kMostJoin; }
 
-cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
-    return a.dim <= 64 ? launch<64>(a, ctas, s) : launch<128>(a, ctas, s);
+cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, const MafatRowsPrefix* prefix, cudaStream_t s) {
+    return a.dim <= 64 ? launch<64>(a, ctas, prefix, s) : launch<128>(a, ctas, prefix, s);
 }
 
 cudaError_t mafat_prepare_attn_rows() {

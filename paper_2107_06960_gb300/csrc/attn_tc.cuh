@@ -498,8 +498,8 @@ __global__ void __launch_bounds__(Cfg<DP, SLOTS>::kThreads, SLOTS == 2 ? 1 : 2)
         const int limit = row >= g.rows ? 0x7fffffff : gather ? t.len : TREE ? b.len : at.limit(a, b);
         const bool dead = TREE && !mafat_attn::live<TREE>(a, at);
         const int first_node = TREE ? mafat_attn::tree_first(a, b) : 0x7fffffff;
-        mafat_attn::Way way;
-        if (TREE && g.tree) way = mafat_attn::Way(a, b, at);
+        mafat_attn::WayAhead way;
+        if (TREE && g.tree) way = mafat_attn::WayAhead(a, b, at);
         const float c = a.scale_log2;
         const int n_tiles = slot < live ? t.n : 0;
         float from = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;  // the base in use: at most 2^8 below the maximum
