@@ -162,6 +162,11 @@ cudaError_t mafat_launch_overlapped(void (*fn)(P...), dim3 grid, dim3 block, siz
     return mafat_launch_clusters(1, fn, grid, block, smem, s, args...);
 }
 
+// CTAs of which two fit an SM and that are no more than the SMs: with this much shared memory each has an SM to itself.  Launched
+// while the one before ends, they would otherwise gather on the SMs that are free first: 6 x 7 requests of 24 nodes over 13517 states
+// (4 query and 2 key heads of 64 channels, fp32, 144 CTAs), one call behind another, took 870 us, 505 by themselves.
+constexpr int kMafatSms = 152, kMafatAlone = 116 * 1024 + 512;
+
 enum MafatNormQuant { MAFAT_NORM_PLAIN = 0, MAFAT_NORM_ROW = 1, MAFAT_NORM_BLOCK = 2 };
 
 int mafat_norm_max_cols();  // of a row
