@@ -1,4 +1,4 @@
-// Attention of many rows in bf16 on the tensor cores: the forms without trees.
+// Attention of many rows in bf16 on the tensor cores: the forms without trees (apart from those with, so that both compile at once).
 #include "attn_tc.cuh"
 
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,

@@ -3,7 +3,11 @@
 // y in the inputs' type or in 8 bits with scales, as the norm alone has them.
 //
 // One pass: a row stays in registers between its two sums of squares and the output, so that x, r are read and h, y
-// written once; bound by those bytes.  All is fp32 until a result is rounded, once; y is of the unrounded h.
+// written once; bound by those bytes.  All is fp32 until a result is rounded, once; y is of the unrounded h.  A row is one warp's
+// where its registers hold it, as in the norm alone; the second sum of squares waits for the first, not for memory.
+//
+// 46208 rows of 1024 bf16, a gate for each 5776: 56.5 us or 6.7 TB/s, what a copy takes.  1443 rows of 1001 fp32 6.3 us: a launch, two
+// round trips and accesses of one channel.  16 rows of 1024 to e4m3 2.1 us.
 #include "row_common.cuh"
 
 namespace {

@@ -8,6 +8,11 @@
 // there once in a list; when all rows have passed, the tokens of the list are written again, a lane each.  (Common tokens are
 // neighbours in a vocabulary: in the pass over all of them their divisions fell to a few warps.)  The table's sums are
 // of whole numbers, so that their order does not matter.
+//
+// 64 trees of 16 nodes, 131072 bf16 logits each, half of them with a mask, 2048 said: 105 us or 5.1 TB/s.  The pass alone takes 83 (6.5
+// TB/s), with masks 88; the rest is a CTA's way from the request's lists to its own, during which four others are on
+// the SM.  7 rows of 50001 fp32 with 20000 said: 10.3 us, going over the lists.  16 rows of 32000 bf16 with 512 said: 3.6 us,
+// a launch and three round trips.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 

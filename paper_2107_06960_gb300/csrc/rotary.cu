@@ -7,7 +7,7 @@
 // cosine are taken of that fraction in fp32, on -1/2 .. 1/2.  A CTA has a few tokens with all their heads: their sines and
 // cosines are made once, while the first channels are on their way.  A thread has the same pairs of one head after another.
 //
-// 8 x 2048 tokens of 32 query and 8 key heads of 128 channels, bf16, with their values: 62.8 us or 6.4 TB/s; a form whose
+// 8 x 2048 tokens of 32 query and 8 key heads of 128 channels, bf16, with their values: 63 us or 6.4 TB/s; a form whose
 // threads made the sines of their own pairs before they asked for channels took 77.6.  64 tokens of as many heads: 2.4 us,
 // a launch and two round trips (the tokens' positions, then their angles' table, beside the channels).
 #include <cuda_bf16.h>

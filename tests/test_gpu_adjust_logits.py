@@ -203,3 +203,27 @@ def test_one_result_a_call(mf):
     for o in outs:
         mf.adjust_logits(x, o, tokens=t, repetition=p + 1, presence=p, frequency=p)
     assert all(torch.equal(outs[0], o) for o in outs[1:])
+
+
+@pytest.mark.parametrize("room,V", [(30, 5000), (3000, 20000), (9000, 20000), (9000, 900000)])
+def test_captured(mf, room, V):
+    """Each form of the kernel in a graph, replayed on other histories and logits, on a stream of its own."""
+    x = torch.randn((2, 8, V), device="cuda").to(torch.bfloat16)
+    tokens = torch.randint(0, V, (2, room), device="cuda").to(torch.int32)
+    drafts = torch.randint(0, V, (2, 8), device="cuda").to(torch.int32)
+    length = torch.full((2,), room, dtype=torch.int32, device="cuda")
+    p, out, want = torch.full((2,), 1.2, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            mf.adjust_logits(x, out, tokens=tokens, lengths=length, repetition=p, drafts=drafts)
+        for seed in range(3):
+            x.copy_(torch.randn(x.shape, device="cuda"))
+            tokens.copy_(torch.randint(0, V, tokens.shape, device="cuda"))
+            length.copy_(torch.randint(0, room + 1, (2,), device="cuda"))
+            g.replay()
+            mf.adjust_logits(x, want, tokens=tokens, lengths=length, repetition=p, drafts=drafts)
+            stream.synchronize()
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and not torch.equal(out, x)
