@@ -1,7 +1,7 @@
 """GB300-native fused-tile execution of CNN layer groups (MAFAT, arXiv 2107.06960).
 
 A thin ctypes binding of ``libmafat.so`` (the C ABI declared in
-``include/mafat.h``): it only marshals arguments.  Every step of the hot path
+``include/mafat.h``): it only marshals arguments (``_match``, in C, looks at the tensors of a call that was made before).  Every step of the hot path
 runs in the library's CUDA kernels; there is no CPU fallback, and importing
 this package fails loudly when the library has not been built
 (``python -c "import __graft_entry__ as g; g.build()"``).
@@ -172,6 +172,10 @@ EXPORTED = [s[0] for s in _SIGNATURES]
 if not os.path.exists(LIB_PATH):
     raise ImportError("libmafat.so is not built (expected at %s); build it with "
                       "paper_2107_06960_gb300.build.build()" % LIB_PATH)
+try:
+    from . import _match
+except ImportError as e:
+    raise ImportError("the binding's _match is not built; build it with paper_2107_06960_gb300.build.build()") from e
 lib = ctypes.CDLL(LIB_PATH)
 for _name, _res, _args in _SIGNATURES:
     _f = getattr(lib, _name)
@@ -619,30 +623,55 @@ class PrefixAttention(_Attention):
             _launch_stream(stream, on, q)))
 
 
+MOST_CALLS = 16  # kept of a function or a plan
+
+
+def _look(t):
+    """(type, shape, strides or None for packed) of a tensor, as _match compares it."""
+    return None if t is None else (t.dtype, tuple(t.shape), None if t.is_contiguous() else tuple(t.stride()))
+
+
+def _keep(calls, tensors, rest, *what):
+    """Keeps a call that has been checked, by what its tensors look like, in front of the list `calls`; nothing of their
+    values or addresses."""
+    if all(t is None or hasattr(t, "dtype") for t in tensors):
+        calls.insert(0, (tuple(_look(t) for t in tensors), rest) + what)
+        del calls[MOST_CALLS:]
+
+
 class TreeAttention(PrefixAttention):
     """mafat_tree_plan / mafat_tree_run: attention of drafted tokens, a tree of up to n_q nodes for each request, to the prefix
     that neighbours share and to the request's own keys: all before the tree's, and of the tree's those that a
     node's bits name.  Made as PrefixAttention is."""
     _plan = "mafat_tree_plan"
 
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        self._calls = []
+
     def run(self, q, prefix_k, prefix_v, own_k, own_v, tree, out, nodes=None, prefix_len=None, prefix_mask=None,
             own_len=None, lse=None, stream=None):
         """tree [prefixes * requests][n_q][ceil(n_q / 32)] int32 words (or [1][n_q][...], one for all): bit j % 32 of word
         j / 32 of row t says that token t reads node j; nodes [prefixes * requests] int32, of each tree (None: n_q): its keys
         are the last of the own_len readable ones, and rows past them get 0.  The rest as in PrefixAttention."""
-        dt, i32_, mask, f32_ = self._types or self._torch()
-        (nq, sq), (npre, spk), (nown, sok) = self._q, self._pk, self._ok
-        on, n_q = self.device, nq[1]
-        shared = getattr(tree, "shape", nq)[0] == 1
-        _check(lib.mafat_tree_run(
-            self.handle, _addr("q", q, nq, dt, on, sq), _addr("prefix_k", prefix_k, npre, dt, on, spk),
-            _addr("prefix_v", prefix_v, npre, dt, on, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], i32_, on),
-            _addr("prefix_mask", prefix_mask, npre[:2], mask, on), _addr("own_k", own_k, nown, dt, on, sok),
-            _addr("own_v", own_v, nown, dt, on, self._ov[1]), _addr("own_len", own_len, nq[:1], i32_, on),
-            _addr("nodes", nodes, nq[:1], i32_, on),
-            _addr("tree", tree, (1 if shared else nq[0], n_q, (n_q + 31) // 32), i32_, on), int(shared),
-            _addr("out", out, nq, dt, on, self._out[1]), _addr("lse", lse, nq[:3], f32_, on),
-            _launch_stream(stream, on, q)))
+        tensors = q, prefix_k, prefix_v, prefix_len, prefix_mask, own_k, own_v, own_len, nodes, tree, out, lse
+        found = None if self.device is None else _match.find(self._calls, tensors, self.device, None)
+        if found:
+            (_, _, shared), a = found
+        else:
+            dt, i32_, mask, f32_ = self._types or self._torch()
+            (nq, sq), (npre, spk), (nown, sok) = self._q, self._pk, self._ok
+            on, n_q = self.device, nq[1]
+            shared = int(getattr(tree, "shape", nq)[0] == 1)
+            a = (_addr("q", q, nq, dt, on, sq), _addr("prefix_k", prefix_k, npre, dt, on, spk),
+                 _addr("prefix_v", prefix_v, npre, dt, on, self._pv[1]), _addr("prefix_len", prefix_len, npre[:1], i32_, on),
+                 _addr("prefix_mask", prefix_mask, npre[:2], mask, on), _addr("own_k", own_k, nown, dt, on, sok),
+                 _addr("own_v", own_v, nown, dt, on, self._ov[1]), _addr("own_len", own_len, nq[:1], i32_, on),
+                 _addr("nodes", nodes, nq[:1], i32_, on),
+                 _addr("tree", tree, (1 if shared else nq[0], n_q, (n_q + 31) // 32), i32_, on),
+                 _addr("out", out, nq, dt, on, self._out[1]), _addr("lse", lse, nq[:3], f32_, on))
+            _keep(self._calls, tensors, None, shared)
+        _check(lib.mafat_tree_run(self.handle, *a[:10], shared, *a[10:], _launch_stream(stream, self.device, q)))
 
 
 def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_group=0, eps=1e-6, stream=None):
@@ -711,38 +740,29 @@ def block_norm(x, residual, residual_out=None, post_weight=None, gate=None, bran
     scale_group as of rms_norm, in float8_e4m3fn.
 
     gate [cols], or [n][cols] of which each row is for rows / n neighbours.  Rows as of rms_norm."""
-    shape, dt, on = x.shape, x.dtype, x.get_device()
+    on = x.get_device()
     if on < 0 or on != _current_device():  # where kernels are launched
         raise MafatError(EINVAL, "x is on %s, which is not the current GPU" % x.device)
-    out_dt = None if y is None else y.dtype
-    # The common call, all packed: checked in one pass, as rms_norm's (5.9 us a call instead of 12).
-    packed = x.is_contiguous() and (y is None or (y.shape == shape and y.is_contiguous() and y.get_device() == on))
-    for t in (residual, residual_out):
-        packed = packed and (t is None or (t.dtype is dt and t.shape == shape and t.is_contiguous() and t.get_device() == on))
-    for t in (gate, post_weight, weight):
-        packed = packed and (t is None or (t.dtype is dt and t.is_contiguous() and t.get_device() == on))
-    if packed:
-        call = _block_norm_call(shape, dt, out_dt, None if gate is None else gate.shape, scale_group, eps, branch_scale,
-                                residual_scale, None)
-        if (post_weight is None or post_weight.shape == call[3]) and (weight is None or weight.shape == call[3]):
-            _check(lib.mafat_block_norm(
-                call[0], x.data_ptr(), None if residual is None else residual.data_ptr(),
-                None if post_weight is None else post_weight.data_ptr(), None if gate is None else gate.data_ptr(),
-                None if weight is None else weight.data_ptr(), None if residual_out is None else residual_out.data_ptr(),
-                None if y is None else y.data_ptr(), None if scales is None else _addr("scales", scales, call[2], call[1], on),
-                _launch_stream(stream, on, x)))
-            return
-    gate2 = gate if gate is None or gate.dim() != 1 else gate[None]
-    rows = tuple(_row_stride(*t) for t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y), ("gate", gate2)))
-    desc, f32_, scales_shape, weight_shape, gate_shape = _block_norm_call(
-        shape, dt, out_dt, None if gate is None else gate2.shape, scale_group, eps, branch_scale, residual_scale, rows)
-    sx, sr, so, sy, sg = [(st, 1) for st in rows]
-    _check(lib.mafat_block_norm(
-        desc, _addr("x", x, shape, dt, on, sx), _addr("residual", residual, shape, dt, on, sr),
-        _addr("post_weight", post_weight, weight_shape, dt, on), _addr("gate", gate2, gate_shape, dt, on, sg),
-        _addr("weight", weight, weight_shape, dt, on), _addr("residual_out", residual_out, shape, dt, on, so),
-        _addr("y", y, shape, out_dt, on, sy), _addr("scales", scales, scales_shape, f32_, on),
-        _launch_stream(stream, on, x)))
+    tensors, rest = (x, residual, post_weight, gate, weight, residual_out, y, scales), (scale_group, eps, branch_scale, residual_scale)
+    found = _match.find(_norm_calls, tensors, on, rest)
+    if found:
+        (_, _, desc), a = found
+    else:
+        shape, dt, out_dt = x.shape, x.dtype, None if y is None else y.dtype
+        gate2 = gate if gate is None or gate.dim() != 1 else gate[None]
+        rows = tuple(_row_stride(*t) for t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y), ("gate", gate2)))
+        desc, f32_, scales_shape, weight_shape, gate_shape = _block_norm_call(
+            shape, dt, out_dt, None if gate is None else gate2.shape, scale_group, eps, branch_scale, residual_scale, rows)
+        sx, sr, so, sy, sg = [(st, 1) for st in rows]
+        a = (_addr("x", x, shape, dt, on, sx), _addr("residual", residual, shape, dt, on, sr),
+             _addr("post_weight", post_weight, weight_shape, dt, on), _addr("gate", gate2, gate_shape, dt, on, sg),
+             _addr("weight", weight, weight_shape, dt, on), _addr("residual_out", residual_out, shape, dt, on, so),
+             _addr("y", y, shape, out_dt, on, sy), _addr("scales", scales, scales_shape, f32_, on))
+        _keep(_norm_calls, tensors, rest, desc)
+    _check(lib.mafat_block_norm(desc, *a, _launch_stream(stream, on, x)))
+
+
+_norm_calls, _logits_calls = [], []
 
 
 @functools.lru_cache(maxsize=256)
@@ -761,8 +781,7 @@ def _block_norm_call(shape, dt, out_dt, gate, scale_group, eps, branch_scale, re
     d = BlockNormDesc(struct_size=ctypes.sizeof(BlockNormDesc), cols=cols, rows=rows, gate_rows=rows // gates if gates else 0,
                       scale_group=scale_group, eps=eps, branch_scale=branch_scale, residual_scale=residual_scale)
     d.dtype, d.out_dtype = (c if isinstance(c, int) else -1 for c in (code.get(dt), code.get(dt if out_dt is None else out_dt)))
-    if strides is not None:
-        d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride, d.gate_stride = strides
+    d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride, d.gate_stride = strides
     return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1), (cols,), (gates or 1, cols)
 
 
@@ -788,7 +807,7 @@ class Rotary:
         _check(lib.mafat_rotary_plan(ctypes.byref(d), ctypes.byref(h)))
         self.handle, self.head_dim, self.dtype = h, head_dim, dtype
         self.device = None if dry_run else _current_device()
-        self._torch = None
+        self._torch, self._calls = None, []
 
     def frequencies(self):
         """(radians a position of each pair, the rotated channels' factor)."""
@@ -800,21 +819,18 @@ class Rotary:
         """positions [batch][n_q] int32; q, q_out [batch][n_q][heads_q][head_dim]; k, v [batch][n_q][heads_kv][head_dim]
         to places [batch][n_q] int32 of k_out, v_out [batch][room][heads_kv][head_dim] (outside them: not written; None:
         token t's is t).  Any strides that are multiples of 16 bytes; q_out may be q, and without places k_out k, v_out v."""
-        dt, i32_ = self._torch or self._types()
-        on, shape = self.device, positions.shape
-        laid, addresses = [], []
-        for t in (q, q_out, k, k_out, v, v_out):
-            if t is None:
-                laid.append(None)
-                addresses.append(None)
-                continue
-            if t.dtype is not dt or t.get_device() != on:
-                _addr(_ROTARY_NAMES[len(laid)], t, t.shape, dt, on, t.stride())  # says what is wrong
-            laid.append((t.shape, t.stride()))
-            addresses.append(t.data_ptr())
-        _check(lib.mafat_rotary_run(self.handle, _rotary_call(shape, self.head_dim, tuple(laid)),
-                                    _addr("positions", positions, shape, i32_, on), _addr("places", places, shape, i32_, on),
-                                    *addresses, _launch_stream(stream, on, positions)))
+        on, tensors = self.device, (positions, places, q, q_out, k, k_out, v, v_out)
+        found = None if on is None else _match.find(self._calls, tensors, on, None)
+        if found:
+            (_, _, call), a = found
+        else:
+            dt, i32_ = self._torch or self._types()
+            shape = positions.shape
+            call = _rotary_call(shape, self.head_dim, tuple(None if t is None else (t.shape, t.stride()) for t in tensors[2:]))
+            a = [_addr("positions", positions, shape, i32_, on), _addr("places", places, shape, i32_, on)]
+            a += [_addr(name, t, t.shape, dt, on, t.stride()) if t is not None else None for name, t in zip(_ROTARY_NAMES, tensors[2:])]
+            _keep(self._calls, tensors, None, call)
+        _check(lib.mafat_rotary_run(self.handle, call, *a, _launch_stream(stream, on, positions)))
 
     def _types(self):
         self._torch = _type(self.dtype), _type("int32")
@@ -875,22 +891,19 @@ def adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None, r
     on = logits.get_device()
     if on < 0 or on != _current_device():
         raise MafatError(EINVAL, "logits are on %s, which is not the current GPU" % logits.device)
-    dt, out_dt, shape = logits.dtype, out.dtype, logits.shape
-    desc, wanted = _logits_call(
-        shape, logits.stride(), out.stride(), dt, out_dt, None if tokens is None else tokens.shape,
-        None if tree is None else tree.shape, None if bias_ids is None else bias_ids.shape,
-        None if masks is None else masks.shape, None if mask_rows is None else mask_rows.dim())
-    addresses = []
-    for t, w in zip((tokens, lengths, prompt_lengths, repetition, presence, frequency, drafts, tree, bias_ids, bias, masks, mask_rows), wanted):
-        if t is None:
-            addresses.append(None)
-        elif t.dtype is w[2] and t.shape == w[1] and t.get_device() == on and t.is_contiguous():
-            addresses.append(t.data_ptr())
-        else:
-            addresses.append(_addr(w[0], t, w[1], w[2], on))
-    if out.get_device() != on or out.shape != shape:
-        _addr("out", out, shape, out_dt, on, out.stride())
-    _check(lib.mafat_adjust_logits(desc, logits.data_ptr(), *addresses, out.data_ptr(), _launch_stream(stream, on, logits)))
+    tensors = (logits, tokens, lengths, prompt_lengths, repetition, presence, frequency, drafts, tree, bias_ids, bias, masks, mask_rows, out)
+    found = _match.find(_logits_calls, tensors, on, None)
+    if found:
+        (_, _, desc), a = found
+    else:
+        desc, wanted = _logits_call(
+            logits.shape, logits.stride(), out.stride(), logits.dtype, out.dtype, None if tokens is None else tokens.shape,
+            None if tree is None else tree.shape, None if bias_ids is None else bias_ids.shape,
+            None if masks is None else masks.shape, None if mask_rows is None else mask_rows.dim())
+        a = [logits.data_ptr()] + [_addr(w[0], t, w[1], w[2], on) for t, w in zip(tensors[1:-1], wanted)]
+        a.append(_addr("out", out, logits.shape, out.dtype, on, out.stride()))
+        _keep(_logits_calls, tensors, None, desc)
+    _check(lib.mafat_adjust_logits(desc, *a, _launch_stream(stream, on, logits)))
 
 
 @functools.lru_cache(maxsize=256)

@@ -12,12 +12,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmafat.so")
+MATCH = os.path.join(HERE, "_match" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))  # the binding's, C for CPython
 SOURCES = ["planner.cpp", "order.cpp", "runtime.cpp", "search.cpp", "kernel_fp32.cu", "kernel_tc.cu", "noalloc.cu",
            "attention.cpp", "attn_simt.cu", "attn_rows.cu", "attn_tc.cu", "attn_tc_tree.cu", "attn_join.cu", "rms_norm.cu",
            "decode.cpp", "block_norm.cu", "rotary.cu", "logits.cu"]
@@ -54,8 +56,21 @@ def _compile(src, extra):
     return obj
 
 
+def _build_match(force):
+    src = os.path.join(CSRC, "match.c")
+    if not force and not _stale(MATCH, [src, __file__]):
+        return
+    tmp = MATCH + ".tmp.%d" % os.getpid()
+    cmd = ["gcc", "-O2", "-std=c11", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"], src, "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("gcc failed for match.c:\n%s%s" % (r.stdout, r.stderr))
+    os.replace(tmp, MATCH)
+
+
 def build(force: bool = False, extra=None) -> str:
     """Compile (if needed) and return the path of libmafat.so."""
+    _build_match(force)
     extra = list(extra or [])
     os.makedirs(BUILD, exist_ok=True)
     if force:

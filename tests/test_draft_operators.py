@@ -305,3 +305,55 @@ def test_forms_that_are_taken(mf, monkeypatch):
     mf.adjust_logits(OnGpu(torch.zeros(2, 100)), OnGpu(torch.zeros(2, 100)), masks=OnGpu(torch.zeros(5, 4, dtype=torch.int32)),
                      mask_rows=OnGpu(torch.zeros(2, dtype=torch.int32)), stream=0, **two)
     assert seen[-1][0]._obj.n_q == 1
+
+
+def test_calls_that_are_kept_are_told_apart(mf, monkeypatch):
+    """More kinds of calls than are kept, in turn: each reaches the library with its own sizes, strides and addresses."""
+    monkeypatch.setattr(mf, "_current_device", lambda: 0)
+    seen = []
+    for entry in ("mafat_block_norm", "mafat_adjust_logits", "mafat_rotary_run"):
+        monkeypatch.setattr(mf.lib, entry, lambda *a: seen.append(a) or mf.OK)
+    rotary = mf.Rotary(64, dry_run=True)
+    rotary.device = 0
+    kinds = [(rows, cols, pad) for rows in (2, 3, 5) for cols in (64, 72, 96) for pad in (0, 8)]
+    assert len(kinds) > mf.MOST_CALLS
+    for turn in range(3):
+        for rows, cols, pad in kinds:
+            x, r, h = (OnGpu(torch.zeros(rows, cols + pad)[:, :cols]) for _ in range(3))
+            for scale in (1.0, 0.5):
+                mf.block_norm(x, r, h, branch_scale=scale, stream=0)
+                d = seen[-1][0]._obj
+                assert (d.rows, d.cols, d.branch_scale) == (rows, cols, scale) and d.x_stride == cols + pad
+                assert list(seen[-1][1:3]) == [x.data_ptr(), r.data_ptr()] and seen[-1][6] == h.data_ptr() and seen[-1][4] is None
+            out = OnGpu(torch.zeros(rows, cols))
+            tokens = OnGpu(torch.zeros(rows, 1 + turn, dtype=torch.int32))
+            mf.adjust_logits(x, out, tokens=tokens, stream=0)
+            d = seen[-1][0]._obj
+            assert (d.batch, d.vocab, d.room, d.logits_stride, d.out_stride) == (rows, cols, 1 + turn, cols + pad, cols)
+            assert seen[-1][1] == x.data_ptr() and seen[-1][2] == tokens.data_ptr() and seen[-1][-2] == out.data_ptr()
+            q = OnGpu(torch.zeros(rows, 2, cols // 8, 64 + pad, dtype=torch.bfloat16)[..., :64])
+            o = OnGpu(torch.zeros(rows, 2, cols // 8, 64, dtype=torch.bfloat16))
+            at = OnGpu(torch.zeros(rows, 2, dtype=torch.int32))
+            rotary.run(at, q=q, q_out=o, stream=0)
+            d = seen[-1][1]._obj
+            assert (d.batch, d.heads_q, d.q_strides[2]) == (rows, cols // 8, 64 + pad) and seen[-1][4:6] == (q.data_ptr(), o.data_ptr())
+    assert len(mf._norm_calls) <= mf.MOST_CALLS and len(rotary._calls) <= mf.MOST_CALLS
+
+
+def test_what_is_not_a_tensor(mf, monkeypatch):
+    """Raw addresses are the caller's word where shapes are not asked for; anything else is an error, not a match."""
+    plan = mf.TreeAttention(2, 2, 5, 30, 10, 4, 2, 64, dry_run=True)
+    seen = []
+    monkeypatch.setattr(mf.lib, "mafat_tree_run", lambda *a: seen.append(a) or mf.OK)
+    plan.device = 0
+    plan._types = mf._type(mf.BF16), mf._type("int32"), mf._type("mask"), mf._type(mf.FP32)
+    for _ in range(2):
+        plan.run(*[4096 * (i + 1) for i in range(7)], stream=0)
+    assert len(seen) == 2 and not plan._calls and seen[0][1] == 4096
+    with pytest.raises(TypeError):
+        mf._match.find([], [], 0, None)
+    with pytest.raises(TypeError):
+        mf._match.find([], (), "0", None)
+    assert mf._match.find([((None,), 1)], (None,), 0, 2) is None and mf._match.find([((None,), 1)], (None,), 0, 1) == (((None,), 1), (None,))
+    assert mf._match.find([((None, None), 1)], (None,), 0, 1) is None
+    assert mf._match.find([(((torch.float32, (2,), None),), 1)], (object(),), 0, 1) is None
