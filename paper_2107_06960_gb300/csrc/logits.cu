@@ -11,7 +11,7 @@
 //
 // 64 trees of 16 nodes, 131072 bf16 logits each, half of them with a mask, 2048 said: 105 us or 5.1 TB/s.  The pass alone takes 83 (6.5
 // TB/s), with masks 88; the rest is a CTA's way from the request's lists to its own, during which four others are on
-// the SM.  7 rows of 50001 fp32 with 20000 said: 10.3 us, going over the lists.  16 rows of 32000 bf16 with 512 said: 3.6 us,
+// the SM.  7 rows of 50001 fp32 with 20000 said: 7.7 us, going over the lists.  16 rows of 32000 bf16 with 512 said: 3.6 us,
 // a launch and three round trips.
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -134,6 +134,10 @@ struct Run {
 template <class T, class O, int THREADS, int N, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_constant__ MafatLogitsArgs a) {
     using S = Run<T, THREADS, N>;
+    // Where histories are long the list is made of the whole table, not with each token, whose addition then has to come back
+    // first: 7 rows of 50001 with 20000 said 7.7 us instead of 10.3, 95 of 128890 with 21842 53 instead of 59 (16 rows of 32000 with
+    // 512, in 256 threads: 3.8 instead of 3.6).
+    constexpr bool kScan = THREADS > 256;
     extern __shared__ __align__(16) uint32_t table[];
     uint16_t* list = (uint16_t*)(table + S::kTokens);
     __shared__ int listed, masks[kMostRows];
@@ -184,7 +188,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
     if (any) {
         auto place = [&](int32_t id) { return (uint32_t)id - (uint32_t)s.first; };  // kTokens and more: elsewhere
         auto note = [&](uint32_t at, uint32_t was) {
-            if (was == 0u) list[atomicAdd(&listed, 1)] = (uint16_t)at;
+            if (!kScan && was == 0u) list[atomicAdd(&listed, 1)] = (uint16_t)at;
         };
         if (a.bias_ids) {
             for (int i = tid; i < a.n_bias; i += THREADS) {
@@ -199,7 +203,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
             for (int i = 0; i < kAhead; ++i) {
                 const int k = from + i * THREADS + tid;
                 const uint32_t at = place(said[i]);
-                if (k < len && at < (uint32_t)S::kTokens)
+                if (at < (uint32_t)S::kTokens && k < len)
                     note(at, k < prompt ? atomicOr(table + at, kPrompt) : atomicAdd(table + at, 1u));
             }
         }
@@ -236,6 +240,32 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
     };
     if (any) {
         __syncthreads();  // table and list are there
+        if constexpr (kScan) {
+            uint32_t hits = 0u;  // of the thread's words
+            static_assert(N * S::V <= 32, "a bit each");
+#pragma unroll
+            for (int k = 0; k < N * S::V / 4; ++k) {
+                const uint4 w = *reinterpret_cast<const uint4*>(table + (k * THREADS + tid) * 4);
+                hits |= ((w.x ? 1u : 0u) | (w.y ? 2u : 0u) | (w.z ? 4u : 0u) | (w.w ? 8u : 0u)) << (4 * k);
+            }
+            const int mine = __popc(hits);
+            if (__any_sync(0xffffffffu, mine)) {
+                int upto = mine;
+#pragma unroll
+                for (int w = 1; w < 32; w *= 2) {
+                    const int x = __shfl_up_sync(0xffffffffu, upto, w);
+                    if (tid % 32 >= w) upto += x;
+                }
+                int at = 0;
+                if (tid % 32 == 31) at = atomicAdd(&listed, upto);
+                at = __shfl_sync(0xffffffffu, at, 31) + upto - mine;
+                for (uint32_t left = hits; left; left &= left - 1u) {
+                    const int bit = __ffs(left) - 1;
+                    list[at++] = (uint16_t)((bit / 4 * THREADS + tid) * 4 + bit % 4);
+                }
+            }
+            __syncthreads();
+        }
         n = listed;
         if (n == 0) t = rows;
         fetch();
@@ -321,18 +351,20 @@ cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_
 
 // Each CTA goes over the whole history: the longer that is, the more threads it has, and the more tokens where there are many
 // logits.  256, 512 and 1024 threads (1024 with one access each, with four), in us:
-//   64 x 16 rows of 131072 bf16, 2048 said           105, 122, 140, 128      16 rows of 32000, 512 said     3.6, 4.0, 4.7, 9.4
-//   102 rows of 111872 bf16, 6305 said              34.8, 33.3, 49.1, 36.2   4 x 27 of 8892 fp32, 5139      13.6, 12.5, 13.0, 9.7
-//   7 rows of 50001 fp32, 20000 said                20.3, 13.6, 10.4, 15.8   5 x 24 of 40256 bf16, 16270    39.5, 31.5, 25.1, 37.9
-//   95 rows of 128890 fp32, 21842 said               104, 89, 117, 59        40 x 36 of 21617 bf16, 8686    159, 151, 207, 145
+//   64 x 16 rows of 131072 bf16, 2048 said           105, 122, 139, 135      16 rows of 32000, 512 said     3.6, 4.4, 5.2, 9.9
+//   102 rows of 111872 bf16, 6305 said              34.8, 32.7, 49.8, 36.7   4 x 27 of 8892 fp32, 5139      13.5, 11.7, 12.8, 9.6
+//   7 rows of 50001 fp32, 20000 said                20.3,  9.5,  7.8, 13.1   57 of 25809 bf16, 24721        34.4, 19.4, 20.5, 23.9
+//   95 rows of 128890 fp32, 21842 said               104,  75,  107,  53     40 x 36 of 21617 bf16, 8686    158, 142, 206, 147
+//   5 x 24 rows of 40256 bf16, 16270 said           39.1, 27.3, 22.8, 34.4   15 x 24 of 11386 bf16, 13653   43.0, 36.0, 44.0, 41.7
 template <class T, class O>
 cudaError_t launch_all(MafatLogitsArgs& a, int64_t batch, cudaStream_t s) {
     constexpr int kSms = 152;
     const int said = a.tokens ? a.room : 0;
     if (said <= 2048) return launch<T, O, 256, 2, 5>(a, batch, 4 * 5 * kSms, s);
-    if (said <= 8192) return launch<T, O, 512, 2, 2>(a, batch, 4 * kSms, s);
-    if (batch * a.n_q * a.vocab * (int64_t)sizeof(T) <= 16 << 20) return launch<T, O, 1024, 1, 1>(a, batch, kSms * 9 / 10, s);
-    return launch<T, O, 1024, 4, 1>(a, batch, 4 * kSms, s);
+    const int64_t bytes = batch * a.n_q * a.vocab * (int64_t)sizeof(T);
+    if (said > 8192 && bytes <= 4 << 20) return launch<T, O, 1024, 1, 1>(a, batch, kSms * 9 / 10, s);
+    if (said > 16384 && bytes > 32 << 20) return launch<T, O, 1024, 4, 1>(a, batch, 4 * kSms, s);
+    return launch<T, O, 512, 2, 2>(a, batch, 4 * kSms, s);
 }
 
 }  // namespace
