@@ -227,3 +227,10 @@ def test_captured(mf, room, V):  # of 16 rows
             mf.adjust_logits(x, want, tokens=tokens, lengths=length, repetition=p, drafts=drafts)
             stream.synchronize()
             assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and not torch.equal(out, x)
+
+
+@pytest.mark.parametrize("dt,out_dt", TYPES)
+@pytest.mark.parametrize("B,T,V,room", [(3, 2, 5000, 9000), (2, 5, 4100, 2049), (2, 3, 9001, 8193), (1, 17, 1000001, 17000)])
+def test_long_histories(mf, dt, out_dt, B, T, V, room):
+    """The forms of more threads, the last of which takes more than 32 MiB of logits."""
+    _logits(mf, B, T, V, dt, out_dt, room=room, n_bias=20, n_masks=3, drafts="tree" if T > 1 else None, lengths=[room - 5] * B, prompts=[room // 3] * B)
