@@ -275,7 +275,7 @@ mafat_status plan_segment(mafat_attn_s& p, AttnSegPlan& g, const Common& c, int 
 // a token over 1444 (16 and 4 of 64) 7.3, 15.5; 8 of 64 over 3 x 13852 (8 and 4 of 128) 75, 133.
 // Two launches whose first has whole results were measured to take 1 to 1.45 times what the model has for them (with
 // parts, the launch to join them, which it counts, falls away).
-constexpr double kTwoLaunches = 1.2, kClusterShare = 0.8;
+constexpr double kTwoLaunches = 1.2, kClusterShare = 0.8, kShortShare = 0.9, kShortItemUs = 1.9;
 void plan_both(mafat_attn_s& p, const Common& c, int sms) {
     if (p.dtype != MAFAT_BF16 || p.n_run != 2 || c.splits != 0 || c.kernel == MAFAT_ATTN_ROWS) return;
     const AttnSegPlan &first = p.seg[p.run[0]], &own = p.seg[p.run[1]];
@@ -302,7 +302,9 @@ void plan_both(mafat_attn_s& p, const Common& c, int sms) {
     // Few rows of trees: clusters that split both sets' keys.  In us, as above (no clusters) and in clusters: a tree of 8 nodes over
     // 1444 + 96 keys (16 and 4 heads of 64) 7.5, 6.9; 8 of them (8 and 2 of 128) 13.4, 10.1; 4 x 2 trees of 3 over 96 + 116 (8 and 2 of
     // 64) 6.0, 5.4; 5 of 3 over 4663 + 4 (8 and 1 of 40) 9.8, 11.3.  Of 35 drawn plans they were slower in all whose time by the
-    // model was more than kClusterShare of the others', and in 3 of the 28 below it, by up to 0.8.
+    // model was more than kClusterShare of the others', and in 3 of the 28 below it, by up to 0.8.  Many short items, one after another
+    // in a CTA, also in one launch: 8 x 30 trees of a node over 50 + 40 (8 and 2 of 64) 13.2, 8.7; 4 x 13 of 2 over 18 + 8 (8 heads of
+    // 128) 14.2, 11.2; 43 of 5 over 22 + 41 (32 and 8 of 64) 11.8, 13.8.
     if (p.kind != kTree || c.kernel == MAFAT_ATTN_TILES || (int64_t)first.n + own.n > kMaxI32 / 16) return;
     Model m{};
     m.sh = shape_of(kRows, p.dim);
@@ -310,18 +312,22 @@ void plan_both(mafat_attn_s& p, const Common& c, int sms) {
     m.items = (int64_t)own.n_seq * p.heads_kv * row_tiles(m.sh, own.rows);
     m.tiles = ((int64_t)first.n + m.sh.keys - 1) / m.sh.keys + ((int64_t)own.n + m.sh.keys - 1) / m.sh.keys;
     m.bytes = 4. * p.heads_kv * p.dim * ((double)own.n_seq * first.n + (double)own.n_seq * own.n);
-    best *= kClusterShare;
-    for (int32_t n = kMostCluster; n > 1; n /= 2) {
-        const double us = m.us(n) + kClusterJoinUs;
-        if (n > m.tiles || m.items * n > (int64_t)sms * m.sh.ctas || us >= best) continue;
-        best = us;
+    double least = best;
+    for (int32_t n = kMostCluster; n > 0; n /= 2) {
+        const int64_t slots = (int64_t)sms * m.sh.ctas;
+        if (n > 1 ? n > m.tiles || m.items * n > slots : m.items > kMaxI32 / 4) continue;
+        // of items of few tiles the start and the end are not hidden behind each other's copies
+        const double us = n > 1 ? m.us(n) + kClusterJoinUs : m.us(1) + (double)((m.items + slots - 1) / slots) * kShortItemUs;
+        if (us >= least || us >= (n > 1 ? kClusterShare : kShortShare) * best) continue;
+        least = us;
         p.both = own;
         p.both.kernel = kRows;
         p.both.row_tiles = (int32_t)row_tiles(m.sh, own.rows);
         p.both.splits = p.both_cluster = n;
         p.both.part0 = 0;
         p.both.cut = 0;
-        p.both.items = p.both.ctas = (int32_t)(m.items * n);
+        p.both.items = (int32_t)(m.items * n);
+        p.both.ctas = n > 1 ? p.both.items : std::min(p.both.items, sms * m.sh.ctas);
     }
 }
 

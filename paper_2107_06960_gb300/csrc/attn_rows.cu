@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
 #pragma unroll 1
     for (Items it; it.item < (uint32_t)g.items; it.step(), which ^= 1u) {
         mafat_attn::Block b(a, Sets<Prefix>::item(a, it.item), 16, kBN, table);
-        if constexpr (kBoth) Sets<Prefix>(a, b, prefix);
+        const Sets<Prefix> now(a, b, prefix);  // the copies may be at the next item's
         mafat_attn::leave_dead<TREE>(a, b);
         const uint8_t* mask = g.mask ? g.mask + (int64_t)b.seq * g.n : nullptr;
         const int first = b.key0 + warp * kRun;
@@ -324,11 +324,11 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const __grid_consta
             int key = first + i * kBN, len = b.len;
             bool own = true;  // the request's keys
             if constexpr (kBoth) {
-                own = !sets.of_prefix(key);
+                own = !now.of_prefix(key);
                 if (own)
-                    key -= sets.own0;
+                    key -= now.own0;
                 else
-                    len = sets.len0;
+                    len = now.len0;
             }
             const uint32_t st = ring + stage * (2 * C::kMatrix);
             if (++stage == (uint32_t)C::kStages) stage = 0u;
@@ -529,8 +529,9 @@ cudaError_t launch_form(const MafatAttnArgs& a, int ctas, cudaStream_t s) {
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, int ctas, const MafatRowsPrefix* prefix, cudaStream_t s) {
     if (prefix)
-        return mafat_launch_clusters(a.cluster, attn_rows_kernel<DP, true, true, MafatRowsPrefix>, (unsigned)ctas, kThreads,
-                                     Cfg<DP, true>::kSmem, s, a, *prefix);
+        return mafat_launch_clusters(
+            a.cluster, a.cluster > 1 ? attn_rows_kernel<DP, true, true, MafatRowsPrefix> : attn_rows_kernel<DP, false, true, MafatRowsPrefix>,
+            (unsigned)ctas, kThreads, a.cluster > 1 ? Cfg<DP, true>::kSmem : Cfg<DP, false>::kSmem, s, a, *prefix);
     return a.tree ? launch_form<DP, true>(a, ctas, s) : launch_form<DP, false>(a, ctas, s);
 }
 template <int DP, bool TREE>
@@ -544,6 +545,9 @@ template <int DP>
 cudaError_t prepare() {
     cudaError_t e = prepare_form<DP, false>();
     if (e != cudaSuccess || (e = prepare_form<DP, true>()) != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(attn_rows_kernel<DP, false, true, MafatRowsPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             Cfg<DP, false>::kSmem);
+    if (e != cudaSuccess) return e;
     return cudaFuncSetAttribute(attn_rows_kernel<DP, true, true, MafatRowsPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 Cfg<DP, true>::kSmem);
 }

@@ -189,3 +189,13 @@ def test_keys_that_idle_sms_take(mf, D, P, lens):
     o, _, plan = _tree(mf, 2, 32, 16, P, 100, 32, 8, D, mf.BF16, prefix_len=lens, nodes=[1 + (5 * b) % 16 for b in range(64)], poison=True)
     s = plan.stats()
     assert s["splits"][0] == 2 and s["ctas"][0] % 2 == 0 and s["ctas"][0] // 2 < 152
+
+
+@pytest.mark.parametrize("G,R,T,P,S,H,Hk,D", [(8, 30, 1, 50, 40, 8, 2, 64), (4, 13, 2, 18, 8, 8, 8, 128), (4, 27, 4, 105, 10, 16, 4, 128), (6, 33, 4, 17, 24, 4, 2, 72)])
+def test_many_short_items(mf, G, R, T, P, S, H, Hk, D):
+    """One launch of CTAs that take several items, each over both sets of keys; sets of every length, also of none."""
+    n = G * R
+    assert mf.TreeAttention(G, R, T, P, S, H, Hk, D, dry_run=True).stats()["whole_ctas"] == 304
+    _tree(mf, G, R, T, P, S, H, Hk, D, mf.BF16, own_len=[(11 * b) % (S + 2) for b in range(n)], prefix_len=[(P * g) // (G - 1) for g in range(G)],
+          nodes=[(3 * b) % (T + 1) for b in range(n)], poison=True, repeat=2)
+    _tree(mf, G, R, T, P, S, H, Hk, D, mf.BF16, poison=True)
