@@ -1,8 +1,9 @@
 """GB300-native fused-tile execution of CNN layer groups (MAFAT, arXiv 2107.06960).
 
 A thin ctypes binding of ``libmafat.so`` (the C ABI declared in
-``include/mafat.h``): it only marshals arguments (``_match``, in C, looks at the tensors of a call that was made before).  Every step of the hot path
-runs in the library's CUDA kernels; there is no CPU fallback, and importing
+``include/mafat.h``): it only marshals arguments (``_match``, in C, makes calls
+that are like one made before).  Every step of the hot path runs in the
+library's CUDA kernels; there is no CPU fallback, and importing
 this package fails loudly when the library has not been built
 (``python -c "import __graft_entry__ as g; g.build()"``).
 
@@ -181,6 +182,9 @@ for _name, _res, _args in _SIGNATURES:
     _f = getattr(lib, _name)
     _f.restype = _res
     _f.argtypes = _args
+_match.bind(*(ctypes.cast(getattr(lib, n), vp).value for n in (
+    "mafat_block_norm", "mafat_rotary_run", "mafat_tree_run", "mafat_adjust_logits")))
+_NORM, _ROTARY, _TREE, _LOGITS = range(4)  # of _match
 
 
 class MafatError(RuntimeError):
@@ -631,11 +635,11 @@ def _look(t):
     return None if t is None else (t.dtype, tuple(t.shape), None if t.is_contiguous() else tuple(t.stride()))
 
 
-def _keep(calls, tensors, rest, *what):
+def _keep(calls, tensors, rest, what, *owned):
     """Keeps a call that has been checked, by what its tensors look like, in front of the list `calls`; nothing of their
-    values or addresses."""
+    values or addresses.  what: a descriptor's address, or a flag, of which `owned` is kept with it."""
     if all(t is None or hasattr(t, "dtype") for t in tensors):
-        calls.insert(0, (tuple(_look(t) for t in tensors), rest) + what)
+        calls.insert(0, (tuple(_look(t) for t in tensors), rest, what) + owned)
         del calls[MOST_CALLS:]
 
 
@@ -655,10 +659,10 @@ class TreeAttention(PrefixAttention):
         j / 32 of row t says that token t reads node j; nodes [prefixes * requests] int32, of each tree (None: n_q): its keys
         are the last of the own_len readable ones, and rows past them get 0.  The rest as in PrefixAttention."""
         tensors = q, prefix_k, prefix_v, prefix_len, prefix_mask, own_k, own_v, own_len, nodes, tree, out, lse
-        found = None if self.device is None else _match.find(self._calls, tensors, self.device, None)
-        if found:
-            (_, _, shared), a = found
-        else:
+        stream, status = _launch_stream(stream, self.device, q), None
+        if self.device is not None:
+            status = _match.run(_TREE, self._calls, tensors, self.device, None, self.handle and self.handle.value, stream)
+        if status is None:
             dt, i32_, mask, f32_ = self._types or self._torch()
             (nq, sq), (npre, spk), (nown, sok) = self._q, self._pk, self._ok
             on, n_q = self.device, nq[1]
@@ -670,8 +674,9 @@ class TreeAttention(PrefixAttention):
                  _addr("nodes", nodes, nq[:1], i32_, on),
                  _addr("tree", tree, (1 if shared else nq[0], n_q, (n_q + 31) // 32), i32_, on),
                  _addr("out", out, nq, dt, on, self._out[1]), _addr("lse", lse, nq[:3], f32_, on))
+            status = lib.mafat_tree_run(self.handle, *a[:10], shared, *a[10:], stream)
             _keep(self._calls, tensors, None, shared)
-        _check(lib.mafat_tree_run(self.handle, *a[:10], shared, *a[10:], _launch_stream(stream, self.device, q)))
+        _check(status)
 
 
 def rms_norm(x, weight, y, residual=None, residual_out=None, scales=None, scale_group=0, eps=1e-6, stream=None):
@@ -744,10 +749,9 @@ def block_norm(x, residual, residual_out=None, post_weight=None, gate=None, bran
     if on < 0 or on != _current_device():  # where kernels are launched
         raise MafatError(EINVAL, "x is on %s, which is not the current GPU" % x.device)
     tensors, rest = (x, residual, post_weight, gate, weight, residual_out, y, scales), (scale_group, eps, branch_scale, residual_scale)
-    found = _match.find(_norm_calls, tensors, on, rest)
-    if found:
-        (_, _, desc), a = found
-    else:
+    stream = _launch_stream(stream, on, x)
+    status = _match.run(_NORM, _norm_calls, tensors, on, rest, None, stream)
+    if status is None:
         shape, dt, out_dt = x.shape, x.dtype, None if y is None else y.dtype
         gate2 = gate if gate is None or gate.dim() != 1 else gate[None]
         rows = tuple(_row_stride(*t) for t in (("x", x), ("residual", residual), ("residual_out", residual_out), ("y", y), ("gate", gate2)))
@@ -758,8 +762,9 @@ def block_norm(x, residual, residual_out=None, post_weight=None, gate=None, bran
              _addr("post_weight", post_weight, weight_shape, dt, on), _addr("gate", gate2, gate_shape, dt, on, sg),
              _addr("weight", weight, weight_shape, dt, on), _addr("residual_out", residual_out, shape, dt, on, so),
              _addr("y", y, shape, out_dt, on, sy), _addr("scales", scales, scales_shape, f32_, on))
-        _keep(_norm_calls, tensors, rest, desc)
-    _check(lib.mafat_block_norm(desc, *a, _launch_stream(stream, on, x)))
+        status = lib.mafat_block_norm(desc, *a, stream)
+        _keep(_norm_calls, tensors, rest, ctypes.addressof(desc), desc)
+    _check(status)
 
 
 _norm_calls, _logits_calls = [], []
@@ -782,7 +787,7 @@ def _block_norm_call(shape, dt, out_dt, gate, scale_group, eps, branch_scale, re
                       scale_group=scale_group, eps=eps, branch_scale=branch_scale, residual_scale=residual_scale)
     d.dtype, d.out_dtype = (c if isinstance(c, int) else -1 for c in (code.get(dt), code.get(dt if out_dt is None else out_dt)))
     d.x_stride, d.residual_stride, d.residual_out_stride, d.y_stride, d.gate_stride = strides
-    return ctypes.byref(d), _type(FP32), (rows, -(-cols // 128) if scale_group else 1), (cols,), (gates or 1, cols)
+    return d, _type(FP32), (rows, -(-cols // 128) if scale_group else 1), (cols,), (gates or 1, cols)
 
 
 class Rotary:
@@ -820,17 +825,18 @@ class Rotary:
         to places [batch][n_q] int32 of k_out, v_out [batch][room][heads_kv][head_dim] (outside them: not written; None:
         token t's is t).  Any strides that are multiples of 16 bytes; q_out may be q, and without places k_out k, v_out v."""
         on, tensors = self.device, (positions, places, q, q_out, k, k_out, v, v_out)
-        found = None if on is None else _match.find(self._calls, tensors, on, None)
-        if found:
-            (_, _, call), a = found
-        else:
+        stream, status = _launch_stream(stream, on, positions), None
+        if on is not None:
+            status = _match.run(_ROTARY, self._calls, tensors, on, None, self.handle and self.handle.value, stream)
+        if status is None:
             dt, i32_ = self._torch or self._types()
             shape = positions.shape
             call = _rotary_call(shape, self.head_dim, tuple(None if t is None else (t.shape, t.stride()) for t in tensors[2:]))
             a = [_addr("positions", positions, shape, i32_, on), _addr("places", places, shape, i32_, on)]
             a += [_addr(name, t, t.shape, dt, on, t.stride()) if t is not None else None for name, t in zip(_ROTARY_NAMES, tensors[2:])]
-            _keep(self._calls, tensors, None, call)
-        _check(lib.mafat_rotary_run(self.handle, call, *a, _launch_stream(stream, on, positions)))
+            status = lib.mafat_rotary_run(self.handle, call, *a, stream)
+            _keep(self._calls, tensors, None, ctypes.addressof(call), call)
+        _check(status)
 
     def _types(self):
         self._torch = _type(self.dtype), _type("int32")
@@ -875,7 +881,7 @@ def _rotary_call(positions, dim, laid):
         if inner != 1 or any(n > 1 and s < dim for n, s in zip(sizes, steps)):
             raise MafatError(EINVAL, "%s: a head's channels must be contiguous, and not shared" % name)
         getattr(c, name + "_strides")[:] = [s if n > 1 else max(s, dim) for n, s in zip(sizes, steps)]
-    return ctypes.byref(c)
+    return c
 
 
 def adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None, repetition=None, presence=None, frequency=None,
@@ -892,18 +898,18 @@ def adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None, r
     if on < 0 or on != _current_device():
         raise MafatError(EINVAL, "logits are on %s, which is not the current GPU" % logits.device)
     tensors = (logits, tokens, lengths, prompt_lengths, repetition, presence, frequency, drafts, tree, bias_ids, bias, masks, mask_rows, out)
-    found = _match.find(_logits_calls, tensors, on, None)
-    if found:
-        (_, _, desc), a = found
-    else:
+    stream = _launch_stream(stream, on, logits)
+    status = _match.run(_LOGITS, _logits_calls, tensors, on, None, None, stream)
+    if status is None:
         desc, wanted = _logits_call(
             logits.shape, logits.stride(), out.stride(), logits.dtype, out.dtype, None if tokens is None else tokens.shape,
             None if tree is None else tree.shape, None if bias_ids is None else bias_ids.shape,
             None if masks is None else masks.shape, None if mask_rows is None else mask_rows.dim())
         a = [logits.data_ptr()] + [_addr(w[0], t, w[1], w[2], on) for t, w in zip(tensors[1:-1], wanted)]
         a.append(_addr("out", out, logits.shape, out.dtype, on, out.stride()))
-        _keep(_logits_calls, tensors, None, desc)
-    _check(lib.mafat_adjust_logits(desc, *a, _launch_stream(stream, on, logits)))
+        status = lib.mafat_adjust_logits(desc, *a, stream)
+        _keep(_logits_calls, tensors, None, ctypes.addressof(desc), desc)
+    _check(status)
 
 
 @functools.lru_cache(maxsize=256)
@@ -924,7 +930,7 @@ def _logits_call(shape, in_strides, out_strides, dt, out_dt, tokens, tree, bias,
     d.logits_stride, d.out_stride = (_logits_stride(n, shape, st) for n, st in (("logits", in_strides), ("out", out_strides)))
     of_batch, of_rows, of_bias = (batch,), (batch, n_q), (1 if d.bias_shared else batch, d.n_bias)
     f32_, i32_ = _type(FP32), _type("int32")
-    return ctypes.byref(d), (
+    return d, (
         ("tokens", (batch, d.room), i32_), ("lengths", of_batch, i32_), ("prompt_lengths", of_batch, i32_),
         ("repetition", of_batch, f32_), ("presence", of_batch, f32_), ("frequency", of_batch, f32_), ("drafts", of_rows, i32_),
         ("tree", (1 if d.tree_shared else batch, n_q, (n_q + 31) // 32), i32_), ("bias_ids", of_bias, i32_), ("bias", of_bias, f32_),

@@ -58,7 +58,7 @@ def _compile(src, extra):
 
 def _build_match(force):
     src = os.path.join(CSRC, "match.c")
-    if not force and not _stale(MATCH, [src, __file__]):
+    if not force and not _stale(MATCH, [src, os.path.join(ROOT, "include", "mafat.h"), __file__]):
         return
     tmp = MATCH + ".tmp.%d" % os.getpid()
     cmd = ["gcc", "-O2", "-std=c11", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"], src, "-o", tmp]

@@ -283,28 +283,28 @@ def test_forms_that_are_taken(mf, monkeypatch):
         monkeypatch.setattr(mf.lib, entry, lambda *a: seen.append(a) or mf.OK)
     norm, rotary, tree, logits = ({n: OnGpu(t) for n, t in calls[k][2].items()} for k in ("norm", "rotary", "tree", "logits"))
     calls["norm"][1](**{**norm, "gate": OnGpu(torch.zeros(64, dtype=torch.bfloat16))})
-    assert seen[-1][0]._obj.gate_rows == 6
+    assert seen[-1][0].gate_rows == 6
     calls["norm"][1](**{**norm, "gate": OnGpu(torch.zeros(3, 80, dtype=torch.bfloat16)[:, :64])})
-    assert seen[-1][0]._obj.gate_rows == 2 and seen[-1][0]._obj.gate_stride == 80
+    assert seen[-1][0].gate_rows == 2 and seen[-1][0].gate_stride == 80
     side = torch.zeros(2, 3, 8, 64, dtype=torch.bfloat16)
     calls["rotary"][1](**{**rotary, "q": OnGpu(side[:, :, :4]), "k": OnGpu(side[:, :, 4:6])})
-    assert list(seen[-1][1]._obj.q_strides) == [1536, 512, 64] and seen[-1][1]._obj.room == 9
+    assert list(seen[-1][1].q_strides) == [1536, 512, 64] and seen[-1][1].room == 9
     calls["tree"][1](**{**tree, "tree": OnGpu(torch.zeros(1, 5, 1, dtype=torch.int32))})
     assert seen[-1][11] == 1
     calls["tree"][1](**tree)
     assert seen[-1][11] == 0
     calls["logits"][1](**{**logits, "tree": OnGpu(torch.zeros(1, 3, 1, dtype=torch.int32)), "bias_ids": OnGpu(torch.zeros(1, 4, dtype=torch.int32)),
                           "bias": OnGpu(torch.zeros(1, 4))})
-    assert seen[-1][0]._obj.tree_shared == 1 and seen[-1][0]._obj.bias_shared == 1
+    assert seen[-1][0].tree_shared == 1 and seen[-1][0].bias_shared == 1
     wide = torch.zeros(2, 3, 128, dtype=torch.bfloat16)[..., :100]
     calls["logits"][1](**{**logits, "logits": OnGpu(wide)})
-    assert seen[-1][0]._obj.logits_stride == 128 and seen[-1][0]._obj.out_stride == 100
+    assert seen[-1][0].logits_stride == 128 and seen[-1][0].out_stride == 100
     with pytest.raises(mf.MafatError):  # rows that are not apart by one step
         calls["logits"][1](**{**logits, "logits": OnGpu(torch.zeros(2, 4, 100, dtype=torch.bfloat16)[:, :3])})
     two = {n: logits[n] for n in ("tokens", "lengths", "repetition")}
     mf.adjust_logits(OnGpu(torch.zeros(2, 100)), OnGpu(torch.zeros(2, 100)), masks=OnGpu(torch.zeros(5, 4, dtype=torch.int32)),
                      mask_rows=OnGpu(torch.zeros(2, dtype=torch.int32)), stream=0, **two)
-    assert seen[-1][0]._obj.n_q == 1
+    assert seen[-1][0].n_q == 1
 
 
 def test_calls_that_are_kept_are_told_apart(mf, monkeypatch):
@@ -322,20 +322,20 @@ def test_calls_that_are_kept_are_told_apart(mf, monkeypatch):
             x, r, h = (OnGpu(torch.zeros(rows, cols + pad)[:, :cols]) for _ in range(3))
             for scale in (1.0, 0.5):
                 mf.block_norm(x, r, h, branch_scale=scale, stream=0)
-                d = seen[-1][0]._obj
+                d = seen[-1][0]
                 assert (d.rows, d.cols, d.branch_scale) == (rows, cols, scale) and d.x_stride == cols + pad
                 assert list(seen[-1][1:3]) == [x.data_ptr(), r.data_ptr()] and seen[-1][6] == h.data_ptr() and seen[-1][4] is None
             out = OnGpu(torch.zeros(rows, cols))
             tokens = OnGpu(torch.zeros(rows, 1 + turn, dtype=torch.int32))
             mf.adjust_logits(x, out, tokens=tokens, stream=0)
-            d = seen[-1][0]._obj
+            d = seen[-1][0]
             assert (d.batch, d.vocab, d.room, d.logits_stride, d.out_stride) == (rows, cols, 1 + turn, cols + pad, cols)
             assert seen[-1][1] == x.data_ptr() and seen[-1][2] == tokens.data_ptr() and seen[-1][-2] == out.data_ptr()
             q = OnGpu(torch.zeros(rows, 2, cols // 8, 64 + pad, dtype=torch.bfloat16)[..., :64])
             o = OnGpu(torch.zeros(rows, 2, cols // 8, 64, dtype=torch.bfloat16))
             at = OnGpu(torch.zeros(rows, 2, dtype=torch.int32))
             rotary.run(at, q=q, q_out=o, stream=0)
-            d = seen[-1][1]._obj
+            d = seen[-1][1]
             assert (d.batch, d.heads_q, d.q_strides[2]) == (rows, cols // 8, 64 + pad) and seen[-1][4:6] == (q.data_ptr(), o.data_ptr())
     assert len(mf._norm_calls) <= mf.MOST_CALLS and len(rotary._calls) <= mf.MOST_CALLS
 
@@ -350,10 +350,61 @@ def test_what_is_not_a_tensor(mf, monkeypatch):
     for _ in range(2):
         plan.run(*[4096 * (i + 1) for i in range(7)], stream=0)
     assert len(seen) == 2 and not plan._calls and seen[0][1] == 4096
-    with pytest.raises(TypeError):
-        mf._match.find([], [], 0, None)
-    with pytest.raises(TypeError):
-        mf._match.find([], (), "0", None)
-    assert mf._match.find([((None,), 1)], (None,), 0, 2) is None and mf._match.find([((None,), 1)], (None,), 0, 1) == (((None,), 1), (None,))
-    assert mf._match.find([((None, None), 1)], (None,), 0, 1) is None
-    assert mf._match.find([(((torch.float32, (2,), None),), 1)], (object(),), 0, 1) is None
+
+
+def test_calls_made_by_the_module(mf, monkeypatch):
+    """Calls that are like one made before go to the library itself, whose refusals of made-up addresses come back; the rest
+    is as if they were the first."""
+    monkeypatch.setattr(mf, "_current_device", lambda: 0)
+    entry, call, tensors = _calls(mf)["norm"]
+    seen = []
+    real = mf.lib.mafat_block_norm
+    monkeypatch.setattr(mf, "_norm_calls", [])
+    monkeypatch.setattr(mf.lib, entry, lambda *a: seen.append(a) or mf.OK)
+    here = {n: OnGpu(t) for n, t in tensors.items()}
+    call(**here)
+    assert len(seen) == 1 and len(mf._norm_calls) == 1
+    here["residual_out"] = here["gate"]  # of another shape: not like it, and refused
+    with pytest.raises(mf.MafatError):
+        call(**here)
+    whole = torch.zeros(6 * 64 + 8, dtype=torch.bfloat16)
+    for shift in (8, 16):  # outputs that overlap an input, or are not aligned: the library's word
+        x = OnGpu(whole[:384].view(6, 64))
+        at = whole[shift:shift + 384] if shift == 8 else whole[4:388]
+        with pytest.raises(mf.MafatError) as e:
+            call(**{**here, "x": x, "residual_out": OnGpu(at.view(6, 64))})
+        assert e.value.status == mf.EINVAL and ("overlaps" in str(e.value) or "aligned" in str(e.value))
+    assert len(seen) == 1 and real is not mf.lib.mafat_block_norm
+
+
+def test_the_module_checks_its_arguments(mf):
+    run = mf._match.run
+    for args in ((0, [], [], 0, None, None, None), (0, (), (), 0, None, None, None), ("0", [], (), 0, None, None, None), (0, [])):
+        with pytest.raises(TypeError):
+            run(*args)
+    for args in ((4, [], (), 0, None, None, None), (-1, [], (), 0, None, None, None), (0, [], (None,) * 7, 0, None, None, None)):
+        with pytest.raises(ValueError):
+            run(*args)
+    none = (None,) * 8
+    assert run(0, [], none, 0, None, None, None) is None
+    assert run(0, [(none, 1, 0)], none, 0, 2, None, None) is None and run(0, [(none[1:], 1, 0)], none, 0, 1, None, None) is None
+    look = (torch.float32, (2,), None)
+    assert run(0, [((look,) + none[1:], 1, 0)], (object(),) + none[1:], 0, 1, None, None) is None
+    assert run(0, [(none, 1, 0)], none, 0, 1, None, None) == mf.EINVAL  # a null descriptor, by the library
+
+
+@pytest.mark.parametrize("which", ["rotary", "tree"])
+def test_closed_plans(mf, monkeypatch, which):
+    entry, call, tensors = _calls(mf)[which]
+    plan = [c.cell_contents for c in call.__closure__][0]
+    plan.device = 0  # as of a plan for the GPU: its calls are kept
+    here = {n: OnGpu(t) for n, t in tensors.items()}
+    with monkeypatch.context() as m:
+        m.setattr(mf.lib, entry, lambda *a: mf.OK)
+        call(**here)
+    assert len(plan._calls) == 1
+    plan.close()
+    for _ in range(2):
+        with pytest.raises(mf.MafatError) as e:
+            call(**here)
+        assert e.value.status == mf.EINVAL
