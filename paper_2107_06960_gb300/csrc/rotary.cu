@@ -20,9 +20,13 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostTokens = 16;  // of a CTA
-constexpr int kMostPairs = 128;  // of a head
+constexpr int kMostTokens = 16;  // of a CTA, where there are heads enough
 constexpr int kTogether = 4;     // accesses of pairs of a thread that are on their way together
+constexpr int kMostPairs = 128;  // of a head
+constexpr int kAngles = 2048;    // of a CTA's tokens
+
+// room for a token's angles: in accesses of 16 bytes
+__host__ __device__ constexpr int angles_of(int rot) { return (rot / 2 + 3) / 4 * 4; }
 
 // 16 bytes that are copied as they are
 template <class T>
@@ -33,8 +37,8 @@ struct alignas(16) Piece {
 // V channels an access; an item is two accesses, of pairs of channels or of neighbours that stay.
 template <class T, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ MafatRotaryArgs a) {
-    __shared__ __align__(16) float cosines[kMostTokens * kMostPairs], sines[kMostTokens * kMostPairs];
-    const int tid = threadIdx.x, half = a.rot / 2;
+    __shared__ __align__(16) float cosines[kAngles + 8], sines[kAngles + 8];
+    const int tid = threadIdx.x, half = a.rot / 2, stride = angles_of(a.rot);
     const int64_t token0 = (int64_t)blockIdx.x * a.per_block;
     const int tokens = (int)min((int64_t)a.per_block, a.tokens - token0);
     // the thread's token, first head and item; threads past the last token have none
@@ -74,8 +78,8 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_consta
         const int32_t top = (int32_t)((turn + 0x80000000u) >> 32);  // of half turns 2^-31
         float s, c;
         sincospif((float)top * 0x1p-31f, &s, &c);
-        cosines[of * kMostPairs + pair] = c * a.magnitude;
-        sines[of * kMostPairs + pair] = s * a.magnitude;
+        cosines[of * stride + pair] = c * a.magnitude;
+        sines[of * stride + pair] = s * a.magnitude;
     }
     if (mine && kept && tv.heads > 0) {  // values, 16 bytes at a time
         constexpr int kWide = 16 / sizeof(T);
@@ -95,12 +99,18 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_consta
     }
     __syncthreads();  // sines and cosines are there
     if (head0 >= heads) return;
+    constexpr int kRun = V < 4 ? V : 4;
     float cs[V], sn[V];
     if (turned) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {  // past the last pair of an item with one access: not used
-            cs[j] = cosines[slot * kMostPairs + lane * V + j];
-            sn[j] = sines[slot * kMostPairs + lane * V + j];
+        for (int j = 0; j < V; j += kRun) {  // past the last pair of an item with one access, up to 7 past the end: not used
+            Vec<float, kRun> x, y;
+            x.load(cosines + slot * stride + lane * V + j, true);
+            y.load(sines + slot * stride + lane * V + j, true);
+            float p[kRun], q[kRun];
+            x.get(p), y.get(q);
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) cs[j + k] = p[k], sn[j + k] = q[k];
         }
     }
     T* q_out = (T*)tq.out + b * tq.out_sb + t * tq.out_st;
@@ -170,10 +180,12 @@ cudaError_t mafat_launch_rotary(MafatRotaryArgs& a, bool bf16, bool interleaved,
     a.lanes_div = MafatDiv((uint32_t)a.lanes);
     a.half_div = MafatDiv((uint32_t)a.rot / 2);
     // A thread has 8 heads of a token (8 x 2048 tokens of 32 + 8 heads of 128 channels: 62.8 us, with 4 heads 68.0, with 2 116.8),
-    // fewer where that leaves CTAs for all SMs (5 x 676 tokens of 8 + 2 heads: a CTA an SM 8.1, two 8.7, four 12.6).
+    // fewer where that leaves CTAs for all SMs (5 x 676 tokens of 8 + 2 heads: a CTA an SM 8.1, two 8.7, four 12.6).  Of few heads more tokens
+    // are a CTA's: 44 x 2615 tokens of 2 + 1 heads of 64 channels 27.4, 16 at a time 39.6; of 4 + 4 heads of 128, 4 x 3844, 23.6 and 20.
     constexpr int kHeads = 8, kSms = 152;
     const int heads = std::max(a.t[0].heads + a.t[1].heads, a.t[2].heads), rows = kThreads / a.lanes;
-    a.per_block = std::max(1, std::min(rows / ((heads + kHeads - 1) / kHeads), kMostTokens));
+    const int angles = kAngles / angles_of(a.rot), most = heads < 4 ? angles : std::min(angles, kMostTokens);
+    a.per_block = std::max(1, std::min(rows / ((heads + kHeads - 1) / kHeads), most));
     while (a.per_block > 1 && a.tokens < (int64_t)kSms * a.per_block) a.per_block = (a.per_block + 1) / 2;
     a.steps = std::min(heads, rows / a.per_block);
     a.steps_div = MafatDiv((uint32_t)a.steps);

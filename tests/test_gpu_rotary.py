@@ -103,6 +103,14 @@ def test_sizes(mf, dtype, B, T, H, Hk, room):
     _rotary(mf, B, T, H, Hk, 128, dtype, 32, True, room=room, side=False)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("H,Hk,D,rot", [(1, 1, 64, 0), (2, 1, 64, 24), (1, 2, 40, 12), (1, 1, 8, 2), (1, 1, 256, 250)])
+def test_many_tokens_of_few_heads(mf, dtype, H, Hk, D, rot):
+    """As many as a block of threads takes, and a last block with few."""
+    for interleaved in (False, True):
+        _rotary(mf, 3, 1777, H, Hk, D, dtype, rot, interleaved, room=1800)
+
+
 @pytest.mark.parametrize("what", ["q", "k", "v", "qk", "qv", "kv"])
 def test_some_of_the_tensors(mf, what):
     _rotary(mf, 3, 7, 4, 2, 64, mf.BF16, what=what)
