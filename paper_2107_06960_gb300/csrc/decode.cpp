@@ -124,6 +124,7 @@ mafat_status mafat_block_norm(const mafat_block_norm_desc* d, const void* x, con
     int64_t bytes[kTensors];
     for (int i = 0; i < 5; ++i) {
         const int64_t n = i == kGate ? d->rows / per_gate : d->rows;
+        if (t[i] && (__int128)(n - 1) * row[i] * esz > (__int128)1 << 62) return fail(MAFAT_EUNSUPPORTED, "a tensor spans more than 2^62 bytes");
         bytes[i] = t[i] ? ((n - 1) * row[i] + d->cols) * (i == kY ? osz : esz) : 0;
     }
     bytes[kWeight] = bytes[kPostWeight] = d->cols * esz;
@@ -357,7 +358,7 @@ mafat_status mafat_adjust_logits(const mafat_logits_desc* d, const void* logits,
         return MAFAT_OK;
     }
     const int64_t words = (d->n_q + 31) / 32, mask_words = (d->vocab + 31) / 32;
-    if (rows * (d->vocab / mafat_logits_run() + 2) > kMaxI32) return fail(MAFAT_EUNSUPPORTED, "too many rows");
+    if (rows > kMaxI32 || rows * (d->vocab / mafat_logits_run() + 2) > kMaxI32) return fail(MAFAT_EUNSUPPORTED, "too many rows");
     if (!logits || !out) return fail(MAFAT_EINVAL, "null logits or out");
     if ((bias_ids != nullptr) != (bias != nullptr)) return fail(MAFAT_EINVAL, "bias_ids and bias are given together");
     if (tree && !drafts) return fail(MAFAT_EINVAL, "a tree without drafts");

@@ -41,7 +41,9 @@ def _norm(mf, at=None, null=(), **change):
 
 @pytest.mark.parametrize("change,status", [
     (dict(struct_size=8), "EINVAL"), (dict(dtype=2), "EINVAL"), (dict(out_dtype=1), "EINVAL"), (dict(cols=0), "EINVAL"),
-    (dict(cols=16385), "EUNSUPPORTED"), (dict(rows=-1), "EINVAL"), (dict(rows=1 << 31), "EUNSUPPORTED"), (dict(eps=-1.0), "EINVAL"),
+    (dict(cols=16385), "EUNSUPPORTED"), (dict(rows=-1), "EINVAL"), (dict(rows=1 << 31), "EUNSUPPORTED"),
+    (dict(rows=(1 << 31) - 1, x_stride=1 << 39), "EUNSUPPORTED"), (dict(rows=(1 << 31) - 1, gate_rows=1, gate_stride=1 << 32), "EUNSUPPORTED"),
+    (dict(eps=-1.0), "EINVAL"),
     (dict(eps=math.nan), "EINVAL"), (dict(eps=math.inf), "EINVAL"), (dict(branch_scale=math.inf), "EINVAL"),
     (dict(residual_scale=math.nan), "EINVAL"), (dict(scale_group=128), "EINVAL"), (dict(gate_rows=-1), "EINVAL"),
     (dict(gate_rows=5), "EINVAL"), (dict(gate_rows=24), "EINVAL"), (dict(x_stride=255), "EINVAL"), (dict(gate_stride=-256), "EINVAL"),
@@ -183,7 +185,8 @@ def _logits(mf, at=None, null=(), **change):
 
 @pytest.mark.parametrize("change,status", [
     (dict(struct_size=1), "EINVAL"), (dict(dtype=2), "EINVAL"), (dict(out_dtype=0), "EINVAL"), (dict(batch=-1), "EINVAL"), (dict(n_q=-1), "EINVAL"),
-    (dict(vocab=0), "EINVAL"), (dict(vocab=(1 << 30) + 1), "EUNSUPPORTED"), (dict(room=-1), "EINVAL"), (dict(room=(1 << 18) - 3), "EUNSUPPORTED"),
+    (dict(vocab=0), "EINVAL"), (dict(vocab=(1 << 30) + 1), "EUNSUPPORTED"),
+    (dict(batch=1 << 30, n_q=(1 << 18) - 64, vocab=1 << 30), "EUNSUPPORTED"), (dict(room=-1), "EINVAL"), (dict(room=(1 << 18) - 3), "EUNSUPPORTED"),
     (dict(n_bias=-1), "EINVAL"), (dict(n_bias=4096), "EUNSUPPORTED"), (dict(n_masks=-1), "EINVAL"), (dict(batch=1 << 30), "EUNSUPPORTED"),
     (dict(logits_stride=999), "EINVAL"), (dict(out_stride=-1000), "EINVAL"), (dict(out_stride=1 << 31), "EUNSUPPORTED"),
     (dict(null=("logits",)), "EINVAL"), (dict(null=("out",)), "EINVAL"), (dict(null=("bias",)), "EINVAL"), (dict(null=("bias_ids",)), "EINVAL"),
