@@ -132,9 +132,11 @@ cudaError_t launch_v(const MafatBlockNormArgs& a, MafatNormQuant q, cudaStream_t
 }  // namespace
 
 cudaError_t mafat_launch_block_norm(const MafatBlockNormArgs& a, bool bf16, int vec, MafatNormQuant quant, cudaStream_t s) {
-    // a warp has 128 channels at least: 4 accesses of one, 2 of two
+    // A warp has 128 channels at least: 4 accesses of one, 2 of two.  20000 rows of 1004 bf16 26.6 us with accesses of four, of two
+    // 28.1; to e4m3 by blocks 31.9, 37.3.
     if (bf16)
         return vec >= 8   ? launch_v<__nv_bfloat16, 8, 1>(a, quant, s)
+               : vec >= 4 ? launch_v<__nv_bfloat16, 4, 1>(a, quant, s)
                : vec >= 2 ? launch_v<__nv_bfloat16, 2, 2>(a, quant, s)
                           : launch_v<__nv_bfloat16, 1, 4>(a, quant, s);
     return vec >= 4   ? launch_v<float, 4, 1>(a, quant, s)

@@ -103,6 +103,13 @@ def test_strides_and_many_rows(mf, dt, quant, cols, pad, rows):
     _block(mf, rows, cols, dt, quant, pad=pad)
 
 
+@pytest.mark.parametrize("quant", [None, "row", "128"])
+@pytest.mark.parametrize("cols,pad", [(4, 0), (132, 0), (484, 4), (1000, 12), (2060, 0), (4900, 4), (16380, 0)])
+@pytest.mark.parametrize("rows", [3, 2100])
+def test_rows_of_whole_accesses_of_four(mf, quant, cols, pad, rows):
+    _block(mf, min(rows, 8000000 // cols), cols, torch.bfloat16, quant, pad=pad, gates=1)
+
+
 @pytest.mark.parametrize("dt", BOTH)
 @pytest.mark.parametrize("how", ["h=r", "h=x", "y=x", "h=r,y=x"])
 @pytest.mark.parametrize("rows,cols", [(5, 5000), (2100, 512)])
