@@ -49,7 +49,7 @@ struct MafatLogitsArgs {
     const uint32_t* masks;
     const int32_t* mask_rows;
     // set by the launch: runs of the vocabulary, groups of a request's rows; rows of a group
-    MafatDiv runs_div, groups_div;
+    MafatDiv items_div, groups_div;
     int32_t rows_of_cta;
     int32_t pass;               // 0: out is logits and nothing is masked: only what is noted is written
     int32_t n_q, vocab, room, n_bias, n_masks, tree_words, mask_words;
