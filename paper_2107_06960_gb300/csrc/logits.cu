@@ -9,10 +9,9 @@
 // neighbours in a vocabulary: in the pass over all of them their divisions fell to a few warps.)  The table's sums are
 // of whole numbers, so that their order does not matter.
 //
-// 64 trees of 16 nodes, 131072 bf16 logits each, half of them with a mask, 2048 said: 105 us or 5.1 TB/s.  The pass alone takes 83 (6.5
-// TB/s), with masks 88; the rest is a CTA's way from the request's lists to its own, during which four others are on
-// the SM.  7 rows of 50001 fp32 with 20000 said: 7.7 us, going over the lists.  16 rows of 32000 bf16 with 512 said: 3.6 us,
-// a launch and three round trips.
+// 64 trees of 16 nodes, 131072 bf16 logits each, half of them with a mask, 2048 said: 100 us or 5.4 TB/s; with each next row in registers
+// 103, with two on their way in shared memory as it is.  20 x 35 rows of 119808 from bf16 to fp32, 140 said: 80 us or 6.2 TB/s.  7 rows
+// of 50001 fp32 with 20000 said: 7.7 us, going over the lists.  16 rows of 32000 bf16 with 512 said: 3.6 us, a launch and three round trips.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -34,9 +33,9 @@ __device__ __forceinline__ float wide(__nv_bfloat16 x) { return __bfloat162float
 __device__ __forceinline__ void narrow(float* p, float x) { *p = x; }
 __device__ __forceinline__ void narrow(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// 16 bytes of logits on their way to `out`, 16 bytes at a time where `whole`; MASK: those without a bit in `allowed` as -inf
-template <bool MASK>
-__device__ __forceinline__ void put(float* out, const Vec<float, 4>& v, uint32_t allowed, bool whole) {
+// Logits on their way to 16 bytes of `out`, at once where `whole`; MASK: those without a bit in `allowed` as -inf
+template <bool MASK, class T>
+__device__ __forceinline__ void put(float* out, const Vec<T, 4>& v, uint32_t allowed, bool whole) {
     float x[4];
     v.get(x);
     if constexpr (MASK)
@@ -48,17 +47,6 @@ __device__ __forceinline__ void put(float* out, const Vec<float, 4>& v, uint32_t
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) out[j] = x[j];
-    }
-}
-template <bool MASK>
-__device__ __forceinline__ void put(float* out, const Vec<__nv_bfloat16, 8>& v, uint32_t allowed, bool whole) {
-    float x[8];
-    v.get(x);
-#pragma unroll
-    for (int j = 0; j < 8; j += 4) {
-        Vec<float, 4> part;
-        part.u = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-        put<MASK>(out + j, part, allowed >> j, whole);
     }
 }
 template <bool MASK>
@@ -85,11 +73,14 @@ __device__ __forceinline__ bool allows(const uint32_t* mask, int token) {
     return !mask || (mask[token >> 5] >> (token & 31) & 1u) != 0u;
 }
 
-// A CTA's run of a row: THREADS threads of N accesses of 16 bytes.  It starts on 16 bytes of the input, before the row's first
-// token where that does not.
-template <class T, int THREADS, int N>
+// A CTA's run of a row: THREADS threads of accesses of V tokens, 16 bytes of the output, in all of N * 16 bytes of the input.  It
+// starts on a whole access of the input, before the row's first token where that does not.  (With accesses of 16 bytes of the input
+// and 32 of the output, in two halves, 20 x 35 rows of 119808 from bf16 to fp32 took 98 us instead of 80.)
+template <class T, class O, int THREADS, int N>
 struct Run {
-    static constexpr int V = 16 / sizeof(T), kTokens = THREADS * N * V, kStep = THREADS * V;
+    static constexpr int V = 16 / sizeof(O), kBytes = V * sizeof(T), A = N * 16 / kBytes, kTokens = THREADS * A * V, kStep = THREADS * V;
+    // Rows that are asked for before they are needed, in shared memory (none: the next one alone, in registers)
+    static constexpr int kAsked = THREADS * N <= 1024 ? 2 : 0;
     static_assert(kTokens <= 65536 && kStep % 32 == 0, "places in 16 bits; a thread's accesses begin at one bit of a word");
     int first, mine, vocab;  // the run's first token, that of the thread's first access
     bool inner;              // all of the run are the row's
@@ -97,29 +88,41 @@ struct Run {
         : first(run * kTokens - (int)((uintptr_t)in / sizeof(T) % V)), mine(first + (int)threadIdx.x * V), vocab(a.vocab),
           inner(first >= 0 && first + kTokens <= a.vocab) {}
     __device__ __forceinline__ bool inside(int i) const { return inner || (mine + i * kStep >= 0 && mine + i * kStep + V <= vocab); }
-    __device__ __forceinline__ void load(const T* in, Vec<T, V> (&v)[N]) const {
+    __device__ __forceinline__ void load(const T* in, Vec<T, V> (&v)[A]) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i].load(in + mine + i * kStep, inside(i));
+        for (int i = 0; i < A; ++i) v[i].load(in + mine + i * kStep, inside(i));
+    }
+    // A later row's on their way to the thread's places in shared memory.
+    __device__ __forceinline__ void ask(const T* in, uint32_t to, bool on) const {
+#pragma unroll
+        for (int i = 0; i < A; ++i)
+            if (on && inside(i)) {
+                if constexpr (kBytes == 16)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * THREADS * kBytes), "l"(in + mine + i * kStep) : "memory");
+                else
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + i * THREADS * kBytes), "l"(in + mine + i * kStep) : "memory");
+            }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     }
     // the words with the thread's bits of a mask; from the second on where an access can pass a word's end
     struct Bits {
-        uint32_t lo[N], hi[N];
+        uint32_t lo[A], hi[A];
     };
     __device__ __forceinline__ void look(const uint32_t* mask, Bits& bits) const {
         const uint32_t* words = mask + (mine >> 5);
         const bool two = (mine & 31) + V > 32;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = 0; i < A; ++i) {
             const bool on = mask && inside(i);
             bits.lo[i] = on ? words[i * (kStep / 32)] : 0u;
             bits.hi[i] = on && two ? words[i * (kStep / 32) + 1] : 0u;
         }
     }
-    template <bool MASK, class O>
-    __device__ __forceinline__ void pass(const T* in, O* out, const uint32_t* mask, const Vec<T, V> (&v)[N], const Bits& bits) const {
+    template <bool MASK>
+    __device__ __forceinline__ void pass(const T* in, O* out, const uint32_t* mask, const Vec<T, V> (&v)[A], const Bits& bits) const {
         const bool whole = ((uintptr_t)(out + first) & 15u) == 0u;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = 0; i < A; ++i) {
             const int e = mine + i * kStep;
             if (inside(i)) {
                 put<MASK>(out + e, v[i], MASK ? __funnelshift_r(bits.lo[i], bits.hi[i], (uint32_t)mine & 31u) : 0u, whole);
@@ -133,17 +136,22 @@ struct Run {
 
 template <class T, class O, int THREADS, int N, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_constant__ MafatLogitsArgs a) {
-    using S = Run<T, THREADS, N>;
+    using S = Run<T, O, THREADS, N>;
     // Where histories are long the list is made of the whole table, not with each token, whose addition then has to come back
-    // first: 7 rows of 50001 with 20000 said 7.7 us instead of 10.3, 95 of 128890 with 21842 53 instead of 59 (16 rows of 32000 with
+    // first: 7 rows of 50001 with 20000 said 7.7 us instead of 10.3, 95 of 128890 with 21842 53 instead of 59, as the rows passed then (16 rows of 32000 with
     // 512, in 256 threads: 3.8 instead of 3.6).
     constexpr bool kScan = THREADS > 256;
-    extern __shared__ __align__(16) uint32_t table[];
+    constexpr int kAsked = S::kAsked;
+    constexpr int kRow = THREADS * S::A;  // places of a row
+    using Places = Vec<T, S::V>;
+    extern __shared__ __align__(16) uint4 shared[];
+    Places* const asked = (Places*)shared + threadIdx.x;  // the thread's of later rows
+    uint32_t* const table = (uint32_t*)((Places*)shared + (a.rows_of_cta > 1 ? kAsked * kRow : 0));
     uint16_t* list = (uint16_t*)(table + S::kTokens);
     __shared__ int listed, masks[kMostRows];
     const int tid = threadIdx.x;
     // All requests' first runs, then their second ones: CTAs of one run have alike much to write again, which tends to be most where
-    // a vocabulary begins, and the last CTAs short.  21 x 8 rows of 123520 with 8271 said 39.3 us, request by request 42.6.
+    // a vocabulary begins, and the last CTAs short.  21 x 8 rows of 123520 with 8271 said 38.8 us, request by request 42.6, as the rows passed then.
     const uint32_t run = a.items_div.div(blockIdx.x), i0 = blockIdx.x - run * a.items_div.d, b = a.groups_div.div(i0);
     const int t0 = (int)(i0 - b * a.groups_div.d) * a.rows_of_cta, rows = min(a.rows_of_cta, a.n_q - t0);
     const int64_t row0 = (int64_t)b * a.n_q + t0;
@@ -152,8 +160,12 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
     const S s(a, (int)run, in);
     launch_wait();
     launch_next();
-    Vec<T, S::V> v[N];
-    if (a.pass) s.load(in, v);
+    Places v[S::A];
+    if (a.pass) {
+        s.load(in, v);
+#pragma unroll
+        for (int r = 1; r <= kAsked; ++r) s.ask(in + r * a.in_s, (uint32_t)__cvta_generic_to_shared(asked + (r - 1) * kRow), r < rows);
+    }
     // what the CTA needs of the request is asked for together: the first of each list before the first barrier
     const bool any = a.tokens || a.drafts || a.bias_ids;
     const int32_t* bias_ids = a.bias_ids + (int64_t)b * a.bias_s;
@@ -244,9 +256,9 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
         __syncthreads();  // table and list are there
         if constexpr (kScan) {
             uint32_t hits = 0u;  // of the thread's words
-            static_assert(N * S::V <= 32, "a bit each");
+            static_assert(S::A * S::V <= 32, "a bit each");
 #pragma unroll
-            for (int k = 0; k < N * S::V / 4; ++k) {
+            for (int k = 0; k < S::A * S::V / 4; ++k) {
                 const uint4 w = *reinterpret_cast<const uint4*>(table + (k * THREADS + tid) * 4);
                 hits |= ((w.x ? 1u : 0u) | (w.y ? 2u : 0u) | (w.z ? 4u : 0u) | (w.w ? 8u : 0u)) << (4 * k);
             }
@@ -277,10 +289,10 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
         for (int r = 0;; ++r) {
             const T* from = in + r * a.in_s;
             O* to = out + r * a.out_s;
-            Vec<T, S::V> next[N];
+            Places next[S::A];
             typename S::Bits next_bits;
             if (r + 1 < rows) {
-                s.load(from + a.in_s, next);
+                if constexpr (kAsked == 0) s.load(from + a.in_s, next);
                 s.look(mask_of(r + 1), next_bits);
             }
             const uint32_t* mask = mask_of(r);
@@ -290,8 +302,17 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
                 s.template pass<false>(from, to, mask, v, bits);
             if (r + 1 == rows) break;
             bits = next_bits;
+            if constexpr (kAsked > 0) {
+                Places* at = asked + r % kAsked * kRow;
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAsked - 1) : "memory");
 #pragma unroll
-            for (int k = 0; k < N; ++k) v[k] = next[k];
+                for (int k = 0; k < S::A; ++k) v[k] = at[k * THREADS];
+                // its places are free: what was read is in registers when the copy is asked for
+                s.ask(from + (1 + kAsked) * a.in_s, (uint32_t)__cvta_generic_to_shared(at), r + 1 + kAsked < rows);
+            } else {
+#pragma unroll
+                for (int k = 0; k < S::A; ++k) v[k] = next[k];
+            }
         }
     }
     if (n == 0) return;
@@ -331,10 +352,10 @@ bool noted(const MafatLogitsArgs& a) { return a.tokens || a.drafts || a.bias_ids
 // A request's rows are shared by as many CTAs as leave `least` in all, so that the table serves several rows.
 template <class T, class O, int THREADS, int N, int BLOCKS>
 cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_t s) {
-    using S = Run<T, THREADS, N>;
+    using S = Run<T, O, THREADS, N>;
     // rows that start alike share a CTA; a row may start V - 1 tokens late
-    const bool alike = a.in_s * sizeof(T) % 16 == 0;
-    const int late = alike && (uintptr_t)a.logits % 16 == 0 ? 0 : S::V - 1;
+    const bool alike = a.in_s % S::V == 0;
+    const int late = alike && (uintptr_t)a.logits % S::kBytes == 0 ? 0 : S::V - 1;
     const int64_t runs = ((int64_t)a.vocab + late + S::kTokens - 1) / S::kTokens;
     int rows = alike ? kMostRows : 1;
     while (rows > 1 && (rows >= 2 * a.n_q || batch * ((a.n_q + rows - 1) / rows) * runs < least)) rows /= 2;
@@ -343,9 +364,11 @@ cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_
     a.items_div = MafatDiv((uint32_t)(batch * groups));
     a.groups_div = MafatDiv((uint32_t)groups);
     const int64_t listed = (a.tokens ? a.room : 0) + (int64_t)(a.drafts ? a.n_q : 0) + (a.bias_ids ? a.n_bias : 0);
-    const size_t smem = noted(a) ? S::kTokens * 4 + (std::min<int64_t>(S::kTokens, listed) * 2 + 15) / 16 * 16 : 0;
+    const size_t ahead = rows > 1 ? S::kAsked * THREADS * N * 16 : 0;
+    const size_t smem = ahead + (noted(a) ? S::kTokens * 4 + (std::min<int64_t>(S::kTokens, listed) * 2 + 15) / 16 * 16 : 0);
     if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, O, THREADS, N, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kTokens * 6);
+        const cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, O, THREADS, N, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   S::kAsked * THREADS * N * 16 + S::kTokens * 6);
         if (e != cudaSuccess) return e;
     }
     return mafat_launch_overlapped(logits_kernel<T, O, THREADS, N, BLOCKS>, (unsigned)(batch * groups * runs), THREADS, smem, s, a);
@@ -353,11 +376,12 @@ cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_
 
 // Each CTA goes over the whole history: the longer that is, the more threads it has, and the more tokens where there are many
 // logits.  256, 512 and 1024 threads (1024 with one access each, with four), in us:
-//   64 x 16 rows of 131072 bf16, 2048 said           105, 122, 139, 135      16 rows of 32000, 512 said     3.6, 4.4, 5.2, 9.9
-//   102 rows of 111872 bf16, 6305 said              34.8, 32.7, 49.8, 36.7   4 x 27 of 8892 fp32, 5139      13.5, 11.7, 12.8, 9.6
-//   7 rows of 50001 fp32, 20000 said                20.3,  9.5,  7.8, 13.1   57 of 25809 bf16, 24721        34.4, 19.4, 20.5, 23.9
-//   95 rows of 128890 fp32, 21842 said               104,  75,  107,  53     40 x 36 of 21617 bf16, 8686    158, 142, 206, 147
-//   5 x 24 rows of 40256 bf16, 16270 said           39.1, 27.3, 22.8, 34.4   15 x 24 of 11386 bf16, 13653   43.0, 36.0, 44.0, 41.7
+//   64 x 16 rows of 131072 bf16, 2048 said          94.7, 109, 115, 120      16 rows of 32000 bf16, 512 said   3.3, 4.0, 4.4, 9.8
+//   102 rows of 111872 bf16, 6305 said             28.5, 27.2, 41.4, 33.1    4 x 27 of 8892 fp32, 5139        12.7,  9.2,  9.8,  9.2
+//   7 rows of 50001 fp32, 20000 said               17.5,  8.4,  7.2, 11.1    57 of 25809 bf16, 24721          29.2, 15.8, 14.2, 20.7
+//   95 rows of 128890 fp32, 21842 said             90.8, 66.1, 98.9, 46.4    40 x 36 of 21617 bf16, 8686       145,  126,  180,  154
+//   5 x 24 rows of 40256 bf16, 16270 said          33.1, 21.9, 20.6, 29.5    15 x 24 of 11386 bf16, 13653     37.2, 28.9, 35.8, 44.4
+// (without masks and biases, to fp32 but for the first)
 template <class T, class O>
 cudaError_t launch_all(MafatLogitsArgs& a, int64_t batch, cudaStream_t s) {
     constexpr int kSms = 152;

@@ -234,3 +234,30 @@ def test_captured(mf, room, V):  # of 16 rows
 def test_long_histories(mf, dt, out_dt, B, T, V, room):
     """The forms of more threads, the last of which takes more than 32 MiB of logits."""
     _logits(mf, B, T, V, dt, out_dt, room=room, n_bias=20, n_masks=3, drafts="tree" if T > 1 else None, lengths=[room - 5] * B, prompts=[room // 3] * B)
+
+
+@pytest.mark.parametrize("dt,out_dt,in_place", [t + (False,) for t in TYPES] + [(torch.bfloat16, None, True), (torch.float32, None, True)])
+@pytest.mark.parametrize("B,T,V,room", [(1600, 17, 504, 40), (1600, 17, 500, 41), (900, 5, 4504, 40), (320, 9, 1000, 3000), (320, 3, 8200, 2050),
+                                        (70, 16, 700, 9000), (200, 17, 5200, 17000), (420, 2, 33000, 17000)])
+def test_rows_that_share_a_block(mf, dt, out_dt, B, T, V, room, in_place):
+    """With so many requests a block of threads has several rows of one, one after another; with one request a row each, to the same
+    bits.  Masks of some rows, padded rows whose padding stays."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(B + T)
+
+    def ids(lo, hi, *shape):
+        return torch.randint(lo, hi, shape, generator=g, device="cuda").to(torch.int32)
+    x = torch.randn((B, T, V + 8), generator=g, device="cuda").to(dt)
+    a = dict(tokens=ids(-1, V + 9, B, room), lengths=ids(0, room + 1, B), prompt_lengths=ids(0, room // 2, B), drafts=ids(0, V // 4, B, T),
+             tree=ids(0, 1 << (T - 1), B, T, 1), bias_ids=ids(0, V, B, 11), mask_rows=ids(-1, 6, B, T))
+    a.update({n: 0.5 + torch.rand(shape, generator=g, device="cuda")
+              for n, shape in (("repetition", (B,)), ("presence", (B,)), ("frequency", (B,)), ("bias", (B, 11)))})
+    masks = ids(-2 ** 31, 2 ** 31, 5, (V + 31) // 32)
+    out = x.clone() if in_place else torch.full((B, T, V + 8), 7.0, dtype=out_dt or dt, device="cuda")
+    pad = out[..., V:].clone()
+    mf.adjust_logits(out[..., :V] if in_place else x[..., :V], out[..., :V], masks=masks, **a)
+    assert torch.equal(out[..., V:], pad)
+    for b in sorted({0, 1, B // 3, B // 2, B - 2, B - 1}):
+        one = torch.empty((1, T, V), dtype=out.dtype, device="cuda")
+        mf.adjust_logits(x[b:b + 1, :, :V].contiguous(), one, masks=masks, **{n: t[b:b + 1] for n, t in a.items()})
+        assert torch.equal(out[b, :, :V], one[0]), b
