@@ -15,7 +15,11 @@ namespace {
 constexpr int kRowWarps = 4;   // rows of a block whose rows take one warp each
 constexpr int kMaxWarps = 16;  // of a row
 constexpr int kMaxThread = 32; // channels of a thread
-constexpr int kFewRows = 2048;
+// Rows have few warps where the GPU is full of them: from so many rows on, or, with accesses of 16 bytes and where no more than a quarter
+// of what a row's warps have room for is lost by it, from so many such warps on.  In us, with as many warps as rows can have and with few:
+// 750 rows of 4096 bf16 8.6, 7.0, 2000 of 2048 10.3, 9.9, 1100 of 512 3.14, 2.98, 520 of 1024 3.03, 3.32, 750 of 600 to e4m3 by blocks 3.25, 3.53; in
+// accesses of one channel 1443 of 1001 fp32 6.3, 7.1; 17146 of 1312 bf16 44.1, 37.8.
+constexpr int kManyRows = 2048, kManyWarps = 1024;
 
 // Sum over the row's warps; `part` is not used by another sum of the row.
 __device__ __forceinline__ float row_sum(float v, float* part, int warps) {
@@ -118,15 +122,22 @@ cudaError_t launch(const MafatBlockNormArgs& a, MafatNormQuant q, int warps, cud
                                    grid, block, 0, s, a);
 }
 
-// Accesses of a thread, as of the norm alone.
+// Accesses of a thread, twice as many until the row's warps hold it: all that it can have, or with `few` the fewest warps.
 template <class T, int V, int N>
-cudaError_t launch_v(const MafatBlockNormArgs& a, MafatNormQuant q, cudaStream_t s) {
+cudaError_t launch_v(const MafatBlockNormArgs& a, MafatNormQuant q, bool few, int most, cudaStream_t s) {
     const int per_warp = 32 * V * N;
-    const int most = q != MAFAT_NORM_BLOCK ? kMaxThread : V == 1 ? 8 : 16;
-    const bool one_warp = a.n.rows >= kFewRows && 2 * N * V <= most;
     if constexpr (2 * N * V <= kMaxThread)
-        if (a.n.cols > per_warp * (one_warp ? 1 : kMaxWarps)) return launch_v<T, V, 2 * N>(a, q, s);
+        if (a.n.cols > per_warp * (few && 2 * N * V <= most ? 1 : kMaxWarps)) return launch_v<T, V, 2 * N>(a, q, few, most, s);
     return launch<T, V, N>(a, q, (a.n.cols + per_warp - 1) / per_warp, s);
+}
+template <class T, int V, int N>
+cudaError_t launch_rows(const MafatBlockNormArgs& a, MafatNormQuant q, cudaStream_t s) {
+    const int most = q != MAFAT_NORM_BLOCK ? kMaxThread : V == 1 ? 8 : 16;  // channels of a thread
+    constexpr int kLeast = 32 * V * N;
+    const int64_t warps = (a.n.cols + 32 * most - 1) / (32 * most), held = (a.n.cols + kLeast - 1) / kLeast * kLeast;
+    const bool few = a.n.rows >= kManyRows ||
+                     (V * sizeof(T) == 16 && a.n.rows * warps >= kManyWarps && (warps == 1 || warps * 32 * most * 4 <= held * 5));
+    return launch_v<T, V, N>(a, q, few, most, s);
 }
 
 }  // namespace
@@ -135,11 +146,11 @@ cudaError_t mafat_launch_block_norm(const MafatBlockNormArgs& a, bool bf16, int 
     // A warp has 128 channels at least: 4 accesses of one, 2 of two.  20000 rows of 1004 bf16 26.6 us with accesses of four, of two
     // 28.1; to e4m3 by blocks 31.9, 37.3.
     if (bf16)
-        return vec >= 8   ? launch_v<__nv_bfloat16, 8, 1>(a, quant, s)
-               : vec >= 4 ? launch_v<__nv_bfloat16, 4, 1>(a, quant, s)
-               : vec >= 2 ? launch_v<__nv_bfloat16, 2, 2>(a, quant, s)
-                          : launch_v<__nv_bfloat16, 1, 4>(a, quant, s);
-    return vec >= 4   ? launch_v<float, 4, 1>(a, quant, s)
-           : vec >= 2 ? launch_v<float, 2, 2>(a, quant, s)
-                      : launch_v<float, 1, 4>(a, quant, s);
+        return vec >= 8   ? launch_rows<__nv_bfloat16, 8, 1>(a, quant, s)
+               : vec >= 4 ? launch_rows<__nv_bfloat16, 4, 1>(a, quant, s)
+               : vec >= 2 ? launch_rows<__nv_bfloat16, 2, 2>(a, quant, s)
+                          : launch_rows<__nv_bfloat16, 1, 4>(a, quant, s);
+    return vec >= 4   ? launch_rows<float, 4, 1>(a, quant, s)
+           : vec >= 2 ? launch_rows<float, 2, 2>(a, quant, s)
+                      : launch_rows<float, 1, 4>(a, quant, s);
 }

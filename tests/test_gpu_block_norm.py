@@ -111,6 +111,13 @@ def test_rows_of_whole_accesses_of_four(mf, quant, cols, pad, rows):
 
 
 @pytest.mark.parametrize("dt", BOTH)
+@pytest.mark.parametrize("quant", [None, "row", "128"])
+@pytest.mark.parametrize("rows,cols", [(600, 2048), (1030, 600), (1030, 512), (1023, 1024), (300, 4096), (1500, 1312), (150, 16384)])
+def test_rows_of_few_and_of_many_warps(mf, dt, quant, rows, cols):
+    _block(mf, rows, cols, dt, quant, gates=rows)
+
+
+@pytest.mark.parametrize("dt", BOTH)
 @pytest.mark.parametrize("how", ["h=r", "h=x", "y=x", "h=r,y=x"])
 @pytest.mark.parametrize("rows,cols", [(5, 5000), (2100, 512)])
 def test_in_place(mf, dt, how, rows, cols):
