@@ -605,7 +605,8 @@ typedef struct {
 
 typedef struct mafat_rotary_s mafat_rotary_t;
 
-/* Makes the table of frequencies on the current device.  Not for use during stream capture. */
+/* Makes the table of frequencies on the current device; it is there when the call returns, for runs on any stream.  Not for use
+ * during stream capture. */
 mafat_status mafat_rotary_plan(const mafat_rotary_desc* desc, mafat_rotary_t** out);
 
 /* One call's sizes and strides ({sequence, token, head} in elements, the rules of the attention plans). */

@@ -217,6 +217,8 @@ mafat_status mafat_rotary_plan(const mafat_rotary_desc* d, mafat_rotary_t** out)
                 st = cuda_fail(e, "cudaMalloc");
             else if ((e = cudaMemcpy(p->turns, turns, rot / 2 * sizeof(uint64_t), cudaMemcpyHostToDevice)) != cudaSuccess)
                 st = cuda_fail(e, "cudaMemcpy");
+            else if ((e = transfers_done()) != cudaSuccess)
+                st = cuda_fail(e, "cudaStreamSynchronize");
         }
     }
     delete[] turns;

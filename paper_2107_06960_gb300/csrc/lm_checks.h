@@ -32,6 +32,10 @@ inline mafat_status cuda_fail(cudaError_t e, const char* what) {
     return fail(e == cudaErrorMemoryAllocation ? MAFAT_ENOMEM : MAFAT_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+// What was copied to the device from pageable memory, or set there, may still be on its way when the call returns, and streams that
+// the legacy stream does not hold up would not wait for it: a plan's maker waits itself.
+inline cudaError_t transfers_done() { return cudaStreamSynchronize(nullptr); }
+
 constexpr int64_t kMaxI32 = std::numeric_limits<int32_t>::max();
 
 inline bool aligned(const void* p, uintptr_t n = 16) { return ((uintptr_t)p & (n - 1)) == 0; }

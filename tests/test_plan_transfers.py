@@ -1,0 +1,49 @@
+"""A plan is whole on the device when its maker returns: what was copied or set for it has been waited for, so that a run on any
+stream, also one that the legacy stream does not hold up, finds it."""
+import ctypes
+
+import pytest
+
+import fake_device
+
+
+@pytest.fixture(scope="module")
+def mf():
+    import __graft_entry__ as g
+    g.build()
+    import paper_2107_06960_gb300 as mf
+    return mf
+
+
+@pytest.fixture(scope="module")
+def fake(mf, tmp_path_factory):
+    return fake_device.build(mf, str(tmp_path_factory.mktemp("fake")))
+
+
+def _is_whole(notes):
+    sent = [i for i, n in enumerate(notes) if n in ("copy in", "set")]
+    assert sent, notes
+    assert "sync 0" in notes[sent[-1] + 1:], notes
+
+
+def _rotary(mf, fake):
+    d = mf.RotaryDesc(struct_size=ctypes.sizeof(mf.RotaryDesc), head_dim=64)
+    h = ctypes.c_void_p()
+    return fake.lib.mafat_rotary_plan(ctypes.byref(d), ctypes.byref(h)), h
+
+
+def test_rotary_plan(mf, fake):
+    fake.reset()
+    status, h = _rotary(mf, fake)
+    assert status == mf.OK
+    _is_whole(fake.notes())
+    fake.lib.mafat_rotary_destroy(h)
+
+
+def test_rotary_plan_whose_transfer_fails(mf, fake):
+    for call in ("copy in", "sync"):
+        fake.reset()
+        fake.fail(call)
+        status, h = _rotary(mf, fake)
+        assert mf.STATUS[status] == "ECUDA" and not h.value
+        assert fake.notes().count("malloc") == fake.notes().count("free") == 1
