@@ -391,6 +391,7 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
         p->part_lse = (float*)((char*)p->workspace + kStatusBytes);
         p->part_o = (float*)((char*)p->workspace + kStatusBytes + lse_bytes);
         if ((e = cudaMemset(p->status, 0, kStatusBytes)) != cudaSuccess) return cuda_fail(e, "cudaMemset");
+        if ((e = transfers_done()) != cudaSuccess) return cuda_fail(e, "cudaStreamSynchronize");
     }
     *out = p;
     mafat_internal_clear_error();
@@ -661,6 +662,7 @@ mafat_status mafat_attn_sync_status(const mafat_attn_t* p, void* stream) {
     if ((e = cudaMemcpy(&st, p->status, sizeof(st), cudaMemcpyDeviceToHost)) != cudaSuccess) return cuda_fail(e, "cudaMemcpy");
     if (st == MAFAT_DEV_OK) return MAFAT_OK;
     if ((e = cudaMemset(p->status, 0, kStatusBytes)) != cudaSuccess) return cuda_fail(e, "cudaMemset");
+    if ((e = transfers_done()) != cudaSuccess) return cuda_fail(e, "cudaStreamSynchronize");
     return fail(MAFAT_EDEVICE, "a device pipeline wait ran out");
 }
 

@@ -1,5 +1,5 @@
 // A CUDA runtime and kernels that only note what they are asked for, in order, so that the library's host side can be run and
-// looked at without a GPU.  fake_fail: the named call fails once.
+// looked at without a GPU.  fake_fail: the named call fails once; fake_next_out: what the next copy to the host starts with.
 #include <cuda_runtime.h>
 
 #include <cstdarg>
@@ -15,6 +15,7 @@
 namespace {
 
 std::string notes, failing;
+uint32_t next_out;
 
 cudaError_t note(const char* name, const char* format = "", ...) {
     char more[128];
@@ -37,6 +38,7 @@ extern "C" {
 const char* fake_notes() { return notes.c_str(); }
 void fake_reset() { notes.clear(), failing.clear(); }
 void fake_fail(const char* name) { failing = name; }
+void fake_next_out(uint32_t word) { next_out = word; }
 
 cudaError_t cudaDeviceGetAttribute(int* value, cudaDeviceAttr, int) { return *value = 152, cudaSuccess; }
 cudaError_t cudaGetDevice(int* device) { return *device = 0, cudaSuccess; }
@@ -50,6 +52,7 @@ cudaError_t cudaMalloc(void** p, size_t n) { return *p = malloc(n < 4096 ? 4096 
 cudaError_t cudaFree(void* p) { return free(p), note("free"); }
 cudaError_t cudaMemcpy(void* to, const void* from, size_t n, cudaMemcpyKind kind) {
     memcpy(to, from, n);
+    if (kind == cudaMemcpyDeviceToHost && next_out) memcpy(to, &next_out, 4), next_out = 0u;
     return note(kind == cudaMemcpyHostToDevice ? "copy in" : "copy out");
 }
 cudaError_t cudaMemset(void* p, int v, size_t n) { return memset(p, v, n), note("set"); }

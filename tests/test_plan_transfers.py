@@ -47,3 +47,43 @@ def test_rotary_plan_whose_transfer_fails(mf, fake):
         status, h = _rotary(mf, fake)
         assert mf.STATUS[status] == "ECUDA" and not h.value
         assert fake.notes().count("malloc") == fake.notes().count("free") == 1
+
+
+def _attention(mf, fake, kind):
+    h = ctypes.c_void_p()
+    if kind == "cross":
+        d = mf.CrossDesc(struct_size=ctypes.sizeof(mf.CrossDesc), batch=2, n_q=1, n_kv=100, heads_q=8, heads_kv=4, head_dim=64)
+        return fake.lib.mafat_cross_plan(ctypes.byref(d), ctypes.byref(h)), h
+    d = mf.PrefixDesc(struct_size=ctypes.sizeof(mf.PrefixDesc), prefixes=2, requests=3, n_q=4, n_prefix=100, n_own=20, heads_q=8,
+                      heads_kv=4, head_dim=64)
+    return getattr(fake.lib, "mafat_%s_plan" % kind)(ctypes.byref(d), ctypes.byref(h)), h
+
+
+@pytest.mark.parametrize("kind", ["cross", "prefix", "tree"])
+def test_attention_plans(mf, fake, kind):
+    fake.reset()
+    status, h = _attention(mf, fake, kind)
+    assert status == mf.OK
+    _is_whole(fake.notes())
+    fake.lib.mafat_attn_destroy(h)
+
+
+@pytest.mark.parametrize("call", ["set", "sync"])
+def test_attention_plan_whose_transfer_fails(mf, fake, call):
+    fake.reset()
+    fake.fail(call)
+    status, h = _attention(mf, fake, "tree")
+    assert mf.STATUS[status] == "ECUDA" and not h.value
+    assert fake.notes().count("malloc") == fake.notes().count("free") == 1
+
+
+def test_a_status_that_is_read_is_cleared_when_the_call_returns(mf, fake):
+    status, h = _attention(mf, fake, "cross")
+    assert status == mf.OK
+    fake.reset()
+    assert fake.lib.mafat_attn_sync_status(h, None) == mf.OK and "set" not in fake.notes()
+    fake.lib.fake_next_out(5)  # the next copy to the host brings this word
+    fake.reset()
+    assert mf.STATUS[fake.lib.mafat_attn_sync_status(h, None)] == "EDEVICE"
+    _is_whole(fake.notes())
+    fake.lib.mafat_attn_destroy(h)
