@@ -62,9 +62,10 @@ mafat_status area_of_current_device(char** out) {
         e = cudaGetSymbolAddress(&ptr, g_noalloc_scratch);
         if (e != cudaSuccess || !ptr)
             return mafat_internal_fail(MAFAT_ECUDA, "cudaGetSymbolAddress of the static scratch area failed");
-        // the status word starts clear on this device (a synchronous memset: this set-up
-        // runs before any stream capture)
+        // the status word starts clear on this device (this set-up runs before any stream capture, and
+        // ends before a run on any stream)
         e = cudaMemset((uint32_t*)ptr + MAFAT_CTR_STATUS, 0, sizeof(uint32_t));
+        if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
         if (e != cudaSuccess) return mafat_internal_fail(MAFAT_ECUDA, cudaGetErrorString(e));
         g_addr[dev] = ptr;
     }
@@ -132,6 +133,7 @@ extern "C" mafat_status mafat_noalloc_sync_status(void* stream) {
     if (e != cudaSuccess) return mafat_internal_fail(MAFAT_ECUDA, cudaGetErrorString(e));
     if (v == MAFAT_DEV_OK) return MAFAT_OK;
     e = cudaMemset(status, 0, sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e != cudaSuccess) return mafat_internal_fail(MAFAT_ECUDA, cudaGetErrorString(e));
     if (v == MAFAT_DEV_TIMEOUT)
         return mafat_internal_fail(MAFAT_ETIMEOUT, "a tile waited on another tile that never completed");

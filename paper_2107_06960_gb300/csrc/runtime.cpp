@@ -526,6 +526,9 @@ mafat_status mafat_plan_ex(const mafat_net_t* net, int32_t n_groups, const int32
                 cudaSuccess)
             return bail(e, "cudaMemcpy");
     }
+    // Copies from pageable memory and memsets may be on their way still; streams that the legacy stream does not hold up would not
+    // wait for them.
+    if ((e = cudaStreamSynchronize(nullptr)) != cudaSuccess) return bail(e, "cudaStreamSynchronize");
     *out = p;
     g_err.clear();
     return MAFAT_OK;
@@ -650,6 +653,7 @@ mafat_status mafat_sync_status(const mafat_plan_t* plan, void* stream) {
     if (e != cudaSuccess) return cuda_fail(e, "cudaMemcpy");
     if (st == MAFAT_DEV_OK) return MAFAT_OK;
     cudaMemset(p->d_ctr + MAFAT_CTR_STATUS, 0, sizeof(uint32_t));
+    cudaStreamSynchronize(nullptr);  // cleared before a next run
     if (st == MAFAT_DEV_TIMEOUT) return fail(MAFAT_ETIMEOUT, "a tile waited on another tile that never completed");
     return fail(MAFAT_EDEVICE, "a device pipeline wait ran out");
 }

@@ -57,6 +57,8 @@ cudaError_t cudaMemcpy(void* to, const void* from, size_t n, cudaMemcpyKind kind
 }
 cudaError_t cudaMemset(void* p, int v, size_t n) { return memset(p, v, n), note("set"); }
 cudaError_t cudaMemcpyAsync(void*, const void*, size_t, cudaMemcpyKind, cudaStream_t) { return note("copy async"); }
+cudaError_t cudaMemsetAsync(void*, int, size_t, cudaStream_t) { return note("set async"); }
+cudaError_t cudaGetSymbolAddress(void** p, const void* symbol) { return *p = const_cast<void*>(symbol), cudaSuccess; }
 cudaError_t cudaStreamSynchronize(cudaStream_t s) { return note("sync", " %llu", (unsigned long long)(uintptr_t)s); }
 cudaError_t cudaStreamCreateWithFlags(cudaStream_t* s, unsigned) { return *s = nullptr, cudaSuccess; }
 cudaError_t cudaStreamDestroy(cudaStream_t) { return cudaSuccess; }

@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(ROOT, "paper_2107_06960_gb300", "csrc")
-SOURCES = ["attention.cpp", "decode.cpp", "runtime.cpp", "planner.cpp", "order.cpp"]
+SOURCES = ["attention.cpp", "decode.cpp", "runtime.cpp", "planner.cpp", "order.cpp", "noalloc.cu"]
 
 
 class Fake:
@@ -39,7 +39,7 @@ def build(mf, folder):
 
     def compile_(src):
         obj = os.path.join(folder, os.path.basename(src) + ".o")
-        subprocess.run(["g++", "-std=c++17", "-O0", "-fPIC"] + include + ["-c", src, "-o", obj], check=True)
+        subprocess.run(["g++", "-std=c++17", "-O0", "-fPIC"] + include + ["-x", "c++", "-c", src, "-o", obj], check=True)
         return obj
     files = [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(HERE, "fake_device.cpp")]
     with cf.ThreadPoolExecutor(max_workers=len(files)) as ex:
