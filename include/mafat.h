@@ -658,7 +658,7 @@ typedef struct {
 
 /* Runs on `stream` (asynchronous, one launch, no workspace, capturable).  Device memory of the current device; logits and
  * out aligned to their elements, the rest to 4 bytes.  out may be logits itself (same type and row stride); other
- * overlaps are refused.  All but logits and out may be NULL:
+ * overlaps are refused.  All but logits and out may be NULL (lengths and mask_rows of lists with a size of 0 are not looked at):
  *   tokens [batch][room], lengths [batch] (clamped to 0 .. room; NULL: room), prompt_lengths [batch] (clamped; NULL: 0)
  *   repetition, presence, frequency [batch] (NULL: 1, 0, 0; repetition above 0)
  *   drafts [batch][n_q] with tree [batch][n_q][ceil(n_q / 32)] words (NULL with drafts: token t has its own and those before it)

@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -920,6 +921,8 @@ def _logits_call(shape, in_strides, out_strides, dt, out_dt, tokens, tree, bias,
     for name, x, n in (("tokens", tokens, 2), ("tree", tree, 3), ("bias_ids", bias, 2), ("masks", masks, 2)):
         if x is not None and len(x) != n:
             raise MafatError(EINVAL, "%s: %d dimensions expected" % (name, n))
+    if masks and mask_rows_dim is None and masks[0] != math.prod(shape[:-1]):
+        raise MafatError(EINVAL, "masks: without mask_rows one for each row expected")
     _type(BF16)
     code = {v: k for k, v in _TYPES.items()}
     batch, n_q, vocab = shape[0], shape[1] if len(shape) == 3 else 1, shape[-1]

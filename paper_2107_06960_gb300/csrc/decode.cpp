@@ -364,9 +364,10 @@ mafat_status mafat_adjust_logits(const mafat_logits_desc* d, const void* logits,
     if (!logits || !out) return fail(MAFAT_EINVAL, "null logits or out");
     if ((bias_ids != nullptr) != (bias != nullptr)) return fail(MAFAT_EINVAL, "bias_ids and bias are given together");
     if (tree && !drafts) return fail(MAFAT_EINVAL, "a tree without drafts");
-    if (mask_rows && !masks) return fail(MAFAT_EINVAL, "mask_rows without masks");
+    // lists without an element may have no address
+    if (mask_rows && !masks && d->n_masks > 0) return fail(MAFAT_EINVAL, "mask_rows without masks");
     if (masks && !mask_rows && d->n_masks != rows) return fail(MAFAT_EINVAL, "without mask_rows each row has its mask");
-    if ((lengths || prompt_lengths) && !tokens) return fail(MAFAT_EINVAL, "lengths without tokens");
+    if ((lengths || prompt_lengths) && !tokens && d->room > 0) return fail(MAFAT_EINVAL, "lengths without tokens");
     const int64_t esz = d->dtype == MAFAT_BF16 ? 2 : 4, osz = d->out_dtype == MAFAT_BF16 ? 2 : 4;
     const int64_t in_s = d->logits_stride == 0 ? d->vocab : d->logits_stride, out_s = d->out_stride == 0 ? d->vocab : d->out_stride;
     if (in_s < d->vocab || out_s < d->vocab) return fail(MAFAT_EINVAL, "a row stride is smaller than vocab");

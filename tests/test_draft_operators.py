@@ -396,6 +396,15 @@ def test_the_module_checks_its_arguments(mf):
     assert run(0, [(none, 1, 0)], none, 0, 1, None, None) == mf.EINVAL  # a null descriptor, by the library
 
 
+@pytest.mark.parametrize("null,sizes", [
+    (("tokens",), dict(room=0)), (("tokens", "lengths"), dict(room=0)), (("tokens", "prompt_lengths"), dict(room=0)),
+    (("masks",), dict(n_masks=0)), (("tokens", "masks", "bias_ids", "bias"), dict(room=0, n_masks=0, n_bias=0))])
+def test_lists_of_nothing(mf, null, sizes):
+    """A tensor without elements has no address: what goes with it is taken, and the call refused for its output alone."""
+    assert _logits(mf, null=null, at=dict(out=AT[0]), out_stride=1001, **sizes) == mf.EINVAL
+    assert mf.lib.mafat_last_error() == b"an output overlaps another tensor"
+
+
 @pytest.mark.parametrize("which", ["rotary", "tree"])
 def test_closed_plans(mf, monkeypatch, which):
     entry, call, tensors = _calls(mf)[which]

@@ -261,3 +261,22 @@ def test_rows_that_share_a_block(mf, dt, out_dt, B, T, V, room, in_place):
         one = torch.empty((1, T, V), dtype=out.dtype, device="cuda")
         mf.adjust_logits(x[b:b + 1, :, :V].contiguous(), one, masks=masks, **{n: t[b:b + 1] for n, t in a.items()})
         assert torch.equal(out[b, :, :V], one[0]), b
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_nothing_said_yet(mf, dt):
+    """Histories with room for no token, and no masks, as tensors of such sizes: what is said has no part in the results."""
+    none = torch.empty((2, 0), dtype=torch.int32, device="cuda")
+    zero, rows = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.full((2, 3), -1, dtype=torch.int32, device="cuda")
+    x = torch.randn((2, 3, 1000), device="cuda").to(dt)
+    drafts = torch.tensor([[5, 6, 7], [5, 5, 999]], dtype=torch.int32, device="cuda")
+    f = torch.tensor([0.25, 0.5], device="cuda")
+    for said in (dict(lengths=zero), dict(prompt_lengths=zero), dict(lengths=zero + 3, prompt_lengths=zero + 2), {}):
+        for masked in ({}, dict(masks=torch.empty((0, 32), dtype=torch.int32, device="cuda"), mask_rows=rows)):
+            for _ in range(2):
+                a, b = torch.full_like(x, math.nan), torch.empty_like(x)
+                mf.adjust_logits(x, a, tokens=none, frequency=f, drafts=drafts, **said, **masked)
+                mf.adjust_logits(x, b, frequency=f, drafts=drafts)
+                assert torch.equal(a, b) and not torch.equal(a, x)
+    with pytest.raises(mf.MafatError):  # each row its mask, of none
+        mf.adjust_logits(x, a, masks=torch.empty((0, 32), dtype=torch.int32, device="cuda"))
