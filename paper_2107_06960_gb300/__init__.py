@@ -676,6 +676,7 @@ class TreeAttention(PrefixAttention):
                  _addr("tree", tree, (1 if shared else nq[0], n_q, (n_q + 31) // 32), i32_, on),
                  _addr("out", out, nq, dt, on, self._out[1]), _addr("lse", lse, nq[:3], f32_, on))
             status = lib.mafat_tree_run(self.handle, *a[:10], shared, *a[10:], stream)
+            _check(status)
             _keep(self._calls, tensors, None, shared)
         _check(status)
 
@@ -764,6 +765,7 @@ def block_norm(x, residual, residual_out=None, post_weight=None, gate=None, bran
              _addr("weight", weight, weight_shape, dt, on), _addr("residual_out", residual_out, shape, dt, on, so),
              _addr("y", y, shape, out_dt, on, sy), _addr("scales", scales, scales_shape, f32_, on))
         status = lib.mafat_block_norm(desc, *a, stream)
+        _check(status)
         _keep(_norm_calls, tensors, rest, ctypes.addressof(desc), desc)
     _check(status)
 
@@ -836,6 +838,7 @@ class Rotary:
             a = [_addr("positions", positions, shape, i32_, on), _addr("places", places, shape, i32_, on)]
             a += [_addr(name, t, t.shape, dt, on, t.stride()) if t is not None else None for name, t in zip(_ROTARY_NAMES, tensors[2:])]
             status = lib.mafat_rotary_run(self.handle, call, *a, stream)
+            _check(status)
             _keep(self._calls, tensors, None, ctypes.addressof(call), call)
         _check(status)
 
@@ -909,6 +912,7 @@ def adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None, r
         a = [logits.data_ptr()] + [_addr(w[0], t, w[1], w[2], on) for t, w in zip(tensors[1:-1], wanted)]
         a.append(_addr("out", out, logits.shape, out.dtype, on, out.stride()))
         status = lib.mafat_adjust_logits(desc, *a, stream)
+        _check(status)
         _keep(_logits_calls, tensors, None, ctypes.addressof(desc), desc)
     _check(status)
 

@@ -396,6 +396,35 @@ def test_the_module_checks_its_arguments(mf):
     assert run(0, [(none, 1, 0)], none, 0, 1, None, None) == mf.EINVAL  # a null descriptor, by the library
 
 
+@pytest.mark.parametrize("which", ["norm", "rotary", "tree", "logits"])
+def test_refused_calls_are_not_kept(mf, monkeypatch, which):
+    """Those that the library refuses leave the kept ones as they were."""
+    monkeypatch.setattr(mf, "_current_device", lambda: 0)
+    monkeypatch.setattr(mf, "_norm_calls", [])
+    monkeypatch.setattr(mf, "_logits_calls", [])
+    entry, call, tensors = _calls(mf)[which]
+    if which in ("rotary", "tree"):
+        plan = [c.cell_contents for c in call.__closure__][0]
+        plan.device = 0
+    calls = {"norm": lambda: mf._norm_calls, "logits": lambda: mf._logits_calls}.get(which, lambda: plan._calls)
+    here = {n: OnGpu(t) for n, t in tensors.items()}
+    with monkeypatch.context() as m:
+        m.setattr(mf.lib, entry, lambda *a: mf.EINVAL)
+        for _ in range(2):
+            with pytest.raises(mf.MafatError):
+                call(**here)
+            assert calls() == []
+        m.setattr(mf.lib, entry, lambda *a: mf.OK)
+        call(**here)
+        kept = list(calls())
+        m.setattr(mf.lib, entry, lambda *a: mf.EUNSUPPORTED)
+        fewer = {"norm": "gate", "rotary": "places", "tree": "lse", "logits": "masks"}[which]
+        more = {"rotary": dict(k_out=here.get("k"), v_out=here.get("v")), "logits": dict(mask_rows=None)}.get(which, {})
+        with pytest.raises(mf.MafatError) as e:
+            call(**{**here, fewer: None, **more})
+        assert e.value.status == mf.EUNSUPPORTED and len(kept) == 1 and list(calls()) == kept
+
+
 @pytest.mark.parametrize("null,sizes", [
     (("tokens",), dict(room=0)), (("tokens", "lengths"), dict(room=0)), (("tokens", "prompt_lengths"), dict(room=0)),
     (("masks",), dict(n_masks=0)), (("tokens", "masks", "bias_ids", "bias"), dict(room=0, n_masks=0, n_bias=0))])
