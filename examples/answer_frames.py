@@ -143,6 +143,7 @@ class DraftingDecoder(Decoder):
         self.parents = [(j + 1) // 2 - 1 for j in range(nodes)]  # two children a node
         self.ways = tree_words(self.parents)
         self.said = torch.zeros(self.batch, self.room, device="cuda", dtype=torch.int32)
+        self.prompt = torch.zeros(self.batch, device="cuda", dtype=torch.int32)  # how much of it is the prompt
         self.repetition = torch.full((self.batch,), 1.2, device="cuda")
         self.frequency = torch.full((self.batch,), 0.1, device="cuda")
 
@@ -163,7 +164,7 @@ class DraftingDecoder(Decoder):
         return h, y
 
     def read_tree(self, tokens, ways, positions):
-        """tokens, positions [batch][n], a tree behind self.length tokens of each request: adjusted logits, fp32."""
+        """tokens, positions [batch][n], a tree behind self.length tokens of each request: what stands before the head, [batch][n][width]."""
         n = tokens.shape[1]
         places = self.length[:, None] + torch.arange(n, device="cuda", dtype=torch.int32)
         x = self.embedding[tokens.reshape(-1)]
@@ -181,11 +182,14 @@ class DraftingDecoder(Decoder):
             o = torch.empty_like(q)
             self.plan("cross", n).run(q, *self.states[i][1], o)
             x = o.view(-1, q_cols) @ self.out[i][1]
-        h, y = self.between(x, h, 2 * self.layers)
-        logits = (y @ self.head).view(self.batch, n, -1)
+        return self.between(x, h, 2 * self.layers)[1].view(self.batch, n, -1)
+
+    def adjusted(self, y, **drafted):
+        """Logits of y [batch][n][width], with penalties for what was said, fp32.  drafted: what each row has besides."""
+        logits = y @ self.head
         out = torch.empty(logits.shape, device="cuda")
-        mf.adjust_logits(logits, out, tokens=self.said, lengths=self.length, repetition=self.repetition, frequency=self.frequency,
-                         drafts=tokens.to(torch.int32), tree=ways)
+        mf.adjust_logits(logits, out, tokens=self.said, lengths=self.length, prompt_lengths=self.prompt, repetition=self.repetition,
+                         frequency=self.frequency, **drafted)
         return out
 
     def keep(self, tokens, path, count):
@@ -200,10 +204,11 @@ class DraftingDecoder(Decoder):
     def read_prompt(self, tokens):
         n = tokens.shape[1]
         positions = torch.arange(n, device="cuda", dtype=torch.int32).expand(self.batch, n).contiguous()
-        logits = self.read_tree(tokens, tree_words(range(-1, n - 1)), positions)
+        y = self.read_tree(tokens, tree_words(range(-1, n - 1)), positions)
         path = torch.arange(n, device="cuda").expand(self.batch, n)
         self.keep(tokens, path, torch.full((self.batch,), n, device="cuda"))
-        return logits[:, -1].argmax(-1)
+        self.prompt += n
+        return self.adjusted(y[:, -1:])[:, 0].argmax(-1)
 
     def step(self, last):
         """last [batch], the token to go on from: the tokens that follow it [batch][depth], how many of them count, the new last."""
@@ -213,7 +218,8 @@ class DraftingDecoder(Decoder):
             depth.append(depth[self.parents[j]] + 1)
         tokens = torch.stack(tokens, 1)
         positions = self.length[:, None] + torch.tensor(depth, device="cuda", dtype=torch.int32)
-        best = self.read_tree(tokens, self.ways, positions.contiguous()).argmax(-1)
+        y = self.read_tree(tokens, self.ways, positions.contiguous())
+        best = self.adjusted(y, drafts=tokens.to(torch.int32), tree=self.ways).argmax(-1)
         # down from the root, as long as a drafted child is what its parent's logits ask for
         at = torch.zeros(self.batch, device="cuda", dtype=torch.long)
         path, on = [at], torch.ones(self.batch, device="cuda", dtype=torch.bool)
