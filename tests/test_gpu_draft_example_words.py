@@ -1,4 +1,4 @@
-"""What the example's drafting form takes for the prompt and for the answer."""
+"""What the example's drafting form takes for the prompt and for the answer, and that it keeps drafts that are right."""
 import importlib.util
 import os
 
@@ -93,3 +93,42 @@ def test_the_prompt_is_no_answer(example, states, adjusted, nodes):
         for r in range(2):
             answer[r] += [int(tokens[0][r])] + t[r, :int(n[r]) - 1].tolist()
             assert d.said[r, PROMPT:int(d.length[r])].tolist() == answer[r]
+
+
+def test_right_drafts_are_kept(example, states, adjusted):
+    """A drafter that is told what the decoder will ask for has all its drafts kept, in a tree's one step as in steps of a token each: the
+    tokens, their places, histories and caches.  Requests are chosen by the steps of a token alone: no token with two
+    successors, and logits whose first is ahead of the second by more than the two forms' roundings."""
+    requests = 12
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    prompt = torch.randint(0, 1000, (requests, PROMPT), generator=g, device="cuda")
+    one, many = _decoder(example, states, requests, 1), _decoder(example, states, requests, 7)
+    last, first = one.read_prompt(prompt), many.read_prompt(prompt)
+    assert torch.equal(last, first) and torch.equal(one.length, many.length)
+    chain, ahead = [last], []
+    for _ in range(3):
+        t, n, last = one.step(last)
+        assert (n == 1).all()
+        chain.append(t[:, 0])
+        two = adjusted[-1][1][:, 0].topk(2).values
+        ahead.append((two[:, 0] - two[:, 1]) / adjusted[-1][1][:, 0].abs().amax(-1))
+    chain, ahead = torch.stack(chain, 1).tolist(), torch.stack(ahead, 1).amin(-1).tolist()
+    follows, chosen = {}, []
+    for r in range(requests):
+        pairs = dict(zip(chain[r], chain[r][1:]))
+        if len(set(chain[r])) == 4 and ahead[r] > 0.02 and all(follows.get(x, y) == y for x, y in pairs.items()):
+            follows.update(pairs)
+            chosen.append(r)
+    assert chosen, ahead
+    for x, y in follows.items():
+        many.next_tokens[x, 0] = y
+    before = many.length.clone()
+    t, n, last = many.step(first)
+    assert torch.equal(many.length, before + n.to(torch.int32))
+    for r in chosen:
+        assert int(n[r]) == 3 and t[r].tolist() == chain[r][1:] and int(last[r]) == chain[r][3], r
+        assert many.said[r, PROMPT:PROMPT + 3].tolist() == chain[r][:3] and torch.equal(many.said[r, :PROMPT + 3], one.said[r, :PROMPT + 3])
+        for cm, co in zip(many.cache, one.cache):
+            x, y = cm[:, r, PROMPT:PROMPT + 3].float(), co[:, r, PROMPT:PROMPT + 3].float()
+            assert (x - y).abs().max() <= 0.05 * y.abs().max(), r
