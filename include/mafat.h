@@ -642,7 +642,8 @@ void mafat_rotary_destroy(mafat_rotary_t* plan);
  *   x = x - frequency * n - presence * [n > 0]    n: how often the answer has it
  *   x = x + bias;  x = -inf where the grammar's mask does not allow the token
  * rounded once.  Said are the request's first lengths[b] tokens and, for row t, the drafted tokens that its bits of `tree`
- * name; the answer is what comes after the first prompt_lengths[b].  Ids outside 0 .. vocab - 1 count for nothing. */
+ * name; the answer is what comes after the first prompt_lengths[b].  Ids outside 0 .. vocab - 1 count for nothing.  Every row
+ * is read and written, and each said or drafted token of a request written again in each of its rows. */
 typedef struct {
     int32_t struct_size;        /* sizeof(mafat_logits_desc) */
     int32_t dtype;              /* of logits: MAFAT_BF16 or MAFAT_FP32 */

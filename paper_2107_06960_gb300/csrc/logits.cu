@@ -23,6 +23,7 @@
 namespace {
 
 constexpr int kMostRows = 16;  // of a CTA
+constexpr int kFewDrafts = 128;  // of a request, that a thread goes over for each token that it writes
 constexpr int kAhead = 8;  // tokens of a history that a thread asks for at once
 // a token's word: entry of the biases (number + 1) | a draft has it | the prompt has it | how often the answer has it
 constexpr int kBiasShift = 20;
@@ -134,7 +135,9 @@ struct Run {
     }
 };
 
-template <class T, class O, int THREADS, int N, int BLOCKS>
+// MANY: of drafts so many that a row's are counted in the table, which then is that row's; else a drafted token's count is made where it
+// is written, going over all drafts.
+template <class T, class O, int THREADS, int N, int BLOCKS, bool MANY>
 __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_constant__ MafatLogitsArgs a) {
     using S = Run<T, O, THREADS, N>;
     // Where histories are long the list is made of the whole table, not with each token, whose addition then has to come back
@@ -199,8 +202,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
     auto mask_of = [&](int t) -> const uint32_t* { return masks[t] < 0 ? nullptr : a.masks + (int64_t)masks[t] * a.mask_words; };
     typename S::Bits bits;
     s.look(a.pass ? mask_of(0) : nullptr, bits);
+    auto place = [&](int32_t id) { return (uint32_t)id - (uint32_t)s.first; };  // kTokens and more: elsewhere
     if (any) {
-        auto place = [&](int32_t id) { return (uint32_t)id - (uint32_t)s.first; };  // kTokens and more: elsewhere
         auto note = [&](uint32_t at, uint32_t was) {
             if (!kScan && was == 0u) list[atomicAdd(&listed, 1)] = (uint16_t)at;
         };
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
         }
         n = listed;
         if (n == 0) t = rows;
-        fetch();
+        if constexpr (!MANY) fetch();
     }
     if (a.pass) {
 #pragma unroll 1
@@ -320,6 +323,39 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
                 frequency = a.frequency ? a.frequency[b] : 0.f;
     const float* bias = a.bias + (int64_t)b * a.bias_s;
     const uint32_t* tree = a.tree + (int64_t)b * a.tree_s;
+    auto write = [&](int row, int at, float x, uint32_t drafted) {
+        const uint32_t word = table[at], count = (word & kCount) + drafted;
+        float y = x;
+        if (count > 0u || (word & kPrompt)) y = y > 0.f ? y / repetition : y * repetition;
+        y -= frequency * (float)count;
+        if (count > 0u) y -= presence;
+        if (word >> kBiasShift) y += bias[(word >> kBiasShift) - 1u];
+        narrow(out + row * a.out_s + s.first + at, y);
+    };
+    if constexpr (MANY) {
+        // From one row to the next a chain has a draft more; of a tree all are looked at, those that the row before had and this one
+        // has not fall away.
+#pragma unroll 1
+        for (int row = 0; row < rows; ++row) {
+            const int own = t0 + row;
+            const uint32_t* way = a.tree ? tree + (int64_t)own * a.tree_words : nullptr;
+            const int from = a.tree || row == 0 ? 0 : own, end = a.tree ? a.n_q : own + 1;
+            for (int j = from + tid; j < end; j += THREADS) {
+                const uint32_t at = place(drafts[j]);
+                if (at >= (uint32_t)S::kTokens) continue;
+                const bool now = !way || (way[j / 32] >> (j % 32) & 1u), was = way && row > 0 && ((way - a.tree_words)[j / 32] >> (j % 32) & 1u);
+                if (now != was) atomicAdd(table + at, now ? 1u : 0xffffffffu);
+            }
+            __syncthreads();  // the row's counts are there, and before the first row what is written over
+            const uint32_t* mask = mask_of(row);
+            for (int k = tid; k < n; k += THREADS) {
+                const int token = s.first + list[k];
+                if (token >= 0 && token < a.vocab && allows(mask, token)) write(row, list[k], wide(in[row * a.in_s + token]), 0u);
+            }
+            __syncthreads();
+        }
+        return;
+    }
     __syncthreads();  // what is written over is there
 #pragma unroll 1
     for (;;) {
@@ -327,20 +363,14 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
         for (int u = 0; u < kTogether; ++u) {
             const int row = patch.row[u];
             if (row < 0) continue;
-            const int token = s.first + patch.at[u];
-            const uint32_t word = table[patch.at[u]];
-            uint32_t count = word & kCount;
-            if (word & kDraft) {  // those that the row's bits name, or up to its own
+            uint32_t drafted = 0u;
+            if (table[patch.at[u]] & kDraft) {  // those that the row's bits name, or up to its own
+                const int token = s.first + patch.at[u];
                 const uint32_t* way = a.tree ? tree + (int64_t)(t0 + row) * a.tree_words : nullptr;
                 const int end = way ? a.n_q : t0 + row + 1;
-                for (int j = 0; j < end; ++j) count += drafts[j] == token && (!way || (way[j / 32] >> (j % 32) & 1u));
+                for (int j = 0; j < end; ++j) drafted += drafts[j] == token && (!way || (way[j / 32] >> (j % 32) & 1u));
             }
-            float y = patch.x[u];
-            if (count > 0u || (word & kPrompt)) y = y > 0.f ? y / repetition : y * repetition;
-            y -= frequency * (float)count;
-            if (count > 0u) y -= presence;
-            if (word >> kBiasShift) y += bias[(word >> kBiasShift) - 1u];
-            narrow(out + row * a.out_s + token, y);
+            write(row, patch.at[u], patch.x[u], drafted);
         }
         if (t >= rows) break;
         fetch();
@@ -350,7 +380,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_co
 bool noted(const MafatLogitsArgs& a) { return a.tokens || a.drafts || a.bias_ids; }
 
 // A request's rows are shared by as many CTAs as leave `least` in all, so that the table serves several rows.
-template <class T, class O, int THREADS, int N, int BLOCKS>
+template <class T, class O, int THREADS, int N, int BLOCKS, bool MANY = false>
 cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_t s) {
     using S = Run<T, O, THREADS, N>;
     // rows that start alike share a CTA; a row may start V - 1 tokens late
@@ -367,11 +397,11 @@ cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_
     const size_t ahead = rows > 1 ? S::kAsked * THREADS * N * 16 : 0;
     const size_t smem = ahead + (noted(a) ? S::kTokens * 4 + (std::min<int64_t>(S::kTokens, listed) * 2 + 15) / 16 * 16 : 0);
     if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, O, THREADS, N, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        const cudaError_t e = cudaFuncSetAttribute(logits_kernel<T, O, THREADS, N, BLOCKS, MANY>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    S::kAsked * THREADS * N * 16 + S::kTokens * 6);
         if (e != cudaSuccess) return e;
     }
-    return mafat_launch_overlapped(logits_kernel<T, O, THREADS, N, BLOCKS>, (unsigned)(batch * groups * runs), THREADS, smem, s, a);
+    return mafat_launch_overlapped(logits_kernel<T, O, THREADS, N, BLOCKS, MANY>, (unsigned)(batch * groups * runs), THREADS, smem, s, a);
 }
 
 // Each CTA goes over the whole history: the longer that is, the more threads it has, and the more tokens where there are many
@@ -386,6 +416,12 @@ template <class T, class O>
 cudaError_t launch_all(MafatLogitsArgs& a, int64_t batch, cudaStream_t s) {
     constexpr int kSms = 152;
     const int said = a.tokens ? a.room : 0;
+    // Drafts counted in the table, and for each token that is written, in us; all are written in each row, and a token's drafts gone
+    // over take as long as there are drafts.  Chains and trees, rows of 32000 bf16: 16 x 65 drafts 31, 32 and 32, 37; 8 x 128
+    // 31, 32 and 34, 45; 4 x 256 31, 33 and 38, 62; 2048 87, 136 and 707, 2152; fp32: 16 x 96 87, 90 and 70, 76; 8 x 128 53, 55 and 51, 59;
+    // 4 x 256 54, 57 and 54, 73.  4096 of 8192 bf16: 83, 132 in 512 threads, 160, 228 in 256; 4162, 13666.
+    if (a.drafts && a.n_q > kFewDrafts)
+        return said <= 2048 && a.n_q <= 2048 ? launch<T, O, 256, 2, 5, true>(a, batch, 4 * 5 * kSms, s) : launch<T, O, 512, 2, 2, true>(a, batch, 4 * kSms, s);
     if (said <= 2048) return launch<T, O, 256, 2, 5>(a, batch, 4 * 5 * kSms, s);
     const int64_t bytes = batch * a.n_q * a.vocab * (int64_t)sizeof(T);
     if (said > 8192 && bytes <= 4 << 20) return launch<T, O, 1024, 1, 1>(a, batch, kSms * 9 / 10, s);
