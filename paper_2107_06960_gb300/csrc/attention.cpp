@@ -45,7 +45,7 @@ const char* const kAttnPlans[] = {"mafat_cross_plan", "mafat_prefix_plan", "mafa
 struct mafat_attn_s {
     AttnKind kind = kCross;
     bool dry_run = false;
-    int device = 0;
+    int device = 0, sms = 0;
     int32_t dtype = 0, batch = 0, n_q = 0, heads_q = 0, heads_kv = 0, dim = 0;
     float scale = 0.f;
     int64_t q[3] = {0, 0, 0}, o[3] = {0, 0, 0};
@@ -368,6 +368,7 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
         if ((e = cudaGetDevice(&p->device)) != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
         sms = sm_count(p->device);
     }
+    p->sms = sms;
     for (int i = 0; i < p->n_seg; ++i)
         if (p->seg[i].n > 0) p->run[p->n_run++] = i;
     if (p->n_run == 0) p->run[p->n_run++] = 0;
@@ -501,6 +502,13 @@ mafat_status run(const mafat_attn_s* p, AttnKind kind, const void* q, const SegD
         x.items = g.items;
         x.cut = g.cut;
         a.overlap = r > 0 && !both;
+        // Fewer CTAs than SMs, of which two fit an SM: launched while the call before ends, they would gather on the SMs that are free
+        // first.  fp32 in us, one call behind another and two programs' calls from two streams, by themselves and two an SM:
+        // 6 x 7 requests of 24 tokens over 13517 + 40 keys (4 and 2 heads of 64) 490, 957 and 837, 883; 4 x 64 tokens of 16 heads of 64 over
+        // 676 34, 63 and 54, 58.  As many as the SMs gain nothing by it (19 x 64 tokens of 8 heads over 5776: 412, 821 and 410, 734), nor does
+        // a launch that runs beside the one before it (4 x 8 requests of 8 over 5776 + 200, 16 and 4 heads of 128: 331, 626 and 323, 597), nor
+        // bf16 tiles of 128 rows (19 x 128 tokens of 8 heads over 676: 9.5, 18.4 and 10.0, 12.4).
+        a.alone = g.kernel == kSimt64 && !a.overlap && g.items < p->sms;
         a.join = r > 0 && p->joined && !both ? p->parts : 0;
         a.cluster = both ? p->both_cluster : p->cluster;
         // where a CTA has several items; of more sequences it has so many that they level it

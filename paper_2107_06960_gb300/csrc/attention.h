@@ -77,6 +77,7 @@ struct MafatAttnArgs {
     // 1: an earlier launch of the same run, which has waited for what came before, is all that this one
     // follows: it waits for its results, or at its end for those that join both
     int32_t overlap;
+    int32_t alone;              // 1: fp32 tiles of 64 rows have an SM to themselves
     uint32_t* status;           // [2] status and abort words, as the plans' counter block starts
     int64_t timeout_ns;
     MafatAttnSeg seg;
@@ -161,11 +162,6 @@ template <class... P, class... A>
 cudaError_t mafat_launch_overlapped(void (*fn)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A&... args) {
     return mafat_launch_clusters(1, fn, grid, block, smem, s, args...);
 }
-
-// CTAs of which two fit an SM and that are no more than the SMs: with this much shared memory each has an SM to itself.  Launched
-// while the one before ends, they would otherwise gather on the SMs that are free first: 6 x 7 requests of 24 nodes over 13517 states
-// (4 query and 2 key heads of 64 channels, fp32, 144 CTAs), one call behind another, took 870 us, 505 by themselves.
-constexpr int kMafatSms = 152, kMafatAlone = 116 * 1024 + 512;
 
 enum MafatNormQuant { MAFAT_NORM_PLAIN = 0, MAFAT_NORM_ROW = 1, MAFAT_NORM_BLOCK = 2 };
 

@@ -93,6 +93,8 @@ struct Writer {
 
 // ---- many rows --------------------------------------------------------------------------------
 
+// With this much shared memory a CTA has its SM to itself.
+constexpr int kAlone = 116 * 1024 + 512;
 constexpr int kTX = 16;  // threads along the keys / channels
 constexpr int kBM = 64;
 
@@ -547,7 +549,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, DP == 64 ? 2 : 1) attn_simt_fe
 template <int DP, bool TREE>
 cudaError_t launch_form(const MafatAttnArgs& a, cudaStream_t s) {
     return mafat_launch_overlapped(a.seg.mask ? attn_simt_kernel<DP, true, TREE> : attn_simt_kernel<DP, false, TREE>,
-                                   a.seg.items, Tile<DP>::kThreads, a.seg.items <= kMafatSms ? kMafatAlone : Tile<DP>::kSmem, s, a);
+                                   a.seg.items, Tile<DP>::kThreads, a.alone ? kAlone : Tile<DP>::kSmem, s, a);
 }
 template <int DP>
 cudaError_t launch(const MafatAttnArgs& a, cudaStream_t s) {
@@ -569,9 +571,9 @@ cudaError_t prepare(const void* fn, int smem) {
 }
 template <int DP, bool TREE>
 cudaError_t prepare_tiles_form() {
-    static_assert(Tile<DP>::kSmem <= kMafatAlone, "one CTA's");
-    const cudaError_t e = prepare((const void*)attn_simt_kernel<DP, false, TREE>, kMafatAlone);
-    return e != cudaSuccess ? e : prepare((const void*)attn_simt_kernel<DP, true, TREE>, kMafatAlone);
+    static_assert(Tile<DP>::kSmem <= kAlone, "one CTA's");
+    const cudaError_t e = prepare((const void*)attn_simt_kernel<DP, false, TREE>, kAlone);
+    return e != cudaSuccess ? e : prepare((const void*)attn_simt_kernel<DP, true, TREE>, kAlone);
 }
 template <int DP>
 cudaError_t prepare_tiles() {

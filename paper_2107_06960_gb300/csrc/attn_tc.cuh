@@ -937,11 +937,10 @@ template <int DP, int SLOTS, bool TREE>
 cudaError_t launch(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, const MafatAttnPrefix* prefix,
                    cudaStream_t s) {
     using C = Cfg<DP, SLOTS>;
-    const int smem = SLOTS == 1 && a.seg.items <= kMafatSms ? kMafatAlone : C::kSmem;
     if (prefix)
-        return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS, MafatAttnPrefix, TREE>, a.seg.items, C::kThreads, smem, s, a, k, v,
+        return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS, MafatAttnPrefix, TREE>, a.seg.items, C::kThreads, C::kSmem, s, a, k, v,
                                        *prefix);
-    return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS, NoPrefix, TREE>, a.seg.items, C::kThreads, smem, s, a, k, v, NoPrefix());
+    return mafat_launch_overlapped(attn_tc_kernel<DP, SLOTS, NoPrefix, TREE>, a.seg.items, C::kThreads, C::kSmem, s, a, k, v, NoPrefix());
 }
 template <int DP, int SLOTS, class Prefix, bool TREE>
 cudaError_t prepare_form() {
@@ -951,8 +950,7 @@ cudaError_t prepare_form() {
     if (e != cudaSuccess) return e;
     // with fewer registers at launch than the roles' shares add up to, setmaxnreg.inc would wait forever
     if (at.numRegs < C::kRegs) return cudaErrorInvalidConfiguration;
-    return cudaFuncSetAttribute(attn_tc_kernel<DP, SLOTS, Prefix, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                SLOTS == 1 ? kMafatAlone : C::kSmem);
+    return cudaFuncSetAttribute(attn_tc_kernel<DP, SLOTS, Prefix, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
 }
 template <int DP, int SLOTS, bool TREE>
 cudaError_t prepare() {

@@ -88,7 +88,9 @@ cudaError_t mafat_prepare_tc(bool, bool) { return note("prepare tc plan"); }
 
 cudaError_t mafat_launch_attn_join(const MafatAttnArgs&, bool, cudaStream_t) { return note("launch join"); }
 cudaError_t mafat_launch_attn_rows(const MafatAttnArgs&, int, const MafatRowsPrefix*, cudaStream_t) { return note("launch rows"); }
-cudaError_t mafat_launch_attn_simt(const MafatAttnArgs&, int rows, cudaStream_t) { return note("launch simt", " %d", rows); }
+cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t) {
+    return note("launch simt", " %d, CTAs %d, alone %d", rows, a.seg.items, a.alone);
+}
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs&, const CUtensorMap&, const CUtensorMap&, int, const MafatAttnPrefix*, cudaStream_t) {
     return note("launch tc");
 }
