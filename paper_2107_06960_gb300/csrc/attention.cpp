@@ -384,8 +384,14 @@ mafat_status finish_plan(mafat_attn_s* p, const Common& c, mafat_attn_t** out) {
     const int64_t lse_bytes = (p->rows_total * p->parts * 4 + 255) / 256 * 256;
     p->workspace_bytes = kStatusBytes + (p->parts > 1 || p->joined ? lse_bytes + p->rows_total * p->parts * p->dim * 4 : 0);
     if (!p->dry_run) {
-        if ((e = mafat_prepare_attn_simt()) != cudaSuccess || (e = mafat_prepare_attn_rows()) != cudaSuccess ||
-            (e = mafat_prepare_attn_tc()) != cudaSuccess)
+        // what the plan can launch, of its type, kind and channels alone: a plan takes 18 us, with all kernels 39, and a program's first
+        // one, which loads them, 1.5 ms instead of 3.7
+        const bool tree = p->kind == kTree;
+        if (c.dtype == MAFAT_FP32)
+            e = mafat_prepare_attn_simt(tree, p->dim);
+        else if ((e = mafat_prepare_attn_rows(tree, p->dim)) == cudaSuccess)
+            e = mafat_prepare_attn_tc(tree, p->dim);
+        if (e != cudaSuccess)
             return cuda_fail(e, "attention kernels");
         if ((e = cudaMalloc(&p->workspace, (size_t)p->workspace_bytes)) != cudaSuccess) return cuda_fail(e, "cudaMalloc");
         p->status = (uint32_t*)p->workspace;

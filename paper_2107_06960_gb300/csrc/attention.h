@@ -85,7 +85,8 @@ struct MafatAttnArgs {
 
 // fp32 on the CUDA cores, tiles of 4, 8 or 64 rows.
 cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s);
-cudaError_t mafat_prepare_attn_simt();
+// Opts into their shared memory what a plan for trees or others, of heads of `dim` channels, can launch, on the current device.
+cudaError_t mafat_prepare_attn_simt(bool tree, int dim);
 int mafat_attn_simt_keys();
 
 // bf16, tiles of 16 rows by runs of 64 keys, ctas CTAs that take one item after another.
@@ -100,7 +101,7 @@ struct MafatRowsPrefix {
     MafatDiv per;
 };
 cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, const MafatRowsPrefix* prefix, cudaStream_t s);
-cudaError_t mafat_prepare_attn_rows();
+cudaError_t mafat_prepare_attn_rows(bool tree, int dim);
 int mafat_attn_rows_keys();
 int mafat_attn_rows_join();  // most parts of an earlier launch that it joins
 
@@ -115,11 +116,11 @@ struct MafatAttnPrefix {
 };
 cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
                                  const MafatAttnPrefix* prefix, cudaStream_t s);
-cudaError_t mafat_prepare_attn_tc();
+cudaError_t mafat_prepare_attn_tc(bool tree, int dim);
 // of these, the forms for trees
 cudaError_t mafat_launch_attn_tc_tree(const MafatAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int slots,
                                       const MafatAttnPrefix* prefix, cudaStream_t s);
-cudaError_t mafat_prepare_attn_tc_tree();
+cudaError_t mafat_prepare_attn_tc_tree(int dim);
 
 // Joins the parts of each row.
 cudaError_t mafat_launch_attn_join(const MafatAttnArgs& a, bool bf16, cudaStream_t s);

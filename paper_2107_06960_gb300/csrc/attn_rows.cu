@@ -542,9 +542,10 @@ cudaError_t prepare_form() {
     return cudaFuncSetAttribute(attn_rows_kernel<DP, true, TREE, NoPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DP, true>::kSmem);
 }
 template <int DP>
-cudaError_t prepare() {
-    cudaError_t e = prepare_form<DP, false>();
-    if (e != cudaSuccess || (e = prepare_form<DP, true>()) != cudaSuccess) return e;
+cudaError_t prepare(bool tree) {
+    if (!tree) return prepare_form<DP, false>();
+    cudaError_t e = prepare_form<DP, true>();
+    if (e != cudaSuccess) return e;
     e = cudaFuncSetAttribute(attn_rows_kernel<DP, false, true, MafatRowsPrefix>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              Cfg<DP, false>::kSmem);
     if (e != cudaSuccess) return e;
@@ -561,7 +562,4 @@ cudaError_t mafat_launch_attn_rows(const MafatAttnArgs& a, int ctas, const Mafat
     return a.dim <= 64 ? launch<64>(a, ctas, prefix, s) : launch<128>(a, ctas, prefix, s);
 }
 
-cudaError_t mafat_prepare_attn_rows() {
-    const cudaError_t e = prepare<64>();
-    return e != cudaSuccess ? e : prepare<128>();
-}
+cudaError_t mafat_prepare_attn_rows(bool tree, int dim) { return dim <= 64 ? prepare<64>(tree) : prepare<128>(tree); }

@@ -575,32 +575,25 @@ cudaError_t prepare_tiles_form() {
     const cudaError_t e = prepare((const void*)attn_simt_kernel<DP, false, TREE>, kAlone);
     return e != cudaSuccess ? e : prepare((const void*)attn_simt_kernel<DP, true, TREE>, kAlone);
 }
-template <int DP>
-cudaError_t prepare_tiles() {
-    const cudaError_t e = prepare_tiles_form<DP, false>();
-    return e != cudaSuccess ? e : prepare_tiles_form<DP, true>();
-}
 template <int R, int DP, bool TREE>
 cudaError_t prepare_few_form() {
     const cudaError_t e = prepare((const void*)attn_simt_few_kernel<R, DP, false, TREE>, Few<R, DP, false>::kSmem);
     return e != cudaSuccess ? e : prepare((const void*)attn_simt_few_kernel<R, DP, true, TREE>, Few<R, DP, true>::kSmem);
 }
-template <int R, int DP>
-cudaError_t prepare_few() {
-    const cudaError_t e = prepare_few_form<R, DP, false>();
-    return e != cudaSuccess ? e : prepare_few_form<R, DP, true>();
+template <int DP, bool TREE>
+cudaError_t prepare_all() {
+    cudaError_t e;
+    if ((e = prepare_few_form<4, DP, TREE>()) != cudaSuccess || (e = prepare_few_form<8, DP, TREE>()) != cudaSuccess) return e;
+    return prepare_tiles_form<DP, TREE>();
 }
 
 }  // namespace
 
 int mafat_attn_simt_keys() { return kBN; }
 
-cudaError_t mafat_prepare_attn_simt() {
-    cudaError_t e;
-    if ((e = prepare_few<4, 64>()) != cudaSuccess || (e = prepare_few<4, 128>()) != cudaSuccess) return e;
-    if ((e = prepare_few<8, 64>()) != cudaSuccess || (e = prepare_few<8, 128>()) != cudaSuccess) return e;
-    if ((e = prepare_tiles<64>()) != cudaSuccess) return e;
-    return prepare_tiles<128>();
+cudaError_t mafat_prepare_attn_simt(bool tree, int dim) {
+    if (tree) return dim <= 64 ? prepare_all<64, true>() : prepare_all<128, true>();
+    return dim <= 64 ? prepare_all<64, false>() : prepare_all<128, false>();
 }
 
 cudaError_t mafat_launch_attn_simt(const MafatAttnArgs& a, int rows, cudaStream_t s) {

@@ -6,7 +6,4 @@ cudaError_t mafat_launch_attn_tc(const MafatAttnArgs& a, const CUtensorMap& k, c
     return a.tree ? mafat_launch_attn_tc_tree(a, k, v, slots, prefix, s) : launch_tc<false>(a, k, v, slots, prefix, s);
 }
 
-cudaError_t mafat_prepare_attn_tc() {
-    const cudaError_t e = prepare_tc<false>();
-    return e != cudaSuccess ? e : mafat_prepare_attn_tc_tree();
-}
+cudaError_t mafat_prepare_attn_tc(bool tree, int dim) { return tree ? mafat_prepare_attn_tc_tree(dim) : prepare_tc<false>(dim); }

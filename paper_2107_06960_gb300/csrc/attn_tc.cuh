@@ -966,12 +966,10 @@ cudaError_t launch_tc(const MafatAttnArgs& a, const CUtensorMap& k, const CUtens
     return a.dim <= 64 ? launch<64, 1, TREE>(a, k, v, prefix, s) : launch<128, 1, TREE>(a, k, v, prefix, s);
 }
 template <bool TREE>
-cudaError_t prepare_tc() {
+cudaError_t prepare_tc(int dim) {
     cudaError_t e;
-    if ((e = prepare<64, 1, TREE>()) != cudaSuccess) return e;
-    if ((e = prepare<128, 1, TREE>()) != cudaSuccess) return e;
-    if ((e = prepare<64, 2, TREE>()) != cudaSuccess) return e;
-    return prepare<128, 2, TREE>();
+    if (dim <= 64) return (e = prepare<64, 1, TREE>()) != cudaSuccess ? e : prepare<64, 2, TREE>();
+    return (e = prepare<128, 1, TREE>()) != cudaSuccess ? e : prepare<128, 2, TREE>();
 }
 
 }  // namespace

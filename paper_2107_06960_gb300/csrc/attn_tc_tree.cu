@@ -6,4 +6,4 @@ cudaError_t mafat_launch_attn_tc_tree(const MafatAttnArgs& a, const CUtensorMap&
     return launch_tc<true>(a, k, v, slots, prefix, s);
 }
 
-cudaError_t mafat_prepare_attn_tc_tree() { return prepare_tc<true>(); }
+cudaError_t mafat_prepare_attn_tc_tree(int dim) { return prepare_tc<true>(dim); }

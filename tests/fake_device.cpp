@@ -80,9 +80,9 @@ int mafat_logits_run() { return 2048; }
 int mafat_norm_max_cols() { return 16384; }
 int mafat_rotary_most_dim() { return 256; }
 
-cudaError_t mafat_prepare_attn_rows() { return note("prepare rows"); }
-cudaError_t mafat_prepare_attn_simt() { return note("prepare simt"); }
-cudaError_t mafat_prepare_attn_tc() { return note("prepare tc"); }
+cudaError_t mafat_prepare_attn_rows(bool tree, int dim) { return note("prepare rows", " %d %d", tree, dim); }
+cudaError_t mafat_prepare_attn_simt(bool tree, int dim) { return note("prepare simt", " %d %d", tree, dim); }
+cudaError_t mafat_prepare_attn_tc(bool tree, int dim) { return note("prepare tc", " %d %d", tree, dim); }
 cudaError_t mafat_prepare_fp32() { return note("prepare fp32"); }
 cudaError_t mafat_prepare_tc(bool, bool) { return note("prepare tc plan"); }
 
