@@ -627,8 +627,8 @@ typedef struct {
  *               is t, and room is n_q
  *   q, q_out  : [batch][n_q][heads_q][head_dim];  k, v : [batch][n_q][heads_kv][head_dim]
  *   k_out, v_out : [batch][room][heads_kv][head_dim]
- * q_out may be q, and without places k_out k and v_out v (same strides); tensors side by side in one matrix are taken as
- * such; other overlaps with an output are refused. */
+ * q_out may be q, and without places k_out k and v_out v (same strides); tensors that lie between one another in one matrix or one
+ * cache, in any order of its dimensions, are taken as such; other overlaps with an output are refused. */
 mafat_status mafat_rotary_run(const mafat_rotary_t* plan, const mafat_rotary_call* call, const int32_t* positions,
                               const int32_t* places, const void* q, void* q_out, const void* k, void* k_out, const void* v,
                               void* v_out, void* stream);

@@ -49,29 +49,37 @@ uint64_t turn_of(double radians) {
     return x + (uint64_t)(int64_t)std::llround(low * 18446744073709551616.);
 }
 
-// Whether two tensors of [n0][n1][heads][dim] share no element: apart, or side by side in the rows of one matrix.
+// Whether two tensors of [n0][n1][heads][dim] share no element, as far as strides show it: their extents are apart, or there is a step of
+// which all strides that reach it are multiples, and past whole steps the elements of each lie in a run of their own.  (Keys and
+// values of one cache, or of one matrix, in any order of its dimensions.)
 struct Placed {
     const void* p;
     const int64_t* n;
     const int64_t* st;
+    bool steps(int i) const { return n[i] > 1; }
+    // what the strides below the step span, 0 where one that reaches it is no multiple
+    int64_t run(int64_t step, int64_t dim) const {
+        int64_t r = dim;
+        for (int i = 0; i < 3; ++i) {
+            if (!steps(i)) continue;
+            if (st[i] < step)
+                r += (n[i] - 1) * st[i];
+            else if (st[i] % step != 0)
+                return 0;
+        }
+        return r;
+    }
 };
 bool apart(const Placed& a, const Placed& b, int64_t dim, int64_t esz) {
     if (!overlap(a.p, extent(a.n, a.st, dim, esz), b.p, extent(b.n, b.st, dim, esz))) return true;
-    // rows of both at the same steps, and inside a row each a run of its own
-    int64_t step = 0;
-    for (int i = 0; i < 2; ++i) {
-        const int64_t sa = a.n[i] > 1 ? a.st[i] : 0, sb = b.n[i] > 1 ? b.st[i] : 0;
-        if (sa && sb && sa != sb) return false;
-        const int64_t s = sa ? sa : sb;
-        if (s && (!step || s < step)) step = s;
-    }
-    if (!step) return false;
-    for (int i = 0; i < 2; ++i)
-        if ((a.n[i] > 1 && a.st[i] % step) || (b.n[i] > 1 && b.st[i] % step)) return false;
-    const int64_t ra = (a.n[2] - 1) * a.st[2] + dim, rb = (b.n[2] - 1) * b.st[2] + dim;
-    int64_t at = ((const char*)b.p - (const char*)a.p) / esz % step;
-    if (at < 0) at += step;
-    return at >= ra && at + rb <= step;
+    const int64_t off = ((const char*)b.p - (const char*)a.p) / esz;
+    for (const Placed* t : {&a, &b})
+        for (int i = 0; i < 3; ++i) {
+            if (!t->steps(i)) continue;
+            const int64_t step = t->st[i], ra = a.run(step, dim), rb = b.run(step, dim), at = (off % step + step) % step;
+            if (ra && rb && at >= ra && at + rb <= step) return true;
+        }
+    return false;
 }
 
 int32_t lowest_bit(int64_t x, int64_t most) { return (int32_t)std::min<int64_t>(x & -x, most); }
