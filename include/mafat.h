@@ -507,9 +507,9 @@ typedef struct {
     int32_t kernel[2], splits[2], ctas[2];
     int32_t parts;              /* of a row that go through the workspace to be joined; 1: none do */
     int32_t launches_per_run;
-    /* not 0: a run without a prefix mask is one launch instead, of so many CTAs of MAFAT_ATTN_TILES (of trees: or
-     * MAFAT_ATTN_ROWS in clusters) that read both sets for rows of one request each and keep no parts in memory; the other fields,
-     * the workspace among them, are those of a run with one */
+    /* not 0: a run without a prefix mask is one launch instead, of so many CTAs of MAFAT_ATTN_TILES that read both sets for rows of
+     * one request each and keep no parts in memory (of trees also of MAFAT_ATTN_ROWS, either clusters that split an item's keys or
+     * CTAs that take whole items one after another); the other fields, the workspace among them, are those of a run with one */
     int32_t whole_ctas;
     int64_t workspace_bytes;
 } mafat_attn_stats_t;

@@ -178,8 +178,9 @@ constexpr double kClusterJoinUs = 0.7, kOwnJoinUs = 1.0;
 int64_t row_tiles(const AttnShape& sh, int32_t rows) { return (rows + sh.rows - 1) / sh.rows; }
 
 // One CTA an SM that leaves SMs idle: those take the last keys of all items, in as many rounds as that needs, while the others
-// have the rest.  64 trees of 16 nodes about 23104 states (128 items of 181 tiles on 152 SMs), with their own keys: 265 us, 278 with
-// whole items.
+// have the rest.  64 trees of 16 nodes about 23104 states (128 items of 181 tiles on 152 SMs), with their own keys: 263 us, 280 with
+// whole items, in turn on one GPU; 265 to 287 on others, by their power.  For trees alone, as are the clusters over both sets below:
+// nothing here needs one, but requests without keep the launches that they were measured with.
 struct Cut {
     uint32_t share;  // of the first part; 0: whole items
     double us;

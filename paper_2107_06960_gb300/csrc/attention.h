@@ -91,7 +91,7 @@ int mafat_attn_simt_keys();
 
 // bf16, tiles of 16 rows by runs of 64 keys, ctas CTAs that take one item after another.
 // prefix: null, or keys that come before the segment's own and that `per` of its sequences after another share; of trees
-// in clusters alone.
+// alone, in clusters that split an item's keys or in CTAs that take whole items.
 struct MafatRowsPrefix {
     const void* k;
     const void* v;

@@ -140,7 +140,7 @@ struct Sets {
     static constexpr bool kBoth = std::is_same<Prefix, MafatRowsPrefix>::value;
     int seq, len0, own0;  // of the prefix: which, readable keys; where own keys begin
     __device__ __forceinline__ Sets() : seq(0), len0(0), own0(0) {}
-    // the item's keys, a run of whole tiles of both sets' (splits: the cluster's CTAs)
+    // the item's keys, a run of whole tiles of both sets' (splits: the cluster's CTAs, or 1: all of them)
     __device__ __forceinline__ Sets(const MafatAttnArgs& a, mafat_attn::Block& b, const Prefix& prefix) : Sets() {
         if constexpr (kBoth) {
             seq = (int)prefix.per.div((uint32_t)b.seq);

@@ -141,7 +141,7 @@ template <class T, class O, int THREADS, int N, int BLOCKS, bool MANY>
 __global__ void __launch_bounds__(THREADS, BLOCKS) logits_kernel(const __grid_constant__ MafatLogitsArgs a) {
     using S = Run<T, O, THREADS, N>;
     // Where histories are long the list is made of the whole table, not with each token, whose addition then has to come back
-    // first: 7 rows of 50001 with 20000 said 7.7 us instead of 10.3, 95 of 128890 with 21842 53 instead of 59, as the rows passed then (16 rows of 32000 with
+    // first: 7 rows of 50001 with 20000 said 7.7 us instead of 10.3, 95 of 128890 with 21842 and masks 53 instead of 59, as the rows passed then (16 rows of 32000 with
     // 512, in 256 threads: 3.8 instead of 3.6).
     constexpr bool kScan = THREADS > 256;
     constexpr int kAsked = S::kAsked;
@@ -406,12 +406,13 @@ cudaError_t launch(MafatLogitsArgs& a, int64_t batch, int64_t least, cudaStream_
 
 // Each CTA goes over the whole history: the longer that is, the more threads it has, and the more tokens where there are many
 // logits.  256, 512 and 1024 threads (1024 with one access each, with four), in us:
-//   64 x 16 rows of 131072 bf16, 2048 said          94.7, 109, 115, 120      16 rows of 32000 bf16, 512 said   3.3, 4.0, 4.4, 9.8
-//   102 rows of 111872 bf16, 6305 said             28.5, 27.2, 41.4, 33.1    4 x 27 of 8892 fp32, 5139        12.7,  9.2,  9.8,  9.2
-//   7 rows of 50001 fp32, 20000 said               17.5,  8.4,  7.2, 11.1    57 of 25809 bf16, 24721          29.2, 15.8, 14.2, 20.7
-//   95 rows of 128890 fp32, 21842 said             90.8, 66.1, 98.9, 46.4    40 x 36 of 21617 bf16, 8686       145,  126,  180,  154
-//   5 x 24 rows of 40256 bf16, 16270 said          33.1, 21.9, 20.6, 29.5    15 x 24 of 11386 bf16, 13653     37.2, 28.9, 35.8, 44.4
+//   64 x 16 rows of 131072 bf16, 2048 said          94.4, 108, 114, 119      16 rows of 32000 bf16, 512 said   3.3, 4.0, 4.3, 9.8
+//   102 rows of 111872 bf16, 6305 said             28.5, 27.1, 41.3, 32.7    4 x 27 of 8892 fp32, 5139        12.7,  9.3,  9.7,  9.3
+//   7 rows of 50001 fp32, 20000 said               17.6,  8.4,  7.2, 11.2    57 of 25809 bf16, 24721          30.0, 16.8, 15.3, 21.2
+//   95 rows of 128890 fp32, 21842 said             90.6, 65.9, 98.8, 46.5    40 x 36 of 21617 bf16, 8686       145,  127,  182,  154
+//   5 x 24 rows of 40256 bf16, 16270 said          32.8, 22.0, 20.8, 29.3    15 x 24 of 11386 bf16, 13653     37.5, 29.0, 36.1, 44.0
 // (without masks and biases, to fp32 but for the first)
+// 2048 ids are one round of kAhead for 256 threads; the other steps lie between the calls above.
 template <class T, class O>
 cudaError_t launch_all(MafatLogitsArgs& a, int64_t batch, cudaStream_t s) {
     constexpr int kSms = 152;
